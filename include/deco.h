@@ -435,6 +435,62 @@ deco_status deco_layered_info(deco_layered *ctx, uint32_t *n_layers, uint64_t *k
 deco_status deco_topk_compress_static(const float *a, uint64_t d, uint64_t k,
                                       deco_pair *msg_out, void *stream);
 
+/* ------------------------------------------- log probabilities of given tokens, and their gradient */
+
+/*
+ * The worker's end of a training step, before the compressed exchange: the loss whose gradient is
+ * handed to deco_ef_compress.  (The paper trains language models and reports their perplexity; it
+ * takes the loss as given.)
+ *
+ * For every row r of `logits` (z = scale * logits[r], scale = 1 / temperature):
+ *   lse[r]      = log sum_j exp(z_j)
+ *   logprob[r]  = z_t - lse[r] for t = targets[r];  0 where t < 0 (a position without a token);
+ *                 NaN where t >= vocab (nothing is read there)
+ *   entropy[r]  = -sum_j p_j log p_j,  p_j = exp(z_j - lse[r]),  0 log 0 = 0
+ *   top_idx[r], top_logprob[r]   the `top` largest logits in descending order, equal ones by
+ *                 increasing index (+0 and -0 are equal, a NaN counts as the largest), and their
+ *                 log probabilities
+ * Logits of -inf have probability 0.  A row of -inf alone has no distribution: lse = -inf,
+ * logprob = -inf (0 where t < 0), entropy = 0, alternatives 0, 1, ... with -inf.  A row that holds
+ * a NaN or +inf gives NaN for every floating output (logprob stays 0 where t < 0).
+ *   logits   DEVICE, [rows] x [vocab] of `dtype` (deco_dtype), consecutive within a row, rows
+ *            row_stride entries apart (>= vocab); any alignment of whole entries
+ *   targets  DEVICE, [rows] int64; may be NULL if logprob is NULL
+ *   logprob, entropy, lse   DEVICE, [rows] fp32 each; any of them may be NULL
+ *   top      at most DECO_LOGPROBS_MAX_TOP (else DECO_ERR_CAPACITY) and at most vocab;
+ *            top_idx [rows][top] and top_logprob [rows][top] are required when top > 0
+ * 1 <= vocab < 2^31, 0 < scale < inf, rows < 2^28.  rows = 0 does nothing.  Sums are held in
+ * fp32.  The same inputs give the same bits.  Works on the CURRENT device, allocates nothing and
+ * keeps nothing between calls: calls on different streams do not disturb each other.
+ */
+#define DECO_LOGPROBS_MAX_TOP 32u
+deco_status deco_token_logprobs(const void *logits, int32_t dtype, uint64_t rows, uint32_t vocab,
+                                uint64_t row_stride, const int64_t *targets, float scale,
+                                float *logprob, float *entropy, float *lse, uint32_t top,
+                                uint32_t *top_idx, float *top_logprob, void *stream);
+
+/*
+ * Gradient of  sum_r g_logprob[r] logprob[r] + g_entropy[r] entropy[r]
+ *              + sum_i g_top[r][i] top_logprob[r][i]   with respect to the logits:
+ *   grad[r][j] = scale * ( sum of the g's whose token is j  -  p_j * (sum of all the g's)
+ *                          - g_entropy[r] * p_j * (log p_j + entropy[r]) )
+ * with the g of a row whose target is < 0 left out.  The alternatives' choice is not
+ * differentiated.  A row whose lse is -inf has the gradient 0; a target >= vocab gives a row of NaN
+ * (if g_logprob is given).
+ *   lse      DEVICE, [rows], as deco_token_logprobs wrote it;  entropy likewise, needed (and
+ *            read) only with g_entropy
+ *   g_logprob (with targets), g_entropy, g_top (with top_idx)   DEVICE, fp32; each may be NULL
+ *   grad     DEVICE, same dtype as the logits, rows grad_row_stride entries apart; it may be the
+ *            logits' own buffer (same row stride), which then is overwritten
+ * Other conditions as above.  An entry of top_idx that is >= vocab is left out.
+ */
+deco_status deco_token_logprobs_grad(const void *logits, int32_t dtype, uint64_t rows,
+                                     uint32_t vocab, uint64_t row_stride, const int64_t *targets,
+                                     float scale, const float *lse, const float *entropy,
+                                     const float *g_logprob, const float *g_entropy, uint32_t top,
+                                     const uint32_t *top_idx, const float *g_top, void *grad,
+                                     uint64_t grad_row_stride, void *stream);
+
 const char *deco_status_string(deco_status s);
 
 #ifdef __cplusplus

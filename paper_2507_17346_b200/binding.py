@@ -28,6 +28,7 @@ DECO_SELECT_AUTO = 0
 DECO_SELECT_EXACT_PASSES = 1
 DECO_COMPRESSOR_TOPK = 0
 DECO_COMPRESSOR_RANDK = 1
+DECO_LOGPROBS_MAX_TOP = 32
 
 
 class deco_pair(ctypes.Structure):
@@ -120,6 +121,10 @@ SIGNATURES = {
     "deco_layered_set_lr": (_i32, [_vp, _f32]),
     "deco_layered_layer": (_i32, [_vp, _u32, _P(_vp), _P(_u64), _P(_u64)]),
     "deco_layered_info": (_i32, [_vp, _P(_u32), _P(_u64), _P(_vp), _P(_u64)]),
+    "deco_token_logprobs": (_i32, [_vp, _i32, _u64, _u32, _u64, _vp, _f32, _vp, _vp, _vp, _u32,
+                                   _vp, _vp, _vp]),
+    "deco_token_logprobs_grad": (_i32, [_vp, _i32, _u64, _u32, _u64, _vp, _f32, _vp, _vp, _vp, _vp,
+                                        _u32, _vp, _vp, _vp, _u64, _vp]),
     "deco_status_string": (ctypes.c_char_p, [_i32]),
 }
 
@@ -461,6 +466,79 @@ def deco_topk_compress_static(a, d, k, msg_out, stream=None):
     callers that cannot allocate: during stream capture, under a foreign memory pool."""
     _check(load().deco_topk_compress_static(_ptr(a), d, k, _ptr(msg_out), _stream(stream)),
            "deco_topk_compress_static")
+
+
+# ------------------------------------------------- log probabilities of given tokens
+
+def _tensor(x, where, name, dtypes, shape=None):
+    """Address of a contiguous CUDA tensor (None stays None).  The library reads whole buffers
+    behind the addresses it is given: a broadcast or strided view would make it read elsewhere."""
+    if x is None:
+        return None
+    if not x.is_cuda:
+        raise ValueError("%s: %s must be a CUDA tensor" % (where, name))
+    if str(x.dtype)[6:] not in dtypes:
+        raise ValueError("%s: %s must be %s, is %s" % (where, name, " or ".join(dtypes), x.dtype))
+    if shape is not None and tuple(x.shape) != tuple(shape):
+        raise ValueError("%s: %s must have shape %s, has %s" % (where, name, tuple(shape),
+                                                               tuple(x.shape)))
+    if not x.is_contiguous():
+        raise ValueError("%s: %s must be contiguous" % (where, name))
+    return x.data_ptr()
+
+
+def _rows_of(x, where, name, like=None):
+    """(address, dtype code, rows, columns, row stride) of a 2-D CUDA tensor whose rows are
+    consecutive in memory; the rows themselves may be any distance apart."""
+    if not x.is_cuda or x.dim() != 2:
+        raise ValueError("%s: %s must be a two-dimensional CUDA tensor" % (where, name))
+    kind = {"float32": DECO_F32, "bfloat16": DECO_BF16}.get(str(x.dtype)[6:])
+    if kind is None:
+        raise ValueError("%s: %s must be float32 or bfloat16, is %s" % (where, name, x.dtype))
+    if like is not None and (x.dtype != like.dtype or x.shape != like.shape):
+        raise ValueError("%s: %s must have the logits' shape and type" % (where, name))
+    rows, cols = x.shape
+    stride = x.stride(0) if rows > 1 else max(cols, x.stride(0))
+    if cols > 1 and x.stride(1) != 1 or stride < cols:
+        raise ValueError("%s: the rows of %s must be consecutive in memory and must not overlap"
+                         % (where, name))
+    return x.data_ptr(), kind, rows, cols, stride
+
+
+def deco_token_logprobs(logits, targets, logprob, entropy=None, lse=None, scale=1.0, top_idx=None,
+                        top_logprob=None, stream=None):
+    """Log probabilities of `targets` ([rows] int64 CUDA tensor) under `logits` ([rows, vocab], f32
+    or bf16), written to `logprob` ([rows] f32); optionally the entropy, the log of the sum of
+    exponentials and the top alternatives (`top_idx` [rows, top] int32 and `top_logprob` [rows, top]
+    f32).  `targets` and `logprob` may both be None."""
+    w = "deco_token_logprobs"
+    p, kind, rows, vocab, stride = _rows_of(logits, w, "logits")
+    top = 0 if top_idx is None else top_idx.shape[-1]
+    _check(load().deco_token_logprobs(
+        p, kind, rows, vocab, stride, _tensor(targets, w, "targets", ("int64",), (rows,)), scale,
+        _tensor(logprob, w, "logprob", ("float32",), (rows,)),
+        _tensor(entropy, w, "entropy", ("float32",), (rows,)),
+        _tensor(lse, w, "lse", ("float32",), (rows,)), top,
+        _tensor(top_idx, w, "top_idx", ("int32",), (rows, top)),
+        _tensor(top_logprob, w, "top_logprob", ("float32",), (rows, top)), _stream(stream)), w)
+
+
+def deco_token_logprobs_grad(logits, targets, lse, grad, g_logprob=None, entropy=None,
+                             g_entropy=None, top_idx=None, g_top=None, scale=1.0, stream=None):
+    """Gradient with respect to the logits of the sums g_logprob . logprob + g_entropy . entropy +
+    g_top . top_logprob, written to `grad` (the logits' shape and type; may be `logits` itself)."""
+    w = "deco_token_logprobs_grad"
+    p, kind, rows, vocab, stride = _rows_of(logits, w, "logits")
+    gp, _, _, _, gstride = _rows_of(grad, w, "grad", logits)
+    top = 0 if g_top is None else g_top.shape[-1]
+    _check(load().deco_token_logprobs_grad(
+        p, kind, rows, vocab, stride, _tensor(targets, w, "targets", ("int64",), (rows,)), scale,
+        _tensor(lse, w, "lse", ("float32",), (rows,)),
+        _tensor(entropy, w, "entropy", ("float32",), (rows,)),
+        _tensor(g_logprob, w, "g_logprob", ("float32",), (rows,)),
+        _tensor(g_entropy, w, "g_entropy", ("float32",), (rows,)), top,
+        _tensor(top_idx, w, "top_idx", ("int32",), (rows, top)) if top else None,
+        _tensor(g_top, w, "g_top", ("float32",), (rows, top)), gp, gstride, _stream(stream)), w)
 
 
 # ------------------------------------------------------------- device views (plumbing)

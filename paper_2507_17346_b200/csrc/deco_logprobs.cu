@@ -1,0 +1,820 @@
+// deco_token_logprobs / deco_token_logprobs_grad: log probabilities of given tokens under rows of
+// logits, with entropy, log-sum-exp and the largest alternatives, and the gradient of all of them.
+//
+// Forward: one pass over the logits.  With c = scale * log2(e) a thread keeps, for the entries
+// it has seen, the maximum m, s = sum 2^t and q = sum 2^t t with t = x c - m c; a larger maximum
+// multiplies s by f = 2^((m_old - m_new) c) and turns q into f (q + (m_old - m_new) c s).  At the
+// end of the row  lse = ln2 (m c + log2 s),  entropy = ln2 (log2 s - q / s),  and
+// logprob = ln2 (t_target - log2 s), in which the rounding of m c cancels.
+//
+// A row is one CTA's work, or a cluster's of 2, 4 or 8 CTAs, each with a contiguous part of it,
+// where the rows alone would leave most of the device idle; the parts are joined through
+// distributed shared memory, so there is no workspace and no second launch.
+#include <cooperative_groups.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "deco.h"
+
+namespace cg = cooperative_groups;
+
+namespace {
+
+constexpr int NT = 256;                  // threads of a CTA
+constexpr int WARPS = NT / 32;
+constexpr int UNROLL = 4;                // 16-byte loads of a thread in flight
+constexpr int GROUPS = 64;               // groups of threads whose maxima bound the alternatives
+constexpr int MAX_TOP = DECO_LOGPROBS_MAX_TOP;
+constexpr int LIST = 1024;               // candidates kept for the alternatives
+constexpr int TIES = 64;                 // ... of those equal to the bound
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LN2 = 0.6931471805599453f;
+// The streaming path treats entries below FLOOR as FLOOR, with weight 0 (masks of -inf, of the
+// type's lowest value, of -1e10 ...).  That is exact for rows whose maximum m has |m c| < SPAN and
+// scales in [SCALE_LO, SCALE_HI]: then (FLOOR - m) c < -2^20, and the rounding of m c, a common
+// factor of all weights, is below 2^(1/16).  All other rows, and rows with a NaN, take the slow path.
+constexpr float FLOOR = -0x1p30f;
+constexpr float SPAN = 0x1p20f;
+constexpr float SCALE_LO = 0x1p-8f, SCALE_HI = 0x1p8f;
+
+static_assert(GROUPS >= 2 * MAX_TOP, "the bound needs more groups than alternatives");
+static_assert(NT % GROUPS == 0 && NT >= MAX_TOP * 8, "merge of eight parts in one go");
+
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
+
+// Total order of the alternatives: descending value, then ascending index.  +0 and -0 have one
+// key, all NaNs another above every number.
+__device__ __forceinline__ uint32_t order_key(float x)
+{
+    if (x != x) return 0xFFFFFFFFu;
+    const uint32_t b = __float_as_uint(x + 0.0f);
+    return (b & 0x80000000u) ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float key_value(uint32_t k)
+{
+    if (k == 0xFFFFFFFFu) return __uint_as_float(0x7FC00000u);
+    return __uint_as_float((k & 0x80000000u) ? k & 0x7FFFFFFFu : ~k);
+}
+__device__ __forceinline__ uint64_t item_key(float x, uint32_t idx)
+{
+    return (static_cast<uint64_t>(order_key(x)) << 32) | (0xFFFFFFFFu - idx);
+}
+
+template <typename T> struct Elem;
+template <> struct Elem<float> {
+    static constexpr int E = 4;
+    template <bool NC> __device__ static float get(const float *p) { return NC ? __ldg(p) : *p; }
+    // clamp at FLOOR (NaN stays) and return the largest entry (NaN ignored)
+    __device__ static float clamp_max(uint32_t (&w)[4])
+    {
+        float m = FLOOR;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float x = max_nan(__uint_as_float(w[i]), FLOOR);
+            w[i] = __float_as_uint(x);
+            m = fmaxf(m, x);
+        }
+        return m;
+    }
+    __device__ static float at(const uint32_t (&w)[4], int e) { return __uint_as_float(w[e]); }
+    static constexpr uint32_t NEG_INF = 0xFF800000u;
+    __device__ static void put(uint32_t (&w)[4], int e, float x) { w[e] = __float_as_uint(x); }
+};
+template <> struct Elem<__nv_bfloat16> {
+    static constexpr int E = 8;
+    template <bool NC> __device__ static float get(const __nv_bfloat16 *p)
+    {
+        const unsigned short *b = reinterpret_cast<const unsigned short *>(p);
+        const uint32_t u = NC ? __ldg(b) : *b;
+        return __uint_as_float(u << 16);
+    }
+    __device__ static float clamp_max(uint32_t (&w)[4])
+    {
+        const uint32_t fl = __float_as_uint(FLOOR);
+        const uint32_t f2 = fl | (fl >> 16);
+        uint32_t m2 = f2;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(w[i]) : "r"(w[i]), "r"(f2));
+            asm("max.bf16x2 %0, %1, %2;" : "=r"(m2) : "r"(m2), "r"(w[i]));
+        }
+        return fmaxf(__uint_as_float(m2 << 16), __uint_as_float(m2 & 0xFFFF0000u));
+    }
+    __device__ static float at(const uint32_t (&w)[4], int e)
+    {
+        return __uint_as_float((e & 1) ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
+    }
+    static constexpr uint32_t NEG_INF = 0xFF80FF80u;
+    __device__ static void put(uint32_t (&w)[4], int e, float x)
+    {
+        const uint32_t b = __float_as_uint(x) >> 16;
+        w[e >> 1] = (e & 1) ? (w[e >> 1] & 0xFFFFu) | (b << 16) : (w[e >> 1] & 0xFFFF0000u) | b;
+    }
+};
+
+// A row seen in 16-byte granules of memory: granule v holds the entries v E - lead .. v E - lead + E - 1,
+// of which those in [0, vocab) exist.  NC: nothing writes the row while the kernel runs.
+template <typename T, bool NC>
+struct Row {
+    const T *p;
+    uint32_t vocab, lead, granules;
+    __device__ Row(const T *p_, uint32_t vocab_) : p(p_), vocab(vocab_)
+    {
+        constexpr uint32_t E = Elem<T>::E;
+        lead = static_cast<uint32_t>((reinterpret_cast<uintptr_t>(p_) & 15u) / sizeof(T));
+        granules = static_cast<uint32_t>((static_cast<uint64_t>(vocab_) + lead + E - 1) / E);
+    }
+    // entries of granule v; those that do not exist read as -inf
+    __device__ __forceinline__ void load(uint32_t v, uint32_t end, uint32_t (&w)[4]) const
+    {
+        constexpr int E = Elem<T>::E;
+        const int64_t first = static_cast<int64_t>(v) * E - lead;
+        if (v < end && first >= 0 && first + E <= vocab) {
+            if (NC) {
+                asm("ld.global.nc.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];"
+                    : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p + first));
+            } else {
+                const uint4 x = *reinterpret_cast<const uint4 *>(p + first);
+                w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+            }
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = Elem<T>::NEG_INF;
+        if (v >= end) return;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (first + e >= 0 && first + e < vocab) Elem<T>::put(w, e, Elem<T>::template get<NC>(p + first + e));
+    }
+};
+
+struct Part {                            // softmax statistics of some entries
+    float m, s, q;
+};
+__device__ __forceinline__ void raise(Part &a, float m, float c)
+{
+    const float d = (a.m - m) * c, f = ex2(d);
+    a.q = f * __fmaf_rn(d, a.s, a.q);
+    a.s = f * a.s;
+    a.m = m;
+}
+__device__ __forceinline__ void join(Part &a, Part b, float c)
+{
+    const float m = fmaxf(a.m, b.m);
+    raise(a, m, c);
+    raise(b, m, c);
+    a.s += b.s;
+    a.q += b.q;
+}
+
+struct Shared {
+    Part part[WARPS];
+    Part cta;                            // this CTA's part of the row
+    float tmax[NT];
+    float bound;
+    uint32_t n_list, n_ties, n_out;
+    uint64_t list[LIST + TIES];          // item keys
+    float list_x[LIST];
+    uint32_t list_idx[LIST];
+    uint32_t ties[TIES];
+    uint64_t top[MAX_TOP];               // this CTA's alternatives, sorted; 0: none
+    uint64_t merged[MAX_TOP * 8];
+    uint64_t final_top[MAX_TOP];
+    uint32_t warp_u32[WARPS];
+    uint32_t key, count;
+};
+
+// The k-th largest of the GROUPS group maxima (thread t is of group t mod GROUPS): at least k
+// entries are not below it.  Every thread returns the bound.
+__device__ float group_bound(Shared &sh, float tm, uint32_t k)
+{
+    const int t = threadIdx.x;
+    sh.tmax[t] = tm;
+    __syncthreads();
+    float g = 0.f;
+    if (t < GROUPS) {
+        g = sh.tmax[t];
+#pragma unroll
+        for (int o = GROUPS; o < NT; o += GROUPS) g = fmaxf(g, sh.tmax[t + o]);
+    }
+    __syncthreads();
+    if (t < GROUPS) sh.tmax[t] = g;
+    __syncthreads();
+    if (t < GROUPS) {
+        uint32_t rank = 0;
+#pragma unroll 16
+        for (int j = 0; j < GROUPS; ++j) {
+            const float o = sh.tmax[j];
+            rank += (o > g || (o == g && j < t)) ? 1u : 0u;
+        }
+        if (rank == k - 1) sh.bound = g;
+    }
+    __syncthreads();
+    return sh.bound;
+}
+
+__device__ __forceinline__ void offer(Shared &sh, float x, uint32_t idx, float bound)
+{
+    if (x > bound) {
+        const uint32_t at = atomicAdd(&sh.n_list, 1u);
+        if (at < LIST) {
+            sh.list_x[at] = x;
+            sh.list_idx[at] = idx;
+        }
+    } else if (x == bound) {
+        const uint32_t at = atomicAdd(&sh.n_ties, 1u);
+        if (at < TIES) sh.ties[at] = idx;
+    }
+}
+
+// Fill out[have .. want) with the largest entries of [lo, hi) whose order key is below `below`,
+// by descending value and ascending index: per distinct value one pass that finds it and one,
+// ended early, that collects its indices in order.  For what the candidate list cannot hold.
+template <typename T>
+__device__ void top_by_passes(Shared &sh, const T *row, uint32_t lo, uint32_t hi, uint64_t below,
+                              uint32_t have, uint32_t want, uint64_t *out)
+{
+    const int t = threadIdx.x, lane = t & 31, wid = t >> 5;
+    while (have < want) {
+        uint32_t best = 0;
+        bool found = false;
+        for (uint64_t j = static_cast<uint64_t>(lo) + t; j < hi; j += NT) {
+            const uint32_t k = order_key(Elem<T>::template get<true>(row + j));
+            if (k < below && (!found || k > best)) { best = k; found = true; }
+        }
+        // order keys of numbers and NaN are never 0 (that would be a NaN's bit pattern)
+        best = __reduce_max_sync(0xFFFFFFFFu, found ? best : 0u);
+        if (lane == 0) sh.warp_u32[wid] = best;
+        __syncthreads();
+        best = 0;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) best = max(best, sh.warp_u32[w]);
+        __syncthreads();
+        if (best == 0) break;                                    // nothing left
+        for (uint64_t base = lo; base < hi && have < want; base += NT) {
+            const uint64_t j = base + t;
+            const bool hit = j < hi && order_key(Elem<T>::template get<true>(row + j)) == best;
+            const uint32_t b = __ballot_sync(0xFFFFFFFFu, hit);
+            if (lane == 0) sh.warp_u32[wid] = __popc(b);
+            __syncthreads();
+            uint32_t before = 0, total = 0;
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) {
+                const uint32_t n = sh.warp_u32[w];
+                before += w < wid ? n : 0u;
+                total += n;
+            }
+            const uint32_t at = have + before + __popc(b & ((1u << lane) - 1u));
+            if (hit && at < want)
+                out[at] = (static_cast<uint64_t>(best) << 32) | (0xFFFFFFFFu - static_cast<uint32_t>(j));
+            have += total;
+            __syncthreads();
+        }
+        below = best;
+    }
+    for (uint32_t i = have + t; i < want; i += NT) out[i] = 0;
+    __syncthreads();
+}
+
+// out[0 .. k) = the k largest of keys[0 .. n) in descending order (distinct keys; 0 fills up)
+__device__ void rank_into(const uint64_t *keys, uint32_t n, uint32_t k, uint64_t *out)
+{
+    for (uint32_t i = threadIdx.x; i < k; i += NT)
+        if (i >= n) out[i] = 0;
+    for (uint32_t i = threadIdx.x; i < n; i += NT) {
+        const uint64_t a = keys[i];
+        uint32_t rank = 0;
+        for (uint32_t j = 0; j < n; ++j) rank += keys[j] > a ? 1u : 0u;
+        if (rank < k) out[rank] = a;
+    }
+    __syncthreads();
+}
+
+struct Args {
+    const void *logits;
+    uint64_t row_stride;
+    uint32_t vocab, top;
+    const int64_t *targets;
+    float scale;
+    int slow;                            // every row by the slow path (extreme scale)
+    float *logprob, *entropy, *lse;
+    uint32_t *top_idx;
+    float *top_logprob;
+};
+
+template <typename T, bool TOP, bool SPLIT>
+__global__ void __launch_bounds__(NT)
+logprobs_kernel(const Args a)
+{
+    constexpr int E = Elem<T>::E;
+    __shared__ Shared sh;
+    const int t = threadIdx.x, lane = t & 31, wid = t >> 5;
+    uint32_t parts = 1, part = 0;
+    uint64_t r = blockIdx.x;
+    if (SPLIT) {
+        parts = cg::this_cluster().num_blocks();
+        part = cg::this_cluster().block_rank();
+        r = blockIdx.x / parts;
+    }
+    const T *row = static_cast<const T *>(a.logits) + r * a.row_stride;
+    const Row<T, true> R(row, a.vocab);
+    const uint32_t v0 = static_cast<uint32_t>(static_cast<uint64_t>(R.granules) * part / parts);
+    const uint32_t v1 = static_cast<uint32_t>(static_cast<uint64_t>(R.granules) * (part + 1) / parts);
+    const float c = a.scale * LOG2E;
+
+    // ---- one pass over this CTA's granules
+    Part my = {FLOOR, 0.f, 0.f};
+    float bound = FLOOR;
+    if (TOP && t == 0) sh.n_list = sh.n_ties = sh.n_out = 0;
+    if (!a.slow) {
+        bool first = true;
+        for (uint32_t vb = v0; vb < v1; vb += NT * UNROLL) {
+            uint32_t w[UNROLL][4];
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u) R.load(vb + u * NT + t, v1, w[u]);
+            float bm = FLOOR;
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u) bm = fmaxf(bm, Elem<T>::clamp_max(w[u]));
+            if (bm > my.m) raise(my, bm, c);
+            if (TOP && first) {
+                bound = group_bound(sh, bm, a.top);
+                first = false;
+            }
+            const float mc = my.m == FLOOR ? 0.f : my.m * c;     // nothing but FLOOR yet: weights 0
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u) {
+                float s = 0.f, q = 0.f;
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float tt = __fmaf_rn(Elem<T>::at(w[u], e), c, -mc);
+                    const float p = ex2(tt);
+                    s += p;
+                    q = __fmaf_rn(p, tt, q);
+                }
+                my.s += s;
+                my.q += q;
+            }
+            if (TOP && bm >= bound) {
+#pragma unroll
+                for (int u = 0; u < UNROLL; ++u) {
+                    const uint32_t v = vb + u * NT + t;
+                    if (v < v1) {
+#pragma unroll
+                        for (int e = 0; e < E; ++e) {
+                            const float x = Elem<T>::at(w[u], e);
+                            if (x >= bound && x > FLOOR) offer(sh, x, v * E + e - R.lead, bound);
+                        }
+                    }
+                }
+            }
+        }
+    }
+
+    // ---- alternatives of this CTA's part
+    if (TOP && !a.slow) {
+        const uint32_t k = a.top;
+        float last = bound;                                      // what the lists were collected with
+        bound = group_bound(sh, my.m, k);                        // (its barriers complete the lists)
+        if (sh.n_list > LIST) {
+            // more candidates than the first entries promised: once more, with the whole part's bound
+            __syncthreads();
+            if (t == 0) sh.n_list = sh.n_ties = 0;
+            last = bound;
+            __syncthreads();
+            for (uint32_t v = v0 + t; v < v1; v += NT) {
+                uint32_t w[4];
+                R.load(v, v1, w);
+                if (Elem<T>::clamp_max(w) >= bound) {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        const float x = Elem<T>::at(w, e);
+                        if (x >= bound && x > FLOOR) offer(sh, x, v * E + e - R.lead, bound);
+                    }
+                }
+            }
+            __syncthreads();
+        }
+        const uint32_t lo = v0 == 0 ? 0u : v0 * E - R.lead;
+        const uint32_t hi = v1 == R.granules ? a.vocab : v1 * E - R.lead;
+        const uint32_t listed = sh.n_list, tied = sh.n_ties;
+        if (listed > LIST) {
+            top_by_passes<T>(sh, row, lo, hi, 1ull << 32, 0, min(k, hi - lo), sh.top);
+        } else {
+            for (uint32_t i = t; i < listed; i += NT)
+                if (sh.list_x[i] >= bound)
+                    sh.list[atomicAdd(&sh.n_out, 1u)] = item_key(sh.list_x[i], sh.list_idx[i]);
+            // entries equal to the bound lie on the ties' list unless the bound has risen since
+            const bool ties_known = tied <= TIES || bound > last;
+            if (bound == last && tied <= TIES && bound > FLOOR)
+                for (uint32_t i = t; i < tied; i += NT)
+                    sh.list[atomicAdd(&sh.n_out, 1u)] = item_key(bound, sh.ties[i]);
+            __syncthreads();
+            const uint32_t n = sh.n_out;
+            rank_into(sh.list, n, k, sh.top);
+            if (n < min(k, hi - lo))                             // masked entries, or too many ties
+                top_by_passes<T>(sh, row, lo, hi,
+                                 ties_known || bound <= FLOOR
+                                     ? (n ? sh.top[n - 1] >> 32 : 1ull << 32)
+                                     : static_cast<uint64_t>(order_key(bound)) + 1,
+                                 n, min(k, hi - lo), sh.top);
+        }
+        for (uint32_t i = t; i < k; i += NT)
+            if (i >= hi - lo) sh.top[i] = 0;
+    }
+
+    // ---- this CTA's statistics
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        Part b;
+        b.m = __shfl_xor_sync(0xFFFFFFFFu, my.m, o);
+        b.s = __shfl_xor_sync(0xFFFFFFFFu, my.s, o);
+        b.q = __shfl_xor_sync(0xFFFFFFFFu, my.q, o);
+        join(my, b, c);
+    }
+    if (lane == 0) sh.part[wid] = my;
+    __syncthreads();
+    Part all = sh.part[0];
+#pragma unroll
+    for (int w = 1; w < WARPS; ++w) join(all, sh.part[w], c);
+    const uint64_t *top = sh.top;
+    if (SPLIT) {
+        cg::cluster_group cl = cg::this_cluster();
+        if (t == 0) sh.cta = all;
+        cl.sync();
+        if (part == 0) {
+            for (uint32_t o = 1; o < parts; ++o) join(all, cl.map_shared_rank(&sh, o)->cta, c);
+            if (TOP) {
+                const uint32_t n = parts * a.top;
+                for (uint32_t i = t; i < n; i += NT)
+                    sh.merged[i] = cl.map_shared_rank(&sh, i / a.top)->top[i % a.top];
+            }
+        }
+        cl.sync();                                               // the others may leave
+        if (part != 0) return;
+        if (TOP) {
+            // empty places (key 0) are ranked by their position: they are never among the first
+            // `top` <= vocab, but the ranks of the others must not collide with theirs
+            const uint32_t n = parts * a.top;
+            for (uint32_t i = t; i < n; i += NT) {
+                const uint64_t x = sh.merged[i];
+                uint32_t rank = 0;
+                for (uint32_t j = 0; j < n; ++j) rank += (sh.merged[j] > x || (sh.merged[j] == x && j < i)) ? 1u : 0u;
+                if (rank < a.top) sh.final_top[rank] = x;
+            }
+            __syncthreads();
+            top = sh.final_top;
+        }
+    }
+
+    // ---- the row's results
+    const int64_t tgt = a.targets ? a.targets[r] : -1;
+    const bool fast = !a.slow && fabsf(all.m * c) < SPAN && all.s < INFINITY;
+    float lse, entropy, lp, zm, zs, logz;
+    bool empty = false;
+    if (fast) {
+        zs = c;
+        zm = all.m * c;
+        logz = log2f(all.s);
+        lse = LN2 * (zm + logz);
+        entropy = fmaxf(LN2 * (logz - __fdiv_rn(all.q, all.s)), 0.f);
+    } else {
+        // NaN, infinities, rows of masked entries only, extreme scales: two plain passes of the
+        // row by this CTA, maximum first.  (scale and differences apart, so that nothing overflows early.)
+        float m = -INFINITY;
+        bool nan = false;
+        for (uint64_t j = t; j < a.vocab; j += NT) {
+            const float x = Elem<T>::template get<true>(row + j);
+            m = fmaxf(m, x);
+            nan |= x != x;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+        nan = __syncthreads_or(nan);
+        if (lane == 0) sh.part[wid].m = m;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) m = fmaxf(m, sh.part[w].m);
+        __syncthreads();
+        empty = !nan && m == -INFINITY;
+        nan |= m == INFINITY;
+        float s = 0.f, q = 0.f;
+        if (!nan && !empty)
+            for (uint64_t j = t; j < a.vocab; j += NT) {
+                const float d = fmaxf((Elem<T>::template get<true>(row + j) - m) * a.scale, -1e30f);
+                const float p = expf(d);
+                s += p;
+                q = __fmaf_rn(p, d, q);
+            }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+            q += __shfl_xor_sync(0xFFFFFFFFu, q, o);
+        }
+        if (lane == 0) { sh.part[wid].s = s; sh.part[wid].q = q; }
+        __syncthreads();
+        s = q = 0.f;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) { s += sh.part[w].s; q += sh.part[w].q; }
+        const float bad = __uint_as_float(0x7FC00000u);
+        zs = a.scale;
+        zm = m;                                                  // subtracted before the scale
+        logz = logf(s);
+        lse = nan ? bad : empty ? -INFINITY : __fmaf_rn(m, a.scale, logz);
+        entropy = nan ? bad : empty ? 0.f : fmaxf(logz - __fdiv_rn(q, s), 0.f);
+        if (nan) logz = bad;
+        if (TOP) {
+            top_by_passes<T>(sh, row, 0, a.vocab, 1ull << 32, 0, a.top, sh.top);
+            top = sh.top;
+        }
+    }
+    auto log_p = [&](float x) {
+        if (empty) return -INFINITY;
+        if (fast && x < FLOOR) return (x - all.m) * a.scale - LN2 * logz;   // x c might overflow
+        if (fast) return LN2 * (__fmaf_rn(x, zs, -zm) - logz);
+        return (x - zm) * zs - logz;
+    };
+    if (t == 0) {
+        if (tgt < 0) lp = 0.f;
+        else if (tgt >= a.vocab) lp = __uint_as_float(0x7FC00000u);
+        else lp = log_p(Elem<T>::template get<true>(row + tgt));
+        if (a.logprob) a.logprob[r] = lp;
+        if (a.entropy) a.entropy[r] = entropy;
+        if (a.lse) a.lse[r] = lse;
+    }
+    if (TOP)
+        for (uint32_t i = t; i < a.top; i += NT) {
+            const uint32_t idx = 0xFFFFFFFFu - static_cast<uint32_t>(top[i]);
+            a.top_idx[r * a.top + i] = idx;
+            a.top_logprob[r * a.top + i] = log_p(key_value(static_cast<uint32_t>(top[i] >> 32)));
+        }
+}
+
+// ------------------------------------------------------------------------------ gradient
+
+struct GradArgs {
+    const void *logits;
+    void *grad;
+    uint64_t row_stride, grad_stride;
+    uint32_t vocab, top, chunks;
+    const int64_t *targets;
+    float scale;
+    const float *lse, *entropy, *g_logprob, *g_entropy;
+    const uint32_t *top_idx;
+    const float *g_top;
+};
+
+template <typename T> __device__ __forceinline__ void put_entry(T *p, float x);
+template <> __device__ __forceinline__ void put_entry<float>(float *p, float x) { *p = x; }
+template <> __device__ __forceinline__ void put_entry<__nv_bfloat16>(__nv_bfloat16 *p, float x) { *p = __float2bfloat16_rn(x); }
+
+// One CTA per chunk of a row: entries are read and written once, 16 bytes at a time, with
+// d = log p and p = exp d.  The target's term is added by the thread that holds its granule.  The
+// alternatives' entries are few: warp 0 reads their logits first (the gradient may lie in the
+// logits' place) and writes them over at the end, the terms of equal tokens added in a fixed order.
+template <typename T, int U>
+__global__ void __launch_bounds__(NT)
+logprobs_grad_kernel(const GradArgs a)
+{
+    constexpr int E = Elem<T>::E;
+    const int t = threadIdx.x, lane = t & 31;
+    const uint64_t r = blockIdx.x / a.chunks;
+    const uint32_t chunk = blockIdx.x % a.chunks;
+    const T *row = static_cast<const T *>(a.logits) + r * a.row_stride;
+    T *out = static_cast<T *>(a.grad) + r * a.grad_stride;
+    const Row<T, false> R(row, a.vocab);
+    const uint64_t v0 = static_cast<uint64_t>(chunk) * (NT * U);
+    const uint32_t end = R.granules;
+    if (v0 >= end) return;
+
+    const float lse = a.lse[r];
+    const bool empty = lse == -INFINITY;
+    const int64_t tgt64 = a.g_logprob ? a.targets[r] : -1;
+    const float bad = __uint_as_float(0x7FC00000u);
+    const float g_t = tgt64 < 0 ? 0.f : tgt64 >= a.vocab ? bad : a.g_logprob[r];
+    const uint32_t tgt = tgt64 < 0 || tgt64 >= a.vocab ? 0xFFFFFFFFu : static_cast<uint32_t>(tgt64);
+    const float g_h = a.g_entropy ? a.g_entropy[r] : 0.f;
+    const float h = a.g_entropy ? a.entropy[r] : 0.f;
+    float total = g_t;
+    uint32_t idx = 0xFFFFFFFFu;
+    float g_i = 0.f;
+    if (a.top) {
+        if (lane < static_cast<int>(a.top)) {
+            idx = a.top_idx[r * a.top + lane];
+            if (idx < a.vocab) g_i = a.g_top[r * a.top + lane];
+            else idx = 0xFFFFFFFFu;
+        }
+        float s = g_i;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+        total += s;
+    }
+    auto entry = [&](float x, float own_g) {
+        const float d = max_nan(__fmaf_rn(x, a.scale, -lse), -1e6f);
+        const float p = ex2(d * LOG2E);
+        const float u = p * __fmaf_rn(g_h, d + h, total);
+        return empty ? 0.f : a.scale * (own_g - u);
+    };
+    // the alternatives in this chunk
+    float x_i = 0.f;
+    bool mine = false;
+    if (a.top && t < 32) {
+        const uint64_t v = (static_cast<uint64_t>(idx) + R.lead) / E;
+        mine = idx != 0xFFFFFFFFu && v >= v0 && v < v0 + NT * U;
+        if (mine) x_i = Elem<T>::template get<false>(row + idx);
+    }
+    if (a.top) __syncthreads();
+    const uint32_t vt = tgt == 0xFFFFFFFFu ? 0xFFFFFFFFu : static_cast<uint32_t>((static_cast<uint64_t>(tgt) + R.lead) / E);
+    const bool same_phase = ((reinterpret_cast<uintptr_t>(row) ^ reinterpret_cast<uintptr_t>(out)) & 15u) == 0;
+    uint32_t w[U][4];
+#pragma unroll
+    for (int u = 0; u < U; ++u) R.load(static_cast<uint32_t>(v0) + u * NT + t, end, w[u]);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const uint32_t v = static_cast<uint32_t>(v0) + u * NT + t;
+        if (v >= end) continue;
+        const int64_t first = static_cast<int64_t>(v) * E - R.lead;
+        float y[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) y[e] = entry(Elem<T>::at(w[u], e), 0.f);
+        if (v == vt) {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (first + e == tgt) y[e] = entry(Elem<T>::at(w[u], e), g_t);
+        }
+        if (same_phase && first >= 0 && first + E <= a.vocab) {
+            uint32_t o[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (E == 4) {
+                    o[i] = __float_as_uint(y[i]);
+                } else {
+                    const __nv_bfloat162 b = __floats2bfloat162_rn(y[(2 * i) % E], y[(2 * i + 1) % E]);
+                    o[i] = *reinterpret_cast<const uint32_t *>(&b);
+                }
+            }
+            asm volatile("st.global.v4.b32 [%0], {%1,%2,%3,%4};"
+                         :: "l"(out + first), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (first + e >= 0 && first + e < a.vocab) put_entry<T>(out + first + e, y[e]);
+        }
+    }
+    if (a.top) {
+        __syncthreads();
+        if (t < 32) {
+            float own = (idx != 0xFFFFFFFFu && idx == tgt) ? g_t : 0.f;
+            for (uint32_t j = 0; j < a.top; ++j) {
+                const uint32_t oj = __shfl_sync(0xFFFFFFFFu, idx, j);
+                const float gj = __shfl_sync(0xFFFFFFFFu, g_i, j);
+                if (oj == idx) own += gj;
+            }
+            if (mine) put_entry<T>(out + idx, entry(x_i, own));
+        }
+    }
+}
+
+int sm_count()
+{
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+        return 0;
+    return n;
+}
+
+template <typename T, bool TOP>
+cudaError_t launch_forward(const Args &a, uint64_t rows, uint32_t parts, cudaStream_t s)
+{
+    if (parts == 1) {
+        logprobs_kernel<T, TOP, false><<<static_cast<unsigned>(rows), NT, 0, s>>>(a);
+        return cudaGetLastError();
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(rows * parts));
+    cfg.blockDim = dim3(NT);
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = parts;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, logprobs_kernel<T, TOP, true>, a);
+}
+
+bool bad_shape(const void *logits, int32_t dtype, uint64_t rows, uint32_t vocab, uint64_t stride, float scale)
+{
+    const uintptr_t unit = dtype == DECO_F32 ? 4 : 2;
+    return !logits || (dtype != DECO_F32 && dtype != DECO_BF16) || vocab == 0 || vocab > 0x7FFFFFFFu ||
+           rows >= (1ull << 28) || stride < vocab || stride > (1ull << 40) || !(scale > 0.f) || scale > 3.0e38f ||
+           (reinterpret_cast<uintptr_t>(logits) & (unit - 1)) != 0;
+}
+
+}  // namespace
+
+extern "C" deco_status deco_token_logprobs(const void *logits, int32_t dtype, uint64_t rows, uint32_t vocab,
+                                           uint64_t row_stride, const int64_t *targets, float scale,
+                                           float *logprob, float *entropy, float *lse, uint32_t top,
+                                           uint32_t *top_idx, float *top_logprob, void *stream)
+{
+    if (top > DECO_LOGPROBS_MAX_TOP) return DECO_ERR_CAPACITY;
+    if (top > vocab || (logprob && !targets)) return DECO_ERR_INVALID_ARG;
+    if (rows == 0) return DECO_OK;
+    if (bad_shape(logits, dtype, rows, vocab, row_stride, scale)) return DECO_ERR_INVALID_ARG;
+    if (top && (!top_idx || !top_logprob)) return DECO_ERR_INVALID_ARG;
+    if (!logprob && !entropy && !lse && !top) return DECO_ERR_INVALID_ARG;
+    const int sms = sm_count();
+    if (sms == 0) return DECO_ERR_CUDA;
+    Args a = {};
+    a.logits = logits;
+    a.row_stride = row_stride;
+    a.vocab = vocab;
+    a.top = top;
+    a.targets = logprob ? targets : nullptr;
+    a.scale = scale;
+    a.slow = !(scale >= SCALE_LO && scale <= SCALE_HI);
+    a.logprob = logprob;
+    a.entropy = entropy;
+    a.lse = lse;
+    a.top_idx = top_idx;
+    a.top_logprob = top_logprob;
+    // A row is split while the CTAs do not fill the device and every part still has half a batch
+    // of loads for each of its threads.
+    const uint64_t batch = static_cast<uint64_t>(NT) * UNROLL * (dtype == DECO_F32 ? 4 : 8);
+    uint32_t parts = 1;
+    while (parts < 8 && rows * parts * 2 <= 4ull * sms && vocab >= parts * batch) parts *= 2;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    cudaError_t err;
+    if (dtype == DECO_F32)
+        err = top ? launch_forward<float, true>(a, rows, parts, s) : launch_forward<float, false>(a, rows, parts, s);
+    else
+        err = top ? launch_forward<__nv_bfloat16, true>(a, rows, parts, s)
+                  : launch_forward<__nv_bfloat16, false>(a, rows, parts, s);
+    return err == cudaSuccess ? DECO_OK : DECO_ERR_CUDA;
+}
+
+extern "C" deco_status deco_token_logprobs_grad(const void *logits, int32_t dtype, uint64_t rows, uint32_t vocab,
+                                                uint64_t row_stride, const int64_t *targets, float scale,
+                                                const float *lse, const float *entropy, const float *g_logprob,
+                                                const float *g_entropy, uint32_t top, const uint32_t *top_idx,
+                                                const float *g_top, void *grad, uint64_t grad_row_stride,
+                                                void *stream)
+{
+    if (top > DECO_LOGPROBS_MAX_TOP) return DECO_ERR_CAPACITY;
+    if (rows == 0) return DECO_OK;
+    if (bad_shape(logits, dtype, rows, vocab, row_stride, scale) ||
+        bad_shape(grad, dtype, rows, vocab, grad_row_stride, scale))
+        return DECO_ERR_INVALID_ARG;
+    if (!lse || (g_logprob && !targets) || (g_entropy && !entropy) || (top && (!top_idx || !g_top)))
+        return DECO_ERR_INVALID_ARG;
+    if (grad == logits && grad_row_stride != row_stride) return DECO_ERR_INVALID_ARG;
+    const int sms = sm_count();
+    if (sms == 0) return DECO_ERR_CUDA;
+    GradArgs a = {};
+    a.logits = logits;
+    a.grad = grad;
+    a.row_stride = row_stride;
+    a.grad_stride = grad_row_stride;
+    a.vocab = vocab;
+    a.top = top;
+    a.targets = targets;
+    a.scale = scale;
+    a.lse = lse;
+    a.entropy = entropy;
+    a.g_logprob = g_logprob;
+    a.g_entropy = g_entropy;
+    a.top_idx = top_idx;
+    a.g_top = g_top;
+    // Short calls take one granule per thread, so that they spread over more SMs.
+    const uint64_t per = dtype == DECO_F32 ? 4 : 8;
+    const uint64_t granules = (static_cast<uint64_t>(vocab) + 2 * per - 2) / per;
+    const bool small = rows * granules <= 4ull * sms * NT * UNROLL;
+    const uint64_t span = static_cast<uint64_t>(NT) * (small ? 1 : UNROLL);
+    const uint64_t chunks = (granules + span - 1) / span;
+    if (rows * chunks > 0x7FFFFFFFull) return DECO_ERR_INVALID_ARG;
+    a.chunks = static_cast<uint32_t>(chunks);
+    const unsigned grid = static_cast<unsigned>(rows * chunks);
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (dtype == DECO_F32) {
+        if (small) logprobs_grad_kernel<float, 1><<<grid, NT, 0, s>>>(a);
+        else logprobs_grad_kernel<float, UNROLL><<<grid, NT, 0, s>>>(a);
+    } else {
+        if (small) logprobs_grad_kernel<__nv_bfloat16, 1><<<grid, NT, 0, s>>>(a);
+        else logprobs_grad_kernel<__nv_bfloat16, UNROLL><<<grid, NT, 0, s>>>(a);
+    }
+    return cudaGetLastError() == cudaSuccess ? DECO_OK : DECO_ERR_CUDA;
+}
