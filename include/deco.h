@@ -491,6 +491,107 @@ deco_status deco_token_logprobs_grad(const void *logits, int32_t dtype, uint64_t
                                      const uint32_t *top_idx, const float *g_top, void *grad,
                                      uint64_t grad_row_stride, void *stream);
 
+/* ------------------------------------------------------------- orthogonalised updates */
+
+/*
+ * Update directions whose matrices are orthogonalised (all singular values pushed towards 1) by
+ * Newton-Schulz products, as the Muon optimiser does, for the matrices of a flat vector of length
+ * d laid out like the gradients and the parameters.  Per matrix Y [rows][cols]:
+ *   X = Y / (|Y|_F + eps)
+ *   steps times:  A = X X^T,  X <- a X + (b A + c A^2) X        (X^T X and X (..) where rows > cols:
+ *                                                                the same polynomial of X)
+ *   out = s X,   s by deco_orth_scale
+ * With momentum: M <- mu M + in (fp32, rounded once), and Y = M, or Y = in + mu M (nesterov).
+ *
+ * Precision: products take fp16 operands (11 bits, scaled by a power of two) and are summed in
+ * fp32 on the tensor cores; X itself is carried as a pair of fp16 numbers (22 bits) until the
+ * last step, so that directions the input lacks are not filled with rounding noise.  The result
+ * is within about 2e-3 of the exact polynomial in the 2-norm, which the rounding to bf16 matches.
+ * |Y|_F is summed in double, so it neither overflows nor underflows.  A matrix that holds a NaN or an infinity gives NaN;
+ * a zero matrix gives zeros.
+ */
+typedef struct {
+    uint64_t offset;        /* first entry in the flat vector */
+    uint32_t rows, cols;    /* >= 1, < 2^20 */
+    uint64_t row_stride;    /* entries between rows; 0 -> cols */
+} deco_matrix;
+
+typedef enum {
+    DECO_ORTH_SCALE_NONE = 0,       /* s = 1 */
+    DECO_ORTH_SCALE_SPECTRAL = 1,   /* s = sqrt(max(1, rows / cols)) */
+    DECO_ORTH_SCALE_RMS = 2         /* s = 0.2 sqrt(max(rows, cols)): entries of the size an
+                                       adaptive update has */
+} deco_orth_scale;
+
+/* Options of deco_orth_init.  A zero-filled struct selects every default. */
+typedef struct {
+    const float *coef;        /* HOST, [steps][3]: a, b, c of each step; NULL -> 3.4445, -4.7750, 2.0315.
+                                 The polynomials must keep singular values of [0, 1] at or below 1.75
+                                 and |b t + c t^2| at or below 3.75 there (t the square of the
+                                 singular value), else DECO_ERR_INVALID_ARG */
+    uint32_t steps;           /* 0 -> 5; at most 16 */
+    float    eps;             /* 0 -> 1e-7 */
+    float    momentum;        /* mu, 0 <= mu < 1 */
+    int32_t  nesterov;
+    int32_t  scale;           /* deco_orth_scale */
+    int32_t  device;          /* CUDA device ordinal */
+    uint64_t workspace_bytes; /* the library works through the matrices in groups whose working
+                                 copies fit in this much device memory (a larger single matrix gets what it
+                                 needs); 0 -> 2 GiB */
+    uint32_t reserved[4];     /* must be zero */
+} deco_orth_options;
+
+typedef struct {
+    uint64_t device_bytes;    /* device memory held by the handle */
+    uint64_t launches;        /* kernels enqueued so far */
+    uint32_t groups;          /* groups the matrices are worked through in */
+    uint32_t device_status;   /* 0, or a deco_status latched by a kernel */
+} deco_orth_stats;
+
+typedef struct deco_orth deco_orth;          /* opaque, owned by the library */
+
+/*
+ * Plans the work and allocates all device memory the handle will ever use.  The matrices lie
+ * inside [0, d) and do not overlap (DECO_ERR_INVALID_ARG); entries of no matrix are allowed.  *out is set only on success.
+ * One handle is used on one stream at a time.
+ */
+deco_status deco_orth_init(deco_orth **out, uint64_t d, const deco_matrix *matrices /* HOST */,
+                           uint32_t n_matrices, const deco_orth_options *opt /* HOST, may be NULL */);
+
+/* Free the handle (waits for the device first).  NULL is allowed. */
+void deco_orth_destroy(deco_orth *h);
+
+/*
+ * One pass.
+ *   in        DEVICE, [d] of in_dtype (deco_dtype), read-only
+ *   momentum  DEVICE, [d] fp32, updated in place; NULL -> no momentum, whatever mu is
+ *   out       DEVICE, [d] bf16; entries of no matrix are left alone.  May not overlap `in` or `momentum`
+ * Any alignment of whole entries.  With momentum, entries of no matrix take M <- mu M + in too.
+ */
+deco_status deco_orth_run(deco_orth *h, const void *in, int32_t in_dtype, float *momentum,
+                          void *out, void *stream);
+
+/*
+ * Server update of iteration t with orthogonalised directions, in place of deco_apply_update (it
+ * must follow deco_aggregate_stale, and t advances).  For every cached aggregate S_s that is due
+ * (s <= t - tau), oldest first:
+ *   M <- mu M + S_s / n                                   (all d entries)
+ *   matrices:      x <- x (1 - gamma wd) - gamma s X(M)
+ *   other entries: x <- x (1 - gamma wd) - gamma M
+ * gamma is the context's stepsize, so the context must have been created with lr_at_server = 1
+ * (messages in units of the gradient), and the handle for the context's d and device, with rows
+ * back to back and without nesterov (which would need the aggregate as a vector); else
+ * DECO_ERR_INVALID_ARG.  X is not rounded to bf16 here.
+ *   momentum  DEVICE, [d] fp32, 16-byte aligned: zero before the first iteration; part of what a
+ *             checkpoint has to keep
+ */
+deco_status deco_apply_update_orth(deco_ctx *ctx, deco_orth *h, float *momentum,
+                                   float weight_decay, void *stream);
+
+/* Waits for `stream`, then fills *out (HOST); returns DECO_ERR_DEVICE_CHECK if a kernel latched an
+ * anomaly (a bounded wait that ran out: DECO_ERR_TIMEOUT in device_status) since the handle was created. */
+deco_status deco_orth_get_stats(deco_orth *h, void *stream, deco_orth_stats *out);
+
 const char *deco_status_string(deco_status s);
 
 #ifdef __cplusplus

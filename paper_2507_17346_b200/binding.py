@@ -29,6 +29,9 @@ DECO_SELECT_EXACT_PASSES = 1
 DECO_COMPRESSOR_TOPK = 0
 DECO_COMPRESSOR_RANDK = 1
 DECO_LOGPROBS_MAX_TOP = 32
+DECO_ORTH_SCALE_NONE = 0
+DECO_ORTH_SCALE_SPECTRAL = 1
+DECO_ORTH_SCALE_RMS = 2
 
 
 class deco_pair(ctypes.Structure):
@@ -65,6 +68,28 @@ class deco_stats(ctypes.Structure):
                 ("exact_pass_workers", ctypes.c_uint64),
                 ("cached_aggregates", ctypes.c_uint64),
                 ("device_bytes", ctypes.c_uint64)]
+
+
+class deco_matrix(ctypes.Structure):
+    _fields_ = [("offset", ctypes.c_uint64), ("rows", ctypes.c_uint32),
+                ("cols", ctypes.c_uint32), ("row_stride", ctypes.c_uint64)]
+
+
+class deco_orth_options(ctypes.Structure):
+    _fields_ = [("coef", ctypes.POINTER(ctypes.c_float)),
+                ("steps", ctypes.c_uint32),
+                ("eps", ctypes.c_float),
+                ("momentum", ctypes.c_float),
+                ("nesterov", ctypes.c_int32),
+                ("scale", ctypes.c_int32),
+                ("device", ctypes.c_int32),
+                ("workspace_bytes", ctypes.c_uint64),
+                ("reserved", ctypes.c_uint32 * 4)]
+
+
+class deco_orth_stats(ctypes.Structure):
+    _fields_ = [("device_bytes", ctypes.c_uint64), ("launches", ctypes.c_uint64),
+                ("groups", ctypes.c_uint32), ("device_status", ctypes.c_uint32)]
 
 
 class DecoError(RuntimeError):
@@ -125,6 +150,11 @@ SIGNATURES = {
                                    _vp, _vp, _vp]),
     "deco_token_logprobs_grad": (_i32, [_vp, _i32, _u64, _u32, _u64, _vp, _f32, _vp, _vp, _vp, _vp,
                                         _u32, _vp, _vp, _vp, _u64, _vp]),
+    "deco_orth_init": (_i32, [_P(_vp), _u64, _P(deco_matrix), _u32, _P(deco_orth_options)]),
+    "deco_orth_destroy": (None, [_vp]),
+    "deco_orth_run": (_i32, [_vp, _vp, _i32, _vp, _vp, _vp]),
+    "deco_apply_update_orth": (_i32, [_vp, _vp, _vp, _f32, _vp]),
+    "deco_orth_get_stats": (_i32, [_vp, _vp, _P(deco_orth_stats)]),
     "deco_status_string": (ctypes.c_char_p, [_i32]),
 }
 
@@ -539,6 +569,67 @@ def deco_token_logprobs_grad(logits, targets, lse, grad, g_logprob=None, entropy
         _tensor(g_entropy, w, "g_entropy", ("float32",), (rows,)), top,
         _tensor(top_idx, w, "top_idx", ("int32",), (rows, top)) if top else None,
         _tensor(g_top, w, "g_top", ("float32",), (rows, top)), gp, gstride, _stream(stream)), w)
+
+
+# ------------------------------------------------------------- orthogonalised updates
+
+_orth_length = {}                 # handle -> length of its flat vectors
+
+
+def deco_orth_init(d, matrices, steps=0, coef=None, eps=0.0, momentum=0.0, nesterov=False,
+                   scale=DECO_ORTH_SCALE_NONE, device=0, workspace_bytes=0):
+    """-> opaque handle (int) for the matrices [(offset, rows, cols[, row_stride]), ...] of flat
+    vectors of length d.  `coef`: one (a, b, c) for every step, or a list of `steps` of them."""
+    ms = (deco_matrix * max(1, len(matrices)))()
+    for m, row in zip(ms, matrices):
+        m.offset, m.rows, m.cols = int(row[0]), int(row[1]), int(row[2])
+        m.row_stride = int(row[3]) if len(row) > 3 else 0
+    opt = deco_orth_options()
+    if coef is not None:
+        n = steps or 5
+        flat = [float(v) for c in (coef if hasattr(coef[0], "__len__") else [coef] * n) for v in c]
+        if len(flat) != 3 * n:
+            raise ValueError("deco_orth_init: coef must hold three numbers for each of %d steps" % n)
+        keep = (_f32 * len(flat))(*flat)
+        opt.coef = ctypes.cast(keep, _P(_f32))
+    opt.steps, opt.eps, opt.momentum, opt.nesterov = steps, eps, momentum, int(bool(nesterov))
+    opt.scale, opt.device, opt.workspace_bytes = scale, device, workspace_bytes
+    h = _vp()
+    _check(load().deco_orth_init(ctypes.byref(h), d, ms, len(matrices), ctypes.byref(opt)),
+           "deco_orth_init")
+    _orth_length[h.value] = d
+    return h.value
+
+
+def deco_orth_destroy(h):
+    _orth_length.pop(h, None)
+    load().deco_orth_destroy(h)
+
+
+def deco_orth_run(h, x, out, momentum=None, stream=None):
+    """Orthogonalise the handle's matrices of the flat vector `x` (f32 or bf16) into `out` (bf16);
+    with `momentum` (f32, updated in place) of the momentum buffer."""
+    w = "deco_orth_run"
+    shape = (_orth_length[h],)
+    xp = _tensor(x, w, "x", ("float32", "bfloat16"), shape)
+    _check(load().deco_orth_run(
+        h, xp, DECO_F32 if "float32" in str(x.dtype) else DECO_BF16,
+        _tensor(momentum, w, "momentum", ("float32",), shape),
+        _tensor(out, w, "out", ("bfloat16",), shape), _stream(stream)), w)
+
+
+def deco_apply_update_orth(ctx, h, momentum, weight_decay=0.0, stream=None):
+    """deco_apply_update with orthogonalised directions; `momentum`: f32 CUDA tensor of length d."""
+    w = "deco_apply_update_orth"
+    _check(load().deco_apply_update_orth(ctx, h, _tensor(momentum, w, "momentum", ("float32",),
+                                                         (_orth_length[h],)),
+                                         weight_decay, _stream(stream)), w)
+
+
+def deco_orth_get_stats(h, stream=None):
+    st = deco_orth_stats()
+    _check(load().deco_orth_get_stats(h, _stream(stream), ctypes.byref(st)), "deco_orth_get_stats")
+    return {f: getattr(st, f) for f, _ in deco_orth_stats._fields_}
 
 
 # ------------------------------------------------------------- device views (plumbing)

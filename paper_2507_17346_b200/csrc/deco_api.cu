@@ -388,12 +388,11 @@ extern "C" deco_status deco_aggregate_stale(deco_ctx *c, void *stream)
 
 namespace {
 
-// Launch the update for every cached aggregate that is due at iteration t (step <= t - tau),
-// oldest first, on stream s.
-deco_status apply_due(deco_ctx *c, cudaStream_t s)
+// Hand every cached aggregate that is due at iteration t (step <= t - tau), oldest first, to
+// `apply` and mark it applied.
+template <typename F>
+deco_status for_each_due(deco_ctx *c, F apply)
 {
-    const float beta = c->lr_at_server ? c->lr : 1.0f;
-    const float neg_scale = -(beta / static_cast<float>(c->n_total));
     if (c->t < c->tau) return DECO_OK;
     const uint64_t due = c->t - c->tau;
     // step ids still cached lie in (t - ring, t]
@@ -401,13 +400,23 @@ deco_status apply_due(deco_ctx *c, cudaStream_t s)
     for (uint64_t step = lo; step <= due; ++step) {
         Slot &sl = c->slot_info[step % c->ring];
         if (!sl.valid || sl.step != step) continue;
-        const deco_pair *slot = c->slots + (step % c->ring) * c->slot_pairs;
-        const cudaError_t err = sl.dense ? launch_apply_dense(c, reinterpret_cast<const float *>(slot), neg_scale, s)
-                                         : launch_apply(c, slot, sl.positions, neg_scale, s);
-        if (err != cudaSuccess) return DECO_ERR_CUDA;
+        const deco_status st = apply(sl, c->slots + (step % c->ring) * c->slot_pairs);
+        if (st != DECO_OK) return st;
         sl.valid = false;
     }
     return DECO_OK;
+}
+
+// Launch the update for every cached aggregate that is due, on stream s.
+deco_status apply_due(deco_ctx *c, cudaStream_t s)
+{
+    const float beta = c->lr_at_server ? c->lr : 1.0f;
+    const float neg_scale = -(beta / static_cast<float>(c->n_total));
+    return for_each_due(c, [&](const Slot &sl, const deco_pair *slot) {
+        const cudaError_t err = sl.dense ? launch_apply_dense(c, reinterpret_cast<const float *>(slot), neg_scale, s)
+                                         : launch_apply(c, slot, sl.positions, neg_scale, s);
+        return err == cudaSuccess ? DECO_OK : DECO_ERR_CUDA;
+    });
 }
 
 void finish_iteration(deco_ctx *c)
@@ -460,6 +469,26 @@ extern "C" deco_status deco_apply_update(deco_ctx *c, void *stream)
     if (wait_for_aggregate(c, as_stream(stream)) != cudaSuccess) return DECO_ERR_CUDA;
     mark(c, 5, as_stream(stream));
     const deco_status st = apply_due(c, as_stream(stream));
+    if (st != DECO_OK) return st;
+    mark(c, 6, as_stream(stream));
+    finish_iteration(c);
+    return DECO_OK;
+}
+
+extern "C" deco_status deco_apply_update_orth(deco_ctx *c, deco_orth *h, float *momentum, float weight_decay,
+                                              void *stream)
+{
+    if (!c || !h || !momentum || (reinterpret_cast<uintptr_t>(momentum) & 15u) || !(weight_decay >= 0.f) ||
+        weight_decay > 1e30f || !c->lr_at_server || !deco::orth_fits(h, c))
+        return DECO_ERR_INVALID_ARG;
+    if (c->phase != 2) return DECO_ERR_STATE;
+    DeviceGuard guard(c->device);
+    if (!guard.ok) return DECO_ERR_CUDA;
+    if (wait_for_aggregate(c, as_stream(stream)) != cudaSuccess) return DECO_ERR_CUDA;
+    mark(c, 5, as_stream(stream));
+    const deco_status st = for_each_due(c, [&](const Slot &sl, const deco_pair *slot) {
+        return deco::orth_update(h, c, sl, slot, momentum, weight_decay, as_stream(stream));
+    });
     if (st != DECO_OK) return st;
     mark(c, 6, as_stream(stream));
     finish_iteration(c);

@@ -313,6 +313,13 @@ cudaError_t launch_small_server(const SmallLayer *table, uint32_t layers, uint32
 // numbers, oldest first) and marked applied, t advances.  Returns the slot written.
 uint32_t advance_iteration_external(deco_ctx *c, std::vector<uint32_t> *due);
 
+// --- orthogonalised server update (deco_orth.cu) ------------------------------------------
+// one due aggregate (slot, its entries at `data`) into the momentum, the parameters updated
+deco_status orth_update(deco_orth *h, const deco_ctx *c, const Slot &slot, const deco_pair *data, float *momentum,
+                        float weight_decay, cudaStream_t s);
+// the handle describes the context's vector on its device and takes plain matrices and momentum
+bool orth_fits(const deco_orth *h, const deco_ctx *c);
+
 // --- kernel launchers (deco_server.cu) ---------------------------------------------------
 cudaError_t launch_aggregate(deco_ctx *c, deco_pair *slot, cudaStream_t s);
 // the same with the aggregate kept as a plain vector of ntiles * TILE entries (dense messages)

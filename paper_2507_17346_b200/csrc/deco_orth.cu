@@ -1,0 +1,1094 @@
+// deco_orth_*: orthogonalised update directions by Newton-Schulz products.
+//
+// For a matrix Y [rows][cols] with short side m and long side n:  X = Y / (|Y|_F + eps), then per step
+//     A = X X^T   (X^T X where rows > cols),   B = b A + c A^2,   X <- a X + B X   (a X + X B).
+// All matrices of a group go through a step together, in three launches: one list of output tiles
+// spans matrices of every shape.  A and B are symmetric: only blocks on and below the diagonal are
+// computed and the others are their mirror images.  X is kept in the orientation of Y, so nothing
+// is ever transposed in memory: the tensor cores take an operand with either of its dimensions
+// consecutive, and one 64 x 64 box loads both kinds.
+//
+// Numbers.  Operands are fp16, scaled by 2^14: |X| <= 1.75 and |B| <= 3.75 in the spectral norm (checked
+// for the coefficients in deco_orth_init), so every entry stays below 65504, and entries down to
+// 3.7e-9 keep all 11 bits.  Sums are fp32.  X is carried as hi + lo, two fp16 numbers; the products read
+// hi, the term a X reads both.  Rounding X to 11 bits there would put noise of 2^-12 |X| into
+// directions in which Y has nothing, and five steps amplify those 485 times (a rank-1 matrix
+// came out 15 % wrong); noise that enters through A, B or the product stays in the row and
+// column space of X and is not amplified.  The last step needs no lo: it amplifies 3.4 times.
+//
+// The rounding of A and B themselves reaches the result through b A and c A^2, which nearly cancel.
+// Over many singular values these errors average out (1.2e-3 of the norm at a short side of 512, against
+// 1.7e-3 of the rounding to bf16), over few they do not (up to 8e-3 at short sides below 16).  So
+// matrices up to FULL_SIDE are multiplied in full, hi and lo of both operands (22 bits), and
+// those up to WIDE_B_SIDE with B as hi + lo (1.8e-3 -> 1.3e-3 at 128).  Both are as fast as the plain products
+// there, since short sides leave the tensor cores waiting for memory.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <vector>
+
+#include "deco_internal.h"
+
+namespace {
+
+constexpr float SCALE = 16384.f;         // of X, A and B in fp16
+constexpr float INV_SCALE = 1.f / 16384.f;
+constexpr double MAX_SIGMA = 1.75, MAX_B = 3.75;
+constexpr uint32_t MAX_STEPS = 16;
+
+// ------------------------------------------------------------------ tables in device memory
+
+struct Mat {
+    uint64_t offset, stride;             // in the flat vectors
+    uint32_t rows, cols;
+    uint32_t ldx, lda;                   // entries between rows of X and of A, B
+    __half *hi[2], *lo[2];               // X and the next X
+    __half *a, *b, *a_lo, *b_lo;         // (a_lo, b_lo where the precision asks for them)
+    uint32_t m, n;                       // short and long side
+    uint32_t tall;                       // rows > cols
+    uint32_t precision;                  // see Precision
+    uint32_t piece0, pieces;             // partial sums of squares
+    float scale;                         // s of deco_orth_scale
+};
+
+// Consecutive entries of the flat vector that one CTA takes in: of one matrix, or of none.
+struct Piece {
+    uint64_t offset;
+    uint32_t count;
+    uint32_t slot;                       // of the partial sum; NO_SLOT: none wanted
+};
+// Rows of a matrix whose rows are not back to back.
+struct RowPiece {
+    uint32_t mat, row0, rows, slot;
+};
+// Rows [row0, row0 + rows) of a matrix that one CTA converts.
+struct ConvertPiece {
+    uint32_t mat, row0, rows, col0;
+};
+struct Tile {
+    uint32_t mat;
+    uint16_t tm, tn;
+};
+
+// Which operands of a matrix's products are carried as hi + lo.
+enum Precision { PLAIN = 0, WIDE_B = 1, FULL = 2 };
+constexpr uint32_t FULL_SIDE = 128, WIDE_B_SIDE = 256;
+// A matrix's tensor maps.
+enum Map { MAP_X = 0 /* hi, lo, next hi, next lo */, MAP_A = 4 /* hi, lo */, MAP_B = 6 /* hi, lo */, MAPS = 8 };
+
+constexpr uint32_t NO_SLOT = 0xFFFFFFFFu;
+constexpr uint32_t PIECE = 16384;
+constexpr int INGEST_THREADS = 256;
+
+// ------------------------------------------------------------------------- taking in
+
+template <typename T> __device__ __forceinline__ float to_f(T x);
+template <> __device__ __forceinline__ float to_f<float>(float x) { return x; }
+template <> __device__ __forceinline__ float to_f<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
+
+__device__ double block_sum(double v)
+{
+    __shared__ double s[INGEST_THREADS / 32];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = 0;
+#pragma unroll
+    for (int w = 0; w < INGEST_THREADS / 32; ++w) v += s[w];
+    __syncthreads();
+    return v;
+}
+
+// What a pass takes in: an input vector, a momentum buffer, or both.
+template <typename T>
+struct Source {
+    const T *in;                         // null: the momentum buffer holds the direction already
+    float *mom;                          // null: no momentum
+    float weight;                        // of the input
+    float mu;
+    int nesterov;
+    __device__ __forceinline__ float input(uint64_t i) const { return in ? weight * to_f<T>(in[i]) : 0.f; }
+    // the direction at entry i, the momentum having been updated
+    __device__ __forceinline__ float direction(uint64_t i) const
+    {
+        if (!mom) return input(i);
+        const float m = mom[i];
+        return nesterov ? __fmaf_rn(mu, m, input(i)) : m;
+    }
+};
+
+// M <- mu M + in over a piece, and the sum of squares of the direction in double.
+template <typename T>
+__global__ void __launch_bounds__(INGEST_THREADS)
+ingest_kernel(const Piece *pieces, const Source<T> src, double *partial)
+{
+    const Piece p = pieces[blockIdx.x];
+    double sum = 0;
+    for (uint32_t j = threadIdx.x; j < p.count; j += INGEST_THREADS) {
+        const uint64_t i = p.offset + j;
+        float y;
+        if (src.mom && src.in) {
+            const float x = src.input(i), m = __fmaf_rn(src.mu, src.mom[i], x);
+            src.mom[i] = m;
+            y = src.nesterov ? __fmaf_rn(src.mu, m, x) : m;
+        } else {
+            y = src.direction(i);
+        }
+        sum = __fma_rn(static_cast<double>(y), static_cast<double>(y), sum);
+    }
+    if (p.slot == NO_SLOT) return;
+    sum = block_sum(sum);
+    if (threadIdx.x == 0) partial[p.slot] = sum;
+}
+
+// The same sum for rows that are not back to back (their momentum has been updated already).
+template <typename T>
+__global__ void __launch_bounds__(INGEST_THREADS)
+ingest_rows_kernel(const RowPiece *pieces, const Mat *mats, const Source<T> src, double *partial)
+{
+    const RowPiece p = pieces[blockIdx.x];
+    const Mat &M = mats[p.mat];
+    double sum = 0;
+    for (uint32_t r = 0; r < p.rows; ++r)
+        for (uint32_t j = threadIdx.x; j < M.cols; j += INGEST_THREADS) {
+            const double y = src.direction(M.offset + (p.row0 + r) * M.stride + j);
+            sum = __fma_rn(y, y, sum);
+        }
+    sum = block_sum(sum);
+    if (threadIdx.x == 0) partial[p.slot] = sum;
+}
+
+constexpr uint32_t CONVERT_COLS = 2048;
+
+// X = Y / (|Y|_F + eps) as hi + lo.  Every CTA adds up its matrix's partial sums itself, in the
+// same order.  The quotient is formed in double: |Y|_F may lie outside the range of fp32.
+template <typename T>
+__global__ void __launch_bounds__(INGEST_THREADS)
+convert_kernel(const ConvertPiece *pieces, const Mat *mats, const Source<T> src, const double *partial, float eps)
+{
+    const ConvertPiece p = pieces[blockIdx.x];
+    const Mat &M = mats[p.mat];
+    double sum = 0;
+    for (uint32_t i = threadIdx.x; i < M.pieces; i += INGEST_THREADS) sum += partial[M.piece0 + i];
+    const double inv = static_cast<double>(SCALE) / (sqrt(block_sum(sum)) + static_cast<double>(eps));
+    const uint32_t w = min(M.cols - p.col0, CONVERT_COLS);
+    for (uint32_t e = threadIdx.x; e < p.rows * w; e += INGEST_THREADS) {
+        const uint32_t r = p.row0 + e / w, c = p.col0 + e % w;
+        const float x = static_cast<float>(static_cast<double>(src.direction(M.offset + r * M.stride + c)) * inv);
+        const __half h = __float2half_rn(x);
+        const uint64_t at = static_cast<uint64_t>(r) * M.ldx + c;
+        M.hi[0][at] = h;
+        M.lo[0][at] = __float2half_rn(x - __half2float(h));
+    }
+}
+
+// --------------------------------------------------------------- products on the tensor cores
+
+enum Phase { GRAM = 0, POLY = 1, APPLY = 2 };
+enum Target { NEXT_X = 0, OUT_BF16 = 1, PARAMS = 2 };
+
+constexpr int BK = 64;                   // k per stage: 128 bytes, one swizzle row
+constexpr int STAGES = 6;
+constexpr uint32_t OPERAND_BYTES = 128 * BK * 2;
+constexpr uint32_t STAGE_BYTES = 2 * OPERAND_BYTES;
+constexpr int GEMM_THREADS = 256;        // warps 0: loads, 1: mma, 2: tensor memory, 4..7: epilogue
+constexpr int EPI_WARPS = 4;
+
+struct GemmArgs {
+    const Mat *mats;
+    const CUtensorMap *maps;             // [mat][MAPS]
+    const Tile *tiles;
+    uint32_t n_tiles;
+    int src;                             // which X holds the current iterate
+    int read_lo, write_lo;
+    float a, b, c;
+    // last step
+    __nv_bfloat16 *out;
+    float *params;
+    float lr, decay;                     // params <- params * decay - lr * s * X
+    uint32_t *status;
+};
+
+struct __align__(8) Control {
+    uint64_t full[STAGES], empty[STAGES], acc_full[2], acc_empty[2];
+    uint32_t tmem;
+    volatile uint32_t abort;
+};
+
+__device__ __forceinline__ uint32_t smem_addr(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+
+__device__ __forceinline__ void bar_init(uint64_t *b, uint32_t count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(smem_addr(b)), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint64_t *b, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(smem_addr(b)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint64_t *b)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(smem_addr(b)) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint64_t *b, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\t"
+                 "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                 "selp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(smem_addr(b)), "r"(parity) : "memory");
+    return ok != 0;
+}
+// Bounded wait: false once the limit has passed or another role has given up; the first to give
+// up leaves DECO_ERR_TIMEOUT in the status word.
+__device__ __noinline__ bool bar_wait_slow(uint64_t *b, uint32_t parity, Control *ctl, uint32_t *status)
+{
+    constexpr long long LIMIT = 4000000000ll;                    // clock cycles: about 2 s
+    const long long t0 = clock64();
+    while (!bar_try(b, parity)) {
+        if (ctl->abort) return false;
+        if (clock64() - t0 > LIMIT) {
+            ctl->abort = 1;
+            atomicExch(status, static_cast<uint32_t>(DECO_ERR_TIMEOUT));
+            return false;
+        }
+    }
+    return true;
+}
+__device__ __forceinline__ bool bar_wait(uint64_t *b, uint32_t parity, Control *ctl, uint32_t *status)
+{
+    return bar_try(b, parity) || bar_wait_slow(b, parity, ctl, status);
+}
+
+__device__ __forceinline__ void map_acquire(const CUtensorMap *map)
+{
+    asm volatile("fence.proxy.tensormap::generic.acquire.gpu [%0], 128;" :: "l"(map) : "memory");
+}
+__device__ __forceinline__ void load_box(void *dst, const CUtensorMap *map, int32_t x, int32_t y, uint64_t *bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 :: "r"(smem_addr(dst)), "l"(map), "r"(x), "r"(y), "r"(smem_addr(bar)) : "memory");
+}
+
+// 128 entries of the operand's outer dimension (from mn) by BK of k, as two boxes of 64 x 64.
+__device__ __forceinline__ void load_operand(uint8_t *dst, const CUtensorMap *map, bool mn_major, int32_t mn, int32_t k,
+                                             uint64_t *bar)
+{
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int32_t o = mn + 64 * i;
+        load_box(dst + i * (OPERAND_BYTES / 2), map, mn_major ? o : k, mn_major ? k : o, bar);
+    }
+}
+
+// Shared-memory descriptor of an operand with 128-byte swizzle.  k consecutive: groups of 8 rows are
+// 1024 bytes apart.  Outer dimension consecutive: 64 of it form a row, 8 k's are 1024 bytes
+// apart, the next 64 of the outer dimension 8192.
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr, bool mn_major)
+{
+    uint64_t d = (addr >> 4) & 0x3FFFu;
+    d |= static_cast<uint64_t>(mn_major ? 8192 >> 4 : 1) << 16;
+    d |= static_cast<uint64_t>(1024 >> 4) << 32;
+    d |= 1ull << 46;
+    d |= 2ull << 61;
+    return d;
+}
+
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint64_t *bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];"
+                 :: "r"(smem_addr(bar)) : "memory");
+}
+__device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&v)[32])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+                 "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+                 "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+                   "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]),
+                   "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]),
+                   "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]),
+                   "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+                 : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+
+constexpr int TILE_MN = 128;
+
+// What a tile of a phase reads: the sum over `passes` pairs of operands, pair i being
+// (a + lo of a if i is in a_lo, b + lo of b if i is in b_lo), over k in [0, k) each.
+struct Operands {
+    const CUtensorMap *a, *b;
+    bool a_mn, b_mn;                     // outer dimension consecutive in memory
+    uint32_t k, passes, a_lo, b_lo;
+    __device__ __forceinline__ const CUtensorMap *map_a(uint32_t i) const { return a + ((a_lo >> i) & 1); }
+    __device__ __forceinline__ const CUtensorMap *map_b(uint32_t i) const { return b + ((b_lo >> i) & 1); }
+};
+template <Phase P>
+__device__ __forceinline__ Operands operands(const GemmArgs &g, const Mat &M, uint32_t mat)
+{
+    const CUtensorMap *at = g.maps + static_cast<uint64_t>(mat) * MAPS;
+    const CUtensorMap *x = at + MAP_X + 2 * g.src, *am = at + MAP_A, *bm = at + MAP_B;
+    const uint32_t full = M.precision == FULL;
+    // hi hi, hi lo, lo hi
+    if (P == GRAM) return {x, x, M.tall != 0, M.tall != 0, M.n, full ? 3u : 1u, 4, 2};
+    if (P == POLY) return {am, am, false, false, M.m, full ? 3u : 1u, 4, 2};
+    // (B, X): hi hi, lo hi, hi lo
+    const uint32_t passes = 1 + M.precision;
+    if (M.tall) return {x, bm, false, false, M.m, passes, 4, 2};
+    return {bm, x, false, true, M.m, passes, 2, 4};
+}
+
+// One 128 x 128 tile at a time per CTA; the epilogue of a tile runs beside the products of the next.
+template <Phase P, Target T>
+__global__ void __launch_bounds__(GEMM_THREADS, 1)
+gemm_kernel(const GemmArgs g)
+{
+    extern __shared__ uint8_t raw[];
+    uint8_t *stages = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    __shared__ Control ctl;
+    const int wid = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) {
+            bar_init(&ctl.full[s], 1);
+            bar_init(&ctl.empty[s], 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            bar_init(&ctl.acc_full[s], 1);
+            bar_init(&ctl.acc_empty[s], EPI_WARPS);
+        }
+        ctl.abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (wid == 2) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                     :: "r"(smem_addr(&ctl.tmem)), "r"(2 * TILE_MN) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = ctl.tmem;
+
+    if (wid == 0) {
+        if (lane == 0) {
+            uint32_t it = 0, seen = 0xFFFFFFFFu;
+            bool ok = true;
+            for (uint32_t t = blockIdx.x; ok && t < g.n_tiles; t += gridDim.x) {
+                const Tile tl = g.tiles[t];
+                const Operands op = operands<P>(g, g.mats[tl.mat], tl.mat);
+                for (uint32_t pass = 0; ok && pass < op.passes; ++pass) {
+                    const CUtensorMap *ma = op.map_a(pass), *mb = op.map_b(pass);
+                    if (tl.mat != seen) {                        // an earlier handle's maps may have lain here
+                        map_acquire(ma);
+                        map_acquire(mb);
+                    }
+                    for (uint32_t k = 0; k < op.k; k += BK, ++it) {
+                        const uint32_t s = it % STAGES;
+                        if (!bar_wait(&ctl.empty[s], ((it / STAGES) & 1) ^ 1, &ctl, g.status)) { ok = false; break; }
+                        bar_expect(&ctl.full[s], STAGE_BYTES);
+                        uint8_t *st = stages + s * STAGE_BYTES;
+                        load_operand(st, ma, op.a_mn, tl.tm * TILE_MN, k, &ctl.full[s]);
+                        load_operand(st + OPERAND_BYTES, mb, op.b_mn, tl.tn * TILE_MN, k, &ctl.full[s]);
+                    }
+                }
+                seen = tl.mat;
+            }
+            // copies in flight land before the CTA leaves
+            for (uint32_t i = it > STAGES ? it - STAGES : 0; i < it; ++i) {
+                const long long t0 = clock64();
+                while (!bar_try(&ctl.full[i % STAGES], (i / STAGES) & 1) && clock64() - t0 < 1000000000ll) {}
+            }
+        }
+    } else if (wid == 1) {
+        if (lane == 0) {
+            uint32_t it = 0, n = 0;
+            bool ok = true;
+            for (uint32_t t = blockIdx.x; ok && t < g.n_tiles; t += gridDim.x, ++n) {
+                const Tile tl = g.tiles[t];
+                const Operands op = operands<P>(g, g.mats[tl.mat], tl.mat);
+                const uint32_t as = n & 1;
+                if (!bar_wait(&ctl.acc_empty[as], ((n >> 1) & 1) ^ 1, &ctl, g.status)) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                // fp16 operands, fp32 sums, N and M, which dimension is consecutive
+                const uint32_t idesc = (1u << 4) | (static_cast<uint32_t>(op.a_mn) << 15) |
+                                       (static_cast<uint32_t>(op.b_mn) << 16) | ((TILE_MN >> 3) << 17) |
+                                       ((TILE_MN >> 4) << 24);
+                const uint32_t blocks = op.passes * ((op.k + BK - 1) / BK);
+                for (uint32_t k = 0; k < blocks; ++k, ++it) {
+                    const uint32_t s = it % STAGES;
+                    if (!bar_wait(&ctl.full[s], (it / STAGES) & 1, &ctl, g.status)) { ok = false; break; }
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t st = smem_addr(stages + s * STAGE_BYTES);
+                    const uint64_t da = operand_desc(st, op.a_mn), db = operand_desc(st + OPERAND_BYTES, op.b_mn);
+                    const uint32_t sa = op.a_mn ? 2048 >> 4 : 32 >> 4, sb = op.b_mn ? 2048 >> 4 : 32 >> 4;
+#pragma unroll
+                    for (uint32_t q = 0; q < BK / 16; ++q)
+                        mma(tmem + as * TILE_MN, da + q * sa, db + q * sb, idesc, (k | q) != 0);
+                    mma_commit(&ctl.empty[s]);
+                }
+                if (ok) mma_commit(&ctl.acc_full[as]);
+            }
+        }
+    } else if (wid >= 4) {
+        const int quad = wid & 3;
+        uint32_t n = 0;
+        for (uint32_t t = blockIdx.x; t < g.n_tiles; t += gridDim.x, ++n) {
+            const Tile tl = g.tiles[t];
+            const Mat &M = g.mats[tl.mat];
+            const uint32_t as = n & 1;
+            if (!bar_wait(&ctl.acc_full[as], (n >> 1) & 1, &ctl, g.status)) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t rows = P == APPLY ? M.rows : M.m, cols = P == APPLY ? M.cols : M.m;
+            const uint32_t r = tl.tm * TILE_MN + quad * 32 + lane;
+#pragma unroll 1
+            for (uint32_t cb = 0; cb < TILE_MN; cb += 32) {
+                uint32_t v[32];
+                __syncwarp();
+                tmem_load32(tmem + (static_cast<uint32_t>(quad * 32) << 16) + as * TILE_MN + cb, v);
+                const uint32_t c0 = tl.tn * TILE_MN + cb;
+                if (r >= rows || c0 >= cols) continue;
+                const uint32_t count = min(32u, cols - c0);
+                if (P != APPLY) {
+                    __half *dst = P == GRAM ? M.a : M.b;
+                    __half *dst_lo = P == GRAM ? M.a_lo : M.b_lo;
+                    __half y[32], yl[32];
+                    const uint64_t at = static_cast<uint64_t>(r) * M.lda + c0;
+#pragma unroll
+                    for (uint32_t j0 = 0; j0 < 32; j0 += 8) {
+                        if (j0 >= count) break;
+                        uint4 old = make_uint4(0, 0, 0, 0), old_lo = old;
+                        if (P == POLY) old = *reinterpret_cast<const uint4 *>(M.a + at + j0);
+                        if (P == POLY && M.precision == FULL) old_lo = *reinterpret_cast<const uint4 *>(M.a_lo + at + j0);
+                        const __half *o = reinterpret_cast<const __half *>(&old), *ol = reinterpret_cast<const __half *>(&old_lo);
+#pragma unroll
+                        for (uint32_t j = 0; j < 8; ++j) {
+                            const float acc = __uint_as_float(v[j0 + j]) * INV_SCALE;
+                            const float x = P == GRAM ? acc
+                                                      : __fmaf_rn(g.c, acc, g.b * (__half2float(o[j]) + __half2float(ol[j])));
+                            y[j0 + j] = __float2half_rn(x);
+                            yl[j0 + j] = __float2half_rn(x - __half2float(y[j0 + j]));
+                        }
+                        *reinterpret_cast<uint4 *>(dst + at + j0) = *reinterpret_cast<uint4 *>(y + j0);
+                        if (dst_lo) *reinterpret_cast<uint4 *>(dst_lo + at + j0) = *reinterpret_cast<uint4 *>(yl + j0);
+                    }
+                    if (tl.tm != tl.tn)                          // the block's mirror image
+#pragma unroll
+                        for (uint32_t j = 0; j < 32; ++j)
+                            if (j < count) {
+                                const uint64_t mirror = static_cast<uint64_t>(c0 + j) * M.lda + r;
+                                dst[mirror] = y[j];
+                                if (dst_lo) dst_lo[mirror] = yl[j];
+                            }
+                } else {
+                    const uint64_t at = static_cast<uint64_t>(r) * M.ldx + c0;
+                    const uint64_t flat = M.offset + r * M.stride + c0;
+#pragma unroll
+                    for (uint32_t j0 = 0; j0 < 32; j0 += 8) {
+                        if (j0 >= count) break;
+                        const uint4 h4 = *reinterpret_cast<const uint4 *>(M.hi[g.src] + at + j0);
+                        uint4 l4 = make_uint4(0, 0, 0, 0);
+                        if (g.read_lo || M.precision == FULL) l4 = *reinterpret_cast<const uint4 *>(M.lo[g.src] + at + j0);
+                        const __half *h = reinterpret_cast<const __half *>(&h4), *l = reinterpret_cast<const __half *>(&l4);
+                        float x[8];
+#pragma unroll
+                        for (uint32_t j = 0; j < 8; ++j)
+                            x[j] = __fmaf_rn(g.a, __half2float(h[j]) + __half2float(l[j]),
+                                             __uint_as_float(v[j0 + j]) * INV_SCALE);
+                        if (T == NEXT_X) {
+                            __half nh[8], nl[8];
+#pragma unroll
+                            for (uint32_t j = 0; j < 8; ++j) {
+                                nh[j] = __float2half_rn(x[j]);
+                                nl[j] = __float2half_rn(x[j] - __half2float(nh[j]));
+                            }
+                            *reinterpret_cast<uint4 *>(M.hi[g.src ^ 1] + at + j0) = *reinterpret_cast<uint4 *>(nh);
+                            if (g.write_lo || M.precision == FULL)
+                                *reinterpret_cast<uint4 *>(M.lo[g.src ^ 1] + at + j0) = *reinterpret_cast<uint4 *>(nl);
+                        } else {
+                            const float s = M.scale * INV_SCALE;
+#pragma unroll
+                            for (uint32_t j = 0; j < 8; ++j) {
+                                if (j0 + j >= count) break;
+                                const uint64_t q = flat + j0 + j;
+                                if (T == OUT_BF16) g.out[q] = __float2bfloat16_rn(s * x[j]);
+                                else g.params[q] = __fmaf_rn(-g.lr, s * x[j], g.decay * g.params[q]);
+                            }
+                        }
+                    }
+                }
+            }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) bar_arrive(&ctl.acc_empty[as]);
+        }
+    }
+    __syncwarp();
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (wid == 2)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(2 * TILE_MN));
+}
+
+constexpr size_t GEMM_SMEM = STAGES * STAGE_BYTES + 1024;
+
+// ------------------------------------------------------------------- server update's own parts
+
+// M <- mu M
+__global__ void __launch_bounds__(INGEST_THREADS)
+decay_kernel(float *m, uint64_t d, float mu)
+{
+    for (uint64_t i = blockIdx.x * static_cast<uint64_t>(INGEST_THREADS) + threadIdx.x; i < d;
+         i += static_cast<uint64_t>(gridDim.x) * INGEST_THREADS)
+        m[i] *= mu;
+}
+
+// M <- M + weight S for an aggregate kept as pairs (each index at most once)
+__global__ void __launch_bounds__(INGEST_THREADS)
+add_pairs_kernel(float *m, uint64_t d, const deco_pair *s, uint64_t positions, float weight, uint32_t *status)
+{
+    for (uint64_t i = blockIdx.x * static_cast<uint64_t>(INGEST_THREADS) + threadIdx.x; i < positions;
+         i += static_cast<uint64_t>(gridDim.x) * INGEST_THREADS) {
+        const deco_pair p = s[i];
+        if (p.idx == DECO_NO_INDEX) continue;
+        if (p.idx >= d) {
+            atomicExch(status, static_cast<uint32_t>(DECO_ERR_DEVICE_CHECK));
+            continue;
+        }
+        m[p.idx] = __fmaf_rn(weight, p.val, m[p.idx]);
+    }
+}
+
+// x <- x decay - lr M for the entries of no matrix
+__global__ void __launch_bounds__(INGEST_THREADS)
+rest_kernel(const Piece *pieces, float *params, const float *m, float lr, float decay)
+{
+    const Piece p = pieces[blockIdx.x];
+    for (uint32_t j = threadIdx.x; j < p.count; j += INGEST_THREADS) {
+        const uint64_t i = p.offset + j;
+        params[i] = __fmaf_rn(-lr, m[i], decay * params[i]);
+    }
+}
+
+// ------------------------------------------------------------------------------------- host
+
+struct Group {
+    uint32_t convert0, n_convert;        // in the handle's lists
+    uint32_t gram0, n_gram, poly0, apply0, n_apply;
+};
+
+struct DeviceGuard {
+    int prev = -1;
+    bool ok = false;
+    explicit DeviceGuard(int dev)
+    {
+        ok = cudaGetDevice(&prev) == cudaSuccess && (prev == dev || cudaSetDevice(dev) == cudaSuccess);
+    }
+    ~DeviceGuard()
+    {
+        if (prev >= 0) cudaSetDevice(prev);
+    }
+};
+
+typedef CUresult (*EncodeFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                             const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                             CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeFn encode_function()
+{
+    void *fn = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess)
+        return nullptr;
+    return reinterpret_cast<EncodeFn>(fn);
+}
+
+// A row-major fp16 matrix, read in 64 x 64 boxes; outside of it zeros are read.
+bool encode(EncodeFn fn, CUtensorMap *map, void *base, uint64_t rows, uint64_t cols, uint64_t ld)
+{
+    const cuuint64_t dims[2] = {cols, rows}, strides[1] = {ld * 2};
+    const cuuint32_t box[2] = {64, 64}, step[2] = {1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, base, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+uint64_t round_up(uint64_t v, uint64_t to) { return (v + to - 1) / to * to; }
+
+// The polynomials, in order, on [0, 1]: largest singular value met and largest |b t + c t^2| on the way.
+bool coefficients_fit(const float *coef, uint32_t steps)
+{
+    double top = 1.0;
+    for (uint32_t i = 0; i < steps; ++i) {
+        const double a = coef[3 * i], b = coef[3 * i + 1], c = coef[3 * i + 2];
+        if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
+        if (top > MAX_SIGMA) return false;
+        // extrema of x (a + b x^2 + c x^4): a + 3 b t + 5 c t^2 = 0;  of b t + c t^2: t = -b / 2c
+        double at[4] = {top, 0, 0, 0};
+        const double disc = 9 * b * b - 20 * a * c;
+        if (c != 0 && disc >= 0) {
+            const double t1 = (-3 * b + sqrt(disc)) / (10 * c), t2 = (-3 * b - sqrt(disc)) / (10 * c);
+            if (t1 > 0) at[1] = sqrt(t1);
+            if (t2 > 0) at[2] = sqrt(t2);
+        } else if (c == 0 && b != 0 && -a / (3 * b) > 0) {
+            at[1] = sqrt(-a / (3 * b));
+        }
+        if (c != 0 && -b / (2 * c) > 0) at[3] = sqrt(-b / (2 * c));
+        double next = 0;
+        for (double x : at) {
+            if (x > top) continue;
+            const double t = x * x;
+            if (fabs(b * t + c * t * t) > MAX_B) return false;
+            next = std::max(next, fabs(x * (a + b * t + c * t * t)));
+        }
+        top = next;
+    }
+    return true;                                                 // the last iterate is not an operand
+}
+
+}  // namespace
+
+struct deco_orth {
+    uint64_t d = 0;
+    int device = 0;
+    uint32_t steps = 5;
+    std::vector<float> coef;
+    float eps = 1e-7f, mu = 0.f;
+    int nesterov = 0;
+    bool strided = false;                // some matrix's rows are not back to back
+    uint32_t sms = 0;
+    std::vector<Group> groups;
+    uint32_t n_pieces = 0, n_rest = 0, n_row_pieces = 0;
+    // device memory
+    uint8_t *workspace = nullptr;
+    Mat *mats = nullptr;
+    CUtensorMap *maps = nullptr;
+    Piece *pieces = nullptr;             // of the matrices, then of the rest
+    RowPiece *row_pieces = nullptr;
+    ConvertPiece *convert = nullptr;
+    Tile *tiles = nullptr;
+    double *partial = nullptr;
+    uint32_t *status = nullptr;
+    uint64_t device_bytes = 0, launches = 0;
+};
+
+namespace {
+
+void release(deco_orth *h)
+{
+    cudaFree(h->workspace);
+    cudaFree(h->mats);
+    cudaFree(h->maps);
+    cudaFree(h->pieces);
+    cudaFree(h->row_pieces);
+    cudaFree(h->convert);
+    cudaFree(h->tiles);
+    cudaFree(h->partial);
+    cudaFree(h->status);
+    delete h;
+}
+
+template <typename T>
+bool upload(deco_orth *h, T **dst, const std::vector<T> &v)
+{
+    const size_t bytes = sizeof(T) * std::max<size_t>(v.size(), 1);
+    if (cudaMalloc(reinterpret_cast<void **>(dst), bytes) != cudaSuccess) return false;
+    h->device_bytes += bytes;
+    return v.empty() || cudaMemcpy(*dst, v.data(), sizeof(T) * v.size(), cudaMemcpyHostToDevice) == cudaSuccess;
+}
+
+void add_pieces(std::vector<Piece> &out, uint64_t lo, uint64_t hi, uint32_t *slot)
+{
+    for (uint64_t at = lo; at < hi; at += PIECE)
+        out.push_back({at, static_cast<uint32_t>(std::min<uint64_t>(PIECE, hi - at)), slot ? (*slot)++ : NO_SLOT});
+}
+
+uint64_t span_end(const deco_matrix &m, uint64_t stride) { return m.offset + (m.rows - 1ull) * stride + m.cols; }
+
+// Matrices inside [0, d) that share no entry.  Spans may interleave only as columns of rows of one length.
+bool layout_ok(uint64_t d, const std::vector<deco_matrix> &ms)
+{
+    for (const deco_matrix &m : ms) {
+        if (m.rows == 0 || m.cols == 0 || m.rows >= (1u << 20) || m.cols >= (1u << 20) || m.row_stride < m.cols) return false;
+        if (m.offset > d || m.row_stride > (1ull << 40) || span_end(m, m.row_stride) > d) return false;
+    }
+    std::vector<uint32_t> order(ms.size());
+    for (uint32_t i = 0; i < ms.size(); ++i) order[i] = i;
+    std::sort(order.begin(), order.end(), [&](uint32_t x, uint32_t y) { return ms[x].offset < ms[y].offset; });
+    std::vector<uint32_t> open;                                  // earlier matrices whose spans may reach on
+    for (uint32_t i : order) {
+        const deco_matrix &b = ms[i];
+        std::vector<uint32_t> still;
+        for (uint32_t j : open) {
+            const deco_matrix &a = ms[j];
+            if (span_end(a, a.row_stride) <= b.offset) continue;
+            still.push_back(j);
+            if (a.row_stride != b.row_stride) return false;
+            const uint64_t s = a.row_stride, ca = a.offset % s, cb = b.offset % s;
+            if (ca + a.cols > s || cb + b.cols > s) return false;
+            if (ca < cb + b.cols && cb < ca + a.cols) {
+                // same columns: rows must not meet
+                const uint64_t ra = a.offset / s, rb = b.offset / s;
+                if (ra < rb + b.rows && rb < ra + a.rows) return false;
+            }
+        }
+        still.push_back(i);
+        open.swap(still);
+    }
+    return true;
+}
+
+deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, uint64_t cap)
+{
+    const EncodeFn enc = encode_function();
+    if (!enc) return DECO_ERR_CUDA;
+    const uint32_t n = static_cast<uint32_t>(ms.size());
+    std::vector<Mat> mats(n);
+    std::vector<uint64_t> bytes(n);
+    for (uint32_t i = 0; i < n; ++i) {
+        Mat &M = mats[i];
+        const deco_matrix &q = ms[i];
+        M.offset = q.offset;
+        M.stride = q.row_stride;
+        M.rows = q.rows;
+        M.cols = q.cols;
+        M.tall = q.rows > q.cols;
+        M.m = std::min(q.rows, q.cols);
+        M.n = std::max(q.rows, q.cols);
+        M.ldx = static_cast<uint32_t>(round_up(q.cols, 8));
+        M.lda = static_cast<uint32_t>(round_up(M.m, 8));
+        M.precision = M.m <= FULL_SIDE ? FULL : M.m <= WIDE_B_SIDE ? WIDE_B : PLAIN;
+        const double r = q.rows, c = q.cols;
+        M.scale = scale == DECO_ORTH_SCALE_SPECTRAL ? static_cast<float>(sqrt(std::max(1.0, r / c)))
+                : scale == DECO_ORTH_SCALE_RMS      ? static_cast<float>(0.2 * sqrt(std::max(r, c)))
+                                                    : 1.f;
+        bytes[i] = 4 * round_up(2ull * M.rows * M.ldx, 256) + (2 + M.precision) * round_up(2ull * M.m * M.lda, 256);
+    }
+    // groups, in order, of what fits the workspace
+    std::vector<uint32_t> group_of(n);
+    uint64_t used = 0, most = 0;
+    uint32_t groups = 0;
+    for (uint32_t i = 0; i < n; ++i) {
+        if (i == 0 || used + bytes[i] > cap) {
+            groups += 1;
+            used = 0;
+        }
+        group_of[i] = groups - 1;
+        used += bytes[i];
+        most = std::max(most, used);
+    }
+    if (most) {
+        if (cudaMalloc(reinterpret_cast<void **>(&h->workspace), most) != cudaSuccess) return DECO_ERR_OOM;
+        h->device_bytes += most;
+        if (cudaMemset(h->workspace, 0, most) != cudaSuccess) return DECO_ERR_CUDA;
+    }
+    std::vector<CUtensorMap> maps(static_cast<uint64_t>(MAPS) * n);
+    uint64_t at = 0;
+    for (uint32_t i = 0; i < n; ++i) {
+        if (i == 0 || group_of[i] != group_of[i - 1]) at = 0;
+        Mat &M = mats[i];
+        const uint64_t xb = round_up(2ull * M.rows * M.ldx, 256), ab = round_up(2ull * M.m * M.lda, 256);
+        auto take = [&](uint64_t b) { __half *p = reinterpret_cast<__half *>(h->workspace + at); at += b; return p; };
+        for (int k = 0; k < 2; ++k) { M.hi[k] = take(xb); M.lo[k] = take(xb); }
+        M.a = take(ab);
+        M.b = take(ab);
+        M.b_lo = M.precision >= WIDE_B ? take(ab) : nullptr;
+        M.a_lo = M.precision == FULL ? take(ab) : nullptr;
+        CUtensorMap *map = &maps[static_cast<uint64_t>(MAPS) * i];
+        bool ok = true;
+        for (int k = 0; k < 2; ++k)
+            ok = ok && encode(enc, map + MAP_X + 2 * k, M.hi[k], M.rows, M.cols, M.ldx) &&
+                 encode(enc, map + MAP_X + 2 * k + 1, M.lo[k], M.rows, M.cols, M.ldx);
+        ok = ok && encode(enc, map + MAP_A, M.a, M.m, M.m, M.lda) && encode(enc, map + MAP_B, M.b, M.m, M.m, M.lda);
+        if (M.a_lo) ok = ok && encode(enc, map + MAP_A + 1, M.a_lo, M.m, M.m, M.lda);
+        if (M.b_lo) ok = ok && encode(enc, map + MAP_B + 1, M.b_lo, M.m, M.m, M.lda);
+        if (!ok) return DECO_ERR_CUDA;
+    }
+    // pieces: matrices whose rows are back to back, in order of their place; then everything else
+    std::vector<uint32_t> order(n);
+    for (uint32_t i = 0; i < n; ++i) order[i] = i;
+    std::sort(order.begin(), order.end(), [&](uint32_t x, uint32_t y) { return mats[x].offset < mats[y].offset; });
+    std::vector<Piece> pieces, rest;
+    std::vector<RowPiece> row_pieces;
+    uint32_t slot = 0;
+    uint64_t end = 0;
+    for (uint32_t i : order) {
+        Mat &M = mats[i];
+        if (M.stride != M.cols && M.rows > 1) continue;
+        add_pieces(rest, end, M.offset, nullptr);
+        M.piece0 = slot;
+        end = M.offset + static_cast<uint64_t>(M.rows) * M.cols;
+        add_pieces(pieces, M.offset, end, &slot);
+        M.pieces = slot - M.piece0;
+    }
+    add_pieces(rest, end, h->d, nullptr);
+    for (uint32_t i : order) {
+        Mat &M = mats[i];
+        if (M.stride == M.cols || M.rows == 1) continue;
+        h->strided = true;
+        M.piece0 = slot;
+        const uint32_t per = std::max(1u, PIECE / M.cols);
+        for (uint32_t r = 0; r < M.rows; r += per) row_pieces.push_back({i, r, std::min(per, M.rows - r), slot++});
+        M.pieces = slot - M.piece0;
+    }
+    h->n_pieces = static_cast<uint32_t>(pieces.size());
+    h->n_rest = static_cast<uint32_t>(rest.size());
+    h->n_row_pieces = static_cast<uint32_t>(row_pieces.size());
+    pieces.insert(pieces.end(), rest.begin(), rest.end());
+    // tiles and convert pieces of each group, the longest products first
+    std::vector<Tile> tiles;
+    std::vector<ConvertPiece> convert;
+    for (uint32_t g = 0, i0 = 0; g < groups; ++g) {
+        uint32_t i1 = i0;
+        while (i1 < n && group_of[i1] == g) ++i1;
+        Group G = {};
+        G.convert0 = static_cast<uint32_t>(convert.size());
+        std::vector<uint32_t> by(i1 - i0);
+        for (uint32_t i = i0; i < i1; ++i) {
+            by[i - i0] = i;
+            const Mat &M = mats[i];
+            for (uint32_t c = 0; c < M.cols; c += CONVERT_COLS) {
+                const uint32_t per = std::max(1u, PIECE / std::min(M.cols - c, CONVERT_COLS));
+                for (uint32_t r = 0; r < M.rows; r += per) convert.push_back({i, r, std::min(per, M.rows - r), c});
+            }
+        }
+        G.n_convert = static_cast<uint32_t>(convert.size()) - G.convert0;
+        auto blocks = [](uint32_t v) { return (v + TILE_MN - 1) / TILE_MN; };
+        auto symmetric = [&]() {
+            for (uint32_t i : by)
+                for (uint32_t r = 0; r < blocks(mats[i].m); ++r)
+                    for (uint32_t c = 0; c <= r; ++c) tiles.push_back({i, static_cast<uint16_t>(r), static_cast<uint16_t>(c)});
+        };
+        std::stable_sort(by.begin(), by.end(), [&](uint32_t x, uint32_t y) { return mats[x].n > mats[y].n; });
+        G.gram0 = static_cast<uint32_t>(tiles.size());
+        symmetric();
+        G.n_gram = static_cast<uint32_t>(tiles.size()) - G.gram0;
+        std::stable_sort(by.begin(), by.end(), [&](uint32_t x, uint32_t y) { return mats[x].m > mats[y].m; });
+        G.poly0 = static_cast<uint32_t>(tiles.size());
+        symmetric();
+        G.apply0 = static_cast<uint32_t>(tiles.size());
+        for (uint32_t i : by)
+            for (uint32_t r = 0; r < blocks(mats[i].rows); ++r)
+                for (uint32_t c = 0; c < blocks(mats[i].cols); ++c)
+                    tiles.push_back({i, static_cast<uint16_t>(r), static_cast<uint16_t>(c)});
+        G.n_apply = static_cast<uint32_t>(tiles.size()) - G.apply0;
+        h->groups.push_back(G);
+        i0 = i1;
+    }
+    std::vector<double> partial(slot, 0.0);
+    std::vector<uint32_t> status(1, 0u);
+    if (!upload(h, &h->mats, mats) || !upload(h, &h->maps, maps) || !upload(h, &h->pieces, pieces) ||
+        !upload(h, &h->row_pieces, row_pieces) || !upload(h, &h->convert, convert) || !upload(h, &h->tiles, tiles) ||
+        !upload(h, &h->partial, partial) || !upload(h, &h->status, status))
+        return DECO_ERR_OOM;
+    // the copies above may still be under way; the handle's first pass may come on any stream
+    return cudaDeviceSynchronize() == cudaSuccess ? DECO_OK : DECO_ERR_CUDA;
+}
+
+template <Phase P, Target T>
+cudaError_t launch_gemm(deco_orth *h, GemmArgs &g, uint32_t first, uint32_t count, cudaStream_t s)
+{
+    g.tiles = h->tiles + first;
+    g.n_tiles = count;
+    const uint32_t grid = std::min(count, h->sms);
+    gemm_kernel<P, T><<<grid, GEMM_THREADS, GEMM_SMEM, s>>>(g);
+    h->launches += 1;
+    return cudaGetLastError();
+}
+
+template <Phase P, Target T>
+cudaError_t allow_smem()
+{
+    return cudaFuncSetAttribute(gemm_kernel<P, T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                static_cast<int>(GEMM_SMEM));
+}
+
+// The whole pass over what `src` describes; params: the server update's target instead of out.
+template <typename T>
+cudaError_t run_pass(deco_orth *h, const Source<T> &src, __nv_bfloat16 *out, float *params, float lr, float decay,
+                     cudaStream_t s)
+{
+    const uint32_t taken = h->n_pieces + (src.mom && src.in ? h->n_rest : 0);
+    if (taken) {
+        ingest_kernel<T><<<taken, INGEST_THREADS, 0, s>>>(h->pieces, src, h->partial);
+        h->launches += 1;
+    }
+    if (h->n_row_pieces) {
+        ingest_rows_kernel<T><<<h->n_row_pieces, INGEST_THREADS, 0, s>>>(h->row_pieces, h->mats, src, h->partial);
+        h->launches += 1;
+    }
+    cudaError_t err = cudaGetLastError();
+    for (const Group &G : h->groups) {
+        if (err != cudaSuccess) return err;
+        convert_kernel<T><<<G.n_convert, INGEST_THREADS, 0, s>>>(h->convert + G.convert0, h->mats, src, h->partial, h->eps);
+        h->launches += 1;
+        err = cudaGetLastError();
+        GemmArgs g = {};
+        g.mats = h->mats;
+        g.maps = h->maps;
+        g.status = h->status;
+        g.out = out;
+        g.params = params;
+        g.lr = lr;
+        g.decay = decay;
+        for (uint32_t i = 0; i < h->steps && err == cudaSuccess; ++i) {
+            const bool last = i + 1 == h->steps;
+            g.src = i & 1;
+            g.read_lo = !last || h->steps == 1;
+            g.write_lo = i + 2 < h->steps;
+            g.a = h->coef[3 * i];
+            g.b = h->coef[3 * i + 1];
+            g.c = h->coef[3 * i + 2];
+            err = launch_gemm<GRAM, NEXT_X>(h, g, G.gram0, G.n_gram, s);
+            if (err == cudaSuccess) err = launch_gemm<POLY, NEXT_X>(h, g, G.poly0, G.n_gram, s);
+            if (err != cudaSuccess) break;
+            err = !last    ? launch_gemm<APPLY, NEXT_X>(h, g, G.apply0, G.n_apply, s)
+                : params   ? launch_gemm<APPLY, PARAMS>(h, g, G.apply0, G.n_apply, s)
+                           : launch_gemm<APPLY, OUT_BF16>(h, g, G.apply0, G.n_apply, s);
+        }
+    }
+    return err;
+}
+
+}  // namespace
+
+extern "C" deco_status deco_orth_init(deco_orth **out, uint64_t d, const deco_matrix *matrices, uint32_t n_matrices,
+                                      const deco_orth_options *opt)
+try {
+    if (!out || d == 0 || d > (1ull << 40) || (n_matrices && !matrices) || n_matrices > (1u << 24)) return DECO_ERR_INVALID_ARG;
+    deco_orth_options o = {};
+    if (opt) o = *opt;
+    for (uint32_t r : o.reserved)
+        if (r) return DECO_ERR_INVALID_ARG;
+    const uint32_t steps = o.steps ? o.steps : 5;
+    if (steps > MAX_STEPS || !(o.eps >= 0.f) || o.eps > 1e30f || !(o.momentum >= 0.f && o.momentum < 1.f) ||
+        o.scale < DECO_ORTH_SCALE_NONE || o.scale > DECO_ORTH_SCALE_RMS)
+        return DECO_ERR_INVALID_ARG;
+    std::vector<float> coef(3 * steps);
+    const float standard[3] = {3.4445f, -4.7750f, 2.0315f};
+    for (uint32_t i = 0; i < 3 * steps; ++i) coef[i] = o.coef ? o.coef[i] : standard[i % 3];
+    if (!coefficients_fit(coef.data(), steps)) return DECO_ERR_INVALID_ARG;
+    std::vector<deco_matrix> ms(matrices, matrices + n_matrices);
+    for (deco_matrix &m : ms)
+        if (m.row_stride == 0 || m.rows == 1) m.row_stride = m.row_stride ? std::max<uint64_t>(m.row_stride, m.cols) : m.cols;
+    if (!layout_ok(d, ms)) return DECO_ERR_INVALID_ARG;
+    DeviceGuard guard(o.device);
+    if (!guard.ok) return DECO_ERR_CUDA;
+    int sms = 0;
+    if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, o.device) != cudaSuccess) return DECO_ERR_CUDA;
+    if (allow_smem<GRAM, NEXT_X>() != cudaSuccess || allow_smem<POLY, NEXT_X>() != cudaSuccess ||
+        allow_smem<APPLY, NEXT_X>() != cudaSuccess || allow_smem<APPLY, OUT_BF16>() != cudaSuccess ||
+        allow_smem<APPLY, PARAMS>() != cudaSuccess)
+        return DECO_ERR_CUDA;
+    deco_orth *h = new deco_orth;
+    deco_status st = DECO_ERR_OOM;
+    try {
+        h->d = d;
+        h->device = o.device;
+        h->steps = steps;
+        h->coef = coef;
+        h->eps = o.eps > 0.f ? o.eps : 1e-7f;
+        h->mu = o.momentum;
+        h->nesterov = o.nesterov != 0;
+        h->sms = static_cast<uint32_t>(sms);
+        st = plan(h, ms, o.scale, o.workspace_bytes ? o.workspace_bytes : 2ull << 30);
+    } catch (...) {
+    }
+    if (st != DECO_OK) {
+        cudaGetLastError();
+        release(h);
+        return st;
+    }
+    *out = h;
+    return DECO_OK;
+} catch (...) {
+    return DECO_ERR_OOM;
+}
+
+extern "C" void deco_orth_destroy(deco_orth *h)
+{
+    if (!h) return;
+    DeviceGuard guard(h->device);
+    cudaDeviceSynchronize();
+    release(h);
+}
+
+extern "C" deco_status deco_orth_run(deco_orth *h, const void *in, int32_t in_dtype, float *momentum, void *out, void *stream)
+{
+    if (!h || !in || !out || (in_dtype != DECO_F32 && in_dtype != DECO_BF16)) return DECO_ERR_INVALID_ARG;
+    const uintptr_t unit = in_dtype == DECO_F32 ? 3 : 1;
+    if ((reinterpret_cast<uintptr_t>(in) & unit) || (reinterpret_cast<uintptr_t>(momentum) & 3) ||
+        (reinterpret_cast<uintptr_t>(out) & 1))
+        return DECO_ERR_INVALID_ARG;
+    DeviceGuard guard(h->device);
+    if (!guard.ok) return DECO_ERR_CUDA;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(out);
+    cudaError_t err;
+    if (in_dtype == DECO_F32)
+        err = run_pass(h, Source<float>{static_cast<const float *>(in), momentum, 1.f, h->mu, h->nesterov}, o, nullptr, 0.f, 0.f, s);
+    else
+        err = run_pass(h, Source<__nv_bfloat16>{static_cast<const __nv_bfloat16 *>(in), momentum, 1.f, h->mu, h->nesterov}, o,
+                       nullptr, 0.f, 0.f, s);
+    return err == cudaSuccess ? DECO_OK : DECO_ERR_CUDA;
+}
+
+deco_status deco::orth_update(deco_orth *h, const deco_ctx *c, const Slot &slot, const deco_pair *data, float *momentum,
+                              float weight_decay, cudaStream_t s)
+{
+    const float weight = 1.f / static_cast<float>(c->n_total);
+    const float decay = 1.f - c->lr * weight_decay;
+    Source<float> src = {nullptr, momentum, weight, h->mu, 0};
+    if (slot.dense) {
+        src.in = reinterpret_cast<const float *>(data);
+    } else {
+        const unsigned grid = h->sms * 8;
+        decay_kernel<<<grid, INGEST_THREADS, 0, s>>>(momentum, h->d, h->mu);
+        add_pairs_kernel<<<grid, INGEST_THREADS, 0, s>>>(momentum, h->d, data, slot.positions, weight, h->status);
+        h->launches += 2;
+    }
+    cudaError_t err = run_pass(h, src, nullptr, c->params, c->lr, decay, s);
+    if (err == cudaSuccess && h->n_rest) {
+        rest_kernel<<<h->n_rest, INGEST_THREADS, 0, s>>>(h->pieces + h->n_pieces, c->params, momentum, c->lr, decay);
+        h->launches += 1;
+        err = cudaGetLastError();
+    }
+    return err == cudaSuccess ? DECO_OK : DECO_ERR_CUDA;
+}
+
+bool deco::orth_fits(const deco_orth *h, const deco_ctx *c)
+{
+    return h->d == c->d && h->device == c->device && !h->strided && !h->nesterov;
+}
+
+extern "C" deco_status deco_orth_get_stats(deco_orth *h, void *stream, deco_orth_stats *out)
+{
+    if (!h || !out) return DECO_ERR_INVALID_ARG;
+    DeviceGuard guard(h->device);
+    if (!guard.ok) return DECO_ERR_CUDA;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    uint32_t status = 0;
+    if (cudaMemcpyAsync(&status, h->status, sizeof(status), cudaMemcpyDeviceToHost, s) != cudaSuccess ||
+        cudaStreamSynchronize(s) != cudaSuccess)
+        return DECO_ERR_CUDA;
+    out->device_bytes = h->device_bytes;
+    out->launches = h->launches;
+    out->groups = static_cast<uint32_t>(h->groups.size());
+    out->device_status = status;
+    return status ? DECO_ERR_DEVICE_CHECK : DECO_OK;
+}

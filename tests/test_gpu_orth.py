@@ -1,0 +1,390 @@
+"""deco_orth_*: orthogonalised updates against the polynomial in 64 bits.
+
+Tolerance in the 2-norm of a matrix.  bf16 outputs: rounding errors uniform within half a unit, 2^-9 to
+2^-8 of a value: 1.7e-3 on average over many entries, at most 2^-8 = 3.9e-3 for one.  Products: each
+step rounds A, B and the operand X to 11 bits (2^-12 on average 0.42 * 2^-11 = 2.0e-4 of a value); a
+rounding of step i reaches the output through the steps behind it, whose mean slope is below 1.5,
+and b A and c A^2 (up to 4.8 and 2.0 times A, of opposite sign) cancel: 5 steps x 3 roundings x about 3
+added in squares, 2.0e-4 * 3 * sqrt(15) = 2.4e-3 at most.  Together sqrt(1.7^2 + 2.4^2) e-3 = 2.9e-3;
+4e-3 is asked for, and 6.5e-3 (2^-8 more or less whole) where a matrix has fewer than 64 entries.
+Momentum is one fused multiply-add: 2^-24 of its terms.
+"""
+import math
+
+import pytest
+import torch
+
+from paper_2507_17346_b200 import binding as B
+
+gpu = pytest.mark.gpu
+COEF = (3.4445, -4.7750, 2.0315)
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    from paper_2507_17346_b200 import build
+    build.build()
+    B.load()
+    if torch.cuda.is_available():
+        torch.cuda.set_device(0)
+
+
+def exact(y, steps=5, coef=None, eps=1e-7):
+    coef = coef or [COEF] * steps
+    x = y.double()
+    x = x / (x.norm() + eps)
+    if x.shape[0] > x.shape[1]:
+        return exact_wide(x.t(), coef).t()
+    return exact_wide(x, coef)
+
+
+def exact_wide(x, coef):
+    for a, b, c in coef:
+        g = x @ x.t()
+        x = a * x + (b * g + c * (g @ g)) @ x
+    return x
+
+
+def tol(numel):
+    return 6.5e-3 if numel < 64 else 4e-3
+
+
+def rel(got, want):
+    return ((got.double() - want).norm() / want.norm()).item()
+
+
+def make(rows, cols, kind, seed, dtype=torch.float32):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    x = r(rows, cols)
+    if kind == "outlier":
+        x[:: max(2, rows // 7)] *= 50
+    elif kind == "rank1":
+        x = r(rows, 1) @ r(1, cols)
+    elif kind == "lowrank":
+        x = r(rows, 4) @ r(4, cols) + 1e-3 * x
+    elif kind == "sparse":
+        x = torch.where(x.abs() > 2.2, x, torch.zeros_like(x))
+        x[rows // 2, cols // 2] = 3.0
+    elif kind == "tiny":
+        x = x * 1e-3
+    return (0.02 * x).to(dtype)
+
+
+def run_one(x, **kw):
+    """x laid in a flat vector with a few entries around it, which must stay as they are."""
+    n = x.numel()
+    flat = torch.full((n + 11,), 5.0, device="cuda", dtype=x.dtype)
+    flat[3:3 + n] = x.reshape(-1)
+    out = torch.full((n + 11,), -9.0, device="cuda", dtype=torch.bfloat16)
+    h = B.deco_orth_init(n + 11, [(3, x.shape[0], x.shape[1])], **kw)
+    try:
+        B.deco_orth_run(h, flat, out)
+        assert B.deco_orth_get_stats(h)["device_status"] == 0
+    finally:
+        B.deco_orth_destroy(h)
+    assert (out[:3] == -9).all() and (out[3 + n:] == -9).all()
+    return out[3:3 + n].view(x.shape)
+
+
+SHAPES = [(1, 1), (1, 7), (9, 1), (2, 3), (5, 5), (8, 64), (64, 8), (63, 65), (64, 147), (147, 64), (128, 128), (129, 127),
+          (130, 1000), (1000, 130), (255, 257), (256, 512), (300, 301), (384, 640), (640, 385), (513, 1100), (1025, 520)]
+
+
+@gpu
+@pytest.mark.parametrize("rows,cols", SHAPES)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_shapes(rows, cols, dtype):
+    x = make(rows, cols, "normal", rows * 7 + cols, dtype)
+    got = run_one(x)
+    assert rel(got, exact(x)) < tol(x.numel())
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["outlier", "rank1", "lowrank", "sparse", "tiny"])
+@pytest.mark.parametrize("rows,cols", [(96, 200), (520, 260), (700, 768)])
+def test_spectra(rows, cols, kind):
+    """Spectra that gradients have; in rank 1 and rank 4 the missing directions must stay empty."""
+    x = make(rows, cols, kind, rows + cols)
+    assert rel(run_one(x), exact(x)) < tol(x.numel())
+
+
+@gpu
+@pytest.mark.parametrize("steps,coef", [(1, None), (2, None), (3, None), (8, None), (5, (2.0, -1.5, 0.5)),
+                                        (4, [(3.0, -3.2, 1.2), (2.5, -2.5, 1.0), (2.0, -1.5, 0.5), (1.875, -1.25, 0.375)])])
+def test_steps_and_coefficients(steps, coef):
+    x = make(200, 333, "normal", steps)
+    each = [COEF] * steps if coef is None else coef if isinstance(coef, list) else [coef] * steps
+    got = run_one(x, steps=steps, coef=coef)
+    # more steps carry more roundings: their squares add up
+    assert rel(got, exact(x, steps, each)) < tol(x.numel()) * math.sqrt(max(1.0, steps / 5))
+
+
+@gpu
+@pytest.mark.parametrize("scale", [0, 1, 2])
+def test_output_scale(scale):
+    for rows, cols in ((260, 100), (100, 260)):
+        x = make(rows, cols, "normal", 3)
+        s = {0: 1.0, 1: math.sqrt(max(1.0, rows / cols)), 2: 0.2 * math.sqrt(max(rows, cols))}[scale]
+        assert rel(run_one(x, scale=scale), s * exact(x)) < tol(x.numel())
+
+
+@gpu
+def test_extreme_norms_zero_and_nan():
+    x = make(70, 90, "normal", 1)
+    for f in (1e30, 1e-30, 3e37):
+        y = x * f
+        assert rel(run_one(y, eps=1e-38), exact(y, eps=1e-38)) < tol(x.numel())
+    small = x * 1e-8                                                # eps takes part
+    assert rel(run_one(small), exact(small)) < tol(x.numel())
+    assert (run_one(torch.zeros_like(x)) == 0).all()
+    bad = x.clone()
+    bad[3, 4] = math.nan
+    assert torch.isnan(run_one(bad)).all()
+    bad[3, 4] = math.inf
+    assert torch.isnan(run_one(bad)).any()
+
+
+def flat_case(shapes, gap, dtype, seed):
+    mats, at = [], gap
+    for r, c in shapes:
+        mats.append((at, r, c))
+        at += r * c + gap
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return mats, at, torch.randn(at, generator=g, device="cuda").mul_(0.02).to(dtype)
+
+
+MANY = [(64, 147), (64, 576), (1, 64), (128, 64), (300, 100), (100, 300), (257, 129), (40, 2100), (2100, 40), (512, 256)]
+
+
+@gpu
+@pytest.mark.parametrize("workspace", [0, 1, 3_000_000])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_many_matrices_with_momentum(dtype, workspace):
+    """Matrices of many shapes in one handle, in one group and in several; two passes with momentum."""
+    for nesterov in (False, True):
+        mats, d, x = flat_case(MANY, 5, dtype, 11)
+        m = torch.randn(d, device="cuda") * 0.05
+        out = torch.full((d,), -9.0, device="cuda", dtype=torch.bfloat16)
+        h = B.deco_orth_init(d, mats, momentum=0.9, nesterov=nesterov, workspace_bytes=workspace)
+        try:
+            for _ in range(2):
+                want = m.double() * float(torch.tensor(0.9)) + x.double()
+                B.deco_orth_run(h, x, out, momentum=m)
+                bound = (want.abs() + x.double().abs()) * 2.0 ** -23 + 1e-38
+                assert ((m.double() - want).abs() <= bound).all()   # entries of no matrix too
+                y = m.double() * float(torch.tensor(0.9)) + x.double() if nesterov else m.double()
+                used = torch.zeros(d, dtype=torch.bool, device="cuda")
+                for at, r, c in mats:
+                    used[at:at + r * c] = True
+                    assert rel(out[at:at + r * c].view(r, c), exact(y[at:at + r * c].view(r, c))) < tol(r * c)
+                assert (out[~used] == -9).all()
+            st = B.deco_orth_get_stats(h)
+            assert st["device_status"] == 0 and st["groups"] == (1 if workspace == 0 else st["groups"])
+            assert workspace == 0 or st["groups"] > 1
+        finally:
+            B.deco_orth_destroy(h)
+
+
+@gpu
+def test_row_strides_and_interleaved_columns():
+    """Three matrices that are column ranges of one buffer of rows, a strided one, and plain ones between."""
+    S = 700
+    mats = [(10, 120, 200, S), (10 + 200, 120, 300, S), (10 + 500, 120, 190, S), (10 + 120 * S, 33, 77)]
+    d = 10 + 120 * S + 33 * 77 + 3
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    x = torch.randn(d, generator=g, device="cuda")
+    for momentum in (False, True):
+        m = torch.randn(d, device="cuda") if momentum else None
+        out = torch.full((d,), -9.0, device="cuda", dtype=torch.bfloat16)
+        h = B.deco_orth_init(d, mats, momentum=0.5)
+        try:
+            y = m.double() * 0.5 + x.double() if momentum else x.double()
+            B.deco_orth_run(h, x, out, momentum=m)
+            if momentum:
+                assert ((m.double() - y).abs() <= (y.abs() + x.double().abs()) * 2.0 ** -23).all()
+            used = torch.zeros(d, dtype=torch.bool, device="cuda")
+            for q in mats:
+                s = q[3] if len(q) > 3 else q[2]
+                pick = lambda t: torch.as_strided(t, (q[1], q[2]), (s, 1), q[0])  # noqa: E731
+                pick(used).fill_(True)
+                assert rel(pick(out), exact(pick(y))) < tol(q[1] * q[2])
+            assert (out[~used] == -9).all()
+        finally:
+            B.deco_orth_destroy(h)
+
+
+@gpu
+def test_same_bits_again_and_on_another_stream():
+    mats, d, x = flat_case(MANY, 0, torch.float32, 3)
+    outs = []
+    h = B.deco_orth_init(d, mats)
+    s = torch.cuda.Stream()
+    try:
+        for stream in (None, None, s):
+            out = torch.zeros(d, device="cuda", dtype=torch.bfloat16)
+            s.wait_stream(torch.cuda.current_stream())
+            B.deco_orth_run(h, x, out, stream=stream)
+            torch.cuda.synchronize()
+            outs.append(out)
+        # handles that come and go in the same memory
+        B.deco_orth_destroy(h)
+        h = B.deco_orth_init(d, list(reversed(mats)))
+        out = torch.zeros(d, device="cuda", dtype=torch.bfloat16)
+        B.deco_orth_run(h, x, out)
+        torch.cuda.synchronize()
+        outs.append(out)
+    finally:
+        B.deco_orth_destroy(h)
+    for o in outs[1:]:
+        assert torch.equal(o, outs[0])
+
+
+@gpu
+def test_larger_than_one_wave():
+    """More tiles than SMs, several tiles per CTA, long products."""
+    mats, d, x = flat_case([(1100, 2300), (2300, 1100), (1000, 1000), (200, 5000)], 0, torch.bfloat16, 5)
+    out = torch.zeros(d, device="cuda", dtype=torch.bfloat16)
+    h = B.deco_orth_init(d, mats)
+    try:
+        B.deco_orth_run(h, x, out)
+        for at, r, c in mats:
+            assert rel(out[at:at + r * c].view(r, c), exact(x[at:at + r * c].view(r, c))) < tol(r * c)
+        assert B.deco_orth_get_stats(h)["device_status"] == 0
+    finally:
+        B.deco_orth_destroy(h)
+
+
+@gpu
+@pytest.mark.parametrize("delta,tau", [(0.01, 0), (0.01, 2), (0.5, 1)])
+def test_server_update(delta, tau):
+    """deco_apply_update_orth in the iteration: sparse and dense aggregates, momentum, weight decay."""
+    shapes, gap, n, lr, wd, mu = [(64, 147), (300, 100), (129, 257)], 13, 3, 0.02, 0.1, 0.9
+    mats, d, _ = flat_case(shapes, gap, torch.float32, 0)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    params = (0.05 * torch.randn(d, generator=g, device="cuda")).contiguous()
+    want = params.double().clone()
+    ctx = B.deco_init(d, n, delta, tau, lr, lr_at_server=True, params=params)
+    h = B.deco_orth_init(d, mats, momentum=mu, scale=B.DECO_ORTH_SCALE_RMS)
+    m = torch.zeros(d, device="cuda")
+    wm = torch.zeros(d, device="cuda", dtype=torch.float64)
+    sums = []
+    mu32, lr32, w32 = (float(torch.tensor(v)) for v in (mu, lr, 1.0 / n))
+    decay = float(torch.tensor(1.0) - torch.tensor(lr) * torch.tensor(wd))
+    try:
+        for t in range(5):
+            B.deco_ef_compress(ctx, torch.randn(n, d, generator=g, device="cuda"))
+            with pytest.raises(B.DecoError):
+                B.deco_apply_update_orth(ctx, h, m, wd)             # out of order
+            B.deco_aggregate_stale(ctx)
+            k, buf = B.deco_get_k(ctx), B.deco_get_buffers(ctx)
+            pairs = B.view_i32(buf["msg"], (n, buf["k_cap"], 2))[:, :k]
+            s = torch.zeros(d, device="cuda", dtype=torch.float64)
+            for i in range(n):
+                s.index_add_(0, pairs[i, :, 0].long(), pairs[i, :, 1].contiguous().view(torch.float32).double())
+            sums.append(s)
+            B.deco_apply_update_orth(ctx, h, m, wd)
+            if t < tau:
+                continue
+            wm = mu32 * wm + w32 * sums[t - tau]
+            used = torch.zeros(d, dtype=torch.bool, device="cuda")
+            step = torch.zeros(d, device="cuda", dtype=torch.float64)
+            for at, r, c in mats:
+                used[at:at + r * c] = True
+                step[at:at + r * c] = (0.2 * math.sqrt(max(r, c)) * exact(wm[at:at + r * c].view(r, c))).reshape(-1)
+            want = want * decay - lr32 * torch.where(used, step, wm)
+            # momentum: three fp32 roundings of terms of its size, five passes
+            assert (m.double() - wm).norm() <= 20 * 2.0 ** -24 * (wm.norm() + sum(x.norm() for x in sums))
+            # parameters of matrices: the products' share of the tolerance on each of the t + 1 updates
+            err = (params.double() - want)
+            assert err[used].norm() <= 2.9e-3 * lr32 * step[used].norm() * (t + 1) + 1e-6 * want.norm()
+            assert err[~used].norm() <= 1e-6 * want.norm()
+        assert B.deco_get_stats(ctx)["step"] == 5 and B.deco_orth_get_stats(h)["device_status"] == 0
+    finally:
+        B.deco_orth_destroy(h)
+        B.deco_destroy(ctx)
+
+
+@gpu
+def test_server_update_refusals():
+    d = 4096
+    m = torch.zeros(d, device="cuda")
+    plain = B.deco_init(d, 1, 0.1, 0, 0.1)
+    server = B.deco_init(d, 1, 0.1, 0, 0.1, lr_at_server=True)
+    good, other = B.deco_orth_init(d, [(0, 64, 64)]), B.deco_orth_init(d + 1, [(0, 64, 64)])
+    strided, nest = B.deco_orth_init(d, [(0, 32, 64, 128)]), B.deco_orth_init(d, [(0, 64, 64)], nesterov=True)
+    try:
+        for ctx in (plain, server):
+            B.deco_ef_compress(ctx, torch.randn(1, d, device="cuda"))
+            B.deco_aggregate_stale(ctx)
+        for ctx, h, mom in ((plain, good, m), (server, strided, m), (server, nest, m),
+                            (server, other, torch.zeros(d + 1, device="cuda"))):
+            with pytest.raises(B.DecoError) as e:
+                B.deco_apply_update_orth(ctx, h, mom)
+            assert e.value.status == B.DECO_ERR_INVALID_ARG
+        with pytest.raises(B.DecoError):
+            B.deco_apply_update_orth(server, good, m, weight_decay=-1.0)
+        with pytest.raises(ValueError):
+            B.deco_apply_update_orth(server, good, torch.zeros(d - 1, device="cuda"))
+        B.deco_apply_update_orth(server, good, m)                   # a refusal changed nothing
+        B.deco_apply_update(plain)
+    finally:
+        for h in (good, other, strided, nest):
+            B.deco_orth_destroy(h)
+        B.deco_destroy(plain)
+        B.deco_destroy(server)
+
+
+@gpu
+def test_run_refusals():
+    h = B.deco_orth_init(100, [(0, 10, 10)])
+    x, out = torch.zeros(100, device="cuda"), torch.zeros(100, device="cuda", dtype=torch.bfloat16)
+    try:
+        for bad in ((x.half(), out, None), (x, out.float(), None), (x[:99], out, None), (x.double(), out, None),
+                    (torch.zeros(200, device="cuda")[::2], out, None), (x, out, out), (x.cpu(), out, None)):
+            with pytest.raises(ValueError):
+                B.deco_orth_run(h, bad[0], bad[1], momentum=bad[2])
+        lib = B.load()
+        assert lib.deco_orth_run(h, x.data_ptr() + 2, B.DECO_F32, None, out.data_ptr(), None) == B.DECO_ERR_INVALID_ARG
+        assert lib.deco_orth_run(h, x.data_ptr(), 5, None, out.data_ptr(), None) == B.DECO_ERR_INVALID_ARG
+        assert lib.deco_orth_run(h, None, 0, None, out.data_ptr(), None) == B.DECO_ERR_INVALID_ARG
+        assert lib.deco_orth_run(None, x.data_ptr(), 0, None, out.data_ptr(), None) == B.DECO_ERR_INVALID_ARG
+    finally:
+        B.deco_orth_destroy(h)
+    empty = B.deco_orth_init(100, [])                               # no matrices: momentum alone
+    try:
+        m = torch.ones(100, device="cuda")
+        B.deco_orth_run(empty, x, out, momentum=m)
+        assert (m == 0).all() and (out == 0).all()
+    finally:
+        B.deco_orth_destroy(empty)
+
+
+@pytest.mark.parametrize("kw", [dict(steps=17), dict(eps=-1.0), dict(momentum=1.0), dict(momentum=-0.1), dict(scale=3),
+                                dict(scale=-1), dict(coef=(9.0, 0.0, 0.0)), dict(coef=(3.4445, -4.775, 9.0)),
+                                dict(coef=(math.nan, 0.0, 0.0)), dict(eps=math.nan)])
+def test_options_are_checked_on_the_host(kw):
+    with pytest.raises(B.DecoError) as e:
+        B.deco_orth_init(100, [(0, 10, 10)], **kw)
+    assert e.value.status == B.DECO_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("mats", [[(0, 0, 5)], [(0, 5, 0)], [(1, 10, 10)], [(0, 5, 5), (24, 5, 5)], [(0, 2, 5, 4)],
+                                  [(0, 4, 10, 20), (5, 4, 10, 20)], [(0, 4, 10, 20), (10, 3, 10, 21)],
+                                  [(0, 4, 10, 20), (30, 1, 5)], [(2 ** 63, 1, 1)]])
+def test_layouts_are_checked_on_the_host(mats):
+    with pytest.raises(B.DecoError) as e:
+        B.deco_orth_init(100, mats)
+    assert e.value.status == B.DECO_ERR_INVALID_ARG
+
+
+def test_init_without_a_device_fails_loudly():
+    if torch.cuda.is_available():
+        pytest.skip("a CUDA device is present")
+    with pytest.raises(B.DecoError) as e:
+        B.deco_orth_init(100, [(0, 10, 10)])
+    assert e.value.status == B.DECO_ERR_CUDA
