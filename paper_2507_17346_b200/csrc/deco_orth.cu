@@ -80,8 +80,9 @@ struct Tile {
 // Which operands of a matrix's products are carried as hi + lo.
 enum Precision { PLAIN = 0, WIDE_B = 1, FULL = 2 };
 constexpr uint32_t FULL_SIDE = 128, WIDE_B_SIDE = 256;
-// A matrix's tensor maps.
-enum Map { MAP_X = 0 /* hi, lo, next hi, next lo */, MAP_A = 4 /* hi, lo */, MAP_B = 6 /* hi, lo */, MAPS = 8 };
+// A matrix's tensor maps: boxes of 64 x 64 for the operands, and from BOX32 on the same with boxes of
+// 32 rows for the epilogue.
+enum Map { MAP_X = 0 /* hi, lo, next hi, next lo */, MAP_A = 4 /* hi, lo */, MAP_B = 6 /* hi, lo */, BOX32 = 8, MAPS = 16 };
 
 constexpr uint32_t NO_SLOT = 0xFFFFFFFFu;
 constexpr uint32_t PIECE = 16384;
@@ -174,6 +175,8 @@ template <typename T>
 __global__ void __launch_bounds__(INGEST_THREADS)
 convert_kernel(const ConvertPiece *pieces, const Mat *mats, const Source<T> src, const double *partial, float eps)
 {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const ConvertPiece p = pieces[blockIdx.x];
     const Mat &M = mats[p.mat];
     double sum = 0;
@@ -196,11 +199,16 @@ enum Phase { GRAM = 0, POLY = 1, APPLY = 2 };
 enum Target { NEXT_X = 0, OUT_BF16 = 1, PARAMS = 2 };
 
 constexpr int BK = 64;                   // k per stage: 128 bytes, one swizzle row
-constexpr int STAGES = 6;
+constexpr int STAGES = 5;
 constexpr uint32_t OPERAND_BYTES = 128 * BK * 2;
 constexpr uint32_t STAGE_BYTES = 2 * OPERAND_BYTES;
-constexpr int GEMM_THREADS = 256;        // warps 0: loads, 1: mma, 2: tensor memory, 4..7: epilogue
-constexpr int EPI_WARPS = 4;
+constexpr int FIRST_EPI_WARP = 4;        // warps 0: loads, 1: mma, 2: tensor memory
+constexpr int EPI_WARPS = 8;             // two per quarter of the tensor memory's lanes, each half of the columns
+constexpr int GEMM_THREADS = 32 * (FIRST_EPI_WARP + EPI_WARPS);
+constexpr int CHUNK = 64;                // columns an epilogue warp takes at a time
+constexpr uint32_t CHUNK_BYTES = 32 * CHUNK * 2;
+constexpr uint32_t STAGING_BYTES = 2 * CHUNK_BYTES;      // of a warp: hi and lo
+constexpr size_t GEMM_SMEM = STAGES * STAGE_BYTES + EPI_WARPS * STAGING_BYTES + 1024;
 
 struct GemmArgs {
     const Mat *mats;
@@ -218,12 +226,19 @@ struct GemmArgs {
 };
 
 struct __align__(8) Control {
-    uint64_t full[STAGES], empty[STAGES], acc_full[2], acc_empty[2];
+    uint64_t full[STAGES], empty[STAGES], acc_full[2], acc_empty[2], staged[EPI_WARPS];
     uint32_t tmem;
     volatile uint32_t abort;
 };
 
 __device__ __forceinline__ uint32_t smem_addr(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+// the same shared-memory address in CTA 0 of the pair
+__device__ __forceinline__ uint32_t leader_addr(uint32_t a)
+{
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(a));
+    return r;
+}
 
 __device__ __forceinline__ void bar_init(uint64_t *b, uint32_t count)
 {
@@ -233,15 +248,19 @@ __device__ __forceinline__ void bar_expect(uint64_t *b, uint32_t bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(smem_addr(b)), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void bar_arrive(uint64_t *b)
+template <int CG>
+__device__ __forceinline__ void bar_arrive_leader(uint64_t *b)
 {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(smem_addr(b)) : "memory");
+    if (CG == 1)
+        asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(smem_addr(b)) : "memory");
+    else
+        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(leader_addr(smem_addr(b))) : "memory");
 }
 __device__ __forceinline__ bool bar_try(uint64_t *b, uint32_t parity)
 {
     uint32_t ok;
     asm volatile("{\n\t.reg .pred p;\n\t"
-                 "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                 "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
                  "selp.u32 %0, 1, 0, p;\n\t}"
                  : "=r"(ok) : "r"(smem_addr(b)), "r"(parity) : "memory");
     return ok != 0;
@@ -271,20 +290,33 @@ __device__ __forceinline__ void map_acquire(const CUtensorMap *map)
 {
     asm volatile("fence.proxy.tensormap::generic.acquire.gpu [%0], 128;" :: "l"(map) : "memory");
 }
-__device__ __forceinline__ void load_box(void *dst, const CUtensorMap *map, int32_t x, int32_t y, uint64_t *bar)
+// Box at (x, y) into this CTA's shared memory; its bytes are counted by the barrier at `bar`, which
+// with CG = 2 is the leading CTA's.
+template <int CG>
+__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, uint32_t bar)
 {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                 :: "r"(smem_addr(dst)), "l"(map), "r"(x), "r"(y), "r"(smem_addr(bar)) : "memory");
+    if (CG == 1)
+        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                     :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];"
+                     :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void store_box(const CUtensorMap *map, int32_t x, int32_t y, uint32_t src)
+{
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];"
+                 :: "l"(map), "r"(x), "r"(y), "r"(src) : "memory");
 }
 
 // 128 entries of the operand's outer dimension (from mn) by BK of k, as two boxes of 64 x 64.
-__device__ __forceinline__ void load_operand(uint8_t *dst, const CUtensorMap *map, bool mn_major, int32_t mn, int32_t k,
-                                             uint64_t *bar)
+template <int CG>
+__device__ __forceinline__ void load_operand(uint32_t dst, const CUtensorMap *map, bool mn_major, int32_t mn, int32_t k,
+                                             uint32_t bar)
 {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int32_t o = mn + 64 * i;
-        load_box(dst + i * (OPERAND_BYTES / 2), map, mn_major ? o : k, mn_major ? k : o, bar);
+        load_box<CG>(dst + i * (OPERAND_BYTES / 2), map, mn_major ? o : k, mn_major ? k : o, bar);
     }
 }
 
@@ -301,16 +333,28 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t addr, bool mn_major)
     return d;
 }
 
+template <int CG>
 __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    if (CG == 1)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
+// Arrive at the barrier (with CG = 2: in both CTAs) once the products issued so far are done.
+template <int CG>
 __device__ __forceinline__ void mma_commit(uint64_t *bar)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];"
-                 :: "r"(smem_addr(bar)) : "memory");
+    if (CG == 1)
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];"
+                     :: "r"(smem_addr(bar)) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                     :: "r"(smem_addr(bar)), "h"(static_cast<uint16_t>(3)) : "memory");
 }
 __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&v)[32])
 {
@@ -325,8 +369,22 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&v)[32])
                  : "r"(addr));
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
-
-constexpr int TILE_MN = 128;
+__device__ __forceinline__ uint4 lds16(uint32_t a)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ void sts16(uint32_t a, uint4 v)
+{
+    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ float2 half2_at(const uint4 &v, int i)
+{
+    const uint32_t w = i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
+    return __half22float2(*reinterpret_cast<const __half2 *>(&w));
+}
+template <typename H2> __device__ __forceinline__ uint32_t bits(H2 h) { return *reinterpret_cast<const uint32_t *>(&h); }
 
 // What a tile of a phase reads: the sum over `passes` pairs of operands, pair i being
 // (a + lo of a if i is in a_lo, b + lo of b if i is in b_lo), over k in [0, k) each.
@@ -352,15 +410,27 @@ __device__ __forceinline__ Operands operands(const GemmArgs &g, const Mat &M, ui
     return {bm, x, false, true, M.m, passes, 2, 4};
 }
 
-// One 128 x 128 tile at a time per CTA; the epilogue of a tile runs beside the products of the next.
-template <Phase P, Target T>
+// A CTA (CG = 1: tiles of 128 x 128) or a pair of CTAs (CG = 2: 256 x 256, each CTA half of the rows of
+// the tile and of either operand) works through the tiles; the epilogue of a tile runs beside
+// the products of the next.
+//
+// Epilogue.  A warp takes 32 rows by 64 columns at a time.  What the formula adds to the product (X, or A)
+// comes as a box into the warp's own staging memory, loaded while the tile's products still run;
+// a thread owns a row there, as in tensor memory, and puts the result in the place of the input;
+// a box store writes it back.  Rows lie 128 bytes apart in the staging memory with their 16-byte units
+// permuted as the box copies do it, so the row-wise accesses meet no bank conflicts.
+template <int CG, Phase P, Target T>
 __global__ void __launch_bounds__(GEMM_THREADS, 1)
 gemm_kernel(const GemmArgs g)
 {
+    constexpr int SIDE = 128 * CG;
     extern __shared__ uint8_t raw[];
-    uint8_t *stages = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
     __shared__ Control ctl;
+    const uint32_t stages = (smem_addr(raw) + 1023) & ~1023u;
     const int wid = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint32_t rank = 0;
+    if (CG == 2) asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    const uint32_t first = blockIdx.x / CG, step = gridDim.x / CG;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
@@ -369,28 +439,43 @@ gemm_kernel(const GemmArgs g)
         }
         for (int s = 0; s < 2; ++s) {
             bar_init(&ctl.acc_full[s], 1);
-            bar_init(&ctl.acc_empty[s], EPI_WARPS);
+            bar_init(&ctl.acc_empty[s], EPI_WARPS * CG);
         }
+        for (int w = 0; w < EPI_WARPS; ++w) bar_init(&ctl.staged[w], 1);
         ctl.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (wid == 2) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
-                     :: "r"(smem_addr(&ctl.tmem)), "r"(2 * TILE_MN) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        if (CG == 1) {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                         :: "r"(smem_addr(&ctl.tmem)), "r"(2 * SIDE) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;"
+                         :: "r"(smem_addr(&ctl.tmem)), "r"(2 * SIDE) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+        }
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    if (CG == 2) {
+        asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    }
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = ctl.tmem;
+    // what comes before is done while the launch before this one ends; its results are read from here on
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     if (wid == 0) {
         if (lane == 0) {
             uint32_t it = 0, seen = 0xFFFFFFFFu;
             bool ok = true;
-            for (uint32_t t = blockIdx.x; ok && t < g.n_tiles; t += gridDim.x) {
+            for (uint32_t t = first; ok && t < g.n_tiles; t += step) {
                 const Tile tl = g.tiles[t];
                 const Operands op = operands<P>(g, g.mats[tl.mat], tl.mat);
+                const int32_t ra = tl.tm * SIDE + rank * 128, rb = tl.tn * SIDE + rank * 128;
                 for (uint32_t pass = 0; ok && pass < op.passes; ++pass) {
                     const CUtensorMap *ma = op.map_a(pass), *mb = op.map_b(pass);
                     if (tl.mat != seen) {                        // an earlier handle's maps may have lain here
@@ -400,25 +485,27 @@ gemm_kernel(const GemmArgs g)
                     for (uint32_t k = 0; k < op.k; k += BK, ++it) {
                         const uint32_t s = it % STAGES;
                         if (!bar_wait(&ctl.empty[s], ((it / STAGES) & 1) ^ 1, &ctl, g.status)) { ok = false; break; }
-                        bar_expect(&ctl.full[s], STAGE_BYTES);
-                        uint8_t *st = stages + s * STAGE_BYTES;
-                        load_operand(st, ma, op.a_mn, tl.tm * TILE_MN, k, &ctl.full[s]);
-                        load_operand(st + OPERAND_BYTES, mb, op.b_mn, tl.tn * TILE_MN, k, &ctl.full[s]);
+                        if (rank == 0) bar_expect(&ctl.full[s], CG * STAGE_BYTES);
+                        const uint32_t bar = CG == 1 ? smem_addr(&ctl.full[s]) : leader_addr(smem_addr(&ctl.full[s]));
+                        const uint32_t st = stages + s * STAGE_BYTES;
+                        load_operand<CG>(st, ma, op.a_mn, ra, k, bar);
+                        load_operand<CG>(st + OPERAND_BYTES, mb, op.b_mn, rb, k, bar);
                     }
                 }
                 seen = tl.mat;
             }
-            // copies in flight land before the CTA leaves
-            for (uint32_t i = it > STAGES ? it - STAGES : 0; i < it; ++i) {
+            // Every copy has landed before a CTA leaves: in the normal course the products and so the
+            // epilogue have waited for all of them; after a wait that ran out they get some time here.
+            if (ctl.abort) {
                 const long long t0 = clock64();
-                while (!bar_try(&ctl.full[i % STAGES], (i / STAGES) & 1) && clock64() - t0 < 1000000000ll) {}
+                while (clock64() - t0 < 20000000ll) {}
             }
         }
     } else if (wid == 1) {
-        if (lane == 0) {
+        if (lane == 0 && rank == 0) {
             uint32_t it = 0, n = 0;
             bool ok = true;
-            for (uint32_t t = blockIdx.x; ok && t < g.n_tiles; t += gridDim.x, ++n) {
+            for (uint32_t t = first; ok && t < g.n_tiles; t += step, ++n) {
                 const Tile tl = g.tiles[t];
                 const Operands op = operands<P>(g, g.mats[tl.mat], tl.mat);
                 const uint32_t as = n & 1;
@@ -426,125 +513,205 @@ gemm_kernel(const GemmArgs g)
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 // fp16 operands, fp32 sums, N and M, which dimension is consecutive
                 const uint32_t idesc = (1u << 4) | (static_cast<uint32_t>(op.a_mn) << 15) |
-                                       (static_cast<uint32_t>(op.b_mn) << 16) | ((TILE_MN >> 3) << 17) |
-                                       ((TILE_MN >> 4) << 24);
+                                       (static_cast<uint32_t>(op.b_mn) << 16) | ((SIDE >> 3) << 17) | ((SIDE >> 4) << 24);
+                const uint32_t sa = op.a_mn ? 2048 >> 4 : 32 >> 4, sb = op.b_mn ? 2048 >> 4 : 32 >> 4;
                 const uint32_t blocks = op.passes * ((op.k + BK - 1) / BK);
                 for (uint32_t k = 0; k < blocks; ++k, ++it) {
                     const uint32_t s = it % STAGES;
                     if (!bar_wait(&ctl.full[s], (it / STAGES) & 1, &ctl, g.status)) { ok = false; break; }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t st = smem_addr(stages + s * STAGE_BYTES);
+                    const uint32_t st = stages + s * STAGE_BYTES;
                     const uint64_t da = operand_desc(st, op.a_mn), db = operand_desc(st + OPERAND_BYTES, op.b_mn);
-                    const uint32_t sa = op.a_mn ? 2048 >> 4 : 32 >> 4, sb = op.b_mn ? 2048 >> 4 : 32 >> 4;
 #pragma unroll
                     for (uint32_t q = 0; q < BK / 16; ++q)
-                        mma(tmem + as * TILE_MN, da + q * sa, db + q * sb, idesc, (k | q) != 0);
-                    mma_commit(&ctl.empty[s]);
+                        mma<CG>(tmem + as * SIDE, da + q * sa, db + q * sb, idesc, (k | q) != 0);
+                    mma_commit<CG>(&ctl.empty[s]);
                 }
-                if (ok) mma_commit(&ctl.acc_full[as]);
+                if (ok) mma_commit<CG>(&ctl.acc_full[as]);
             }
         }
-    } else if (wid >= 4) {
-        const int quad = wid & 3;
-        uint32_t n = 0;
-        for (uint32_t t = blockIdx.x; t < g.n_tiles; t += gridDim.x, ++n) {
+    } else if (wid >= FIRST_EPI_WARP) {
+        const int ew = wid - FIRST_EPI_WARP, quad = wid & 3, side = ew >> 2;
+        const uint32_t hi_buf = stages + STAGES * STAGE_BYTES + ew * STAGING_BYTES, lo_buf = hi_buf + CHUNK_BYTES;
+        const uint32_t my_row = lane * 128, perm = lane & 7;
+        constexpr uint32_t CHUNKS = SIDE / 2 / CHUNK;            // of this warp, per tile
+        uint32_t n = 0, loads = 0;
+        bool ok = true;
+        for (uint32_t t = first; ok && t < g.n_tiles; t += step, ++n) {
             const Tile tl = g.tiles[t];
             const Mat &M = g.mats[tl.mat];
             const uint32_t as = n & 1;
-            if (!bar_wait(&ctl.acc_full[as], (n >> 1) & 1, &ctl, g.status)) break;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t rows = P == APPLY ? M.rows : M.m, cols = P == APPLY ? M.cols : M.m;
-            const uint32_t r = tl.tm * TILE_MN + quad * 32 + lane;
+            const uint32_t r0 = tl.tm * SIDE + rank * 128 + quad * 32, r = r0 + lane;
+            const uint32_t c_first = tl.tn * SIDE + side * (SIDE / 2);
+            const bool full = M.precision == FULL;
+            const bool in_lo = P == POLY ? full : P == APPLY ? g.read_lo || full : false;
+            const bool out_lo = P == GRAM ? full : P == POLY ? M.precision != PLAIN : g.write_lo || full;
+            const bool live = r0 < rows;
+            const CUtensorMap *maps = g.maps + static_cast<uint64_t>(tl.mat) * MAPS + BOX32;
+            const CUtensorMap *in_map = maps + (P == POLY ? MAP_A : MAP_X + 2 * g.src);
+            const CUtensorMap *out_map = maps + (P == GRAM ? MAP_A : P == POLY ? MAP_B : MAP_X + 2 * (g.src ^ 1));
+            const uint32_t chunks = !live || c_first >= cols ? 0 : min(CHUNKS, (cols - c_first + CHUNK - 1) / CHUNK);
+            auto fetch = [&](uint32_t c0) {                      // lane 0: the chunk's input, once the staging memory is free
+                asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                bar_expect(&ctl.staged[ew], in_lo ? 2 * CHUNK_BYTES : CHUNK_BYTES);
+                const uint32_t bar = smem_addr(&ctl.staged[ew]);
+                load_box<1>(hi_buf, in_map, c0, r0, bar);
+                if (in_lo) load_box<1>(lo_buf, in_map + 1, c0, r0, bar);
+            };
+            if (P != GRAM && chunks && lane == 0) fetch(c_first);
+            ok = bar_wait(&ctl.acc_full[as], (n >> 1) & 1, &ctl, g.status);
+            if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
-            for (uint32_t cb = 0; cb < TILE_MN; cb += 32) {
-                uint32_t v[32];
-                __syncwarp();
-                tmem_load32(tmem + (static_cast<uint32_t>(quad * 32) << 16) + as * TILE_MN + cb, v);
-                const uint32_t c0 = tl.tn * TILE_MN + cb;
-                if (r >= rows || c0 >= cols) continue;
-                const uint32_t count = min(32u, cols - c0);
-                if (P != APPLY) {
-                    __half *dst = P == GRAM ? M.a : M.b;
-                    __half *dst_lo = P == GRAM ? M.a_lo : M.b_lo;
-                    __half y[32], yl[32];
-                    const uint64_t at = static_cast<uint64_t>(r) * M.lda + c0;
-#pragma unroll
-                    for (uint32_t j0 = 0; j0 < 32; j0 += 8) {
-                        if (j0 >= count) break;
-                        uint4 old = make_uint4(0, 0, 0, 0), old_lo = old;
-                        if (P == POLY) old = *reinterpret_cast<const uint4 *>(M.a + at + j0);
-                        if (P == POLY && M.precision == FULL) old_lo = *reinterpret_cast<const uint4 *>(M.a_lo + at + j0);
-                        const __half *o = reinterpret_cast<const __half *>(&old), *ol = reinterpret_cast<const __half *>(&old_lo);
-#pragma unroll
-                        for (uint32_t j = 0; j < 8; ++j) {
-                            const float acc = __uint_as_float(v[j0 + j]) * INV_SCALE;
-                            const float x = P == GRAM ? acc
-                                                      : __fmaf_rn(g.c, acc, g.b * (__half2float(o[j]) + __half2float(ol[j])));
-                            y[j0 + j] = __float2half_rn(x);
-                            yl[j0 + j] = __float2half_rn(x - __half2float(y[j0 + j]));
-                        }
-                        *reinterpret_cast<uint4 *>(dst + at + j0) = *reinterpret_cast<uint4 *>(y + j0);
-                        if (dst_lo) *reinterpret_cast<uint4 *>(dst_lo + at + j0) = *reinterpret_cast<uint4 *>(yl + j0);
-                    }
-                    if (tl.tm != tl.tn)                          // the block's mirror image
-#pragma unroll
-                        for (uint32_t j = 0; j < 32; ++j)
-                            if (j < count) {
-                                const uint64_t mirror = static_cast<uint64_t>(c0 + j) * M.lda + r;
-                                dst[mirror] = y[j];
-                                if (dst_lo) dst_lo[mirror] = yl[j];
-                            }
+            for (uint32_t ch = 0; ch < chunks; ++ch) {
+                const uint32_t c0 = c_first + ch * CHUNK;
+                if (P != GRAM) {
+                    if (ch && lane == 0) fetch(c0);
+                    ok = bar_wait(&ctl.staged[ew], loads & 1, &ctl, g.status);
+                    if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
+                    loads += 1;
                 } else {
-                    const uint64_t at = static_cast<uint64_t>(r) * M.ldx + c0;
-                    const uint64_t flat = M.offset + r * M.stride + c0;
+                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                    __syncwarp();
+                }
 #pragma unroll
-                    for (uint32_t j0 = 0; j0 < 32; j0 += 8) {
-                        if (j0 >= count) break;
-                        const uint4 h4 = *reinterpret_cast<const uint4 *>(M.hi[g.src] + at + j0);
-                        uint4 l4 = make_uint4(0, 0, 0, 0);
-                        if (g.read_lo || M.precision == FULL) l4 = *reinterpret_cast<const uint4 *>(M.lo[g.src] + at + j0);
-                        const __half *h = reinterpret_cast<const __half *>(&h4), *l = reinterpret_cast<const __half *>(&l4);
+                for (uint32_t h = 0; h < 2; ++h) {
+                    uint32_t v[32];
+                    tmem_load32(tmem + (static_cast<uint32_t>(quad * 32) << 16) + as * SIDE + side * (SIDE / 2) + ch * CHUNK + h * 32, v);
+#pragma unroll
+                    for (uint32_t u = 0; u < 4; ++u) {
+                        const uint32_t at = my_row + (((h * 4 + u) ^ perm) << 4);
+                        uint4 ih = make_uint4(0, 0, 0, 0), il = ih;
+                        if (P != GRAM) ih = lds16(hi_buf + at);
+                        if (P != GRAM && in_lo) il = lds16(lo_buf + at);
                         float x[8];
 #pragma unroll
-                        for (uint32_t j = 0; j < 8; ++j)
-                            x[j] = __fmaf_rn(g.a, __half2float(h[j]) + __half2float(l[j]),
-                                             __uint_as_float(v[j0 + j]) * INV_SCALE);
-                        if (T == NEXT_X) {
-                            __half nh[8], nl[8];
+                        for (int i = 0; i < 4; ++i) {
+                            const float2 a = half2_at(ih, i), b = half2_at(il, i);
 #pragma unroll
-                            for (uint32_t j = 0; j < 8; ++j) {
-                                nh[j] = __float2half_rn(x[j]);
-                                nl[j] = __float2half_rn(x[j] - __half2float(nh[j]));
-                            }
-                            *reinterpret_cast<uint4 *>(M.hi[g.src ^ 1] + at + j0) = *reinterpret_cast<uint4 *>(nh);
-                            if (g.write_lo || M.precision == FULL)
-                                *reinterpret_cast<uint4 *>(M.lo[g.src ^ 1] + at + j0) = *reinterpret_cast<uint4 *>(nl);
-                        } else {
-                            const float s = M.scale * INV_SCALE;
-#pragma unroll
-                            for (uint32_t j = 0; j < 8; ++j) {
-                                if (j0 + j >= count) break;
-                                const uint64_t q = flat + j0 + j;
-                                if (T == OUT_BF16) g.out[q] = __float2bfloat16_rn(s * x[j]);
-                                else g.params[q] = __fmaf_rn(-g.lr, s * x[j], g.decay * g.params[q]);
+                            for (int j = 0; j < 2; ++j) {
+                                const float acc = __uint_as_float(v[u * 8 + 2 * i + j]) * INV_SCALE;
+                                const float in = j ? a.y + b.y : a.x + b.x;
+                                x[2 * i + j] = P == GRAM ? acc : P == POLY ? __fmaf_rn(g.c, acc, g.b * in) : __fmaf_rn(g.a, in, acc);
                             }
                         }
+                        if (T == NEXT_X) {
+                            uint32_t oh[4], ol[4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const __half2 hh = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
+                                const float2 back = __half22float2(hh);
+                                oh[i] = bits(hh);
+                                ol[i] = bits(__floats2half2_rn(x[2 * i] - back.x, x[2 * i + 1] - back.y));
+                            }
+                            sts16(hi_buf + at, make_uint4(oh[0], oh[1], oh[2], oh[3]));
+                            if (out_lo) sts16(lo_buf + at, make_uint4(ol[0], ol[1], ol[2], ol[3]));
+                            if (P != APPLY && tl.tm != tl.tn && r < rows) {     // the block's mirror image
+                                unsigned short *m = reinterpret_cast<unsigned short *>(P == GRAM ? M.a : M.b);
+                                unsigned short *ml = reinterpret_cast<unsigned short *>(P == GRAM ? M.a_lo : M.b_lo);
+#pragma unroll
+                                for (uint32_t j = 0; j < 8; ++j) {
+                                    const uint32_t c = c0 + h * 32 + u * 8 + j;
+                                    if (c < cols) {
+                                        m[static_cast<uint64_t>(c) * M.lda + r] = static_cast<unsigned short>(oh[j >> 1] >> (16 * (j & 1)));
+                                        if (out_lo) ml[static_cast<uint64_t>(c) * M.lda + r] = static_cast<unsigned short>(ol[j >> 1] >> (16 * (j & 1)));
+                                    }
+                                }
+                            }
+                        } else if (T == OUT_BF16) {
+                            const float s = M.scale * INV_SCALE;
+                            uint32_t o[4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) o[i] = bits(__floats2bfloat162_rn(s * x[2 * i], s * x[2 * i + 1]));
+                            sts16(hi_buf + at, make_uint4(o[0], o[1], o[2], o[3]));
+                        } else {
+                            const float s = M.scale * INV_SCALE;
+                            uint32_t o[8];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(s * x[i]);
+                            sts16(hi_buf + at, make_uint4(o[0], o[1], o[2], o[3]));
+                            sts16(lo_buf + at, make_uint4(o[4], o[5], o[6], o[7]));
+                        }
                     }
+                }
+                if (T == NEXT_X) {
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {
+                        store_box(out_map, c0, r0, hi_buf);
+                        if (out_lo) store_box(out_map + 1, c0, r0, lo_buf);
+                        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    }
+                } else if (T == OUT_BF16) {
+                    // rows of the flat vector: 8 lanes write 128 bytes of one, whatever its alignment allows
+                    __syncwarp();
+                    __nv_bfloat16 *base = g.out + M.offset + c0;
+                    const bool wide = ((reinterpret_cast<uintptr_t>(base) & 15u) | (M.stride & 7u)) == 0;
+#pragma unroll
+                    for (uint32_t i = 0; i < 8; ++i) {
+                        const uint32_t rr = i * 4 + (lane >> 3), q = lane & 7;
+                        if (r0 + rr >= rows || c0 + q * 8 >= cols) continue;
+                        const uint4 o = lds16(hi_buf + rr * 128 + ((q ^ (rr & 7)) << 4));
+                        __nv_bfloat16 *p = base + (r0 + rr) * M.stride + q * 8;
+                        if (wide && c0 + q * 8 + 8 <= cols) {
+                            *reinterpret_cast<uint4 *>(p) = o;
+                        } else {
+                            const uint32_t w[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+                            for (uint32_t j = 0; j < 8; ++j)
+                                if (c0 + q * 8 + j < cols)
+                                    reinterpret_cast<unsigned short *>(p)[j] = static_cast<unsigned short>(w[j >> 1] >> (16 * (j & 1)));
+                        }
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                } else {
+                    __syncwarp();
+                    float *base = g.params + M.offset + c0;
+                    const bool wide = ((reinterpret_cast<uintptr_t>(base) & 15u) | (M.stride & 3u)) == 0;
+#pragma unroll 4
+                    for (uint32_t i = 0; i < 16; ++i) {
+                        const uint32_t rr = i * 2 + (lane >> 4), q = lane & 15;
+                        if (r0 + rr >= rows || c0 + q * 4 >= cols) continue;
+                        const uint4 o = lds16((q & 1 ? lo_buf : hi_buf) + rr * 128 + (((q >> 1) ^ (rr & 7)) << 4));
+                        const float y[4] = {__uint_as_float(o.x), __uint_as_float(o.y), __uint_as_float(o.z), __uint_as_float(o.w)};
+                        float *p = base + (r0 + rr) * M.stride + q * 4;
+                        if (wide && c0 + q * 4 + 4 <= cols) {
+                            float4 x = *reinterpret_cast<float4 *>(p);
+                            x.x = __fmaf_rn(-g.lr, y[0], g.decay * x.x);
+                            x.y = __fmaf_rn(-g.lr, y[1], g.decay * x.y);
+                            x.z = __fmaf_rn(-g.lr, y[2], g.decay * x.z);
+                            x.w = __fmaf_rn(-g.lr, y[3], g.decay * x.w);
+                            *reinterpret_cast<float4 *>(p) = x;
+                        } else {
+#pragma unroll
+                            for (uint32_t j = 0; j < 4; ++j)
+                                if (c0 + q * 4 + j < cols) p[j] = __fmaf_rn(-g.lr, y[j], g.decay * p[j]);
+                        }
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
                 }
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
-            if (lane == 0) bar_arrive(&ctl.acc_empty[as]);
+            if (lane == 0) bar_arrive_leader<CG>(&ctl.acc_empty[as]);
         }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
-    if (wid == 2)
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(2 * TILE_MN));
+    if (CG == 2) {
+        asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    }
+    if (wid == 2) {
+        if (CG == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(2 * SIDE));
+        else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(2 * SIDE));
+    }
 }
-
-constexpr size_t GEMM_SMEM = STAGES * STAGE_BYTES + 1024;
 
 // ------------------------------------------------------------------- server update's own parts
 
@@ -586,9 +753,13 @@ rest_kernel(const Piece *pieces, float *params, const float *m, float lr, float 
 
 // ------------------------------------------------------------------------------------- host
 
+// The tiles of a phase: where in the handle's list, how many, and by one CTA or a pair of them.
+struct Span {
+    uint32_t first, count, cg;
+};
 struct Group {
-    uint32_t convert0, n_convert;        // in the handle's lists
-    uint32_t gram0, n_gram, poly0, apply0, n_apply;
+    uint32_t convert0, n_convert;        // in the handle's list
+    Span phase[3];                       // GRAM, POLY, APPLY
 };
 
 struct DeviceGuard {
@@ -618,11 +789,12 @@ EncodeFn encode_function()
     return reinterpret_cast<EncodeFn>(fn);
 }
 
-// A row-major fp16 matrix, read in 64 x 64 boxes; outside of it zeros are read.
-bool encode(EncodeFn fn, CUtensorMap *map, void *base, uint64_t rows, uint64_t cols, uint64_t ld)
+// A row-major fp16 matrix in boxes of 64 columns; outside of it zeros are read and nothing is written.
+bool encode(EncodeFn fn, CUtensorMap *map, void *base, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t box_rows = 64)
 {
     const cuuint64_t dims[2] = {cols, rows}, strides[1] = {ld * 2};
-    const cuuint32_t box[2] = {64, 64}, step[2] = {1, 1};
+    const cuuint32_t box[2] = {64, box_rows}, step[2] = {1, 1};
+    if (box_rows == 64 && !encode(fn, map + BOX32, base, rows, cols, ld, 32)) return false;
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, base, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -753,6 +925,12 @@ bool layout_ok(uint64_t d, const std::vector<deco_matrix> &ms)
     return true;
 }
 
+uint32_t passes(const Mat &M, int phase) { return phase == APPLY ? 1 + M.precision : M.precision == FULL ? 3 : 1; }
+
+// Clock cycles of a tile of k products deep: 4096 multiply-adds per SM and cycle, of which tiles of one
+// CTA reach less (they read twice the shared memory per product), and the ends that do not overlap.
+double tile_cost(uint32_t cg, uint32_t k) { return cg == 1 ? 5.2 * k + 1500 : 8.4 * k + 2500; }
+
 deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, uint64_t cap)
 {
     const EncodeFn enc = encode_function();
@@ -868,25 +1046,37 @@ deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, ui
             }
         }
         G.n_convert = static_cast<uint32_t>(convert.size()) - G.convert0;
-        auto blocks = [](uint32_t v) { return (v + TILE_MN - 1) / TILE_MN; };
-        auto symmetric = [&]() {
-            for (uint32_t i : by)
-                for (uint32_t r = 0; r < blocks(mats[i].m); ++r)
-                    for (uint32_t c = 0; c <= r; ++c) tiles.push_back({i, static_cast<uint16_t>(r), static_cast<uint16_t>(c)});
-        };
-        std::stable_sort(by.begin(), by.end(), [&](uint32_t x, uint32_t y) { return mats[x].n > mats[y].n; });
-        G.gram0 = static_cast<uint32_t>(tiles.size());
-        symmetric();
-        G.n_gram = static_cast<uint32_t>(tiles.size()) - G.gram0;
-        std::stable_sort(by.begin(), by.end(), [&](uint32_t x, uint32_t y) { return mats[x].m > mats[y].m; });
-        G.poly0 = static_cast<uint32_t>(tiles.size());
-        symmetric();
-        G.apply0 = static_cast<uint32_t>(tiles.size());
-        for (uint32_t i : by)
-            for (uint32_t r = 0; r < blocks(mats[i].rows); ++r)
-                for (uint32_t c = 0; c < blocks(mats[i].cols); ++c)
-                    tiles.push_back({i, static_cast<uint16_t>(r), static_cast<uint16_t>(c)});
-        G.n_apply = static_cast<uint32_t>(tiles.size()) - G.apply0;
+        for (int phase = 0; phase < 3; ++phase) {
+            // longest products first, and the tile size under which the busiest CTA is done first
+            auto depth = [&](uint32_t i) { return (phase == GRAM ? mats[i].n : mats[i].m) * passes(mats[i], phase); };
+            std::stable_sort(by.begin(), by.end(), [&](uint32_t x, uint32_t y) { return depth(x) > depth(y); });
+            double best = 0;
+            std::vector<Tile> chosen;
+            for (uint32_t cg = 1; cg <= 2; ++cg) {
+                const uint32_t side = 128 * cg;
+                auto blocks = [&](uint32_t v) { return (v + side - 1) / side; };
+                std::vector<Tile> list;
+                std::vector<double> busy(h->sms / cg, 0.0);
+                for (uint32_t i : by) {
+                    const Mat &M = mats[i];
+                    const uint32_t nr = blocks(phase == APPLY ? M.rows : M.m), nc = blocks(phase == APPLY ? M.cols : M.m);
+                    for (uint32_t r = 0; r < nr; ++r)
+                        for (uint32_t c = 0; c < (phase == APPLY ? nc : r + 1); ++c) {
+                            busy[list.size() % busy.size()] += tile_cost(cg, depth(i));
+                            list.push_back({i, static_cast<uint16_t>(r), static_cast<uint16_t>(c)});
+                        }
+                }
+                const double cost = *std::max_element(busy.begin(), busy.end());
+                if (cg == 1 || cost < best) {
+                    best = cost;
+                    chosen.swap(list);
+                    G.phase[phase].cg = cg;
+                }
+            }
+            G.phase[phase].first = static_cast<uint32_t>(tiles.size());
+            G.phase[phase].count = static_cast<uint32_t>(chosen.size());
+            tiles.insert(tiles.end(), chosen.begin(), chosen.end());
+        }
         h->groups.push_back(G);
         i0 = i1;
     }
@@ -900,22 +1090,45 @@ deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, ui
     return cudaDeviceSynchronize() == cudaSuccess ? DECO_OK : DECO_ERR_CUDA;
 }
 
-template <Phase P, Target T>
-cudaError_t launch_gemm(deco_orth *h, GemmArgs &g, uint32_t first, uint32_t count, cudaStream_t s)
+// Launched so that its start may overlap the end of the launch before it (the kernels wait for its results).
+template <typename... A>
+cudaError_t launch_after(deco_orth *h, void (*kernel)(A...), uint32_t grid, uint32_t threads, size_t smem, uint32_t cluster,
+                         cudaStream_t s, A... args)
 {
-    g.tiles = h->tiles + first;
-    g.n_tiles = count;
-    const uint32_t grid = std::min(count, h->sms);
-    gemm_kernel<P, T><<<grid, GEMM_THREADS, GEMM_SMEM, s>>>(g);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = cluster;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     h->launches += 1;
-    return cudaGetLastError();
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
 template <Phase P, Target T>
-cudaError_t allow_smem()
+cudaError_t launch_gemm(deco_orth *h, GemmArgs g, const Span &span, cudaStream_t s)
 {
-    return cudaFuncSetAttribute(gemm_kernel<P, T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                static_cast<int>(GEMM_SMEM));
+    g.tiles = h->tiles + span.first;
+    g.n_tiles = span.count;
+    const uint32_t grid = std::min(span.count, h->sms / span.cg) * span.cg;
+    return span.cg == 1 ? launch_after(h, gemm_kernel<1, P, T>, grid, GEMM_THREADS, GEMM_SMEM, 1, s, g)
+                        : launch_after(h, gemm_kernel<2, P, T>, grid, GEMM_THREADS, GEMM_SMEM, 2, s, g);
+}
+
+template <Phase P, Target T>
+bool allow_smem()
+{
+    return cudaFuncSetAttribute(gemm_kernel<1, P, T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                static_cast<int>(GEMM_SMEM)) == cudaSuccess &&
+           cudaFuncSetAttribute(gemm_kernel<2, P, T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                static_cast<int>(GEMM_SMEM)) == cudaSuccess;
 }
 
 // The whole pass over what `src` describes; params: the server update's target instead of out.
@@ -935,9 +1148,9 @@ cudaError_t run_pass(deco_orth *h, const Source<T> &src, __nv_bfloat16 *out, flo
     cudaError_t err = cudaGetLastError();
     for (const Group &G : h->groups) {
         if (err != cudaSuccess) return err;
-        convert_kernel<T><<<G.n_convert, INGEST_THREADS, 0, s>>>(h->convert + G.convert0, h->mats, src, h->partial, h->eps);
-        h->launches += 1;
-        err = cudaGetLastError();
+        err = launch_after(h, convert_kernel<T>, G.n_convert, INGEST_THREADS, 0, 1, s,
+                           static_cast<const ConvertPiece *>(h->convert + G.convert0), static_cast<const Mat *>(h->mats),
+                           src, static_cast<const double *>(h->partial), h->eps);
         GemmArgs g = {};
         g.mats = h->mats;
         g.maps = h->maps;
@@ -954,12 +1167,12 @@ cudaError_t run_pass(deco_orth *h, const Source<T> &src, __nv_bfloat16 *out, flo
             g.a = h->coef[3 * i];
             g.b = h->coef[3 * i + 1];
             g.c = h->coef[3 * i + 2];
-            err = launch_gemm<GRAM, NEXT_X>(h, g, G.gram0, G.n_gram, s);
-            if (err == cudaSuccess) err = launch_gemm<POLY, NEXT_X>(h, g, G.poly0, G.n_gram, s);
+            err = launch_gemm<GRAM, NEXT_X>(h, g, G.phase[GRAM], s);
+            if (err == cudaSuccess) err = launch_gemm<POLY, NEXT_X>(h, g, G.phase[POLY], s);
             if (err != cudaSuccess) break;
-            err = !last    ? launch_gemm<APPLY, NEXT_X>(h, g, G.apply0, G.n_apply, s)
-                : params   ? launch_gemm<APPLY, PARAMS>(h, g, G.apply0, G.n_apply, s)
-                           : launch_gemm<APPLY, OUT_BF16>(h, g, G.apply0, G.n_apply, s);
+            err = !last    ? launch_gemm<APPLY, NEXT_X>(h, g, G.phase[APPLY], s)
+                : params   ? launch_gemm<APPLY, PARAMS>(h, g, G.phase[APPLY], s)
+                           : launch_gemm<APPLY, OUT_BF16>(h, g, G.phase[APPLY], s);
         }
     }
     return err;
@@ -991,9 +1204,8 @@ try {
     if (!guard.ok) return DECO_ERR_CUDA;
     int sms = 0;
     if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, o.device) != cudaSuccess) return DECO_ERR_CUDA;
-    if (allow_smem<GRAM, NEXT_X>() != cudaSuccess || allow_smem<POLY, NEXT_X>() != cudaSuccess ||
-        allow_smem<APPLY, NEXT_X>() != cudaSuccess || allow_smem<APPLY, OUT_BF16>() != cudaSuccess ||
-        allow_smem<APPLY, PARAMS>() != cudaSuccess)
+    if (!allow_smem<GRAM, NEXT_X>() || !allow_smem<POLY, NEXT_X>() || !allow_smem<APPLY, NEXT_X>() ||
+        !allow_smem<APPLY, OUT_BF16>() || !allow_smem<APPLY, PARAMS>())
         return DECO_ERR_CUDA;
     deco_orth *h = new deco_orth;
     deco_status st = DECO_ERR_OOM;
