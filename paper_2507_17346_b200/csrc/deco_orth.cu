@@ -54,6 +54,7 @@ struct Mat {
     uint32_t m, n;                       // short and long side
     uint32_t tall;                       // rows > cols
     uint32_t precision;                  // see Precision
+    uint32_t spread;                     // rows not back to back
     uint32_t piece0, pieces;             // partial sums of squares
     float scale;                         // s of deco_orth_scale
 };
@@ -267,23 +268,23 @@ __device__ __forceinline__ bool bar_try(uint64_t *b, uint32_t parity)
 }
 // Bounded wait: false once the limit has passed or another role has given up; the first to give
 // up leaves DECO_ERR_TIMEOUT in the status word.
-__device__ __noinline__ bool bar_wait_slow(uint64_t *b, uint32_t parity, Control *ctl, uint32_t *status)
+__device__ __noinline__ bool bar_wait_slow(uint64_t *b, uint32_t parity, volatile uint32_t *abort, uint32_t *status)
 {
     constexpr long long LIMIT = 4000000000ll;                    // clock cycles: about 2 s
     const long long t0 = clock64();
     while (!bar_try(b, parity)) {
-        if (ctl->abort) return false;
+        if (*abort) return false;
         if (clock64() - t0 > LIMIT) {
-            ctl->abort = 1;
+            *abort = 1;
             atomicExch(status, static_cast<uint32_t>(DECO_ERR_TIMEOUT));
             return false;
         }
     }
     return true;
 }
-__device__ __forceinline__ bool bar_wait(uint64_t *b, uint32_t parity, Control *ctl, uint32_t *status)
+__device__ __forceinline__ bool bar_wait(uint64_t *b, uint32_t parity, volatile uint32_t *abort, uint32_t *status)
 {
-    return bar_try(b, parity) || bar_wait_slow(b, parity, ctl, status);
+    return bar_try(b, parity) || bar_wait_slow(b, parity, abort, status);
 }
 
 __device__ __forceinline__ void map_acquire(const CUtensorMap *map)
@@ -484,7 +485,7 @@ gemm_kernel(const GemmArgs g)
                     }
                     for (uint32_t k = 0; k < op.k; k += BK, ++it) {
                         const uint32_t s = it % STAGES;
-                        if (!bar_wait(&ctl.empty[s], ((it / STAGES) & 1) ^ 1, &ctl, g.status)) { ok = false; break; }
+                        if (!bar_wait(&ctl.empty[s], ((it / STAGES) & 1) ^ 1, &ctl.abort, g.status)) { ok = false; break; }
                         if (rank == 0) bar_expect(&ctl.full[s], CG * STAGE_BYTES);
                         const uint32_t bar = CG == 1 ? smem_addr(&ctl.full[s]) : leader_addr(smem_addr(&ctl.full[s]));
                         const uint32_t st = stages + s * STAGE_BYTES;
@@ -509,7 +510,7 @@ gemm_kernel(const GemmArgs g)
                 const Tile tl = g.tiles[t];
                 const Operands op = operands<P>(g, g.mats[tl.mat], tl.mat);
                 const uint32_t as = n & 1;
-                if (!bar_wait(&ctl.acc_empty[as], ((n >> 1) & 1) ^ 1, &ctl, g.status)) break;
+                if (!bar_wait(&ctl.acc_empty[as], ((n >> 1) & 1) ^ 1, &ctl.abort, g.status)) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 // fp16 operands, fp32 sums, N and M, which dimension is consecutive
                 const uint32_t idesc = (1u << 4) | (static_cast<uint32_t>(op.a_mn) << 15) |
@@ -518,7 +519,7 @@ gemm_kernel(const GemmArgs g)
                 const uint32_t blocks = op.passes * ((op.k + BK - 1) / BK);
                 for (uint32_t k = 0; k < blocks; ++k, ++it) {
                     const uint32_t s = it % STAGES;
-                    if (!bar_wait(&ctl.full[s], (it / STAGES) & 1, &ctl, g.status)) { ok = false; break; }
+                    if (!bar_wait(&ctl.full[s], (it / STAGES) & 1, &ctl.abort, g.status)) { ok = false; break; }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint32_t st = stages + s * STAGE_BYTES;
                     const uint64_t da = operand_desc(st, op.a_mn), db = operand_desc(st + OPERAND_BYTES, op.b_mn);
@@ -560,7 +561,7 @@ gemm_kernel(const GemmArgs g)
                 if (in_lo) load_box<1>(lo_buf, in_map + 1, c0, r0, bar);
             };
             if (P != GRAM && chunks && lane == 0) fetch(c_first);
-            ok = bar_wait(&ctl.acc_full[as], (n >> 1) & 1, &ctl, g.status);
+            ok = bar_wait(&ctl.acc_full[as], (n >> 1) & 1, &ctl.abort, g.status);
             if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
@@ -568,7 +569,7 @@ gemm_kernel(const GemmArgs g)
                 const uint32_t c0 = c_first + ch * CHUNK;
                 if (P != GRAM) {
                     if (ch && lane == 0) fetch(c0);
-                    ok = bar_wait(&ctl.staged[ew], loads & 1, &ctl, g.status);
+                    ok = bar_wait(&ctl.staged[ew], loads & 1, &ctl.abort, g.status);
                     if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
                     loads += 1;
                 } else {
@@ -713,6 +714,371 @@ gemm_kernel(const GemmArgs g)
     }
 }
 
+// ------------------------------------------------------------- short sides: one launch for it all
+
+// Matrices with a short side of at most FULL_SIDE whose entries fit the shared memory of a cluster go
+// through all steps in one launch.  The long side is cut into tiles of 128, dealt to the cluster's CTAs;
+// a CTA keeps its part of X, hi and lo, as rows along the long side.  Per step it forms its part of
+// A (products over its tiles), the parts are added through distributed shared memory, every CTA adding
+// up its share of the entries and handing the sums to all, in a fixed order, and then makes B and the
+// products with its own part by itself.  All products are taken in full (hi hi + hi lo + lo hi).  What
+// bounds this kernel is the chain of waits (two cluster barriers and three products per step), not
+// bytes or products: 15 separate launches took 111 us for 64 x 147.
+
+constexpr int NARROW_THREADS = 256;
+constexpr uint32_t NARROW_TILE_LIMIT = 5;        // tiles of 128 per CTA at short sides up to 64
+constexpr uint32_t NARROW_MAX_CLUSTER = 8;
+
+struct NarrowArgs {
+    const Mat *mats;
+    const uint32_t *list;                // matrices, one per cluster
+    float coef[3 * MAX_STEPS];
+    uint32_t steps;
+    float eps;
+    __nv_bfloat16 *out;
+    float *params;
+    float lr, decay;
+    uint32_t *status;
+};
+
+struct NarrowControl {
+    uint64_t done;
+    double sum;
+    uint32_t tmem;
+    volatile uint32_t abort;
+};
+
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t peer_addr(uint32_t a, uint32_t rank)
+{
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ float4 peer_load(uint32_t a)
+{
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ void peer_store(uint32_t a, uint4 v)
+{
+    asm volatile("st.shared::cluster.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ void tmem_load8(uint32_t addr, float (&v)[8])
+{
+    uint32_t u[8];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]) : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(u[i]);
+}
+// 8 numbers as hi and lo fp16
+__device__ __forceinline__ void split8(const float (&x)[8], uint4 &hi, uint4 &lo)
+{
+    uint32_t h[4], l[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __half2 a = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
+        const float2 back = __half22float2(a);
+        h[i] = bits(a);
+        l[i] = bits(__floats2half2_rn(x[2 * i] - back.x, x[2 * i + 1] - back.y));
+    }
+    hi = make_uint4(h[0], h[1], h[2], h[3]);
+    lo = make_uint4(l[0], l[1], l[2], l[3]);
+}
+__device__ __forceinline__ void join8(uint4 hi, uint4 lo, float (&x)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 a = half2_at(hi, i), b = half2_at(lo, i);
+        x[2 * i] = a.x + b.x;
+        x[2 * i + 1] = a.y + b.y;
+    }
+}
+
+// Shared memory, each part 1024-byte aligned: X hi, X lo (64 columns of the short side per block: rows of
+// 128 bytes, tiles * 128 of them), then A or B hi, lo (blocks of 128 rows), then this CTA's part of A in fp32.
+struct NarrowLayout {
+    uint32_t blocks, x_block, x, ab, part, total;
+    __host__ __device__ NarrowLayout(uint32_t side, uint32_t tiles)
+    {
+        blocks = side <= 64 ? 1 : 2;
+        x_block = tiles * 128 * 128;
+        x = blocks * x_block;
+        ab = blocks * 128 * 128;
+        part = side * side * 4;
+        total = 2 * x + 2 * ab + part + 1024;
+    }
+};
+
+// Dynamic shared memory is rounded up to this, so that an SM never holds two of these CTAs: each takes all of
+// the tensor memory, and CTAs of two clusters waiting for each other's would wait for good.
+constexpr uint32_t NARROW_MIN_SMEM = 120 * 1024;
+static_assert(NARROW_THREADS == INGEST_THREADS, "block_sum");
+
+// Smallest power of two of CTAs that gives each one tile, at most NARROW_MAX_CLUSTER.
+uint32_t narrow_cluster(uint32_t n)
+{
+    uint32_t c = 1;
+    while (c < NARROW_MAX_CLUSTER && c * 128 < n) c *= 2;
+    return c;
+}
+uint32_t narrow_tiles(uint32_t n) { return ((n + 127) / 128 + narrow_cluster(n) - 1) / narrow_cluster(n); }
+bool is_narrow(uint32_t m, uint32_t n) { return m <= FULL_SIDE && narrow_tiles(n) <= (m <= 64 ? NARROW_TILE_LIMIT : 1); }
+
+// C: CTAs per matrix
+template <typename T, uint32_t C>
+__global__ void __launch_bounds__(NARROW_THREADS, 1)
+narrow_kernel(const NarrowArgs g, const Source<T> src)
+{
+    extern __shared__ uint8_t raw[];
+    __shared__ NarrowControl ctl;
+    const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31, quad = wid & 3, half = wid >> 2;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const uint32_t rank = C == 1 ? 0 : blockIdx.x % C;
+    const Mat &M = g.mats[g.list[blockIdx.x / C]];
+    const uint32_t m = M.m, n = M.n, side = (m + 15) & ~15u;
+    const bool tall = M.tall;
+    const uint32_t all_tiles = (n + 127) / 128, per = (all_tiles + C - 1) / C;
+    const uint32_t tile0 = min(rank * per, all_tiles), tiles = min(per, all_tiles - tile0);
+    const uint32_t j0 = tile0 * 128, count = min(n - min(n, j0), tiles * 128);       // this CTA's share of the long side
+    const NarrowLayout L(side, per);
+    const uint32_t base = (smem_addr(raw) + 1023) & ~1023u;
+    const uint32_t x_hi = base, x_lo = x_hi + L.x, ab_hi = x_lo + L.x, ab_lo = ab_hi + L.ab, part = ab_lo + L.ab;
+
+    if (tid == 0) {
+        bar_init(&ctl.done, 1);
+        ctl.abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (wid == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                     :: "r"(smem_addr(&ctl.tmem)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+
+    // ---- momentum and norm
+    auto place = [&](uint32_t i, uint32_t j) { return M.offset + (tall ? j * M.stride + i : i * M.stride + j); };
+    const bool update = src.mom && src.in && !M.spread;
+    double sum = 0;
+    // consecutive threads along what is consecutive in memory
+    const uint32_t fast = tall ? m : count, total = m * count;
+    for (uint32_t e = tid; e < total; e += NARROW_THREADS) {
+        const uint32_t q = e / fast, p = e - q * fast;
+        const uint64_t at = tall ? place(p, j0 + q) : place(q, j0 + p);
+        float y;
+        if (update) {
+            const float x = src.input(at), mo = __fmaf_rn(src.mu, src.mom[at], x);
+            src.mom[at] = mo;
+            y = src.nesterov ? __fmaf_rn(src.mu, mo, x) : mo;
+        } else {
+            y = src.direction(at);
+        }
+        sum = __fma_rn(static_cast<double>(y), static_cast<double>(y), sum);
+    }
+    sum = block_sum(sum);
+    if (tid == 0) ctl.sum = sum;
+    // X starts as zeros: what lies beyond the matrix stays zero
+    for (uint32_t b = tid * 16; b < 2 * L.x + 2 * L.ab; b += NARROW_THREADS * 16) sts16(base + b, make_uint4(0, 0, 0, 0));
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = ctl.tmem;
+    if (C > 1) {
+        cluster_sync();
+        sum = 0;
+        for (uint32_t o = 0; o < C; ++o) {
+            double s;
+            asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(s) : "r"(peer_addr(smem_addr(&ctl.sum), o)) : "memory");
+            sum += s;
+        }
+    }
+    const double inv = static_cast<double>(SCALE) / (sqrt(sum) + static_cast<double>(g.eps));
+    for (uint32_t e = tid; e < total; e += NARROW_THREADS) {
+        const uint32_t q = e / fast, p = e - q * fast;
+        const uint32_t i = tall ? p : q, j = tall ? q : p;
+        const float x = static_cast<float>(static_cast<double>(src.direction(place(i, j0 + j))) * inv);
+        const __half h = __float2half_rn(x), l = __float2half_rn(x - __half2float(h));
+        const uint32_t at = (i >> 6) * L.x_block + j * 128 + ((((i & 63) >> 3) ^ (j & 7)) << 4) + (i & 7) * 2;
+        asm volatile("st.shared.b16 [%0], %1;" :: "r"(x_hi + at), "h"(__half_as_ushort(h)) : "memory");
+        asm volatile("st.shared.b16 [%0], %1;" :: "r"(x_lo + at), "h"(__half_as_ushort(l)) : "memory");
+    }
+
+    // ---- steps
+    uint32_t phase = 0;
+    bool ok = true;
+    // every thread's writes to the operands, then the products of thread 0, then everyone waits for them
+    auto products = [&](auto issue) {
+        asm volatile("fence.proxy.async;" ::: "memory");
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncthreads();
+        if (tid == 0) {
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            issue();
+            mma_commit<1>(&ctl.done);
+        }
+        __syncwarp();
+        ok = ok && bar_wait(&ctl.done, phase & 1, &ctl.abort, g.status);
+        phase += 1;
+        __syncwarp();
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    };
+    const uint32_t row_tmem = tmem + (static_cast<uint32_t>(quad * 32) << 16);
+    const uint32_t d_apply = 128;                                // columns 0 .. 127: A, A^2;  from 128: products with X
+    const uint32_t units = side / 8;                             // 8 columns each
+    const uint32_t i_row = quad * 32 + lane;                     // this thread's row of A and B
+    const uint32_t idesc = (1u << 4) | ((side >> 3) << 17) | ((128 >> 4) << 24);
+    const float last_scale = M.scale * INV_SCALE;
+#pragma unroll 1
+    for (uint32_t st = 0; st < g.steps; ++st) {
+        const float ca = g.coef[3 * st], cb = g.coef[3 * st + 1], cc = g.coef[3 * st + 2];
+        // A: both operands have the short side consecutive; rows beyond it repeat the first block
+        products([&]() {
+            uint32_t acc = 0;
+            const uint64_t lbo = static_cast<uint64_t>(L.blocks == 2 ? L.x_block >> 4 : 0) << 16;
+            const uint64_t dh = (operand_desc(x_hi, false) & ~(0x3FFFull << 16)) | lbo;
+            const uint64_t dl = (operand_desc(x_lo, false) & ~(0x3FFFull << 16)) | lbo;
+            for (int pass = 0; pass < 3; ++pass)
+                for (uint32_t k = 0; k < tiles * 8; ++k) {
+                    mma<1>(tmem, (pass == 2 ? dl : dh) + k * 128, (pass == 1 ? dl : dh) + k * 128, idesc | (3u << 15), acc);
+                    acc = 1;
+                }
+        });
+        if (C == 1) {
+            for (uint32_t u = half; u < units; u += 2) {
+                float v[8];
+                __syncwarp();
+                tmem_load8(row_tmem + u * 8, v);
+                if (i_row < side) {
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) v[q] *= INV_SCALE;
+                    uint4 hi, lo;
+                    split8(v, hi, lo);
+                    const uint32_t at = (u >> 3) * (128 * 128) + i_row * 128 + (((u & 7) ^ (i_row & 7)) << 4);
+                    sts16(ab_hi + at, hi);
+                    sts16(ab_lo + at, lo);
+                }
+            }
+        } else {
+            for (uint32_t u = half; u < units; u += 2) {
+                float v[8];
+                __syncwarp();
+                if (tiles) tmem_load8(row_tmem + u * 8, v);
+                else
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) v[q] = 0.f;
+                if (i_row < side) {
+                    // 16-byte units of a row permuted within groups of 8 (or 4): no bank conflicts between rows
+                    const uint32_t perm = i_row & 3;
+                    const uint32_t at = part + i_row * side * 4;
+                    sts16(at + (((2 * u) ^ perm) << 4), make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));
+                    sts16(at + (((2 * u + 1) ^ perm) << 4), make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])));
+                }
+            }
+            cluster_sync();
+            for (uint32_t e = rank * NARROW_THREADS + tid; e < side * units; e += C * NARROW_THREADS) {
+                const uint32_t i = e / units, u = e - i * units, perm = i & 3;
+                const uint32_t at = part + i * side * 4;
+                float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+                for (uint32_t o = 0; o < C; ++o) {
+                    const uint32_t p = peer_addr(at, o);
+                    const float4 a = peer_load(p + (((2 * u) ^ perm) << 4)), b = peer_load(p + (((2 * u + 1) ^ perm) << 4));
+                    v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
+                    v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+                }
+#pragma unroll
+                for (int q = 0; q < 8; ++q) v[q] *= INV_SCALE;
+                uint4 hi, lo;
+                split8(v, hi, lo);
+                const uint32_t to = (u >> 3) * (128 * 128) + i * 128 + (((u & 7) ^ (i & 7)) << 4);
+#pragma unroll
+                for (uint32_t o = 0; o < C; ++o) {
+                    peer_store(peer_addr(ab_hi + to, o), hi);
+                    peer_store(peer_addr(ab_lo + to, o), lo);
+                }
+            }
+            asm volatile("fence.proxy.async;" ::: "memory");
+            cluster_sync();
+        }
+        // A^2, then B in the place of A
+        const uint64_t ah = operand_desc(ab_hi, false), al = operand_desc(ab_lo, false);
+        auto at_k = [](uint64_t d, uint32_t k, uint32_t block) { return d + (k >> 2) * (block >> 4) + (k & 3) * 2; };
+        products([&]() {
+            for (int pass = 0; pass < 3; ++pass)
+                for (uint32_t k = 0; k < side / 16; ++k)
+                    mma<1>(tmem, at_k(pass == 2 ? al : ah, k, 128 * 128), at_k(pass == 1 ? al : ah, k, 128 * 128), idesc,
+                           (pass | k) != 0);
+        });
+        for (uint32_t u = half; u < units; u += 2) {
+            float v[8];
+            __syncwarp();
+            tmem_load8(row_tmem + u * 8, v);
+            if (i_row < side) {
+                const uint32_t at = (u >> 3) * (128 * 128) + i_row * 128 + (((u & 7) ^ (i_row & 7)) << 4);
+                float x[8];
+                join8(lds16(ab_hi + at), lds16(ab_lo + at), x);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) x[q] = __fmaf_rn(cc, v[q] * INV_SCALE, cb * x[q]);
+                uint4 hi, lo;
+                split8(x, hi, lo);
+                sts16(ab_hi + at, hi);
+                sts16(ab_lo + at, lo);
+            }
+        }
+        // X B, tile by tile
+        products([&]() {
+            for (uint32_t t = 0; t < tiles; ++t) {
+                const uint64_t xh = operand_desc(x_hi + t * (128 * 128), false), xl = operand_desc(x_lo + t * (128 * 128), false);
+                for (int pass = 0; pass < 3; ++pass)
+                    for (uint32_t k = 0; k < side / 16; ++k)
+                        mma<1>(tmem + d_apply + t * side, at_k(pass == 2 ? xl : xh, k, L.x_block),
+                               at_k(pass == 1 ? al : ah, k, 128 * 128), idesc, (pass | k) != 0);
+            }
+        });
+        const bool last = st + 1 == g.steps;
+        for (uint32_t w = half; w < tiles * units; w += 2) {
+            const uint32_t t = w / units, u = w - t * units;
+            float v[8];
+            __syncwarp();
+            tmem_load8(row_tmem + d_apply + t * side + u * 8, v);
+            const uint32_t j = t * 128 + i_row;
+            const uint32_t at = (u >> 3) * L.x_block + j * 128 + (((u & 7) ^ (j & 7)) << 4);
+            float x[8];
+            join8(lds16(x_hi + at), lds16(x_lo + at), x);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) x[q] = __fmaf_rn(ca, x[q], v[q] * INV_SCALE);
+            if (!last) {
+                uint4 hi, lo;
+                split8(x, hi, lo);
+                sts16(x_hi + at, hi);
+                sts16(x_lo + at, lo);
+            } else if (j < count) {
+#pragma unroll
+                for (uint32_t q = 0; q < 8; ++q) {
+                    const uint32_t i = u * 8 + q;
+                    if (i >= m) break;
+                    const uint64_t p = place(i, j0 + j);
+                    if (g.params) g.params[p] = __fmaf_rn(-g.lr, last_scale * x[q], g.decay * g.params[p]);
+                    else g.out[p] = __float2bfloat16_rn(last_scale * x[q]);
+                }
+            }
+        }
+    }
+    // the launch before this one may still run: its results are this one's to be waited for as well
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (C > 1) cluster_sync();
+    if (wid == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(512));
+}
+
 // ------------------------------------------------------------------- server update's own parts
 
 // M <- mu M
@@ -753,7 +1119,7 @@ rest_kernel(const Piece *pieces, float *params, const float *m, float lr, float 
 
 // ------------------------------------------------------------------------------------- host
 
-// The tiles of a phase: where in the handle's list, how many, and by one CTA or a pair of them.
+// Work of one launch: where in the handle's list, how much, and by how many CTAs each.
 struct Span {
     uint32_t first, count, cg;
 };
@@ -845,6 +1211,8 @@ struct deco_orth {
     bool strided = false;                // some matrix's rows are not back to back
     uint32_t sms = 0;
     std::vector<Group> groups;
+    std::vector<Span> narrow;            // matrices of narrow_kernel, by cluster size
+    uint32_t narrow_smem = 0;
     uint32_t n_pieces = 0, n_rest = 0, n_row_pieces = 0;
     // device memory
     uint8_t *workspace = nullptr;
@@ -854,6 +1222,7 @@ struct deco_orth {
     RowPiece *row_pieces = nullptr;
     ConvertPiece *convert = nullptr;
     Tile *tiles = nullptr;
+    uint32_t *narrow_list = nullptr;
     double *partial = nullptr;
     uint32_t *status = nullptr;
     uint64_t device_bytes = 0, launches = 0;
@@ -870,6 +1239,7 @@ void release(deco_orth *h)
     cudaFree(h->row_pieces);
     cudaFree(h->convert);
     cudaFree(h->tiles);
+    cudaFree(h->narrow_list);
     cudaFree(h->partial);
     cudaFree(h->status);
     delete h;
@@ -938,6 +1308,7 @@ deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, ui
     const uint32_t n = static_cast<uint32_t>(ms.size());
     std::vector<Mat> mats(n);
     std::vector<uint64_t> bytes(n);
+    std::vector<uint32_t> wide;                                  // matrices that go through gemm_kernel
     for (uint32_t i = 0; i < n; ++i) {
         Mat &M = mats[i];
         const deco_matrix &q = ms[i];
@@ -951,18 +1322,33 @@ deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, ui
         M.ldx = static_cast<uint32_t>(round_up(q.cols, 8));
         M.lda = static_cast<uint32_t>(round_up(M.m, 8));
         M.precision = M.m <= FULL_SIDE ? FULL : M.m <= WIDE_B_SIDE ? WIDE_B : PLAIN;
+        M.spread = q.row_stride != q.cols && q.rows > 1;
         const double r = q.rows, c = q.cols;
         M.scale = scale == DECO_ORTH_SCALE_SPECTRAL ? static_cast<float>(sqrt(std::max(1.0, r / c)))
                 : scale == DECO_ORTH_SCALE_RMS      ? static_cast<float>(0.2 * sqrt(std::max(r, c)))
                                                     : 1.f;
+        if (is_narrow(M.m, M.n)) continue;
         bytes[i] = 4 * round_up(2ull * M.rows * M.ldx, 256) + (2 + M.precision) * round_up(2ull * M.m * M.lda, 256);
+        wide.push_back(i);
+    }
+    std::vector<uint32_t> narrow_list;
+    for (uint32_t c = NARROW_MAX_CLUSTER; c >= 1; c /= 2) {
+        Span span = {static_cast<uint32_t>(narrow_list.size()), 0, c};
+        for (uint32_t i = 0; i < n; ++i)
+            if (is_narrow(mats[i].m, mats[i].n) && narrow_cluster(mats[i].n) == c) {
+                narrow_list.push_back(i);
+                const NarrowLayout L((mats[i].m + 15) & ~15u, narrow_tiles(mats[i].n));
+                h->narrow_smem = std::max(h->narrow_smem, std::max(L.total, NARROW_MIN_SMEM));
+            }
+        span.count = static_cast<uint32_t>(narrow_list.size()) - span.first;
+        if (span.count) h->narrow.push_back(span);
     }
     // groups, in order, of what fits the workspace
-    std::vector<uint32_t> group_of(n);
+    std::vector<uint32_t> group_of(n, NO_SLOT);
     uint64_t used = 0, most = 0;
     uint32_t groups = 0;
-    for (uint32_t i = 0; i < n; ++i) {
-        if (i == 0 || used + bytes[i] > cap) {
+    for (uint32_t i : wide) {
+        if (groups == 0 || used + bytes[i] > cap) {
             groups += 1;
             used = 0;
         }
@@ -977,8 +1363,10 @@ deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, ui
     }
     std::vector<CUtensorMap> maps(static_cast<uint64_t>(MAPS) * n);
     uint64_t at = 0;
-    for (uint32_t i = 0; i < n; ++i) {
-        if (i == 0 || group_of[i] != group_of[i - 1]) at = 0;
+    uint32_t placed = NO_SLOT;
+    for (uint32_t i : wide) {
+        if (group_of[i] != placed) at = 0;
+        placed = group_of[i];
         Mat &M = mats[i];
         const uint64_t xb = round_up(2ull * M.rows * M.ldx, 256), ab = round_up(2ull * M.m * M.lda, 256);
         auto take = [&](uint64_t b) { __half *p = reinterpret_cast<__half *>(h->workspace + at); at += b; return p; };
@@ -1007,18 +1395,20 @@ deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, ui
     uint64_t end = 0;
     for (uint32_t i : order) {
         Mat &M = mats[i];
-        if (M.stride != M.cols && M.rows > 1) continue;
+        if (M.spread) continue;
         add_pieces(rest, end, M.offset, nullptr);
-        M.piece0 = slot;
         end = M.offset + static_cast<uint64_t>(M.rows) * M.cols;
+        if (group_of[i] == NO_SLOT) continue;                    // narrow_kernel takes its own in
+        M.piece0 = slot;
         add_pieces(pieces, M.offset, end, &slot);
         M.pieces = slot - M.piece0;
     }
     add_pieces(rest, end, h->d, nullptr);
     for (uint32_t i : order) {
         Mat &M = mats[i];
-        if (M.stride == M.cols || M.rows == 1) continue;
+        if (!M.spread) continue;
         h->strided = true;
+        if (group_of[i] == NO_SLOT) continue;
         M.piece0 = slot;
         const uint32_t per = std::max(1u, PIECE / M.cols);
         for (uint32_t r = 0; r < M.rows; r += per) row_pieces.push_back({i, r, std::min(per, M.rows - r), slot++});
@@ -1031,14 +1421,13 @@ deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, ui
     // tiles and convert pieces of each group, the longest products first
     std::vector<Tile> tiles;
     std::vector<ConvertPiece> convert;
-    for (uint32_t g = 0, i0 = 0; g < groups; ++g) {
-        uint32_t i1 = i0;
-        while (i1 < n && group_of[i1] == g) ++i1;
+    for (uint32_t g = 0; g < groups; ++g) {
         Group G = {};
         G.convert0 = static_cast<uint32_t>(convert.size());
-        std::vector<uint32_t> by(i1 - i0);
-        for (uint32_t i = i0; i < i1; ++i) {
-            by[i - i0] = i;
+        std::vector<uint32_t> by;
+        for (uint32_t i : wide) {
+            if (group_of[i] != g) continue;
+            by.push_back(i);
             const Mat &M = mats[i];
             for (uint32_t c = 0; c < M.cols; c += CONVERT_COLS) {
                 const uint32_t per = std::max(1u, PIECE / std::min(M.cols - c, CONVERT_COLS));
@@ -1078,12 +1467,12 @@ deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, ui
             tiles.insert(tiles.end(), chosen.begin(), chosen.end());
         }
         h->groups.push_back(G);
-        i0 = i1;
     }
     std::vector<double> partial(slot, 0.0);
     std::vector<uint32_t> status(1, 0u);
     if (!upload(h, &h->mats, mats) || !upload(h, &h->maps, maps) || !upload(h, &h->pieces, pieces) ||
         !upload(h, &h->row_pieces, row_pieces) || !upload(h, &h->convert, convert) || !upload(h, &h->tiles, tiles) ||
+        !upload(h, &h->narrow_list, narrow_list) ||
         !upload(h, &h->partial, partial) || !upload(h, &h->status, status))
         return DECO_ERR_OOM;
     // the copies above may still be under way; the handle's first pass may come on any stream
@@ -1122,6 +1511,39 @@ cudaError_t launch_gemm(deco_orth *h, GemmArgs g, const Span &span, cudaStream_t
                         : launch_after(h, gemm_kernel<2, P, T>, grid, GEMM_THREADS, GEMM_SMEM, 2, s, g);
 }
 
+template <typename T, uint32_t C>
+cudaError_t launch_narrow(deco_orth *h, const NarrowArgs &a, const Source<T> &src, uint32_t count, bool first, cudaStream_t s)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(count * C);
+    cfg.blockDim = dim3(NARROW_THREADS);
+    cfg.dynamicSmemBytes = h->narrow_smem;
+    cfg.stream = s;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = C;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    // the launches of one pass may run side by side; the first waits for what comes before the pass
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = first ? 1 : 2;
+    h->launches += 1;
+    return cudaLaunchKernelEx(&cfg, narrow_kernel<T, C>, a, src);
+}
+
+template <typename T>
+bool allow_narrow_smem()
+{
+    const int most = 227 * 1024;
+    auto set = [&](void (*k)(const NarrowArgs, const Source<T>)) {
+        cudaFuncAttributes fa;
+        return cudaFuncGetAttributes(&fa, k) == cudaSuccess &&
+               cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, most - static_cast<int>(fa.sharedSizeBytes)) == cudaSuccess;
+    };
+    return set(narrow_kernel<T, 1>) && set(narrow_kernel<T, 2>) && set(narrow_kernel<T, 4>) && set(narrow_kernel<T, 8>);
+}
+
 template <Phase P, Target T>
 bool allow_smem()
 {
@@ -1146,6 +1568,25 @@ cudaError_t run_pass(deco_orth *h, const Source<T> &src, __nv_bfloat16 *out, flo
         h->launches += 1;
     }
     cudaError_t err = cudaGetLastError();
+    NarrowArgs na = {};
+    na.mats = h->mats;
+    std::copy(h->coef.begin(), h->coef.end(), na.coef);
+    na.steps = h->steps;
+    na.eps = h->eps;
+    na.out = out;
+    na.params = params;
+    na.lr = lr;
+    na.decay = decay;
+    na.status = h->status;
+    for (const Span &q : h->narrow) {
+        if (err != cudaSuccess) return err;
+        na.list = h->narrow_list + q.first;
+        const bool first = &q == &h->narrow.front();
+        err = q.cg == 8   ? launch_narrow<T, 8>(h, na, src, q.count, first, s)
+              : q.cg == 4 ? launch_narrow<T, 4>(h, na, src, q.count, first, s)
+              : q.cg == 2 ? launch_narrow<T, 2>(h, na, src, q.count, first, s)
+                          : launch_narrow<T, 1>(h, na, src, q.count, first, s);
+    }
     for (const Group &G : h->groups) {
         if (err != cudaSuccess) return err;
         err = launch_after(h, convert_kernel<T>, G.n_convert, INGEST_THREADS, 0, 1, s,
@@ -1205,7 +1646,8 @@ try {
     int sms = 0;
     if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, o.device) != cudaSuccess) return DECO_ERR_CUDA;
     if (!allow_smem<GRAM, NEXT_X>() || !allow_smem<POLY, NEXT_X>() || !allow_smem<APPLY, NEXT_X>() ||
-        !allow_smem<APPLY, OUT_BF16>() || !allow_smem<APPLY, PARAMS>())
+        !allow_smem<APPLY, OUT_BF16>() || !allow_smem<APPLY, PARAMS>() || !allow_narrow_smem<float>() ||
+        !allow_narrow_smem<__nv_bfloat16>())
         return DECO_ERR_CUDA;
     deco_orth *h = new deco_orth;
     deco_status st = DECO_ERR_OOM;
