@@ -498,15 +498,16 @@ deco_status deco_token_logprobs_grad(const void *logits, int32_t dtype, uint64_t
  * Newton-Schulz products, as the Muon optimiser does, for the matrices of a flat vector of length
  * d laid out like the gradients and the parameters.  Per matrix Y [rows][cols]:
  *   X = Y / (|Y|_F + eps)
- *   steps times:  A = X X^T,  X <- a X + (b A + c A^2) X        (X^T X and X (..) where rows > cols:
- *                                                                the same polynomial of X)
+ *   steps times:  A = X X^T,  X <- (a + b A + c A^2) X     (X^T X and X (...) where rows > cols: the same polynomial)
  *   out = s X,   s by deco_orth_scale
  * With momentum: M <- mu M + in (fp32, rounded once), and Y = M, or Y = in + mu M (nesterov).
  *
  * Precision: products take fp16 operands (11 bits, scaled by a power of two) and are summed in
  * fp32 on the tensor cores; X itself is carried as a pair of fp16 numbers (22 bits) until the
- * last step, so that directions the input lacks are not filled with rounding noise.  The result
- * is within about 2e-3 of the exact polynomial in the 2-norm, which the rounding to bf16 matches.
+ * last step, so that directions the input lacks are not filled with rounding noise, and short sides
+ * up to 128 are multiplied with 22 bits throughout.  With the standard coefficients the result is
+ * within about 2e-3 of the exact polynomial in the 2-norm, which the rounding to bf16 matches; the error
+ * grows with the terms that cancel, |a| + |b| + |c|.
  * |Y|_F is summed in double, so it neither overflows nor underflows.  A matrix that holds a NaN or an infinity gives NaN;
  * a zero matrix gives zeros.
  */
@@ -526,8 +527,8 @@ typedef enum {
 /* Options of deco_orth_init.  A zero-filled struct selects every default. */
 typedef struct {
     const float *coef;        /* HOST, [steps][3]: a, b, c of each step; NULL -> 3.4445, -4.7750, 2.0315.
-                                 The polynomials must keep singular values of [0, 1] at or below 1.75
-                                 and |b t + c t^2| at or below 3.75 there (t the square of the
+                                 The polynomials must keep singular values of [0, 1] at or below 2.5
+                                 and |a + b t + c t^2| at or below 15 there (t the square of the
                                  singular value), else DECO_ERR_INVALID_ARG */
     uint32_t steps;           /* 0 -> 5; at most 16 */
     float    eps;             /* 0 -> 1e-7 */
@@ -552,7 +553,8 @@ typedef struct deco_orth deco_orth;          /* opaque, owned by the library */
 
 /*
  * Plans the work and allocates all device memory the handle will ever use.  The matrices lie
- * inside [0, d) and do not overlap (DECO_ERR_INVALID_ARG); entries of no matrix are allowed.  *out is set only on success.
+ * inside [0, d) and do not overlap; from its first entry to its last a matrix may be interleaved
+ * with others only as column ranges of rows of one row_stride (else DECO_ERR_INVALID_ARG); entries of no matrix are allowed.  *out is set only on success.
  * One handle is used on one stream at a time.
  */
 deco_status deco_orth_init(deco_orth **out, uint64_t d, const deco_matrix *matrices /* HOST */,

@@ -1,26 +1,26 @@
 // deco_orth_*: orthogonalised update directions by Newton-Schulz products.
 //
 // For a matrix Y [rows][cols] with short side m and long side n:  X = Y / (|Y|_F + eps), then per step
-//     A = X X^T   (X^T X where rows > cols),   B = b A + c A^2,   X <- a X + B X   (a X + X B).
+//     A = X X^T   (X^T X where rows > cols),   P = a + b A + c A^2,   X <- P X   (X P).
 // All matrices of a group go through a step together, in three launches: one list of output tiles
-// spans matrices of every shape.  A and B are symmetric: only blocks on and below the diagonal are
+// spans matrices of every shape.  A and P are symmetric: only blocks on and below the diagonal are
 // computed and the others are their mirror images.  X is kept in the orientation of Y, so nothing
 // is ever transposed in memory: the tensor cores take an operand with either of its dimensions
 // consecutive, and one 64 x 64 box loads both kinds.
 //
-// Numbers.  Operands are fp16, scaled by 2^14: |X| <= 1.75 and |B| <= 3.75 in the spectral norm (checked
-// for the coefficients in deco_orth_init), so every entry stays below 65504, and entries down to
-// 3.7e-9 keep all 11 bits.  Sums are fp32.  X is carried as hi + lo, two fp16 numbers; the products read
-// hi, the term a X reads both.  Rounding X to 11 bits there would put noise of 2^-12 |X| into
-// directions in which Y has nothing, and five steps amplify those 485 times (a rank-1 matrix
-// came out 15 % wrong); noise that enters through A, B or the product stays in the row and
+// Numbers.  Operands are fp16, X scaled by 2^14, A by 2^13, P by 2^12: |X| <= 2.5 and |P| <= 15 in the spectral
+// norm (checked for the coefficients in deco_orth_init), so every entry stays below 65504, and entries
+// down to 3.7e-9 (A: 7.5e-9, P: 1.5e-8) keep all 11 bits.  Sums are fp32.  X is carried as hi + lo, two fp16 numbers; the
+// product reads hi, and a lo is added to it.  Without lo, rounding X to 11 bits would put noise of 2^-12 |X|
+// into directions in which Y has nothing, and five steps amplify those 485 times (a rank-1 matrix
+// came out 15 % wrong); noise that enters through A or P stays in the row and
 // column space of X and is not amplified.  The last step needs no lo: it amplifies 3.4 times.
 //
-// The rounding of A and B themselves reaches the result through b A and c A^2, which nearly cancel.
-// Over many singular values these errors average out (1.2e-3 of the norm at a short side of 512, against
+// The rounding of A and P themselves reaches the result through b A and c A^2, which nearly cancel.
+// Over many singular values these errors average out (1.3e-3 of the norm at a short side of 512, against
 // 1.7e-3 of the rounding to bf16), over few they do not (up to 8e-3 at short sides below 16).  So
 // matrices up to FULL_SIDE are multiplied in full, hi and lo of both operands (22 bits), and
-// those up to WIDE_B_SIDE with B as hi + lo (1.8e-3 -> 1.3e-3 at 128).  Both are as fast as the plain products
+// those up to WIDE_P_SIDE with P as hi + lo (1.5e-3 -> 1.2e-3 at 160).  Both are as fast as the plain products
 // there, since short sides leave the tensor cores waiting for memory.
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -38,9 +38,10 @@
 
 namespace {
 
-constexpr float SCALE = 16384.f;         // of X, A and B in fp16
-constexpr float INV_SCALE = 1.f / 16384.f;
-constexpr double MAX_SIGMA = 1.75, MAX_B = 3.75;
+constexpr float X_SCALE = 16384.f, A_SCALE = 8192.f, P_SCALE = 4096.f;      // of X, A and P in fp16
+constexpr float XX_TO_A = A_SCALE / (X_SCALE * X_SCALE), A_TO_P = P_SCALE / A_SCALE, AA_TO_P = A_TO_P / A_SCALE;
+constexpr float INV_X_SCALE = 1.f / X_SCALE, INV_P_SCALE = 1.f / P_SCALE;
+constexpr double MAX_SIGMA = 2.5, MAX_P = 15.0;
 constexpr uint32_t MAX_STEPS = 16;
 
 // ------------------------------------------------------------------ tables in device memory
@@ -48,9 +49,9 @@ constexpr uint32_t MAX_STEPS = 16;
 struct Mat {
     uint64_t offset, stride;             // in the flat vectors
     uint32_t rows, cols;
-    uint32_t ldx, lda;                   // entries between rows of X and of A, B
+    uint32_t ldx, lda;                   // entries between rows of X and of A, P
     __half *hi[2], *lo[2];               // X and the next X
-    __half *a, *b, *a_lo, *b_lo;         // (a_lo, b_lo where the precision asks for them)
+    __half *a, *p, *a_lo, *p_lo;         // (a_lo, p_lo where the precision asks for them)
     uint32_t m, n;                       // short and long side
     uint32_t tall;                       // rows > cols
     uint32_t precision;                  // see Precision
@@ -79,11 +80,12 @@ struct Tile {
 };
 
 // Which operands of a matrix's products are carried as hi + lo.
-enum Precision { PLAIN = 0, WIDE_B = 1, FULL = 2 };
-constexpr uint32_t FULL_SIDE = 128, WIDE_B_SIDE = 256;
-// A matrix's tensor maps: boxes of 64 x 64 for the operands, and from BOX32 on the same with boxes of
-// 32 rows for the epilogue.
-enum Map { MAP_X = 0 /* hi, lo, next hi, next lo */, MAP_A = 4 /* hi, lo */, MAP_B = 6 /* hi, lo */, BOX32 = 8, MAPS = 16 };
+enum Precision { PLAIN = 0, WIDE_P = 1, FULL = 2 };
+constexpr uint32_t FULL_SIDE = 128, WIDE_P_SIDE = 256;
+// A matrix's tensor maps: boxes of 64 x 64 for the operands; from BOX32 on the same with boxes of
+// 32 rows for the epilogue; and A and P in boxes of 64 rows by 32 for mirror images.
+enum Map { MAP_X = 0 /* hi, lo, next hi, next lo */, MAP_A = 4 /* hi, lo */, MAP_P = 6 /* hi, lo */, BOX32 = 8,
+           MIRROR_A = 16, MIRROR_P = 17, MAPS = 18 };
 
 constexpr uint32_t NO_SLOT = 0xFFFFFFFFu;
 constexpr uint32_t PIECE = 16384;
@@ -95,16 +97,17 @@ template <typename T> __device__ __forceinline__ float to_f(T x);
 template <> __device__ __forceinline__ float to_f<float>(float x) { return x; }
 template <> __device__ __forceinline__ float to_f<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
 
+template <int THREADS>
 __device__ double block_sum(double v)
 {
-    __shared__ double s[INGEST_THREADS / 32];
+    __shared__ double s[THREADS / 32];
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
     if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
     __syncthreads();
     v = 0;
 #pragma unroll
-    for (int w = 0; w < INGEST_THREADS / 32; ++w) v += s[w];
+    for (int w = 0; w < THREADS / 32; ++w) v += s[w];
     __syncthreads();
     return v;
 }
@@ -147,7 +150,7 @@ ingest_kernel(const Piece *pieces, const Source<T> src, double *partial)
         sum = __fma_rn(static_cast<double>(y), static_cast<double>(y), sum);
     }
     if (p.slot == NO_SLOT) return;
-    sum = block_sum(sum);
+    sum = block_sum<INGEST_THREADS>(sum);
     if (threadIdx.x == 0) partial[p.slot] = sum;
 }
 
@@ -164,7 +167,7 @@ ingest_rows_kernel(const RowPiece *pieces, const Mat *mats, const Source<T> src,
             const double y = src.direction(M.offset + (p.row0 + r) * M.stride + j);
             sum = __fma_rn(y, y, sum);
         }
-    sum = block_sum(sum);
+    sum = block_sum<INGEST_THREADS>(sum);
     if (threadIdx.x == 0) partial[p.slot] = sum;
 }
 
@@ -182,7 +185,7 @@ convert_kernel(const ConvertPiece *pieces, const Mat *mats, const Source<T> src,
     const Mat &M = mats[p.mat];
     double sum = 0;
     for (uint32_t i = threadIdx.x; i < M.pieces; i += INGEST_THREADS) sum += partial[M.piece0 + i];
-    const double inv = static_cast<double>(SCALE) / (sqrt(block_sum(sum)) + static_cast<double>(eps));
+    const double inv = static_cast<double>(X_SCALE) / (sqrt(block_sum<INGEST_THREADS>(sum)) + static_cast<double>(eps));
     const uint32_t w = min(M.cols - p.col0, CONVERT_COLS);
     for (uint32_t e = threadIdx.x; e < p.rows * w; e += INGEST_THREADS) {
         const uint32_t r = p.row0 + e / w, c = p.col0 + e % w;
@@ -380,6 +383,15 @@ __device__ __forceinline__ void sts16(uint32_t a, uint4 v)
 {
     asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
+// Four 8 x 8 pieces of 2-byte numbers, transposed: lane l passes row l % 8 of piece l / 8, where from and where to.
+__device__ __forceinline__ void transpose4(uint32_t from, uint32_t to)
+{
+    uint32_t a, b, c, d;
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(a), "=r"(b), "=r"(c), "=r"(d) : "r"(from) : "memory");
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1,%2,%3,%4};"
+                 :: "r"(to), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
 __device__ __forceinline__ float2 half2_at(const uint4 &v, int i)
 {
     const uint32_t w = i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
@@ -400,26 +412,31 @@ template <Phase P>
 __device__ __forceinline__ Operands operands(const GemmArgs &g, const Mat &M, uint32_t mat)
 {
     const CUtensorMap *at = g.maps + static_cast<uint64_t>(mat) * MAPS;
-    const CUtensorMap *x = at + MAP_X + 2 * g.src, *am = at + MAP_A, *bm = at + MAP_B;
+    const CUtensorMap *x = at + MAP_X + 2 * g.src, *am = at + MAP_A, *pm = at + MAP_P;
     const uint32_t full = M.precision == FULL;
     // hi hi, hi lo, lo hi
     if (P == GRAM) return {x, x, M.tall != 0, M.tall != 0, M.n, full ? 3u : 1u, 4, 2};
     if (P == POLY) return {am, am, false, false, M.m, full ? 3u : 1u, 4, 2};
-    // (B, X): hi hi, lo hi, hi lo
+    // (P, X): hi hi, lo hi, hi lo
     const uint32_t passes = 1 + M.precision;
-    if (M.tall) return {x, bm, false, false, M.m, passes, 4, 2};
-    return {bm, x, false, true, M.m, passes, 2, 4};
+    if (M.tall) return {x, pm, false, false, M.m, passes, 4, 2};
+    return {pm, x, false, true, M.m, passes, 2, 4};
 }
 
 // A CTA (CG = 1: tiles of 128 x 128) or a pair of CTAs (CG = 2: 256 x 256, each CTA half of the rows of
 // the tile and of either operand) works through the tiles; the epilogue of a tile runs beside
 // the products of the next.
 //
-// Epilogue.  A warp takes 32 rows by 64 columns at a time.  What the formula adds to the product (X, or A)
-// comes as a box into the warp's own staging memory, loaded while the tile's products still run;
+// Epilogue.  A warp takes 32 rows by 64 columns at a time.  What the formula adds to the product (A, or
+// X's lo) comes as a box into the warp's own staging memory, loaded while the tile's products still run;
 // a thread owns a row there, as in tensor memory, and puts the result in the place of the input;
 // a box store writes it back.  Rows lie 128 bytes apart in the staging memory with their 16-byte units
-// permuted as the box copies do it, so the row-wise accesses meet no bank conflicts.
+// permuted as the box copies do it, so the row-wise accesses meet no bank conflicts.  A block's mirror
+// image is transposed in 8 x 8 pieces through the other half of the staging memory: 2-byte stores
+// straight to global memory made the products of A with itself 1.4 times slower.
+//
+// Four decoder blocks: tensor cores busy 80 % of the cycles with the epilogue left out, where shared memory, read
+// by them and filled by the loads, is the limit; that is why the epilogue moves as little through it as it can.
 template <int CG, Phase P, Target T>
 __global__ void __launch_bounds__(GEMM_THREADS, 1)
 gemm_kernel(const GemmArgs g)
@@ -546,28 +563,30 @@ gemm_kernel(const GemmArgs g)
             const uint32_t r0 = tl.tm * SIDE + rank * 128 + quad * 32, r = r0 + lane;
             const uint32_t c_first = tl.tn * SIDE + side * (SIDE / 2);
             const bool full = M.precision == FULL;
-            const bool in_lo = P == POLY ? full : P == APPLY ? g.read_lo || full : false;
+            // POLY adds A (lo with full precision), APPLY adds lo of X unless the products did
+            const bool in_hi = P == POLY, in_lo = P == POLY ? full : P == APPLY ? g.read_lo && !full : false;
             const bool out_lo = P == GRAM ? full : P == POLY ? M.precision != PLAIN : g.write_lo || full;
+            const bool fetches = in_hi || in_lo;
             const bool live = r0 < rows;
             const CUtensorMap *maps = g.maps + static_cast<uint64_t>(tl.mat) * MAPS + BOX32;
             const CUtensorMap *in_map = maps + (P == POLY ? MAP_A : MAP_X + 2 * g.src);
-            const CUtensorMap *out_map = maps + (P == GRAM ? MAP_A : P == POLY ? MAP_B : MAP_X + 2 * (g.src ^ 1));
+            const CUtensorMap *out_map = maps + (P == GRAM ? MAP_A : P == POLY ? MAP_P : MAP_X + 2 * (g.src ^ 1));
             const uint32_t chunks = !live || c_first >= cols ? 0 : min(CHUNKS, (cols - c_first + CHUNK - 1) / CHUNK);
             auto fetch = [&](uint32_t c0) {                      // lane 0: the chunk's input, once the staging memory is free
                 asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-                bar_expect(&ctl.staged[ew], in_lo ? 2 * CHUNK_BYTES : CHUNK_BYTES);
+                bar_expect(&ctl.staged[ew], in_hi && in_lo ? 2 * CHUNK_BYTES : CHUNK_BYTES);
                 const uint32_t bar = smem_addr(&ctl.staged[ew]);
-                load_box<1>(hi_buf, in_map, c0, r0, bar);
+                if (in_hi) load_box<1>(hi_buf, in_map, c0, r0, bar);
                 if (in_lo) load_box<1>(lo_buf, in_map + 1, c0, r0, bar);
             };
-            if (P != GRAM && chunks && lane == 0) fetch(c_first);
+            if (fetches && chunks && lane == 0) fetch(c_first);
             ok = bar_wait(&ctl.acc_full[as], (n >> 1) & 1, &ctl.abort, g.status);
             if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
             for (uint32_t ch = 0; ch < chunks; ++ch) {
                 const uint32_t c0 = c_first + ch * CHUNK;
-                if (P != GRAM) {
+                if (fetches) {
                     if (ch && lane == 0) fetch(c0);
                     ok = bar_wait(&ctl.staged[ew], loads & 1, &ctl.abort, g.status);
                     if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
@@ -584,17 +603,22 @@ gemm_kernel(const GemmArgs g)
                     for (uint32_t u = 0; u < 4; ++u) {
                         const uint32_t at = my_row + (((h * 4 + u) ^ perm) << 4);
                         uint4 ih = make_uint4(0, 0, 0, 0), il = ih;
-                        if (P != GRAM) ih = lds16(hi_buf + at);
-                        if (P != GRAM && in_lo) il = lds16(lo_buf + at);
+                        if (in_hi) ih = lds16(hi_buf + at);
+                        if (in_lo) il = lds16(lo_buf + at);
                         float x[8];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const float2 a = half2_at(ih, i), b = half2_at(il, i);
 #pragma unroll
                             for (int j = 0; j < 2; ++j) {
-                                const float acc = __uint_as_float(v[u * 8 + 2 * i + j]) * INV_SCALE;
+                                const float acc = __uint_as_float(v[u * 8 + 2 * i + j]);
                                 const float in = j ? a.y + b.y : a.x + b.x;
-                                x[2 * i + j] = P == GRAM ? acc : P == POLY ? __fmaf_rn(g.c, acc, g.b * in) : __fmaf_rn(g.a, in, acc);
+                                float y;
+                                if (P == GRAM) y = acc * XX_TO_A;
+                                else if (P == POLY) y = __fmaf_rn(g.c * AA_TO_P, acc, (g.b * A_TO_P) * in);
+                                else y = __fmaf_rn(g.a, in, acc * INV_P_SCALE);
+                                if (P == POLY && c0 + h * 32 + u * 8 + 2 * i + j == r) y += g.a * P_SCALE;
+                                x[2 * i + j] = y;
                             }
                         }
                         if (T == NEXT_X) {
@@ -608,26 +632,26 @@ gemm_kernel(const GemmArgs g)
                             }
                             sts16(hi_buf + at, make_uint4(oh[0], oh[1], oh[2], oh[3]));
                             if (out_lo) sts16(lo_buf + at, make_uint4(ol[0], ol[1], ol[2], ol[3]));
-                            if (P != APPLY && tl.tm != tl.tn && r < rows) {     // the block's mirror image
-                                unsigned short *m = reinterpret_cast<unsigned short *>(P == GRAM ? M.a : M.b);
-                                unsigned short *ml = reinterpret_cast<unsigned short *>(P == GRAM ? M.a_lo : M.b_lo);
+                            if (P != APPLY && tl.tm != tl.tn && out_lo && r < rows) {   // no staging memory to spare
+                                unsigned short *m = reinterpret_cast<unsigned short *>(P == GRAM ? M.a : M.p);
+                                unsigned short *ml = reinterpret_cast<unsigned short *>(P == GRAM ? M.a_lo : M.p_lo);
 #pragma unroll
                                 for (uint32_t j = 0; j < 8; ++j) {
                                     const uint32_t c = c0 + h * 32 + u * 8 + j;
                                     if (c < cols) {
                                         m[static_cast<uint64_t>(c) * M.lda + r] = static_cast<unsigned short>(oh[j >> 1] >> (16 * (j & 1)));
-                                        if (out_lo) ml[static_cast<uint64_t>(c) * M.lda + r] = static_cast<unsigned short>(ol[j >> 1] >> (16 * (j & 1)));
+                                        ml[static_cast<uint64_t>(c) * M.lda + r] = static_cast<unsigned short>(ol[j >> 1] >> (16 * (j & 1)));
                                     }
                                 }
                             }
                         } else if (T == OUT_BF16) {
-                            const float s = M.scale * INV_SCALE;
+                            const float s = M.scale * INV_X_SCALE;
                             uint32_t o[4];
 #pragma unroll
                             for (int i = 0; i < 4; ++i) o[i] = bits(__floats2bfloat162_rn(s * x[2 * i], s * x[2 * i + 1]));
                             sts16(hi_buf + at, make_uint4(o[0], o[1], o[2], o[3]));
                         } else {
-                            const float s = M.scale * INV_SCALE;
+                            const float s = M.scale * INV_X_SCALE;
                             uint32_t o[8];
 #pragma unroll
                             for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(s * x[i]);
@@ -637,11 +661,23 @@ gemm_kernel(const GemmArgs g)
                     }
                 }
                 if (T == NEXT_X) {
+                    const bool mirror = P != APPLY && tl.tm != tl.tn && !out_lo;
+                    if (mirror) {
+                        __syncwarp();
+#pragma unroll
+                        for (uint32_t u = 0; u < 8; ++u) {
+                            // four 8 x 8 pieces of 8 columns; row c of the mirror image is 64 bytes, its 16-byte units permuted
+                            const uint32_t c = u * 8 + (lane & 7);
+                            transpose4(hi_buf + my_row + ((u ^ perm) << 4),
+                                       lo_buf + c * 64 + (((lane >> 3) ^ ((c >> 1) & 3)) << 4));
+                        }
+                    }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
                     if (lane == 0) {
                         store_box(out_map, c0, r0, hi_buf);
                         if (out_lo) store_box(out_map + 1, c0, r0, lo_buf);
+                        if (mirror) store_box(maps - BOX32 + (P == GRAM ? MIRROR_A : MIRROR_P), r0, c0, lo_buf);
                         asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                     }
                 } else if (T == OUT_BF16) {
@@ -720,12 +756,12 @@ gemm_kernel(const GemmArgs g)
 // through all steps in one launch.  The long side is cut into tiles of 128, dealt to the cluster's CTAs;
 // a CTA keeps its part of X, hi and lo, as rows along the long side.  Per step it forms its part of
 // A (products over its tiles), the parts are added through distributed shared memory, every CTA adding
-// up its share of the entries and handing the sums to all, in a fixed order, and then makes B and the
+// up its share of the entries and handing the sums to all, in a fixed order, and then makes P and the
 // products with its own part by itself.  All products are taken in full (hi hi + hi lo + lo hi).  What
 // bounds this kernel is the chain of waits (two cluster barriers and three products per step), not
 // bytes or products: 15 separate launches took 111 us for 64 x 147.
 
-constexpr int NARROW_THREADS = 256;
+constexpr int NARROW_THREADS = 512;
 constexpr uint32_t NARROW_TILE_LIMIT = 5;        // tiles of 128 per CTA at short sides up to 64
 constexpr uint32_t NARROW_MAX_CLUSTER = 8;
 
@@ -769,14 +805,16 @@ __device__ __forceinline__ void peer_store(uint32_t a, uint4 v)
 {
     asm volatile("st.shared::cluster.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
-__device__ __forceinline__ void tmem_load8(uint32_t addr, float (&v)[8])
+__device__ __forceinline__ void tmem_load16(uint32_t addr, float (&v)[2][8])
 {
-    uint32_t u[8];
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]) : "r"(addr));
+    uint32_t u[16];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]),
+                   "=r"(u[8]), "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15])
+                 : "r"(addr));
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(u[i]);
+    for (int i = 0; i < 16; ++i) v[i >> 3][i & 7] = __uint_as_float(u[i]);
 }
 // 8 numbers as hi and lo fp16
 __device__ __forceinline__ void split8(const float (&x)[8], uint4 &hi, uint4 &lo)
@@ -803,7 +841,7 @@ __device__ __forceinline__ void join8(uint4 hi, uint4 lo, float (&x)[8])
 }
 
 // Shared memory, each part 1024-byte aligned: X hi, X lo (64 columns of the short side per block: rows of
-// 128 bytes, tiles * 128 of them), then A or B hi, lo (blocks of 128 rows), then this CTA's part of A in fp32.
+// 128 bytes, tiles * 128 of them), then A or P hi, lo (blocks of 128 rows), then this CTA's part of A in fp32.
 struct NarrowLayout {
     uint32_t blocks, x_block, x, ab, part, total;
     __host__ __device__ NarrowLayout(uint32_t side, uint32_t tiles)
@@ -820,7 +858,6 @@ struct NarrowLayout {
 // Dynamic shared memory is rounded up to this, so that an SM never holds two of these CTAs: each takes all of
 // the tensor memory, and CTAs of two clusters waiting for each other's would wait for good.
 constexpr uint32_t NARROW_MIN_SMEM = 120 * 1024;
-static_assert(NARROW_THREADS == INGEST_THREADS, "block_sum");
 
 // Smallest power of two of CTAs that gives each one tile, at most NARROW_MAX_CLUSTER.
 uint32_t narrow_cluster(uint32_t n)
@@ -839,7 +876,7 @@ narrow_kernel(const NarrowArgs g, const Source<T> src)
 {
     extern __shared__ uint8_t raw[];
     __shared__ NarrowControl ctl;
-    const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31, quad = wid & 3, half = wid >> 2;
+    const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31, quad = wid & 3, part_of = wid >> 2;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const uint32_t rank = C == 1 ? 0 : blockIdx.x % C;
     const Mat &M = g.mats[g.list[blockIdx.x / C]];
@@ -866,26 +903,60 @@ narrow_kernel(const NarrowArgs g, const Source<T> src)
     // ---- momentum and norm
     auto place = [&](uint32_t i, uint32_t j) { return M.offset + (tall ? j * M.stride + i : i * M.stride + j); };
     const bool update = src.mom && src.in && !M.spread;
-    double sum = 0;
-    // consecutive threads along what is consecutive in memory
-    const uint32_t fast = tall ? m : count, total = m * count;
-    for (uint32_t e = tid; e < total; e += NARROW_THREADS) {
-        const uint32_t q = e / fast, p = e - q * fast;
-        const uint64_t at = tall ? place(p, j0 + q) : place(q, j0 + p);
-        float y;
-        if (update) {
-            const float x = src.input(at), mo = __fmaf_rn(src.mu, src.mom[at], x);
-            src.mom[at] = mo;
-            y = src.nesterov ? __fmaf_rn(src.mu, mo, x) : mo;
-        } else {
-            y = src.direction(at);
-        }
-        sum = __fma_rn(static_cast<double>(y), static_cast<double>(y), sum);
-    }
-    sum = block_sum(sum);
-    if (tid == 0) ctl.sum = sum;
     // X starts as zeros: what lies beyond the matrix stays zero
     for (uint32_t b = tid * 16; b < 2 * L.x + 2 * L.ab; b += NARROW_THREADS * 16) sts16(base + b, make_uint4(0, 0, 0, 0));
+    __syncthreads();
+    // Consecutive threads along what is consecutive in memory, LOADS entries of a thread in flight.  The
+    // entries wait in the places of their hi and lo for the norm, upper and lower half of the fp32 number.
+    constexpr uint32_t LOADS = 8;
+    const uint32_t fast = max(1u, tall ? m : count), total = m * count;
+    const uint32_t dq = NARROW_THREADS / fast, dp = NARROW_THREADS % fast;
+    auto walk = [&](uint32_t &q, uint32_t &p) {
+        q += dq;
+        p += dp;
+        if (p >= fast) { p -= fast; q += 1; }
+    };
+    auto spot = [&](uint32_t q, uint32_t p) {
+        const uint32_t i = tall ? p : q, j = tall ? q : p;
+        return (i >> 6) * L.x_block + j * 128 + ((((i & 63) >> 3) ^ (j & 7)) << 4) + (i & 7) * 2;
+    };
+    double sum = 0;
+    uint32_t q0 = tid / fast, p0 = tid % fast;
+    for (uint32_t e = tid; e < total; e += NARROW_THREADS * LOADS) {
+        uint32_t q = q0, p = p0;
+        float x[LOADS], mo[LOADS];
+#pragma unroll
+        for (uint32_t u = 0; u < LOADS; ++u) {
+            x[u] = mo[u] = 0.f;
+            if (e + u * NARROW_THREADS < total) {
+                const uint64_t at = tall ? place(p, j0 + q) : place(q, j0 + p);
+                x[u] = src.input(at);
+                if (src.mom) mo[u] = src.mom[at];
+            }
+            walk(q, p);
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < LOADS; ++u) {
+            if (e + u * NARROW_THREADS < total) {
+                float y = x[u];
+                if (src.mom) {
+                    float mu_x = mo[u];
+                    if (update) {
+                        mu_x = __fmaf_rn(src.mu, mo[u], x[u]);
+                        src.mom[tall ? place(p0, j0 + q0) : place(q0, j0 + p0)] = mu_x;
+                    }
+                    y = src.nesterov ? __fmaf_rn(src.mu, mu_x, x[u]) : mu_x;
+                }
+                sum = __fma_rn(static_cast<double>(y), static_cast<double>(y), sum);
+                const uint32_t at = spot(q0, p0), w = __float_as_uint(y);
+                asm volatile("st.shared.b16 [%0], %1;" :: "r"(x_hi + at), "h"(static_cast<unsigned short>(w >> 16)) : "memory");
+                asm volatile("st.shared.b16 [%0], %1;" :: "r"(x_lo + at), "h"(static_cast<unsigned short>(w)) : "memory");
+            }
+            walk(q0, p0);
+        }
+    }
+    sum = block_sum<NARROW_THREADS>(sum);
+    if (tid == 0) ctl.sum = sum;
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -899,15 +970,23 @@ narrow_kernel(const NarrowArgs g, const Source<T> src)
             sum += s;
         }
     }
-    const double inv = static_cast<double>(SCALE) / (sqrt(sum) + static_cast<double>(g.eps));
-    for (uint32_t e = tid; e < total; e += NARROW_THREADS) {
-        const uint32_t q = e / fast, p = e - q * fast;
-        const uint32_t i = tall ? p : q, j = tall ? q : p;
-        const float x = static_cast<float>(static_cast<double>(src.direction(place(i, j0 + j))) * inv);
-        const __half h = __float2half_rn(x), l = __float2half_rn(x - __half2float(h));
-        const uint32_t at = (i >> 6) * L.x_block + j * 128 + ((((i & 63) >> 3) ^ (j & 7)) << 4) + (i & 7) * 2;
-        asm volatile("st.shared.b16 [%0], %1;" :: "r"(x_hi + at), "h"(__half_as_ushort(h)) : "memory");
-        asm volatile("st.shared.b16 [%0], %1;" :: "r"(x_lo + at), "h"(__half_as_ushort(l)) : "memory");
+    const double inv = static_cast<double>(X_SCALE) / (sqrt(sum) + static_cast<double>(g.eps));
+    const uint32_t units = side / 8;                             // 8 columns each
+    for (uint32_t e = tid; e < count * units; e += NARROW_THREADS) {
+        const uint32_t u = e / count, j = e - u * count;
+        const uint32_t at = (u >> 3) * L.x_block + j * 128 + (((u & 7) ^ (j & 7)) << 4);
+        const uint4 a = lds16(x_hi + at), b = lds16(x_lo + at);
+        const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = static_cast<float>(static_cast<double>(__uint_as_float((aw[i] << 16) | (bw[i] & 0xFFFFu))) * inv);
+            x[2 * i + 1] = static_cast<float>(static_cast<double>(__uint_as_float((aw[i] & 0xFFFF0000u) | (bw[i] >> 16))) * inv);
+        }
+        uint4 hi, lo;
+        split8(x, hi, lo);
+        sts16(x_hi + at, hi);
+        sts16(x_lo + at, lo);
     }
 
     // ---- steps
@@ -915,7 +994,7 @@ narrow_kernel(const NarrowArgs g, const Source<T> src)
     bool ok = true;
     // every thread's writes to the operands, then the products of thread 0, then everyone waits for them
     auto products = [&](auto issue) {
-        asm volatile("fence.proxy.async;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         __syncthreads();
         if (tid == 0) {
@@ -931,142 +1010,157 @@ narrow_kernel(const NarrowArgs g, const Source<T> src)
     };
     const uint32_t row_tmem = tmem + (static_cast<uint32_t>(quad * 32) << 16);
     const uint32_t d_apply = 128;                                // columns 0 .. 127: A, A^2;  from 128: products with X
-    const uint32_t units = side / 8;                             // 8 columns each
-    const uint32_t i_row = quad * 32 + lane;                     // this thread's row of A and B
+    const uint32_t groups = side / 16;                           // 16 columns each: what a warp takes at a time
+    const uint32_t i_row = quad * 32 + lane;                     // this thread's row of A and P
     const uint32_t idesc = (1u << 4) | ((side >> 3) << 17) | ((128 >> 4) << 24);
-    const float last_scale = M.scale * INV_SCALE;
+    // A's operands have the short side consecutive; with one block of it, rows beyond repeat the first
+    const uint64_t lbo = static_cast<uint64_t>(L.blocks == 2 ? L.x_block >> 4 : 0) << 16;
+    const uint64_t gram_hi = (operand_desc(x_hi, false) & ~(0x3FFFull << 16)) | lbo;
+    const uint64_t gram_lo = (operand_desc(x_lo, false) & ~(0x3FFFull << 16)) | lbo;
+    const uint64_t ap_hi = operand_desc(ab_hi, false), ap_lo = operand_desc(ab_lo, false);
+    auto unit_at = [&](uint32_t u, uint32_t row, uint32_t block) { return (u >> 3) * block + row * 128 + (((u & 7) ^ (row & 7)) << 4); };
 #pragma unroll 1
     for (uint32_t st = 0; st < g.steps; ++st) {
         const float ca = g.coef[3 * st], cb = g.coef[3 * st + 1], cc = g.coef[3 * st + 2];
-        // A: both operands have the short side consecutive; rows beyond it repeat the first block
         products([&]() {
-            uint32_t acc = 0;
-            const uint64_t lbo = static_cast<uint64_t>(L.blocks == 2 ? L.x_block >> 4 : 0) << 16;
-            const uint64_t dh = (operand_desc(x_hi, false) & ~(0x3FFFull << 16)) | lbo;
-            const uint64_t dl = (operand_desc(x_lo, false) & ~(0x3FFFull << 16)) | lbo;
-            for (int pass = 0; pass < 3; ++pass)
-                for (uint32_t k = 0; k < tiles * 8; ++k) {
-                    mma<1>(tmem, (pass == 2 ? dl : dh) + k * 128, (pass == 1 ? dl : dh) + k * 128, idesc | (3u << 15), acc);
-                    acc = 1;
-                }
+#pragma unroll 4
+            for (uint32_t k = 0; k < tiles * 8; ++k) {
+                mma<1>(tmem, gram_hi + k * 128, gram_hi + k * 128, idesc | (3u << 15), k);
+                mma<1>(tmem, gram_hi + k * 128, gram_lo + k * 128, idesc | (3u << 15), 1);
+                mma<1>(tmem, gram_lo + k * 128, gram_hi + k * 128, idesc | (3u << 15), 1);
+            }
         });
-        if (C == 1) {
-            for (uint32_t u = half; u < units; u += 2) {
-                float v[8];
-                __syncwarp();
-                tmem_load8(row_tmem + u * 8, v);
-                if (i_row < side) {
+        for (uint32_t q = part_of; q < groups; q += NARROW_THREADS / 128) {
+            float v[2][8] = {};
+            __syncwarp();
+            if (tiles) tmem_load16(row_tmem + q * 16, v);
+            if (i_row >= side) continue;
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) v[q] *= INV_SCALE;
+            for (uint32_t k = 0; k < 2; ++k) {
+                const uint32_t u = q * 2 + k;
+                if (C == 1) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[k][e] *= XX_TO_A;
                     uint4 hi, lo;
-                    split8(v, hi, lo);
-                    const uint32_t at = (u >> 3) * (128 * 128) + i_row * 128 + (((u & 7) ^ (i_row & 7)) << 4);
-                    sts16(ab_hi + at, hi);
-                    sts16(ab_lo + at, lo);
-                }
-            }
-        } else {
-            for (uint32_t u = half; u < units; u += 2) {
-                float v[8];
-                __syncwarp();
-                if (tiles) tmem_load8(row_tmem + u * 8, v);
-                else
+                    split8(v[k], hi, lo);
+                    sts16(ab_hi + unit_at(u, i_row, 128 * 128), hi);
+                    sts16(ab_lo + unit_at(u, i_row, 128 * 128), lo);
+                } else {
+                    // 16-byte units of a row permuted within groups of 4: few bank conflicts between rows
+                    const uint32_t perm = i_row & 3, at = part + i_row * side * 4;
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) v[q] = 0.f;
-                if (i_row < side) {
-                    // 16-byte units of a row permuted within groups of 8 (or 4): no bank conflicts between rows
-                    const uint32_t perm = i_row & 3;
-                    const uint32_t at = part + i_row * side * 4;
-                    sts16(at + (((2 * u) ^ perm) << 4), make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));
-                    sts16(at + (((2 * u + 1) ^ perm) << 4), make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])));
+                    for (uint32_t e = 0; e < 2; ++e)
+                        sts16(at + (((2 * u + e) ^ perm) << 4),
+                              make_uint4(__float_as_uint(v[k][4 * e]), __float_as_uint(v[k][4 * e + 1]),
+                                         __float_as_uint(v[k][4 * e + 2]), __float_as_uint(v[k][4 * e + 3])));
                 }
             }
+        }
+        if (C > 1) {
             cluster_sync();
             for (uint32_t e = rank * NARROW_THREADS + tid; e < side * units; e += C * NARROW_THREADS) {
                 const uint32_t i = e / units, u = e - i * units, perm = i & 3;
                 const uint32_t at = part + i * side * 4;
-                float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+                float4 a[C], b[C];
 #pragma unroll
                 for (uint32_t o = 0; o < C; ++o) {
                     const uint32_t p = peer_addr(at, o);
-                    const float4 a = peer_load(p + (((2 * u) ^ perm) << 4)), b = peer_load(p + (((2 * u + 1) ^ perm) << 4));
-                    v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
-                    v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+                    a[o] = peer_load(p + (((2 * u) ^ perm) << 4));
+                    b[o] = peer_load(p + (((2 * u + 1) ^ perm) << 4));
+                }
+                float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+                for (uint32_t o = 0; o < C; ++o) {
+                    v[0] += a[o].x; v[1] += a[o].y; v[2] += a[o].z; v[3] += a[o].w;
+                    v[4] += b[o].x; v[5] += b[o].y; v[6] += b[o].z; v[7] += b[o].w;
                 }
 #pragma unroll
-                for (int q = 0; q < 8; ++q) v[q] *= INV_SCALE;
+                for (int k = 0; k < 8; ++k) v[k] *= XX_TO_A;
                 uint4 hi, lo;
                 split8(v, hi, lo);
-                const uint32_t to = (u >> 3) * (128 * 128) + i * 128 + (((u & 7) ^ (i & 7)) << 4);
+                const uint32_t to = unit_at(u, i, 128 * 128);
 #pragma unroll
                 for (uint32_t o = 0; o < C; ++o) {
                     peer_store(peer_addr(ab_hi + to, o), hi);
                     peer_store(peer_addr(ab_lo + to, o), lo);
                 }
             }
-            asm volatile("fence.proxy.async;" ::: "memory");
+            asm volatile("fence.proxy.async.shared::cluster;" ::: "memory");
             cluster_sync();
         }
-        // A^2, then B in the place of A
-        const uint64_t ah = operand_desc(ab_hi, false), al = operand_desc(ab_lo, false);
-        auto at_k = [](uint64_t d, uint32_t k, uint32_t block) { return d + (k >> 2) * (block >> 4) + (k & 3) * 2; };
+        // A^2, then P in the place of A
         products([&]() {
-            for (int pass = 0; pass < 3; ++pass)
-                for (uint32_t k = 0; k < side / 16; ++k)
-                    mma<1>(tmem, at_k(pass == 2 ? al : ah, k, 128 * 128), at_k(pass == 1 ? al : ah, k, 128 * 128), idesc,
-                           (pass | k) != 0);
+#pragma unroll 2
+            for (uint32_t k = 0; k < groups; ++k) {
+                const uint64_t d = static_cast<uint64_t>((k >> 2) * (128 * 128 >> 4) + (k & 3) * 2);
+                mma<1>(tmem, ap_hi + d, ap_hi + d, idesc, k);
+                mma<1>(tmem, ap_hi + d, ap_lo + d, idesc, 1);
+                mma<1>(tmem, ap_lo + d, ap_hi + d, idesc, 1);
+            }
         });
-        for (uint32_t u = half; u < units; u += 2) {
-            float v[8];
+        for (uint32_t q = part_of; q < groups; q += NARROW_THREADS / 128) {
+            float v[2][8];
             __syncwarp();
-            tmem_load8(row_tmem + u * 8, v);
-            if (i_row < side) {
-                const uint32_t at = (u >> 3) * (128 * 128) + i_row * 128 + (((u & 7) ^ (i_row & 7)) << 4);
+            tmem_load16(row_tmem + q * 16, v);
+            if (i_row >= side) continue;
+#pragma unroll
+            for (uint32_t k = 0; k < 2; ++k) {
+                const uint32_t u = q * 2 + k, at = unit_at(u, i_row, 128 * 128);
                 float x[8];
                 join8(lds16(ab_hi + at), lds16(ab_lo + at), x);
 #pragma unroll
-                for (int q = 0; q < 8; ++q) x[q] = __fmaf_rn(cc, v[q] * INV_SCALE, cb * x[q]);
+                for (uint32_t e = 0; e < 8; ++e) {
+                    x[e] = __fmaf_rn(cc * AA_TO_P, v[k][e], (cb * A_TO_P) * x[e]);
+                    if (u * 8 + e == i_row) x[e] += ca * P_SCALE;
+                }
                 uint4 hi, lo;
                 split8(x, hi, lo);
                 sts16(ab_hi + at, hi);
                 sts16(ab_lo + at, lo);
             }
         }
-        // X B, tile by tile
+        // X P, tile by tile
         products([&]() {
             for (uint32_t t = 0; t < tiles; ++t) {
                 const uint64_t xh = operand_desc(x_hi + t * (128 * 128), false), xl = operand_desc(x_lo + t * (128 * 128), false);
-                for (int pass = 0; pass < 3; ++pass)
-                    for (uint32_t k = 0; k < side / 16; ++k)
-                        mma<1>(tmem + d_apply + t * side, at_k(pass == 2 ? xl : xh, k, L.x_block),
-                               at_k(pass == 1 ? al : ah, k, 128 * 128), idesc, (pass | k) != 0);
+#pragma unroll 2
+                for (uint32_t k = 0; k < groups; ++k) {
+                    const uint64_t dx = static_cast<uint64_t>((k >> 2) * (L.x_block >> 4) + (k & 3) * 2);
+                    const uint64_t dp = static_cast<uint64_t>((k >> 2) * (128 * 128 >> 4) + (k & 3) * 2);
+                    mma<1>(tmem + d_apply + t * side, xh + dx, ap_hi + dp, idesc, k);
+                    mma<1>(tmem + d_apply + t * side, xh + dx, ap_lo + dp, idesc, 1);
+                    mma<1>(tmem + d_apply + t * side, xl + dx, ap_hi + dp, idesc, 1);
+                }
             }
         });
         const bool last = st + 1 == g.steps;
-        for (uint32_t w = half; w < tiles * units; w += 2) {
-            const uint32_t t = w / units, u = w - t * units;
-            float v[8];
+        const float last_scale = M.scale * (INV_X_SCALE * INV_P_SCALE);
+        for (uint32_t w = part_of; w < tiles * groups; w += NARROW_THREADS / 128) {
+            const uint32_t t = w / groups, q = w - t * groups;
+            float v[2][8];
             __syncwarp();
-            tmem_load8(row_tmem + d_apply + t * side + u * 8, v);
+            tmem_load16(row_tmem + d_apply + t * side + q * 16, v);
             const uint32_t j = t * 128 + i_row;
-            const uint32_t at = (u >> 3) * L.x_block + j * 128 + (((u & 7) ^ (j & 7)) << 4);
-            float x[8];
-            join8(lds16(x_hi + at), lds16(x_lo + at), x);
 #pragma unroll
-            for (int q = 0; q < 8; ++q) x[q] = __fmaf_rn(ca, x[q], v[q] * INV_SCALE);
-            if (!last) {
-                uint4 hi, lo;
-                split8(x, hi, lo);
-                sts16(x_hi + at, hi);
-                sts16(x_lo + at, lo);
-            } else if (j < count) {
+            for (uint32_t k = 0; k < 2; ++k) {
+                const uint32_t u = q * 2 + k;
+                if (!last) {
 #pragma unroll
-                for (uint32_t q = 0; q < 8; ++q) {
-                    const uint32_t i = u * 8 + q;
-                    if (i >= m) break;
-                    const uint64_t p = place(i, j0 + j);
-                    if (g.params) g.params[p] = __fmaf_rn(-g.lr, last_scale * x[q], g.decay * g.params[p]);
-                    else g.out[p] = __float2bfloat16_rn(last_scale * x[q]);
+                    for (int e = 0; e < 8; ++e) v[k][e] *= INV_P_SCALE;
+                    uint4 hi, lo;
+                    split8(v[k], hi, lo);
+                    const uint32_t at = unit_at(u, j, L.x_block);
+                    sts16(x_hi + at, hi);
+                    sts16(x_lo + at, lo);
+                } else if (j < count) {
+#pragma unroll
+                    for (uint32_t e = 0; e < 8; ++e) {
+                        const uint32_t i = u * 8 + e;
+                        if (i >= m) break;
+                        const uint64_t p = place(i, j0 + j);
+                        if (g.params) g.params[p] = __fmaf_rn(-g.lr, last_scale * v[k][e], g.decay * g.params[p]);
+                        else g.out[p] = __float2bfloat16_rn(last_scale * v[k][e]);
+                    }
                 }
             }
         }
@@ -1155,44 +1249,43 @@ EncodeFn encode_function()
     return reinterpret_cast<EncodeFn>(fn);
 }
 
-// A row-major fp16 matrix in boxes of 64 columns; outside of it zeros are read and nothing is written.
-bool encode(EncodeFn fn, CUtensorMap *map, void *base, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t box_rows = 64)
+// A row-major fp16 matrix in boxes of 64 or 32 columns; outside of it zeros are read and nothing is written.
+bool encode(EncodeFn fn, CUtensorMap *map, void *base, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t box_cols,
+            uint32_t box_rows)
 {
     const cuuint64_t dims[2] = {cols, rows}, strides[1] = {ld * 2};
-    const cuuint32_t box[2] = {64, box_rows}, step[2] = {1, 1};
-    if (box_rows == 64 && !encode(fn, map + BOX32, base, rows, cols, ld, 32)) return false;
+    const cuuint32_t box[2] = {box_cols, box_rows}, step[2] = {1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, base, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 uint64_t round_up(uint64_t v, uint64_t to) { return (v + to - 1) / to * to; }
 
-// The polynomials, in order, on [0, 1]: largest singular value met and largest |b t + c t^2| on the way.
+// The polynomials, in order, on [0, 1]: largest singular value met and largest |a + b t + c t^2| on the way.
 bool coefficients_fit(const float *coef, uint32_t steps)
 {
     double top = 1.0;
     for (uint32_t i = 0; i < steps; ++i) {
         const double a = coef[3 * i], b = coef[3 * i + 1], c = coef[3 * i + 2];
-        if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
-        if (top > MAX_SIGMA) return false;
-        // extrema of x (a + b x^2 + c x^4): a + 3 b t + 5 c t^2 = 0;  of b t + c t^2: t = -b / 2c
-        double at[4] = {top, 0, 0, 0};
+        if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c) || top > MAX_SIGMA) return false;
+        // ends, extrema of x (a + b x^2 + c x^4): a + 3 b t + 5 c t^2 = 0, and of a + b t + c t^2: t = -b / 2c
+        double at[5] = {0, top, 0, 0, 0};
         const double disc = 9 * b * b - 20 * a * c;
         if (c != 0 && disc >= 0) {
             const double t1 = (-3 * b + sqrt(disc)) / (10 * c), t2 = (-3 * b - sqrt(disc)) / (10 * c);
-            if (t1 > 0) at[1] = sqrt(t1);
-            if (t2 > 0) at[2] = sqrt(t2);
+            if (t1 > 0) at[2] = sqrt(t1);
+            if (t2 > 0) at[3] = sqrt(t2);
         } else if (c == 0 && b != 0 && -a / (3 * b) > 0) {
-            at[1] = sqrt(-a / (3 * b));
+            at[2] = sqrt(-a / (3 * b));
         }
-        if (c != 0 && -b / (2 * c) > 0) at[3] = sqrt(-b / (2 * c));
+        if (c != 0 && -b / (2 * c) > 0) at[4] = sqrt(-b / (2 * c));
         double next = 0;
         for (double x : at) {
             if (x > top) continue;
-            const double t = x * x;
-            if (fabs(b * t + c * t * t) > MAX_B) return false;
-            next = std::max(next, fabs(x * (a + b * t + c * t * t)));
+            const double t = x * x, p = a + b * t + c * t * t;
+            if (fabs(p) > MAX_P) return false;
+            next = std::max(next, fabs(x * p));
         }
         top = next;
     }
@@ -1321,7 +1414,7 @@ deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, ui
         M.n = std::max(q.rows, q.cols);
         M.ldx = static_cast<uint32_t>(round_up(q.cols, 8));
         M.lda = static_cast<uint32_t>(round_up(M.m, 8));
-        M.precision = M.m <= FULL_SIDE ? FULL : M.m <= WIDE_B_SIDE ? WIDE_B : PLAIN;
+        M.precision = M.m <= FULL_SIDE ? FULL : M.m <= WIDE_P_SIDE ? WIDE_P : PLAIN;
         M.spread = q.row_stride != q.cols && q.rows > 1;
         const double r = q.rows, c = q.cols;
         M.scale = scale == DECO_ORTH_SCALE_SPECTRAL ? static_cast<float>(sqrt(std::max(1.0, r / c)))
@@ -1372,17 +1465,25 @@ deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, ui
         auto take = [&](uint64_t b) { __half *p = reinterpret_cast<__half *>(h->workspace + at); at += b; return p; };
         for (int k = 0; k < 2; ++k) { M.hi[k] = take(xb); M.lo[k] = take(xb); }
         M.a = take(ab);
-        M.b = take(ab);
-        M.b_lo = M.precision >= WIDE_B ? take(ab) : nullptr;
+        M.p = take(ab);
+        M.p_lo = M.precision >= WIDE_P ? take(ab) : nullptr;
         M.a_lo = M.precision == FULL ? take(ab) : nullptr;
         CUtensorMap *map = &maps[static_cast<uint64_t>(MAPS) * i];
         bool ok = true;
-        for (int k = 0; k < 2; ++k)
-            ok = ok && encode(enc, map + MAP_X + 2 * k, M.hi[k], M.rows, M.cols, M.ldx) &&
-                 encode(enc, map + MAP_X + 2 * k + 1, M.lo[k], M.rows, M.cols, M.ldx);
-        ok = ok && encode(enc, map + MAP_A, M.a, M.m, M.m, M.lda) && encode(enc, map + MAP_B, M.b, M.m, M.m, M.lda);
-        if (M.a_lo) ok = ok && encode(enc, map + MAP_A + 1, M.a_lo, M.m, M.m, M.lda);
-        if (M.b_lo) ok = ok && encode(enc, map + MAP_B + 1, M.b_lo, M.m, M.m, M.lda);
+        auto both = [&](int which, __half *p, uint32_t rows, uint32_t cols, uint32_t ld) {
+            ok = ok && (!p || (encode(enc, map + which, p, rows, cols, ld, 64, 64) &&
+                               encode(enc, map + BOX32 + which, p, rows, cols, ld, 64, 32)));
+        };
+        for (int k = 0; k < 2; ++k) {
+            both(MAP_X + 2 * k, M.hi[k], M.rows, M.cols, M.ldx);
+            both(MAP_X + 2 * k + 1, M.lo[k], M.rows, M.cols, M.ldx);
+        }
+        both(MAP_A, M.a, M.m, M.m, M.lda);
+        both(MAP_A + 1, M.a_lo, M.m, M.m, M.lda);
+        both(MAP_P, M.p, M.m, M.m, M.lda);
+        both(MAP_P + 1, M.p_lo, M.m, M.m, M.lda);
+        ok = ok && encode(enc, map + MIRROR_A, M.a, M.m, M.m, M.lda, 32, 64) &&
+             encode(enc, map + MIRROR_P, M.p, M.m, M.m, M.lda, 32, 64);
         if (!ok) return DECO_ERR_CUDA;
     }
     // pieces: matrices whose rows are back to back, in order of their place; then everything else
@@ -1603,7 +1704,7 @@ cudaError_t run_pass(deco_orth *h, const Source<T> &src, __nv_bfloat16 *out, flo
         for (uint32_t i = 0; i < h->steps && err == cudaSuccess; ++i) {
             const bool last = i + 1 == h->steps;
             g.src = i & 1;
-            g.read_lo = !last || h->steps == 1;
+            g.read_lo = !last || h->steps == 1;                  // (see the numbers above)
             g.write_lo = i + 2 < h->steps;
             g.a = h->coef[3 * i];
             g.b = h->coef[3 * i + 1];
