@@ -31,7 +31,9 @@
 
 #include <algorithm>
 #include <cmath>
+#include <functional>
 #include <new>
+#include <queue>
 #include <vector>
 
 #include "deco_internal.h"
@@ -112,6 +114,15 @@ __device__ double block_sum(double v)
     return v;
 }
 
+__device__ __forceinline__ float4 read4(const float *p) { return *reinterpret_cast<const float4 *>(p); }
+__device__ __forceinline__ float4 read4(const __nv_bfloat16 *p)
+{
+    const uint2 w = *reinterpret_cast<const uint2 *>(p);
+    return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u), __uint_as_float(w.y << 16),
+                       __uint_as_float(w.y & 0xFFFF0000u));
+}
+__device__ __forceinline__ float4 scaled(float4 v, float w) { return make_float4(w * v.x, w * v.y, w * v.z, w * v.w); }
+
 // What a pass takes in: an input vector, a momentum buffer, or both.
 template <typename T>
 struct Source {
@@ -121,6 +132,21 @@ struct Source {
     float mu;
     int nesterov;
     __device__ __forceinline__ float input(uint64_t i) const { return in ? weight * to_f<T>(in[i]) : 0.f; }
+    // whether entries i .. i + 3 can be read at once from every array there is
+    __device__ __forceinline__ bool wide(uint64_t i) const
+    {
+        return (reinterpret_cast<uintptr_t>(in + i) & (4 * sizeof(T) - 1)) * (in != nullptr) == 0 &&
+               (reinterpret_cast<uintptr_t>(mom + i) & 15u) * (mom != nullptr) == 0;
+    }
+    __device__ __forceinline__ float4 input4(uint64_t i) const { return in ? scaled(read4(in + i), weight) : make_float4(0, 0, 0, 0); }
+    __device__ __forceinline__ float4 direction4(uint64_t i) const
+    {
+        if (!mom) return input4(i);
+        const float4 m = read4(mom + i);
+        if (!nesterov) return m;
+        const float4 x = input4(i);
+        return make_float4(__fmaf_rn(mu, m.x, x.x), __fmaf_rn(mu, m.y, x.y), __fmaf_rn(mu, m.z, x.z), __fmaf_rn(mu, m.w, x.w));
+    }
     // the direction at entry i, the momentum having been updated
     __device__ __forceinline__ float direction(uint64_t i) const
     {
@@ -130,24 +156,60 @@ struct Source {
     }
 };
 
-// M <- mu M + in over a piece, and the sum of squares of the direction in double.
+// M <- mu M + in over a piece, and the sum of squares of the direction in double (it neither overflows nor
+// loses small entries).  Bound by memory: 12 bytes an entry with fp32 input and momentum.
 template <typename T>
 __global__ void __launch_bounds__(INGEST_THREADS)
 ingest_kernel(const Piece *pieces, const Source<T> src, double *partial)
 {
+    constexpr int FLIGHT = 4;            // 16-byte reads of a thread under way
     const Piece p = pieces[blockIdx.x];
+    const bool update = src.mom && src.in;
     double sum = 0;
-    for (uint32_t j = threadIdx.x; j < p.count; j += INGEST_THREADS) {
-        const uint64_t i = p.offset + j;
-        float y;
-        if (src.mom && src.in) {
-            const float x = src.input(i), m = __fmaf_rn(src.mu, src.mom[i], x);
-            src.mom[i] = m;
-            y = src.nesterov ? __fmaf_rn(src.mu, m, x) : m;
-        } else {
-            y = src.direction(i);
+    auto take = [&](float y) { sum = __fma_rn(static_cast<double>(y), static_cast<double>(y), sum); };
+    auto single = [&](uint64_t i) {
+        if (!update) return take(src.direction(i));
+        const float x = src.input(i), m = __fmaf_rn(src.mu, src.mom[i], x);
+        src.mom[i] = m;
+        take(src.nesterov ? __fmaf_rn(src.mu, m, x) : m);
+    };
+    // entries before the first place where every array is aligned (none of them aligned together: all)
+    uint32_t head = 0;
+    while (head < 4 && head < p.count && !src.wide(p.offset + head)) ++head;
+    if (head == 4) head = p.count;
+    const uint32_t quads = (p.count - head) / 4;
+    for (uint32_t j = threadIdx.x; j < head; j += INGEST_THREADS) single(p.offset + j);
+    for (uint32_t j = head + 4 * quads + threadIdx.x; j < p.count; j += INGEST_THREADS) single(p.offset + j);
+    const uint64_t first = p.offset + head;
+    for (uint32_t q0 = threadIdx.x; q0 < quads; q0 += INGEST_THREADS * FLIGHT) {
+        float4 x[FLIGHT], m[FLIGHT];
+#pragma unroll
+        for (int f = 0; f < FLIGHT; ++f) {
+            const uint32_t q = q0 + f * INGEST_THREADS;
+            if (q >= quads) continue;
+            x[f] = src.input4(first + 4ull * q);
+            if (src.mom) m[f] = read4(src.mom + first + 4ull * q);
         }
-        sum = __fma_rn(static_cast<double>(y), static_cast<double>(y), sum);
+#pragma unroll
+        for (int f = 0; f < FLIGHT; ++f) {
+            const uint32_t q = q0 + f * INGEST_THREADS;
+            if (q >= quads) continue;
+            float4 y = x[f];
+            if (src.mom) {
+                if (update) {
+                    m[f] = make_float4(__fmaf_rn(src.mu, m[f].x, x[f].x), __fmaf_rn(src.mu, m[f].y, x[f].y),
+                                       __fmaf_rn(src.mu, m[f].z, x[f].z), __fmaf_rn(src.mu, m[f].w, x[f].w));
+                    *reinterpret_cast<float4 *>(src.mom + first + 4ull * q) = m[f];
+                }
+                y = !src.nesterov ? m[f]
+                                  : make_float4(__fmaf_rn(src.mu, m[f].x, x[f].x), __fmaf_rn(src.mu, m[f].y, x[f].y),
+                                                __fmaf_rn(src.mu, m[f].z, x[f].z), __fmaf_rn(src.mu, m[f].w, x[f].w));
+            }
+            take(y.x);
+            take(y.y);
+            take(y.z);
+            take(y.w);
+        }
     }
     if (p.slot == NO_SLOT) return;
     sum = block_sum<INGEST_THREADS>(sum);
@@ -186,14 +248,37 @@ convert_kernel(const ConvertPiece *pieces, const Mat *mats, const Source<T> src,
     double sum = 0;
     for (uint32_t i = threadIdx.x; i < M.pieces; i += INGEST_THREADS) sum += partial[M.piece0 + i];
     const double inv = static_cast<double>(X_SCALE) / (sqrt(block_sum<INGEST_THREADS>(sum)) + static_cast<double>(eps));
-    const uint32_t w = min(M.cols - p.col0, CONVERT_COLS);
-    for (uint32_t e = threadIdx.x; e < p.rows * w; e += INGEST_THREADS) {
-        const uint32_t r = p.row0 + e / w, c = p.col0 + e % w;
-        const float x = static_cast<float>(static_cast<double>(src.direction(M.offset + r * M.stride + c)) * inv);
-        const __half h = __float2half_rn(x);
-        const uint64_t at = static_cast<uint64_t>(r) * M.ldx + c;
-        M.hi[0][at] = h;
-        M.lo[0][at] = __float2half_rn(x - __half2float(h));
+    const bool plain = inv > 1e-30 && inv < 1e30;                // the factor itself is an fp32 number
+    const float inv32 = static_cast<float>(inv);
+    // 8 columns at a time: rows of X start on 16 bytes, and their length is rounded up to 8
+    const uint32_t w = min(M.cols - p.col0, CONVERT_COLS), units = (w + 7) / 8;
+    for (uint32_t e = threadIdx.x; e < p.rows * units; e += INGEST_THREADS) {
+        const uint32_t r = p.row0 + e / units, c = p.col0 + (e % units) * 8;
+        const uint64_t from = M.offset + r * M.stride + c, to = static_cast<uint64_t>(r) * M.ldx + c;
+        float y[8];
+        if (c + 8 <= M.cols && src.wide(from)) {
+            const float4 a = src.direction4(from), b = src.direction4(from + 4);
+            y[0] = a.x; y[1] = a.y; y[2] = a.z; y[3] = a.w;
+            y[4] = b.x; y[5] = b.y; y[6] = b.z; y[7] = b.w;
+        } else {
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) y[j] = c + j < M.cols ? src.direction(from + j) : 0.f;
+        }
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float x[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                x[k] = plain ? y[2 * j + k] * inv32 : static_cast<float>(static_cast<double>(y[2 * j + k]) * inv);
+            const __half2 h = __floats2half2_rn(x[0], x[1]);
+            const float2 back = __half22float2(h);
+            const __half2 l = __floats2half2_rn(x[0] - back.x, x[1] - back.y);
+            hi[j] = *reinterpret_cast<const uint32_t *>(&h);
+            lo[j] = *reinterpret_cast<const uint32_t *>(&l);
+        }
+        *reinterpret_cast<uint4 *>(M.hi[0] + to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        *reinterpret_cast<uint4 *>(M.lo[0] + to) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
     }
 }
 
@@ -218,7 +303,7 @@ struct GemmArgs {
     const Mat *mats;
     const CUtensorMap *maps;             // [mat][MAPS]
     const Tile *tiles;
-    uint32_t n_tiles;
+    const uint32_t *starts;              // [CTAs or pairs + 1]
     int src;                             // which X holds the current iterate
     int read_lo, write_lo;
     float a, b, c;
@@ -448,7 +533,7 @@ gemm_kernel(const GemmArgs g)
     const int wid = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint32_t rank = 0;
     if (CG == 2) asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-    const uint32_t first = blockIdx.x / CG, step = gridDim.x / CG;
+    const uint32_t first = g.starts[blockIdx.x / CG], end = g.starts[blockIdx.x / CG + 1];
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
@@ -490,7 +575,7 @@ gemm_kernel(const GemmArgs g)
         if (lane == 0) {
             uint32_t it = 0, seen = 0xFFFFFFFFu;
             bool ok = true;
-            for (uint32_t t = first; ok && t < g.n_tiles; t += step) {
+            for (uint32_t t = first; ok && t < end; ++t) {
                 const Tile tl = g.tiles[t];
                 const Operands op = operands<P>(g, g.mats[tl.mat], tl.mat);
                 const int32_t ra = tl.tm * SIDE + rank * 128, rb = tl.tn * SIDE + rank * 128;
@@ -523,7 +608,7 @@ gemm_kernel(const GemmArgs g)
         if (lane == 0 && rank == 0) {
             uint32_t it = 0, n = 0;
             bool ok = true;
-            for (uint32_t t = first; ok && t < g.n_tiles; t += step, ++n) {
+            for (uint32_t t = first; ok && t < end; ++t, ++n) {
                 const Tile tl = g.tiles[t];
                 const Operands op = operands<P>(g, g.mats[tl.mat], tl.mat);
                 const uint32_t as = n & 1;
@@ -555,7 +640,7 @@ gemm_kernel(const GemmArgs g)
         constexpr uint32_t CHUNKS = SIDE / 2 / CHUNK;            // of this warp, per tile
         uint32_t n = 0, loads = 0;
         bool ok = true;
-        for (uint32_t t = first; ok && t < g.n_tiles; t += step, ++n) {
+        for (uint32_t t = first; ok && t < end; ++t, ++n) {
             const Tile tl = g.tiles[t];
             const Mat &M = g.mats[tl.mat];
             const uint32_t as = n & 1;
@@ -1216,6 +1301,7 @@ rest_kernel(const Piece *pieces, float *params, const float *m, float lr, float 
 // Work of one launch: where in the handle's list, how much, and by how many CTAs each.
 struct Span {
     uint32_t first, count, cg;
+    uint32_t starts, lanes;              // gemm_kernel: lane l takes tiles starts[l] .. starts[l + 1] - 1 of the launch
 };
 struct Group {
     uint32_t convert0, n_convert;        // in the handle's list
@@ -1315,7 +1401,7 @@ struct deco_orth {
     RowPiece *row_pieces = nullptr;
     ConvertPiece *convert = nullptr;
     Tile *tiles = nullptr;
-    uint32_t *narrow_list = nullptr;
+    uint32_t *starts = nullptr, *narrow_list = nullptr;
     double *partial = nullptr;
     uint32_t *status = nullptr;
     uint64_t device_bytes = 0, launches = 0;
@@ -1332,6 +1418,7 @@ void release(deco_orth *h)
     cudaFree(h->row_pieces);
     cudaFree(h->convert);
     cudaFree(h->tiles);
+    cudaFree(h->starts);
     cudaFree(h->narrow_list);
     cudaFree(h->partial);
     cudaFree(h->status);
@@ -1390,9 +1477,11 @@ bool layout_ok(uint64_t d, const std::vector<deco_matrix> &ms)
 
 uint32_t passes(const Mat &M, int phase) { return phase == APPLY ? 1 + M.precision : M.precision == FULL ? 3 : 1; }
 
-// Clock cycles of a tile of k products deep: 4096 multiply-adds per SM and cycle, of which tiles of one
-// CTA reach less (they read twice the shared memory per product), and the ends that do not overlap.
-double tile_cost(uint32_t cg, uint32_t k) { return cg == 1 ? 5.2 * k + 1500 : 8.4 * k + 2500; }
+// Clock cycles of a tile of k products deep.  An SM takes in 40 to 50 bytes of operands a cycle, 4 a row and
+// k: with 256 rows per CTA either way that is 10 to 13 cycles for each k of a tile, where the products take 4
+// (one CTA) or 8 (a pair); measured 13 for a lone CTA, 9 to 10 with all SMs at work on pairs of
+// CTAs.  Then the ends that do not overlap.
+double tile_cost(uint32_t cg, uint32_t k) { return cg == 1 ? 9.0 * k + 3000 : 10.0 * k + 4500; }
 
 deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, uint64_t cap)
 {
@@ -1426,7 +1515,7 @@ deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, ui
     }
     std::vector<uint32_t> narrow_list;
     for (uint32_t c = NARROW_MAX_CLUSTER; c >= 1; c /= 2) {
-        Span span = {static_cast<uint32_t>(narrow_list.size()), 0, c};
+        Span span = {static_cast<uint32_t>(narrow_list.size()), 0, c, 0, 0};
         for (uint32_t i = 0; i < n; ++i)
             if (is_narrow(mats[i].m, mats[i].n) && narrow_cluster(mats[i].n) == c) {
                 narrow_list.push_back(i);
@@ -1522,6 +1611,7 @@ deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, ui
     // tiles and convert pieces of each group, the longest products first
     std::vector<Tile> tiles;
     std::vector<ConvertPiece> convert;
+    std::vector<uint32_t> starts;
     for (uint32_t g = 0; g < groups; ++g) {
         Group G = {};
         G.convert0 = static_cast<uint32_t>(convert.size());
@@ -1541,31 +1631,46 @@ deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, ui
             auto depth = [&](uint32_t i) { return (phase == GRAM ? mats[i].n : mats[i].m) * passes(mats[i], phase); };
             std::stable_sort(by.begin(), by.end(), [&](uint32_t x, uint32_t y) { return depth(x) > depth(y); });
             double best = 0;
-            std::vector<Tile> chosen;
+            std::vector<std::vector<Tile>> chosen;
             for (uint32_t cg = 1; cg <= 2; ++cg) {
                 const uint32_t side = 128 * cg;
                 auto blocks = [&](uint32_t v) { return (v + side - 1) / side; };
-                std::vector<Tile> list;
-                std::vector<double> busy(h->sms / cg, 0.0);
+                // every tile, the longest first, to the lane that is free first
+                std::vector<std::vector<Tile>> lanes(h->sms / cg);
+                typedef std::pair<double, uint32_t> Load;
+                std::priority_queue<Load, std::vector<Load>, std::greater<Load>> free;
+                for (uint32_t l = 0; l < lanes.size(); ++l) free.push({0.0, l});
+                double cost = 0;
                 for (uint32_t i : by) {
                     const Mat &M = mats[i];
                     const uint32_t nr = blocks(phase == APPLY ? M.rows : M.m), nc = blocks(phase == APPLY ? M.cols : M.m);
                     for (uint32_t r = 0; r < nr; ++r)
                         for (uint32_t c = 0; c < (phase == APPLY ? nc : r + 1); ++c) {
-                            busy[list.size() % busy.size()] += tile_cost(cg, depth(i));
-                            list.push_back({i, static_cast<uint16_t>(r), static_cast<uint16_t>(c)});
+                            const Load at = free.top();
+                            free.pop();
+                            lanes[at.second].push_back({i, static_cast<uint16_t>(r), static_cast<uint16_t>(c)});
+                            free.push({at.first + tile_cost(cg, depth(i)), at.second});
+                            cost = std::max(cost, at.first + tile_cost(cg, depth(i)));
                         }
                 }
-                const double cost = *std::max_element(busy.begin(), busy.end());
                 if (cg == 1 || cost < best) {
                     best = cost;
-                    chosen.swap(list);
+                    chosen.swap(lanes);
                     G.phase[phase].cg = cg;
                 }
             }
-            G.phase[phase].first = static_cast<uint32_t>(tiles.size());
-            G.phase[phase].count = static_cast<uint32_t>(chosen.size());
-            tiles.insert(tiles.end(), chosen.begin(), chosen.end());
+            Span &span = G.phase[phase];
+            span.first = static_cast<uint32_t>(tiles.size());
+            span.starts = static_cast<uint32_t>(starts.size());
+            span.count = span.lanes = 0;
+            for (const std::vector<Tile> &l : chosen) {
+                if (l.empty()) continue;
+                starts.push_back(span.count);
+                tiles.insert(tiles.end(), l.begin(), l.end());
+                span.count += static_cast<uint32_t>(l.size());
+                span.lanes += 1;
+            }
+            starts.push_back(span.count);
         }
         h->groups.push_back(G);
     }
@@ -1573,7 +1678,7 @@ deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, ui
     std::vector<uint32_t> status(1, 0u);
     if (!upload(h, &h->mats, mats) || !upload(h, &h->maps, maps) || !upload(h, &h->pieces, pieces) ||
         !upload(h, &h->row_pieces, row_pieces) || !upload(h, &h->convert, convert) || !upload(h, &h->tiles, tiles) ||
-        !upload(h, &h->narrow_list, narrow_list) ||
+        !upload(h, &h->starts, starts) || !upload(h, &h->narrow_list, narrow_list) ||
         !upload(h, &h->partial, partial) || !upload(h, &h->status, status))
         return DECO_ERR_OOM;
     // the copies above may still be under way; the handle's first pass may come on any stream
@@ -1606,8 +1711,8 @@ template <Phase P, Target T>
 cudaError_t launch_gemm(deco_orth *h, GemmArgs g, const Span &span, cudaStream_t s)
 {
     g.tiles = h->tiles + span.first;
-    g.n_tiles = span.count;
-    const uint32_t grid = std::min(span.count, h->sms / span.cg) * span.cg;
+    g.starts = h->starts + span.starts;
+    const uint32_t grid = span.lanes * span.cg;
     return span.cg == 1 ? launch_after(h, gemm_kernel<1, P, T>, grid, GEMM_THREADS, GEMM_SMEM, 1, s, g)
                         : launch_after(h, gemm_kernel<2, P, T>, grid, GEMM_THREADS, GEMM_SMEM, 2, s, g);
 }
