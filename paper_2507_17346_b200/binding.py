@@ -199,6 +199,9 @@ def _ptr(x):
 def _stream(stream):
     if stream is None:
         import torch
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # 3 us less than a Stream object
+        if raw is not None and torch.cuda.is_initialized():
+            return raw(torch.cuda.current_device())
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, int):
         return stream
@@ -500,21 +503,35 @@ def deco_topk_compress_static(a, d, k, msg_out, stream=None):
 
 # ------------------------------------------------- log probabilities of given tokens
 
+_dtypes = {}                      # torch type -> its name; filled at the first call, torch being imported lazily
+
+
+def _dtype_name(x):
+    name = _dtypes.get(x.dtype)
+    if name is None:
+        name = _dtypes[x.dtype] = str(x.dtype)[6:]
+    return name
+
+
 def _tensor(x, where, name, dtypes, shape=None):
     """Address of a contiguous CUDA tensor (None stays None).  The library reads whole buffers
     behind the addresses it is given: a broadcast or strided view would make it read elsewhere."""
     if x is None:
         return None
+    if x.is_cuda and _dtype_name(x) in dtypes and (shape is None or x.shape == shape) and \
+            x.is_contiguous():
+        return x.data_ptr()
     if not x.is_cuda:
         raise ValueError("%s: %s must be a CUDA tensor" % (where, name))
-    if str(x.dtype)[6:] not in dtypes:
+    if _dtype_name(x) not in dtypes:
         raise ValueError("%s: %s must be %s, is %s" % (where, name, " or ".join(dtypes), x.dtype))
-    if shape is not None and tuple(x.shape) != tuple(shape):
+    if shape is not None and x.shape != shape:
         raise ValueError("%s: %s must have shape %s, has %s" % (where, name, tuple(shape),
                                                                tuple(x.shape)))
-    if not x.is_contiguous():
-        raise ValueError("%s: %s must be contiguous" % (where, name))
-    return x.data_ptr()
+    raise ValueError("%s: %s must be contiguous" % (where, name))
+
+
+_ROW_KINDS = {"float32": DECO_F32, "bfloat16": DECO_BF16}
 
 
 def _rows_of(x, where, name, like=None):
@@ -522,14 +539,16 @@ def _rows_of(x, where, name, like=None):
     consecutive in memory; the rows themselves may be any distance apart."""
     if not x.is_cuda or x.dim() != 2:
         raise ValueError("%s: %s must be a two-dimensional CUDA tensor" % (where, name))
-    kind = {"float32": DECO_F32, "bfloat16": DECO_BF16}.get(str(x.dtype)[6:])
+    kind = _ROW_KINDS.get(_dtype_name(x))
     if kind is None:
         raise ValueError("%s: %s must be float32 or bfloat16, is %s" % (where, name, x.dtype))
     if like is not None and (x.dtype != like.dtype or x.shape != like.shape):
         raise ValueError("%s: %s must have the logits' shape and type" % (where, name))
     rows, cols = x.shape
-    stride = x.stride(0) if rows > 1 else max(cols, x.stride(0))
-    if cols > 1 and x.stride(1) != 1 or stride < cols:
+    stride, step = x.stride()
+    if rows <= 1:
+        stride = max(cols, stride)
+    if cols > 1 and step != 1 or stride < cols:
         raise ValueError("%s: the rows of %s must be consecutive in memory and must not overlap"
                          % (where, name))
     return x.data_ptr(), kind, rows, cols, stride

@@ -10,6 +10,14 @@
 // A row is one CTA's work, or a cluster's of 2, 4 or 8 CTAs, each with a contiguous part of it,
 // where the rows alone would leave most of the device idle; the parts are joined through
 // distributed shared memory, so there is no workspace and no second launch.
+//
+// What bounds it: one exponential per logit takes as long as reading two bytes of it from memory (16 a cycle
+// and SM against 44 bytes a nanosecond), and the other instructions about as long again, so the pass works on
+// pairs of logits (fma and add of two fp32 numbers at once) and has no bounds check inside a row.
+//
+// Alternatives: a thread's maximum over its entries is known when the pass ends.  The k-th largest of 64
+// groups' maxima is a bound which at least k entries reach and few more than k do; only threads
+// whose maximum reaches it have their entries read again (from L2), 32 granules at a time by their warp.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -24,12 +32,13 @@ namespace {
 
 constexpr int NT = 256;                  // threads of a CTA
 constexpr int WARPS = NT / 32;
-constexpr int UNROLL = 4;                // 16-byte loads of a thread in flight
+constexpr int UNROLL = 2;                // 16-byte loads of a thread per batch; one more batch is in flight
+constexpr int GRAD_UNROLL = 4;           // granules of a thread in the gradient
 constexpr int GROUPS = 64;               // groups of threads whose maxima bound the alternatives
 constexpr int MAX_TOP = DECO_LOGPROBS_MAX_TOP;
 constexpr int LIST = 1024;               // candidates kept for the alternatives
-constexpr int TIES = 64;                 // ... of those equal to the bound
 constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LOG2E_LO = 1.9259629911266175e-8f;               // log2(e) - LOG2E
 constexpr float LN2 = 0.6931471805599453f;
 // The streaming path treats entries below FLOOR as FLOOR, with weight 0 (masks of -inf, of the
 // type's lowest value, of -1e10 ...).  That is exact for rows whose maximum m has |m c| < SPAN and
@@ -73,6 +82,39 @@ __device__ __forceinline__ uint64_t item_key(float x, uint32_t idx)
     return (static_cast<uint64_t>(order_key(x)) << 32) | (0xFFFFFFFFu - idx);
 }
 
+// Two fp32 numbers in one register pair.
+__device__ __forceinline__ uint64_t pair(float a, float b)
+{
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
+    return v;
+}
+__device__ __forceinline__ void unpair(uint64_t v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t ex2_2(uint64_t v)
+{
+    float a, b;
+    unpair(v, a, b);
+    return pair(ex2(a), ex2(b));
+}
+
 template <typename T> struct Elem;
 template <> struct Elem<float> {
     static constexpr int E = 4;
@@ -90,6 +132,7 @@ template <> struct Elem<float> {
         return m;
     }
     __device__ static float at(const uint32_t (&w)[4], int e) { return __uint_as_float(w[e]); }
+    __device__ static uint64_t two(const uint32_t (&w)[4], int i) { return pair(at(w, 2 * i), at(w, 2 * i + 1)); }
     static constexpr uint32_t NEG_INF = 0xFF800000u;
     __device__ static void put(uint32_t (&w)[4], int e, float x) { w[e] = __float_as_uint(x); }
 };
@@ -117,6 +160,7 @@ template <> struct Elem<__nv_bfloat16> {
     {
         return __uint_as_float((e & 1) ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
     }
+    __device__ static uint64_t two(const uint32_t (&w)[4], int i) { return pair(at(w, 2 * i), at(w, 2 * i + 1)); }
     static constexpr uint32_t NEG_INF = 0xFF80FF80u;
     __device__ static void put(uint32_t (&w)[4], int e, float x)
     {
@@ -137,19 +181,30 @@ struct Row {
         lead = static_cast<uint32_t>((reinterpret_cast<uintptr_t>(p_) & 15u) / sizeof(T));
         granules = static_cast<uint32_t>((static_cast<uint64_t>(vocab_) + lead + E - 1) / E);
     }
+    // granules v .. v + n - 1 lie inside the row and below end
+    __device__ __forceinline__ bool inside(uint32_t v, uint32_t n, uint32_t end) const
+    {
+        return v > 0 && v + n <= end && v + n < granules;
+    }
+    __device__ __forceinline__ const T *at(uint32_t v) const { return p + (static_cast<int64_t>(v) * Elem<T>::E - lead); }
+    // a whole granule
+    __device__ __forceinline__ static void load_at(const T *q, uint32_t (&w)[4])
+    {
+        if (NC) {
+            asm("ld.global.nc.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];"
+                : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(q));
+        } else {
+            const uint4 x = *reinterpret_cast<const uint4 *>(q);
+            w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+        }
+    }
     // entries of granule v; those that do not exist read as -inf
     __device__ __forceinline__ void load(uint32_t v, uint32_t end, uint32_t (&w)[4]) const
     {
         constexpr int E = Elem<T>::E;
         const int64_t first = static_cast<int64_t>(v) * E - lead;
         if (v < end && first >= 0 && first + E <= vocab) {
-            if (NC) {
-                asm("ld.global.nc.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];"
-                    : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p + first));
-            } else {
-                const uint4 x = *reinterpret_cast<const uint4 *>(p + first);
-                w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
-            }
+            load_at(p + first, w);
             return;
         }
 #pragma unroll
@@ -183,13 +238,10 @@ __device__ __forceinline__ void join(Part &a, Part b, float c)
 struct Shared {
     Part part[WARPS];
     Part cta;                            // this CTA's part of the row
-    float tmax[NT];
+    alignas(16) float tmax[NT];
     float bound;
-    uint32_t n_list, n_ties, n_out;
-    uint64_t list[LIST + TIES];          // item keys
-    float list_x[LIST];
-    uint32_t list_idx[LIST];
-    uint32_t ties[TIES];
+    uint32_t n_list;
+    uint64_t list[LIST];                 // item keys of the entries that reach the bound
     uint64_t top[MAX_TOP];               // this CTA's alternatives, sorted; 0: none
     uint64_t merged[MAX_TOP * 8];
     uint64_t final_top[MAX_TOP];
@@ -215,29 +267,18 @@ __device__ float group_bound(Shared &sh, float tm, uint32_t k)
     __syncthreads();
     if (t < GROUPS) {
         uint32_t rank = 0;
-#pragma unroll 16
-        for (int j = 0; j < GROUPS; ++j) {
-            const float o = sh.tmax[j];
-            rank += (o > g || (o == g && j < t)) ? 1u : 0u;
+#pragma unroll
+        for (int j = 0; j < GROUPS; j += 4) {
+            const float4 o = *reinterpret_cast<const float4 *>(sh.tmax + j);
+            rank += (o.x > g || (o.x == g && j < t)) ? 1u : 0u;
+            rank += (o.y > g || (o.y == g && j + 1 < t)) ? 1u : 0u;
+            rank += (o.z > g || (o.z == g && j + 2 < t)) ? 1u : 0u;
+            rank += (o.w > g || (o.w == g && j + 3 < t)) ? 1u : 0u;
         }
         if (rank == k - 1) sh.bound = g;
     }
     __syncthreads();
     return sh.bound;
-}
-
-__device__ __forceinline__ void offer(Shared &sh, float x, uint32_t idx, float bound)
-{
-    if (x > bound) {
-        const uint32_t at = atomicAdd(&sh.n_list, 1u);
-        if (at < LIST) {
-            sh.list_x[at] = x;
-            sh.list_idx[at] = idx;
-        }
-    } else if (x == bound) {
-        const uint32_t at = atomicAdd(&sh.n_ties, 1u);
-        if (at < TIES) sh.ties[at] = idx;
-    }
 }
 
 // Fill out[have .. want) with the largest entries of [lo, hi) whose order key is below `below`,
@@ -297,6 +338,7 @@ __device__ void rank_into(const uint64_t *keys, uint32_t n, uint32_t k, uint64_t
     for (uint32_t i = threadIdx.x; i < n; i += NT) {
         const uint64_t a = keys[i];
         uint32_t rank = 0;
+#pragma unroll 8
         for (uint32_t j = 0; j < n; ++j) rank += keys[j] > a ? 1u : 0u;
         if (rank < k) out[rank] = a;
     }
@@ -337,99 +379,95 @@ logprobs_kernel(const Args a)
 
     // ---- one pass over this CTA's granules
     Part my = {FLOOR, 0.f, 0.f};
-    float bound = FLOOR;
-    if (TOP && t == 0) sh.n_list = sh.n_ties = sh.n_out = 0;
+    if (TOP && t == 0) sh.n_list = 0;
     if (!a.slow) {
-        bool first = true;
-        for (uint32_t vb = v0; vb < v1; vb += NT * UNROLL) {
-            uint32_t w[UNROLL][4];
+        // the next batch of a thread is under way while it works on one
+        uint32_t w[UNROLL][4], next[UNROLL][4];
+        auto fetch = [&](uint32_t vb) {
+            if (R.inside(vb, NT * UNROLL, v1)) {
+                const T *q = R.at(vb + t);
 #pragma unroll
-            for (int u = 0; u < UNROLL; ++u) R.load(vb + u * NT + t, v1, w[u]);
+                for (int u = 0; u < UNROLL; ++u) R.load_at(q + u * NT * E, next[u]);
+            } else {
+#pragma unroll
+                for (int u = 0; u < UNROLL; ++u) R.load(vb + u * NT + t, v1, next[u]);
+            }
+        };
+        fetch(v0);
+        const uint64_t c2 = pair(c, c);
+        for (uint32_t vb = v0; vb < v1; vb += NT * UNROLL) {
             float bm = FLOOR;
 #pragma unroll
-            for (int u = 0; u < UNROLL; ++u) bm = fmaxf(bm, Elem<T>::clamp_max(w[u]));
-            if (bm > my.m) raise(my, bm, c);
-            if (TOP && first) {
-                bound = group_bound(sh, bm, a.top);
-                first = false;
-            }
-            const float mc = my.m == FLOOR ? 0.f : my.m * c;     // nothing but FLOOR yet: weights 0
-#pragma unroll
             for (int u = 0; u < UNROLL; ++u) {
-                float s = 0.f, q = 0.f;
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const float tt = __fmaf_rn(Elem<T>::at(w[u], e), c, -mc);
-                    const float p = ex2(tt);
-                    s += p;
-                    q = __fmaf_rn(p, tt, q);
-                }
-                my.s += s;
-                my.q += q;
+                for (int i = 0; i < 4; ++i) w[u][i] = next[u][i];
+                bm = fmaxf(bm, Elem<T>::clamp_max(w[u]));
             }
-            if (TOP && bm >= bound) {
+            if (vb + NT * UNROLL < v1) fetch(vb + NT * UNROLL);
+            if (bm > my.m) raise(my, bm, c);
+            const float mc = my.m == FLOOR ? 0.f : my.m * c;     // nothing but FLOOR yet: weights 0
+            const uint64_t shift = pair(-mc, -mc);
+            uint64_t s = pair(my.s, 0.f), q = pair(my.q, 0.f);
 #pragma unroll
-                for (int u = 0; u < UNROLL; ++u) {
-                    const uint32_t v = vb + u * NT + t;
-                    if (v < v1) {
+            for (int u = 0; u < UNROLL; ++u)
 #pragma unroll
-                        for (int e = 0; e < E; ++e) {
-                            const float x = Elem<T>::at(w[u], e);
-                            if (x >= bound && x > FLOOR) offer(sh, x, v * E + e - R.lead, bound);
-                        }
-                    }
+                for (int i = 0; i < E / 2; ++i) {
+                    const uint64_t tt = fma2(Elem<T>::two(w[u], i), c2, shift);
+                    const uint64_t p = ex2_2(tt);
+                    s = add2(s, p);
+                    q = fma2(p, tt, q);
                 }
-            }
+            float s1, q1;
+            unpair(s, my.s, s1);
+            unpair(q, my.q, q1);
+            my.s += s1;
+            my.q += q1;
         }
     }
 
     // ---- alternatives of this CTA's part
     if (TOP && !a.slow) {
         const uint32_t k = a.top;
-        float last = bound;                                      // what the lists were collected with
-        bound = group_bound(sh, my.m, k);                        // (its barriers complete the lists)
-        if (sh.n_list > LIST) {
-            // more candidates than the first entries promised: once more, with the whole part's bound
-            __syncthreads();
-            if (t == 0) sh.n_list = sh.n_ties = 0;
-            last = bound;
-            __syncthreads();
-            for (uint32_t v = v0 + t; v < v1; v += NT) {
-                uint32_t w[4];
-                R.load(v, v1, w);
-                if (Elem<T>::clamp_max(w) >= bound) {
+        const float bound = group_bound(sh, my.m, k);
+        // the entries of the threads that reach it
+        constexpr int AT_ONCE = 4;                               // of these threads, so that their reads overlap
+        for (uint32_t who = __ballot_sync(0xFFFFFFFFu, my.m >= bound && my.m > FLOOR); who;) {
+            uint32_t first[AT_ONCE];
+#pragma unroll
+            for (int j = 0; j < AT_ONCE; ++j) {
+                first[j] = who ? v0 + wid * 32 + __ffs(who) - 1 + lane * NT : v1;
+                who &= who - 1;
+            }
+            for (uint32_t step = 0; v0 + step < v1; step += 32 * NT) {
+                uint32_t g[AT_ONCE][4];
+#pragma unroll
+                for (int j = 0; j < AT_ONCE; ++j) R.load(first[j] + step, v1, g[j]);
+#pragma unroll
+                for (int j = 0; j < AT_ONCE; ++j) {
+                    uint32_t hits = 0;
 #pragma unroll
                     for (int e = 0; e < E; ++e) {
-                        const float x = Elem<T>::at(w, e);
-                        if (x >= bound && x > FLOOR) offer(sh, x, v * E + e - R.lead, bound);
+                        const float x = Elem<T>::at(g[j], e);
+                        hits |= x >= bound && x > FLOOR ? 1u << e : 0u;
+                    }
+                    for (; hits; hits &= hits - 1) {
+                        const uint32_t idx = (first[j] + step) * E + __ffs(hits) - 1 - R.lead;
+                        const uint32_t at = atomicAdd(&sh.n_list, 1u);
+                        if (at < LIST) sh.list[at] = item_key(Elem<T>::template get<true>(row + idx), idx);
                     }
                 }
             }
-            __syncthreads();
         }
+        __syncthreads();
         const uint32_t lo = v0 == 0 ? 0u : v0 * E - R.lead;
         const uint32_t hi = v1 == R.granules ? a.vocab : v1 * E - R.lead;
-        const uint32_t listed = sh.n_list, tied = sh.n_ties;
-        if (listed > LIST) {
-            top_by_passes<T>(sh, row, lo, hi, 1ull << 32, 0, min(k, hi - lo), sh.top);
+        const uint32_t listed = sh.n_list, want = min(k, hi - lo);
+        if (listed > LIST) {                                     // ties without end, or one thread's entries above all others
+            top_by_passes<T>(sh, row, lo, hi, 1ull << 32, 0, want, sh.top);
         } else {
-            for (uint32_t i = t; i < listed; i += NT)
-                if (sh.list_x[i] >= bound)
-                    sh.list[atomicAdd(&sh.n_out, 1u)] = item_key(sh.list_x[i], sh.list_idx[i]);
-            // entries equal to the bound lie on the ties' list unless the bound has risen since
-            const bool ties_known = tied <= TIES || bound > last;
-            if (bound == last && tied <= TIES && bound > FLOOR)
-                for (uint32_t i = t; i < tied; i += NT)
-                    sh.list[atomicAdd(&sh.n_out, 1u)] = item_key(bound, sh.ties[i]);
-            __syncthreads();
-            const uint32_t n = sh.n_out;
-            rank_into(sh.list, n, k, sh.top);
-            if (n < min(k, hi - lo))                             // masked entries, or too many ties
-                top_by_passes<T>(sh, row, lo, hi,
-                                 ties_known || bound <= FLOOR
-                                     ? (n ? sh.top[n - 1] >> 32 : 1ull << 32)
-                                     : static_cast<uint64_t>(order_key(bound)) + 1,
-                                 n, min(k, hi - lo), sh.top);
+            rank_into(sh.list, listed, k, sh.top);
+            if (listed < want)                                   // fewer than k entries above FLOOR
+                top_by_passes<T>(sh, row, lo, hi, listed ? sh.top[listed - 1] >> 32 : 1ull << 32, listed, want, sh.top);
         }
         for (uint32_t i = t; i < k; i += NT)
             if (i >= hi - lo) sh.top[i] = 0;
@@ -471,6 +509,7 @@ logprobs_kernel(const Args a)
             for (uint32_t i = t; i < n; i += NT) {
                 const uint64_t x = sh.merged[i];
                 uint32_t rank = 0;
+#pragma unroll 8
                 for (uint32_t j = 0; j < n; ++j) rank += (sh.merged[j] > x || (sh.merged[j] == x && j < i)) ? 1u : 0u;
                 if (rank < a.top) sh.final_top[rank] = x;
             }
@@ -581,10 +620,11 @@ template <> __device__ __forceinline__ void put_entry<float>(float *p, float x) 
 template <> __device__ __forceinline__ void put_entry<__nv_bfloat16>(__nv_bfloat16 *p, float x) { *p = __float2bfloat16_rn(x); }
 
 // One CTA per chunk of a row: entries are read and written once, 16 bytes at a time, with
-// d = log p and p = exp d.  The target's term is added by the thread that holds its granule.  The
+// from the saved lse.  The target's term is added by the thread that holds its granule.  The
 // alternatives' entries are few: warp 0 reads their logits first (the gradient may lie in the
 // logits' place) and writes them over at the end, the terms of equal tokens added in a fixed order.
-template <typename T, int U>
+// ENT: there is a gradient of the entropy.
+template <typename T, int U, bool ENT>
 __global__ void __launch_bounds__(NT)
 logprobs_grad_kernel(const GradArgs a)
 {
@@ -621,12 +661,21 @@ logprobs_grad_kernel(const GradArgs a)
         for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
         total += s;
     }
-    auto entry = [&](float x, float own_g) {
+    // In full, for any lse and scale: d = log p.
+    auto careful = [&](float x, float own_g) {
         const float d = max_nan(__fmaf_rn(x, a.scale, -lse), -1e6f);
         const float p = ex2(d * LOG2E);
         const float u = p * __fmaf_rn(g_h, d + h, total);
         return empty ? 0.f : a.scale * (own_g - u);
     };
+    // For lse and scale in the usual range: p = f 2^t, t = x c - L, where L is lse log2(e) rounded and
+    // f = 2^-(what the rounding left);  log p + entropy = ln2 t + (entropy - ln2 (the rest)).  So an entry is
+    // 2^t (A t + B), or 2^t B without the entropy's term; logits below FLOOR count as FLOOR there (p = 0).
+    const float c = a.scale * LOG2E, big = lse * LOG2E;
+    const float rest = __fmaf_rn(lse, LOG2E, -big) + lse * LOG2E_LO;
+    const float f = -a.scale * ex2(-rest);
+    const float coef_a = f * g_h * LN2, coef_b = f * __fmaf_rn(g_h, h - LN2 * rest, total);
+    const bool usual = fabsf(big) < SPAN && a.scale >= SCALE_LO && a.scale <= SCALE_HI;
     // the alternatives in this chunk
     float x_i = 0.f;
     bool mine = false;
@@ -639,29 +688,56 @@ logprobs_grad_kernel(const GradArgs a)
     const uint32_t vt = tgt == 0xFFFFFFFFu ? 0xFFFFFFFFu : static_cast<uint32_t>((static_cast<uint64_t>(tgt) + R.lead) / E);
     const bool same_phase = ((reinterpret_cast<uintptr_t>(row) ^ reinterpret_cast<uintptr_t>(out)) & 15u) == 0;
     uint32_t w[U][4];
+    const uint32_t vb = static_cast<uint32_t>(v0);
+    const bool whole = R.inside(vb, NT * U, end);
+    if (whole) {
+        const T *q = R.at(vb + t);
 #pragma unroll
-    for (int u = 0; u < U; ++u) R.load(static_cast<uint32_t>(v0) + u * NT + t, end, w[u]);
+        for (int u = 0; u < U; ++u) R.load_at(q + u * NT * E, w[u]);
+    } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u) R.load(vb + u * NT + t, end, w[u]);
+    }
+    const uint64_t c2 = pair(c, c), shift = pair(-big, -big), a2 = pair(coef_a, coef_a), b2 = pair(coef_b, coef_b);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const uint32_t v = static_cast<uint32_t>(v0) + u * NT + t;
-        if (v >= end) continue;
-        const int64_t first = static_cast<int64_t>(v) * E - R.lead;
-        float y[E];
+        const uint32_t v = vb + u * NT + t;
+        if (!whole && v >= end) continue;
+        uint64_t y[E / 2];
+        if (usual) {
+            if (ENT) Elem<T>::clamp_max(w[u]);
 #pragma unroll
-        for (int e = 0; e < E; ++e) y[e] = entry(Elem<T>::at(w[u], e), 0.f);
-        if (v == vt) {
+            for (int i = 0; i < E / 2; ++i) {
+                const uint64_t tt = fma2(Elem<T>::two(w[u], i), c2, shift);
+                const uint64_t p = ex2_2(tt);
+                y[i] = mul2(p, ENT ? fma2(tt, a2, b2) : b2);
+            }
+        } else {
 #pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (first + e == tgt) y[e] = entry(Elem<T>::at(w[u], e), g_t);
+            for (int i = 0; i < E / 2; ++i) y[i] = pair(careful(Elem<T>::at(w[u], 2 * i), 0.f), careful(Elem<T>::at(w[u], 2 * i + 1), 0.f));
         }
-        if (same_phase && first >= 0 && first + E <= a.vocab) {
+        const int64_t first = static_cast<int64_t>(v) * E - R.lead;
+        if (v == vt && !empty) {
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) {
+                float y0, y1;
+                unpair(y[i], y0, y1);
+                y0 += first + 2 * i == tgt ? a.scale * g_t : 0.f;
+                y1 += first + 2 * i + 1 == tgt ? a.scale * g_t : 0.f;
+                y[i] = pair(y0, y1);
+            }
+        }
+        if (same_phase && (whole || (first >= 0 && first + E <= a.vocab))) {
             uint32_t o[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < E / 2; ++i) {
+                float y0, y1;
+                unpair(y[i], y0, y1);
                 if (E == 4) {
-                    o[i] = __float_as_uint(y[i]);
+                    o[2 * i % 4] = __float_as_uint(y0);
+                    o[(2 * i + 1) % 4] = __float_as_uint(y1);
                 } else {
-                    const __nv_bfloat162 b = __floats2bfloat162_rn(y[(2 * i) % E], y[(2 * i + 1) % E]);
+                    const __nv_bfloat162 b = __floats2bfloat162_rn(y0, y1);
                     o[i] = *reinterpret_cast<const uint32_t *>(&b);
                 }
             }
@@ -669,8 +745,15 @@ logprobs_grad_kernel(const GradArgs a)
                          :: "l"(out + first), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
         } else {
 #pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (first + e >= 0 && first + e < a.vocab) put_entry<T>(out + first + e, y[e]);
+            for (int i = 0; i < E / 2; ++i) {
+                float yy[2];
+                unpair(y[i], yy[0], yy[1]);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int64_t e = first + 2 * i + j;
+                    if (e >= 0 && e < a.vocab) put_entry<T>(out + e, yy[j]);
+                }
+            }
         }
     }
     if (a.top) {
@@ -682,7 +765,7 @@ logprobs_grad_kernel(const GradArgs a)
                 const float gj = __shfl_sync(0xFFFFFFFFu, g_i, j);
                 if (oj == idx) own += gj;
             }
-            if (mine) put_entry<T>(out + idx, entry(x_i, own));
+            if (mine) put_entry<T>(out + idx, careful(x_i, own));
         }
     }
 }
@@ -714,6 +797,16 @@ cudaError_t launch_forward(const Args &a, uint64_t rows, uint32_t parts, cudaStr
     cfg.attrs = at;
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, logprobs_kernel<T, TOP, true>, a);
+}
+
+template <typename T>
+void launch_grad(const GradArgs &a, unsigned grid, bool small, cudaStream_t s)
+{
+    const bool ent = a.g_entropy != nullptr;
+    if (small && ent) logprobs_grad_kernel<T, 1, true><<<grid, NT, 0, s>>>(a);
+    else if (small) logprobs_grad_kernel<T, 1, false><<<grid, NT, 0, s>>>(a);
+    else if (ent) logprobs_grad_kernel<T, GRAD_UNROLL, true><<<grid, NT, 0, s>>>(a);
+    else logprobs_grad_kernel<T, GRAD_UNROLL, false><<<grid, NT, 0, s>>>(a);
 }
 
 bool bad_shape(const void *logits, int32_t dtype, uint64_t rows, uint32_t vocab, uint64_t stride, float scale)
@@ -802,19 +895,14 @@ extern "C" deco_status deco_token_logprobs_grad(const void *logits, int32_t dtyp
     // Short calls take one granule per thread, so that they spread over more SMs.
     const uint64_t per = dtype == DECO_F32 ? 4 : 8;
     const uint64_t granules = (static_cast<uint64_t>(vocab) + 2 * per - 2) / per;
-    const bool small = rows * granules <= 4ull * sms * NT * UNROLL;
-    const uint64_t span = static_cast<uint64_t>(NT) * (small ? 1 : UNROLL);
+    const bool small = rows * granules <= 4ull * sms * NT * GRAD_UNROLL;
+    const uint64_t span = static_cast<uint64_t>(NT) * (small ? 1 : GRAD_UNROLL);
     const uint64_t chunks = (granules + span - 1) / span;
     if (rows * chunks > 0x7FFFFFFFull) return DECO_ERR_INVALID_ARG;
     a.chunks = static_cast<uint32_t>(chunks);
     const unsigned grid = static_cast<unsigned>(rows * chunks);
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (dtype == DECO_F32) {
-        if (small) logprobs_grad_kernel<float, 1><<<grid, NT, 0, s>>>(a);
-        else logprobs_grad_kernel<float, UNROLL><<<grid, NT, 0, s>>>(a);
-    } else {
-        if (small) logprobs_grad_kernel<__nv_bfloat16, 1><<<grid, NT, 0, s>>>(a);
-        else logprobs_grad_kernel<__nv_bfloat16, UNROLL><<<grid, NT, 0, s>>>(a);
-    }
+    if (dtype == DECO_F32) launch_grad<float>(a, grid, small, s);
+    else launch_grad<__nv_bfloat16>(a, grid, small, s);
     return cudaGetLastError() == cudaSuccess ? DECO_OK : DECO_ERR_CUDA;
 }
