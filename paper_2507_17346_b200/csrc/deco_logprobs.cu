@@ -133,6 +133,12 @@ template <> struct Elem<float> {
     }
     __device__ static float at(const uint32_t (&w)[4], int e) { return __uint_as_float(w[e]); }
     __device__ static uint64_t two(const uint32_t (&w)[4], int i) { return pair(at(w, 2 * i), at(w, 2 * i + 1)); }
+    // the same for an e that is not known to the compiler
+    __device__ static float pick(const uint32_t (&w)[4], int e)
+    {
+        const uint32_t a = e & 1 ? w[1] : w[0], b = e & 1 ? w[3] : w[2];
+        return __uint_as_float(e & 2 ? b : a);
+    }
     static constexpr uint32_t NEG_INF = 0xFF800000u;
     __device__ static void put(uint32_t (&w)[4], int e, float x) { w[e] = __float_as_uint(x); }
 };
@@ -161,6 +167,11 @@ template <> struct Elem<__nv_bfloat16> {
         return __uint_as_float((e & 1) ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
     }
     __device__ static uint64_t two(const uint32_t (&w)[4], int i) { return pair(at(w, 2 * i), at(w, 2 * i + 1)); }
+    __device__ static float pick(const uint32_t (&w)[4], int e)
+    {
+        const uint32_t a = e & 2 ? w[1] : w[0], b = e & 2 ? w[3] : w[2], c = e & 4 ? b : a;
+        return __uint_as_float(e & 1 ? c & 0xFFFF0000u : c << 16);
+    }
     static constexpr uint32_t NEG_INF = 0xFF80FF80u;
     __device__ static void put(uint32_t (&w)[4], int e, float x)
     {
@@ -237,7 +248,7 @@ __device__ __forceinline__ void join(Part &a, Part b, float c)
 
 struct Shared {
     Part part[WARPS];
-    Part cta;                            // this CTA's part of the row
+    Part cta, row;                       // this CTA's part of the row; the whole row
     alignas(16) float tmax[NT];
     float bound;
     uint32_t n_list;
@@ -377,12 +388,21 @@ logprobs_kernel(const Args a)
     const uint32_t v1 = static_cast<uint32_t>(static_cast<uint64_t>(R.granules) * (part + 1) / parts);
     const float c = a.scale * LOG2E;
 
+    // the target's logit, wanted at the end
+    int64_t tgt = -1;
+    float x_tgt = 0.f;
+    if (t == 0 && part == 0 && a.targets) {
+        tgt = a.targets[r];
+        if (tgt >= 0 && tgt < a.vocab) x_tgt = Elem<T>::template get<true>(row + tgt);
+    }
+
     // ---- one pass over this CTA's granules
     Part my = {FLOOR, 0.f, 0.f};
     if (TOP && t == 0) sh.n_list = 0;
+    uint32_t w[UNROLL][4];
     if (!a.slow) {
         // the next batch of a thread is under way while it works on one
-        uint32_t w[UNROLL][4], next[UNROLL][4];
+        uint32_t next[UNROLL][4];
         auto fetch = [&](uint32_t vb) {
             if (R.inside(vb, NT * UNROLL, v1)) {
                 const T *q = R.at(vb + t);
@@ -430,8 +450,26 @@ logprobs_kernel(const Args a)
         const uint32_t k = a.top;
         const float bound = group_bound(sh, my.m, k);
         // the entries of the threads that reach it
+        auto list_hits = [&](const uint32_t (&g)[4], uint32_t v) {
+            uint32_t hits = 0;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float x = Elem<T>::at(g, e);
+                hits |= x >= bound && x > FLOOR ? 1u << e : 0u;
+            }
+            for (; hits; hits &= hits - 1) {
+                const int e = __ffs(hits) - 1;
+                const uint32_t at = atomicAdd(&sh.n_list, 1u);
+                if (at < LIST) sh.list[at] = item_key(Elem<T>::pick(g, e), v * E + e - R.lead);
+            }
+        };
+        const bool one_batch = v1 - v0 <= NT * UNROLL;           // a thread still holds all of its own
+        if (one_batch && v1 > v0 && my.m >= bound) {
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u) list_hits(w[u], v0 + u * NT + t);
+        }
         constexpr int AT_ONCE = 4;                               // of these threads, so that their reads overlap
-        for (uint32_t who = __ballot_sync(0xFFFFFFFFu, my.m >= bound && my.m > FLOOR); who;) {
+        for (uint32_t who = __ballot_sync(0xFFFFFFFFu, !one_batch && my.m >= bound && my.m > FLOOR); who;) {
             uint32_t first[AT_ONCE];
 #pragma unroll
             for (int j = 0; j < AT_ONCE; ++j) {
@@ -443,19 +481,7 @@ logprobs_kernel(const Args a)
 #pragma unroll
                 for (int j = 0; j < AT_ONCE; ++j) R.load(first[j] + step, v1, g[j]);
 #pragma unroll
-                for (int j = 0; j < AT_ONCE; ++j) {
-                    uint32_t hits = 0;
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        const float x = Elem<T>::at(g[j], e);
-                        hits |= x >= bound && x > FLOOR ? 1u << e : 0u;
-                    }
-                    for (; hits; hits &= hits - 1) {
-                        const uint32_t idx = (first[j] + step) * E + __ffs(hits) - 1 - R.lead;
-                        const uint32_t at = atomicAdd(&sh.n_list, 1u);
-                        if (at < LIST) sh.list[at] = item_key(Elem<T>::template get<true>(row + idx), idx);
-                    }
-                }
+                for (int j = 0; j < AT_ONCE; ++j) list_hits(g[j], first[j] + step);
             }
         }
         __syncthreads();
@@ -493,7 +519,18 @@ logprobs_kernel(const Args a)
         if (t == 0) sh.cta = all;
         cl.sync();
         if (part == 0) {
-            for (uint32_t o = 1; o < parts; ++o) join(all, cl.map_shared_rank(&sh, o)->cta, c);
+            if (wid == 0) {
+                // lane o: part o's statistics (lanes from `parts` on repeat them), joined by halves
+                Part b = cl.map_shared_rank(&sh, lane & (parts - 1))->cta;
+                for (uint32_t o = 1; o < parts; o *= 2) {
+                    Part other;
+                    other.m = __shfl_xor_sync(0xFFFFFFFFu, b.m, o);
+                    other.s = __shfl_xor_sync(0xFFFFFFFFu, b.s, o);
+                    other.q = __shfl_xor_sync(0xFFFFFFFFu, b.q, o);
+                    join(b, other, c);
+                }
+                if (lane == 0) sh.row = b;
+            }
             if (TOP) {
                 const uint32_t n = parts * a.top;
                 for (uint32_t i = t; i < n; i += NT)
@@ -502,16 +539,24 @@ logprobs_kernel(const Args a)
         }
         cl.sync();                                               // the others may leave
         if (part != 0) return;
+        all = sh.row;
         if (TOP) {
-            // empty places (key 0) are ranked by their position: they are never among the first
-            // `top` <= vocab, but the ranks of the others must not collide with theirs
+            // sorted lists: an entry's place is its place in its own list and the number of larger ones in the others
             const uint32_t n = parts * a.top;
             for (uint32_t i = t; i < n; i += NT) {
                 const uint64_t x = sh.merged[i];
-                uint32_t rank = 0;
-#pragma unroll 8
-                for (uint32_t j = 0; j < n; ++j) rank += (sh.merged[j] > x || (sh.merged[j] == x && j < i)) ? 1u : 0u;
-                if (rank < a.top) sh.final_top[rank] = x;
+                const uint32_t own = i / a.top;
+                uint32_t rank = i - own * a.top;
+#pragma unroll
+                for (uint32_t o = 0; o < 8; ++o) {
+                    if (o >= parts || o == own) continue;
+                    uint32_t n_larger = 0;                       // binary search in a descending list
+#pragma unroll
+                    for (uint32_t step = MAX_TOP; step > 0; step /= 2)
+                        if (n_larger + step <= a.top && sh.merged[o * a.top + n_larger + step - 1] > x) n_larger += step;
+                    rank += n_larger;
+                }
+                if (x != 0 && rank < a.top) sh.final_top[rank] = x;     // (0: an empty place; vocab >= top entries exist)
             }
             __syncthreads();
             top = sh.final_top;
@@ -519,7 +564,6 @@ logprobs_kernel(const Args a)
     }
 
     // ---- the row's results
-    const int64_t tgt = a.targets ? a.targets[r] : -1;
     const bool fast = !a.slow && fabsf(all.m * c) < SPAN && all.s < INFINITY;
     float lse, entropy, lp, zm, zs, logz;
     bool empty = false;
@@ -588,7 +632,7 @@ logprobs_kernel(const Args a)
     if (t == 0) {
         if (tgt < 0) lp = 0.f;
         else if (tgt >= a.vocab) lp = __uint_as_float(0x7FC00000u);
-        else lp = log_p(Elem<T>::template get<true>(row + tgt));
+        else lp = log_p(x_tgt);
         if (a.logprob) a.logprob[r] = lp;
         if (a.entropy) a.entropy[r] = entropy;
         if (a.lse) a.lse[r] = lse;
