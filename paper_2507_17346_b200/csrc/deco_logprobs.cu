@@ -237,18 +237,24 @@ __device__ __forceinline__ void raise(Part &a, float m, float c)
     a.s = f * a.s;
     a.m = m;
 }
-__device__ __forceinline__ void join(Part &a, Part b, float c)
+// The statistics of the first `width` lanes together (width a power of two; the lanes beyond repeat them),
+// in every lane: their maximum first, so that each is raised once.
+__device__ __forceinline__ Part join_lanes(Part a, float c, uint32_t width)
 {
-    const float m = fmaxf(a.m, b.m);
+    float m = a.m;
+    for (uint32_t o = 1; o < width; o *= 2) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
     raise(a, m, c);
-    raise(b, m, c);
-    a.s += b.s;
-    a.q += b.q;
+    for (uint32_t o = 1; o < width; o *= 2) {
+        a.s += __shfl_xor_sync(0xFFFFFFFFu, a.s, o);
+        a.q += __shfl_xor_sync(0xFFFFFFFFu, a.q, o);
+    }
+    return a;
 }
 
 struct Shared {
     Part part[WARPS];
-    Part cta, row;                       // this CTA's part of the row; the whole row
+    Part cta;                            // this CTA's part of the row
+    int fast;
     alignas(16) float tmax[NT];
     float bound;
     uint32_t n_list;
@@ -500,19 +506,11 @@ logprobs_kernel(const Args a)
     }
 
     // ---- this CTA's statistics
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        Part b;
-        b.m = __shfl_xor_sync(0xFFFFFFFFu, my.m, o);
-        b.s = __shfl_xor_sync(0xFFFFFFFFu, my.s, o);
-        b.q = __shfl_xor_sync(0xFFFFFFFFu, my.q, o);
-        join(my, b, c);
-    }
+    my = join_lanes(my, c, 32);
     if (lane == 0) sh.part[wid] = my;
     __syncthreads();
-    Part all = sh.part[0];
-#pragma unroll
-    for (int w = 1; w < WARPS; ++w) join(all, sh.part[w], c);
+    Part all = {};
+    if (wid == 0) all = join_lanes(sh.part[lane & (WARPS - 1)], c, WARPS);
     const uint64_t *top = sh.top;
     if (SPLIT) {
         cg::cluster_group cl = cg::this_cluster();
@@ -520,16 +518,8 @@ logprobs_kernel(const Args a)
         cl.sync();
         if (part == 0) {
             if (wid == 0) {
-                // lane o: part o's statistics (lanes from `parts` on repeat them), joined by halves
-                Part b = cl.map_shared_rank(&sh, lane & (parts - 1))->cta;
-                for (uint32_t o = 1; o < parts; o *= 2) {
-                    Part other;
-                    other.m = __shfl_xor_sync(0xFFFFFFFFu, b.m, o);
-                    other.s = __shfl_xor_sync(0xFFFFFFFFu, b.s, o);
-                    other.q = __shfl_xor_sync(0xFFFFFFFFu, b.q, o);
-                    join(b, other, c);
-                }
-                if (lane == 0) sh.row = b;
+                // lane o: part o's statistics (lanes from `parts` on repeat them)
+                all = join_lanes(cl.map_shared_rank(&sh, lane & (parts - 1))->cta, c, parts);
             }
             if (TOP) {
                 const uint32_t n = parts * a.top;
@@ -539,7 +529,6 @@ logprobs_kernel(const Args a)
         }
         cl.sync();                                               // the others may leave
         if (part != 0) return;
-        all = sh.row;
         if (TOP) {
             // sorted lists: an entry's place is its place in its own list and the number of larger ones in the others
             const uint32_t n = parts * a.top;
@@ -564,7 +553,11 @@ logprobs_kernel(const Args a)
     }
 
     // ---- the row's results
-    const bool fast = !a.slow && fabsf(all.m * c) < SPAN && all.s < INFINITY;
+    // warp 0 holds the statistics; the slow path takes every warp
+    if (t == 0) sh.fast = !a.slow && fabsf(all.m * c) < SPAN && all.s < INFINITY;
+    __syncthreads();
+    const bool fast = sh.fast != 0;
+    if (fast && wid != 0) return;
     float lse, entropy, lp, zm, zs, logz;
     bool empty = false;
     if (fast) {
@@ -638,7 +631,7 @@ logprobs_kernel(const Args a)
         if (a.lse) a.lse[r] = lse;
     }
     if (TOP)
-        for (uint32_t i = t; i < a.top; i += NT) {
+        for (uint32_t i = t; i < a.top; i += NT) {               // (top <= 32: warp 0)
             const uint32_t idx = 0xFFFFFFFFu - static_cast<uint32_t>(top[i]);
             a.top_idx[r * a.top + i] = idx;
             a.top_logprob[r * a.top + i] = log_p(key_value(static_cast<uint32_t>(top[i] >> 32)));
