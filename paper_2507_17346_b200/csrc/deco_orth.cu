@@ -991,55 +991,48 @@ narrow_kernel(const NarrowArgs g, const Source<T> src)
     // X starts as zeros: what lies beyond the matrix stays zero
     for (uint32_t b = tid * 16; b < 2 * L.x + 2 * L.ab; b += NARROW_THREADS * 16) sts16(base + b, make_uint4(0, 0, 0, 0));
     __syncthreads();
-    // Consecutive threads along what is consecutive in memory, LOADS entries of a thread in flight.  The
-    // entries wait in the places of their hi and lo for the norm, upper and lower half of the fp32 number.
-    constexpr uint32_t LOADS = 8;
-    const uint32_t fast = max(1u, tall ? m : count), total = m * count;
-    const uint32_t dq = NARROW_THREADS / fast, dp = NARROW_THREADS % fast;
-    auto walk = [&](uint32_t &q, uint32_t &p) {
-        q += dq;
-        p += dp;
-        if (p >= fast) { p -= fast; q += 1; }
-    };
+    // A warp per row of memory (short rows: several), AHEAD entries of a lane under way.  The entries wait
+    // in the places of their hi and lo for the norm, upper and lower half of the fp32 number.
+    const uint32_t fast = tall ? m : count, slow = tall ? count : m;
+    const uint64_t origin = M.offset + (tall ? j0 * M.stride : j0);
+    uint32_t width = 1;                                          // lanes of a row
+    while (width < 32 && width < fast) width *= 2;
+    const uint32_t rows_at_once = NARROW_THREADS / width;
     auto spot = [&](uint32_t q, uint32_t p) {
         const uint32_t i = tall ? p : q, j = tall ? q : p;
         return (i >> 6) * L.x_block + j * 128 + ((((i & 63) >> 3) ^ (j & 7)) << 4) + (i & 7) * 2;
     };
     double sum = 0;
-    uint32_t q0 = tid / fast, p0 = tid % fast;
-    for (uint32_t e = tid; e < total; e += NARROW_THREADS * LOADS) {
-        uint32_t q = q0, p = p0;
-        float x[LOADS], mo[LOADS];
+    constexpr uint32_t AHEAD = 8;
+    for (uint32_t p = tid % width; p < fast; p += width)
+        for (uint32_t q0 = tid / width; q0 < slow; q0 += rows_at_once * AHEAD) {
+            float x[AHEAD], mo[AHEAD];
 #pragma unroll
-        for (uint32_t u = 0; u < LOADS; ++u) {
-            x[u] = mo[u] = 0.f;
-            if (e + u * NARROW_THREADS < total) {
-                const uint64_t at = tall ? place(p, j0 + q) : place(q, j0 + p);
-                x[u] = src.input(at);
-                if (src.mom) mo[u] = src.mom[at];
+            for (uint32_t u = 0; u < AHEAD; ++u) {
+                const uint32_t q = q0 + u * rows_at_once;
+                const uint64_t at = origin + q * M.stride + p;
+                x[u] = q < slow ? src.input(at) : 0.f;
+                mo[u] = q < slow && src.mom ? src.mom[at] : 0.f;
             }
-            walk(q, p);
-        }
 #pragma unroll
-        for (uint32_t u = 0; u < LOADS; ++u) {
-            if (e + u * NARROW_THREADS < total) {
+            for (uint32_t u = 0; u < AHEAD; ++u) {
+                const uint32_t q = q0 + u * rows_at_once;
+                if (q >= slow) break;
                 float y = x[u];
                 if (src.mom) {
-                    float mu_x = mo[u];
+                    float mom = mo[u];
                     if (update) {
-                        mu_x = __fmaf_rn(src.mu, mo[u], x[u]);
-                        src.mom[tall ? place(p0, j0 + q0) : place(q0, j0 + p0)] = mu_x;
+                        mom = __fmaf_rn(src.mu, mom, x[u]);
+                        src.mom[origin + q * M.stride + p] = mom;
                     }
-                    y = src.nesterov ? __fmaf_rn(src.mu, mu_x, x[u]) : mu_x;
+                    y = src.nesterov ? __fmaf_rn(src.mu, mom, x[u]) : mom;
                 }
                 sum = __fma_rn(static_cast<double>(y), static_cast<double>(y), sum);
-                const uint32_t at = spot(q0, p0), w = __float_as_uint(y);
+                const uint32_t at = spot(q, p), w = __float_as_uint(y);
                 asm volatile("st.shared.b16 [%0], %1;" :: "r"(x_hi + at), "h"(static_cast<unsigned short>(w >> 16)) : "memory");
                 asm volatile("st.shared.b16 [%0], %1;" :: "r"(x_lo + at), "h"(static_cast<unsigned short>(w)) : "memory");
             }
-            walk(q0, p0);
         }
-    }
     sum = block_sum<NARROW_THREADS>(sum);
     if (tid == 0) ctl.sum = sum;
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -1143,7 +1136,7 @@ narrow_kernel(const NarrowArgs g, const Source<T> src)
         }
         if (C > 1) {
             cluster_sync();
-            for (uint32_t e = rank * NARROW_THREADS + tid; e < side * units; e += C * NARROW_THREADS) {
+            for (uint32_t e = tid * C + rank; e < side * units; e += C * NARROW_THREADS) {
                 const uint32_t i = e / units, u = e - i * units, perm = i & 3;
                 const uint32_t at = part + i * side * 4;
                 float4 a[C], b[C];
@@ -1392,6 +1385,9 @@ struct deco_orth {
     std::vector<Group> groups;
     std::vector<Span> narrow;            // matrices of narrow_kernel, by cluster size
     uint32_t narrow_smem = 0;
+    // where there are matrices of both kinds, narrow_kernel runs beside gemm_kernel
+    cudaStream_t side = nullptr;
+    cudaEvent_t fork = nullptr, join = nullptr;
     uint32_t n_pieces = 0, n_rest = 0, n_row_pieces = 0;
     // device memory
     uint8_t *workspace = nullptr;
@@ -1411,6 +1407,9 @@ namespace {
 
 void release(deco_orth *h)
 {
+    if (h->side) cudaStreamDestroy(h->side);
+    if (h->fork) cudaEventDestroy(h->fork);
+    if (h->join) cudaEventDestroy(h->join);
     cudaFree(h->workspace);
     cudaFree(h->mats);
     cudaFree(h->maps);
@@ -1681,6 +1680,11 @@ deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, ui
         !upload(h, &h->starts, starts) || !upload(h, &h->narrow_list, narrow_list) ||
         !upload(h, &h->partial, partial) || !upload(h, &h->status, status))
         return DECO_ERR_OOM;
+    if (!h->narrow.empty() && !h->groups.empty() &&
+        (cudaStreamCreateWithFlags(&h->side, cudaStreamNonBlocking) != cudaSuccess ||
+         cudaEventCreateWithFlags(&h->fork, cudaEventDisableTiming) != cudaSuccess ||
+         cudaEventCreateWithFlags(&h->join, cudaEventDisableTiming) != cudaSuccess))
+        return DECO_ERR_CUDA;
     // the copies above may still be under way; the handle's first pass may come on any stream
     return cudaDeviceSynchronize() == cudaSuccess ? DECO_OK : DECO_ERR_CUDA;
 }
@@ -1784,15 +1788,21 @@ cudaError_t run_pass(deco_orth *h, const Source<T> &src, __nv_bfloat16 *out, flo
     na.lr = lr;
     na.decay = decay;
     na.status = h->status;
+    const cudaStream_t ns = h->side ? h->side : s;
+    if (h->side && err == cudaSuccess) {
+        err = cudaEventRecord(h->fork, s);
+        if (err == cudaSuccess) err = cudaStreamWaitEvent(h->side, h->fork, 0);
+    }
     for (const Span &q : h->narrow) {
         if (err != cudaSuccess) return err;
         na.list = h->narrow_list + q.first;
         const bool first = &q == &h->narrow.front();
-        err = q.cg == 8   ? launch_narrow<T, 8>(h, na, src, q.count, first, s)
-              : q.cg == 4 ? launch_narrow<T, 4>(h, na, src, q.count, first, s)
-              : q.cg == 2 ? launch_narrow<T, 2>(h, na, src, q.count, first, s)
-                          : launch_narrow<T, 1>(h, na, src, q.count, first, s);
+        err = q.cg == 8   ? launch_narrow<T, 8>(h, na, src, q.count, first, ns)
+              : q.cg == 4 ? launch_narrow<T, 4>(h, na, src, q.count, first, ns)
+              : q.cg == 2 ? launch_narrow<T, 2>(h, na, src, q.count, first, ns)
+                          : launch_narrow<T, 1>(h, na, src, q.count, first, ns);
     }
+    if (h->side && err == cudaSuccess) err = cudaEventRecord(h->join, h->side);
     for (const Group &G : h->groups) {
         if (err != cudaSuccess) return err;
         err = launch_after(h, convert_kernel<T>, G.n_convert, INGEST_THREADS, 0, 1, s,
@@ -1822,6 +1832,7 @@ cudaError_t run_pass(deco_orth *h, const Source<T> &src, __nv_bfloat16 *out, flo
                            : launch_gemm<APPLY, OUT_BF16>(h, g, G.phase[APPLY], s);
         }
     }
+    if (h->side && err == cudaSuccess) err = cudaStreamWaitEvent(s, h->join, 0);
     return err;
 }
 
