@@ -944,15 +944,20 @@ struct NarrowLayout {
 // the tensor memory, and CTAs of two clusters waiting for each other's would wait for good.
 constexpr uint32_t NARROW_MIN_SMEM = 120 * 1024;
 
-// Smallest power of two of CTAs that gives each one tile, at most NARROW_MAX_CLUSTER.
-uint32_t narrow_cluster(uint32_t n)
+// Smallest power of two of CTAs, at most NARROW_MAX_CLUSTER, that leaves each at most two tiles (one, where
+// shared memory holds no more).  A second tile costs a CTA 3200 cycles a step, a cluster's exchange 4500.
+uint32_t narrow_cluster(uint32_t m, uint32_t n)
 {
     uint32_t c = 1;
-    while (c < NARROW_MAX_CLUSTER && c * 128 < n) c *= 2;
+    while (c < NARROW_MAX_CLUSTER && c * (m <= 64 ? 256 : 128) < n) c *= 2;
     return c;
 }
-uint32_t narrow_tiles(uint32_t n) { return ((n + 127) / 128 + narrow_cluster(n) - 1) / narrow_cluster(n); }
-bool is_narrow(uint32_t m, uint32_t n) { return m <= FULL_SIDE && narrow_tiles(n) <= (m <= 64 ? NARROW_TILE_LIMIT : 1); }
+uint32_t narrow_tiles(uint32_t m, uint32_t n)
+{
+    const uint32_t c = narrow_cluster(m, n);
+    return ((n + 127) / 128 + c - 1) / c;
+}
+bool is_narrow(uint32_t m, uint32_t n) { return m <= FULL_SIDE && narrow_tiles(m, n) <= (m <= 64 ? NARROW_TILE_LIMIT : 1); }
 
 // C: CTAs per matrix
 template <typename T, uint32_t C>
@@ -991,7 +996,7 @@ narrow_kernel(const NarrowArgs g, const Source<T> src)
     // X starts as zeros: what lies beyond the matrix stays zero
     for (uint32_t b = tid * 16; b < 2 * L.x + 2 * L.ab; b += NARROW_THREADS * 16) sts16(base + b, make_uint4(0, 0, 0, 0));
     __syncthreads();
-    // A warp per row of memory (short rows: several), AHEAD entries of a lane under way.  The entries wait
+    // A warp per row of memory (short rows: several), many entries of a lane under way.  The entries wait
     // in the places of their hi and lo for the norm, upper and lower half of the fp32 number.
     const uint32_t fast = tall ? m : count, slow = tall ? count : m;
     const uint64_t origin = M.offset + (tall ? j0 * M.stride : j0);
@@ -1003,35 +1008,40 @@ narrow_kernel(const NarrowArgs g, const Source<T> src)
         return (i >> 6) * L.x_block + j * 128 + ((((i & 63) >> 3) ^ (j & 7)) << 4) + (i & 7) * 2;
     };
     double sum = 0;
-    constexpr uint32_t AHEAD = 8;
-    for (uint32_t p = tid % width; p < fast; p += width)
-        for (uint32_t q0 = tid / width; q0 < slow; q0 += rows_at_once * AHEAD) {
-            float x[AHEAD], mo[AHEAD];
+    constexpr uint32_t ROWS = 4, COLS = 4;                       // under way: rows and pieces of a row
+    for (uint32_t q0 = tid / width; q0 < slow; q0 += rows_at_once * ROWS)
+        for (uint32_t p0 = tid % width; p0 < fast; p0 += width * COLS) {
+            float x[ROWS][COLS], mo[ROWS][COLS];
 #pragma unroll
-            for (uint32_t u = 0; u < AHEAD; ++u) {
-                const uint32_t q = q0 + u * rows_at_once;
-                const uint64_t at = origin + q * M.stride + p;
-                x[u] = q < slow ? src.input(at) : 0.f;
-                mo[u] = q < slow && src.mom ? src.mom[at] : 0.f;
-            }
+            for (uint32_t u = 0; u < ROWS; ++u)
 #pragma unroll
-            for (uint32_t u = 0; u < AHEAD; ++u) {
-                const uint32_t q = q0 + u * rows_at_once;
-                if (q >= slow) break;
-                float y = x[u];
-                if (src.mom) {
-                    float mom = mo[u];
-                    if (update) {
-                        mom = __fmaf_rn(src.mu, mom, x[u]);
-                        src.mom[origin + q * M.stride + p] = mom;
-                    }
-                    y = src.nesterov ? __fmaf_rn(src.mu, mom, x[u]) : mom;
+                for (uint32_t v = 0; v < COLS; ++v) {
+                    const uint32_t q = q0 + u * rows_at_once, p = p0 + v * width;
+                    const bool there = q < slow && p < fast;
+                    const uint64_t at = origin + q * M.stride + p;
+                    x[u][v] = there ? src.input(at) : 0.f;
+                    mo[u][v] = there && src.mom ? src.mom[at] : 0.f;
                 }
-                sum = __fma_rn(static_cast<double>(y), static_cast<double>(y), sum);
-                const uint32_t at = spot(q, p), w = __float_as_uint(y);
-                asm volatile("st.shared.b16 [%0], %1;" :: "r"(x_hi + at), "h"(static_cast<unsigned short>(w >> 16)) : "memory");
-                asm volatile("st.shared.b16 [%0], %1;" :: "r"(x_lo + at), "h"(static_cast<unsigned short>(w)) : "memory");
-            }
+#pragma unroll
+            for (uint32_t u = 0; u < ROWS; ++u)
+#pragma unroll
+                for (uint32_t v = 0; v < COLS; ++v) {
+                    const uint32_t q = q0 + u * rows_at_once, p = p0 + v * width;
+                    if (q >= slow || p >= fast) continue;
+                    float y = x[u][v];
+                    if (src.mom) {
+                        float mom = mo[u][v];
+                        if (update) {
+                            mom = __fmaf_rn(src.mu, mom, y);
+                            src.mom[origin + q * M.stride + p] = mom;
+                        }
+                        y = src.nesterov ? __fmaf_rn(src.mu, mom, y) : mom;
+                    }
+                    sum = __fma_rn(static_cast<double>(y), static_cast<double>(y), sum);
+                    const uint32_t at = spot(q, p), w = __float_as_uint(y);
+                    asm volatile("st.shared.b16 [%0], %1;" :: "r"(x_hi + at), "h"(static_cast<unsigned short>(w >> 16)) : "memory");
+                    asm volatile("st.shared.b16 [%0], %1;" :: "r"(x_lo + at), "h"(static_cast<unsigned short>(w)) : "memory");
+                }
         }
     sum = block_sum<NARROW_THREADS>(sum);
     if (tid == 0) ctl.sum = sum;
@@ -1136,13 +1146,15 @@ narrow_kernel(const NarrowArgs g, const Source<T> src)
         }
         if (C > 1) {
             cluster_sync();
-            for (uint32_t e = tid * C + rank; e < side * units; e += C * NARROW_THREADS) {
+            // This CTA's share: side * units / C pieces of 8 entries, back to back, so that a warp reads and
+            // writes consecutive memory of one CTA at a time; the parts are added in the CTAs' order.
+            const uint32_t share = side * units / C;
+            for (uint32_t e = rank * share + tid; e < (rank + 1) * share; e += NARROW_THREADS) {
                 const uint32_t i = e / units, u = e - i * units, perm = i & 3;
-                const uint32_t at = part + i * side * 4;
                 float4 a[C], b[C];
 #pragma unroll
                 for (uint32_t o = 0; o < C; ++o) {
-                    const uint32_t p = peer_addr(at, o);
+                    const uint32_t p = peer_addr(part + i * side * 4, o);
                     a[o] = peer_load(p + (((2 * u) ^ perm) << 4));
                     b[o] = peer_load(p + (((2 * u + 1) ^ perm) << 4));
                 }
@@ -1163,8 +1175,7 @@ narrow_kernel(const NarrowArgs g, const Source<T> src)
                     peer_store(peer_addr(ab_lo + to, o), lo);
                 }
             }
-            asm volatile("fence.proxy.async.shared::cluster;" ::: "memory");
-            cluster_sync();
+            cluster_sync();                                      // (the readers' fence comes with the products)
         }
         // A^2, then P in the place of A
         products([&]() {
@@ -1516,9 +1527,9 @@ deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, ui
     for (uint32_t c = NARROW_MAX_CLUSTER; c >= 1; c /= 2) {
         Span span = {static_cast<uint32_t>(narrow_list.size()), 0, c, 0, 0};
         for (uint32_t i = 0; i < n; ++i)
-            if (is_narrow(mats[i].m, mats[i].n) && narrow_cluster(mats[i].n) == c) {
+            if (is_narrow(mats[i].m, mats[i].n) && narrow_cluster(mats[i].m, mats[i].n) == c) {
                 narrow_list.push_back(i);
-                const NarrowLayout L((mats[i].m + 15) & ~15u, narrow_tiles(mats[i].n));
+                const NarrowLayout L((mats[i].m + 15) & ~15u, narrow_tiles(mats[i].m, mats[i].n));
                 h->narrow_smem = std::max(h->narrow_smem, std::max(L.total, NARROW_MIN_SMEM));
             }
         span.count = static_cast<uint32_t>(narrow_list.size()) - span.first;
