@@ -567,9 +567,17 @@ gemm_kernel(const GemmArgs g)
     }
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = ctl.tmem;
-    // what comes before is done while the launch before this one ends; its results are read from here on
-    asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    // the first tile's tables, which no launch writes, are fetched while the launch before this one ends
+    if (lane == 0 && first < end) {
+        const uint32_t mat = g.tiles[first].mat;
+        const Operands op = operands<P>(g, g.mats[mat], mat);
+        asm volatile("prefetch.tensormap [%0];" :: "l"(op.a) : "memory");
+        asm volatile("prefetch.tensormap [%0];" :: "l"(op.b) : "memory");
+    }
+    __syncwarp();
+    // that launch's results are read from here on
+    asm volatile("griddepcontrol.wait;" ::: "memory");
 
     if (wid == 0) {
         if (lane == 0) {
@@ -1520,7 +1528,8 @@ deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, ui
                 : scale == DECO_ORTH_SCALE_RMS      ? static_cast<float>(0.2 * sqrt(std::max(r, c)))
                                                     : 1.f;
         if (is_narrow(M.m, M.n)) continue;
-        bytes[i] = 4 * round_up(2ull * M.rows * M.ldx, 256) + (2 + M.precision) * round_up(2ull * M.m * M.lda, 256);
+        bytes[i] = (M.precision == FULL ? 4 : 3) * round_up(2ull * M.rows * M.ldx, 256) +
+                   (2 + M.precision) * round_up(2ull * M.m * M.lda, 256);
         wide.push_back(i);
     }
     std::vector<uint32_t> narrow_list;
@@ -1562,7 +1571,11 @@ deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, ui
         Mat &M = mats[i];
         const uint64_t xb = round_up(2ull * M.rows * M.ldx, 256), ab = round_up(2ull * M.m * M.lda, 256);
         auto take = [&](uint64_t b) { __half *p = reinterpret_cast<__half *>(h->workspace + at); at += b; return p; };
-        for (int k = 0; k < 2; ++k) { M.hi[k] = take(xb); M.lo[k] = take(xb); }
+        M.hi[0] = take(xb);
+        M.hi[1] = take(xb);
+        M.lo[0] = take(xb);
+        // where only the epilogue touches lo, each entry is read and written by the same tile: one copy does
+        M.lo[1] = M.precision == FULL ? take(xb) : M.lo[0];
         M.a = take(ab);
         M.p = take(ab);
         M.p_lo = M.precision >= WIDE_P ? take(ab) : nullptr;
