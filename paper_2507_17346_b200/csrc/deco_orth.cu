@@ -79,6 +79,8 @@ struct ConvertPiece {
 struct Tile {
     uint32_t mat;
     uint16_t tm, tn;
+    uint16_t part, parts;                // of the sum over k (GRAM)
+    uint32_t slot;                       // where the parts' sums go, parts > 1
 };
 
 // Which operands of a matrix's products are carried as hi + lo.
@@ -87,7 +89,7 @@ constexpr uint32_t FULL_SIDE = 128, WIDE_P_SIDE = 256;
 // A matrix's tensor maps: boxes of 64 x 64 for the operands; from BOX32 on the same with boxes of
 // 32 rows for the epilogue; and A and P in boxes of 64 rows by 32 for mirror images.
 enum Map { MAP_X = 0 /* hi, lo, next hi, next lo */, MAP_A = 4 /* hi, lo */, MAP_P = 6 /* hi, lo */, BOX32 = 8,
-           MIRROR_A = 16, MIRROR_P = 17, MAPS = 18 };
+           MIRROR_A = 16, MIRROR_P = 18 /* hi, lo */, MAPS = 20 };
 
 constexpr uint32_t NO_SLOT = 0xFFFFFFFFu;
 constexpr uint32_t PIECE = 16384;
@@ -297,6 +299,7 @@ constexpr int GEMM_THREADS = 32 * (FIRST_EPI_WARP + EPI_WARPS);
 constexpr int CHUNK = 64;                // columns an epilogue warp takes at a time
 constexpr uint32_t CHUNK_BYTES = 32 * CHUNK * 2;
 constexpr uint32_t STAGING_BYTES = 2 * CHUNK_BYTES;      // of a warp: hi and lo
+constexpr uint32_t PART_FLOATS = 128 * 128;
 constexpr size_t GEMM_SMEM = STAGES * STAGE_BYTES + EPI_WARPS * STAGING_BYTES + 1024;
 
 struct GemmArgs {
@@ -304,6 +307,8 @@ struct GemmArgs {
     const CUtensorMap *maps;             // [mat][MAPS]
     const Tile *tiles;
     const uint32_t *starts;              // [CTAs or pairs + 1]
+    float *part_sums;                    // [slot][PART_FLOATS]
+    uint32_t *arrived;                   // [slot][EPI_WARPS]: parts of a tile that are done, in its first slot
     int src;                             // which X holds the current iterate
     int read_lo, write_lo;
     float a, b, c;
@@ -377,7 +382,7 @@ __device__ __forceinline__ bool bar_wait(uint64_t *b, uint32_t parity, volatile 
 
 __device__ __forceinline__ void map_acquire(const CUtensorMap *map)
 {
-    asm volatile("fence.proxy.tensormap::generic.acquire.gpu [%0], 128;" :: "l"(map) : "memory");
+    asm volatile("fence.proxy.tensormap::generic.acquire.sys [%0], 128;" :: "l"(map) : "memory");
 }
 // Box at (x, y) into this CTA's shared memory; its bytes are counted by the barrier at `bar`, which
 // with CG = 2 is the leading CTA's.
@@ -395,18 +400,6 @@ __device__ __forceinline__ void store_box(const CUtensorMap *map, int32_t x, int
 {
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];"
                  :: "l"(map), "r"(x), "r"(y), "r"(src) : "memory");
-}
-
-// 128 entries of the operand's outer dimension (from mn) by BK of k, as two boxes of 64 x 64.
-template <int CG>
-__device__ __forceinline__ void load_operand(uint32_t dst, const CUtensorMap *map, bool mn_major, int32_t mn, int32_t k,
-                                             uint32_t bar)
-{
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int32_t o = mn + 64 * i;
-        load_box<CG>(dst + i * (OPERAND_BYTES / 2), map, mn_major ? o : k, mn_major ? k : o, bar);
-    }
 }
 
 // Shared-memory descriptor of an operand with 128-byte swizzle.  k consecutive: groups of 8 rows are
@@ -468,14 +461,16 @@ __device__ __forceinline__ void sts16(uint32_t a, uint4 v)
 {
     asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
-// Four 8 x 8 pieces of 2-byte numbers, transposed: lane l passes row l % 8 of piece l / 8, where from and where to.
-__device__ __forceinline__ void transpose4(uint32_t from, uint32_t to)
+// Four 8 x 8 pieces of 2-byte numbers, transposed, and back to memory: lane l passes row l % 8 of piece l / 8.
+__device__ __forceinline__ void transposed(uint32_t from, uint32_t (&v)[4])
 {
-    uint32_t a, b, c, d;
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
-                 : "=r"(a), "=r"(b), "=r"(c), "=r"(d) : "r"(from) : "memory");
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(from) : "memory");
+}
+__device__ __forceinline__ void store_pieces(uint32_t to, const uint32_t (&v)[4])
+{
     asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1,%2,%3,%4};"
-                 :: "r"(to), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+                 :: "r"(to), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
 }
 __device__ __forceinline__ float2 half2_at(const uint4 &v, int i)
 {
@@ -492,6 +487,9 @@ struct Operands {
     uint32_t k, passes, a_lo, b_lo;
     __device__ __forceinline__ const CUtensorMap *map_a(uint32_t i) const { return a + ((a_lo >> i) & 1); }
     __device__ __forceinline__ const CUtensorMap *map_b(uint32_t i) const { return b + ((b_lo >> i) & 1); }
+    // blocks of BK in all passes, and where a part of them starts
+    __device__ __forceinline__ uint32_t blocks() const { return passes * ((k + BK - 1) / BK); }
+    __device__ __forceinline__ uint32_t start(uint32_t part, uint32_t parts) const { return blocks() * part / parts; }
 };
 template <Phase P>
 __device__ __forceinline__ Operands operands(const GemmArgs &g, const Mat &M, uint32_t mat)
@@ -517,7 +515,7 @@ __device__ __forceinline__ Operands operands(const GemmArgs &g, const Mat &M, ui
 // a thread owns a row there, as in tensor memory, and puts the result in the place of the input;
 // a box store writes it back.  Rows lie 128 bytes apart in the staging memory with their 16-byte units
 // permuted as the box copies do it, so the row-wise accesses meet no bank conflicts.  A block's mirror
-// image is transposed in 8 x 8 pieces through the other half of the staging memory: 2-byte stores
+// image is transposed in 8 x 8 pieces in registers and stored as a box too: 2-byte stores
 // straight to global memory made the products of A with itself 1.4 times slower.
 //
 // Four decoder blocks: tensor cores busy 80 % of the cycles with the epilogue left out, where shared memory, read
@@ -559,6 +557,13 @@ gemm_kernel(const GemmArgs g)
             asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
         }
     }
+    // Tensor maps lie in global memory, where the host has put them, perhaps over those of an earlier handle: a
+    // block has to acquire each before its first use (600 cycles; all threads at once, and
+    // while the launch before this one ends).
+    for (uint32_t e = threadIdx.x; e < (end - first) * MAPS; e += GEMM_THREADS) {
+        const uint32_t t = first + e / MAPS, mat = g.tiles[t].mat;
+        if (t == first || g.tiles[t - 1].mat != mat) map_acquire(g.maps + static_cast<uint64_t>(mat) * MAPS + e % MAPS);
+    }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     if (CG == 2) {
@@ -568,42 +573,50 @@ gemm_kernel(const GemmArgs g)
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = ctl.tmem;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    // the first tile's tables, which no launch writes, are fetched while the launch before this one ends
-    if (lane == 0 && first < end) {
-        const uint32_t mat = g.tiles[first].mat;
-        const Operands op = operands<P>(g, g.mats[mat], mat);
-        asm volatile("prefetch.tensormap [%0];" :: "l"(op.a) : "memory");
-        asm volatile("prefetch.tensormap [%0];" :: "l"(op.b) : "memory");
-    }
-    __syncwarp();
-    // that launch's results are read from here on
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    // The results of the launch before this one are read behind this, in the roles that read any: what they need
+    // to know of their first tile is on hand by then.
+    auto results_of_before = []() { asm volatile("griddepcontrol.wait;" ::: "memory"); };
 
     if (wid == 0) {
         if (lane == 0) {
-            uint32_t it = 0, seen = 0xFFFFFFFFu;
+            // This thread's loop is what the tensor cores wait for (a division in it cost 5 % of a large pass):
+            // addresses and coordinates are carried along.
+            uint32_t s = 0, parity = 1;
+            const uint32_t full0 = smem_addr(ctl.full), bar0 = CG == 1 ? full0 : leader_addr(full0);
             bool ok = true;
             for (uint32_t t = first; ok && t < end; ++t) {
                 const Tile tl = g.tiles[t];
                 const Operands op = operands<P>(g, g.mats[tl.mat], tl.mat);
                 const int32_t ra = tl.tm * SIDE + rank * 128, rb = tl.tn * SIDE + rank * 128;
-                for (uint32_t pass = 0; ok && pass < op.passes; ++pass) {
-                    const CUtensorMap *ma = op.map_a(pass), *mb = op.map_b(pass);
-                    if (tl.mat != seen) {                        // an earlier handle's maps may have lain here
-                        map_acquire(ma);
-                        map_acquire(mb);
+                const uint32_t per_pass = (op.k + BK - 1) / BK;
+                const uint32_t b0 = op.start(tl.part, tl.parts), b1 = op.start(tl.part + 1, tl.parts);
+                uint32_t pass = b0 / per_pass;
+                int32_t k = static_cast<int32_t>((b0 - pass * per_pass) * BK);
+                const CUtensorMap *ma = op.map_a(pass), *mb = op.map_b(pass);
+                // an operand's 128 entries come as two boxes of 64 x 64, side by side in its outer dimension
+                const int32_t a_out = op.a_mn ? 64 : 0, b_out = op.b_mn ? 64 : 0;
+                if (t == first) results_of_before();
+                for (uint32_t b = b0; b < b1; ++b) {
+                    if (k >= static_cast<int32_t>(op.k)) {
+                        k = 0;
+                        pass += 1;
+                        ma = op.map_a(pass);
+                        mb = op.map_b(pass);
                     }
-                    for (uint32_t k = 0; k < op.k; k += BK, ++it) {
-                        const uint32_t s = it % STAGES;
-                        if (!bar_wait(&ctl.empty[s], ((it / STAGES) & 1) ^ 1, &ctl.abort, g.status)) { ok = false; break; }
-                        if (rank == 0) bar_expect(&ctl.full[s], CG * STAGE_BYTES);
-                        const uint32_t bar = CG == 1 ? smem_addr(&ctl.full[s]) : leader_addr(smem_addr(&ctl.full[s]));
-                        const uint32_t st = stages + s * STAGE_BYTES;
-                        load_operand<CG>(st, ma, op.a_mn, ra, k, bar);
-                        load_operand<CG>(st + OPERAND_BYTES, mb, op.b_mn, rb, k, bar);
+                    if (!bar_wait(&ctl.empty[s], parity, &ctl.abort, g.status)) { ok = false; break; }
+                    if (rank == 0) bar_expect(&ctl.full[s], CG * STAGE_BYTES);
+                    const uint32_t bar = bar0 + s * 8, st = stages + s * STAGE_BYTES;
+                    const int32_t ax = op.a_mn ? ra : k, ay = op.a_mn ? k : ra, bx = op.b_mn ? rb : k, by = op.b_mn ? k : rb;
+                    load_box<CG>(st, ma, ax, ay, bar);
+                    load_box<CG>(st + OPERAND_BYTES / 2, ma, ax + a_out, ay + 64 - a_out, bar);
+                    load_box<CG>(st + OPERAND_BYTES, mb, bx, by, bar);
+                    load_box<CG>(st + OPERAND_BYTES + OPERAND_BYTES / 2, mb, bx + b_out, by + 64 - b_out, bar);
+                    k += BK;
+                    if (++s == STAGES) {
+                        s = 0;
+                        parity ^= 1;
                     }
                 }
-                seen = tl.mat;
             }
             // Every copy has landed before a CTA leaves: in the normal course the products and so the
             // epilogue have waited for all of them; after a wait that ran out they get some time here.
@@ -614,7 +627,7 @@ gemm_kernel(const GemmArgs g)
         }
     } else if (wid == 1) {
         if (lane == 0 && rank == 0) {
-            uint32_t it = 0, n = 0;
+            uint32_t s = 0, parity = 0, n = 0;
             bool ok = true;
             for (uint32_t t = first; ok && t < end; ++t, ++n) {
                 const Tile tl = g.tiles[t];
@@ -626,17 +639,19 @@ gemm_kernel(const GemmArgs g)
                 const uint32_t idesc = (1u << 4) | (static_cast<uint32_t>(op.a_mn) << 15) |
                                        (static_cast<uint32_t>(op.b_mn) << 16) | ((SIDE >> 3) << 17) | ((SIDE >> 4) << 24);
                 const uint32_t sa = op.a_mn ? 2048 >> 4 : 32 >> 4, sb = op.b_mn ? 2048 >> 4 : 32 >> 4;
-                const uint32_t blocks = op.passes * ((op.k + BK - 1) / BK);
-                for (uint32_t k = 0; k < blocks; ++k, ++it) {
-                    const uint32_t s = it % STAGES;
-                    if (!bar_wait(&ctl.full[s], (it / STAGES) & 1, &ctl.abort, g.status)) { ok = false; break; }
+                const uint64_t desc_a = operand_desc(stages, op.a_mn), desc_b = operand_desc(stages + OPERAND_BYTES, op.b_mn);
+                const uint32_t blocks = op.start(tl.part + 1, tl.parts) - op.start(tl.part, tl.parts), acc = tmem + as * SIDE;
+                for (uint32_t k = 0; k < blocks; ++k) {
+                    if (!bar_wait(&ctl.full[s], parity, &ctl.abort, g.status)) { ok = false; break; }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t st = stages + s * STAGE_BYTES;
-                    const uint64_t da = operand_desc(st, op.a_mn), db = operand_desc(st + OPERAND_BYTES, op.b_mn);
+                    const uint64_t da = desc_a + s * (STAGE_BYTES >> 4), db = desc_b + s * (STAGE_BYTES >> 4);
 #pragma unroll
-                    for (uint32_t q = 0; q < BK / 16; ++q)
-                        mma<CG>(tmem + as * SIDE, da + q * sa, db + q * sb, idesc, (k | q) != 0);
+                    for (uint32_t q = 0; q < BK / 16; ++q) mma<CG>(acc, da + q * sa, db + q * sb, idesc, (k | q) != 0);
                     mma_commit<CG>(&ctl.empty[s]);
+                    if (++s == STAGES) {
+                        s = 0;
+                        parity ^= 1;
+                    }
                 }
                 if (ok) mma_commit<CG>(&ctl.acc_full[as]);
             }
@@ -672,6 +687,7 @@ gemm_kernel(const GemmArgs g)
                 if (in_hi) load_box<1>(hi_buf, in_map, c0, r0, bar);
                 if (in_lo) load_box<1>(lo_buf, in_map + 1, c0, r0, bar);
             };
+            if (t == first) results_of_before();
             if (fetches && chunks && lane == 0) fetch(c_first);
             ok = bar_wait(&ctl.acc_full[as], (n >> 1) & 1, &ctl.abort, g.status);
             if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
@@ -679,6 +695,34 @@ gemm_kernel(const GemmArgs g)
 #pragma unroll 1
             for (uint32_t ch = 0; ch < chunks; ++ch) {
                 const uint32_t c0 = c_first + ch * CHUNK;
+                const uint32_t acc_at = tmem + (static_cast<uint32_t>(quad * 32) << 16) + as * SIDE + side * (SIDE / 2) + ch * CHUNK;
+                const bool split = P == GRAM && CG == 1 && tl.parts > 1;
+                float4 *sums = nullptr;
+                if (split) {
+                    // A part's sums are left in memory; the warp that comes last of its tile's parts adds them up, in
+                    // the order of the parts whoever it is, and goes on with the total.
+                    sums = reinterpret_cast<float4 *>(g.part_sums + static_cast<uint64_t>(tl.slot) * PART_FLOATS + ew * 2048) + lane;
+                    float4 *mine = sums + static_cast<uint64_t>(tl.part) * (PART_FLOATS / 4);
+#pragma unroll
+                    for (uint32_t h = 0; h < 2; ++h) {
+                        uint32_t v[32];
+                        __syncwarp();
+                        tmem_load32(acc_at + h * 32, v);
+#pragma unroll
+                        for (uint32_t u = 0; u < 8; ++u)
+                            __stcg(mine + (h * 8 + u) * 32, make_float4(__uint_as_float(v[4 * u]), __uint_as_float(v[4 * u + 1]),
+                                                                        __uint_as_float(v[4 * u + 2]), __uint_as_float(v[4 * u + 3])));
+                    }
+                    __threadfence();
+                    __syncwarp();
+                    uint32_t before = 0;
+                    uint32_t *count = g.arrived + static_cast<uint64_t>(tl.slot) * EPI_WARPS + ew;
+                    if (lane == 0) before = atomicAdd(count, 1u);
+                    before = __shfl_sync(0xFFFFFFFFu, before, 0);
+                    if (before + 1 != tl.parts) continue;
+                    if (lane == 0) *count = 0;                   // for the next launch
+                    __threadfence();
+                }
                 if (fetches) {
                     if (ch && lane == 0) fetch(c0);
                     ok = bar_wait(&ctl.staged[ew], loads & 1, &ctl.abort, g.status);
@@ -691,7 +735,22 @@ gemm_kernel(const GemmArgs g)
 #pragma unroll
                 for (uint32_t h = 0; h < 2; ++h) {
                     uint32_t v[32];
-                    tmem_load32(tmem + (static_cast<uint32_t>(quad * 32) << 16) + as * SIDE + side * (SIDE / 2) + ch * CHUNK + h * 32, v);
+                    if (!split) {
+                        tmem_load32(acc_at + h * 32, v);
+                    } else {
+#pragma unroll
+                        for (uint32_t u = 0; u < 8; ++u) {
+                            float4 a = make_float4(0, 0, 0, 0);
+                            for (uint32_t q = 0; q < tl.parts; ++q) {
+                                const float4 x = __ldcg(sums + static_cast<uint64_t>(q) * (PART_FLOATS / 4) + (h * 8 + u) * 32);
+                                a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
+                            }
+                            v[4 * u] = __float_as_uint(a.x);
+                            v[4 * u + 1] = __float_as_uint(a.y);
+                            v[4 * u + 2] = __float_as_uint(a.z);
+                            v[4 * u + 3] = __float_as_uint(a.w);
+                        }
+                    }
 #pragma unroll
                     for (uint32_t u = 0; u < 4; ++u) {
                         const uint32_t at = my_row + (((h * 4 + u) ^ perm) << 4);
@@ -725,18 +784,6 @@ gemm_kernel(const GemmArgs g)
                             }
                             sts16(hi_buf + at, make_uint4(oh[0], oh[1], oh[2], oh[3]));
                             if (out_lo) sts16(lo_buf + at, make_uint4(ol[0], ol[1], ol[2], ol[3]));
-                            if (P != APPLY && tl.tm != tl.tn && out_lo && r < rows) {   // no staging memory to spare
-                                unsigned short *m = reinterpret_cast<unsigned short *>(P == GRAM ? M.a : M.p);
-                                unsigned short *ml = reinterpret_cast<unsigned short *>(P == GRAM ? M.a_lo : M.p_lo);
-#pragma unroll
-                                for (uint32_t j = 0; j < 8; ++j) {
-                                    const uint32_t c = c0 + h * 32 + u * 8 + j;
-                                    if (c < cols) {
-                                        m[static_cast<uint64_t>(c) * M.lda + r] = static_cast<unsigned short>(oh[j >> 1] >> (16 * (j & 1)));
-                                        ml[static_cast<uint64_t>(c) * M.lda + r] = static_cast<unsigned short>(ol[j >> 1] >> (16 * (j & 1)));
-                                    }
-                                }
-                            }
                         } else if (T == OUT_BF16) {
                             const float s = M.scale * INV_X_SCALE;
                             uint32_t o[4];
@@ -754,15 +801,20 @@ gemm_kernel(const GemmArgs g)
                     }
                 }
                 if (T == NEXT_X) {
-                    const bool mirror = P != APPLY && tl.tm != tl.tn && !out_lo;
-                    if (mirror) {
+                    const bool mirror = P != APPLY && tl.tm != tl.tn;
+                    const CUtensorMap *image = maps - BOX32 + (P == GRAM ? MIRROR_A : MIRROR_P);
+                    // row c of the mirror image is 64 bytes, its 16-byte units permuted; four 8 x 8 pieces at a time
+                    auto piece_at = [&](uint32_t u) {
+                        const uint32_t c = u * 8 + (lane & 7);
+                        return c * 64 + (((lane >> 3) ^ ((c >> 1) & 3)) << 4);
+                    };
+                    if (mirror && !out_lo) {                     // through the half that lo does not need
                         __syncwarp();
 #pragma unroll
                         for (uint32_t u = 0; u < 8; ++u) {
-                            // four 8 x 8 pieces of 8 columns; row c of the mirror image is 64 bytes, its 16-byte units permuted
-                            const uint32_t c = u * 8 + (lane & 7);
-                            transpose4(hi_buf + my_row + ((u ^ perm) << 4),
-                                       lo_buf + c * 64 + (((lane >> 3) ^ ((c >> 1) & 3)) << 4));
+                            uint32_t v[4];
+                            transposed(hi_buf + my_row + ((u ^ perm) << 4), v);
+                            store_pieces(lo_buf + piece_at(u), v);
                         }
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -770,8 +822,27 @@ gemm_kernel(const GemmArgs g)
                     if (lane == 0) {
                         store_box(out_map, c0, r0, hi_buf);
                         if (out_lo) store_box(out_map + 1, c0, r0, lo_buf);
-                        if (mirror) store_box(maps - BOX32 + (P == GRAM ? MIRROR_A : MIRROR_P), r0, c0, lo_buf);
+                        if (mirror && !out_lo) store_box(image, r0, c0, lo_buf);
                         asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    }
+                    if (mirror && out_lo) {                      // each half once more, when its box is on its way
+#pragma unroll 1
+                        for (uint32_t which = 0; which < 2; ++which) {
+                            const uint32_t buf = which ? lo_buf : hi_buf;
+                            uint32_t v[8][4];
+#pragma unroll
+                            for (uint32_t u = 0; u < 8; ++u) transposed(buf + my_row + ((u ^ perm) << 4), v[u]);
+                            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                            __syncwarp();
+#pragma unroll
+                            for (uint32_t u = 0; u < 8; ++u) store_pieces(buf + piece_at(u), v[u]);
+                            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                            __syncwarp();
+                            if (lane == 0) {
+                                store_box(image + which, r0, c0, buf);
+                                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                            }
+                        }
                     }
                 } else if (T == OUT_BF16) {
                     // rows of the flat vector: 8 lanes write 128 bytes of one, whatever its alignment allows
@@ -1417,6 +1488,8 @@ struct deco_orth {
     ConvertPiece *convert = nullptr;
     Tile *tiles = nullptr;
     uint32_t *starts = nullptr, *narrow_list = nullptr;
+    float *part_sums = nullptr;
+    uint32_t *arrived = nullptr;
     double *partial = nullptr;
     uint32_t *status = nullptr;
     uint64_t device_bytes = 0, launches = 0;
@@ -1437,6 +1510,8 @@ void release(deco_orth *h)
     cudaFree(h->convert);
     cudaFree(h->tiles);
     cudaFree(h->starts);
+    cudaFree(h->part_sums);
+    cudaFree(h->arrived);
     cudaFree(h->narrow_list);
     cudaFree(h->partial);
     cudaFree(h->status);
@@ -1499,6 +1574,8 @@ uint32_t passes(const Mat &M, int phase) { return phase == APPLY ? 1 + M.precisi
 // k: with 256 rows per CTA either way that is 10 to 13 cycles for each k of a tile, where the products take 4
 // (one CTA) or 8 (a pair); measured 13 for a lone CTA, 9 to 10 with all SMs at work on pairs of
 // CTAs.  Then the ends that do not overlap.
+// Parts of a sum are worth their join from some length on: MIN_PART of k takes 9000 cycles, the join of four 5000.
+constexpr uint32_t MAX_PARTS = 8, MIN_PART = 512;
 double tile_cost(uint32_t cg, uint32_t k) { return cg == 1 ? 9.0 * k + 3000 : 10.0 * k + 4500; }
 
 deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, uint64_t cap)
@@ -1594,8 +1671,9 @@ deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, ui
         both(MAP_A + 1, M.a_lo, M.m, M.m, M.lda);
         both(MAP_P, M.p, M.m, M.m, M.lda);
         both(MAP_P + 1, M.p_lo, M.m, M.m, M.lda);
-        ok = ok && encode(enc, map + MIRROR_A, M.a, M.m, M.m, M.lda, 32, 64) &&
-             encode(enc, map + MIRROR_P, M.p, M.m, M.m, M.lda, 32, 64);
+        __half *mirrored[4] = {M.a, M.a_lo, M.p, M.p_lo};
+        for (int k = 0; k < 4; ++k)
+            ok = ok && (!mirrored[k] || encode(enc, map + MIRROR_A + k, mirrored[k], M.m, M.m, M.lda, 32, 64));
         if (!ok) return DECO_ERR_CUDA;
     }
     // pieces: matrices whose rows are back to back, in order of their place; then everything else
@@ -1635,6 +1713,7 @@ deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, ui
     std::vector<Tile> tiles;
     std::vector<ConvertPiece> convert;
     std::vector<uint32_t> starts;
+    uint32_t part_slots = 0;
     for (uint32_t g = 0; g < groups; ++g) {
         Group G = {};
         G.convert0 = static_cast<uint32_t>(convert.size());
@@ -1655,8 +1734,10 @@ deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, ui
             std::stable_sort(by.begin(), by.end(), [&](uint32_t x, uint32_t y) { return depth(x) > depth(y); });
             double best = 0;
             std::vector<std::vector<Tile>> chosen;
-            for (uint32_t cg = 1; cg <= 2; ++cg) {
-                const uint32_t side = 128 * cg;
+            uint32_t best_slots = 0;
+            // one CTA per tile, the sums of GRAM in up to MAX_PARTS parts, or a pair of CTAs per tile
+            for (uint32_t way = 1; way <= (phase == GRAM ? 2 * MAX_PARTS : 2u); way *= 2) {
+                const uint32_t cg = way == 2 ? 2 : 1, most_parts = way <= 2 ? 1 : way / 2, side = 128 * cg;
                 auto blocks = [&](uint32_t v) { return (v + side - 1) / side; };
                 // every tile, the longest first, to the lane that is free first
                 std::vector<std::vector<Tile>> lanes(h->sms / cg);
@@ -1664,24 +1745,33 @@ deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, ui
                 std::priority_queue<Load, std::vector<Load>, std::greater<Load>> free;
                 for (uint32_t l = 0; l < lanes.size(); ++l) free.push({0.0, l});
                 double cost = 0;
+                uint32_t slots = 0;
                 for (uint32_t i : by) {
                     const Mat &M = mats[i];
                     const uint32_t nr = blocks(phase == APPLY ? M.rows : M.m), nc = blocks(phase == APPLY ? M.cols : M.m);
+                    const uint32_t parts = std::max(1u, std::min(most_parts, depth(i) / MIN_PART));
                     for (uint32_t r = 0; r < nr; ++r)
                         for (uint32_t c = 0; c < (phase == APPLY ? nc : r + 1); ++c) {
-                            const Load at = free.top();
-                            free.pop();
-                            lanes[at.second].push_back({i, static_cast<uint16_t>(r), static_cast<uint16_t>(c)});
-                            free.push({at.first + tile_cost(cg, depth(i)), at.second});
-                            cost = std::max(cost, at.first + tile_cost(cg, depth(i)));
+                            for (uint32_t q = 0; q < parts; ++q) {
+                                const Load at = free.top();
+                                const double until = at.first + tile_cost(cg, depth(i) / parts) + (parts > 1 ? 2500 + 700 * parts : 0);
+                                free.pop();
+                                lanes[at.second].push_back({i, static_cast<uint16_t>(r), static_cast<uint16_t>(c),
+                                                            static_cast<uint16_t>(q), static_cast<uint16_t>(parts), slots});
+                                free.push({until, at.second});
+                                cost = std::max(cost, until);
+                            }
+                            slots += parts > 1 ? parts : 0;
                         }
                 }
-                if (cg == 1 || cost < best) {
+                if (way == 1 || cost < best) {
                     best = cost;
+                    best_slots = slots;
                     chosen.swap(lanes);
                     G.phase[phase].cg = cg;
                 }
             }
+            part_slots = std::max(part_slots, best_slots);
             Span &span = G.phase[phase];
             span.first = static_cast<uint32_t>(tiles.size());
             span.starts = static_cast<uint32_t>(starts.size());
@@ -1698,11 +1788,16 @@ deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, ui
         h->groups.push_back(G);
     }
     std::vector<double> partial(slot, 0.0);
-    std::vector<uint32_t> status(1, 0u);
+    std::vector<uint32_t> status(1, 0u), arrived(static_cast<size_t>(part_slots) * EPI_WARPS, 0u);
+    if (part_slots) {
+        const uint64_t part_bytes = static_cast<uint64_t>(part_slots) * PART_FLOATS * sizeof(float);
+        if (cudaMalloc(reinterpret_cast<void **>(&h->part_sums), part_bytes) != cudaSuccess) return DECO_ERR_OOM;
+        h->device_bytes += part_bytes;
+    }
     if (!upload(h, &h->mats, mats) || !upload(h, &h->maps, maps) || !upload(h, &h->pieces, pieces) ||
         !upload(h, &h->row_pieces, row_pieces) || !upload(h, &h->convert, convert) || !upload(h, &h->tiles, tiles) ||
         !upload(h, &h->starts, starts) || !upload(h, &h->narrow_list, narrow_list) ||
-        !upload(h, &h->partial, partial) || !upload(h, &h->status, status))
+        !upload(h, &h->arrived, arrived) || !upload(h, &h->partial, partial) || !upload(h, &h->status, status))
         return DECO_ERR_OOM;
     if (!h->narrow.empty() && !h->groups.empty() &&
         (cudaStreamCreateWithFlags(&h->side, cudaStreamNonBlocking) != cudaSuccess ||
@@ -1836,6 +1931,8 @@ cudaError_t run_pass(deco_orth *h, const Source<T> &src, __nv_bfloat16 *out, flo
         g.mats = h->mats;
         g.maps = h->maps;
         g.status = h->status;
+        g.part_sums = h->part_sums;
+        g.arrived = h->arrived;
         g.out = out;
         g.params = params;
         g.lr = lr;
