@@ -161,6 +161,17 @@ def make_workload(name, scale=1.0):
 WORKLOADS = ["flat_1m", "resnet18", "gpt2_small", "sweep_100m", "decoder_1b"]
 
 
+def matrices(wl):
+    """[(offset, rows, cols)] of the workload's tensors of two and more dimensions in its flat
+    vector, a convolution as [out, in * kernel]: what deco_orth_init takes."""
+    out, at = [], 0
+    for t in wl.tensors:
+        if len(t.shape) > 1:
+            out.append((at, t.shape[0], t.fan_in))
+        at += t.numel
+    return out
+
+
 # -------------------------------------------------------------------------- gradients
 
 def _gen(device, seed):

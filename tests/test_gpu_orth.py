@@ -395,3 +395,67 @@ def test_init_without_a_device_fails_loudly():
     with pytest.raises(B.DecoError) as e:
         B.deco_orth_init(100, [(0, 10, 10)])
     assert e.value.status == B.DECO_ERR_CUDA
+
+
+def test_workload_matrices_cover_the_tensors():
+    from paper_2507_17346_b200 import workloads as W
+    wl = W.make_workload("resnet18", 0.25)
+    mats = W.matrices(wl)
+    assert len(mats) == 21 and all(r * c > 0 for _, r, c in mats)
+    assert sum(r * c for _, r, c in mats) + sum(t.numel for t in wl.tensors if len(t.shape) == 1) == wl.d
+    assert all(a[0] + a[1] * a[2] <= b[0] for a, b in zip(mats, mats[1:]))
+
+
+@gpu
+@pytest.mark.parametrize("name,scale", [("resnet18", 0.25), ("gpt2_small", 0.1), ("decoder_1b", 0.1)])
+def test_workload_shapes(name, scale):
+    """The workloads' own tensors (embeddings, convolutions, thin projections), vectors between them."""
+    from paper_2507_17346_b200 import workloads as W
+    wl = W.make_workload(name, scale)
+    mats = W.matrices(wl)
+    x = W.gradients_batched(wl, 0, W.entry_scales(wl, "cuda"))[0].contiguous()
+    m = torch.zeros(wl.d, device="cuda")
+    out = torch.zeros(wl.d, device="cuda", dtype=torch.bfloat16)
+    h = B.deco_orth_init(wl.d, mats, momentum=0.95)
+    try:
+        B.deco_orth_run(h, x, out, momentum=m)
+        assert torch.equal(m, x.float())
+        for at, r, c in mats:
+            assert rel(out[at:at + r * c].view(r, c), exact(x[at:at + r * c].view(r, c))) < tol(r * c)
+        assert B.deco_orth_get_stats(h)["device_status"] == 0
+    finally:
+        B.deco_orth_destroy(h)
+
+
+@gpu
+def test_captured_in_a_graph():
+    """A pass holds nothing that stream capture forbids: both kinds of matrices, fork and join included."""
+    mats, d, x = flat_case([(64, 147), (300, 200), (520, 400)], 3, torch.float32, 9)
+    out, again = (torch.zeros(d, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    h = B.deco_orth_init(d, mats)
+    try:
+        B.deco_orth_run(h, x, out)
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            B.deco_orth_run(h, x, again, stream=s)
+        again.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, again)
+    finally:
+        B.deco_orth_destroy(h)
+
+
+@gpu
+def test_example_trains():
+    """Loss, compressed exchange and orthogonalised update together: the loss falls most of the way from
+    log(vocab) to the entropy rate of the tokens."""
+    from paper_2507_17346_b200 import example_lm
+    losses, model, chain = example_lm.train(steps=120, workers=3, vocab=256, width=64, hidden=128, batch=512)
+    start, floor = math.log(256), chain.entropy_rate()
+    assert abs(losses[0] - start) < 1.0
+    assert losses[-1] < floor + 0.5 * (start - floor), (losses[0], losses[-1], floor)
+    found, entropy = example_lm.alternatives(model, 7)
+    assert len(found) == 5 and all(a[1] >= b[1] for a, b in zip(found, found[1:])) and entropy > 0
