@@ -76,12 +76,16 @@ struct RowPiece {
 struct ConvertPiece {
     uint32_t mat, row0, rows, col0;
 };
-struct Tile {
+struct alignas(16) Tile {
     uint32_t mat;
     uint16_t tm, tn;
     uint16_t part, parts;                // of the sum over k (GRAM)
     uint32_t slot;                       // where the parts' sums go, parts > 1
+    uint32_t k;                          // length of the sum; k, tall and precision as in the matrix's entry: what the
+    uint16_t tall, precision;            // loading thread needs is one read away
+    uint32_t unused[2];
 };
+static_assert(sizeof(Tile) == 32, "two 16-byte reads");
 
 // Which operands of a matrix's products are carried as hi + lo.
 enum Precision { PLAIN = 0, WIDE_P = 1, FULL = 2 };
@@ -290,7 +294,7 @@ enum Phase { GRAM = 0, POLY = 1, APPLY = 2 };
 enum Target { NEXT_X = 0, OUT_BF16 = 1, PARAMS = 2 };
 
 constexpr int BK = 64;                   // k per stage: 128 bytes, one swizzle row
-constexpr int STAGES = 5;
+constexpr int STAGES = 5;                // (four, and a third staging box per warp, were slower for pairs)
 constexpr uint32_t OPERAND_BYTES = 128 * BK * 2;
 constexpr uint32_t STAGE_BYTES = 2 * OPERAND_BYTES;
 constexpr int FIRST_EPI_WARP = 4;        // warps 0: loads, 1: mma, 2: tensor memory
@@ -298,8 +302,8 @@ constexpr int EPI_WARPS = 8;             // two per quarter of the tensor memory
 constexpr int GEMM_THREADS = 32 * (FIRST_EPI_WARP + EPI_WARPS);
 constexpr int CHUNK = 64;                // columns an epilogue warp takes at a time
 constexpr uint32_t CHUNK_BYTES = 32 * CHUNK * 2;
-constexpr uint32_t STAGING_BYTES = 2 * CHUNK_BYTES;      // of a warp: hi and lo
 constexpr uint32_t PART_FLOATS = 128 * 128;
+constexpr uint32_t STAGING_BYTES = 2 * CHUNK_BYTES;      // of a warp
 constexpr size_t GEMM_SMEM = STAGES * STAGE_BYTES + EPI_WARPS * STAGING_BYTES + 1024;
 
 struct GemmArgs {
@@ -492,18 +496,19 @@ struct Operands {
     __device__ __forceinline__ uint32_t start(uint32_t part, uint32_t parts) const { return blocks() * part / parts; }
 };
 template <Phase P>
-__device__ __forceinline__ Operands operands(const GemmArgs &g, const Mat &M, uint32_t mat)
+__device__ __forceinline__ Operands operands(const GemmArgs &g, const Tile &tl)
 {
-    const CUtensorMap *at = g.maps + static_cast<uint64_t>(mat) * MAPS;
+    const CUtensorMap *at = g.maps + static_cast<uint64_t>(tl.mat) * MAPS;
     const CUtensorMap *x = at + MAP_X + 2 * g.src, *am = at + MAP_A, *pm = at + MAP_P;
-    const uint32_t full = M.precision == FULL;
+    const uint32_t full = tl.precision == FULL;
+    const bool tall = tl.tall != 0;
     // hi hi, hi lo, lo hi
-    if (P == GRAM) return {x, x, M.tall != 0, M.tall != 0, M.n, full ? 3u : 1u, 4, 2};
-    if (P == POLY) return {am, am, false, false, M.m, full ? 3u : 1u, 4, 2};
+    if (P == GRAM) return {x, x, tall, tall, tl.k, full ? 3u : 1u, 4, 2};
+    if (P == POLY) return {am, am, false, false, tl.k, full ? 3u : 1u, 4, 2};
     // (P, X): hi hi, lo hi, hi lo
-    const uint32_t passes = 1 + M.precision;
-    if (M.tall) return {x, pm, false, false, M.m, passes, 4, 2};
-    return {pm, x, false, true, M.m, passes, 2, 4};
+    const uint32_t passes = 1u + tl.precision;
+    if (tall) return {x, pm, false, false, tl.k, passes, 4, 2};
+    return {pm, x, false, true, tl.k, passes, 2, 4};
 }
 
 // A CTA (CG = 1: tiles of 128 x 128) or a pair of CTAs (CG = 2: 256 x 256, each CTA half of the rows of
@@ -584,9 +589,11 @@ gemm_kernel(const GemmArgs g)
             uint32_t s = 0, parity = 1;
             const uint32_t full0 = smem_addr(ctl.full), bar0 = CG == 1 ? full0 : leader_addr(full0);
             bool ok = true;
+            Tile next = g.tiles[first];
             for (uint32_t t = first; ok && t < end; ++t) {
-                const Tile tl = g.tiles[t];
-                const Operands op = operands<P>(g, g.mats[tl.mat], tl.mat);
+                const Tile tl = next;
+                if (t + 1 < end) next = g.tiles[t + 1];          // (there when this tile is done)
+                const Operands op = operands<P>(g, tl);
                 const int32_t ra = tl.tm * SIDE + rank * 128, rb = tl.tn * SIDE + rank * 128;
                 const uint32_t per_pass = (op.k + BK - 1) / BK;
                 const uint32_t b0 = op.start(tl.part, tl.parts), b1 = op.start(tl.part + 1, tl.parts);
@@ -629,9 +636,11 @@ gemm_kernel(const GemmArgs g)
         if (lane == 0 && rank == 0) {
             uint32_t s = 0, parity = 0, n = 0;
             bool ok = true;
+            Tile next = g.tiles[first];
             for (uint32_t t = first; ok && t < end; ++t, ++n) {
-                const Tile tl = g.tiles[t];
-                const Operands op = operands<P>(g, g.mats[tl.mat], tl.mat);
+                const Tile tl = next;
+                if (t + 1 < end) next = g.tiles[t + 1];
+                const Operands op = operands<P>(g, tl);
                 const uint32_t as = n & 1;
                 if (!bar_wait(&ctl.acc_empty[as], ((n >> 1) & 1) ^ 1, &ctl.abort, g.status)) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -658,7 +667,10 @@ gemm_kernel(const GemmArgs g)
         }
     } else if (wid >= FIRST_EPI_WARP) {
         const int ew = wid - FIRST_EPI_WARP, quad = wid & 3, side = ew >> 2;
-        const uint32_t hi_buf = stages + STAGES * STAGE_BYTES + ew * STAGING_BYTES, lo_buf = hi_buf + CHUNK_BYTES;
+        // POLY adds A to the product and APPLY X's lo: these come in, and go out, through one box, what else goes out
+        // through the other
+        const uint32_t staging = stages + STAGES * STAGE_BYTES + ew * STAGING_BYTES;
+        const uint32_t hi_buf = staging + (P == APPLY ? CHUNK_BYTES : 0), lo_buf = staging + (P == APPLY ? 0 : CHUNK_BYTES);
         const uint32_t my_row = lane * 128, perm = lane & 7;
         constexpr uint32_t CHUNKS = SIDE / 2 / CHUNK;            // of this warp, per tile
         uint32_t n = 0, loads = 0;
@@ -728,14 +740,12 @@ gemm_kernel(const GemmArgs g)
                     ok = bar_wait(&ctl.staged[ew], loads & 1, &ctl.abort, g.status);
                     if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
                     loads += 1;
-                } else {
-                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-                    __syncwarp();
                 }
 #pragma unroll
                 for (uint32_t h = 0; h < 2; ++h) {
                     uint32_t v[32];
                     if (!split) {
+                        if (h) __syncwarp();
                         tmem_load32(acc_at + h * 32, v);
                     } else {
 #pragma unroll
@@ -750,6 +760,10 @@ gemm_kernel(const GemmArgs g)
                             v[4 * u + 2] = __float_as_uint(a.z);
                             v[4 * u + 3] = __float_as_uint(a.w);
                         }
+                    }
+                    if (h == 0 && !fetches) {                    // the boxes written next may still be on their way out
+                        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                        __syncwarp();
                     }
 #pragma unroll
                     for (uint32_t u = 0; u < 4; ++u) {
@@ -1757,7 +1771,9 @@ deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, ui
                                 const double until = at.first + tile_cost(cg, depth(i) / parts) + (parts > 1 ? 2500 + 700 * parts : 0);
                                 free.pop();
                                 lanes[at.second].push_back({i, static_cast<uint16_t>(r), static_cast<uint16_t>(c),
-                                                            static_cast<uint16_t>(q), static_cast<uint16_t>(parts), slots});
+                                                            static_cast<uint16_t>(q), static_cast<uint16_t>(parts), slots,
+                                                            phase == GRAM ? M.n : M.m, static_cast<uint16_t>(M.tall),
+                                                            static_cast<uint16_t>(M.precision), {0, 0}});
                                 free.push({until, at.second});
                                 cost = std::max(cost, until);
                             }
