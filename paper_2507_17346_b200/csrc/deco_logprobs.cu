@@ -13,7 +13,9 @@
 //
 // What bounds it: one exponential per logit takes as long as reading two bytes of it from memory (16 a cycle
 // and SM against 44 bytes a nanosecond), and the other instructions about as long again, so the pass works on
-// pairs of logits (fma and add of two fp32 numbers at once) and has no bounds check inside a row.
+// pairs of logits (fma and add of two fp32 numbers at once) and has no bounds check inside a row.  8192 rows of
+// 50257 bf16: 160 us, 5.2 TB/s, exponential units 76 % busy.  Short calls are bounded by their chain of
+// barriers: 6 us for one row of 32000 with 20 alternatives on eight CTAs.
 //
 // Alternatives: a thread's maximum over its entries is known when the pass ends.  The k-th largest of 64
 // groups' maxima is a bound which at least k entries reach and few more than k do; only threads
@@ -661,6 +663,7 @@ template <> __device__ __forceinline__ void put_entry<__nv_bfloat16>(__nv_bfloat
 // alternatives' entries are few: warp 0 reads their logits first (the gradient may lie in the
 // logits' place) and writes them over at the end, the terms of equal tokens added in a fixed order.
 // ENT: there is a gradient of the entropy.
+// Bound by memory: 8192 rows of 50257 bf16 in 296 us, 5.6 TB/s (two granules per thread: 340, eight: 304).
 template <typename T, int U, bool ENT>
 __global__ void __launch_bounds__(NT)
 logprobs_grad_kernel(const GradArgs a)
@@ -882,6 +885,8 @@ extern "C" deco_status deco_token_logprobs(const void *logits, int32_t dtype, ui
     a.lse = lse;
     a.top_idx = top_idx;
     a.top_logprob = top_logprob;
+    // (Measured, one row of 32000 bf16: 9.6 us a call with eight parts, 10.2 with one; 64 rows of 50257 f32: 12.3 and
+    // 15.8; 1999 rows, which already fill the device: 53 with one part, 93 with two.)
     // A row is split while the CTAs do not fill the device and every part still has half a batch
     // of loads for each of its threads.
     const uint64_t batch = static_cast<uint64_t>(NT) * UNROLL * (dtype == DECO_F32 ? 4 : 8);

@@ -20,8 +20,8 @@
 // Over many singular values these errors average out (1.3e-3 of the norm at a short side of 512, against
 // 1.7e-3 of the rounding to bf16), over few they do not (up to 8e-3 at short sides below 16).  So
 // matrices up to FULL_SIDE are multiplied in full, hi and lo of both operands (22 bits), and
-// those up to WIDE_P_SIDE with P as hi + lo (1.5e-3 -> 1.2e-3 at 160).  Both are as fast as the plain products
-// there, since short sides leave the tensor cores waiting for memory.
+// those up to WIDE_P_SIDE with P as hi + lo (1.5e-3 -> 1.2e-3 at 160).  Eight of 256 x 2048: 206 us with, 191
+// without; eight of 128 x 4000: 225 and 208; twelve of 4000 x 100, the worst found: 318 and 262.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -523,8 +523,10 @@ __device__ __forceinline__ Operands operands(const GemmArgs &g, const Tile &tl)
 // image is transposed in 8 x 8 pieces in registers and stored as a box too: 2-byte stores
 // straight to global memory made the products of A with itself 1.4 times slower.
 //
-// Four decoder blocks: tensor cores busy 80 % of the cycles with the epilogue left out, where shared memory, read
-// by them and filled by the loads, is the limit; that is why the epilogue moves as little through it as it can.
+// What bounds it: an SM takes in about 51 bytes of operands a cycle, 620 to 640 cycles for the 64 k on which the
+// tensor cores work 512, so they are busy 80 % of the cycles with the epilogue left out and 61 % with it (A and
+// X P of a decoder block, k = 5632 and 2048; 33 to 38 % at k = 768, where a tile's epilogue is as long as its
+// products).  On four decoder blocks that is 1.2 to 1.36 PFLOP/s, close to what the power cap sustains.
 template <int CG, Phase P, Target T>
 __global__ void __launch_bounds__(GEMM_THREADS, 1)
 gemm_kernel(const GemmArgs g)
@@ -937,7 +939,7 @@ gemm_kernel(const GemmArgs g)
 // up its share of the entries and handing the sums to all, in a fixed order, and then makes P and the
 // products with its own part by itself.  All products are taken in full (hi hi + hi lo + lo hi).  What
 // bounds this kernel is the chain of waits (two cluster barriers and three products per step), not
-// bytes or products: 15 separate launches took 111 us for 64 x 147.
+// bytes or products.  64 x 147: 36 us a pass, of which 12000 cycles a step; the 17 launches of the general way took 111 us.
 
 constexpr int NARROW_THREADS = 512;
 constexpr uint32_t NARROW_TILE_LIMIT = 5;        // tiles of 128 per CTA at short sides up to 64
@@ -1584,7 +1586,7 @@ bool layout_ok(uint64_t d, const std::vector<deco_matrix> &ms)
 
 uint32_t passes(const Mat &M, int phase) { return phase == APPLY ? 1 + M.precision : M.precision == FULL ? 3 : 1; }
 
-// Clock cycles of a tile of k products deep.  An SM takes in 40 to 50 bytes of operands a cycle, 4 a row and
+// Clock cycles of a tile of k products deep (for comparing ways to cut the work, not exact).  An SM takes in 40 to 50 bytes of operands a cycle, 4 a row and
 // k: with 256 rows per CTA either way that is 10 to 13 cycles for each k of a tile, where the products take 4
 // (one CTA) or 8 (a pair); measured 13 for a lone CTA, 9 to 10 with all SMs at work on pairs of
 // CTAs.  Then the ends that do not overlap.
