@@ -2,10 +2,12 @@
 // logits, with entropy, log-sum-exp and the largest alternatives, and the gradient of all of them.
 //
 // Forward: one pass over the logits.  With c = scale * log2(e) a thread keeps, for the entries
-// it has seen, the maximum m, s = sum 2^t and q = sum 2^t t with t = x c - m c; a larger maximum
-// multiplies s by f = 2^((m_old - m_new) c) and turns q into f (q + (m_old - m_new) c s).  At the
-// end of the row  lse = ln2 (m c + log2 s),  entropy = ln2 (log2 s - q / s),  and
-// logprob = ln2 (t_target - log2 s), in which the rounding of m c cancels.
+// it has seen, the maximum m, s = sum 2^t and q = sum 2^t t with t = x c - S, where S is m c rounded.
+// A larger maximum multiplies s by f = 2^(S_old - S_new) and turns q into f (q + (S_old - S_new) s): the
+// difference of the rounded numbers, against which the sums were taken, so that what rounding
+// did to S is in no result, however far from 0 the logits are.  At the end of the row
+// entropy = ln2 (log2 s - q / s),  logprob = ln2 (t_target - log2 s)  and
+// lse = m scale + ln2 (log2 s - (m c - S)).
 //
 // A row is one CTA's work, or a cluster's of 2, 4 or 8 CTAs, each with a contiguous part of it,
 // where the rows alone would leave most of the device idle; the parts are joined through
@@ -44,8 +46,8 @@ constexpr float LOG2E_LO = 1.9259629911266175e-8f;               // log2(e) - LO
 constexpr float LN2 = 0.6931471805599453f;
 // The streaming path treats entries below FLOOR as FLOOR, with weight 0 (masks of -inf, of the
 // type's lowest value, of -1e10 ...).  That is exact for rows whose maximum m has |m c| < SPAN and
-// scales in [SCALE_LO, SCALE_HI]: then (FLOOR - m) c < -2^20, and the rounding of m c, a common
-// factor of all weights, is below 2^(1/16).  All other rows, and rows with a NaN, take the slow path.
+// scales in [SCALE_LO, SCALE_HI]: then (FLOOR - m) c < -2^20, and a weight of the maximum, 2^(m c - S), lies
+// within 2^(1/16) of 1.  All other rows, and rows with a NaN, take the slow path.
 constexpr float FLOOR = -0x1p30f;
 constexpr float SPAN = 0x1p20f;
 constexpr float SCALE_LO = 0x1p-8f, SCALE_HI = 0x1p8f;
@@ -229,12 +231,13 @@ struct Row {
     }
 };
 
-struct Part {                            // softmax statistics of some entries
+struct Part {                            // softmax statistics of some entries, against S = m c rounded
     float m, s, q;
 };
-__device__ __forceinline__ void raise(Part &a, float m, float c)
+// (shift, to: S of a.m and of m)
+__device__ __forceinline__ void raise(Part &a, float shift, float m, float to)
 {
-    const float d = (a.m - m) * c, f = ex2(d);
+    const float d = shift - to, f = ex2(d);
     a.q = f * __fmaf_rn(d, a.s, a.q);
     a.s = f * a.s;
     a.m = m;
@@ -245,7 +248,7 @@ __device__ __forceinline__ Part join_lanes(Part a, float c, uint32_t width)
 {
     float m = a.m;
     for (uint32_t o = 1; o < width; o *= 2) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-    raise(a, m, c);
+    raise(a, __fmul_rn(a.m, c), m, __fmul_rn(m, c));
     for (uint32_t o = 1; o < width; o *= 2) {
         a.s += __shfl_xor_sync(0xFFFFFFFFu, a.s, o);
         a.q += __shfl_xor_sync(0xFFFFFFFFu, a.q, o);
@@ -423,6 +426,7 @@ logprobs_kernel(const Args a)
         };
         fetch(v0);
         const uint64_t c2 = pair(c, c);
+        float mc = __fmul_rn(my.m, c);
         for (uint32_t vb = v0; vb < v1; vb += NT * UNROLL) {
             float bm = FLOOR;
 #pragma unroll
@@ -432,9 +436,13 @@ logprobs_kernel(const Args a)
                 bm = fmaxf(bm, Elem<T>::clamp_max(w[u]));
             }
             if (vb + NT * UNROLL < v1) fetch(vb + NT * UNROLL);
-            if (bm > my.m) raise(my, bm, c);
-            const float mc = my.m == FLOOR ? 0.f : my.m * c;     // nothing but FLOOR yet: weights 0
-            const uint64_t shift = pair(-mc, -mc);
+            if (bm > my.m) {
+                const float to = __fmul_rn(bm, c);
+                raise(my, mc, bm, to);
+                mc = to;
+            }
+            const float from = my.m == FLOOR ? 0.f : -mc;        // nothing but FLOOR yet: weights 0
+            const uint64_t shift = pair(from, from);
             uint64_t s = pair(my.s, 0.f), q = pair(my.q, 0.f);
 #pragma unroll
             for (int u = 0; u < UNROLL; ++u)
@@ -564,9 +572,9 @@ logprobs_kernel(const Args a)
     bool empty = false;
     if (fast) {
         zs = c;
-        zm = all.m * c;
+        zm = __fmul_rn(all.m, c);
         logz = log2f(all.s);
-        lse = LN2 * (zm + logz);
+        lse = __fmaf_rn(all.m, a.scale, LN2 * (logz - __fmaf_rn(all.m, c, -zm)));
         entropy = fmaxf(LN2 * (logz - __fdiv_rn(all.q, all.s)), 0.f);
     } else {
         // NaN, infinities, rows of masked entries only, extreme scales: two plain passes of the

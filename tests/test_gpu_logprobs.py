@@ -253,6 +253,18 @@ def test_outputs_are_optional_and_repeatable():
         assert torch.equal(full[k], other[k])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("offset", [300.0, -1000.0, 1e4, -5e5, 5.5e5])
+def test_common_offset_of_the_logits(offset, dtype):
+    """A constant added to a row changes its lse and nothing else: the tolerances are those without
+    it.  Rows on one CTA and on several, whose threads and parts have different maxima."""
+    for rows, scale in ((3, 1.0), (700, 1.0), (3, 1.25)):
+        x = rows_of(rows, 9001, dtype, 11, sigma=2.5)
+        x += offset
+        t = targets_for(rows, 9001, 6)
+        check(call(x, t, 8, scale), reference(x, t, 8, scale), 9001, 8)
+
+
 # ------------------------------------------------------------------------------- gradient
 
 def grads_for(rows, top, seed):
