@@ -42,7 +42,6 @@ constexpr int GROUPS = 64;               // groups of threads whose maxima bound
 constexpr int MAX_TOP = DECO_LOGPROBS_MAX_TOP;
 constexpr int LIST = 1024;               // candidates kept for the alternatives
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr float LOG2E_LO = 1.9259629911266175e-8f;               // log2(e) - LOG2E
 constexpr float LN2 = 0.6931471805599453f;
 // The streaming path treats entries below FLOOR as FLOOR, with weight 0 (masks of -inf, of the
 // type's lowest value, of -1e10 ...).  That is exact for rows whose maximum m has |m c| < SPAN and
@@ -657,6 +656,7 @@ struct GradArgs {
     uint32_t vocab, top, chunks;
     const int64_t *targets;
     float scale;
+    float c, c_rest;                     // scale log2(e) rounded, and c / scale - LOG2E (a division per thread cost 12 %)
     const float *lse, *entropy, *g_logprob, *g_entropy;
     const uint32_t *top_idx;
     const float *g_top;
@@ -717,10 +717,12 @@ logprobs_grad_kernel(const GradArgs a)
         return empty ? 0.f : a.scale * (own_g - u);
     };
     // For lse and scale in the usual range: p = f 2^t, t = x c - L, where L is lse log2(e) rounded and
-    // f = 2^-(what the rounding left);  log p + entropy = ln2 t + (entropy - ln2 (the rest)).  So an entry is
+    // f = 2^-rest.  rest is what lse / scale times c, c as rounded, has over L: an error of c then acts on
+    // x - lse / scale, which is small where p is not, instead of on x and lse apart.
+    // log p + entropy = ln2 t + (entropy - ln2 rest).  So an entry is
     // 2^t (A t + B), or 2^t B without the entropy's term; logits below FLOOR count as FLOOR there (p = 0).
-    const float c = a.scale * LOG2E, big = lse * LOG2E;
-    const float rest = __fmaf_rn(lse, LOG2E, -big) + lse * LOG2E_LO;
+    const float c = a.c, big = lse * LOG2E;
+    const float rest = __fmaf_rn(lse, LOG2E, -big) + lse * a.c_rest;
     const float f = -a.scale * ex2(-rest);
     const float coef_a = f * g_h * LN2, coef_b = f * __fmaf_rn(g_h, h - LN2 * rest, total);
     const bool usual = fabsf(big) < SPAN && a.scale >= SCALE_LO && a.scale <= SCALE_HI;
@@ -936,6 +938,8 @@ extern "C" deco_status deco_token_logprobs_grad(const void *logits, int32_t dtyp
     a.top = top;
     a.targets = targets;
     a.scale = scale;
+    a.c = scale * LOG2E;
+    a.c_rest = static_cast<float>(static_cast<double>(a.c) / scale - static_cast<double>(LOG2E));
     a.lse = lse;
     a.entropy = entropy;
     a.g_logprob = g_logprob;

@@ -389,6 +389,41 @@ def test_gradient_against_differences():
         assert abs(dx[r, j].item() - want) < 2e-5
 
 
+def grad_from_lse(x, t, scale, lse, entropy, idx, gl, gh, gt):
+    """The formula in 64 bits with p = exp(z - lse) of the lse as given; and p."""
+    z = x.double() * scale
+    lp = z - lse.double()[:, None]
+    ref = {"p": lp.exp(), "lp": lp, "entropy": entropy.double()}
+    return grad_reference(x, t, scale, ref, idx, gl, gh, gt), ref["p"]
+
+
+@pytest.mark.parametrize("ent", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("offset", [0.0, 300.0, -1e4, 5e5])
+def test_gradient_follows_the_lse_it_is_given(offset, dtype, ent):
+    """p = exp(z - lse) for the lse handed in, which is exact here whatever its size: a weight's error
+    is that of a sum without an offset (82 eps and 20 for the row's factor), times what it multiplies.
+    Logits more than 40 below lse have p < 2^-57 and do not show."""
+    rows, v, top = 5, 9001, 4
+    for scale in (1.0, 1.25, 0.3):
+        scale = float(np.float32(scale))
+        x = rows_of(rows, v, dtype, 21, sigma=2.5)
+        x += offset
+        t = targets_for(rows, v, 3)
+        out = call(x, t, top, scale)
+        gl, gh, gt = grads_for(rows, top, 8)
+        gh = gh if ent else None
+        want, p = grad_from_lse(x, t, scale, out["lse"], out["entropy"], out["top_idx"], gl, gh, gt)
+        f = gl.abs().double() + gt.abs().double().sum(1)
+        w = f[:, None] + (gh.abs().double() * (41 + out["entropy"].double()) if ent else 0 * f)[:, None]
+        own = torch.zeros_like(want).scatter_(1, t.clamp_min(0)[:, None], 1.0).scatter_(1, out["top_idx"].long(), 1.0)
+        tol = scale * (102 * EPS * p * w + 16 * EPS * own * f[:, None]) + want.abs() * 2.0 ** (-8 if dtype == "bf16" else -23)
+        dx = torch.empty_like(x)
+        B.deco_token_logprobs_grad(x, t, out["lse"], dx, g_logprob=gl, entropy=out["entropy"], g_entropy=gh,
+                                   top_idx=out["top_idx"], g_top=gt, scale=scale)
+        close(dx, want, tol + 1e-36)
+
+
 # ------------------------------------------------------------------------------- refusals
 
 def test_refusals():
