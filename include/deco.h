@@ -474,9 +474,11 @@ deco_status deco_token_logprobs(const void *logits, int32_t dtype, uint64_t rows
  *              + sum_i g_top[r][i] top_logprob[r][i]   with respect to the logits:
  *   grad[r][j] = scale * ( sum of the g's whose token is j  -  p_j * (sum of all the g's)
  *                          - g_entropy[r] * p_j * (log p_j + entropy[r]) )
- * with the g of a row whose target is < 0 left out.  The alternatives' choice is not
- * differentiated.  A row whose lse is -inf has the gradient 0; a target >= vocab gives a row of NaN
- * (if g_logprob is given).
+ * with the g_logprob of a row whose target is < 0 left out.  The alternatives' choice is not
+ * differentiated.  p_j is exp(z_j - lse[r]) and so carries the rounding of lse, 2^-24 |lse|; where |lse|
+ * is 2^20 ln 2 or more or infinite (a row of the type's lowest value, say), the row's own maximum and
+ * sum are formed again and lse is not used.  A row of -inf alone has the gradient 0; a target >= vocab
+ * gives any other row NaN (if g_logprob is given).
  *   lse      DEVICE, [rows], as deco_token_logprobs wrote it;  entropy likewise, needed (and
  *            read) only with g_entropy
  *   g_logprob (with targets), g_entropy, g_top (with top_idx)   DEVICE, fp32; each may be NULL

@@ -424,6 +424,47 @@ def test_gradient_follows_the_lse_it_is_given(offset, dtype, ent):
         close(dx, want, tol + 1e-36)
 
 
+@pytest.mark.parametrize("inplace", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,vocab", [(6, 37), (6, 50257), (150, 9001)])
+def test_gradient_of_rows_whose_lse_has_lost_its_last_digits(rows, vocab, dtype, inplace):
+    """Rows of the type's lowest value or another finite mask alone, and logits of 1e7 and more: the spacing of
+    fp32 there is larger than log(vocab), so an lse does not tell one token from all.  With z - max exact (these
+    logits and scales) p is off by that of expf and the sum: 8 eps, |z - max| eps, |log sum| eps, sum_tol."""
+    lowest = torch.finfo(DT[dtype]).min
+    for scale in (1.0, 2.0):                                       # twice the lowest value overflows
+        x = rows_of(rows, vocab, dtype, 31, pad=3, lead=1)
+        x[0], x[1], x[2] = lowest, -1e9, -1e25
+        x[3] = lowest
+        x[3, 3::7] = -3e8                                          # a few above the others, equal
+        x[4] = 2.0 ** 24 * (1 + torch.arange(vocab, device="cuda") % 3)
+        x[5] = -math.inf
+        t = targets_for(rows, vocab, 2)
+        t[:6] = torch.tensor([2, vocab - 1, -1, 3, 5, 1], device="cuda")
+        top = 3
+        out, ref = call(x, t, top, scale), reference(x, t, top, scale)
+        gl, gh, gt = grads_for(rows, top, 5)
+        keep = slice(0, 5)
+        for g_h in (None, gh):
+            want = grad_reference(x, t, scale, ref, ref["top_idx"], gl, g_h, gt)[keep]
+            f = (gl.abs().double() + gt.abs().double().sum(1))[keep, None]
+            h = ref["entropy"][keep, None]
+            w = f + (gh.abs().double()[keep, None] * (41 + h) if g_h is not None else 0)
+            own = torch.zeros_like(want).scatter_(1, t[keep].clamp_min(0)[:, None], 1.0)
+            own.scatter_(1, out["top_idx"][keep].long(), 1.0)
+            p = ref["p"][keep]
+            tol = scale * (((50 + h) * 2 * EPS + 2 * sum_tol(vocab)) * p * w + 16 * EPS * own * f)
+            tol = tol + want.abs() * 2.0 ** (-8 if dtype == "bf16" else -23)
+            logits = x.clone() if inplace else x
+            dx = logits if inplace else torch.empty_like(x)
+            B.deco_token_logprobs_grad(logits, t, out["lse"], dx, g_logprob=gl, entropy=out["entropy"], g_entropy=g_h,
+                                       top_idx=out["top_idx"], g_top=gt, scale=scale)
+            close(dx[keep], want, tol + 1e-38)
+            assert (dx[5] == 0).all()
+            if rows > 6:                                           # ordinary rows of the same call
+                assert torch.isfinite(dx[6:]).all() and (dx[6:] != 0).any(1).all()
+
+
 # ------------------------------------------------------------------------------- refusals
 
 def test_refusals():
