@@ -747,7 +747,7 @@ gemm_kernel(const GemmArgs g)
                 for (uint32_t h = 0; h < 2; ++h) {
                     uint32_t v[32];
                     if (!split) {
-                        if (h) __syncwarp();
+                        __syncwarp();
                         tmem_load32(acc_at + h * 32, v);
                     } else {
 #pragma unroll
@@ -846,6 +846,7 @@ gemm_kernel(const GemmArgs g)
                         for (uint32_t which = 0; which < 2; ++which) {
                             const uint32_t buf = which ? lo_buf : hi_buf;
                             uint32_t v[8][4];
+                            __syncwarp();
 #pragma unroll
                             for (uint32_t u = 0; u < 8; ++u) transposed(buf + my_row + ((u ^ perm) << 4), v[u]);
                             if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
@@ -964,8 +965,10 @@ struct NarrowControl {
     volatile uint32_t abort;
 };
 
+// (All lanes of a warp must come to an .aligned instruction together, whatever loop they leave before it.)
 __device__ __forceinline__ void cluster_sync()
 {
+    __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
@@ -1080,6 +1083,7 @@ narrow_kernel(const NarrowArgs g, const Source<T> src)
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (wid == 0) {
+        __syncwarp();
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                      :: "r"(smem_addr(&ctl.tmem)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
@@ -1177,6 +1181,7 @@ narrow_kernel(const NarrowArgs g, const Source<T> src)
     bool ok = true;
     // every thread's writes to the operands, then the products of thread 0, then everyone waits for them
     auto products = [&](auto issue) {
+        __syncwarp();
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         __syncthreads();
@@ -1349,6 +1354,7 @@ narrow_kernel(const NarrowArgs g, const Source<T> src)
             }
         }
     }
+    __syncwarp();
     // the launch before this one may still run: its results are this one's to be waited for as well
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");

@@ -105,6 +105,18 @@ def test_shapes(rows, cols, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("rows,cols", [(48, 100), (48, 1500), (1500, 41), (80, 128), (80, 1000), (1000, 72), (112, 250),
+                                       (97, 1024), (1024, 111), (176, 3000), (208, 176)])
+def test_short_sides_that_are_no_multiple_of_a_warp(rows, cols):
+    """Lanes beyond the short side leave the kernels' loops early: one to eight CTAs, and the general way."""
+    x = make(rows, cols, "normal", rows + cols)
+    first = run_one(x)
+    assert rel(first, exact(x)) < tol(x.numel())
+    for _ in range(3):
+        assert torch.equal(run_one(x), first)
+
+
+@gpu
 @pytest.mark.parametrize("kind", ["outlier", "rank1", "lowrank", "sparse", "tiny"])
 @pytest.mark.parametrize("rows,cols", [(96, 200), (520, 260), (700, 768)])
 def test_spectra(rows, cols, kind):
