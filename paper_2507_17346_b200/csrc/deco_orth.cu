@@ -1065,7 +1065,6 @@ narrow_kernel(const NarrowArgs g, const Source<T> src)
     extern __shared__ uint8_t raw[];
     __shared__ NarrowControl ctl;
     const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31, quad = wid & 3, part_of = wid >> 2;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const uint32_t rank = C == 1 ? 0 : blockIdx.x % C;
     const Mat &M = g.mats[g.list[blockIdx.x / C]];
     const uint32_t m = M.m, n = M.n, side = (m + 15) & ~15u;
@@ -1095,6 +1094,9 @@ narrow_kernel(const NarrowArgs g, const Source<T> src)
     // X starts as zeros: what lies beyond the matrix stays zero
     for (uint32_t b = tid * 16; b < 2 * L.x + 2 * L.ab; b += NARROW_THREADS * 16) sts16(base + b, make_uint4(0, 0, 0, 0));
     __syncthreads();
+    // Not before the tensor memory is taken: a dependent launch with tensor memory of its own could
+    // come to hold columns here that the allocation above waits for, while it waits for this launch.
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     // A warp per row of memory (short rows: several), many entries of a lane under way.  The entries wait
     // in the places of their hi and lo for the norm, upper and lower half of the fp32 number.
     const uint32_t fast = tall ? m : count, slow = tall ? count : m;

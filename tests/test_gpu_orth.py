@@ -471,3 +471,40 @@ def test_example_trains():
     assert losses[-1] < floor + 0.5 * (start - floor), (losses[0], losses[-1], floor)
     found, entropy = example_lm.alternatives(model, 7)
     assert len(found) == 5 and all(a[1] >= b[1] for a, b in zip(found, found[1:])) and entropy > 0
+
+
+def test_tensor_memory_is_taken_before_dependents_may_start():
+    """In every kernel that takes tensor memory, the allocation and a block barrier come before
+    griddepcontrol.launch_dependents: a dependent that holds columns waits for this launch to end."""
+    import os
+    import re
+    path = os.path.join(os.path.dirname(B.__file__), "csrc", "deco_orth.cu")
+    kernels = re.split(r"^__global__", open(path).read(), flags=re.M)[1:]
+    seen = 0
+    for k in kernels:
+        k = re.split(r"^}", k, flags=re.M)[0]
+        if "tcgen05.alloc" not in k or "griddepcontrol.launch_dependents" not in k:
+            continue
+        seen += 1
+        alloc, start = k.rindex("tcgen05.alloc"), k.index("griddepcontrol.launch_dependents")
+        assert alloc < start and "__syncthreads()" in k[alloc:start]
+    assert seen == 2
+
+
+@gpu
+def test_short_sides_alone_on_the_callers_stream():
+    """Matrices of every cluster size and nothing else: their launches overlap on the caller's stream."""
+    mats, d, x = flat_case([(64, 147), (64, 900), (1100, 30), (20, 4000), (100, 128), (200, 90), (120, 700), (1, 5000)],
+                           3, torch.float32, 17)
+    m = torch.zeros(d, device="cuda")
+    out = torch.full((d,), -9.0, device="cuda", dtype=torch.bfloat16)
+    h = B.deco_orth_init(d, mats, momentum=0.9)
+    try:
+        for _ in range(3):
+            B.deco_orth_run(h, x, out, momentum=m)
+        for at, r, c in mats:
+            assert rel(out[at:at + r * c].view(r, c), exact(m[at:at + r * c].view(r, c))) < tol(r * c)
+        st = B.deco_orth_get_stats(h)
+        assert st["device_status"] == 0 and st["groups"] == 0
+    finally:
+        B.deco_orth_destroy(h)
