@@ -454,7 +454,8 @@ deco_status deco_topk_compress_static(const float *a, uint64_t d, uint64_t k,
  * logprob = -inf (0 where t < 0), entropy = 0, alternatives 0, 1, ... with -inf.  A row that holds
  * a NaN or +inf gives NaN for every floating output (logprob stays 0 where t < 0).
  *   logits   DEVICE, [rows] x [vocab] of `dtype` (deco_dtype), consecutive within a row, rows
- *            row_stride entries apart (>= vocab); any alignment of whole entries
+ *            row_stride entries apart (>= vocab); any alignment of whole entries (so for every pointer
+ *            here and below, else DECO_ERR_INVALID_ARG)
  *   targets  DEVICE, [rows] int64; may be NULL if logprob is NULL
  *   logprob, entropy, lse   DEVICE, [rows] fp32 each; any of them may be NULL
  *   top      at most DECO_LOGPROBS_MAX_TOP (else DECO_ERR_CAPACITY) and at most vocab;

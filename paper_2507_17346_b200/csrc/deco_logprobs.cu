@@ -28,6 +28,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <initializer_list>
+
 #include "deco.h"
 
 namespace cg = cooperative_groups;
@@ -940,6 +942,14 @@ bool bad_shape(const void *logits, int32_t dtype, uint64_t rows, uint32_t vocab,
            (reinterpret_cast<uintptr_t>(logits) & (unit - 1)) != 0;
 }
 
+// an address that is no multiple of its entries' size would fault on the device (NULL is fine)
+bool misaligned(std::initializer_list<const void *> words, const int64_t *targets)
+{
+    for (const void *p : words)
+        if (reinterpret_cast<uintptr_t>(p) & 3u) return true;
+    return (reinterpret_cast<uintptr_t>(targets) & 7u) != 0;
+}
+
 }  // namespace
 
 extern "C" deco_status deco_token_logprobs(const void *logits, int32_t dtype, uint64_t rows, uint32_t vocab,
@@ -953,6 +963,7 @@ extern "C" deco_status deco_token_logprobs(const void *logits, int32_t dtype, ui
     if (bad_shape(logits, dtype, rows, vocab, row_stride, scale)) return DECO_ERR_INVALID_ARG;
     if (top && (!top_idx || !top_logprob)) return DECO_ERR_INVALID_ARG;
     if (!logprob && !entropy && !lse && !top) return DECO_ERR_INVALID_ARG;
+    if (misaligned({logprob, entropy, lse, top_idx, top_logprob}, targets)) return DECO_ERR_INVALID_ARG;
     const int sms = sm_count();
     if (sms == 0) return DECO_ERR_CUDA;
     Args a = {};
@@ -999,6 +1010,7 @@ extern "C" deco_status deco_token_logprobs_grad(const void *logits, int32_t dtyp
         return DECO_ERR_INVALID_ARG;
     if (!lse || (g_logprob && !targets) || (g_entropy && !entropy) || (top && (!top_idx || !g_top)))
         return DECO_ERR_INVALID_ARG;
+    if (misaligned({lse, entropy, g_logprob, g_entropy, top_idx, g_top}, targets)) return DECO_ERR_INVALID_ARG;
     if (grad == logits && grad_row_stride != row_stride) return DECO_ERR_INVALID_ARG;
     const int sms = sm_count();
     if (sms == 0) return DECO_ERR_CUDA;

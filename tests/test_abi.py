@@ -121,3 +121,29 @@ def test_argument_errors_need_no_device(B):
     assert lib.deco_ef_compress(None, None, None) == B.DECO_ERR_INVALID_ARG
     assert lib.deco_get_k(None, None) == B.DECO_ERR_INVALID_ARG
     lib.deco_destroy(None)
+
+
+def test_token_logprobs_refuse_addresses_between_entries(B):
+    """Every pointer that is no multiple of its entries' size is refused before any device call."""
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("made-up addresses: only where no kernel could be launched")
+    lib, P = B.load(), 1 << 20
+    good = dict(targets=P, logprob=P, entropy=P, lse=P, top_idx=P, top_logprob=P)
+    for name in good:
+        for off in (1, 2, 4):
+            if off == 4 and name != "targets":
+                continue
+            a = dict(good, **{name: P + off})
+            assert lib.deco_token_logprobs(P, B.DECO_F32, 2, 64, 64, a["targets"], 1.0, a["logprob"], a["entropy"],
+                                           a["lse"], 2, a["top_idx"], a["top_logprob"],
+                                           None) == B.DECO_ERR_INVALID_ARG, (name, off)
+    good = dict(targets=P, lse=P, entropy=P, g_logprob=P, g_entropy=P, top_idx=P, g_top=P, grad=P)
+    for name in good:
+        for off in (1, 2, 4):
+            if off == 4 and name != "targets":
+                continue
+            a = dict(good, **{name: P + off})
+            assert lib.deco_token_logprobs_grad(P, B.DECO_F32, 2, 64, 64, a["targets"], 1.0, a["lse"], a["entropy"],
+                                                a["g_logprob"], a["g_entropy"], 2, a["top_idx"], a["g_top"], a["grad"],
+                                                64, None) == B.DECO_ERR_INVALID_ARG, (name, off)
