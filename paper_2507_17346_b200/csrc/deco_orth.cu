@@ -1908,21 +1908,12 @@ bool allow_smem()
                                 static_cast<int>(GEMM_SMEM)) == cudaSuccess;
 }
 
-// The whole pass over what `src` describes; params: the server update's target instead of out.
+// Everything behind the taking in: short sides on stream ns, the rest on stream s.
 template <typename T>
-cudaError_t run_pass(deco_orth *h, const Source<T> &src, __nv_bfloat16 *out, float *params, float lr, float decay,
-                     cudaStream_t s)
+cudaError_t run_matrices(deco_orth *h, const Source<T> &src, __nv_bfloat16 *out, float *params, float lr, float decay,
+                         cudaStream_t s, cudaStream_t ns)
 {
-    const uint32_t taken = h->n_pieces + (src.mom && src.in ? h->n_rest : 0);
-    if (taken) {
-        ingest_kernel<T><<<taken, INGEST_THREADS, 0, s>>>(h->pieces, src, h->partial);
-        h->launches += 1;
-    }
-    if (h->n_row_pieces) {
-        ingest_rows_kernel<T><<<h->n_row_pieces, INGEST_THREADS, 0, s>>>(h->row_pieces, h->mats, src, h->partial);
-        h->launches += 1;
-    }
-    cudaError_t err = cudaGetLastError();
+    cudaError_t err = cudaSuccess;
     NarrowArgs na = {};
     na.mats = h->mats;
     std::copy(h->coef.begin(), h->coef.end(), na.coef);
@@ -1933,11 +1924,6 @@ cudaError_t run_pass(deco_orth *h, const Source<T> &src, __nv_bfloat16 *out, flo
     na.lr = lr;
     na.decay = decay;
     na.status = h->status;
-    const cudaStream_t ns = h->side ? h->side : s;
-    if (h->side && err == cudaSuccess) {
-        err = cudaEventRecord(h->fork, s);
-        if (err == cudaSuccess) err = cudaStreamWaitEvent(h->side, h->fork, 0);
-    }
     for (const Span &q : h->narrow) {
         if (err != cudaSuccess) return err;
         na.list = h->narrow_list + q.first;
@@ -1947,7 +1933,6 @@ cudaError_t run_pass(deco_orth *h, const Source<T> &src, __nv_bfloat16 *out, flo
               : q.cg == 2 ? launch_narrow<T, 2>(h, na, src, q.count, first, ns)
                           : launch_narrow<T, 1>(h, na, src, q.count, first, ns);
     }
-    if (h->side && err == cudaSuccess) err = cudaEventRecord(h->join, h->side);
     for (const Group &G : h->groups) {
         if (err != cudaSuccess) return err;
         err = launch_after(h, convert_kernel<T>, G.n_convert, INGEST_THREADS, 0, 1, s,
@@ -1979,8 +1964,34 @@ cudaError_t run_pass(deco_orth *h, const Source<T> &src, __nv_bfloat16 *out, flo
                            : launch_gemm<APPLY, OUT_BF16>(h, g, G.phase[APPLY], s);
         }
     }
-    if (h->side && err == cudaSuccess) err = cudaStreamWaitEvent(s, h->join, 0);
     return err;
+}
+
+// The whole pass over what `src` describes; params: the server update's target instead of out.
+template <typename T>
+cudaError_t run_pass(deco_orth *h, const Source<T> &src, __nv_bfloat16 *out, float *params, float lr, float decay,
+                     cudaStream_t s)
+{
+    const uint32_t taken = h->n_pieces + (src.mom && src.in ? h->n_rest : 0);
+    if (taken) {
+        ingest_kernel<T><<<taken, INGEST_THREADS, 0, s>>>(h->pieces, src, h->partial);
+        h->launches += 1;
+    }
+    if (h->n_row_pieces) {
+        ingest_rows_kernel<T><<<h->n_row_pieces, INGEST_THREADS, 0, s>>>(h->row_pieces, h->mats, src, h->partial);
+        h->launches += 1;
+    }
+    cudaError_t err = cudaGetLastError();
+    if (!h->side || err != cudaSuccess) return err != cudaSuccess ? err : run_matrices(h, src, out, params, lr, decay, s, s);
+    // The handle's own stream starts where the caller's has got to, and the caller's waits for it at the end, also
+    // when a launch in between has failed: what did start writes the caller's buffers.
+    err = cudaEventRecord(h->fork, s);
+    if (err == cudaSuccess) err = cudaStreamWaitEvent(h->side, h->fork, 0);
+    if (err != cudaSuccess) return err;
+    err = run_matrices(h, src, out, params, lr, decay, s, h->side);
+    cudaError_t joined = cudaEventRecord(h->join, h->side);
+    if (joined == cudaSuccess) joined = cudaStreamWaitEvent(s, h->join, 0);
+    return err != cudaSuccess ? err : joined;
 }
 
 }  // namespace
