@@ -921,7 +921,9 @@ cudaError_t launch_forward(const Args &a, uint64_t rows, uint32_t parts, cudaStr
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, logprobs_kernel<T, TOP, true>, a);
+    const cudaError_t err = cudaLaunchKernelEx(&cfg, logprobs_kernel<T, TOP, true>, a);
+    if (err != cudaSuccess) cudaGetLastError();                  // (pending, it would be taken for the next call's)
+    return err;
 }
 
 template <typename T>

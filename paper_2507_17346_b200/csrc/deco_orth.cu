@@ -1834,6 +1834,15 @@ deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, ui
     return cudaDeviceSynchronize() == cudaSuccess ? DECO_OK : DECO_ERR_CUDA;
 }
 
+// What a launch returned.  An error is this pass's alone: left pending in the runtime, it would be taken for the
+// next pass's, which would stop behind its update of the momentum.
+cudaError_t launched(deco_orth *h, cudaError_t err)
+{
+    if (err == cudaSuccess) h->launches += 1;
+    else cudaGetLastError();
+    return err;
+}
+
 // Launched so that its start may overlap the end of the launch before it (the kernels wait for its results).
 template <typename... A>
 cudaError_t launch_after(deco_orth *h, void (*kernel)(A...), uint32_t grid, uint32_t threads, size_t smem, uint32_t cluster,
@@ -1852,8 +1861,7 @@ cudaError_t launch_after(deco_orth *h, void (*kernel)(A...), uint32_t grid, uint
     at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = cluster > 1 ? 2 : 1;
-    h->launches += 1;
-    return cudaLaunchKernelEx(&cfg, kernel, args...);
+    return launched(h, cudaLaunchKernelEx(&cfg, kernel, args...));
 }
 
 template <Phase P, Target T>
@@ -1883,8 +1891,7 @@ cudaError_t launch_narrow(deco_orth *h, const NarrowArgs &a, const Source<T> &sr
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = first ? 1 : 2;
-    h->launches += 1;
-    return cudaLaunchKernelEx(&cfg, narrow_kernel<T, C>, a, src);
+    return launched(h, cudaLaunchKernelEx(&cfg, narrow_kernel<T, C>, a, src));
 }
 
 template <typename T>

@@ -51,7 +51,6 @@ void fake_reset(int64_t fail_launch)
     entries.clear();
     launches = 0;
     fail_at = fail_launch;
-    last_error = cudaSuccess;
 }
 uint64_t fake_log(Entry *out, uint64_t room)
 {

@@ -1,4 +1,4 @@
-"""deco_orth_run when a launch fails, against a CUDA runtime that only keeps a log (fake_cudart.cpp; no device, no
+"""deco_orth_run and deco_token_logprobs when a launch fails, against a CUDA runtime that only keeps a log (fake_cudart.cpp; no device, no
 kernel runs): whatever fails, the caller's stream waits for what was enqueued on the handle's own stream."""
 import ctypes
 import os
@@ -20,16 +20,17 @@ class Entry(ctypes.Structure):
 
 @pytest.fixture(scope="module")
 def lib(tmp_path_factory):
-    """deco_orth.cu (its device code unassembled) with the runtime of this test."""
+    """The two files (their device code unassembled) with the runtime of this test."""
     so = str(tmp_path_factory.mktemp("fake") / "liborth_fake.so")
     cmd = [os.environ.get("NVCC", "nvcc"), "-gencode", "arch=compute_100a,code=compute_100a", "-std=c++17", "-O1",
            "-shared", "-cudart", "none", "-Xcompiler", "-fPIC", "-Xlinker", "-Bsymbolic", "-I",
            os.path.join(build.ROOT, "include"), "-I", build.CSRC, "-o", so, os.path.join(build.CSRC, "deco_orth.cu"),
+           os.path.join(build.CSRC, "deco_logprobs.cu"),
            os.path.join(os.path.dirname(os.path.abspath(__file__)), "fake_cudart.cpp")]
     res = subprocess.run(cmd, capture_output=True, text=True)
     assert res.returncode == 0, res.stdout + res.stderr
     lib = ctypes.CDLL(so)
-    for name in ("deco_orth_init", "deco_orth_run", "deco_orth_destroy"):
+    for name in ("deco_orth_init", "deco_orth_run", "deco_orth_destroy", "deco_token_logprobs"):
         fn = getattr(lib, name)
         fn.restype, fn.argtypes = B.SIGNATURES[name]
     lib.fake_reset.argtypes = [ctypes.c_int64]
@@ -77,5 +78,19 @@ def test_a_failed_launch_leaves_nothing_unordered(lib, shapes, workspace):
             status, log = run(lib, h, n)
             assert status == B.DECO_ERR_CUDA and sum(e.op == LAUNCH_FAILED for e in log) == 1
             assert joined(log), "launch %d of %d" % (n, count)
+            status, log = run(lib, h, 0)                           # its error is not the next pass's
+            assert status == B.DECO_OK and sum(e.op == LAUNCH for e in log) == count
     finally:
         lib.deco_orth_destroy(h)
+
+
+@pytest.mark.parametrize("rows,vocab", [(1, 32000), (2000, 1000)])   # on eight CTAs, and on one
+def test_a_failed_call_of_token_logprobs_leaves_no_error_behind(lib, rows, vocab):
+    def call(fail_at):
+        lib.fake_reset(fail_at)
+        return lib.deco_token_logprobs(0x10000, B.DECO_F32, rows, vocab, vocab, 0x20000, 1.0, 0x30000, None, None, 0,
+                                       None, None, CALLER)
+    assert call(0) == B.DECO_OK
+    assert call(1) == B.DECO_ERR_CUDA
+    lib.cudaGetLastError.restype = ctypes.c_int
+    assert lib.cudaGetLastError() == 0 and call(0) == B.DECO_OK
