@@ -513,16 +513,24 @@ def _dtype_name(x):
     return name
 
 
-def _tensor(x, where, name, dtypes, shape=None):
-    """Address of a contiguous CUDA tensor (None stays None).  The library reads whole buffers
-    behind the addresses it is given: a broadcast or strided view would make it read elsewhere."""
+def _wrong_device(x, where, name, device):
+    return ValueError("%s: %s is on cuda:%d, the call works on cuda:%d"
+                      % (where, name, x.get_device(), device))
+
+
+def _tensor(x, where, name, device, dtypes, shape=None):
+    """Address of a contiguous CUDA tensor on `device` (None stays None).  The library reads whole
+    buffers behind the addresses it is given: a broadcast or strided view would make it read
+    elsewhere, another device's memory may not be readable at all."""
     if x is None:
         return None
     if x.is_cuda and _dtype_name(x) in dtypes and (shape is None or x.shape == shape) and \
-            x.is_contiguous():
+            x.get_device() == device and x.is_contiguous():
         return x.data_ptr()
     if not x.is_cuda:
         raise ValueError("%s: %s must be a CUDA tensor" % (where, name))
+    if x.get_device() != device:
+        raise _wrong_device(x, where, name, device)
     if _dtype_name(x) not in dtypes:
         raise ValueError("%s: %s must be %s, is %s" % (where, name, " or ".join(dtypes), x.dtype))
     if shape is not None and x.shape != shape:
@@ -534,11 +542,38 @@ def _tensor(x, where, name, dtypes, shape=None):
 _ROW_KINDS = {"float32": DECO_F32, "bfloat16": DECO_BF16}
 
 
-def _rows_of(x, where, name, like=None):
-    """(address, dtype code, rows, columns, row stride) of a 2-D CUDA tensor whose rows are
-    consecutive in memory; the rows themselves may be any distance apart."""
+_queries = None                   # torch's current device and current stream of a device, once looked up
+
+
+def _look_up():
+    global _queries
+    import torch
+    torch.cuda.current_device()                                         # (initialises)
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    _queries = (getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device),
+                raw or (lambda device: torch.cuda.current_stream(device).cuda_stream))
+    return _queries
+
+
+def _current_device():
+    return (_queries or _look_up())[0]()
+
+
+def _stream_on(stream, device):
+    """_stream for a call that works on `device`, whichever is current."""
+    return (_queries or _look_up())[1](device) if stream is None else _stream(stream)
+
+
+def _rows_of(x, where, name, device=None, like=None):
+    """(address, dtype code, rows, columns, row stride, device) of a 2-D CUDA tensor on `device`
+    (None: the current one) whose rows are consecutive in memory; the rows themselves may be any
+    distance apart."""
     if not x.is_cuda or x.dim() != 2:
         raise ValueError("%s: %s must be a two-dimensional CUDA tensor" % (where, name))
+    if device is None:
+        device = _current_device()
+    if x.get_device() != device:
+        raise _wrong_device(x, where, name, device)
     kind = _ROW_KINDS.get(_dtype_name(x))
     if kind is None:
         raise ValueError("%s: %s must be float32 or bfloat16, is %s" % (where, name, x.dtype))
@@ -551,7 +586,7 @@ def _rows_of(x, where, name, like=None):
     if cols > 1 and step != 1 or stride < cols:
         raise ValueError("%s: the rows of %s must be consecutive in memory and must not overlap"
                          % (where, name))
-    return x.data_ptr(), kind, rows, cols, stride
+    return x.data_ptr(), kind, rows, cols, stride, device
 
 
 def deco_token_logprobs(logits, targets, logprob, entropy=None, lse=None, scale=1.0, top_idx=None,
@@ -561,15 +596,15 @@ def deco_token_logprobs(logits, targets, logprob, entropy=None, lse=None, scale=
     exponentials and the top alternatives (`top_idx` [rows, top] int32 and `top_logprob` [rows, top]
     f32).  `targets` and `logprob` may both be None."""
     w = "deco_token_logprobs"
-    p, kind, rows, vocab, stride = _rows_of(logits, w, "logits")
+    p, kind, rows, vocab, stride, dev = _rows_of(logits, w, "logits")
     top = 0 if top_idx is None else top_idx.shape[-1]
     _check(load().deco_token_logprobs(
-        p, kind, rows, vocab, stride, _tensor(targets, w, "targets", ("int64",), (rows,)), scale,
-        _tensor(logprob, w, "logprob", ("float32",), (rows,)),
-        _tensor(entropy, w, "entropy", ("float32",), (rows,)),
-        _tensor(lse, w, "lse", ("float32",), (rows,)), top,
-        _tensor(top_idx, w, "top_idx", ("int32",), (rows, top)),
-        _tensor(top_logprob, w, "top_logprob", ("float32",), (rows, top)), _stream(stream)), w)
+        p, kind, rows, vocab, stride, _tensor(targets, w, "targets", dev, ("int64",), (rows,)), scale,
+        _tensor(logprob, w, "logprob", dev, ("float32",), (rows,)),
+        _tensor(entropy, w, "entropy", dev, ("float32",), (rows,)),
+        _tensor(lse, w, "lse", dev, ("float32",), (rows,)), top,
+        _tensor(top_idx, w, "top_idx", dev, ("int32",), (rows, top)),
+        _tensor(top_logprob, w, "top_logprob", dev, ("float32",), (rows, top)), _stream_on(stream, dev)), w)
 
 
 def deco_token_logprobs_grad(logits, targets, lse, grad, g_logprob=None, entropy=None,
@@ -577,22 +612,22 @@ def deco_token_logprobs_grad(logits, targets, lse, grad, g_logprob=None, entropy
     """Gradient with respect to the logits of the sums g_logprob . logprob + g_entropy . entropy +
     g_top . top_logprob, written to `grad` (the logits' shape and type; may be `logits` itself)."""
     w = "deco_token_logprobs_grad"
-    p, kind, rows, vocab, stride = _rows_of(logits, w, "logits")
-    gp, _, _, _, gstride = _rows_of(grad, w, "grad", logits)
+    p, kind, rows, vocab, stride, dev = _rows_of(logits, w, "logits")
+    gp, _, _, _, gstride, _ = _rows_of(grad, w, "grad", dev, logits)
     top = 0 if g_top is None else g_top.shape[-1]
     _check(load().deco_token_logprobs_grad(
-        p, kind, rows, vocab, stride, _tensor(targets, w, "targets", ("int64",), (rows,)), scale,
-        _tensor(lse, w, "lse", ("float32",), (rows,)),
-        _tensor(entropy, w, "entropy", ("float32",), (rows,)),
-        _tensor(g_logprob, w, "g_logprob", ("float32",), (rows,)),
-        _tensor(g_entropy, w, "g_entropy", ("float32",), (rows,)), top,
-        _tensor(top_idx, w, "top_idx", ("int32",), (rows, top)) if top else None,
-        _tensor(g_top, w, "g_top", ("float32",), (rows, top)), gp, gstride, _stream(stream)), w)
+        p, kind, rows, vocab, stride, _tensor(targets, w, "targets", dev, ("int64",), (rows,)), scale,
+        _tensor(lse, w, "lse", dev, ("float32",), (rows,)),
+        _tensor(entropy, w, "entropy", dev, ("float32",), (rows,)),
+        _tensor(g_logprob, w, "g_logprob", dev, ("float32",), (rows,)),
+        _tensor(g_entropy, w, "g_entropy", dev, ("float32",), (rows,)), top,
+        _tensor(top_idx, w, "top_idx", dev, ("int32",), (rows, top)) if top else None,
+        _tensor(g_top, w, "g_top", dev, ("float32",), (rows, top)), gp, gstride, _stream_on(stream, dev)), w)
 
 
 # ------------------------------------------------------------- orthogonalised updates
 
-_orth_length = {}                 # handle -> length of its flat vectors
+_orth_handles = {}                # handle -> length of its flat vectors, device
 
 
 def deco_orth_init(d, matrices, steps=0, coef=None, eps=0.0, momentum=0.0, nesterov=False,
@@ -616,12 +651,12 @@ def deco_orth_init(d, matrices, steps=0, coef=None, eps=0.0, momentum=0.0, neste
     h = _vp()
     _check(load().deco_orth_init(ctypes.byref(h), d, ms, len(matrices), ctypes.byref(opt)),
            "deco_orth_init")
-    _orth_length[h.value] = d
+    _orth_handles[h.value] = d, device
     return h.value
 
 
 def deco_orth_destroy(h):
-    _orth_length.pop(h, None)
+    _orth_handles.pop(h, None)
     load().deco_orth_destroy(h)
 
 
@@ -629,25 +664,26 @@ def deco_orth_run(h, x, out, momentum=None, stream=None):
     """Orthogonalise the handle's matrices of the flat vector `x` (f32 or bf16) into `out` (bf16);
     with `momentum` (f32, updated in place) of the momentum buffer."""
     w = "deco_orth_run"
-    shape = (_orth_length[h],)
-    xp = _tensor(x, w, "x", ("float32", "bfloat16"), shape)
+    d, dev = _orth_handles[h]
+    xp = _tensor(x, w, "x", dev, ("float32", "bfloat16"), (d,))
     _check(load().deco_orth_run(
         h, xp, DECO_F32 if "float32" in str(x.dtype) else DECO_BF16,
-        _tensor(momentum, w, "momentum", ("float32",), shape),
-        _tensor(out, w, "out", ("bfloat16",), shape), _stream(stream)), w)
+        _tensor(momentum, w, "momentum", dev, ("float32",), (d,)),
+        _tensor(out, w, "out", dev, ("bfloat16",), (d,)), _stream_on(stream, dev)), w)
 
 
 def deco_apply_update_orth(ctx, h, momentum, weight_decay=0.0, stream=None):
     """deco_apply_update with orthogonalised directions; `momentum`: f32 CUDA tensor of length d."""
     w = "deco_apply_update_orth"
-    _check(load().deco_apply_update_orth(ctx, h, _tensor(momentum, w, "momentum", ("float32",),
-                                                         (_orth_length[h],)),
-                                         weight_decay, _stream(stream)), w)
+    d, dev = _orth_handles[h]
+    _check(load().deco_apply_update_orth(ctx, h, _tensor(momentum, w, "momentum", dev, ("float32",), (d,)),
+                                         weight_decay, _stream_on(stream, dev)), w)
 
 
 def deco_orth_get_stats(h, stream=None):
     st = deco_orth_stats()
-    _check(load().deco_orth_get_stats(h, _stream(stream), ctypes.byref(st)), "deco_orth_get_stats")
+    s = _stream_on(stream, _orth_handles[h][1]) if h in _orth_handles else _stream(stream)
+    _check(load().deco_orth_get_stats(h, s, ctypes.byref(st)), "deco_orth_get_stats")
     return {f: getattr(st, f) for f, _ in deco_orth_stats._fields_}
 
 
