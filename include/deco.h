@@ -542,7 +542,10 @@ typedef struct {
     uint64_t workspace_bytes; /* the library works through the matrices in groups whose working
                                  copies fit in this much device memory (a larger single matrix gets what it
                                  needs); 0 -> 2 GiB */
-    uint32_t reserved[4];     /* must be zero */
+    uint32_t tile_ctas;       /* CTAs that work on an output tile together: 1, or 2 for pairs; 0 -> by phase,
+                                 whichever is expected to be done first.  The results are those of
+                                 the same formula with the same operands' precision either way */
+    uint32_t reserved[3];     /* must be zero */
 } deco_orth_options;
 
 typedef struct {

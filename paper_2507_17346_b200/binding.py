@@ -84,7 +84,8 @@ class deco_orth_options(ctypes.Structure):
                 ("scale", ctypes.c_int32),
                 ("device", ctypes.c_int32),
                 ("workspace_bytes", ctypes.c_uint64),
-                ("reserved", ctypes.c_uint32 * 4)]
+                ("tile_ctas", ctypes.c_uint32),
+                ("reserved", ctypes.c_uint32 * 3)]
 
 
 class deco_orth_stats(ctypes.Structure):
@@ -631,7 +632,7 @@ _orth_handles = {}                # handle -> length of its flat vectors, device
 
 
 def deco_orth_init(d, matrices, steps=0, coef=None, eps=0.0, momentum=0.0, nesterov=False,
-                   scale=DECO_ORTH_SCALE_NONE, device=0, workspace_bytes=0):
+                   scale=DECO_ORTH_SCALE_NONE, device=0, workspace_bytes=0, tile_ctas=0):
     """-> opaque handle (int) for the matrices [(offset, rows, cols[, row_stride]), ...] of flat
     vectors of length d.  `coef`: one (a, b, c) for every step, or a list of `steps` of them."""
     ms = (deco_matrix * max(1, len(matrices)))()
@@ -648,6 +649,7 @@ def deco_orth_init(d, matrices, steps=0, coef=None, eps=0.0, momentum=0.0, neste
         opt.coef = ctypes.cast(keep, _P(_f32))
     opt.steps, opt.eps, opt.momentum, opt.nesterov = steps, eps, momentum, int(bool(nesterov))
     opt.scale, opt.device, opt.workspace_bytes = scale, device, workspace_bytes
+    opt.tile_ctas = tile_ctas
     h = _vp()
     _check(load().deco_orth_init(ctypes.byref(h), d, ms, len(matrices), ctypes.byref(opt)),
            "deco_orth_init")

@@ -1602,7 +1602,7 @@ uint32_t passes(const Mat &M, int phase) { return phase == APPLY ? 1 + M.precisi
 constexpr uint32_t MAX_PARTS = 8, MIN_PART = 512;
 double tile_cost(uint32_t cg, uint32_t k) { return cg == 1 ? 9.0 * k + 3000 : 10.0 * k + 4500; }
 
-deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, uint64_t cap)
+deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, uint64_t cap, uint32_t tile_ctas)
 {
     const EncodeFn enc = encode_function();
     if (!enc) return DECO_ERR_CUDA;
@@ -1762,6 +1762,7 @@ deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, ui
             // one CTA per tile, the sums of GRAM in up to MAX_PARTS parts, or a pair of CTAs per tile
             for (uint32_t way = 1; way <= (phase == GRAM ? 2 * MAX_PARTS : 2u); way *= 2) {
                 const uint32_t cg = way == 2 ? 2 : 1, most_parts = way <= 2 ? 1 : way / 2, side = 128 * cg;
+                if (tile_ctas != 0 && tile_ctas != cg) continue;
                 auto blocks = [&](uint32_t v) { return (v + side - 1) / side; };
                 // every tile, the longest first, to the lane that is free first
                 std::vector<std::vector<Tile>> lanes(h->sms / cg);
@@ -1790,7 +1791,7 @@ deco_status plan(deco_orth *h, const std::vector<deco_matrix> &ms, int scale, ui
                             slots += parts > 1 ? parts : 0;
                         }
                 }
-                if (way == 1 || cost < best) {
+                if (chosen.empty() || cost < best) {
                     best = cost;
                     best_slots = slots;
                     chosen.swap(lanes);
@@ -2013,7 +2014,7 @@ try {
         if (r) return DECO_ERR_INVALID_ARG;
     const uint32_t steps = o.steps ? o.steps : 5;
     if (steps > MAX_STEPS || !(o.eps >= 0.f) || o.eps > 1e30f || !(o.momentum >= 0.f && o.momentum < 1.f) ||
-        o.scale < DECO_ORTH_SCALE_NONE || o.scale > DECO_ORTH_SCALE_RMS)
+        o.scale < DECO_ORTH_SCALE_NONE || o.scale > DECO_ORTH_SCALE_RMS || o.tile_ctas > 2)
         return DECO_ERR_INVALID_ARG;
     std::vector<float> coef(3 * steps);
     const float standard[3] = {3.4445f, -4.7750f, 2.0315f};
@@ -2042,7 +2043,7 @@ try {
         h->mu = o.momentum;
         h->nesterov = o.nesterov != 0;
         h->sms = static_cast<uint32_t>(sms);
-        st = plan(h, ms, o.scale, o.workspace_bytes ? o.workspace_bytes : 2ull << 30);
+        st = plan(h, ms, o.scale, o.workspace_bytes ? o.workspace_bytes : 2ull << 30, o.tile_ctas);
     } catch (...) {
     }
     if (st != DECO_OK) {

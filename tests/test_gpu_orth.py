@@ -508,3 +508,157 @@ def test_short_sides_alone_on_the_callers_stream():
         assert st["device_status"] == 0 and st["groups"] == 0
     finally:
         B.deco_orth_destroy(h)
+
+
+# ------------------------------------------------------- every way through the products on tiles
+
+# short sides up to 128 whose entries no cluster holds (hi and lo of every operand), up to 256 (of P), above
+GENERAL = [(100, 1300), (1301, 99), (128, 1040), (200, 333), (333, 201), (256, 1024), (300, 301), (301, 300), (520, 264),
+           (640, 385), (768, 768), (1025, 520)]
+
+
+def check_all(out, y, mats, scale=1.0):
+    """Every matrix of `out` against the polynomial of `y`, the other entries against -9."""
+    used = torch.zeros(len(out), dtype=torch.bool, device="cuda")
+    for q in mats:
+        pick = lambda t: torch.as_strided(t, (q[1], q[2]), (q[3] if len(q) > 3 else q[2], 1), q[0])  # noqa: B023, E731
+        assert not pick(used).any()
+        pick(used).fill_(True)
+        assert rel(pick(out), scale * exact(pick(y))) < tol(q[1] * q[2]), q
+    assert (out[~used] == -9).all()
+
+
+@gpu
+@pytest.mark.parametrize("tile_ctas", [1, 2])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("gap", [3, 8])
+def test_one_cta_and_pairs_in_every_phase(tile_ctas, dtype, gap):
+    """The three phases on tiles of one CTA and of a pair, for every precision, orientation and alignment."""
+    mats, d, x = flat_case(GENERAL, gap, dtype, 23)
+    out = torch.full((d,), -9.0, device="cuda", dtype=torch.bfloat16)
+    h = B.deco_orth_init(d, mats, tile_ctas=tile_ctas)
+    try:
+        B.deco_orth_run(h, x, out)
+        check_all(out, x, mats)
+        first = out.clone()
+        B.deco_orth_run(h, x, out)
+        assert torch.equal(out, first)
+        assert B.deco_orth_get_stats(h)["device_status"] == 0
+    finally:
+        B.deco_orth_destroy(h)
+
+
+@gpu
+@pytest.mark.parametrize("tile_ctas", [0, 1, 2])
+@pytest.mark.parametrize("nesterov", [None, False, True])
+@pytest.mark.parametrize("S,lead", [(1500, 10), (1504, 16)])
+def test_strided_matrices_above_the_short_sides(S, lead, nesterov, tile_ctas):
+    """Column ranges of one buffer of rows, wide and tall ones with rows apart, plain ones between; without
+    momentum (nesterov None) and with."""
+    at = lead + 310 * S
+    mats = [(lead, 310, 600, S), (lead + 600, 300, 500, S), (lead + 1100, 310, 381, S), (at, 700, 300, 304),
+            (at + 700 * 304, 270, 900, 901), (at + 700 * 304 + 270 * 901, 300, 200), (at + 700 * 304 + 270 * 901 + 60000, 140, 200, 208)]
+    d = mats[-1][0] + 140 * 208 + 5
+    g = torch.Generator(device="cuda")
+    g.manual_seed(4)
+    x = torch.randn(d, generator=g, device="cuda")
+    m = None if nesterov is None else torch.randn(d, generator=g, device="cuda")
+    out = torch.full((d,), -9.0, device="cuda", dtype=torch.bfloat16)
+    h = B.deco_orth_init(d, mats, momentum=0.5, nesterov=bool(nesterov), tile_ctas=tile_ctas)
+    try:
+        y = x.double() if m is None else 0.5 * m.double() + x.double()
+        B.deco_orth_run(h, x, out, momentum=m)
+        if m is not None:
+            assert ((m.double() - y).abs() <= (y.abs() + x.double().abs()) * 2.0 ** -23).all()
+        check_all(out, 0.5 * y + x.double() if nesterov else y, mats)
+        assert B.deco_orth_get_stats(h)["device_status"] == 0
+    finally:
+        B.deco_orth_destroy(h)
+
+
+@gpu
+@pytest.mark.parametrize("rows,cols", [(70, 90), (100, 1300), (200, 300), (300, 400), (400, 300)])
+def test_extreme_norms_zero_nan_and_infinity(rows, cols):
+    """In one launch and through the general way, whose entries are divided by the norm in fp32 or in double."""
+    x = make(rows, cols, "normal", 1)
+    for f in (1e30, 1e-30, 3e37):
+        assert rel(run_one(x * f, eps=1e-38), exact(x * f, eps=1e-38)) < tol(x.numel())
+    assert rel(run_one(x * 1e-9), exact(x * 1e-9)) < tol(x.numel())  # eps takes part
+    assert (run_one(torch.zeros_like(x)) == 0).all()
+    for bad in (math.nan, math.inf, -math.inf):
+        for where in ((3, 4), (rows - 1, cols - 1)):
+            y = x.clone()
+            y[where] = bad
+            assert torch.isnan(run_one(y)).all()
+
+
+@gpu
+@pytest.mark.parametrize("tile_ctas", [0, 1, 2])
+@pytest.mark.parametrize("delta", [0.01, 0.5])
+@pytest.mark.parametrize("gap", [8, 13])
+def test_server_update_of_larger_matrices(gap, delta, tile_ctas):
+    """The parameters' rows in fp32, 16 bytes at a time and singly; products with every precision, on one CTA and
+    on pairs; sparse (0.01) and dense (0.5) aggregates; short sides beside them.  Tolerance as in test_server_update."""
+    shapes, n, lr, wd, mu, steps = [(64, 148), (300, 400), (520, 264), (200, 512), (100, 1300), (1040, 300)], 2, 0.02, 0.1, 0.9, 2
+    mats, d, _ = flat_case(shapes, gap, torch.float32, 0)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(6)
+    params = (0.05 * torch.randn(d, generator=g, device="cuda")).contiguous()
+    want = params.double().clone()
+    ctx = B.deco_init(d, n, delta, 0, lr, lr_at_server=True, params=params)
+    h = B.deco_orth_init(d, mats, momentum=mu, scale=B.DECO_ORTH_SCALE_SPECTRAL, tile_ctas=tile_ctas)
+    m = torch.zeros(d, device="cuda")
+    wm = torch.zeros(d, device="cuda", dtype=torch.float64)
+    mu32, lr32, w32 = (float(torch.tensor(v)) for v in (mu, lr, 1.0 / n))
+    decay = float(torch.tensor(1.0) - torch.tensor(lr) * torch.tensor(wd))
+    used = torch.zeros(d, dtype=torch.bool, device="cuda")
+    for at, r, c in mats:
+        used[at:at + r * c] = True
+    try:
+        for t in range(steps):
+            B.deco_ef_compress(ctx, torch.randn(n, d, generator=g, device="cuda"))
+            B.deco_aggregate_stale(ctx)
+            k, buf = B.deco_get_k(ctx), B.deco_get_buffers(ctx)
+            pairs = B.view_i32(buf["msg"], (n, buf["k_cap"], 2))[:, :k]
+            s = torch.zeros(d, device="cuda", dtype=torch.float64)
+            for i in range(n):
+                s.index_add_(0, pairs[i, :, 0].long(), pairs[i, :, 1].contiguous().view(torch.float32).double())
+            B.deco_apply_update_orth(ctx, h, m, wd)
+            wm = mu32 * wm + w32 * s
+            step = torch.zeros(d, device="cuda", dtype=torch.float64)
+            for at, r, c in mats:
+                y = math.sqrt(max(1.0, r / c)) * exact(wm[at:at + r * c].view(r, c))
+                step[at:at + r * c] = y.reshape(-1)
+            want = want * decay - lr32 * torch.where(used, step, wm)
+            err = params.double() - want
+            for at, r, c in mats:
+                e, y = err[at:at + r * c], step[at:at + r * c]
+                assert e.norm() <= 2.9e-3 * lr32 * y.norm() * (t + 1) + 1e-6 * want.norm(), (r, c)
+            assert err[~used].norm() <= 1e-6 * want.norm()
+        assert B.deco_orth_get_stats(h)["device_status"] == 0
+    finally:
+        B.deco_orth_destroy(h)
+        B.deco_destroy(ctx)
+
+
+@gpu
+@pytest.mark.parametrize("shapes", [[(2304, 768)] * 12 + [(768, 768)] * 12, [(2303, 769)] * 6 + [(769, 771)] * 7,
+                                    [(2048, 2048), (256, 2048), (5632, 2048), (2048, 5632)],
+                                    [(96, 2048)] * 60 + [(2048, 200)] * 40])
+def test_many_large_matrices(shapes):
+    """What a server update of a language model has: enough tiles for pairs in every phase by the library's own choice."""
+    mats, d, x = flat_case(shapes, 0, torch.bfloat16, 29)
+    out = torch.full((d,), -9.0, device="cuda", dtype=torch.bfloat16)
+    h = B.deco_orth_init(d, mats)
+    try:
+        B.deco_orth_run(h, x, out)
+        check_all(out, x, mats)
+        assert B.deco_orth_get_stats(h)["device_status"] == 0
+    finally:
+        B.deco_orth_destroy(h)
+
+
+def test_tile_ctas_is_checked_on_the_host():
+    with pytest.raises(B.DecoError) as e:
+        B.deco_orth_init(100, [(0, 10, 10)], tile_ctas=3)
+    assert e.value.status == B.DECO_ERR_INVALID_ARG
