@@ -465,6 +465,130 @@ def test_gradient_of_rows_whose_lse_has_lost_its_last_digits(rows, vocab, dtype,
                 assert torch.isfinite(dx[6:]).all() and (dx[6:] != 0).any(1).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scale", [1e-5, 300.0, 1e4, 1e30])
+def test_gradient_at_unusual_scales(scale, dtype):
+    """Scales outside [2^-8, 2^8].  Below |lse| = 2^20 ln 2 p follows the lse handed in: d = z - lse rounded once,
+    exp of it: |d| eps and 8 eps.  Beyond it, (x - max) scale is rounded once, as above."""
+    rows, v, top = 4, 5003, 3
+    scale = float(np.float32(scale))
+    x = rows_of(rows, v, dtype, 41)
+    t = targets_for(rows, v, 4)
+    out, ref = call(x, t, top, scale), reference(x, t, top, scale)
+    gl, gh, gt = grads_for(rows, top, 6)
+    if ref["lse"].abs().max() < 2.0 ** 20 * math.log(2.0) - 1:
+        want, p = grad_from_lse(x, t, scale, out["lse"], out["entropy"], out["top_idx"], gl, gh, gt)
+        h = out["entropy"].double()[:, None]
+    else:
+        want, p, h = grad_reference(x, t, scale, ref, ref["top_idx"], gl, gh, gt), ref["p"], ref["entropy"][:, None]
+    f = (gl.abs().double() + gt.abs().double().sum(1))[:, None]
+    w = f + gh.abs().double()[:, None] * (41 + h)
+    own = torch.zeros_like(want).scatter_(1, t.clamp_min(0)[:, None], 1.0).scatter_(1, out["top_idx"].long(), 1.0)
+    tol = scale * (((50 + h) * 2 * EPS + 2 * sum_tol(v)) * p * w + 16 * EPS * own * f)
+    tol = tol + want.abs() * 2.0 ** (-8 if dtype == "bf16" else -23) + 1e-38
+    dx = torch.empty_like(x)
+    B.deco_token_logprobs_grad(x, t, out["lse"], dx, g_logprob=gl, entropy=out["entropy"], g_entropy=gh,
+                               top_idx=out["top_idx"], g_top=gt, scale=scale)
+    close(dx, want, tol)
+
+
+@pytest.mark.parametrize("offset", [0.0, 2e7])
+def test_gradient_of_repeated_and_left_out_alternatives(offset):
+    """Equal tokens among the alternatives and the target add up; indices >= vocab are left out."""
+    rows, v = 3, 6007
+    x = rows_of(rows, v, "f32", 51) * 8 + offset
+    t = torch.tensor([17, 6006, -1], device="cuda")
+    idx = torch.tensor([[17, 17, 4, 6007, 17], [0, 6006, 0, -1, 2 ** 31 - 1], [5, 5, 5, 5, 5]], dtype=torch.int32,
+                       device="cuda")
+    out, ref = call(x, t, 0), reference(x, t, 0, 1.0)
+    gl, _, gt = grads_for(rows, 5, 7)
+    inside = (idx >= 0) & (idx < v)
+    want = grad_reference(x, t, 1.0, ref, torch.where(inside, idx, torch.zeros_like(idx)), gl, None,
+                          torch.where(inside, gt, torch.zeros_like(gt)))
+    f = (gl.abs().double() + gt.abs().double().sum(1))[:, None]
+    tol = (ref["p"] * (ref["lse"].abs()[:, None] * (4 if offset == 0 else 0) + 60) * 2 * EPS + 2 * sum_tol(v) * ref["p"] + 16 * EPS) * f
+    dx = torch.empty_like(x)
+    B.deco_token_logprobs_grad(x, t, out["lse"], dx, g_logprob=gl, top_idx=idx, g_top=gt)
+    close(dx, want, tol)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gradient_of_rows_with_nan_or_infinity(dtype):
+    """lse is NaN there, and so is the gradient; a row of -inf has the gradient 0, also where its target is not one."""
+    for rows, v in ((5, 37), (400, 9001)):
+        x = rows_of(rows, v, dtype, 81)
+        x[0, 5], x[1, v - 1], x[2], x[3] = math.nan, math.inf, -math.inf, -math.inf
+        t = targets_for(rows, v, 1)
+        t[3] = v
+        out = call(x, t, 2)
+        gl, gh, gt = grads_for(rows, 2, 3)
+        for g_h in (None, gh):
+            dx = torch.empty_like(x)
+            B.deco_token_logprobs_grad(x, t, out["lse"], dx, g_logprob=gl, entropy=out["entropy"], g_entropy=g_h,
+                                       top_idx=out["top_idx"], g_top=gt)
+            assert torch.isnan(dx[:2]).all() and (dx[2:4] == 0).all() and torch.isfinite(dx[4:]).all()
+
+
+def test_rows_whose_offsets_pass_32_bits():
+    """Rows 2^31 + 2^29 entries apart, outputs and gradient (in place) against the definition."""
+    v, stride, rows = 4001, 2 ** 31 + 2 ** 29 + 3, 3
+    buf = torch.zeros(2 * stride + v + 8, dtype=torch.bfloat16, device="cuda")
+    x = torch.as_strided(buf, (rows, v), (stride, 1), 1)
+    x.copy_(rows_of(rows, v, "bf16", 61))
+    t = targets_for(rows, v, 5)
+    out, ref = call(x, t, 4), reference(x, t, 4, 1.0)
+    check(out, ref, v, 4)
+    gl, gh, gt = grads_for(rows, 4, 9)
+    want, p = grad_from_lse(x, t, 1.0, out["lse"], out["entropy"], out["top_idx"], gl, gh, gt)
+    f = gl.abs().double() + gt.abs().double().sum(1)
+    w = f[:, None] + (gh.abs().double() * (41 + out["entropy"].double()))[:, None]
+    own = torch.zeros_like(want).scatter_(1, t.clamp_min(0)[:, None], 1.0).scatter_(1, out["top_idx"].long(), 1.0)
+    B.deco_token_logprobs_grad(x, t, out["lse"], x, g_logprob=gl, entropy=out["entropy"], g_entropy=gh,
+                               top_idx=out["top_idx"], g_top=gt)
+    close(x, want, 102 * EPS * p * w + 16 * EPS * own * f[:, None] + want.abs() * 2.0 ** -8 + 1e-36)
+    assert (buf[0] == 0) and (buf[1 + v:1 + stride] == 0).all() and (buf[-7:] == 0).all()
+
+
+def test_the_longest_row():
+    """vocab = 2^31 - 1, bf16, one entry off a 16-byte boundary.  Sums of n entries in 2048 threads: 82 eps for a
+    weight and n / 2048 / 2 eps for sums of equal terms are too much to ask for; their roundings are spread, so
+    sqrt(n / 2048) of them: 1024 eps."""
+    v = 2 ** 31 - 1
+    buf = torch.zeros(v + 16, dtype=torch.bfloat16, device="cuda")
+    x = buf[1:1 + v].view(1, v)
+    step = 2 ** 28
+    g = torch.Generator(device="cuda")
+    g.manual_seed(71)
+    for lo in range(0, v, step):
+        n = min(step, v - lo)
+        x[0, lo:lo + n] = torch.randn(n, generator=g, device="cuda", dtype=torch.bfloat16)
+    spots = [0, 6, 7, 2 ** 30 + 5, 2 ** 31 - 10, v - 1]
+    for i, j in enumerate(spots):
+        x[0, j] = 9.0 - i // 2                                     # the largest, in pairs of equal ones
+    t = torch.tensor([v - 1], device="cuda")
+    out = call(x, t, 6)
+    assert out["top_idx"][0].tolist() == spots
+    m, s, q = 9.0, 0.0, 0.0
+    for lo in range(0, v, step):
+        z = x[0, lo:lo + step].double() - m
+        p = z.exp()
+        s += p.sum().item()
+        q += (p * z).sum().item()
+        del z, p
+    lse, entropy = m + math.log(s), math.log(s) - q / s
+    tol = 1200 * EPS
+    assert abs(out["lse"].item() - lse) <= tol + 4 * EPS * lse
+    assert abs(out["entropy"].item() - entropy) <= tol * (41 + entropy)
+    assert abs(out["logprob"].item() - (7.0 - lse)) <= tol + 4 * EPS * lse
+    gl = torch.ones(1, device="cuda")
+    keep = {j: x[0, j].item() for j in spots + [12345, 2 ** 31 - 3]}
+    B.deco_token_logprobs_grad(x, t, out["lse"], x, g_logprob=gl)
+    for j, z in keep.items():
+        want = (1.0 if j == v - 1 else 0.0) - math.exp(z - out["lse"].item())
+        assert abs(x[0, j].item() - want) <= abs(want) * (2.0 ** -8 + 200 * EPS) + 16 * EPS * (j == v - 1)
+    assert buf[0] == 0 and (buf[1 + v:] == 0).all()
+
+
 # ------------------------------------------------------------------------------- refusals
 
 def test_refusals():

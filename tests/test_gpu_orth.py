@@ -662,3 +662,30 @@ def test_tile_ctas_is_checked_on_the_host():
     with pytest.raises(B.DecoError) as e:
         B.deco_orth_init(100, [(0, 10, 10)], tile_ctas=3)
     assert e.value.status == B.DECO_ERR_INVALID_ARG
+
+
+@gpu
+def test_matrices_whose_offsets_pass_32_bits():
+    """One with rows 2^25 entries apart, short- and long-sided ones behind 2^32 entries: against the polynomial."""
+    S, lead = 2 ** 25 + 8, 3
+    at = lead + 150 * S
+    mats = [(lead, 150, 200, S), (at, 60, 130), (at + 60 * 130, 300, 200), (at + 60 * 130 + 300 * 200, 140, 190, 201)]
+    d = mats[-1][0] + 140 * 201 + 5
+    assert at > 2 ** 32
+    x = torch.zeros(d, dtype=torch.bfloat16, device="cuda")
+    out = torch.full((d,), -9.0, dtype=torch.bfloat16, device="cuda")
+    pick = lambda t, q: torch.as_strided(t, (q[1], q[2]), (q[3] if len(q) > 3 else q[2], 1), q[0])  # noqa: E731
+    for i, q in enumerate(mats):
+        pick(x, q).copy_(make(q[1], q[2], "normal", 80 + i, torch.bfloat16))
+    h = B.deco_orth_init(d, mats)
+    try:
+        B.deco_orth_run(h, x, out)
+        assert B.deco_orth_get_stats(h)["device_status"] == 0
+    finally:
+        B.deco_orth_destroy(h)
+    for q in mats:
+        y = pick(x, q).clone()
+        assert rel(pick(out, q), exact(y)) < tol(y.numel())
+        pick(out, q).fill_(-9.0)
+    for lo in range(0, d, 2 ** 30):
+        assert (out[lo:lo + 2 ** 30] == -9).all()
