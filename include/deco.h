@@ -558,7 +558,8 @@ typedef struct {
 typedef struct deco_orth deco_orth;          /* opaque, owned by the library */
 
 /*
- * Plans the work and allocates all device memory the handle will ever use.  The matrices lie
+ * Plans the work and allocates all device memory the handle will ever use; copies its tables and waits for
+ * the device, so it belongs before a loop (1 to 4 ms for a network's matrices).  The matrices lie
  * inside [0, d) and do not overlap; from its first entry to its last a matrix may be interleaved
  * with others only as column ranges of rows of one row_stride (else DECO_ERR_INVALID_ARG); entries of no matrix are allowed.  *out is set only on success.
  * One handle is used on one stream at a time.

@@ -526,7 +526,8 @@ __device__ __forceinline__ Operands operands(const GemmArgs &g, const Tile &tl)
 // What bounds it: an SM takes in about 51 bytes of operands a cycle, 620 to 640 cycles for the 64 k on which the
 // tensor cores work 512, so they are busy 80 % of the cycles with the epilogue left out and 61 % with it (A and
 // X P of a decoder block, k = 5632 and 2048; 33 to 38 % at k = 768, where a tile's epilogue is as long as its
-// products).  On four decoder blocks that is 1.2 to 1.36 PFLOP/s, close to what the power cap sustains.
+// products).  On four decoder blocks, launches one at a time and one triangle of A and P counted: A 1.20, P 1.06,
+// X P 1.25 PFLOP/s, together 1.20; one block: 1.09, 0.80, 1.25, together 1.11.
 template <int CG, Phase P, Target T>
 __global__ void __launch_bounds__(GEMM_THREADS, 1)
 gemm_kernel(const GemmArgs g)
@@ -936,11 +937,14 @@ gemm_kernel(const GemmArgs g)
 // Matrices with a short side of at most FULL_SIDE whose entries fit the shared memory of a cluster go
 // through all steps in one launch.  The long side is cut into tiles of 128, dealt to the cluster's CTAs;
 // a CTA keeps its part of X, hi and lo, as rows along the long side.  Per step it forms its part of
-// A (products over its tiles), the parts are added through distributed shared memory, every CTA adding
+// A (products over its tiles); in a cluster the parts are added through distributed shared memory, every CTA adding
 // up its share of the entries and handing the sums to all, in a fixed order, and then makes P and the
-// products with its own part by itself.  All products are taken in full (hi hi + hi lo + lo hi).  What
-// bounds this kernel is the chain of waits (two cluster barriers and three products per step), not
-// bytes or products.  64 x 147: 36 us a pass, of which 12000 cycles a step; the 17 launches of the general way took 111 us.
+// products with its own part by itself.  All products are taken in full (hi hi + hi lo + lo hi).  What bounds this
+// kernel is the chain of products and epilogues, each waiting for the one before it, not bytes.  64 x 147, one
+// CTA, 36 us a pass; cycles of a step: A 2640 and its epilogue 510, A^2 1050, P 1050, X P 1940, X 1450, together 8900
+// (23 us in five steps; the rest is the launch, the norm and the writing).  64 x 1000, a cluster of four: 12300, of
+// which 3500 are the exchange of A's parts with its two cluster barriers.  128 x 128: 10900.  The 17 launches of
+// the general way took 111 us for 64 x 147.
 
 constexpr int NARROW_THREADS = 512;
 constexpr uint32_t NARROW_TILE_LIMIT = 5;        // tiles of 128 per CTA at short sides up to 64
@@ -1042,8 +1046,9 @@ struct NarrowLayout {
 // the tensor memory, and CTAs of two clusters waiting for each other's would wait for good.
 constexpr uint32_t NARROW_MIN_SMEM = 120 * 1024;
 
-// Smallest power of two of CTAs, at most NARROW_MAX_CLUSTER, that leaves each at most two tiles (one, where
-// shared memory holds no more).  A second tile costs a CTA 3200 cycles a step, a cluster's exchange 4500.
+// Smallest power of two of CTAs, at most NARROW_MAX_CLUSTER, that leaves each at most two tiles (one, where shared
+// memory holds no more; with the largest cluster up to NARROW_TILE_LIMIT).  A second tile costs a CTA 2400 cycles
+// a step (64 x 256 against 64 x 128), a cluster's exchange 3500.
 uint32_t narrow_cluster(uint32_t m, uint32_t n)
 {
     uint32_t c = 1;

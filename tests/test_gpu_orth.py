@@ -2,7 +2,7 @@
 
 Tolerance in the 2-norm of a matrix.  bf16 outputs: rounding errors uniform within half a unit, 2^-9 to
 2^-8 of a value: 1.7e-3 on average over many entries, at most 2^-8 = 3.9e-3 for one.  Products: each
-step rounds A, B and the operand X to 11 bits (2^-12 on average 0.42 * 2^-11 = 2.0e-4 of a value); a
+step rounds A, P and the operand X to 11 bits (2^-12 on average 0.42 * 2^-11 = 2.0e-4 of a value); a
 rounding of step i reaches the output through the steps behind it, whose mean slope is below 1.5,
 and b A and c A^2 (up to 4.8 and 2.0 times A, of opposite sign) cancel: 5 steps x 3 roundings x about 3
 added in squares, 2.0e-4 * 3 * sqrt(15) = 2.4e-3 at most.  Together sqrt(1.7^2 + 2.4^2) e-3 = 2.9e-3;
