@@ -48,9 +48,12 @@ constexpr float LN2 = 0.6931471805599453f;
 // The streaming path treats entries below FLOOR as FLOOR, with weight 0 (masks of -inf, of the
 // type's lowest value, of -1e10 ...).  That is exact for rows whose maximum m has |m c| < SPAN and
 // scales in [SCALE_LO, SCALE_HI]: then (FLOOR - m) c < -2^20, and a weight of the maximum, 2^(m c - S), lies
-// within 2^(1/16) of 1.  All other rows, and rows with a NaN, take the slow path.
+// within 2^(1/16) of 1.  All other rows, and rows with a NaN, take the slow path.  While a thread
+// has seen nothing above FAR / c (masked entries alone) it sums against 0, so that they all have weight 0, as they
+// have in a row of this path: S may be -2^32 there, and its rounding would make weights of 2^128.
 constexpr float FLOOR = -0x1p30f;
 constexpr float SPAN = 0x1p20f;
+constexpr float FAR = -4.f * SPAN;       // of m c
 constexpr float SCALE_LO = 0x1p-8f, SCALE_HI = 0x1p8f;
 
 static_assert(GROUPS >= 2 * MAX_TOP, "the bound needs more groups than alternatives");
@@ -441,7 +444,7 @@ logprobs_kernel(const Args a)
                 raise(my, mc, bm, to);
                 mc = to;
             }
-            const float from = my.m == FLOOR ? 0.f : -mc;        // nothing but FLOOR yet: weights 0
+            const float from = mc < FAR ? 0.f : -mc;             // masked entries alone so far: weights 0
             const uint64_t shift = pair(from, from);
             uint64_t s = pair(my.s, 0.f), q = pair(my.q, 0.f);
 #pragma unroll

@@ -254,6 +254,24 @@ def test_outputs_are_optional_and_repeatable():
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,vocab", [(40, 37), (40, 9001), (700, 3001)])
+@pytest.mark.parametrize("scale", [0.3, 1.5, 1.9, 1.963087797164917, 2.7261552810668945, 12.0, 200.0])
+def test_masks_at_other_scales(scale, rows, vocab, dtype):
+    """Finite masks of every size, which threads may see and nothing else; allowed tokens of nearly equal logits."""
+    scale = float(np.float32(scale))
+    for i, fill in enumerate((-1e9, -1.07e9, -3e8, -2.5e7, -3e6, -7e5, -1e4)):
+        x = rows_of(rows, vocab, dtype, 13 + i, sigma=0.01)
+        keep = torch.zeros(rows, vocab, dtype=torch.bool, device="cuda")
+        for r in range(rows):
+            keep[r, r % 37::(5, 9, 40, 700)[r % 4]] = True
+        keep[5] = False                                            # nothing allowed
+        x.masked_fill_(~keep, fill)
+        t = (torch.arange(rows, device="cuda") % 37).long()
+        out, ref = call(x, t, 1, scale), reference(x, t, 1, scale)
+        check(out, ref, vocab, 1)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("offset", [300.0, -1000.0, 1e4, -5e5, 5.5e5])
 def test_common_offset_of_the_logits(offset, dtype):
     """A constant added to a row changes its lse and nothing else: the tolerances are those without
