@@ -601,6 +601,70 @@ deco_status deco_apply_update_orth(deco_ctx *ctx, deco_orth *h, float *momentum,
  * anomaly (a bounded wait that ran out: DECO_ERR_TIMEOUT in device_status) since the handle was created. */
 deco_status deco_orth_get_stats(deco_orth *h, void *stream, deco_orth_stats *out);
 
+/* ------------------------------------------- inside the gradient: layer norm and activations in 8 bits */
+
+/*
+ * What lies between a worker's loss and deco_ef_compress: the norm of every layer with its gradient, activations put
+ * away in a quarter or half of their bytes, and the gradients that are computed from them.  Gradients of weights are
+ * written, or added, straight to where the exchange takes them from: the matrix's place in the flat gradient vector, in
+ * its type.  (The paper takes a worker's gradient as given.)
+ *
+ * Rows.  x, y, dy, ... are [rows] x [cols] of `dtype` (deco_dtype), consecutive within a row, rows `stride` entries
+ * apart (>= cols); any alignment of whole entries, else DECO_ERR_INVALID_ARG.  16-byte accesses are used where all rows of a
+ * call start on 16 bytes and cols is a multiple of 8.  rows < 2^28, cols <= 2^24.  All pointers are DEVICE.  Sums are held
+ * in fp32.  The same inputs give the same bits.  Calls work on the CURRENT device, allocate nothing and keep nothing between calls;
+ * calls that run at the same time need workspaces of their own.
+ *
+ * A checkpoint in 8 bits of [rows] x [cols]: with blocks = ceil(cols / 32),
+ *   codes      [rows][32 blocks] int8, 16-byte aligned;  exponents  [rows][blocks] uint8
+ * Entry j of a row stands for codes[j] * 2^(exponents[j / 32] - 127).  The exponent is the smallest one for which the
+ * block's largest magnitude rounds to at most 127 (at least 1), the code is the entry over that power of two rounded to even: at
+ * most half a step of 2^-6 of the block's largest magnitude, and exact wherever it is read back (bf16 too).  Codes beyond the
+ * row's end are 0.  (With the exponent 249, of blocks that reach 1.992 * 2^127, codes end at 63: 64 of that step are no fp32
+ * number.)  A block that holds a NaN or an infinity has the exponent 255 and stands for NaN.
+ */
+
+/*
+ * Per row:  u = x, or u = x + add rounded to dtype;  mean = sum u / cols;  rstd = 1 / sqrt(sum (u - mean)^2 / cols + eps);
+ *   y = (u - mean) * rstd * weight + bias
+ *   add        NULL, or rows of dtype (a residual);  sum: NULL, or where u is stored (only with add)
+ *   weight, bias   [cols] fp32; NULL: 1 and 0
+ *   mean, rstd     [rows] fp32, what the gradient needs; may be NULL
+ *   codes, exponents   NULL, or the checkpoint of u
+ * 0 < eps < inf.  y, and sum, may be x's or add's own buffer (same stride), not each other's.  A row with a NaN or an infinity
+ * gives NaN; entries beyond 2^60 in magnitude may overflow the variance, which gives 0 or NaN.
+ */
+deco_status deco_layernorm(const void *x, int32_t dtype, uint64_t rows, uint32_t cols, uint64_t x_stride,
+                           const void *add, uint64_t add_stride, void *sum, uint64_t sum_stride,
+                           const float *weight, const float *bias, float eps, void *y, uint64_t y_stride,
+                           float *mean, float *rstd, int8_t *codes, uint8_t *exponents, void *stream);
+
+/*
+ * Its gradient.  With h = (x - mean) * rstd and g = dy * weight:
+ *   dx = rstd * (g - sum g / cols - h * sum (g h) / cols)  (+ add)
+ *   dweight = sum over rows of dy h,   dbias = sum over rows of dy
+ *   x          rows of dtype (what was normalised: sum where there was one); or NULL, and codes and exponents its checkpoint
+ *   add        NULL, or rows of dtype: the gradient that reaches x beside the norm
+ *   dx         may be x's, dy's or add's own buffer (same stride)
+ *   dweight, dbias   [cols] of grad_dtype, overwritten, or added to if `accumulate`; either may be NULL
+ *   workspace  at least deco_layernorm_grad_workspace(rows, cols) bytes, 16-byte aligned, whose contents do not matter
+ *              (may be NULL if dweight and dbias are, and cols <= 8192); fewer: DECO_ERR_CAPACITY
+ * rows = 0 gives sums of 0.
+ */
+uint64_t deco_layernorm_grad_workspace(uint64_t rows, uint32_t cols);
+deco_status deco_layernorm_grad(const void *x, int32_t dtype, uint64_t rows, uint32_t cols, uint64_t x_stride,
+                                const int8_t *codes, const uint8_t *exponents, const float *mean,
+                                const float *rstd, const float *weight, const void *dy, uint64_t dy_stride,
+                                const void *add, uint64_t add_stride, void *dx, uint64_t dx_stride,
+                                void *dweight, void *dbias, int32_t grad_dtype, int32_t accumulate,
+                                void *workspace, uint64_t workspace_bytes, void *stream);
+
+/* Put x away in 8 bits, and take a checkpoint's values back. */
+deco_status deco_pack8(const void *x, int32_t dtype, uint64_t rows, uint32_t cols, uint64_t x_stride,
+                       int8_t *codes, uint8_t *exponents, void *stream);
+deco_status deco_unpack8(const int8_t *codes, const uint8_t *exponents, uint64_t rows, uint32_t cols,
+                         void *y, int32_t dtype, uint64_t y_stride, void *stream);
+
 const char *deco_status_string(deco_status s);
 
 #ifdef __cplusplus

@@ -156,6 +156,13 @@ SIGNATURES = {
     "deco_orth_run": (_i32, [_vp, _vp, _i32, _vp, _vp, _vp]),
     "deco_apply_update_orth": (_i32, [_vp, _vp, _vp, _f32, _vp]),
     "deco_orth_get_stats": (_i32, [_vp, _vp, _P(deco_orth_stats)]),
+    "deco_layernorm": (_i32, [_vp, _i32, _u64, _u32, _u64, _vp, _u64, _vp, _u64, _vp, _vp, _f32, _vp, _u64, _vp, _vp,
+                              _vp, _vp, _vp]),
+    "deco_layernorm_grad_workspace": (_u64, [_u64, _u32]),
+    "deco_layernorm_grad": (_i32, [_vp, _i32, _u64, _u32, _u64, _vp, _vp, _vp, _vp, _vp, _vp, _u64, _vp, _u64, _vp,
+                                   _u64, _vp, _vp, _i32, _i32, _vp, _u64, _vp]),
+    "deco_pack8": (_i32, [_vp, _i32, _u64, _u32, _u64, _vp, _vp, _vp]),
+    "deco_unpack8": (_i32, [_vp, _vp, _u64, _u32, _vp, _i32, _u64, _vp]),
     "deco_status_string": (ctypes.c_char_p, [_i32]),
 }
 
@@ -687,6 +694,127 @@ def deco_orth_get_stats(h, stream=None):
     s = _stream_on(stream, _orth_handles[h][1]) if h in _orth_handles else _stream(stream)
     _check(load().deco_orth_get_stats(h, s, ctypes.byref(st)), "deco_orth_get_stats")
     return {f: getattr(st, f) for f, _ in deco_orth_stats._fields_}
+
+
+# ------------------------------------------------------------- inside the gradient
+
+def packed8_empty(rows, cols, device=None):
+    """(codes, exponents): room for the 8-bit checkpoint of [rows, cols] activations."""
+    import torch
+    blocks = (cols + 31) // 32
+    device = device if device is not None else "cuda"
+    return (torch.empty(rows, 32 * blocks, dtype=torch.int8, device=device),
+            torch.empty(rows, blocks, dtype=torch.uint8, device=device))
+
+
+def _like(x, where, name, device, dtype, shape):
+    """(address, row stride) of a 2-D CUDA tensor of that type and shape; (None, 0) for None."""
+    if x is None:
+        return None, 0
+    if x.dtype != dtype or x.shape != shape:
+        raise ValueError("%s: %s must be %s of shape %s" % (where, name, dtype, tuple(shape)))
+    row = _rows_of(x, where, name, device)
+    return row[0], row[4]
+
+
+def _packed(packed, where, device, rows, cols):
+    """Addresses of a checkpoint's two tensors."""
+    if packed is None:
+        return None, None
+    codes, exps = packed
+    blocks = (cols + 31) // 32
+    return (_tensor(codes, where, "codes", device, ("int8",), (rows, 32 * blocks)),
+            _tensor(exps, where, "exponents", device, ("uint8",), (rows, blocks)))
+
+
+def _workspace(workspace, where, nbytes, device, stream):
+    """(tensor, address, bytes): the caller's, or one that belongs to the call's stream."""
+    if workspace is not None:
+        p = _tensor(workspace, where, "workspace", device, ("uint8",))
+        return workspace, p, workspace.numel()
+    if nbytes == 0:
+        return None, None, 0
+    import torch
+    if stream is None:
+        room = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    else:
+        with torch.cuda.stream(torch.cuda.ExternalStream(_stream(stream), device)):
+            room = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return room, room.data_ptr(), nbytes
+
+
+def deco_layernorm(x, weight, bias, y, mean=None, rstd=None, eps=1e-5, add=None, total=None, packed=None, stream=None):
+    """Layer norm of the rows of `x` ([rows, cols], f32 or bf16) into `y`; `weight` and `bias` [cols] f32 or None.  With
+    `add` (a residual) of x + add, which is stored in `total` if given.  `mean`, `rstd` ([rows] f32): what the gradient
+    needs.  `packed`: (codes, exponents) to put what was normalised away in 8 bits."""
+    w = "deco_layernorm"
+    p, kind, rows, cols, stride, dev = _rows_of(x, w, "x")
+    ap, astride = _like(add, w, "add", dev, x.dtype, x.shape)
+    tp, tstride = _like(total, w, "total", dev, x.dtype, x.shape)
+    yp, ystride = _like(y, w, "y", dev, x.dtype, x.shape)
+    codes, exps = _packed(packed, w, dev, rows, cols)
+    _check(load().deco_layernorm(
+        p, kind, rows, cols, stride, ap, astride, tp, tstride, _tensor(weight, w, "weight", dev, ("float32",), (cols,)),
+        _tensor(bias, w, "bias", dev, ("float32",), (cols,)), eps, yp, ystride,
+        _tensor(mean, w, "mean", dev, ("float32",), (rows,)), _tensor(rstd, w, "rstd", dev, ("float32",), (rows,)),
+        codes, exps, _stream_on(stream, dev)), w)
+
+
+def deco_layernorm_grad_workspace(rows, cols):
+    """Bytes of workspace that deco_layernorm_grad needs."""
+    return load().deco_layernorm_grad_workspace(rows, cols)
+
+
+def _grad_kind(where, *grads):
+    """Type code of gradients that are given (all of one type); f32 if none is."""
+    kinds = {g.dtype for g in grads if g is not None}
+    if len(kinds) > 1:
+        raise ValueError("%s: the gradients must have one type" % where)
+    return DECO_BF16 if kinds and "bfloat16" in str(kinds.pop()) else DECO_F32
+
+
+def deco_layernorm_grad(x, mean, rstd, weight, dy, dx, dweight=None, dbias=None, add=None, accumulate=False,
+                        workspace=None, stream=None):
+    """Gradient of deco_layernorm: `dx` ([rows, cols], the type of `dy`), and if given `dweight` and `dbias` ([cols], f32 or
+    bf16; added to with `accumulate`).  `x`: what was normalised, or its checkpoint (codes, exponents).  `add`: the
+    gradient that reaches x beside the norm.  `workspace`: uint8 tensor of deco_layernorm_grad_workspace bytes; by
+    default the call makes one."""
+    w = "deco_layernorm_grad"
+    p, kind, rows, cols, stride, dev = _rows_of(dy, w, "dy")
+    codes = exps = None
+    if isinstance(x, (tuple, list)):
+        codes, exps = _packed(x, w, dev, rows, cols)
+        xp, xstride = None, 0
+    else:
+        xp, xstride = _like(x, w, "x", dev, dy.dtype, dy.shape)
+    ap, astride = _like(add, w, "add", dev, dy.dtype, dy.shape)
+    dp, dstride = _like(dx, w, "dx", dev, dy.dtype, dy.shape)
+    gkind = _grad_kind(w, dweight, dbias)
+    need = load().deco_layernorm_grad_workspace(rows, cols)
+    room, wp, nbytes = _workspace(workspace, w, need, dev, stream)
+    both = ("float32", "bfloat16")
+    _check(load().deco_layernorm_grad(
+        xp, kind, rows, cols, xstride, codes, exps, _tensor(mean, w, "mean", dev, ("float32",), (rows,)),
+        _tensor(rstd, w, "rstd", dev, ("float32",), (rows,)), _tensor(weight, w, "weight", dev, ("float32",), (cols,)),
+        p, stride, ap, astride, dp, dstride, _tensor(dweight, w, "dweight", dev, both, (cols,)),
+        _tensor(dbias, w, "dbias", dev, both, (cols,)), gkind, int(bool(accumulate)), wp, nbytes,
+        _stream_on(stream, dev)), w)
+
+
+def deco_pack8(x, packed, stream=None):
+    """Put the rows of `x` ([rows, cols], f32 or bf16) away in 8 bits: `packed` = (codes, exponents), see packed8_empty."""
+    w = "deco_pack8"
+    p, kind, rows, cols, stride, dev = _rows_of(x, w, "x")
+    codes, exps = _packed(packed, w, dev, rows, cols)
+    _check(load().deco_pack8(p, kind, rows, cols, stride, codes, exps, _stream_on(stream, dev)), w)
+
+
+def deco_unpack8(packed, y, stream=None):
+    """The values of a checkpoint into `y` ([rows, cols], f32 or bf16; exact in both)."""
+    w = "deco_unpack8"
+    p, kind, rows, cols, stride, dev = _rows_of(y, w, "y")
+    codes, exps = _packed(packed, w, dev, rows, cols)
+    _check(load().deco_unpack8(codes, exps, rows, cols, p, kind, stride, _stream_on(stream, dev)), w)
 
 
 # ------------------------------------------------------------- device views (plumbing)
