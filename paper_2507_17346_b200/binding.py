@@ -163,6 +163,8 @@ SIGNATURES = {
                                    _u64, _vp, _vp, _i32, _i32, _vp, _u64, _vp]),
     "deco_pack8": (_i32, [_vp, _i32, _u64, _u32, _u64, _vp, _vp, _vp]),
     "deco_unpack8": (_i32, [_vp, _vp, _u64, _u32, _vp, _i32, _u64, _vp]),
+    "deco_weight_grad8_workspace": (_u64, [_vp, _i32, _u64, _u32, _u64, _u32, _i32, _i32]),
+    "deco_weight_grad8": (_i32, [_vp, _i32, _u64, _u32, _u64, _vp, _vp, _u32, _vp, _vp, _i32, _i32, _i32, _vp, _u64, _vp]),
     "deco_status_string": (ctypes.c_char_p, [_i32]),
 }
 
@@ -815,6 +817,32 @@ def deco_unpack8(packed, y, stream=None):
     p, kind, rows, cols, stride, dev = _rows_of(y, w, "y")
     codes, exps = _packed(packed, w, dev, rows, cols)
     _check(load().deco_unpack8(codes, exps, rows, cols, p, kind, stride, _stream_on(stream, dev)), w)
+
+
+def deco_weight_grad8_workspace(dy, cols, bias=True, grad_dtype=DECO_F32):
+    """Bytes of workspace that deco_weight_grad8 needs for this `dy` and an input of `cols` columns."""
+    p, kind, rows, out, stride, _ = _rows_of(dy, "deco_weight_grad8_workspace", "dy")
+    return load().deco_weight_grad8_workspace(p, kind, rows, out, stride, cols, int(bool(bias)), grad_dtype)
+
+
+def deco_weight_grad8(dy, packed, dw, db=None, transposed=False, accumulate=False, workspace=None, stream=None):
+    """Weight gradient of a linear layer whose input was kept in 8 bits: `dy` [tokens, out] (f32 or bf16), `packed` = (codes,
+    exponents) of the input [tokens, cols], `dw` [out, cols] ([cols, out] with `transposed`) and if given `db` [out], of one
+    type (f32 or bf16), views of the flat gradient vector perhaps; added to with `accumulate`.  `workspace`: uint8
+    tensor of deco_weight_grad8_workspace bytes; by default the call makes one."""
+    w = "deco_weight_grad8"
+    p, kind, rows, out, stride, dev = _rows_of(dy, w, "dy")
+    if dw.dim() != 2 or dw.shape[1 if transposed else 0] != out:
+        raise ValueError("%s: dw must have shape %s" % (w, "(cols, %d)" % out if transposed else "(%d, cols)" % out))
+    cols = dw.shape[0 if transposed else 1]
+    both = ("float32", "bfloat16")
+    codes, exps = _packed(packed, w, dev, rows, cols)
+    gkind = _grad_kind(w, dw, db)
+    need = load().deco_weight_grad8_workspace(p, kind, rows, out, stride, cols, int(db is not None), gkind)
+    room, wp, nbytes = _workspace(workspace, w, need, dev, stream)
+    _check(load().deco_weight_grad8(
+        p, kind, rows, out, stride, codes, exps, cols, _tensor(dw, w, "dw", dev, both), _tensor(db, w, "db", dev, both, (out,)),
+        gkind, int(bool(transposed)), int(bool(accumulate)), wp, nbytes, _stream_on(stream, dev)), w)
 
 
 # ------------------------------------------------------------- device views (plumbing)

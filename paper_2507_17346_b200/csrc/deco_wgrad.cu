@@ -1,0 +1,681 @@
+// deco_weight_grad8: the weight gradient of a linear layer whose input was put away in 8 bits,
+//     dW[o][i] = sum_t dY[t][o] X[t][i],   db[o] = sum_t dY[t][o],
+// on the tensor cores.  X's entries, 8-bit integers times a power of two, are bf16 numbers, so the products are exact and
+// X is never written out: eight warps read codes (a byte an entry), make bf16 of them (five instructions for two) and
+// put them into shared memory as the operand, while dY comes by box copies.  Both operands have their outer
+// dimension consecutive, 128-byte swizzle.
+//
+// fp32 dY is taken as the sum of bf16 numbers, hi + mid + lo (24 bits; hi + mid where the result is bf16), split by a
+// launch before; the same launch lays out bf16 rows that do not start on 16 bytes.
+//
+// db.  Sixteen columns of ones behind a CTA's columns of X in shared memory make it one more column of the
+// product, for an eighth of the tensor cores' time in the tiles of the first columns, and no second pass over dY.
+//
+// Sums.  The tensor cores' fp32 sums are cut off, not rounded: over 8192 products the result is 9e-6 off (in the 2-norm), over
+// 512 5e-7.  So, where the result is fp32, the accumulators are emptied every CHUNK blocks of 64 tokens into
+// registers of the converting warps, where sums are rounded; the two accumulators take turns, and the products go on.
+// lo's and mid's products of a chunk come before hi's, while the sum is still small.
+//
+// Shares.  The blocks of all tiles in a row, cut into equal ranges, one per CTA: a CTA begins and ends inside tiles.  Parts
+// of a tile are left in the workspace and added in their order by a second launch: the same bits every time.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <atomic>
+
+#include "deco.h"
+#include "deco_packed8.h"
+#include "deco_tensor.h"
+
+namespace {
+
+using namespace deco::tensor;
+using deco::BLOCK8;
+
+constexpr int BK = 64;                   // tokens per stage
+constexpr int STAGES = 6;
+constexpr uint32_t TILE_M = 128;         // of dY's columns, a CTA's
+constexpr uint32_t MAX_H = 128;          // of X's columns, a CTA's, with those of ones
+constexpr uint32_t ONES = 16;            // columns of ones, a CTA's
+constexpr uint32_t SLAB = BK * 128;      // 64 columns of an operand
+constexpr uint32_t OPERAND = 2 * SLAB, STAGE_BYTES = 2 * OPERAND;
+constexpr int WORK_WARPS = 8;            // convert, and empty the accumulators
+constexpr int WORK_THREADS = 32 * WORK_WARPS;
+constexpr int THREADS = WORK_THREADS + 64;       // and one warp that loads, one that multiplies
+constexpr uint32_t STAGING_FLOATS = 32 * 33;     // of a warp
+constexpr size_t SMEM = STAGES * STAGE_BYTES + WORK_WARPS * STAGING_FLOATS * 4 + 1024;
+constexpr uint32_t CHUNK = 8;            // blocks an accumulator takes before it is emptied
+constexpr uint32_t SMS = 148;
+constexpr uint32_t MIN_BLOCKS = 8;       // a CTA's share, if tiles have to be cut for it
+constexpr int UNITS = BK * MAX_H / 8 / WORK_THREADS;     // 8-code units of a thread per block
+
+// A tile is CG * 128 columns of dY by CG * h of X, h a multiple of 16.  A CTA (of a pair) makes the operand of h of the
+// product's columns and, in tiles that sum db too, of 16 of ones behind them.
+struct Args {
+    const int8_t *codes;
+    const uint8_t *exps;
+    uint32_t rows, blocks8;              // tokens, blocks of a row of X
+    uint32_t out, cols;
+    uint32_t h, tiles_n, k_blocks;
+    uint32_t planes, plane_rows, chunk;
+    uint64_t units;                      // tiles * k_blocks
+    uint32_t workers;                    // CTAs or pairs
+    void *dw, *db;
+    int transposed, accumulate;
+    float *slots;                        // [worker][2][CG][columns of a tile's product][TILE_M]
+};
+
+struct __align__(8) Control {
+    uint64_t full[STAGES], empty[STAGES], acc_full[2], acc_empty[2];
+    uint32_t tmem;
+    volatile uint32_t abort;
+};
+
+// The blocks of a worker in their order: segments of tiles, in them chunks, in those planes (the smallest first), in those
+// blocks of tokens.
+struct Cursor {
+    uint32_t tile, first, last;          // segment
+    uint32_t c0, c1;                     // chunk
+    uint32_t plane, k;                   // block
+    bool done;
+    __device__ void segment(const Args &g, uint64_t u, uint64_t end)
+    {
+        done = u >= end;
+        if (done) return;
+        tile = static_cast<uint32_t>(u / g.k_blocks);
+        first = c0 = k = static_cast<uint32_t>(u - static_cast<uint64_t>(tile) * g.k_blocks);
+        last = static_cast<uint32_t>(min(static_cast<uint64_t>(g.k_blocks), k + (end - u)));
+        c1 = min(c0 + g.chunk, last);
+        plane = g.planes - 1;
+    }
+    __device__ Cursor(const Args &g, uint32_t worker) { segment(g, g.units * worker / g.workers, g.units * (worker + 1) / g.workers); }
+    __device__ bool chunk_ends() const { return k + 1 == c1 && plane == 0; }
+    __device__ void advance(const Args &g, uint32_t worker)
+    {
+        if (++k < c1) return;
+        if (plane) {
+            plane -= 1;
+            k = c0;
+        } else if (c1 < last) {
+            c0 = k = c1;
+            c1 = min(c0 + g.chunk, last);
+            plane = g.planes - 1;
+        } else {
+            segment(g, static_cast<uint64_t>(tile) * g.k_blocks + last, g.units * (worker + 1) / g.workers);
+        }
+    }
+    // of the chunk: where its sums begin and end
+    enum : uint32_t { BEGINS = 1, ENDS = 2, FROM_TOP = 4, WHOLE = 8 };
+    __device__ uint32_t flags(const Args &g) const
+    {
+        return (c0 == first ? BEGINS : 0u) | (c1 == last ? ENDS : 0u) | (first == 0 ? FROM_TOP : 0u) |
+               (last - first == g.k_blocks ? WHOLE : 0u);
+    }
+};
+
+// Columns of a tile's product: `width` of them, of which `in` belong to X, as column `col` of the tile.
+template <int CG>
+struct Columns {
+    uint32_t h, half, width;
+    bool ones;
+    __device__ Columns(const Args &g, uint32_t nt) : h(g.h), ones(g.db && nt == 0)
+    {
+        half = h + (ones ? ONES : 0);
+        width = CG * half;
+    }
+    __device__ bool in(uint32_t n) const { return n < h || (CG == 2 && n >= half && n < half + h); }
+    __device__ uint32_t col(uint32_t n) const { return CG == 2 && n >= half ? n - half + h : n; }
+};
+
+template <typename G> __device__ __forceinline__ float grad_at(const G *p);
+template <> __device__ __forceinline__ float grad_at<float>(const float *p) { return *p; }
+template <> __device__ __forceinline__ float grad_at<__nv_bfloat16>(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
+__device__ __forceinline__ void put_grad(float *p, float v) { *p = v; }
+__device__ __forceinline__ void put_grad(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
+template <typename G> __device__ __forceinline__ void store_grad(void *base, uint64_t at, float v, int accumulate)
+{
+    G *p = static_cast<G *>(base) + at;
+    put_grad(p, accumulate ? grad_at<G>(p) + v : v);
+}
+
+// Eight codes times 2^(exp - 127) as bf16.  A code's low seven bits in the place of a bf16 fraction with the exponent of
+// 128 are 128 + those bits; its sign bit in the place of the lowest exponent bit makes 256 of 128: the
+// difference is the code, exactly.
+__device__ __forceinline__ uint4 converted(uint2 codes, uint32_t exp)
+{
+    const uint32_t one = exp == 255u ? 0x7FC0u : exp << 7, scale = one | one << 16;
+    uint32_t o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t p = __byte_perm(i < 2 ? codes.x : codes.y, 0, i & 1 ? 0x4342 : 0x4140);
+        const uint32_t a = (p & 0x007F007Fu) | 0x43004300u, b = (p & 0x00800080u) | 0x43004300u;
+        uint32_t d;
+        asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+        asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(o[i]) : "r"(d), "r"(scale));
+    }
+    return make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+// Where the 8 columns from 8 c on of token k lie in an operand's stage.
+__device__ __forceinline__ uint32_t unit_offset(uint32_t k, uint32_t c)
+{
+    return (c >> 3) * SLAB + k * 128 + (((c & 7) ^ (k & 7)) << 4);
+}
+
+template <int CG, typename G>
+__global__ void __launch_bounds__(THREADS, 1)
+wgrad_kernel(const __grid_constant__ CUtensorMap map, const Args g)
+{
+    constexpr uint32_t GROUPS = 2 * CG;          // of 32 columns of the product, a warp's
+    constexpr uint32_t SIDE = GROUPS * 32;
+    extern __shared__ uint8_t raw[];
+    __shared__ Control ctl;
+    const uint32_t stages = (smem_addr(raw) + 1023) & ~1023u;
+    const uint32_t wid = threadIdx.x >> 5, lane = threadIdx.x & 31, worker = blockIdx.x / CG;
+    uint32_t rank = 0;
+    if (CG == 2) asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) {
+            bar_init(&ctl.full[s], 1 + CG * WORK_WARPS);
+            bar_init(&ctl.empty[s], 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            bar_init(&ctl.acc_full[s], 1);
+            bar_init(&ctl.acc_empty[s], CG * WORK_WARPS);
+        }
+        ctl.abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (wid == WORK_WARPS + 1) tmem_alloc<CG>(&ctl.tmem, 512);
+    if (g.db && threadIdx.x < BK)                                // the columns of ones, which nothing overwrites
+        for (int s = 0; s < STAGES; ++s)
+            for (uint32_t c = 0; c < ONES / 8; ++c)
+                sts16(stages + s * STAGE_BYTES + OPERAND + unit_offset(threadIdx.x, g.h / 8 + c),
+                      make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u));
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (CG == 2) {
+        asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = ctl.tmem;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+
+    if (wid == WORK_WARPS) {
+        if (lane == 0) {
+            uint32_t s = 0, parity = 1;
+            const uint32_t full0 = smem_addr(ctl.full), bar0 = CG == 1 ? full0 : leader_addr(full0);
+            for (Cursor cur(g, worker); !cur.done; cur.advance(g, worker)) {
+                if (!bar_wait(&ctl.empty[s], parity, &ctl.abort)) break;
+                const uint32_t st = stages + s * STAGE_BYTES, bar = bar0 + s * 8;
+                const int32_t x = ((cur.tile / g.tiles_n) * CG + rank) * TILE_M, y = cur.plane * g.plane_rows + cur.k * BK;
+                if (rank == 0) bar_expect(&ctl.full[s], CG * OPERAND);
+                load_box<CG>(st, &map, x, y, bar);
+                load_box<CG>(st + SLAB, &map, x + 64, y, bar);
+                if (++s == STAGES) {
+                    s = 0;
+                    parity ^= 1;
+                }
+            }
+            if (ctl.abort) {                                     // copies under way get time to land
+                const long long t0 = clock64();
+                while (clock64() - t0 < 20000000ll) {}
+            }
+        }
+    } else if (wid == WORK_WARPS + 1) {
+        if (lane == 0 && rank == 0) {
+            uint32_t s = 0, parity = 0, n = 0;
+            bool first = true;                                   // block of a chunk
+            for (Cursor cur(g, worker); !cur.done; cur.advance(g, worker)) {
+                const uint32_t as = n & 1;
+                if (first && !bar_wait(&ctl.acc_empty[as], ((n >> 1) & 1) ^ 1, &ctl.abort)) break;
+                if (!bar_wait(&ctl.full[s], parity, &ctl.abort)) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const Columns<CG> c(g, cur.tile % g.tiles_n);
+                // bf16 operands, fp32 sums, outer dimensions consecutive, N and M
+                const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) |
+                                       ((c.width >> 3) << 17) | ((CG * TILE_M >> 4) << 24);
+                const uint64_t da = operand_desc(stages + s * STAGE_BYTES, true);
+                const uint64_t db = operand_desc(stages + s * STAGE_BYTES + OPERAND, true);
+#pragma unroll
+                for (uint32_t q = 0; q < BK / 16; ++q)
+                    mma<CG>(tmem + as * 256, da + q * (2048 >> 4), db + q * (2048 >> 4), idesc, !first || q != 0);
+                mma_commit<CG>(&ctl.empty[s]);
+                first = cur.chunk_ends();
+                if (first) {
+                    mma_commit<CG>(&ctl.acc_full[as]);
+                    n += 1;
+                }
+                if (++s == STAGES) {
+                    s = 0;
+                    parity ^= 1;
+                }
+            }
+        }
+    } else {
+        const uint32_t quad = wid & 3, side = wid >> 2;          // lanes of the tensor memory, half of the columns
+        float *staging = reinterpret_cast<float *>(raw + (stages - smem_addr(raw)) + STAGES * STAGE_BYTES) + wid * STAGING_FLOATS;
+        const uint32_t pitch = g.blocks8 * BLOCK8;
+        // this thread's units of a block: token * 16 + unit of the row (BK * 16: none)
+        uint32_t unit[UNITS];
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i) {
+            const uint32_t id = i * WORK_THREADS + threadIdx.x, per_row = g.h / 8, token = id / per_row;
+            unit[i] = token < BK ? token * 16 + id - token * per_row : BK * 16;
+        }
+        uint2 code[UNITS];
+        uint32_t exp[UNITS];
+        Cursor ahead(g, worker);                                 // the block that is being read
+        auto fetch = [&](int i) {
+            const uint32_t col = ((ahead.tile % g.tiles_n) * CG + rank) * g.h + (unit[i] & 15) * 8, t = ahead.k * BK + (unit[i] >> 4);
+            code[i] = make_uint2(0, 0);
+            exp[i] = 0;
+            if (unit[i] < BK * 16 && t < g.rows && col < pitch) {
+                code[i] = __ldg(reinterpret_cast<const uint2 *>(g.codes + static_cast<uint64_t>(t) * pitch + col));
+                exp[i] = __ldg(g.exps + static_cast<uint64_t>(t) * g.blocks8 + col / BLOCK8);
+            }
+        };
+        float sum[GROUPS][32];                                   // this warp's half of the columns, a row a thread
+        uint32_t s = 0, parity = 1, emptied = 0, staged = 0;
+        bool dead = false, pending = false, ended = false;
+        uint32_t end_tile = 0, end_flags = 0, full_tile = 0, full_flags = 0;     // chunk just staged; chunk to be emptied
+        bool have = !ahead.done;                                 // a block is in the registers
+        uint32_t now_tile = 0, now_flags = 0;
+        bool now_ends = false;
+        auto read_next = [&]() {
+            now_tile = ahead.tile;
+            now_flags = ahead.flags(g);
+            now_ends = ahead.chunk_ends();
+        };
+        if (have) {
+#pragma unroll
+            for (int i = 0; i < UNITS; ++i) fetch(i);
+            read_next();
+            ahead.advance(g, worker);
+        }
+        // Block after block is converted; a chunk is emptied when STAGES blocks of the next are staged: then its products are
+        // done, and the tensor cores have work while this goes on.
+#pragma unroll 1
+        while (true) {
+            if (pending && (ended || !have || staged == STAGES)) {
+                pending = false;
+                const uint32_t as = emptied & 1;
+                if (!dead) dead = !bar_wait(&ctl.acc_full[as], (emptied >> 1) & 1, &ctl.abort);
+                dead = __any_sync(0xFFFFFFFFu, dead);
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t nt = full_tile % g.tiles_n, mt = (full_tile / g.tiles_n) * CG + rank;
+                const Columns<CG> c(g, nt);
+                const bool begins = full_flags & Cursor::BEGINS;
+#pragma unroll
+                for (uint32_t h = 0; h < GROUPS; ++h) {
+                    if (side * SIDE + h * 32 >= c.width) continue;
+                    uint32_t v[32];
+                    __syncwarp();
+                    tmem_load32(tmem + ((quad * 32) << 16) + as * 256 + side * SIDE + h * 32, v);
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) sum[h][j] = begins ? __uint_as_float(v[j]) : sum[h][j] + __uint_as_float(v[j]);
+                    if (dead) {                                  // a wait has run out: what comes is no sum
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) sum[h][j] = __uint_as_float(0x7FC00000u);
+                    }
+                }
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) bar_arrive_leader<CG>(&ctl.acc_empty[as]);
+                emptied += 1;
+                if (full_flags & Cursor::ENDS) {                 // of a segment: its sums go out
+                    const uint32_t o = mt * TILE_M + quad * 32 + lane, col0 = nt * CG * g.h;
+                    float *slot = g.slots + ((worker * 2ull + (full_flags & Cursor::FROM_TOP ? 1 : 0)) * CG + rank) * (CG * MAX_H * TILE_M) +
+                                  quad * 32 + lane;
+#pragma unroll
+                    for (uint32_t h = 0; h < GROUPS; ++h) {
+                        const uint32_t n0 = side * SIDE + h * 32;
+                        if (n0 >= c.width) continue;
+                        if (!(full_flags & Cursor::WHOLE)) {
+#pragma unroll
+                            for (uint32_t j = 0; j < 32; ++j)
+                                if (n0 + j < c.width) __stcg(slot + (n0 + j) * TILE_M, sum[h][j]);
+                            continue;
+                        }
+                        if (g.transposed) {
+#pragma unroll
+                            for (uint32_t j = 0; j < 32; ++j)
+                                if (c.in(n0 + j) && col0 + c.col(n0 + j) < g.cols && o < g.out)
+                                    store_grad<G>(g.dw, static_cast<uint64_t>(col0 + c.col(n0 + j)) * g.out + o, sum[h][j], g.accumulate);
+                        } else {
+                            const uint32_t col = col0 + c.col(n0 + lane);
+                            const bool in = c.in(n0 + lane) && col < g.cols;
+                            __syncwarp();
+#pragma unroll
+                            for (uint32_t j = 0; j < 32; ++j) staging[lane * 33 + j] = sum[h][j];
+                            __syncwarp();
+#pragma unroll 4
+                            for (uint32_t r = 0; r < 32; ++r) {
+                                const uint32_t row = mt * TILE_M + quad * 32 + r;
+                                if (in && row < g.out)
+                                    store_grad<G>(g.dw, static_cast<uint64_t>(row) * g.cols + col, staging[r * 33 + lane], g.accumulate);
+                            }
+                        }
+                        if (c.ones && n0 <= c.h && c.h < n0 + 32 && o < g.out)               // the first column of ones
+                            store_grad<G>(g.db, o, c.h & 16 ? sum[h][16] : sum[h][0], g.accumulate);
+                    }
+                }
+            }
+            if (ended) {
+                ended = false;
+                pending = true;
+                staged = 0;
+                full_tile = end_tile;
+                full_flags = end_flags;
+                if (!have) continue;
+            }
+            if (!have) break;
+            if (!dead) dead = !bar_wait(&ctl.empty[s], parity, &ctl.abort);
+            dead = __any_sync(0xFFFFFFFFu, dead);
+            const uint32_t base = stages + s * STAGE_BYTES + OPERAND;
+            const bool more = !ahead.done;
+#pragma unroll
+            for (int i = 0; i < UNITS; ++i) {
+                const uint4 o = converted(code[i], exp[i]);
+                if (more) fetch(i);
+                if (unit[i] < BK * 16 && !dead) sts16(base + unit_offset(unit[i] >> 4, unit[i] & 15), o);
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) bar_arrive_leader<CG>(&ctl.full[s]);
+            if (++s == STAGES) {
+                s = 0;
+                parity ^= 1;
+            }
+            staged += 1;
+            if (now_ends) {
+                ended = true;
+                end_tile = now_tile;
+                end_flags = now_flags;
+            }
+            have = more;
+            if (more) {
+                read_next();
+                ahead.advance(g, worker);
+            }
+        }
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (CG == 2) {                                               // (the pair's barriers are used until both are done)
+        asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    }
+    if (wid == WORK_WARPS + 1) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        tmem_free<CG>(tmem, 512);
+    }
+}
+
+// Tiles that lie in several workers' ranges: their parts added up in order, 32 columns and 128 rows a block of threads.
+template <int CG, typename G>
+__global__ void __launch_bounds__(256)
+join_kernel(const Args g)
+{
+    __shared__ float s[32][TILE_M + 1];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const uint32_t tile = blockIdx.x / CG, rank = blockIdx.x % CG, nt = tile % g.tiles_n, mt = (tile / g.tiles_n) * CG + rank;
+    const uint32_t n0 = blockIdx.y * 32;
+    const uint64_t first = static_cast<uint64_t>(tile) * g.k_blocks, last = first + g.k_blocks - 1;
+    auto owner = [&](uint64_t u) {                               // the worker whose range holds u
+        uint32_t c = static_cast<uint32_t>(u * g.workers / g.units);
+        while (g.units * (c + 1) / g.workers <= u) ++c;
+        while (g.units * c / g.workers > u) --c;
+        return c;
+    };
+    const uint32_t a = owner(first), b = owner(last);
+    const Columns<CG> c(g, nt);
+    if (a == b || n0 >= c.width) return;
+    const uint32_t row = threadIdx.x & (TILE_M - 1), j0 = threadIdx.x / TILE_M * 16;
+    float v[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) v[j] = 0.f;
+    for (uint32_t w = a; w <= b; ++w) {
+        // (a range in which the tile begins has it in the second slot, one that begins inside the tile in the first)
+        const float *p = g.slots + ((w * 2ull + (w == a)) * CG + rank) * (CG * MAX_H * TILE_M) + row;
+#pragma unroll
+        for (uint32_t j = 0; j < 16; ++j)
+            if (n0 + j0 + j < c.width) v[j] += __ldcg(p + (n0 + j0 + j) * TILE_M);
+    }
+    const uint32_t o = mt * TILE_M + row, col0 = nt * CG * g.h;
+    if (c.ones && n0 + j0 == c.h && o < g.out) store_grad<G>(g.db, o, v[0], g.accumulate);
+    if (g.transposed) {
+#pragma unroll
+        for (uint32_t j = 0; j < 16; ++j) {
+            const uint32_t n = n0 + j0 + j, col = col0 + c.col(n);
+            if (c.in(n) && col < g.cols && o < g.out)
+                store_grad<G>(g.dw, static_cast<uint64_t>(col) * g.out + o, v[j], g.accumulate);
+        }
+        return;
+    }
+#pragma unroll
+    for (uint32_t j = 0; j < 16; ++j) s[j0 + j][row] = v[j];
+    __syncthreads();
+    const uint32_t lane = threadIdx.x & 31, col = col0 + c.col(n0 + lane);
+    const bool in = c.in(n0 + lane) && col < g.cols;
+    for (uint32_t r = threadIdx.x >> 5; r < TILE_M; r += 8)
+        if (in && mt * TILE_M + r < g.out)
+            store_grad<G>(g.dw, static_cast<uint64_t>(mt * TILE_M + r) * g.cols + col, s[lane][r], g.accumulate);
+}
+
+// dY as bf16 rows that start on 16 bytes, in planes of which each holds what the ones before it left; rows beyond the last are 0.
+template <typename T>
+__global__ void __launch_bounds__(256)
+planes_kernel(const T *dy, uint64_t stride, uint32_t rows, uint32_t out, uint32_t pitch, uint32_t planes, uint32_t plane_rows,
+              __nv_bfloat16 *to)
+{
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const uint32_t col = (blockIdx.x * 256 + threadIdx.x) * 8;
+    if (col >= pitch) return;
+    for (uint32_t row = blockIdx.y; row < plane_rows; row += gridDim.y) {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            v[j] = 0.f;
+            if (row < rows && col + j < out) v[j] = static_cast<float>(dy[row * stride + col + j]);
+        }
+        for (uint32_t p = 0; p < planes; ++p) {
+            uint32_t w[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float x = v[j];
+                const bool number = fabsf(x) <= 3.402823466e38f;
+                // (a number that would round to infinity: the largest bf16 number, and the rest in the next plane)
+                float h = __bfloat162float(__float2bfloat16_rn(x));
+                if (number && fabsf(h) > 3.402823466e38f) h = copysignf(__uint_as_float(0x7F7F0000u), x);
+                v[j] = number ? x - h : 0.f;
+                w[j] = __float_as_uint(h) >> 16;
+            }
+            *reinterpret_cast<uint4 *>(to + (static_cast<uint64_t>(p) * plane_rows + row) * pitch + col) =
+                make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------ host
+
+constexpr uint64_t MAX_ROWS = 1ull << 28;
+constexpr uint32_t MAX_COLS = 1u << 24;
+constexpr uint64_t MAX_STRIDE = 1ull << 40;
+
+bool aligned_to(const void *p, uintptr_t unit) { return (reinterpret_cast<uintptr_t>(p) & (unit - 1)) == 0; }
+bool is_dtype(int32_t d) { return d == DECO_F32 || d == DECO_BF16; }
+
+struct Plan {
+    uint32_t planes;                     // 0: dY is read where it is
+    uint32_t plane_rows, pitch;
+    uint32_t cg, h, tiles_n, tiles_m, k_blocks, workers;
+    uint64_t units;
+    bool cut;                            // some tile lies in more than one range
+    uint64_t plane_bytes() const { return 2ull * planes * plane_rows * pitch; }
+    uint64_t bytes() const { return plane_bytes() + (cut ? 2ull * workers * cg * cg * MAX_H * TILE_M * 4 : 0); }
+};
+Plan make_plan(const void *dy, int32_t dtype, uint64_t rows, uint32_t out, uint64_t stride, uint32_t cols, bool bias,
+               int32_t grad_dtype)
+{
+    Plan p = {};
+    if (dtype == DECO_F32) p.planes = grad_dtype == DECO_F32 ? 3 : 2;
+    else if (!aligned_to(dy, 16) || stride % 8 || stride >= (1ull << 39)) p.planes = 1;      // (what box copies can address)
+    p.plane_rows = static_cast<uint32_t>((rows + BK - 1) / BK * BK);
+    p.pitch = (out + 7) / 8 * 8;
+    p.k_blocks = static_cast<uint32_t>((rows + BK - 1) / BK);
+    // Pairs of CTAs read half as much per product; small results are left to single CTAs, whose tiles are a quarter.
+    const uint64_t area = static_cast<uint64_t>((out + TILE_M - 1) / TILE_M) * ((cols + MAX_H - 1) / MAX_H);
+    p.cg = area * p.k_blocks >= 4 * SMS * MIN_BLOCKS ? 2 : 1;
+    const uint32_t most = p.cg * (MAX_H - (bias ? ONES : 0)), unit = 16 * p.cg;
+    p.tiles_n = (cols + most - 1) / most;
+    p.h = ((cols + p.tiles_n - 1) / p.tiles_n + unit - 1) / unit * 16;
+    p.tiles_m = (out + p.cg * TILE_M - 1) / (p.cg * TILE_M);
+    const uint64_t tiles = static_cast<uint64_t>(p.tiles_m) * p.tiles_n;
+    p.units = tiles * p.k_blocks;
+    p.workers = static_cast<uint32_t>(std::min<uint64_t>(SMS / p.cg, std::max(tiles, p.units / MIN_BLOCKS)));
+    p.cut = p.units % p.workers || (p.units / p.workers) % p.k_blocks;
+    return p;
+}
+
+template <int CG, typename G>
+bool allow()
+{
+    return cudaFuncSetAttribute(wgrad_kernel<CG, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(SMEM)) == cudaSuccess;
+}
+// the kernels' shared memory, once per device
+bool allow_shared_memory()
+{
+    static std::atomic<uint64_t> done{0};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return false;
+    if (dev < 64 && (done.load() >> dev & 1)) return true;
+    if (!allow<1, float>() || !allow<1, __nv_bfloat16>() || !allow<2, float>() || !allow<2, __nv_bfloat16>()) {
+        cudaGetLastError();
+        return false;
+    }
+    if (dev < 64) done.fetch_or(1ull << dev);
+    return true;
+}
+
+template <typename... P, typename... A>
+cudaError_t launch(void (*kernel)(P...), uint32_t cluster, dim3 grid, unsigned block, size_t smem, cudaStream_t s, A... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = cluster;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    const cudaError_t err = cudaLaunchKernelEx(&cfg, kernel, args...);
+    if (err != cudaSuccess) cudaGetLastError();                  // (pending, it would be taken for the next call's)
+    return err;
+}
+
+template <int CG, typename G>
+cudaError_t launch_all(const CUtensorMap &map, const Args &a, const Plan &p, cudaStream_t s)
+{
+    cudaError_t err = launch(wgrad_kernel<CG, G>, CG, dim3(p.workers * CG), THREADS, SMEM, s, map, a);
+    if (err == cudaSuccess && p.cut)
+        err = launch(join_kernel<CG, G>, 1, dim3(p.tiles_m * p.tiles_n * CG, CG * MAX_H / 32), 256, 0, s, a);
+    return err;
+}
+
+}  // namespace
+
+extern "C" uint64_t deco_weight_grad8_workspace(const void *dy, int32_t dtype, uint64_t rows, uint32_t out,
+                                                uint64_t dy_stride, uint32_t cols, int32_t bias, int32_t grad_dtype)
+{
+    if (rows == 0 || rows >= MAX_ROWS || out == 0 || out > MAX_COLS || cols == 0 || cols > MAX_COLS) return 0;
+    return make_plan(dy, dtype, rows, out, dy_stride, cols, bias != 0, grad_dtype).bytes();
+}
+
+extern "C" deco_status deco_weight_grad8(const void *dy, int32_t dtype, uint64_t rows, uint32_t out, uint64_t dy_stride,
+                                         const int8_t *codes, const uint8_t *exponents, uint32_t cols, void *dw, void *db,
+                                         int32_t grad_dtype, int32_t transposed, int32_t accumulate, void *workspace,
+                                         uint64_t workspace_bytes, void *stream)
+{
+    if (!is_dtype(dtype) || !is_dtype(grad_dtype) || rows >= MAX_ROWS || out == 0 || out > MAX_COLS || cols == 0 ||
+        cols > MAX_COLS)
+        return DECO_ERR_INVALID_ARG;
+    const uint32_t gsize = grad_dtype == DECO_F32 ? 4 : 2;
+    if (!dw || !aligned_to(dw, gsize) || !aligned_to(db, gsize)) return DECO_ERR_INVALID_ARG;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (rows == 0) {                                             // sums of nothing
+        if (accumulate) return DECO_OK;
+        if (cudaMemsetAsync(dw, 0, static_cast<uint64_t>(out) * cols * gsize, s) != cudaSuccess ||
+            (db && cudaMemsetAsync(db, 0, static_cast<uint64_t>(out) * gsize, s) != cudaSuccess)) {
+            cudaGetLastError();
+            return DECO_ERR_CUDA;
+        }
+        return DECO_OK;
+    }
+    if (!dy || !aligned_to(dy, dtype == DECO_F32 ? 4 : 2) || dy_stride < out || dy_stride > MAX_STRIDE) return DECO_ERR_INVALID_ARG;
+    if (!codes || !exponents || !aligned_to(codes, 16)) return DECO_ERR_INVALID_ARG;
+    const Plan p = make_plan(dy, dtype, rows, out, dy_stride, cols, db != nullptr, grad_dtype);
+    if (static_cast<uint64_t>(p.tiles_m) * p.tiles_n * p.cg > 0x7FFFFFFFull || static_cast<uint64_t>(p.planes) * p.plane_rows > 0x7FFFFFFFull)
+        return DECO_ERR_INVALID_ARG;
+    if (p.bytes()) {
+        if (!workspace || !aligned_to(workspace, 16)) return DECO_ERR_INVALID_ARG;
+        if (workspace_bytes < p.bytes()) return DECO_ERR_CAPACITY;
+    }
+    static const EncodeFn encode = encode_function();
+    if (!encode || !allow_shared_memory()) return DECO_ERR_CUDA;
+    const void *operand = p.planes ? workspace : dy;
+    const cuuint64_t dims[2] = {out, p.planes ? static_cast<cuuint64_t>(p.planes) * p.plane_rows : rows};
+    const cuuint64_t strides[1] = {2 * (p.planes ? p.pitch : dy_stride)};
+    const cuuint32_t box[2] = {64, BK}, step[2] = {1, 1};
+    CUtensorMap map;
+    if (encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(operand), dims, strides, box, step,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return DECO_ERR_CUDA;
+    Args a = {};
+    a.codes = codes;
+    a.exps = exponents;
+    a.rows = static_cast<uint32_t>(rows);
+    a.blocks8 = (cols + BLOCK8 - 1) / BLOCK8;
+    a.out = out;
+    a.cols = cols;
+    a.h = p.h;
+    a.tiles_n = p.tiles_n;
+    a.k_blocks = p.k_blocks;
+    a.planes = std::max<uint32_t>(1, p.planes);
+    a.plane_rows = p.plane_rows;
+    a.chunk = grad_dtype == DECO_F32 ? CHUNK : p.k_blocks;       // (bf16 rounds by 2^-9: sums may be cut off)
+    a.units = p.units;
+    a.workers = p.workers;
+    a.dw = dw;
+    a.db = db;
+    a.transposed = transposed != 0;
+    a.accumulate = accumulate != 0;
+    a.slots = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + p.plane_bytes());
+    if (p.planes) {
+        const dim3 grid((p.pitch + 2047) / 2048, std::min<uint32_t>(p.plane_rows, 8 * SMS));
+        __nv_bfloat16 *to = static_cast<__nv_bfloat16 *>(workspace);
+        if (dtype == DECO_F32)
+            planes_kernel<float><<<grid, 256, 0, s>>>(static_cast<const float *>(dy), dy_stride, a.rows, out, p.pitch, p.planes,
+                                                      p.plane_rows, to);
+        else
+            planes_kernel<__nv_bfloat16><<<grid, 256, 0, s>>>(static_cast<const __nv_bfloat16 *>(dy), dy_stride, a.rows, out, p.pitch,
+                                                              p.planes, p.plane_rows, to);
+        if (cudaGetLastError() != cudaSuccess) return DECO_ERR_CUDA;
+    }
+    const bool f32 = grad_dtype == DECO_F32;
+    const cudaError_t err = p.cg == 2 ? (f32 ? launch_all<2, float>(map, a, p, s) : launch_all<2, __nv_bfloat16>(map, a, p, s))
+                                      : (f32 ? launch_all<1, float>(map, a, p, s) : launch_all<1, __nv_bfloat16>(map, a, p, s));
+    return err == cudaSuccess ? DECO_OK : DECO_ERR_CUDA;
+}
