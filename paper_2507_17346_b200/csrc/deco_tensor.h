@@ -49,25 +49,60 @@ __device__ __forceinline__ bool bar_try(uint64_t *b, uint32_t parity)
                  : "=r"(ok) : "r"(smem_addr(b)), "r"(parity) : "memory");
     return ok != 0;
 }
+constexpr long long WAIT_LIMIT = 4000000000ll;                   // clock cycles: about 2 s
+
 // Bounded wait: false once the limit has passed or another role has given up; the first to give
-// up leaves DECO_ERR_TIMEOUT in the status word, if there is one.
+// up leaves DECO_ERR_TIMEOUT in the status word.
 static __device__ __noinline__ bool bar_wait_slow(uint64_t *b, uint32_t parity, volatile uint32_t *abort, uint32_t *status)
 {
-    constexpr long long LIMIT = 4000000000ll;                    // clock cycles: about 2 s
     const long long t0 = clock64();
     while (!bar_try(b, parity)) {
         if (*abort) return false;
-        if (clock64() - t0 > LIMIT) {
+        if (clock64() - t0 > WAIT_LIMIT) {
             *abort = 1;
-            if (status) atomicExch(status, static_cast<uint32_t>(DECO_ERR_TIMEOUT));
+            atomicExch(status, static_cast<uint32_t>(DECO_ERR_TIMEOUT));
             return false;
         }
     }
     return true;
 }
-__device__ __forceinline__ bool bar_wait(uint64_t *b, uint32_t parity, volatile uint32_t *abort, uint32_t *status = nullptr)
+__device__ __forceinline__ bool bar_wait(uint64_t *b, uint32_t parity, volatile uint32_t *abort, uint32_t *status)
 {
     return bar_try(b, parity) || bar_wait_slow(b, parity, abort, status);
+}
+// The same without a call, for kernels whose warps have different numbers of registers, and for what was written in this CTA's
+// own shared memory or by the asynchronous engines: the scope of the cluster costs each wait 100 cycles.
+__device__ __forceinline__ bool bar_try_cta(uint64_t *b, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\t"
+                 "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                 "selp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(smem_addr(b)), "r"(parity) : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ bool bar_wait_cta(uint64_t *b, uint32_t parity, volatile uint32_t *abort)
+{
+    if (bar_try_cta(b, parity)) return true;
+    const long long t0 = clock64();
+    while (!bar_try_cta(b, parity)) {
+        if (*abort) return false;
+        if (clock64() - t0 > WAIT_LIMIT) {
+            *abort = 1;
+            return false;
+        }
+    }
+    return true;
+}
+// Arrive at the barrier of the pair's first CTA, where what was written before stays in this CTA's own shared memory, for
+// the tensor cores (behind a proxy fence): a release at the cluster's scope would wait 1500 cycles for all the thread's stores.
+template <int CG>
+__device__ __forceinline__ void bar_arrive_leader_cta(uint64_t *b)
+{
+    if (CG == 1)
+        bar_arrive(b);
+    else
+        asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" :: "r"(leader_addr(smem_addr(b))) : "memory");
 }
 
 // Box at (x, y) into this CTA's shared memory; its bytes are counted by the barrier at `bar`, which
@@ -146,6 +181,15 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&v)[32])
                    "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]),
                    "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]),
                    "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+                 : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_load16(uint32_t addr, uint32_t (&v)[16])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+                 "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+                   "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
                  : "r"(addr));
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }

@@ -1,9 +1,9 @@
 // deco_weight_grad8: the weight gradient of a linear layer whose input was put away in 8 bits,
 //     dW[o][i] = sum_t dY[t][o] X[t][i],   db[o] = sum_t dY[t][o],
 // on the tensor cores.  X's entries, 8-bit integers times a power of two, are bf16 numbers, so the products are exact and
-// X is never written out: eight warps read codes (a byte an entry), make bf16 of them (five instructions for two) and
-// put them into shared memory as the operand, while dY comes by box copies.  Both operands have their outer
-// dimension consecutive, 128-byte swizzle.
+// X is never written out: box copies bring codes (a byte an entry) into shared memory, eight warps make bf16 of them
+// (five instructions for two) and put them in the place of the operand, while dY comes as it is.  Both operands have
+// their outer dimension consecutive, 128-byte swizzle.
 //
 // fp32 dY is taken as the sum of bf16 numbers, hi + mid + lo (24 bits; hi + mid where the result is bf16), split by a
 // launch before; the same launch lays out bf16 rows that do not start on 16 bytes.
@@ -13,7 +13,7 @@
 //
 // Sums.  The tensor cores' fp32 sums are cut off, not rounded: over 8192 products the result is 9e-6 off (in the 2-norm), over
 // 512 5e-7.  So, where the result is fp32, the accumulators are emptied every CHUNK blocks of 64 tokens into
-// registers of the converting warps, where sums are rounded; the two accumulators take turns, and the products go on.
+// registers, where sums are rounded; the two accumulators take turns, and the products go on.
 // lo's and mid's products of a chunk come before hi's, while the sum is still small.
 //
 // Shares.  The blocks of all tiles in a row, cut into equal ranges, one per CTA: a CTA begins and ends inside tiles.  Parts
@@ -36,26 +36,30 @@ using namespace deco::tensor;
 using deco::BLOCK8;
 
 constexpr int BK = 64;                   // tokens per stage
-constexpr int STAGES = 6;
+constexpr int STAGES = 5;                // of operands, and of codes and steps on their way to being converted
 constexpr uint32_t TILE_M = 128;         // of dY's columns, a CTA's
 constexpr uint32_t MAX_H = 128;          // of X's columns, a CTA's, with those of ones
 constexpr uint32_t ONES = 16;            // columns of ones, a CTA's
 constexpr uint32_t SLAB = BK * 128;      // 64 columns of an operand
 constexpr uint32_t OPERAND = 2 * SLAB, STAGE_BYTES = 2 * OPERAND;
-constexpr int WORK_WARPS = 8;            // convert, and empty the accumulators
-constexpr int WORK_THREADS = 32 * WORK_WARPS;
-constexpr int THREADS = WORK_THREADS + 64;       // and one warp that loads, one that multiplies
-constexpr uint32_t STAGING_FLOATS = 32 * 33;     // of a warp
-constexpr size_t SMEM = STAGES * STAGE_BYTES + WORK_WARPS * STAGING_FLOATS * 4 + 1024;
+constexpr uint32_t RAW_BYTES = BK * MAX_H + BK * 16;     // codes; per token eight steps of 16 columns each, in bf16
+// Warps: eight empty the accumulators; eight convert, two a block; one loads dY, one multiplies, two load X.
+constexpr int SUM_WARPS = 8, CONVERT_WARPS = 8, TEAM_WARPS = 2, TEAMS = CONVERT_WARPS / TEAM_WARPS;
+constexpr uint32_t FIRST_CONVERT = SUM_WARPS, LOAD = FIRST_CONVERT + CONVERT_WARPS, MULTIPLY = LOAD + 1, FIRST_X = LOAD + 2;
+constexpr int THREADS = 32 * (SUM_WARPS + CONVERT_WARPS + 4);
+// Registers: a launch gives 640 threads 96 each (61440).  256 threads hold 128 sums each, the others need few:
+// 256 * 168 + 256 * 48 + 128 * 48 = 61440.
+constexpr int SUM_REGISTERS = 168, CONVERT_REGISTERS = 48, OTHER_REGISTERS = 48;
+constexpr uint32_t STAGING_COLS = 16, STAGING_FLOATS = 32 * (STAGING_COLS + 1);      // of a warp
+constexpr size_t SMEM = STAGES * (STAGE_BYTES + RAW_BYTES) + SUM_WARPS * STAGING_FLOATS * 4 + 1024;
 constexpr uint32_t CHUNK = 8;            // blocks an accumulator takes before it is emptied
 constexpr uint32_t SMS = 148;
 constexpr uint32_t MIN_BLOCKS = 8;       // a CTA's share, if tiles have to be cut for it
-constexpr int UNITS = BK * MAX_H / 8 / WORK_THREADS;     // 8-code units of a thread per block
+constexpr int UNITS = BK * MAX_H / 16 / (32 * TEAM_WARPS);       // 16-code units of a converting thread per block
 
 // A tile is CG * 128 columns of dY by CG * h of X, h a multiple of 16.  A CTA (of a pair) makes the operand of h of the
 // product's columns and, in tiles that sum db too, of 16 of ones behind them.
 struct Args {
-    const int8_t *codes;
     const uint8_t *exps;
     uint32_t rows, blocks8;              // tokens, blocks of a row of X
     uint32_t out, cols;
@@ -69,7 +73,7 @@ struct Args {
 };
 
 struct __align__(8) Control {
-    uint64_t full[STAGES], empty[STAGES], acc_full[2], acc_empty[2];
+    uint64_t full[STAGES], empty[STAGES], raw_full[STAGES], raw_empty[STAGES], acc_full[2], acc_empty[2];
     uint32_t tmem;
     volatile uint32_t abort;
 };
@@ -107,12 +111,12 @@ struct Cursor {
             segment(g, static_cast<uint64_t>(tile) * g.k_blocks + last, g.units * (worker + 1) / g.workers);
         }
     }
-    // of the chunk: where its sums begin and end
-    enum : uint32_t { BEGINS = 1, ENDS = 2, FROM_TOP = 4, WHOLE = 8 };
-    __device__ uint32_t flags(const Args &g) const
+    // to the first block of the next chunk
+    __device__ void next_chunk(const Args &g, uint32_t worker)
     {
-        return (c0 == first ? BEGINS : 0u) | (c1 == last ? ENDS : 0u) | (first == 0 ? FROM_TOP : 0u) |
-               (last - first == g.k_blocks ? WHOLE : 0u);
+        k = c1 - 1;
+        plane = 0;
+        advance(g, worker);
     }
 };
 
@@ -141,22 +145,27 @@ template <typename G> __device__ __forceinline__ void store_grad(void *base, uin
     put_grad(p, accumulate ? grad_at<G>(p) + v : v);
 }
 
-// Eight codes times 2^(exp - 127) as bf16.  A code's low seven bits in the place of a bf16 fraction with the exponent of
+// Eight codes times their step (bf16, twice) as bf16.  A code's low seven bits in the place of a bf16 fraction with the exponent of
 // 128 are 128 + those bits; its sign bit in the place of the lowest exponent bit makes 256 of 128: the
 // difference is the code, exactly.
-__device__ __forceinline__ uint4 converted(uint2 codes, uint32_t exp)
+__device__ __forceinline__ uint4 converted(uint32_t c0, uint32_t c1, uint32_t step)
 {
-    const uint32_t one = exp == 255u ? 0x7FC0u : exp << 7, scale = one | one << 16;
     uint32_t o[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const uint32_t p = __byte_perm(i < 2 ? codes.x : codes.y, 0, i & 1 ? 0x4342 : 0x4140);
+        const uint32_t p = __byte_perm(i < 2 ? c0 : c1, 0, i & 1 ? 0x4342 : 0x4140);
         const uint32_t a = (p & 0x007F007Fu) | 0x43004300u, b = (p & 0x00800080u) | 0x43004300u;
         uint32_t d;
         asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-        asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(o[i]) : "r"(d), "r"(scale));
+        asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(o[i]) : "r"(d), "r"(step));
     }
     return make_uint4(o[0], o[1], o[2], o[3]);
+}
+__device__ __forceinline__ uint32_t lds2(uint32_t a)
+{
+    uint16_t v;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a) : "memory");
+    return v;
 }
 
 // Where the 8 columns from 8 c on of token k lie in an operand's stage.
@@ -167,7 +176,7 @@ __device__ __forceinline__ uint32_t unit_offset(uint32_t k, uint32_t c)
 
 template <int CG, typename G>
 __global__ void __launch_bounds__(THREADS, 1)
-wgrad_kernel(const __grid_constant__ CUtensorMap map, const Args g)
+wgrad_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap code_map, const Args g)
 {
     constexpr uint32_t GROUPS = 2 * CG;          // of 32 columns of the product, a warp's
     constexpr uint32_t SIDE = GROUPS * 32;
@@ -179,17 +188,19 @@ wgrad_kernel(const __grid_constant__ CUtensorMap map, const Args g)
     if (CG == 2) asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
-            bar_init(&ctl.full[s], 1 + CG * WORK_WARPS);
+            bar_init(&ctl.full[s], 1 + CG * TEAM_WARPS);
             bar_init(&ctl.empty[s], 1);
+            bar_init(&ctl.raw_full[s], 3);
+            bar_init(&ctl.raw_empty[s], TEAM_WARPS);
         }
         for (int s = 0; s < 2; ++s) {
             bar_init(&ctl.acc_full[s], 1);
-            bar_init(&ctl.acc_empty[s], CG * WORK_WARPS);
+            bar_init(&ctl.acc_empty[s], CG * SUM_WARPS);
         }
         ctl.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (wid == WORK_WARPS + 1) tmem_alloc<CG>(&ctl.tmem, 512);
+    if (wid == MULTIPLY) tmem_alloc<CG>(&ctl.tmem, 512);
     if (g.db && threadIdx.x < BK)                                // the columns of ones, which nothing overwrites
         for (int s = 0; s < STAGES; ++s)
             for (uint32_t c = 0; c < ONES / 8; ++c)
@@ -203,16 +214,17 @@ wgrad_kernel(const __grid_constant__ CUtensorMap map, const Args g)
         asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
     }
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    const uint32_t tmem = ctl.tmem;
+    const uint32_t tmem = ctl.tmem, raws = stages + STAGES * STAGE_BYTES;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
-    if (wid == WORK_WARPS) {
-        if (lane == 0) {
+    if (wid >= LOAD) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(OTHER_REGISTERS));
+        if (wid == LOAD && lane == 0) {
             uint32_t s = 0, parity = 1;
             const uint32_t full0 = smem_addr(ctl.full), bar0 = CG == 1 ? full0 : leader_addr(full0);
             for (Cursor cur(g, worker); !cur.done; cur.advance(g, worker)) {
-                if (!bar_wait(&ctl.empty[s], parity, &ctl.abort)) break;
+                if (!bar_wait_cta(&ctl.empty[s], parity, &ctl.abort)) break;
                 const uint32_t st = stages + s * STAGE_BYTES, bar = bar0 + s * 8;
                 const int32_t x = ((cur.tile / g.tiles_n) * CG + rank) * TILE_M, y = cur.plane * g.plane_rows + cur.k * BK;
                 if (rank == 0) bar_expect(&ctl.full[s], CG * OPERAND);
@@ -228,19 +240,20 @@ wgrad_kernel(const __grid_constant__ CUtensorMap map, const Args g)
                 while (clock64() - t0 < 20000000ll) {}
             }
         }
-    } else if (wid == WORK_WARPS + 1) {
-        if (lane == 0 && rank == 0) {
-            uint32_t s = 0, parity = 0, n = 0;
+        if (wid == MULTIPLY && lane == 0 && rank == 0) {
+            uint32_t s = 0, parity = 0, n = 0, idesc = 0;
             bool first = true;                                   // block of a chunk
             for (Cursor cur(g, worker); !cur.done; cur.advance(g, worker)) {
                 const uint32_t as = n & 1;
-                if (first && !bar_wait(&ctl.acc_empty[as], ((n >> 1) & 1) ^ 1, &ctl.abort)) break;
-                if (!bar_wait(&ctl.full[s], parity, &ctl.abort)) break;
+                if (first) {
+                    const Columns<CG> c(g, cur.tile % g.tiles_n);
+                    // bf16 operands, fp32 sums, outer dimensions consecutive, N and M
+                    idesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((c.width >> 3) << 17) |
+                            ((CG * TILE_M >> 4) << 24);
+                    if (!bar_wait_cta(&ctl.acc_empty[as], ((n >> 1) & 1) ^ 1, &ctl.abort)) break;
+                }
+                if (!bar_wait_cta(&ctl.full[s], parity, &ctl.abort)) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const Columns<CG> c(g, cur.tile % g.tiles_n);
-                // bf16 operands, fp32 sums, outer dimensions consecutive, N and M
-                const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) |
-                                       ((c.width >> 3) << 17) | ((CG * TILE_M >> 4) << 24);
                 const uint64_t da = operand_desc(stages + s * STAGE_BYTES, true);
                 const uint64_t db = operand_desc(stages + s * STAGE_BYTES + OPERAND, true);
 #pragma unroll
@@ -258,151 +271,175 @@ wgrad_kernel(const __grid_constant__ CUtensorMap map, const Args g)
                 }
             }
         }
-    } else {
-        const uint32_t quad = wid & 3, side = wid >> 2;          // lanes of the tensor memory, half of the columns
-        float *staging = reinterpret_cast<float *>(raw + (stages - smem_addr(raw)) + STAGES * STAGE_BYTES) + wid * STAGING_FLOATS;
-        const uint32_t pitch = g.blocks8 * BLOCK8;
-        // this thread's units of a block: token * 16 + unit of the row (BK * 16: none)
-        uint32_t unit[UNITS];
+        if (wid >= FIRST_X) {
+            // Codes by box copy; steps by plain loads, a token a lane and turn, the next ones on their way while these are
+            // stored.  The two warps take a half of each block's tokens.
+            const uint32_t token = (wid - FIRST_X) * 32 + lane;
+            uint32_t s = 0, parity = 1;
+            Cursor cur(g, worker);
+            uint32_t e[5], col0 = 0;
+            auto fetch = [&]() {
+                col0 = ((cur.tile % g.tiles_n) * CG + rank) * g.h;
+                const uint32_t t = cur.k * BK + token, b = col0 / BLOCK8;
+                const uint8_t *p = g.exps + static_cast<uint64_t>(t) * g.blocks8 + b;
+#pragma unroll
+                for (uint32_t j = 0; j < 5; ++j) {
+                    e[j] = 0;
+                    if (t < g.rows && b + j < g.blocks8) e[j] = __ldg(p + j);
+                }
+            };
+            if (!cur.done) fetch();
+            while (!cur.done) {
+                const uint32_t to = raws + s * RAW_BYTES;
+                if (!bar_wait_cta(&ctl.raw_empty[s], parity, &ctl.abort)) break;
+                if (wid == FIRST_X && lane == 0) {
+                    bar_expect(&ctl.raw_full[s], BK * g.h);
+                    load_box<1>(to, &code_map, col0, cur.k * BK, smem_addr(&ctl.raw_full[s]));
+                }
+                // a tile begins at a block of 32 columns or in its middle
+                const bool middle = col0 & 16;
+                uint32_t w[4];
+#pragma unroll
+                for (uint32_t j = 0; j < 5; ++j) e[j] = e[j] == 255u ? 0x7FC0u : e[j] << 7;
+#pragma unroll
+                for (uint32_t u = 0; u < 4; ++u) w[u] = e[u] | (middle ? e[u + 1] : e[u]) << 16;
+                cur.advance(g, worker);
+                if (!cur.done) fetch();
+                sts16(to + BK * MAX_H + token * 16, make_uint4(w[0], w[1], w[2], w[3]));
+                __syncwarp();
+                if (lane == 0) bar_arrive(&ctl.raw_full[s]);
+                if (++s == STAGES) {
+                    s = 0;
+                    parity ^= 1;
+                }
+            }
+        }
+    } else if (wid >= FIRST_CONVERT) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(CONVERT_REGISTERS));
+        // A team of two warps converts every fourth block.  This thread's units: where the step lies, and the two places
+        // of the bf16 numbers.  Lanes next to each other take units next to each other, and those of the second 64
+        // columns their second half first: no bank conflicts.
+        const uint32_t team = (wid - FIRST_CONVERT) / TEAM_WARPS, me = ((wid - FIRST_CONVERT) % TEAM_WARPS) * 32 + lane;
+        const uint32_t per_row = g.h / 16, count = BK * per_row;
+        uint32_t step_to[UNITS];                                 // bits 0 to 13: place; 16 to 25: step; 31: second half first
 #pragma unroll
         for (int i = 0; i < UNITS; ++i) {
-            const uint32_t id = i * WORK_THREADS + threadIdx.x, per_row = g.h / 8, token = id / per_row;
-            unit[i] = token < BK ? token * 16 + id - token * per_row : BK * 16;
+            const uint32_t id = i * 32 * TEAM_WARPS + me, token = id / per_row, c = id - token * per_row, swap = (c >> 2) & 1;
+            step_to[i] = id < count ? unit_offset(token, 2 * c + swap) | (token * 16 + c * 2) << 16 | swap << 31 : 0;
         }
-        uint2 code[UNITS];
-        uint32_t exp[UNITS];
-        Cursor ahead(g, worker);                                 // the block that is being read
-        auto fetch = [&](int i) {
-            const uint32_t col = ((ahead.tile % g.tiles_n) * CG + rank) * g.h + (unit[i] & 15) * 8, t = ahead.k * BK + (unit[i] >> 4);
-            code[i] = make_uint2(0, 0);
-            exp[i] = 0;
-            if (unit[i] < BK * 16 && t < g.rows && col < pitch) {
-                code[i] = __ldg(reinterpret_cast<const uint2 *>(g.codes + static_cast<uint64_t>(t) * pitch + col));
-                exp[i] = __ldg(g.exps + static_cast<uint64_t>(t) * g.blocks8 + col / BLOCK8);
-            }
-        };
-        float sum[GROUPS][32];                                   // this warp's half of the columns, a row a thread
-        uint32_t s = 0, parity = 1, emptied = 0, staged = 0;
-        bool dead = false, pending = false, ended = false;
-        uint32_t end_tile = 0, end_flags = 0, full_tile = 0, full_flags = 0;     // chunk just staged; chunk to be emptied
-        bool have = !ahead.done;                                 // a block is in the registers
-        uint32_t now_tile = 0, now_flags = 0;
-        bool now_ends = false;
-        auto read_next = [&]() {
-            now_tile = ahead.tile;
-            now_flags = ahead.flags(g);
-            now_ends = ahead.chunk_ends();
-        };
-        if (have) {
-#pragma unroll
-            for (int i = 0; i < UNITS; ++i) fetch(i);
-            read_next();
-            ahead.advance(g, worker);
-        }
-        // Block after block is converted; a chunk is emptied when STAGES blocks of the next are staged: then its products are
-        // done, and the tensor cores have work while this goes on.
-#pragma unroll 1
-        while (true) {
-            if (pending && (ended || !have || staged == STAGES)) {
-                pending = false;
-                const uint32_t as = emptied & 1;
-                if (!dead) dead = !bar_wait(&ctl.acc_full[as], (emptied >> 1) & 1, &ctl.abort);
-                dead = __any_sync(0xFFFFFFFFu, dead);
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t nt = full_tile % g.tiles_n, mt = (full_tile / g.tiles_n) * CG + rank;
-                const Columns<CG> c(g, nt);
-                const bool begins = full_flags & Cursor::BEGINS;
-#pragma unroll
-                for (uint32_t h = 0; h < GROUPS; ++h) {
-                    if (side * SIDE + h * 32 >= c.width) continue;
-                    uint32_t v[32];
-                    __syncwarp();
-                    tmem_load32(tmem + ((quad * 32) << 16) + as * 256 + side * SIDE + h * 32, v);
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) sum[h][j] = begins ? __uint_as_float(v[j]) : sum[h][j] + __uint_as_float(v[j]);
-                    if (dead) {                                  // a wait has run out: what comes is no sum
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) sum[h][j] = __uint_as_float(0x7FC00000u);
-                    }
-                }
-                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) bar_arrive_leader<CG>(&ctl.acc_empty[as]);
-                emptied += 1;
-                if (full_flags & Cursor::ENDS) {                 // of a segment: its sums go out
-                    const uint32_t o = mt * TILE_M + quad * 32 + lane, col0 = nt * CG * g.h;
-                    float *slot = g.slots + ((worker * 2ull + (full_flags & Cursor::FROM_TOP ? 1 : 0)) * CG + rank) * (CG * MAX_H * TILE_M) +
-                                  quad * 32 + lane;
-#pragma unroll
-                    for (uint32_t h = 0; h < GROUPS; ++h) {
-                        const uint32_t n0 = side * SIDE + h * 32;
-                        if (n0 >= c.width) continue;
-                        if (!(full_flags & Cursor::WHOLE)) {
-#pragma unroll
-                            for (uint32_t j = 0; j < 32; ++j)
-                                if (n0 + j < c.width) __stcg(slot + (n0 + j) * TILE_M, sum[h][j]);
-                            continue;
-                        }
-                        if (g.transposed) {
-#pragma unroll
-                            for (uint32_t j = 0; j < 32; ++j)
-                                if (c.in(n0 + j) && col0 + c.col(n0 + j) < g.cols && o < g.out)
-                                    store_grad<G>(g.dw, static_cast<uint64_t>(col0 + c.col(n0 + j)) * g.out + o, sum[h][j], g.accumulate);
-                        } else {
-                            const uint32_t col = col0 + c.col(n0 + lane);
-                            const bool in = c.in(n0 + lane) && col < g.cols;
-                            __syncwarp();
-#pragma unroll
-                            for (uint32_t j = 0; j < 32; ++j) staging[lane * 33 + j] = sum[h][j];
-                            __syncwarp();
-#pragma unroll 4
-                            for (uint32_t r = 0; r < 32; ++r) {
-                                const uint32_t row = mt * TILE_M + quad * 32 + r;
-                                if (in && row < g.out)
-                                    store_grad<G>(g.dw, static_cast<uint64_t>(row) * g.cols + col, staging[r * 33 + lane], g.accumulate);
-                            }
-                        }
-                        if (c.ones && n0 <= c.h && c.h < n0 + 32 && o < g.out)               // the first column of ones
-                            store_grad<G>(g.db, o, c.h & 16 ? sum[h][16] : sum[h][0], g.accumulate);
-                    }
-                }
-            }
-            if (ended) {
-                ended = false;
-                pending = true;
-                staged = 0;
-                full_tile = end_tile;
-                full_flags = end_flags;
-                if (!have) continue;
-            }
-            if (!have) break;
-            if (!dead) dead = !bar_wait(&ctl.empty[s], parity, &ctl.abort);
-            dead = __any_sync(0xFFFFFFFFu, dead);
+        const uint64_t u0 = g.units * worker / g.workers, u1 = g.units * (worker + 1) / g.workers;
+        const uint64_t blocks = (u1 - u0) * g.planes;
+        uint32_t s = team % STAGES, parity = 0;                  // (TEAMS < STAGES)
+        for (uint64_t n = team; n < blocks; n += TEAMS) {
+            const uint32_t from = raws + s * RAW_BYTES + me * 16, steps = raws + s * RAW_BYTES + BK * MAX_H;
             const uint32_t base = stages + s * STAGE_BYTES + OPERAND;
-            const bool more = !ahead.done;
+            bool ok = bar_wait_cta(&ctl.raw_full[s], parity, &ctl.abort);
+            ok = ok && bar_wait_cta(&ctl.empty[s], parity ^ 1, &ctl.abort);
+            if (!__all_sync(0xFFFFFFFFu, ok)) break;
 #pragma unroll
             for (int i = 0; i < UNITS; ++i) {
-                const uint4 o = converted(code[i], exp[i]);
-                if (more) fetch(i);
-                if (unit[i] < BK * 16 && !dead) sts16(base + unit_offset(unit[i] >> 4, unit[i] & 15), o);
+                if (i * 32 * TEAM_WARPS + me >= count) continue;
+                const uint4 code = lds16(from + i * 512 * TEAM_WARPS);
+                const uint32_t step = lds2(steps + ((step_to[i] >> 16) & 0x3FFu)) * 0x10001u;
+                const uint4 a = converted(code.x, code.y, step), b = converted(code.z, code.w, step);
+                const bool swap = step_to[i] >> 31;
+                const uint32_t to = base + (step_to[i] & 0x3FFFu);
+                sts16(to, swap ? b : a);
+                sts16(to ^ 16, swap ? a : b);
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            if (lane == 0) bar_arrive_leader<CG>(&ctl.full[s]);
-            if (++s == STAGES) {
-                s = 0;
+            if (lane == 0) {
+                bar_arrive(&ctl.raw_empty[s]);
+                bar_arrive_leader_cta<CG>(&ctl.full[s]);
+            }
+            s += TEAMS;
+            if (s >= STAGES) {
+                s -= STAGES;
                 parity ^= 1;
             }
-            staged += 1;
-            if (now_ends) {
-                ended = true;
-                end_tile = now_tile;
-                end_flags = now_flags;
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(SUM_REGISTERS));
+        const uint32_t quad = wid & 3, side = wid >> 2;          // lanes of the tensor memory, half of the columns
+        float *staging = reinterpret_cast<float *>(raw + (raws - smem_addr(raw)) + STAGES * RAW_BYTES) + wid * STAGING_FLOATS;
+        float sum[GROUPS][32];                                   // this warp's half of the columns, a row a thread
+        uint32_t n = 0;
+        bool dead = false;                                       // a wait has run out: NaN from here on
+        for (Cursor cur(g, worker); !cur.done; cur.next_chunk(g, worker)) {
+            const uint32_t as = n & 1;
+            if (cur.c0 == cur.first) {
+#pragma unroll
+                for (uint32_t h = 0; h < GROUPS; ++h)
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) sum[h][j] = 0.f;
             }
-            have = more;
-            if (more) {
-                read_next();
-                ahead.advance(g, worker);
+            if (!dead) dead = !bar_wait_cta(&ctl.acc_full[as], (n >> 1) & 1, &ctl.abort);
+            dead = __any_sync(0xFFFFFFFFu, dead);
+            n += 1;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t nt = cur.tile % g.tiles_n;
+            const Columns<CG> c(g, nt);
+#pragma unroll
+            for (uint32_t h = 0; h < GROUPS; ++h) {
+#pragma unroll
+                for (uint32_t p = 0; p < 32; p += 16) {
+                    if (side * SIDE + h * 32 + p >= c.width) continue;
+                    uint32_t v[16];
+                    __syncwarp();
+                    tmem_load16(tmem + ((quad * 32) << 16) + as * 256 + side * SIDE + h * 32 + p, v);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sum[h][p + j] += __uint_as_float(v[j]);
+                }
+            }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) bar_arrive_leader_cta<CG>(&ctl.acc_empty[as]);
+            if (cur.c1 != cur.last) continue;
+            // the segment's last chunk: its sums go out
+            const bool whole = cur.last - cur.first == g.k_blocks;
+            const uint32_t mt = (cur.tile / g.tiles_n) * CG + rank, o = mt * TILE_M + quad * 32 + lane, col0 = nt * CG * g.h;
+            float *slot = g.slots + ((worker * 2ull + (cur.first == 0)) * CG + rank) * (CG * MAX_H * TILE_M) + quad * 32 + lane;
+#pragma unroll
+            for (uint32_t h = 0; h < GROUPS; ++h) {
+                const uint32_t n0 = side * SIDE + h * 32;
+                if (n0 >= c.width) continue;
+                if (dead) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) sum[h][j] = __uint_as_float(0x7FC00000u);
+                }
+                if (!whole) {
+#pragma unroll
+                    for (uint32_t j = 0; j < 32; ++j)
+                        if (n0 + j < c.width) __stcg(slot + (n0 + j) * TILE_M, sum[h][j]);
+                    continue;
+                }
+                if (g.transposed) {
+#pragma unroll
+                    for (uint32_t j = 0; j < 32; ++j)
+                        if (c.in(n0 + j) && col0 + c.col(n0 + j) < g.cols && o < g.out)
+                            store_grad<G>(g.dw, static_cast<uint64_t>(col0 + c.col(n0 + j)) * g.out + o, sum[h][j], g.accumulate);
+                } else {
+                    // sixteen columns at a time, so that half a warp writes consecutive entries of a row
+#pragma unroll
+                    for (uint32_t p = 0; p < 32; p += STAGING_COLS) {
+                        const uint32_t at = n0 + p + (lane & (STAGING_COLS - 1)), col = col0 + c.col(at);
+                        const bool in = c.in(at) && col < g.cols;
+                        __syncwarp();
+#pragma unroll
+                        for (uint32_t j = 0; j < STAGING_COLS; ++j) staging[lane * (STAGING_COLS + 1) + j] = sum[h][p + j];
+                        __syncwarp();
+#pragma unroll 4
+                        for (uint32_t q = lane / STAGING_COLS; q < 32; q += 32 / STAGING_COLS) {
+                            const uint32_t row = mt * TILE_M + quad * 32 + q;
+                            if (in && row < g.out)
+                                store_grad<G>(g.dw, static_cast<uint64_t>(row) * g.cols + col,
+                                              staging[q * (STAGING_COLS + 1) + (lane & (STAGING_COLS - 1))], g.accumulate);
+                        }
+                    }
+                }
+                if (c.ones && n0 <= c.h && c.h < n0 + 32 && o < g.out)               // the first column of ones
+                    store_grad<G>(g.db, o, c.h & 16 ? sum[h][16] : sum[h][0], g.accumulate);
             }
         }
     }
@@ -412,7 +449,7 @@ wgrad_kernel(const __grid_constant__ CUtensorMap map, const Args g)
         asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
         asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
     }
-    if (wid == WORK_WARPS + 1) {
+    if (wid == MULTIPLY) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         tmem_free<CG>(tmem, 512);
     }
@@ -544,6 +581,16 @@ Plan make_plan(const void *dy, int32_t dtype, uint64_t rows, uint32_t out, uint6
     return p;
 }
 
+// Boxes of `box_cols` columns and BK rows; outside of the matrix zeros are read.
+bool box_map(EncodeFn fn, CUtensorMap *map, CUtensorMapDataType type, const void *base, uint64_t cols, uint64_t rows,
+             uint64_t row_bytes, uint32_t box_cols, CUtensorMapSwizzle swizzle)
+{
+    const cuuint64_t dims[2] = {cols, rows}, strides[1] = {row_bytes};
+    const cuuint32_t box[2] = {box_cols, BK}, step[2] = {1, 1};
+    return fn(map, type, 2, const_cast<void *>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int CG, typename G>
 bool allow()
 {
@@ -586,9 +633,9 @@ cudaError_t launch(void (*kernel)(P...), uint32_t cluster, dim3 grid, unsigned b
 }
 
 template <int CG, typename G>
-cudaError_t launch_all(const CUtensorMap &map, const Args &a, const Plan &p, cudaStream_t s)
+cudaError_t launch_all(const CUtensorMap &map, const CUtensorMap &code_map, const Args &a, const Plan &p, cudaStream_t s)
 {
-    cudaError_t err = launch(wgrad_kernel<CG, G>, CG, dim3(p.workers * CG), THREADS, SMEM, s, map, a);
+    cudaError_t err = launch(wgrad_kernel<CG, G>, CG, dim3(p.workers * CG), THREADS, SMEM, s, map, code_map, a);
     if (err == cudaSuccess && p.cut)
         err = launch(join_kernel<CG, G>, 1, dim3(p.tiles_m * p.tiles_n * CG, CG * MAX_H / 32), 256, 0, s, a);
     return err;
@@ -635,16 +682,13 @@ extern "C" deco_status deco_weight_grad8(const void *dy, int32_t dtype, uint64_t
     static const EncodeFn encode = encode_function();
     if (!encode || !allow_shared_memory()) return DECO_ERR_CUDA;
     const void *operand = p.planes ? workspace : dy;
-    const cuuint64_t dims[2] = {out, p.planes ? static_cast<cuuint64_t>(p.planes) * p.plane_rows : rows};
-    const cuuint64_t strides[1] = {2 * (p.planes ? p.pitch : dy_stride)};
-    const cuuint32_t box[2] = {64, BK}, step[2] = {1, 1};
-    CUtensorMap map;
-    if (encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(operand), dims, strides, box, step,
-               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    const uint64_t pitch = (cols + BLOCK8 - 1) / BLOCK8 * static_cast<uint64_t>(BLOCK8);
+    CUtensorMap map, code_map;
+    if (!box_map(encode, &map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, operand, out, p.planes ? static_cast<uint64_t>(p.planes) * p.plane_rows : rows,
+                 2 * (p.planes ? p.pitch : dy_stride), 64, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !box_map(encode, &code_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, pitch, rows, pitch, p.h, CU_TENSOR_MAP_SWIZZLE_NONE))
         return DECO_ERR_CUDA;
     Args a = {};
-    a.codes = codes;
     a.exps = exponents;
     a.rows = static_cast<uint32_t>(rows);
     a.blocks8 = (cols + BLOCK8 - 1) / BLOCK8;
@@ -675,7 +719,7 @@ extern "C" deco_status deco_weight_grad8(const void *dy, int32_t dtype, uint64_t
         if (cudaGetLastError() != cudaSuccess) return DECO_ERR_CUDA;
     }
     const bool f32 = grad_dtype == DECO_F32;
-    const cudaError_t err = p.cg == 2 ? (f32 ? launch_all<2, float>(map, a, p, s) : launch_all<2, __nv_bfloat16>(map, a, p, s))
-                                      : (f32 ? launch_all<1, float>(map, a, p, s) : launch_all<1, __nv_bfloat16>(map, a, p, s));
+    const cudaError_t err = p.cg == 2 ? (f32 ? launch_all<2, float>(map, code_map, a, p, s) : launch_all<2, __nv_bfloat16>(map, code_map, a, p, s))
+                                      : (f32 ? launch_all<1, float>(map, code_map, a, p, s) : launch_all<1, __nv_bfloat16>(map, code_map, a, p, s));
     return err == cudaSuccess ? DECO_OK : DECO_ERR_CUDA;
 }
