@@ -163,7 +163,7 @@ SIGNATURES = {
                                    _u64, _vp, _vp, _i32, _i32, _vp, _u64, _vp]),
     "deco_pack8": (_i32, [_vp, _i32, _u64, _u32, _u64, _vp, _vp, _vp]),
     "deco_unpack8": (_i32, [_vp, _vp, _u64, _u32, _vp, _i32, _u64, _vp]),
-    "deco_weight_grad8_workspace": (_u64, [_vp, _i32, _u64, _u32, _u64, _u32, _i32, _i32]),
+    "deco_weight_grad8_workspace": (_u64, [_vp, _i32, _u64, _u32, _u64, _u32, _i32]),
     "deco_weight_grad8": (_i32, [_vp, _i32, _u64, _u32, _u64, _vp, _vp, _u32, _vp, _vp, _i32, _i32, _i32, _vp, _u64, _vp]),
     "deco_status_string": (ctypes.c_char_p, [_i32]),
 }
@@ -819,10 +819,10 @@ def deco_unpack8(packed, y, stream=None):
     _check(load().deco_unpack8(codes, exps, rows, cols, p, kind, stride, _stream_on(stream, dev)), w)
 
 
-def deco_weight_grad8_workspace(dy, cols, bias=True, grad_dtype=DECO_F32):
+def deco_weight_grad8_workspace(dy, cols, grad_dtype=DECO_F32):
     """Bytes of workspace that deco_weight_grad8 needs for this `dy` and an input of `cols` columns."""
     p, kind, rows, out, stride, _ = _rows_of(dy, "deco_weight_grad8_workspace", "dy")
-    return load().deco_weight_grad8_workspace(p, kind, rows, out, stride, cols, int(bool(bias)), grad_dtype)
+    return load().deco_weight_grad8_workspace(p, kind, rows, out, stride, cols, grad_dtype)
 
 
 def deco_weight_grad8(dy, packed, dw, db=None, transposed=False, accumulate=False, workspace=None, stream=None):
@@ -838,7 +838,7 @@ def deco_weight_grad8(dy, packed, dw, db=None, transposed=False, accumulate=Fals
     both = ("float32", "bfloat16")
     codes, exps = _packed(packed, w, dev, rows, cols)
     gkind = _grad_kind(w, dw, db)
-    need = load().deco_weight_grad8_workspace(p, kind, rows, out, stride, cols, int(db is not None), gkind)
+    need = load().deco_weight_grad8_workspace(p, kind, rows, out, stride, cols, gkind)
     room, wp, nbytes = _workspace(workspace, w, need, dev, stream)
     _check(load().deco_weight_grad8(
         p, kind, rows, out, stride, codes, exps, cols, _tensor(dw, w, "dw", dev, both), _tensor(db, w, "db", dev, both, (out,)),

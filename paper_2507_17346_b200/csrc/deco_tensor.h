@@ -94,6 +94,18 @@ __device__ __forceinline__ bool bar_wait_cta(uint64_t *b, uint32_t parity, volat
     }
     return true;
 }
+// All lanes together, with one answer.
+__device__ __forceinline__ bool bar_wait_warp(uint64_t *b, uint32_t parity, volatile uint32_t *abort)
+{
+    return __all_sync(0xFFFFFFFFu, bar_wait_cta(b, parity, abort));
+}
+// One lane of a warp whose lanes are all here.
+__device__ __forceinline__ bool elected()
+{
+    uint32_t is;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
+    return is != 0;
+}
 // Arrive at the barrier of the pair's first CTA, where what was written before stays in this CTA's own shared memory, for
 // the tensor cores (behind a proxy fence): a release at the cluster's scope would wait 1500 cycles for all the thread's stores.
 template <int CG>

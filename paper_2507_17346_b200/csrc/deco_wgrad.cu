@@ -36,26 +36,30 @@ using namespace deco::tensor;
 using deco::BLOCK8;
 
 constexpr int BK = 64;                   // tokens per stage
-constexpr int STAGES = 5;                // of operands, and of codes and steps on their way to being converted
 constexpr uint32_t TILE_M = 128;         // of dY's columns, a CTA's
-constexpr uint32_t MAX_H = 128;          // of X's columns, a CTA's, with those of ones
+constexpr uint32_t MAX_H = 112, MAX_HALF = 128;  // of X's columns, a CTA's; with those of ones
 constexpr uint32_t ONES = 16;            // columns of ones, a CTA's
 constexpr uint32_t SLAB = BK * 128;      // 64 columns of an operand
-constexpr uint32_t OPERAND = 2 * SLAB, STAGE_BYTES = 2 * OPERAND;
-constexpr uint32_t RAW_BYTES = BK * MAX_H + BK * 16;     // codes; per token eight steps of 16 columns each, in bf16
+constexpr uint32_t OPERAND = 2 * SLAB;
+// Codes of a block, tokens an odd number of 16 bytes apart (no bank conflicts), and per token the steps of up to eight times
+// 16 columns, in bf16.
+constexpr uint32_t CODE_BYTES = BK * MAX_H, RAW_BYTES = CODE_BYTES + BK * 16;
 // Warps: eight empty the accumulators; eight convert, two a block; one loads dY, one multiplies, two load X.
 constexpr int SUM_WARPS = 8, CONVERT_WARPS = 8, TEAM_WARPS = 2, TEAMS = CONVERT_WARPS / TEAM_WARPS;
 constexpr uint32_t FIRST_CONVERT = SUM_WARPS, LOAD = FIRST_CONVERT + CONVERT_WARPS, MULTIPLY = LOAD + 1, FIRST_X = LOAD + 2;
 constexpr int THREADS = 32 * (SUM_WARPS + CONVERT_WARPS + 4);
+// Stages of dY, of X as bf16, of X as codes and steps.  The rings of X are multiples of the teams, and that of codes of
+// the two warps that load it, long: every buffer is always the same team's and the same loader's, who so see each of its
+// phases.  (A wait for a phase that others have waited for in between could take an older one's parity for it.)
+constexpr int A_STAGES = 5, B_STAGES = TEAMS, RAW_STAGES = 2 * TEAMS;
 // Registers: a launch gives 640 threads 96 each (61440).  256 threads hold 128 sums each, the others need few:
-// 256 * 168 + 256 * 48 + 128 * 48 = 61440.
-constexpr int SUM_REGISTERS = 168, CONVERT_REGISTERS = 48, OTHER_REGISTERS = 48;
-constexpr uint32_t STAGING_COLS = 16, STAGING_FLOATS = 32 * (STAGING_COLS + 1);      // of a warp
-constexpr size_t SMEM = STAGES * (STAGE_BYTES + RAW_BYTES) + SUM_WARPS * STAGING_FLOATS * 4 + 1024;
+// 256 * 168 + 256 * 40 + 128 * 56 = 60416.
+constexpr int SUM_REGISTERS = 168, CONVERT_REGISTERS = 40, OTHER_REGISTERS = 56;
+constexpr uint32_t STAGING_COLS = 8, STAGING_FLOATS = 32 * (STAGING_COLS + 1);      // of a warp
+constexpr size_t SMEM = (A_STAGES + B_STAGES) * OPERAND + RAW_STAGES * RAW_BYTES + SUM_WARPS * STAGING_FLOATS * 4 + 1024;
 constexpr uint32_t CHUNK = 8;            // blocks an accumulator takes before it is emptied
 constexpr uint32_t SMS = 148;
 constexpr uint32_t MIN_BLOCKS = 8;       // a CTA's share, if tiles have to be cut for it
-constexpr int UNITS = BK * MAX_H / 16 / (32 * TEAM_WARPS);       // 16-code units of a converting thread per block
 
 // A tile is CG * 128 columns of dY by CG * h of X, h a multiple of 16.  A CTA (of a pair) makes the operand of h of the
 // product's columns and, in tiles that sum db too, of 16 of ones behind them.
@@ -63,7 +67,7 @@ struct Args {
     const uint8_t *exps;
     uint32_t rows, blocks8;              // tokens, blocks of a row of X
     uint32_t out, cols;
-    uint32_t h, tiles_n, k_blocks;
+    uint32_t h, code_pitch, tiles_n, k_blocks;
     uint32_t planes, plane_rows, chunk;
     uint64_t units;                      // tiles * k_blocks
     uint32_t workers;                    // CTAs or pairs
@@ -73,30 +77,50 @@ struct Args {
 };
 
 struct __align__(8) Control {
-    uint64_t full[STAGES], empty[STAGES], raw_full[STAGES], raw_empty[STAGES], acc_full[2], acc_empty[2];
+    uint64_t a_full[A_STAGES], a_empty[A_STAGES], b_full[B_STAGES], b_empty[B_STAGES];
+    uint64_t raw_full[RAW_STAGES], raw_empty[RAW_STAGES], acc_full[2], acc_empty[2];
     uint32_t tmem;
     volatile uint32_t abort;
 };
 
-// The blocks of a worker in their order: segments of tiles, in them chunks, in those planes (the smallest first), in those
-// blocks of tokens.
+// A worker's blocks in their order: segments of tiles, in them chunks, in those planes (the smallest first), in those blocks of
+// tokens.  Each of the three functions may end the walk by false.
+template <typename S, typename B, typename C>
+__device__ __forceinline__ void walk(const Args &g, uint32_t worker, S segment, B block, C chunk)
+{
+    const uint64_t end = g.units * (worker + 1) / g.workers;
+    for (uint64_t u = g.units * worker / g.workers; u < end;) {
+        const uint32_t tile = static_cast<uint32_t>(u / g.k_blocks);
+        const uint32_t first = static_cast<uint32_t>(u - static_cast<uint64_t>(tile) * g.k_blocks);
+        const uint32_t last = static_cast<uint32_t>(min(static_cast<uint64_t>(g.k_blocks), first + (end - u)));
+        if (!segment(tile, first, last)) return;
+        for (uint32_t c0 = first; c0 < last;) {
+            const uint32_t c1 = min(c0 + g.chunk, last);
+            for (uint32_t plane = g.planes; plane-- > 0;)
+                for (uint32_t k = c0; k < c1; ++k)
+                    if (!block(k, plane)) return;
+            c0 = c1;
+            if (!chunk(c0 == last)) return;
+        }
+        u += last - first;
+    }
+}
+
+// The same a block at a time, for those who are ahead of themselves.
 struct Cursor {
-    uint32_t tile, first, last;          // segment
-    uint32_t c0, c1;                     // chunk
-    uint32_t plane, k;                   // block
+    uint32_t tile, last, c0, c1, plane, k;
     bool done;
     __device__ void segment(const Args &g, uint64_t u, uint64_t end)
     {
         done = u >= end;
         if (done) return;
         tile = static_cast<uint32_t>(u / g.k_blocks);
-        first = c0 = k = static_cast<uint32_t>(u - static_cast<uint64_t>(tile) * g.k_blocks);
+        c0 = k = static_cast<uint32_t>(u - static_cast<uint64_t>(tile) * g.k_blocks);
         last = static_cast<uint32_t>(min(static_cast<uint64_t>(g.k_blocks), k + (end - u)));
         c1 = min(c0 + g.chunk, last);
         plane = g.planes - 1;
     }
     __device__ Cursor(const Args &g, uint32_t worker) { segment(g, g.units * worker / g.workers, g.units * (worker + 1) / g.workers); }
-    __device__ bool chunk_ends() const { return k + 1 == c1 && plane == 0; }
     __device__ void advance(const Args &g, uint32_t worker)
     {
         if (++k < c1) return;
@@ -110,13 +134,6 @@ struct Cursor {
         } else {
             segment(g, static_cast<uint64_t>(tile) * g.k_blocks + last, g.units * (worker + 1) / g.workers);
         }
-    }
-    // to the first block of the next chunk
-    __device__ void next_chunk(const Args &g, uint32_t worker)
-    {
-        k = c1 - 1;
-        plane = 0;
-        advance(g, worker);
     }
 };
 
@@ -161,13 +178,6 @@ __device__ __forceinline__ uint4 converted(uint32_t c0, uint32_t c1, uint32_t st
     }
     return make_uint4(o[0], o[1], o[2], o[3]);
 }
-__device__ __forceinline__ uint32_t lds2(uint32_t a)
-{
-    uint16_t v;
-    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a) : "memory");
-    return v;
-}
-
 // Where the 8 columns from 8 c on of token k lie in an operand's stage.
 __device__ __forceinline__ uint32_t unit_offset(uint32_t k, uint32_t c)
 {
@@ -182,15 +192,21 @@ wgrad_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
     constexpr uint32_t SIDE = GROUPS * 32;
     extern __shared__ uint8_t raw[];
     __shared__ Control ctl;
-    const uint32_t stages = (smem_addr(raw) + 1023) & ~1023u;
+    const uint32_t a_at = (smem_addr(raw) + 1023) & ~1023u, b_at = a_at + A_STAGES * OPERAND, raws = b_at + B_STAGES * OPERAND;
     const uint32_t wid = threadIdx.x >> 5, lane = threadIdx.x & 31, worker = blockIdx.x / CG;
     uint32_t rank = 0;
     if (CG == 2) asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     if (threadIdx.x == 0) {
-        for (int s = 0; s < STAGES; ++s) {
-            bar_init(&ctl.full[s], 1 + CG * TEAM_WARPS);
-            bar_init(&ctl.empty[s], 1);
-            bar_init(&ctl.raw_full[s], 3);
+        for (int s = 0; s < A_STAGES; ++s) {
+            bar_init(&ctl.a_full[s], 1);
+            bar_init(&ctl.a_empty[s], 1);
+        }
+        for (int s = 0; s < B_STAGES; ++s) {
+            bar_init(&ctl.b_full[s], CG * TEAM_WARPS);
+            bar_init(&ctl.b_empty[s], 1);
+        }
+        for (int s = 0; s < RAW_STAGES; ++s) {
+            bar_init(&ctl.raw_full[s], 2);
             bar_init(&ctl.raw_empty[s], TEAM_WARPS);
         }
         for (int s = 0; s < 2; ++s) {
@@ -202,9 +218,9 @@ wgrad_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
     }
     if (wid == MULTIPLY) tmem_alloc<CG>(&ctl.tmem, 512);
     if (g.db && threadIdx.x < BK)                                // the columns of ones, which nothing overwrites
-        for (int s = 0; s < STAGES; ++s)
+        for (int s = 0; s < B_STAGES; ++s)
             for (uint32_t c = 0; c < ONES / 8; ++c)
-                sts16(stages + s * STAGE_BYTES + OPERAND + unit_offset(threadIdx.x, g.h / 8 + c),
+                sts16(b_at + s * OPERAND + unit_offset(threadIdx.x, g.h / 8 + c),
                       make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u));
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -214,192 +230,228 @@ wgrad_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
         asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
     }
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    const uint32_t tmem = ctl.tmem, raws = stages + STAGES * STAGE_BYTES;
+    const uint32_t tmem = ctl.tmem;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
     if (wid >= LOAD) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(OTHER_REGISTERS));
-        if (wid == LOAD && lane == 0) {
+        const auto nothing = [](bool) { return true; };
+        if (wid == LOAD) {
             uint32_t s = 0, parity = 1;
-            const uint32_t full0 = smem_addr(ctl.full), bar0 = CG == 1 ? full0 : leader_addr(full0);
-            for (Cursor cur(g, worker); !cur.done; cur.advance(g, worker)) {
-                if (!bar_wait_cta(&ctl.empty[s], parity, &ctl.abort)) break;
-                const uint32_t st = stages + s * STAGE_BYTES, bar = bar0 + s * 8;
-                const int32_t x = ((cur.tile / g.tiles_n) * CG + rank) * TILE_M, y = cur.plane * g.plane_rows + cur.k * BK;
-                if (rank == 0) bar_expect(&ctl.full[s], CG * OPERAND);
-                load_box<CG>(st, &map, x, y, bar);
-                load_box<CG>(st + SLAB, &map, x + 64, y, bar);
-                if (++s == STAGES) {
-                    s = 0;
-                    parity ^= 1;
-                }
-            }
+            int32_t x = 0;
+            const uint32_t full0 = smem_addr(ctl.a_full), bar0 = CG == 1 ? full0 : leader_addr(full0);
+            walk(g, worker,
+                 [&](uint32_t tile, uint32_t, uint32_t) {
+                     x = ((tile / g.tiles_n) * CG + rank) * TILE_M;
+                     return true;
+                 },
+                 [&](uint32_t k, uint32_t plane) {
+                     if (!bar_wait_warp(&ctl.a_empty[s], parity, &ctl.abort)) return false;
+                     if (lane == 0) {
+                         const uint32_t st = a_at + s * OPERAND, bar = bar0 + s * 8;
+                         const int32_t y = plane * g.plane_rows + k * BK;
+                         if (rank == 0) bar_expect(&ctl.a_full[s], CG * OPERAND);
+                         load_box<CG>(st, &map, x, y, bar);
+                         load_box<CG>(st + SLAB, &map, x + 64, y, bar);
+                     }
+                     if (++s == A_STAGES) {
+                         s = 0;
+                         parity ^= 1;
+                     }
+                     return true;
+                 },
+                 nothing);
             if (ctl.abort) {                                     // copies under way get time to land
                 const long long t0 = clock64();
                 while (clock64() - t0 < 20000000ll) {}
             }
-        }
-        if (wid == MULTIPLY && lane == 0 && rank == 0) {
-            uint32_t s = 0, parity = 0, n = 0, idesc = 0;
-            bool first = true;                                   // block of a chunk
-            for (Cursor cur(g, worker); !cur.done; cur.advance(g, worker)) {
-                const uint32_t as = n & 1;
-                if (first) {
-                    const Columns<CG> c(g, cur.tile % g.tiles_n);
-                    // bf16 operands, fp32 sums, outer dimensions consecutive, N and M
-                    idesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((c.width >> 3) << 17) |
-                            ((CG * TILE_M >> 4) << 24);
-                    if (!bar_wait_cta(&ctl.acc_empty[as], ((n >> 1) & 1) ^ 1, &ctl.abort)) break;
-                }
-                if (!bar_wait_cta(&ctl.full[s], parity, &ctl.abort)) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint64_t da = operand_desc(stages + s * STAGE_BYTES, true);
-                const uint64_t db = operand_desc(stages + s * STAGE_BYTES + OPERAND, true);
+        } else if (wid == MULTIPLY && rank == 0) {
+            // This warp's loop is what the tensor cores wait for: it runs with all lanes, so that the descriptors can stay in
+            // uniform registers, and one lane issues.
+            const bool issues = elected();
+            uint32_t sa = 0, pa = 0, sb = 0, pb = 0, n = 0, idesc = 0, acc = 0, more = 0;
+            const uint64_t desc_a = operand_desc(a_at, true), desc_b = operand_desc(b_at, true);
+            uint64_t da = desc_a, db = desc_b;
+            walk(g, worker,
+                 [&](uint32_t tile, uint32_t, uint32_t) {
+                     const Columns<CG> c(g, tile % g.tiles_n);
+                     // bf16 operands, fp32 sums, outer dimensions consecutive, N and M
+                     idesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((c.width >> 3) << 17) |
+                             ((CG * TILE_M >> 4) << 24);
+                     return true;
+                 },
+                 [&](uint32_t, uint32_t) {
+                     if (!more) {                                // a chunk begins
+                         if (!bar_wait_warp(&ctl.acc_empty[n & 1], ((n >> 1) & 1) ^ 1, &ctl.abort)) return false;
+                         acc = tmem + (n & 1) * 256;
+                     }
+                     if (!bar_wait_warp(&ctl.a_full[sa], pa, &ctl.abort) || !bar_wait_warp(&ctl.b_full[sb], pb, &ctl.abort)) return false;
+                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                     if (issues) {
 #pragma unroll
-                for (uint32_t q = 0; q < BK / 16; ++q)
-                    mma<CG>(tmem + as * 256, da + q * (2048 >> 4), db + q * (2048 >> 4), idesc, !first || q != 0);
-                mma_commit<CG>(&ctl.empty[s]);
-                first = cur.chunk_ends();
-                if (first) {
-                    mma_commit<CG>(&ctl.acc_full[as]);
-                    n += 1;
-                }
-                if (++s == STAGES) {
-                    s = 0;
-                    parity ^= 1;
-                }
-            }
-        }
-        if (wid >= FIRST_X) {
-            // Codes by box copy; steps by plain loads, a token a lane and turn, the next ones on their way while these are
-            // stored.  The two warps take a half of each block's tokens.
-            const uint32_t token = (wid - FIRST_X) * 32 + lane;
-            uint32_t s = 0, parity = 1;
+                         for (uint32_t q = 0; q < BK / 16; ++q)
+                             mma<CG>(acc, da + q * (2048 >> 4), db + q * (2048 >> 4), idesc, q ? 1u : more);
+                         mma_commit<CG>(&ctl.a_empty[sa]);
+                         mma_commit<CG>(&ctl.b_empty[sb]);
+                     }
+                     more = 1;
+                     da += OPERAND >> 4;
+                     db += OPERAND >> 4;
+                     if (++sa == A_STAGES) {
+                         sa = 0;
+                         pa ^= 1;
+                         da = desc_a;
+                     }
+                     if (++sb == B_STAGES) {
+                         sb = 0;
+                         pb ^= 1;
+                         db = desc_b;
+                     }
+                     return true;
+                 },
+                 [&](bool) {
+                     if (issues) mma_commit<CG>(&ctl.acc_full[n & 1]);
+                     n += 1;
+                     more = 0;
+                     return true;
+                 });
+        } else if (wid >= FIRST_X) {
+            // Codes by box copy; steps by plain loads, two tokens a lane.  The two warps take turns, and a warp's loads are two of
+            // its blocks ahead of what it stores.
+            uint32_t e[2][2][5], x[2], y[2];
+            bool have[2];
             Cursor cur(g, worker);
-            uint32_t e[5], col0 = 0;
-            auto fetch = [&]() {
-                col0 = ((cur.tile % g.tiles_n) * CG + rank) * g.h;
-                const uint32_t t = cur.k * BK + token, b = col0 / BLOCK8;
-                const uint8_t *p = g.exps + static_cast<uint64_t>(t) * g.blocks8 + b;
+            if (wid != FIRST_X) cur.advance(g, worker);
+            auto fetch = [&](int i) {
+                have[i] = !cur.done;
+                if (cur.done) return;
+                x[i] = ((cur.tile % g.tiles_n) * CG + rank) * g.h;
+                y[i] = cur.k * BK;
+                const uint32_t b = x[i] / BLOCK8;
 #pragma unroll
-                for (uint32_t j = 0; j < 5; ++j) {
-                    e[j] = 0;
-                    if (t < g.rows && b + j < g.blocks8) e[j] = __ldg(p + j);
+                for (uint32_t l = 0; l < 2; ++l) {
+                    const uint32_t t = y[i] + l * 32 + lane;
+                    const uint8_t *p = g.exps + static_cast<uint64_t>(t) * g.blocks8 + b;
+#pragma unroll
+                    for (uint32_t j = 0; j < 5; ++j) e[i][l][j] = t < g.rows && b + j < g.blocks8 ? __ldg(p + j) : 0u;
                 }
-            };
-            if (!cur.done) fetch();
-            while (!cur.done) {
-                const uint32_t to = raws + s * RAW_BYTES;
-                if (!bar_wait_cta(&ctl.raw_empty[s], parity, &ctl.abort)) break;
-                if (wid == FIRST_X && lane == 0) {
-                    bar_expect(&ctl.raw_full[s], BK * g.h);
-                    load_box<1>(to, &code_map, col0, cur.k * BK, smem_addr(&ctl.raw_full[s]));
-                }
-                // a tile begins at a block of 32 columns or in its middle
-                const bool middle = col0 & 16;
-                uint32_t w[4];
-#pragma unroll
-                for (uint32_t j = 0; j < 5; ++j) e[j] = e[j] == 255u ? 0x7FC0u : e[j] << 7;
-#pragma unroll
-                for (uint32_t u = 0; u < 4; ++u) w[u] = e[u] | (middle ? e[u + 1] : e[u]) << 16;
                 cur.advance(g, worker);
-                if (!cur.done) fetch();
-                sts16(to + BK * MAX_H + token * 16, make_uint4(w[0], w[1], w[2], w[3]));
+                if (!cur.done) cur.advance(g, worker);
+            };
+            fetch(0);
+            fetch(1);
+            uint32_t s = wid - FIRST_X, parity = 1;
+            auto store = [&](int i) {
+                if (!have[i] || !bar_wait_warp(&ctl.raw_empty[s], parity, &ctl.abort)) return false;
+                const uint32_t to = raws + s * RAW_BYTES;
+                if (lane == 0) {
+                    bar_expect(&ctl.raw_full[s], BK * g.code_pitch);
+                    load_box<1>(to, &code_map, x[i], y[i], smem_addr(&ctl.raw_full[s]));
+                }
+#pragma unroll
+                for (uint32_t l = 0; l < 2; ++l) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (uint32_t j = 0; j < 5; ++j) e[i][l][j] = e[i][l][j] == 255u ? 0x7FC0u : e[i][l][j] << 7;
+                    // a tile begins at a block of 32 columns or in its middle
+#pragma unroll
+                    for (uint32_t u = 0; u < 4; ++u) w[u] = e[i][l][u] | (x[i] & 16 ? e[i][l][u + 1] : e[i][l][u]) << 16;
+                    sts16(to + CODE_BYTES + (l * 32 + lane) * 16, make_uint4(w[0], w[1], w[2], w[3]));
+                }
                 __syncwarp();
                 if (lane == 0) bar_arrive(&ctl.raw_full[s]);
-                if (++s == STAGES) {
-                    s = 0;
+                s += 2;
+                if (s >= RAW_STAGES) {
+                    s -= RAW_STAGES;
                     parity ^= 1;
                 }
-            }
+                fetch(i);
+                return true;
+            };
+            while (store(0) && store(1)) {}
         }
     } else if (wid >= FIRST_CONVERT) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(CONVERT_REGISTERS));
-        // A team of two warps converts every fourth block.  This thread's units: where the step lies, and the two places
-        // of the bf16 numbers.  Lanes next to each other take units next to each other, and those of the second 64
-        // columns their second half first: no bank conflicts.
-        const uint32_t team = (wid - FIRST_CONVERT) / TEAM_WARPS, me = ((wid - FIRST_CONVERT) % TEAM_WARPS) * 32 + lane;
-        const uint32_t per_row = g.h / 16, count = BK * per_row;
-        uint32_t step_to[UNITS];                                 // bits 0 to 13: place; 16 to 25: step; 31: second half first
-#pragma unroll
-        for (int i = 0; i < UNITS; ++i) {
-            const uint32_t id = i * 32 * TEAM_WARPS + me, token = id / per_row, c = id - token * per_row, swap = (c >> 2) & 1;
-            step_to[i] = id < count ? unit_offset(token, 2 * c + swap) | (token * 16 + c * 2) << 16 | swap << 31 : 0;
-        }
+        // A team of two warps converts every fourth block, a thread a token: lanes next to each other meet no bank
+        // conflicts, since rows of codes are an odd number of 16 bytes apart and the operand's units are permuted.
+        const uint32_t team = (wid - FIRST_CONVERT) / TEAM_WARPS, token = ((wid - FIRST_CONVERT) % TEAM_WARPS) * 32 + lane;
+        const uint32_t per_row = g.h / 16;
         const uint64_t u0 = g.units * worker / g.workers, u1 = g.units * (worker + 1) / g.workers;
-        const uint64_t blocks = (u1 - u0) * g.planes;
-        uint32_t s = team % STAGES, parity = 0;                  // (TEAMS < STAGES)
-        for (uint64_t n = team; n < blocks; n += TEAMS) {
-            const uint32_t from = raws + s * RAW_BYTES + me * 16, steps = raws + s * RAW_BYTES + BK * MAX_H;
-            const uint32_t base = stages + s * STAGE_BYTES + OPERAND;
-            bool ok = bar_wait_cta(&ctl.raw_full[s], parity, &ctl.abort);
-            ok = ok && bar_wait_cta(&ctl.empty[s], parity ^ 1, &ctl.abort);
-            if (!__all_sync(0xFFFFFFFFu, ok)) break;
+        const uint32_t to = b_at + team * OPERAND + unit_offset(token, 0);
+        uint32_t second = 0, raw_parity = 0, parity = 1;         // the team's second buffer of codes
+        for (uint64_t left = (u1 - u0) * g.planes, n = team; n < left; n += TEAMS) {
+            const uint32_t r = team + second * TEAMS, from = raws + r * RAW_BYTES + token * g.code_pitch;
+            if (!bar_wait_warp(&ctl.raw_full[r], raw_parity, &ctl.abort)) break;
+            const uint4 st = lds16(raws + r * RAW_BYTES + CODE_BYTES + token * 16);
+            const uint32_t step[4] = {st.x, st.y, st.z, st.w};
+            uint4 code = lds16(from);
+            if (!bar_wait_warp(&ctl.b_empty[team], parity, &ctl.abort)) break;
+            parity ^= 1;
 #pragma unroll
-            for (int i = 0; i < UNITS; ++i) {
-                if (i * 32 * TEAM_WARPS + me >= count) continue;
-                const uint4 code = lds16(from + i * 512 * TEAM_WARPS);
-                const uint32_t step = lds2(steps + ((step_to[i] >> 16) & 0x3FFu)) * 0x10001u;
-                const uint4 a = converted(code.x, code.y, step), b = converted(code.z, code.w, step);
-                const bool swap = step_to[i] >> 31;
-                const uint32_t to = base + (step_to[i] & 0x3FFFu);
-                sts16(to, swap ? b : a);
-                sts16(to ^ 16, swap ? a : b);
+            for (uint32_t c = 0; c < MAX_H / 16; ++c) {
+                if (c >= per_row) break;
+                const uint4 now = code;
+                if (c + 1 < MAX_H / 16) code = lds16(from + (c + 1) * 16);
+                const uint32_t twice = __byte_perm(step[c >> 1], 0, c & 1 ? 0x3232 : 0x1010);
+                // (unit 2 c of the row lies at 2 c exclusive-or token: the permutation of the row's first, turned)
+                const uint32_t at = (to ^ ((2 * c & 7) << 4)) + (c >> 2) * SLAB;
+                sts16(at, converted(now.x, now.y, twice));
+                sts16(at ^ 16, converted(now.z, now.w, twice));
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) {
-                bar_arrive(&ctl.raw_empty[s]);
-                bar_arrive_leader_cta<CG>(&ctl.full[s]);
+                bar_arrive(&ctl.raw_empty[r]);
+                bar_arrive_leader_cta<CG>(&ctl.b_full[team]);
             }
-            s += TEAMS;
-            if (s >= STAGES) {
-                s -= STAGES;
-                parity ^= 1;
-            }
+            raw_parity ^= second;
+            second ^= 1;
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(SUM_REGISTERS));
         const uint32_t quad = wid & 3, side = wid >> 2;          // lanes of the tensor memory, half of the columns
-        float *staging = reinterpret_cast<float *>(raw + (raws - smem_addr(raw)) + STAGES * RAW_BYTES) + wid * STAGING_FLOATS;
+        float *staging = reinterpret_cast<float *>(raw + (raws - smem_addr(raw)) + RAW_STAGES * RAW_BYTES) + wid * STAGING_FLOATS;
         float sum[GROUPS][32];                                   // this warp's half of the columns, a row a thread
         uint32_t n = 0;
-        bool dead = false;                                       // a wait has run out: NaN from here on
-        for (Cursor cur(g, worker); !cur.done; cur.next_chunk(g, worker)) {
-            const uint32_t as = n & 1;
-            if (cur.c0 == cur.first) {
+        bool dead = false;                                       // a wait has run out, NaN from here on
+        const uint64_t end = g.units * (worker + 1) / g.workers;
+        for (uint64_t u = g.units * worker / g.workers; u < end;) {      // (as walk does)
+            const uint32_t tile = static_cast<uint32_t>(u / g.k_blocks), nt = tile % g.tiles_n;
+            const uint32_t first = static_cast<uint32_t>(u - static_cast<uint64_t>(tile) * g.k_blocks);
+            const uint32_t last = static_cast<uint32_t>(min(static_cast<uint64_t>(g.k_blocks), first + (end - u)));
+            u += last - first;
 #pragma unroll
-                for (uint32_t h = 0; h < GROUPS; ++h)
+            for (uint32_t h = 0; h < GROUPS; ++h)
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) sum[h][j] = 0.f;
-            }
-            if (!dead) dead = !bar_wait_cta(&ctl.acc_full[as], (n >> 1) & 1, &ctl.abort);
-            dead = __any_sync(0xFFFFFFFFu, dead);
-            n += 1;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t nt = cur.tile % g.tiles_n;
+                for (int j = 0; j < 32; ++j) sum[h][j] = 0.f;
             const Columns<CG> c(g, nt);
+#pragma unroll 1
+            for (uint32_t c0 = first; c0 < last; c0 += g.chunk) {
+                const uint32_t as = n & 1;
+                if (!dead) dead = !bar_wait_warp(&ctl.acc_full[as], (n >> 1) & 1, &ctl.abort);
+                n += 1;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
-            for (uint32_t h = 0; h < GROUPS; ++h) {
+                for (uint32_t h = 0; h < GROUPS; ++h) {
 #pragma unroll
-                for (uint32_t p = 0; p < 32; p += 16) {
-                    if (side * SIDE + h * 32 + p >= c.width) continue;
-                    uint32_t v[16];
-                    __syncwarp();
-                    tmem_load16(tmem + ((quad * 32) << 16) + as * 256 + side * SIDE + h * 32 + p, v);
+                    for (uint32_t p = 0; p < 32; p += 16) {
+                        if (side * SIDE + h * 32 + p >= c.width) continue;
+                        uint32_t v[16];
+                        __syncwarp();
+                        tmem_load16(tmem + ((quad * 32) << 16) + as * 256 + side * SIDE + h * 32 + p, v);
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) sum[h][p + j] += __uint_as_float(v[j]);
+                        for (int j = 0; j < 16; ++j) sum[h][p + j] += __uint_as_float(v[j]);
+                    }
                 }
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) bar_arrive_leader_cta<CG>(&ctl.acc_empty[as]);
             }
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) bar_arrive_leader_cta<CG>(&ctl.acc_empty[as]);
-            if (cur.c1 != cur.last) continue;
-            // the segment's last chunk: its sums go out
-            const bool whole = cur.last - cur.first == g.k_blocks;
-            const uint32_t mt = (cur.tile / g.tiles_n) * CG + rank, o = mt * TILE_M + quad * 32 + lane, col0 = nt * CG * g.h;
-            float *slot = g.slots + ((worker * 2ull + (cur.first == 0)) * CG + rank) * (CG * MAX_H * TILE_M) + quad * 32 + lane;
+            const uint32_t mt = (tile / g.tiles_n) * CG + rank;
+            const bool whole = last - first == g.k_blocks, from_top = first == 0;
+            const uint32_t o = mt * TILE_M + quad * 32 + lane, col0 = nt * CG * g.h;
+            float *slot = g.slots + ((worker * 2ull + from_top) * CG + rank) * (CG * MAX_HALF * TILE_M) + quad * 32 + lane;
 #pragma unroll
             for (uint32_t h = 0; h < GROUPS; ++h) {
                 const uint32_t n0 = side * SIDE + h * 32;
@@ -420,7 +472,7 @@ wgrad_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
                         if (c.in(n0 + j) && col0 + c.col(n0 + j) < g.cols && o < g.out)
                             store_grad<G>(g.dw, static_cast<uint64_t>(col0 + c.col(n0 + j)) * g.out + o, sum[h][j], g.accumulate);
                 } else {
-                    // sixteen columns at a time, so that half a warp writes consecutive entries of a row
+                    // a few columns at a time, so that neighbouring lanes write neighbouring entries
 #pragma unroll
                     for (uint32_t p = 0; p < 32; p += STAGING_COLS) {
                         const uint32_t at = n0 + p + (lane & (STAGING_COLS - 1)), col = col0 + c.col(at);
@@ -480,7 +532,7 @@ join_kernel(const Args g)
     for (int j = 0; j < 16; ++j) v[j] = 0.f;
     for (uint32_t w = a; w <= b; ++w) {
         // (a range in which the tile begins has it in the second slot, one that begins inside the tile in the first)
-        const float *p = g.slots + ((w * 2ull + (w == a)) * CG + rank) * (CG * MAX_H * TILE_M) + row;
+        const float *p = g.slots + ((w * 2ull + (w == a)) * CG + rank) * (CG * MAX_HALF * TILE_M) + row;
 #pragma unroll
         for (uint32_t j = 0; j < 16; ++j)
             if (n0 + j0 + j < c.width) v[j] += __ldcg(p + (n0 + j0 + j) * TILE_M);
@@ -556,10 +608,9 @@ struct Plan {
     uint64_t units;
     bool cut;                            // some tile lies in more than one range
     uint64_t plane_bytes() const { return 2ull * planes * plane_rows * pitch; }
-    uint64_t bytes() const { return plane_bytes() + (cut ? 2ull * workers * cg * cg * MAX_H * TILE_M * 4 : 0); }
+    uint64_t bytes() const { return plane_bytes() + (cut ? 2ull * workers * cg * cg * MAX_HALF * TILE_M * 4 : 0); }
 };
-Plan make_plan(const void *dy, int32_t dtype, uint64_t rows, uint32_t out, uint64_t stride, uint32_t cols, bool bias,
-               int32_t grad_dtype)
+Plan make_plan(const void *dy, int32_t dtype, uint64_t rows, uint32_t out, uint64_t stride, uint32_t cols, int32_t grad_dtype)
 {
     Plan p = {};
     if (dtype == DECO_F32) p.planes = grad_dtype == DECO_F32 ? 3 : 2;
@@ -570,7 +621,7 @@ Plan make_plan(const void *dy, int32_t dtype, uint64_t rows, uint32_t out, uint6
     // Pairs of CTAs read half as much per product; small results are left to single CTAs, whose tiles are a quarter.
     const uint64_t area = static_cast<uint64_t>((out + TILE_M - 1) / TILE_M) * ((cols + MAX_H - 1) / MAX_H);
     p.cg = area * p.k_blocks >= 4 * SMS * MIN_BLOCKS ? 2 : 1;
-    const uint32_t most = p.cg * (MAX_H - (bias ? ONES : 0)), unit = 16 * p.cg;
+    const uint32_t most = p.cg * MAX_H, unit = 16 * p.cg;
     p.tiles_n = (cols + most - 1) / most;
     p.h = ((cols + p.tiles_n - 1) / p.tiles_n + unit - 1) / unit * 16;
     p.tiles_m = (out + p.cg * TILE_M - 1) / (p.cg * TILE_M);
@@ -637,17 +688,17 @@ cudaError_t launch_all(const CUtensorMap &map, const CUtensorMap &code_map, cons
 {
     cudaError_t err = launch(wgrad_kernel<CG, G>, CG, dim3(p.workers * CG), THREADS, SMEM, s, map, code_map, a);
     if (err == cudaSuccess && p.cut)
-        err = launch(join_kernel<CG, G>, 1, dim3(p.tiles_m * p.tiles_n * CG, CG * MAX_H / 32), 256, 0, s, a);
+        err = launch(join_kernel<CG, G>, 1, dim3(p.tiles_m * p.tiles_n * CG, CG * MAX_HALF / 32), 256, 0, s, a);
     return err;
 }
 
 }  // namespace
 
 extern "C" uint64_t deco_weight_grad8_workspace(const void *dy, int32_t dtype, uint64_t rows, uint32_t out,
-                                                uint64_t dy_stride, uint32_t cols, int32_t bias, int32_t grad_dtype)
+                                                uint64_t dy_stride, uint32_t cols, int32_t grad_dtype)
 {
     if (rows == 0 || rows >= MAX_ROWS || out == 0 || out > MAX_COLS || cols == 0 || cols > MAX_COLS) return 0;
-    return make_plan(dy, dtype, rows, out, dy_stride, cols, bias != 0, grad_dtype).bytes();
+    return make_plan(dy, dtype, rows, out, dy_stride, cols, grad_dtype).bytes();
 }
 
 extern "C" deco_status deco_weight_grad8(const void *dy, int32_t dtype, uint64_t rows, uint32_t out, uint64_t dy_stride,
@@ -672,7 +723,7 @@ extern "C" deco_status deco_weight_grad8(const void *dy, int32_t dtype, uint64_t
     }
     if (!dy || !aligned_to(dy, dtype == DECO_F32 ? 4 : 2) || dy_stride < out || dy_stride > MAX_STRIDE) return DECO_ERR_INVALID_ARG;
     if (!codes || !exponents || !aligned_to(codes, 16)) return DECO_ERR_INVALID_ARG;
-    const Plan p = make_plan(dy, dtype, rows, out, dy_stride, cols, db != nullptr, grad_dtype);
+    const Plan p = make_plan(dy, dtype, rows, out, dy_stride, cols, grad_dtype);
     if (static_cast<uint64_t>(p.tiles_m) * p.tiles_n * p.cg > 0x7FFFFFFFull || static_cast<uint64_t>(p.planes) * p.plane_rows > 0x7FFFFFFFull)
         return DECO_ERR_INVALID_ARG;
     if (p.bytes()) {
@@ -683,10 +734,12 @@ extern "C" deco_status deco_weight_grad8(const void *dy, int32_t dtype, uint64_t
     if (!encode || !allow_shared_memory()) return DECO_ERR_CUDA;
     const void *operand = p.planes ? workspace : dy;
     const uint64_t pitch = (cols + BLOCK8 - 1) / BLOCK8 * static_cast<uint64_t>(BLOCK8);
+    // (as a box, so it may reach into the next tile's columns)
+    const uint32_t code_pitch = p.h / 16 % 2 ? p.h : p.h + 16;
     CUtensorMap map, code_map;
     if (!box_map(encode, &map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, operand, out, p.planes ? static_cast<uint64_t>(p.planes) * p.plane_rows : rows,
                  2 * (p.planes ? p.pitch : dy_stride), 64, CU_TENSOR_MAP_SWIZZLE_128B) ||
-        !box_map(encode, &code_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, pitch, rows, pitch, p.h, CU_TENSOR_MAP_SWIZZLE_NONE))
+        !box_map(encode, &code_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, pitch, rows, pitch, code_pitch, CU_TENSOR_MAP_SWIZZLE_NONE))
         return DECO_ERR_CUDA;
     Args a = {};
     a.exps = exponents;
@@ -695,6 +748,7 @@ extern "C" deco_status deco_weight_grad8(const void *dy, int32_t dtype, uint64_t
     a.out = out;
     a.cols = cols;
     a.h = p.h;
+    a.code_pitch = code_pitch;
     a.tiles_n = p.tiles_n;
     a.k_blocks = p.k_blocks;
     a.planes = std::max<uint32_t>(1, p.planes);
