@@ -673,7 +673,7 @@ deco_status deco_unpack8(const int8_t *codes, const uint8_t *exponents, uint64_t
  *   dw, db     [out][cols] (or [cols][out]) and [out] of grad_dtype, back to back, any alignment of whole entries: a matrix's place in
  *              the flat gradient vector.  Overwritten, or added to if `accumulate`; db may be NULL
  *   workspace  at least deco_weight_grad8_workspace(...) bytes for the same dy (whose alignment matters), dtype, rows, out, dy_stride,
- *              cols and grad_dtype; 16-byte aligned, its contents do not matter; fewer: DECO_ERR_CAPACITY.  May be NULL where that is 0
+ *              cols and grad_dtype; 16-byte aligned, its contents do not matter; fewer: DECO_ERR_CAPACITY
  * Products are exact: X's values are bf16 numbers, fp32 dy is taken as a sum of three (two where grad_dtype is bf16).  Sums are fp32,
  * on the tensor cores over at most 512 tokens at a time where grad_dtype is fp32.  out, cols <= 2^24.  rows = 0 gives sums of 0.
  * Should one of the kernel's bounded waits run out, the sums concerned come out as NaN.

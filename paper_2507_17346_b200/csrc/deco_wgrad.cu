@@ -16,8 +16,9 @@
 // registers, where sums are rounded; the two accumulators take turns, and the products go on.
 // lo's and mid's products of a chunk come before hi's, while the sum is still small.
 //
-// Shares.  The blocks of all tiles in a row, cut into equal ranges, one per CTA: a CTA begins and ends inside tiles.  Parts
-// of a tile are left in the workspace and added in their order by a second launch: the same bits every time.
+// Shares.  The blocks of all tiles in a row, cut into equal ranges, one per worker (a CTA or a pair): where whole tiles
+// would leave too many idle, a worker begins and ends inside tiles.  Parts of a tile are left in the workspace, and whoever
+// comes last adds them up, in their order whoever it is: the same bits every time.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -43,99 +44,80 @@ constexpr uint32_t SLAB = BK * 128;      // 64 columns of an operand
 constexpr uint32_t OPERAND = 2 * SLAB;
 // Codes of a block, tokens an odd number of 16 bytes apart (no bank conflicts), and per token the steps of up to eight times
 // 16 columns, in bf16.
-constexpr uint32_t CODE_BYTES = BK * MAX_H, RAW_BYTES = CODE_BYTES + BK * 16;
-// Warps: eight empty the accumulators; eight convert, two a block; one loads dY, one multiplies, two load X.
-constexpr int SUM_WARPS = 8, CONVERT_WARPS = 8, TEAM_WARPS = 2, TEAMS = CONVERT_WARPS / TEAM_WARPS;
-constexpr uint32_t FIRST_CONVERT = SUM_WARPS, LOAD = FIRST_CONVERT + CONVERT_WARPS, MULTIPLY = LOAD + 1, FIRST_X = LOAD + 2;
+constexpr uint32_t CODE_BYTES = BK * MAX_H, STEP_BYTES = BK * 16, RAW_BYTES = CODE_BYTES + STEP_BYTES;
+// Warps: eight empty the accumulators; twelve convert, four a block; one loads dY, one multiplies, one loads X.
+constexpr int SUM_WARPS = 8, CONVERT_WARPS = 12, TEAM_WARPS = 4, TEAMS = CONVERT_WARPS / TEAM_WARPS;
+constexpr uint32_t FIRST_CONVERT = SUM_WARPS, LOAD = FIRST_CONVERT + CONVERT_WARPS, MULTIPLY = LOAD + 1, LOAD_X = LOAD + 2;
 constexpr int THREADS = 32 * (SUM_WARPS + CONVERT_WARPS + 4);
-// Stages of dY, of X as bf16, of X as codes and steps.  The rings of X are multiples of the teams, and that of codes of
-// the two warps that load it, long: every buffer is always the same team's and the same loader's, who so see each of its
-// phases.  (A wait for a phase that others have waited for in between could take an older one's parity for it.)
-constexpr int A_STAGES = 5, B_STAGES = TEAMS, RAW_STAGES = 2 * TEAMS;
-// Registers: a launch gives 640 threads 96 each (61440).  256 threads hold 128 sums each, the others need few:
-// 256 * 168 + 256 * 40 + 128 * 56 = 60416.
-constexpr int SUM_REGISTERS = 168, CONVERT_REGISTERS = 40, OTHER_REGISTERS = 56;
-constexpr uint32_t STAGING_COLS = 8, STAGING_FLOATS = 32 * (STAGING_COLS + 1);      // of a warp
-constexpr size_t SMEM = (A_STAGES + B_STAGES) * OPERAND + RAW_STAGES * RAW_BYTES + SUM_WARPS * STAGING_FLOATS * 4 + 1024;
+// Stages of dY, of X as bf16, of X as codes and steps.  The rings of X are multiples of the teams: every buffer is always
+// the same team's, which so sees each of its phases.  (A wait for a phase after one that only others have waited for could
+// take an older one's parity for it.)
+constexpr int A_STAGES = 4, X_STAGES = 2 * TEAMS;
+// Registers: a launch gives 768 threads 80 each (61440).  256 threads hold 128 sums each, the others need few:
+// 256 * 168 + 384 * 32 + 128 * 48 = 61440.
+constexpr int SUM_REGISTERS = 168, CONVERT_REGISTERS = 32, OTHER_REGISTERS = 48;
+constexpr uint32_t STAGING_COLS = 16, STAGING_FLOATS = 32 * (STAGING_COLS + 1);      // of a warp
+constexpr size_t SMEM = A_STAGES * OPERAND + X_STAGES * (OPERAND + RAW_BYTES) + SUM_WARPS * STAGING_FLOATS * 4 + 1024;
 constexpr uint32_t CHUNK = 8;            // blocks an accumulator takes before it is emptied
 constexpr uint32_t SMS = 148;
-constexpr uint32_t MIN_BLOCKS = 8;       // a CTA's share, if tiles have to be cut for it
+constexpr uint32_t MIN_BLOCKS = 8;       // a worker's share, if tiles have to be cut for it
+constexpr uint32_t PART_BLOCKS = 8, EVEN_BLOCKS = 24;     // what cutting tiles costs
 
 // A tile is CG * 128 columns of dY by CG * h of X, h a multiple of 16.  A CTA (of a pair) makes the operand of h of the
 // product's columns and, in tiles that sum db too, of 16 of ones behind them.
 struct Args {
-    const uint8_t *exps;
-    uint32_t rows, blocks8;              // tokens, blocks of a row of X
+    const uint4 *steps;                  // [tile column's share of a CTA][k_blocks * BK] tokens: of eight times 16 columns, in bf16
     uint32_t out, cols;
     uint32_t h, code_pitch, tiles_n, k_blocks;
     uint32_t planes, plane_rows, chunk;
-    uint64_t units;                      // tiles * k_blocks
     uint32_t workers;                    // CTAs or pairs
+    uint32_t grain;                      // ranges are whole numbers of so many blocks: 1, or k_blocks (whole tiles)
+    uint64_t grains;
     void *dw, *db;
     int transposed, accumulate;
-    float *slots;                        // [worker][2][CG][columns of a tile's product][TILE_M]
+    float *slots;                        // [worker][2][CG][columns of a tile's product][TILE_M]: parts of tiles
+    uint32_t *arrived;                   // [tile][CG][SUM_WARPS]: how many of a tile's parts are there
+    // where a worker's range of blocks begins
+    __host__ __device__ __forceinline__ uint64_t begin(uint32_t worker) const { return grains * worker / workers * grain; }
 };
 
 struct __align__(8) Control {
-    uint64_t a_full[A_STAGES], a_empty[A_STAGES], b_full[B_STAGES], b_empty[B_STAGES];
-    uint64_t raw_full[RAW_STAGES], raw_empty[RAW_STAGES], acc_full[2], acc_empty[2];
+    uint64_t a_full[A_STAGES], a_empty[A_STAGES], b_full[X_STAGES], b_empty[X_STAGES];
+    uint64_t raw_full[X_STAGES], raw_empty[X_STAGES], acc_full[2], acc_empty[2];
     uint32_t tmem;
     volatile uint32_t abort;
 };
 
 // A worker's blocks in their order: segments of tiles, in them chunks, in those planes (the smallest first), in those blocks of
-// tokens.  Each of the three functions may end the walk by false.
-template <typename S, typename B, typename C>
-__device__ __forceinline__ void walk(const Args &g, uint32_t worker, S segment, B block, C chunk)
+// tokens.  Either function may end the walk by false.
+template <typename S, typename B>
+__device__ __forceinline__ void walk(const Args &g, uint32_t worker, S segment, B block)
 {
-    const uint64_t end = g.units * (worker + 1) / g.workers;
-    for (uint64_t u = g.units * worker / g.workers; u < end;) {
+    const uint64_t end = g.begin(worker + 1);
+    for (uint64_t u = g.begin(worker); u < end;) {
         const uint32_t tile = static_cast<uint32_t>(u / g.k_blocks);
         const uint32_t first = static_cast<uint32_t>(u - static_cast<uint64_t>(tile) * g.k_blocks);
         const uint32_t last = static_cast<uint32_t>(min(static_cast<uint64_t>(g.k_blocks), first + (end - u)));
-        if (!segment(tile, first, last)) return;
+        if (!segment(tile)) return;
         for (uint32_t c0 = first; c0 < last;) {
             const uint32_t c1 = min(c0 + g.chunk, last);
             for (uint32_t plane = g.planes; plane-- > 0;)
                 for (uint32_t k = c0; k < c1; ++k)
                     if (!block(k, plane)) return;
             c0 = c1;
-            if (!chunk(c0 == last)) return;
         }
         u += last - first;
     }
 }
 
-// The same a block at a time, for those who are ahead of themselves.
-struct Cursor {
-    uint32_t tile, last, c0, c1, plane, k;
-    bool done;
-    __device__ void segment(const Args &g, uint64_t u, uint64_t end)
-    {
-        done = u >= end;
-        if (done) return;
-        tile = static_cast<uint32_t>(u / g.k_blocks);
-        c0 = k = static_cast<uint32_t>(u - static_cast<uint64_t>(tile) * g.k_blocks);
-        last = static_cast<uint32_t>(min(static_cast<uint64_t>(g.k_blocks), k + (end - u)));
-        c1 = min(c0 + g.chunk, last);
-        plane = g.planes - 1;
-    }
-    __device__ Cursor(const Args &g, uint32_t worker) { segment(g, g.units * worker / g.workers, g.units * (worker + 1) / g.workers); }
-    __device__ void advance(const Args &g, uint32_t worker)
-    {
-        if (++k < c1) return;
-        if (plane) {
-            plane -= 1;
-            k = c0;
-        } else if (c1 < last) {
-            c0 = k = c1;
-            c1 = min(c0 + g.chunk, last);
-            plane = g.planes - 1;
-        } else {
-            segment(g, static_cast<uint64_t>(tile) * g.k_blocks + last, g.units * (worker + 1) / g.workers);
-        }
-    }
-};
+// The worker whose range holds block u.
+__device__ __forceinline__ uint32_t owner(const Args &g, uint64_t u)
+{
+    uint32_t w = static_cast<uint32_t>(u / g.grain * g.workers / g.grains);
+    while (g.begin(w + 1) <= u) ++w;
+    while (g.begin(w) > u) --w;
+    return w;
+}
 
 // Columns of a tile's product: `width` of them, of which `in` belong to X, as column `col` of the tile.
 template <int CG>
@@ -178,6 +160,9 @@ __device__ __forceinline__ uint4 converted(uint32_t c0, uint32_t c1, uint32_t st
     }
     return make_uint4(o[0], o[1], o[2], o[3]);
 }
+// 2^(b - 127), or NaN, as bf16.
+__device__ __forceinline__ uint32_t bf16_step(uint32_t b) { return b == 255u ? 0x7FC0u : b << 7; }
+
 // Where the 8 columns from 8 c on of token k lie in an operand's stage.
 __device__ __forceinline__ uint32_t unit_offset(uint32_t k, uint32_t c)
 {
@@ -188,11 +173,10 @@ template <int CG, typename G>
 __global__ void __launch_bounds__(THREADS, 1)
 wgrad_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap code_map, const Args g)
 {
-    constexpr uint32_t GROUPS = 2 * CG;          // of 32 columns of the product, a warp's
-    constexpr uint32_t SIDE = GROUPS * 32;
+    constexpr uint32_t SIDE = CG * 64;           // columns of the product, a warp's
     extern __shared__ uint8_t raw[];
     __shared__ Control ctl;
-    const uint32_t a_at = (smem_addr(raw) + 1023) & ~1023u, b_at = a_at + A_STAGES * OPERAND, raws = b_at + B_STAGES * OPERAND;
+    const uint32_t a_at = (smem_addr(raw) + 1023) & ~1023u, b_at = a_at + A_STAGES * OPERAND, raws = b_at + X_STAGES * OPERAND;
     const uint32_t wid = threadIdx.x >> 5, lane = threadIdx.x & 31, worker = blockIdx.x / CG;
     uint32_t rank = 0;
     if (CG == 2) asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
@@ -201,12 +185,10 @@ wgrad_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
             bar_init(&ctl.a_full[s], 1);
             bar_init(&ctl.a_empty[s], 1);
         }
-        for (int s = 0; s < B_STAGES; ++s) {
+        for (int s = 0; s < X_STAGES; ++s) {
             bar_init(&ctl.b_full[s], CG * TEAM_WARPS);
             bar_init(&ctl.b_empty[s], 1);
-        }
-        for (int s = 0; s < RAW_STAGES; ++s) {
-            bar_init(&ctl.raw_full[s], 2);
+            bar_init(&ctl.raw_full[s], 1);
             bar_init(&ctl.raw_empty[s], TEAM_WARPS);
         }
         for (int s = 0; s < 2; ++s) {
@@ -218,7 +200,7 @@ wgrad_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
     }
     if (wid == MULTIPLY) tmem_alloc<CG>(&ctl.tmem, 512);
     if (g.db && threadIdx.x < BK)                                // the columns of ones, which nothing overwrites
-        for (int s = 0; s < B_STAGES; ++s)
+        for (int s = 0; s < X_STAGES; ++s)
             for (uint32_t c = 0; c < ONES / 8; ++c)
                 sts16(b_at + s * OPERAND + unit_offset(threadIdx.x, g.h / 8 + c),
                       make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u));
@@ -236,13 +218,12 @@ wgrad_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
 
     if (wid >= LOAD) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(OTHER_REGISTERS));
-        const auto nothing = [](bool) { return true; };
         if (wid == LOAD) {
             uint32_t s = 0, parity = 1;
             int32_t x = 0;
             const uint32_t full0 = smem_addr(ctl.a_full), bar0 = CG == 1 ? full0 : leader_addr(full0);
             walk(g, worker,
-                 [&](uint32_t tile, uint32_t, uint32_t) {
+                 [&](uint32_t tile) {
                      x = ((tile / g.tiles_n) * CG + rank) * TILE_M;
                      return true;
                  },
@@ -260,8 +241,7 @@ wgrad_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
                          parity ^= 1;
                      }
                      return true;
-                 },
-                 nothing);
+                 });
             if (ctl.abort) {                                     // copies under way get time to land
                 const long long t0 = clock64();
                 while (clock64() - t0 < 20000000ll) {}
@@ -270,229 +250,237 @@ wgrad_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
             // This warp's loop is what the tensor cores wait for: it runs with all lanes, so that the descriptors can stay in
             // uniform registers, and one lane issues.
             const bool issues = elected();
-            uint32_t sa = 0, pa = 0, sb = 0, pb = 0, n = 0, idesc = 0, acc = 0, more = 0;
+            uint32_t sa = 0, pa = 0, sb = 0, pb = 0, n = 0;
             const uint64_t desc_a = operand_desc(a_at, true), desc_b = operand_desc(b_at, true);
-            uint64_t da = desc_a, db = desc_b;
-            walk(g, worker,
-                 [&](uint32_t tile, uint32_t, uint32_t) {
-                     const Columns<CG> c(g, tile % g.tiles_n);
-                     // bf16 operands, fp32 sums, outer dimensions consecutive, N and M
-                     idesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((c.width >> 3) << 17) |
-                             ((CG * TILE_M >> 4) << 24);
-                     return true;
-                 },
-                 [&](uint32_t, uint32_t) {
-                     if (!more) {                                // a chunk begins
-                         if (!bar_wait_warp(&ctl.acc_empty[n & 1], ((n >> 1) & 1) ^ 1, &ctl.abort)) return false;
-                         acc = tmem + (n & 1) * 256;
-                     }
-                     if (!bar_wait_warp(&ctl.a_full[sa], pa, &ctl.abort) || !bar_wait_warp(&ctl.b_full[sb], pb, &ctl.abort)) return false;
-                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                     if (issues) {
+            bool ok = true;
+            const uint64_t end = g.begin(worker + 1);
+            for (uint64_t u = g.begin(worker); ok && u < end;) {    // (as walk does; all blocks of a chunk are alike here)
+                const uint32_t tile = static_cast<uint32_t>(u / g.k_blocks);
+                const uint32_t first = static_cast<uint32_t>(u - static_cast<uint64_t>(tile) * g.k_blocks);
+                const uint32_t last = static_cast<uint32_t>(min(static_cast<uint64_t>(g.k_blocks), first + (end - u)));
+                u += last - first;
+                const Columns<CG> c(g, tile % g.tiles_n);
+                // bf16 operands, fp32 sums, outer dimensions consecutive, N and M
+                const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((c.width >> 3) << 17) |
+                                       ((CG * TILE_M >> 4) << 24);
+                for (uint32_t c0 = first; ok && c0 < last; c0 += g.chunk, ++n) {
+                    const uint32_t blocks = (min(c0 + g.chunk, last) - c0) * g.planes, acc = tmem + (n & 1) * 256;
+                    ok = bar_wait_warp(&ctl.acc_empty[n & 1], ((n >> 1) & 1) ^ 1, &ctl.abort);
+#pragma unroll 1
+                    for (uint32_t b = 0; ok && b < blocks; ++b) {
+                        // (both at once: a wait that need not wait takes 70 cycles)
+                        const bool a_there = bar_try_cta(&ctl.a_full[sa], pa), b_there = bar_try_cta(&ctl.b_full[sb], pb);
+                        ok = __all_sync(0xFFFFFFFFu, (a_there || bar_wait_cta(&ctl.a_full[sa], pa, &ctl.abort)) &&
+                                                         (b_there || bar_wait_cta(&ctl.b_full[sb], pb, &ctl.abort)));
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        if (issues && ok) {
+                            const uint64_t da = desc_a + sa * (OPERAND >> 4), db = desc_b + sb * (OPERAND >> 4);
 #pragma unroll
-                         for (uint32_t q = 0; q < BK / 16; ++q)
-                             mma<CG>(acc, da + q * (2048 >> 4), db + q * (2048 >> 4), idesc, q ? 1u : more);
-                         mma_commit<CG>(&ctl.a_empty[sa]);
-                         mma_commit<CG>(&ctl.b_empty[sb]);
-                     }
-                     more = 1;
-                     da += OPERAND >> 4;
-                     db += OPERAND >> 4;
-                     if (++sa == A_STAGES) {
-                         sa = 0;
-                         pa ^= 1;
-                         da = desc_a;
-                     }
-                     if (++sb == B_STAGES) {
-                         sb = 0;
-                         pb ^= 1;
-                         db = desc_b;
-                     }
+                            for (uint32_t q = 0; q < BK / 16; ++q)
+                                mma<CG>(acc, da + q * (2048 >> 4), db + q * (2048 >> 4), idesc, b | q);
+                            mma_commit<CG>(&ctl.a_empty[sa]);
+                            mma_commit<CG>(&ctl.b_empty[sb]);
+                        }
+                        if (++sa == A_STAGES) {
+                            sa = 0;
+                            pa ^= 1;
+                        }
+                        if (++sb == X_STAGES) {
+                            sb = 0;
+                            pb ^= 1;
+                        }
+                    }
+                    if (issues && ok) mma_commit<CG>(&ctl.acc_full[n & 1]);
+                }
+            }
+        } else if (wid == LOAD_X) {
+            uint32_t s = 0, parity = 1, j = 0;
+            walk(g, worker,
+                 [&](uint32_t tile) {
+                     j = (tile % g.tiles_n) * CG + rank;
                      return true;
                  },
-                 [&](bool) {
-                     if (issues) mma_commit<CG>(&ctl.acc_full[n & 1]);
-                     n += 1;
-                     more = 0;
+                 [&](uint32_t k, uint32_t) {
+                     if (!bar_wait_warp(&ctl.raw_empty[s], parity, &ctl.abort)) return false;
+                     if (lane == 0) {
+                         const uint32_t to = raws + s * RAW_BYTES, bar = smem_addr(&ctl.raw_full[s]);
+                         bar_expect(&ctl.raw_full[s], BK * g.code_pitch + STEP_BYTES);
+                         load_box<1>(to, &code_map, j * g.h, k * BK, bar);
+                         load_bytes(to + CODE_BYTES, g.steps + (static_cast<uint64_t>(j) * g.k_blocks + k) * BK, STEP_BYTES, bar);
+                     }
+                     if (++s == X_STAGES) {
+                         s = 0;
+                         parity ^= 1;
+                     }
                      return true;
                  });
-        } else if (wid >= FIRST_X) {
-            // Codes by box copy; steps by plain loads, two tokens a lane.  The two warps take turns, and a warp's loads are two of
-            // its blocks ahead of what it stores.
-            uint32_t e[2][2][5], x[2], y[2];
-            bool have[2];
-            Cursor cur(g, worker);
-            if (wid != FIRST_X) cur.advance(g, worker);
-            auto fetch = [&](int i) {
-                have[i] = !cur.done;
-                if (cur.done) return;
-                x[i] = ((cur.tile % g.tiles_n) * CG + rank) * g.h;
-                y[i] = cur.k * BK;
-                const uint32_t b = x[i] / BLOCK8;
-#pragma unroll
-                for (uint32_t l = 0; l < 2; ++l) {
-                    const uint32_t t = y[i] + l * 32 + lane;
-                    const uint8_t *p = g.exps + static_cast<uint64_t>(t) * g.blocks8 + b;
-#pragma unroll
-                    for (uint32_t j = 0; j < 5; ++j) e[i][l][j] = t < g.rows && b + j < g.blocks8 ? __ldg(p + j) : 0u;
-                }
-                cur.advance(g, worker);
-                if (!cur.done) cur.advance(g, worker);
-            };
-            fetch(0);
-            fetch(1);
-            uint32_t s = wid - FIRST_X, parity = 1;
-            auto store = [&](int i) {
-                if (!have[i] || !bar_wait_warp(&ctl.raw_empty[s], parity, &ctl.abort)) return false;
-                const uint32_t to = raws + s * RAW_BYTES;
-                if (lane == 0) {
-                    bar_expect(&ctl.raw_full[s], BK * g.code_pitch);
-                    load_box<1>(to, &code_map, x[i], y[i], smem_addr(&ctl.raw_full[s]));
-                }
-#pragma unroll
-                for (uint32_t l = 0; l < 2; ++l) {
-                    uint32_t w[4];
-#pragma unroll
-                    for (uint32_t j = 0; j < 5; ++j) e[i][l][j] = e[i][l][j] == 255u ? 0x7FC0u : e[i][l][j] << 7;
-                    // a tile begins at a block of 32 columns or in its middle
-#pragma unroll
-                    for (uint32_t u = 0; u < 4; ++u) w[u] = e[i][l][u] | (x[i] & 16 ? e[i][l][u + 1] : e[i][l][u]) << 16;
-                    sts16(to + CODE_BYTES + (l * 32 + lane) * 16, make_uint4(w[0], w[1], w[2], w[3]));
-                }
-                __syncwarp();
-                if (lane == 0) bar_arrive(&ctl.raw_full[s]);
-                s += 2;
-                if (s >= RAW_STAGES) {
-                    s -= RAW_STAGES;
-                    parity ^= 1;
-                }
-                fetch(i);
-                return true;
-            };
-            while (store(0) && store(1)) {}
         }
     } else if (wid >= FIRST_CONVERT) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(CONVERT_REGISTERS));
-        // A team of two warps converts every fourth block, a thread a token: lanes next to each other meet no bank
-        // conflicts, since rows of codes are an odd number of 16 bytes apart and the operand's units are permuted.
-        const uint32_t team = (wid - FIRST_CONVERT) / TEAM_WARPS, token = ((wid - FIRST_CONVERT) % TEAM_WARPS) * 32 + lane;
+        // A team of four warps converts every third block, a thread half a token's units, eight codes each.  No bank conflicts:
+        // rows of codes are an odd number of 16 bytes apart, and of eight lanes that store at a time the tokens are all even or all odd.
+        const uint32_t team = (wid - FIRST_CONVERT) / TEAM_WARPS, half = lane & 1;
+        const uint32_t token = ((wid - FIRST_CONVERT) % TEAM_WARPS) * 16 + (lane >> 4) * 8 + ((lane >> 1) & 3) * 2 + ((lane >> 3) & 1);
         const uint32_t per_row = g.h / 16;
-        const uint64_t u0 = g.units * worker / g.workers, u1 = g.units * (worker + 1) / g.workers;
-        const uint32_t to = b_at + team * OPERAND + unit_offset(token, 0);
-        uint32_t second = 0, raw_parity = 0, parity = 1;         // the team's second buffer of codes
+        const uint64_t u0 = g.begin(worker), u1 = g.begin(worker + 1);
+        const uint32_t to0 = b_at + unit_offset(token, half), from0 = raws + token * g.code_pitch + half * 8;
+        uint32_t r = team, parity = 0;                           // the team's two buffers take turns
         for (uint64_t left = (u1 - u0) * g.planes, n = team; n < left; n += TEAMS) {
-            const uint32_t r = team + second * TEAMS, from = raws + r * RAW_BYTES + token * g.code_pitch;
-            if (!bar_wait_warp(&ctl.raw_full[r], raw_parity, &ctl.abort)) break;
+            const uint32_t from = from0 + r * RAW_BYTES, to = to0 + r * OPERAND;
+            if (!bar_wait_warp(&ctl.raw_full[r], parity, &ctl.abort)) break;
             const uint4 st = lds16(raws + r * RAW_BYTES + CODE_BYTES + token * 16);
             const uint32_t step[4] = {st.x, st.y, st.z, st.w};
-            uint4 code = lds16(from);
-            if (!bar_wait_warp(&ctl.b_empty[team], parity, &ctl.abort)) break;
-            parity ^= 1;
+            uint2 code = lds8(from);
+            if (!bar_wait_warp(&ctl.b_empty[r], parity ^ 1, &ctl.abort)) break;
 #pragma unroll
             for (uint32_t c = 0; c < MAX_H / 16; ++c) {
                 if (c >= per_row) break;
-                const uint4 now = code;
-                if (c + 1 < MAX_H / 16) code = lds16(from + (c + 1) * 16);
+                const uint2 now = code;
+                if (c + 1 < MAX_H / 16) code = lds8(from + (c + 1) * 16);
                 const uint32_t twice = __byte_perm(step[c >> 1], 0, c & 1 ? 0x3232 : 0x1010);
-                // (unit 2 c of the row lies at 2 c exclusive-or token: the permutation of the row's first, turned)
-                const uint32_t at = (to ^ ((2 * c & 7) << 4)) + (c >> 2) * SLAB;
-                sts16(at, converted(now.x, now.y, twice));
-                sts16(at ^ 16, converted(now.z, now.w, twice));
+                // (unit 2 c + half of the row lies at that exclusive-or token: the permutation of the row's first, turned)
+                sts16((to ^ ((2 * c & 7) << 4)) + (c >> 2) * SLAB, converted(now.x, now.y, twice));
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) {
                 bar_arrive(&ctl.raw_empty[r]);
-                bar_arrive_leader_cta<CG>(&ctl.b_full[team]);
+                bar_arrive_leader_cta<CG>(&ctl.b_full[r]);
             }
-            raw_parity ^= second;
-            second ^= 1;
+            r += TEAMS;
+            if (r >= X_STAGES) {
+                r -= X_STAGES;
+                parity ^= 1;
+            }
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(SUM_REGISTERS));
         const uint32_t quad = wid & 3, side = wid >> 2;          // lanes of the tensor memory, half of the columns
-        float *staging = reinterpret_cast<float *>(raw + (raws - smem_addr(raw)) + RAW_STAGES * RAW_BYTES) + wid * STAGING_FLOATS;
-        float sum[GROUPS][32];                                   // this warp's half of the columns, a row a thread
+        float *staging = reinterpret_cast<float *>(raw + (raws - smem_addr(raw)) + X_STAGES * RAW_BYTES) + wid * STAGING_FLOATS;
+        float sum[SIDE];                                         // this warp's half of the columns, a row a thread
         uint32_t n = 0;
         bool dead = false;                                       // a wait has run out, NaN from here on
-        const uint64_t end = g.units * (worker + 1) / g.workers;
-        for (uint64_t u = g.units * worker / g.workers; u < end;) {      // (as walk does)
-            const uint32_t tile = static_cast<uint32_t>(u / g.k_blocks), nt = tile % g.tiles_n;
+        const uint64_t end = g.begin(worker + 1);
+        for (uint64_t u = g.begin(worker); u < end;) {           // (as walk does)
+            const uint32_t tile = static_cast<uint32_t>(u / g.k_blocks), nt = tile % g.tiles_n, mt = (tile / g.tiles_n) * CG + rank;
             const uint32_t first = static_cast<uint32_t>(u - static_cast<uint64_t>(tile) * g.k_blocks);
             const uint32_t last = static_cast<uint32_t>(min(static_cast<uint64_t>(g.k_blocks), first + (end - u)));
             u += last - first;
-#pragma unroll
-            for (uint32_t h = 0; h < GROUPS; ++h)
-#pragma unroll
-                for (int j = 0; j < 32; ++j) sum[h][j] = 0.f;
             const Columns<CG> c(g, nt);
-#pragma unroll 1
-            for (uint32_t c0 = first; c0 < last; c0 += g.chunk) {
-                const uint32_t as = n & 1;
-                if (!dead) dead = !bar_wait_warp(&ctl.acc_full[as], (n >> 1) & 1, &ctl.abort);
-                n += 1;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t mine = c.width > side * SIDE ? min(SIDE, c.width - side * SIDE) : 0;      // of this warp's columns
+            const uint32_t lanes = tmem + ((quad * 32) << 16) + side * SIDE;
+            const bool several = first + g.chunk < last;
 #pragma unroll
-                for (uint32_t h = 0; h < GROUPS; ++h) {
-#pragma unroll
-                    for (uint32_t p = 0; p < 32; p += 16) {
-                        if (side * SIDE + h * 32 + p >= c.width) continue;
-                        uint32_t v[16];
-                        __syncwarp();
-                        tmem_load16(tmem + ((quad * 32) << 16) + as * 256 + side * SIDE + h * 32 + p, v);
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) sum[h][p + j] += __uint_as_float(v[j]);
-                    }
-                }
+            for (uint32_t j = 0; j < SIDE; ++j) sum[j] = 0.f;
+            auto done = [&]() {
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) bar_arrive_leader_cta<CG>(&ctl.acc_empty[as]);
-            }
-            const uint32_t mt = (tile / g.tiles_n) * CG + rank;
-            const bool whole = last - first == g.k_blocks, from_top = first == 0;
-            const uint32_t o = mt * TILE_M + quad * 32 + lane, col0 = nt * CG * g.h;
-            float *slot = g.slots + ((worker * 2ull + from_top) * CG + rank) * (CG * MAX_HALF * TILE_M) + quad * 32 + lane;
+                if (lane == 0) bar_arrive_leader_cta<CG>(&ctl.acc_empty[n & 1]);
+                n += 1;
+            };
+            for (uint32_t c0 = first;;) {
+                if (!dead) dead = !bar_wait_warp(&ctl.acc_full[n & 1], (n >> 1) & 1, &ctl.abort);
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                if (several) {
 #pragma unroll
-            for (uint32_t h = 0; h < GROUPS; ++h) {
-                const uint32_t n0 = side * SIDE + h * 32;
-                if (n0 >= c.width) continue;
-                if (dead) {
+                    for (uint32_t p = 0; p < SIDE; p += 16) {
+                        if (p >= mine) break;
+                        uint32_t v[16];
+                        tmem_load16(lanes + (n & 1) * 256 + p, v);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) sum[h][j] = __uint_as_float(0x7FC00000u);
-                }
-                if (!whole) {
-#pragma unroll
-                    for (uint32_t j = 0; j < 32; ++j)
-                        if (n0 + j < c.width) __stcg(slot + (n0 + j) * TILE_M, sum[h][j]);
-                    continue;
-                }
-                if (g.transposed) {
-#pragma unroll
-                    for (uint32_t j = 0; j < 32; ++j)
-                        if (c.in(n0 + j) && col0 + c.col(n0 + j) < g.cols && o < g.out)
-                            store_grad<G>(g.dw, static_cast<uint64_t>(col0 + c.col(n0 + j)) * g.out + o, sum[h][j], g.accumulate);
-                } else {
-                    // a few columns at a time, so that neighbouring lanes write neighbouring entries
-#pragma unroll
-                    for (uint32_t p = 0; p < 32; p += STAGING_COLS) {
-                        const uint32_t at = n0 + p + (lane & (STAGING_COLS - 1)), col = col0 + c.col(at);
-                        const bool in = c.in(at) && col < g.cols;
-                        __syncwarp();
-#pragma unroll
-                        for (uint32_t j = 0; j < STAGING_COLS; ++j) staging[lane * (STAGING_COLS + 1) + j] = sum[h][p + j];
-                        __syncwarp();
-#pragma unroll 4
-                        for (uint32_t q = lane / STAGING_COLS; q < 32; q += 32 / STAGING_COLS) {
-                            const uint32_t row = mt * TILE_M + quad * 32 + q;
-                            if (in && row < g.out)
-                                store_grad<G>(g.dw, static_cast<uint64_t>(row) * g.cols + col,
-                                              staging[q * (STAGING_COLS + 1) + (lane & (STAGING_COLS - 1))], g.accumulate);
-                        }
+                        for (int j = 0; j < 16; ++j) sum[p + j] += __uint_as_float(v[j]);
                     }
                 }
-                if (c.ones && n0 <= c.h && c.h < n0 + 32 && o < g.out)               // the first column of ones
-                    store_grad<G>(g.db, o, c.h & 16 ? sum[h][16] : sum[h][0], g.accumulate);
+                c0 += g.chunk;
+                if (c0 >= last) break;
+                done();
             }
+            // The segment is complete.  Its sums go back to where its last chunk's were: from there a short loop can take them.
+            const uint32_t acc = lanes + (n & 1) * 256;
+            if (several) {
+#pragma unroll
+                for (uint32_t p = 0; p < SIDE; p += 16)
+                    if (p < mine) tmem_store16(acc + p, sum + p);
+                asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+            }
+            const bool whole = last - first == g.k_blocks;
+            const uint64_t top = static_cast<uint64_t>(tile) * g.k_blocks;
+            const uint32_t a = whole ? worker : owner(g, top), b = whole ? worker : owner(g, top + g.k_blocks - 1);
+            // (a range in which the tile begins has it in the second slot, one that begins inside the tile in the first)
+            auto slot = [&](uint32_t w) {
+                return g.slots + ((w * 2ull + (w == a)) * CG + rank) * (CG * MAX_HALF * TILE_M) + side * SIDE * TILE_M + quad * 32 + lane;
+            };
+            bool out = true;
+            if (!whole) {
+                float *to = slot(worker);
+#pragma unroll 1
+                for (uint32_t p = 0; p < mine; p += 16) {
+                    uint32_t v[16];
+                    tmem_load16(acc + p, v);
+#pragma unroll
+                    for (uint32_t j = 0; j < 16; ++j) __stcg(to + (p + j) * TILE_M, dead ? __uint_as_float(0x7FC00000u) : __uint_as_float(v[j]));
+                }
+                __threadfence();
+                __syncwarp();
+                uint32_t before = 0;
+                if (lane == 0) before = atomicAdd(g.arrived + (static_cast<uint64_t>(tile) * CG + rank) * SUM_WARPS + wid, 1u);
+                out = __shfl_sync(0xFFFFFFFFu, before, 0) == b - a;
+                __threadfence();
+            }
+#pragma unroll 1
+            for (uint32_t p = 0; out && p < mine; p += 16) {
+                uint32_t v[16];
+                float x[16];
+                tmem_load16(acc + p, v);
+                if (whole) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) x[j] = __uint_as_float(v[j]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) x[j] = 0.f;
+#pragma unroll 1
+                    for (uint32_t w = a; w <= b; ++w) {
+                        const float *part = slot(w) + p * TILE_M;
+                        float y[16];
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) y[j] = w == worker ? __uint_as_float(v[j]) : __ldcg(part + j * TILE_M);
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) x[j] += y[j];
+                    }
+                }
+                if (dead) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) x[j] = __uint_as_float(0x7FC00000u);
+                }
+                const uint32_t n0 = side * SIDE + p, col0 = nt * CG * g.h, o = mt * TILE_M + quad * 32 + lane;
+                if (c.ones && n0 == c.h) {                                           // (the columns of ones are all alike)
+                    if (o < g.out) store_grad<G>(g.db, o, x[0], g.accumulate);
+                    continue;
+                }
+                if (!c.in(n0)) continue;
+                const uint32_t col = col0 + c.col(n0);                               // of the sixteen, one behind the other
+                if (g.transposed) {
+#pragma unroll
+                    for (uint32_t j = 0; j < 16; ++j)
+                        if (col + j < g.cols && o < g.out)
+                            store_grad<G>(g.dw, static_cast<uint64_t>(col + j) * g.out + o, x[j], g.accumulate);
+                    continue;
+                }
+                // through shared memory, so that neighbouring lanes write neighbouring entries
+                __syncwarp();
+#pragma unroll
+                for (uint32_t j = 0; j < 16; ++j) staging[lane * (STAGING_COLS + 1) + j] = x[j];
+                __syncwarp();
+                const uint32_t at = col + (lane & 15);
+#pragma unroll 8
+                for (uint32_t q = lane >> 4; q < 32; q += 2) {
+                    const uint32_t row = mt * TILE_M + quad * 32 + q;
+                    if (at < g.cols && row < g.out)
+                        store_grad<G>(g.dw, static_cast<uint64_t>(row) * g.cols + at, staging[q * (STAGING_COLS + 1) + (lane & 15)],
+                                      g.accumulate);
+                }
+            }
+            done();
         }
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -507,55 +495,31 @@ wgrad_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
     }
 }
 
-// Tiles that lie in several workers' ranges: their parts added up in order, 32 columns and 128 rows a block of threads.
-template <int CG, typename G>
+// What the products need besides: the steps of X as bf16, 16 bytes per token and CTA's share of a tile's columns (0 beyond
+// the last token), and the parts' counters at 0.
 __global__ void __launch_bounds__(256)
-join_kernel(const Args g)
+prepare_kernel(const uint8_t *exps, uint32_t rows, uint32_t blocks8, uint32_t h, uint32_t shares, uint32_t tokens, uint4 *steps,
+               uint32_t *counters, uint32_t n_counters)
 {
-    __shared__ float s[32][TILE_M + 1];
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const uint32_t tile = blockIdx.x / CG, rank = blockIdx.x % CG, nt = tile % g.tiles_n, mt = (tile / g.tiles_n) * CG + rank;
-    const uint32_t n0 = blockIdx.y * 32;
-    const uint64_t first = static_cast<uint64_t>(tile) * g.k_blocks, last = first + g.k_blocks - 1;
-    auto owner = [&](uint64_t u) {                               // the worker whose range holds u
-        uint32_t c = static_cast<uint32_t>(u * g.workers / g.units);
-        while (g.units * (c + 1) / g.workers <= u) ++c;
-        while (g.units * c / g.workers > u) --c;
-        return c;
-    };
-    const uint32_t a = owner(first), b = owner(last);
-    const Columns<CG> c(g, nt);
-    if (a == b || n0 >= c.width) return;
-    const uint32_t row = threadIdx.x & (TILE_M - 1), j0 = threadIdx.x / TILE_M * 16;
-    float v[16];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const uint32_t first = blockIdx.x * 256 + threadIdx.x, all = gridDim.x * 256;
+    for (uint32_t i = first; i < n_counters; i += all) counters[i] = 0;
+    // (neighbouring threads take neighbouring shares of a token, whose bytes lie side by side)
+    const uint64_t n = static_cast<uint64_t>(shares) * tokens;
+    for (uint64_t i = first; i < n; i += all) {
+        const uint32_t t = static_cast<uint32_t>(i / shares), j = static_cast<uint32_t>(i - static_cast<uint64_t>(t) * shares);
+        uint32_t e[5];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) v[j] = 0.f;
-    for (uint32_t w = a; w <= b; ++w) {
-        // (a range in which the tile begins has it in the second slot, one that begins inside the tile in the first)
-        const float *p = g.slots + ((w * 2ull + (w == a)) * CG + rank) * (CG * MAX_HALF * TILE_M) + row;
-#pragma unroll
-        for (uint32_t j = 0; j < 16; ++j)
-            if (n0 + j0 + j < c.width) v[j] += __ldcg(p + (n0 + j0 + j) * TILE_M);
-    }
-    const uint32_t o = mt * TILE_M + row, col0 = nt * CG * g.h;
-    if (c.ones && n0 + j0 == c.h && o < g.out) store_grad<G>(g.db, o, v[0], g.accumulate);
-    if (g.transposed) {
-#pragma unroll
-        for (uint32_t j = 0; j < 16; ++j) {
-            const uint32_t n = n0 + j0 + j, col = col0 + c.col(n);
-            if (c.in(n) && col < g.cols && o < g.out)
-                store_grad<G>(g.dw, static_cast<uint64_t>(col) * g.out + o, v[j], g.accumulate);
+        for (uint32_t q = 0; q < 5; ++q) {
+            const uint32_t b = j * h / BLOCK8 + q;
+            e[q] = t < rows && b < blocks8 ? bf16_step(exps[static_cast<uint64_t>(t) * blocks8 + b]) : 0u;
         }
-        return;
-    }
+        // a share begins at a block of 32 columns or in its middle
+        uint32_t o[4];
 #pragma unroll
-    for (uint32_t j = 0; j < 16; ++j) s[j0 + j][row] = v[j];
-    __syncthreads();
-    const uint32_t lane = threadIdx.x & 31, col = col0 + c.col(n0 + lane);
-    const bool in = c.in(n0 + lane) && col < g.cols;
-    for (uint32_t r = threadIdx.x >> 5; r < TILE_M; r += 8)
-        if (in && mt * TILE_M + r < g.out)
-            store_grad<G>(g.dw, static_cast<uint64_t>(mt * TILE_M + r) * g.cols + col, s[lane][r], g.accumulate);
+        for (uint32_t u = 0; u < 4; ++u) o[u] = e[u] | ((j * h) & 16 ? e[u + 1] : e[u]) << 16;
+        steps[static_cast<uint64_t>(j) * tokens + t] = make_uint4(o[0], o[1], o[2], o[3]);
+    }
 }
 
 // dY as bf16 rows that start on 16 bytes, in planes of which each holds what the ones before it left; rows beyond the last are 0.
@@ -604,18 +568,20 @@ bool is_dtype(int32_t d) { return d == DECO_F32 || d == DECO_BF16; }
 struct Plan {
     uint32_t planes;                     // 0: dY is read where it is
     uint32_t plane_rows, pitch;
-    uint32_t cg, h, tiles_n, tiles_m, k_blocks, workers;
-    uint64_t units;
-    bool cut;                            // some tile lies in more than one range
+    uint32_t cg, h, tiles_n, tiles_m, k_blocks, workers, grain;
+    uint64_t tiles;
+    bool cut;                            // tiles may lie in more than one range
     uint64_t plane_bytes() const { return 2ull * planes * plane_rows * pitch; }
-    uint64_t bytes() const { return plane_bytes() + (cut ? 2ull * workers * cg * cg * MAX_HALF * TILE_M * 4 : 0); }
+    uint64_t slot_bytes() const { return cut ? 2ull * workers * cg * cg * MAX_HALF * TILE_M * 4 : 0; }
+    uint64_t counters() const { return cut ? tiles * cg * SUM_WARPS : 0; }
+    uint64_t step_bytes() const { return 16ull * tiles_n * cg * k_blocks * BK; }
+    uint64_t bytes() const { return plane_bytes() + step_bytes() + slot_bytes() + 4 * counters(); }
 };
 Plan make_plan(const void *dy, int32_t dtype, uint64_t rows, uint32_t out, uint64_t stride, uint32_t cols, int32_t grad_dtype)
 {
     Plan p = {};
     if (dtype == DECO_F32) p.planes = grad_dtype == DECO_F32 ? 3 : 2;
     else if (!aligned_to(dy, 16) || stride % 8 || stride >= (1ull << 39)) p.planes = 1;      // (what box copies can address)
-    p.plane_rows = static_cast<uint32_t>((rows + BK - 1) / BK * BK);
     p.pitch = (out + 7) / 8 * 8;
     p.k_blocks = static_cast<uint32_t>((rows + BK - 1) / BK);
     // Pairs of CTAs read half as much per product; small results are left to single CTAs, whose tiles are a quarter.
@@ -625,10 +591,31 @@ Plan make_plan(const void *dy, int32_t dtype, uint64_t rows, uint32_t out, uint6
     p.tiles_n = (cols + most - 1) / most;
     p.h = ((cols + p.tiles_n - 1) / p.tiles_n + unit - 1) / unit * 16;
     p.tiles_m = (out + p.cg * TILE_M - 1) / (p.cg * TILE_M);
-    const uint64_t tiles = static_cast<uint64_t>(p.tiles_m) * p.tiles_n;
-    p.units = tiles * p.k_blocks;
-    p.workers = static_cast<uint32_t>(std::min<uint64_t>(SMS / p.cg, std::max(tiles, p.units / MIN_BLOCKS)));
-    p.cut = p.units % p.workers || (p.units / p.workers) % p.k_blocks;
+    p.tiles = static_cast<uint64_t>(p.tiles_m) * p.tiles_n;
+    // How long the worker with most to do takes, in blocks: with whole tiles, with tiles in 2 to 8 equal parts (a part's way through
+    // memory takes as long as some blocks), or with all blocks dealt out evenly, wherever that cuts tiles.
+    const uint64_t most_workers = SMS / p.cg, kb = p.k_blocks;
+    uint64_t best = (p.tiles + most_workers - 1) / most_workers * kb;
+    uint32_t parts = 1;
+    for (uint32_t q = 2; q <= 8; ++q) {
+        const uint64_t grain = (kb + q - 1) / q, cost = (p.tiles * q + most_workers - 1) / most_workers * grain + PART_BLOCKS * (q - 1);
+        if (grain >= MIN_BLOCKS && cost < best) {
+            best = cost;
+            parts = q;
+        }
+    }
+    const uint64_t units = p.tiles * kb, even_workers = std::min(most_workers, std::max<uint64_t>(1, units / MIN_BLOCKS));
+    p.cut = parts > 1;
+    p.grain = static_cast<uint32_t>((kb + parts - 1) / parts);
+    if ((units + even_workers - 1) / even_workers + EVEN_BLOCKS < best) {
+        p.cut = true;
+        p.grain = 1;
+        p.workers = static_cast<uint32_t>(even_workers);
+    } else {
+        p.k_blocks = p.grain * parts;                            // (blocks beyond the last are zeros)
+        p.workers = static_cast<uint32_t>(std::min(p.tiles * parts, most_workers));
+    }
+    p.plane_rows = p.k_blocks * BK;
     return p;
 }
 
@@ -686,10 +673,7 @@ cudaError_t launch(void (*kernel)(P...), uint32_t cluster, dim3 grid, unsigned b
 template <int CG, typename G>
 cudaError_t launch_all(const CUtensorMap &map, const CUtensorMap &code_map, const Args &a, const Plan &p, cudaStream_t s)
 {
-    cudaError_t err = launch(wgrad_kernel<CG, G>, CG, dim3(p.workers * CG), THREADS, SMEM, s, map, code_map, a);
-    if (err == cudaSuccess && p.cut)
-        err = launch(join_kernel<CG, G>, 1, dim3(p.tiles_m * p.tiles_n * CG, CG * MAX_HALF / 32), 256, 0, s, a);
-    return err;
+    return launch(wgrad_kernel<CG, G>, CG, dim3(p.workers * CG), THREADS, SMEM, s, map, code_map, a);
 }
 
 }  // namespace
@@ -724,12 +708,10 @@ extern "C" deco_status deco_weight_grad8(const void *dy, int32_t dtype, uint64_t
     if (!dy || !aligned_to(dy, dtype == DECO_F32 ? 4 : 2) || dy_stride < out || dy_stride > MAX_STRIDE) return DECO_ERR_INVALID_ARG;
     if (!codes || !exponents || !aligned_to(codes, 16)) return DECO_ERR_INVALID_ARG;
     const Plan p = make_plan(dy, dtype, rows, out, dy_stride, cols, grad_dtype);
-    if (static_cast<uint64_t>(p.tiles_m) * p.tiles_n * p.cg > 0x7FFFFFFFull || static_cast<uint64_t>(p.planes) * p.plane_rows > 0x7FFFFFFFull)
+    if (p.tiles * p.cg * SUM_WARPS > 0x7FFFFFFFull || static_cast<uint64_t>(p.planes) * p.plane_rows > 0x7FFFFFFFull)
         return DECO_ERR_INVALID_ARG;
-    if (p.bytes()) {
-        if (!workspace || !aligned_to(workspace, 16)) return DECO_ERR_INVALID_ARG;
-        if (workspace_bytes < p.bytes()) return DECO_ERR_CAPACITY;
-    }
+    if (!workspace || !aligned_to(workspace, 16)) return DECO_ERR_INVALID_ARG;
+    if (workspace_bytes < p.bytes()) return DECO_ERR_CAPACITY;
     static const EncodeFn encode = encode_function();
     if (!encode || !allow_shared_memory()) return DECO_ERR_CUDA;
     const void *operand = p.planes ? workspace : dy;
@@ -742,9 +724,6 @@ extern "C" deco_status deco_weight_grad8(const void *dy, int32_t dtype, uint64_t
         !box_map(encode, &code_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, pitch, rows, pitch, code_pitch, CU_TENSOR_MAP_SWIZZLE_NONE))
         return DECO_ERR_CUDA;
     Args a = {};
-    a.exps = exponents;
-    a.rows = static_cast<uint32_t>(rows);
-    a.blocks8 = (cols + BLOCK8 - 1) / BLOCK8;
     a.out = out;
     a.cols = cols;
     a.h = p.h;
@@ -754,21 +733,32 @@ extern "C" deco_status deco_weight_grad8(const void *dy, int32_t dtype, uint64_t
     a.planes = std::max<uint32_t>(1, p.planes);
     a.plane_rows = p.plane_rows;
     a.chunk = grad_dtype == DECO_F32 ? CHUNK : p.k_blocks;       // (bf16 rounds by 2^-9: sums may be cut off)
-    a.units = p.units;
     a.workers = p.workers;
+    a.grain = p.grain;
+    a.grains = p.tiles * (p.k_blocks / p.grain);
     a.dw = dw;
     a.db = db;
     a.transposed = transposed != 0;
     a.accumulate = accumulate != 0;
-    a.slots = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + p.plane_bytes());
+    uint8_t *room = static_cast<uint8_t *>(workspace) + p.plane_bytes();
+    uint4 *steps = reinterpret_cast<uint4 *>(room);
+    a.steps = steps;
+    a.slots = reinterpret_cast<float *>(room + p.step_bytes());
+    a.arrived = reinterpret_cast<uint32_t *>(room + p.step_bytes() + p.slot_bytes());
+    const uint32_t shares = p.tiles_n * p.cg;
+    const uint64_t records = static_cast<uint64_t>(shares) * p.plane_rows;
+    prepare_kernel<<<static_cast<unsigned>(std::min<uint64_t>(8 * SMS, (records + 255) / 256)), 256, 0, s>>>(
+        exponents, static_cast<uint32_t>(rows), static_cast<uint32_t>(pitch / BLOCK8), p.h, shares, p.plane_rows, steps, a.arrived,
+        static_cast<uint32_t>(p.counters()));
+    if (cudaGetLastError() != cudaSuccess) return DECO_ERR_CUDA;
     if (p.planes) {
         const dim3 grid((p.pitch + 2047) / 2048, std::min<uint32_t>(p.plane_rows, 8 * SMS));
         __nv_bfloat16 *to = static_cast<__nv_bfloat16 *>(workspace);
         if (dtype == DECO_F32)
-            planes_kernel<float><<<grid, 256, 0, s>>>(static_cast<const float *>(dy), dy_stride, a.rows, out, p.pitch, p.planes,
+            planes_kernel<float><<<grid, 256, 0, s>>>(static_cast<const float *>(dy), dy_stride, static_cast<uint32_t>(rows), out, p.pitch, p.planes,
                                                       p.plane_rows, to);
         else
-            planes_kernel<__nv_bfloat16><<<grid, 256, 0, s>>>(static_cast<const __nv_bfloat16 *>(dy), dy_stride, a.rows, out, p.pitch,
+            planes_kernel<__nv_bfloat16><<<grid, 256, 0, s>>>(static_cast<const __nv_bfloat16 *>(dy), dy_stride, static_cast<uint32_t>(rows), out, p.pitch,
                                                               p.planes, p.plane_rows, to);
         if (cudaGetLastError() != cudaSuccess) return DECO_ERR_CUDA;
     }
