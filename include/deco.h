@@ -611,7 +611,7 @@ deco_status deco_orth_get_stats(deco_orth *h, void *stream, deco_orth_stats *out
  *
  * Rows.  x, y, dy, ... are [rows] x [cols] of `dtype` (deco_dtype), consecutive within a row, rows `stride` entries
  * apart (>= cols); any alignment of whole entries, else DECO_ERR_INVALID_ARG.  16-byte accesses are used where all rows of a
- * call start on 16 bytes and cols is a multiple of 8.  rows < 2^28, cols <= 2^24.  All pointers are DEVICE.  Sums are held
+ * call start on 16 bytes and are whole multiples of that.  rows < 2^28, cols <= 2^24.  All pointers are DEVICE.  Sums are held
  * in fp32.  The same inputs give the same bits.  Calls work on the CURRENT device, allocate nothing and keep nothing between calls;
  * calls that run at the same time need workspaces of their own.
  *

@@ -31,10 +31,13 @@
 #include <initializer_list>
 
 #include "deco.h"
+#include "deco_pairs.h"
 
 namespace cg = cooperative_groups;
 
 namespace {
+
+using namespace deco::pairs;
 
 constexpr int NT = 256;                  // threads of a CTA
 constexpr int WARPS = NT / 32;
@@ -90,32 +93,6 @@ __device__ __forceinline__ uint64_t item_key(float x, uint32_t idx)
     return (static_cast<uint64_t>(order_key(x)) << 32) | (0xFFFFFFFFu - idx);
 }
 
-// Two fp32 numbers in one register pair.
-__device__ __forceinline__ uint64_t pair(float a, float b)
-{
-    uint64_t v;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
-    return v;
-}
-__device__ __forceinline__ void unpair(uint64_t v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
-{
-    uint64_t d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
-{
-    uint64_t d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
-{
-    uint64_t d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
 __device__ __forceinline__ uint64_t ex2_2(uint64_t v)
 {
     float a, b;

@@ -1,10 +1,12 @@
 // deco_layernorm, deco_layernorm_grad, deco_pack8, deco_unpack8: layer norm with its gradient, and
 // activations put away in 8 bits.
 //
-// All four are bound by memory.  A row belongs to a group of warps.  A thread owns the same columns of every row of its
-// group: item i of thread t holds the V columns from (i * threads + t) * V.  V = 8 where every row of every
-// array starts on 16 bytes and the width is a multiple of 8 (16-byte accesses), V = 1 otherwise (any alignment, any
-// stride; consecutive lanes hold consecutive columns).  Either way a block of 32 columns lies in one warp.
+// All four are bound by memory; at 16 bits there are six entries a cycle and SM to be dealt with, so arithmetic goes by pairs of
+// fp32 numbers.  A row belongs to a group of warps.  A thread owns the same columns of every row of its group: where every
+// row of every array starts on 16 bytes, granules of 16 bytes (V = 4 or 8 entries), granule i of thread t from column
+// (i * threads + t) * V on, so that a warp's access is 512 consecutive bytes (two granules of 16 bytes side by side in a thread made
+// fp32 rows 1.7 times slower: every 32-byte sector is asked for twice); with V = 1 (any alignment, any stride) entry i is column
+// i * threads + t.  Either way a block of 32 columns lies in one warp.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <math.h>
@@ -15,68 +17,102 @@
 
 #include "deco.h"
 #include "deco_packed8.h"
+#include "deco_pairs.h"
 
 namespace {
 
+using namespace deco::pairs;
 using deco::BLOCK8;
+using deco::converted;
 
 constexpr uint32_t FULL = 0xFFFFFFFFu;
+constexpr int THREADS = 512;             // of a CTA whose groups go from row to row
+constexpr int ANY_ENTRIES = 16;          // of a thread that holds a part of a row of any alignment
 
 // ----------------------------------------------------------------------------- entries
 
-// `n` consecutive entries as fp32: V = 8 with 16-byte accesses, V = 1 with one of the entry's size.
-template <int V> __device__ __forceinline__ void get(const float *p, float (&v)[V])
+__device__ __forceinline__ float get1(const float *p) { return *p; }
+__device__ __forceinline__ float get1(const __nv_bfloat16 *p)
 {
-    if (V == 1) {
-        v[0] = *p;
-    } else {
-#pragma unroll
-        for (int i = 0; i < V / 4; ++i) {
-            const float4 w = reinterpret_cast<const float4 *>(p)[i];
-            v[4 * i] = w.x; v[4 * i + 1] = w.y; v[4 * i + 2] = w.z; v[4 * i + 3] = w.w;
-        }
-    }
+    return __uint_as_float(static_cast<uint32_t>(*reinterpret_cast<const unsigned short *>(p)) << 16);
 }
-template <int V> __device__ __forceinline__ void get(const __nv_bfloat16 *p, float (&v)[V])
-{
-    if (V == 1) {
-        v[0] = __uint_as_float(static_cast<uint32_t>(*reinterpret_cast<const unsigned short *>(p)) << 16);
-    } else {
-        const uint4 w = *reinterpret_cast<const uint4 *>(p);
-        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int i = 0; i < V / 2; ++i) {
-            v[2 * i] = __uint_as_float(u[i] << 16);
-            v[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
-        }
-    }
-}
-template <int V> __device__ __forceinline__ void put(float *p, const float (&v)[V])
-{
-    if (V == 1) {
-        *p = v[0];
-    } else {
-#pragma unroll
-        for (int i = 0; i < V / 4; ++i)
-            reinterpret_cast<float4 *>(p)[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-    }
-}
-template <int V> __device__ __forceinline__ void put(__nv_bfloat16 *p, const float (&v)[V])
-{
-    if (V == 1) {
-        *p = __float2bfloat16_rn(v[0]);
-    } else {
-        uint32_t u[4];
-#pragma unroll
-        for (int i = 0; i < V / 2; ++i) {
-            const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-            u[i] = *reinterpret_cast<const uint32_t *>(&b);
-        }
-        *reinterpret_cast<uint4 *>(p) = make_uint4(u[0], u[1], u[2], u[3]);
-    }
-}
+__device__ __forceinline__ void put1(float *p, float v) { *p = v; }
+__device__ __forceinline__ void put1(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
 __device__ __forceinline__ float rounded(float x, const float *) { return x; }
 __device__ __forceinline__ float rounded(float x, const __nv_bfloat16 *) { return __bfloat162float(__float2bfloat16_rn(x)); }
+
+// The entries of 16 bytes, as pairs.
+template <typename T> constexpr int VEC = 16 / sizeof(T);
+__device__ __forceinline__ void pairs_of(const uint4 &w, uint64_t *v, const float *)
+{
+    v[0] = pair(__uint_as_float(w.x), __uint_as_float(w.y));
+    v[1] = pair(__uint_as_float(w.z), __uint_as_float(w.w));
+}
+__device__ __forceinline__ void pairs_of(const uint4 &w, uint64_t *v, const __nv_bfloat16 *)
+{
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = pair(__uint_as_float(u[i] << 16), __uint_as_float(u[i] & 0xFFFF0000u));
+}
+__device__ __forceinline__ void put_granule(float *p, const uint64_t *v)
+{
+    float4 f;
+    unpair(v[0], f.x, f.y);
+    unpair(v[1], f.z, f.w);
+    *reinterpret_cast<float4 *>(p) = f;
+}
+__device__ __forceinline__ void put_granule(__nv_bfloat16 *p, const uint64_t *v)
+{
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float a, b;
+        unpair(v[i], a, b);
+        const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+        u[i] = *reinterpret_cast<const uint32_t *>(&h);
+    }
+    *reinterpret_cast<uint4 *>(p) = make_uint4(u[0], u[1], u[2], u[3]);
+}
+
+// N entries of a row that a thread owns, in pairs: pair i holds entries 2 i and 2 i + 1 of the thread.  Columns beyond the row
+// read as 0 and are not stored.
+template <int V, int N>
+struct Own {
+    uint32_t cols, threads, t;
+    __device__ __forceinline__ uint32_t col(int e) const { return (e / V * threads + t) * V + e % V; }
+    template <typename T> __device__ __forceinline__ void load(const T *p, bool live, uint64_t (&v)[N / 2]) const
+    {
+        static_assert(V == 1, "granules come through the ring");
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+            const uint32_t a = col(2 * i), b = col(2 * i + 1);
+            v[i] = pair(live && a < cols ? get1(p + a) : 0.f, live && b < cols ? get1(p + b) : 0.f);
+        }
+    }
+    template <typename T> __device__ __forceinline__ void store(T *p, bool live, const uint64_t (&v)[N / 2]) const
+    {
+        if (V > 1) {
+#pragma unroll
+            for (int e = 0; e < N; e += V)
+                if (live && col(e) < cols) put_granule(p + col(e), v + e / 2);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) {
+                float a, b;
+                unpair(v[i], a, b);
+                if (live && col(2 * i) < cols) put1(p + col(2 * i), a);
+                if (live && col(2 * i + 1) < cols) put1(p + col(2 * i + 1), b);
+            }
+        }
+    }
+    // pair i of an array of fp32 numbers per column
+    __device__ __forceinline__ uint64_t per_column(const float *p, float otherwise, int i) const
+    {
+        if (!p) return pair(otherwise, otherwise);
+        const uint32_t a = col(2 * i), b = col(2 * i + 1);
+        return pair(a < cols ? p[a] : otherwise, b < cols ? p[b] : otherwise);
+    }
+};
 
 __device__ __forceinline__ float warp_sum(float v)
 {
@@ -84,7 +120,25 @@ __device__ __forceinline__ float warp_sum(float v)
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(FULL, v, o);
     return v;
 }
+__device__ __forceinline__ float both(uint64_t v)
+{
+    float a, b;
+    unpair(v, a, b);
+    return a + b;
+}
+__device__ __forceinline__ uint64_t twice(float a) { return pair(a, a); }
 
+// Steps of a group that a thread has asked for ahead (16-byte accesses), in units of shared memory that are its alone.
+constexpr int AHEAD = 3;
+
+__device__ __forceinline__ void copy_async(uint32_t to, const void *from)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory");
+}
+template <int BYTES> __device__ __forceinline__ void copy_async_small(uint32_t to, const void *from)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" :: "r"(to), "l"(from), "n"(BYTES) : "memory");
+}
 // --------------------------------------------------------------------- 8-bit checkpoints
 
 // Exponent byte of a block whose largest magnitude has the bits `top` (sign cleared): the smallest b >= 1 for
@@ -98,89 +152,203 @@ __device__ __forceinline__ uint32_t exponent_byte(uint32_t top)
 }
 __device__ __forceinline__ uint32_t magnitude_bits(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
 
-// Store V entries (0 beyond the row's end) of a row's checkpoint; the warp together, `in` where there is something to
-// store.  Products with a power of two are exact, so each code is rounded once.
-template <int V>
-__device__ __forceinline__ void put_packed(int8_t *codes, uint8_t *exps, uint32_t col, bool in, const float (&v)[V])
+// x / 2^(b - 127) to the nearest integer, as the lowest byte: the product with a power of two is exact, and the sum with
+// 1.5 * 2^23 rounds it to an integer, ties to even, whose two's complement its lowest bits are.
+constexpr float TO_INTEGER = 12582912.f;
+__device__ __forceinline__ float inverse_step(uint32_t b) { return __uint_as_float((254u - b) << 23); }
+// Of the largest step, 64 are 2^128, which is no fp32 number: 63 are kept there.
+__device__ __forceinline__ float kept(float x, uint32_t b)
 {
-    uint32_t top = 0;
-#pragma unroll
-    for (int j = 0; j < V; ++j) top = max(top, in ? magnitude_bits(v[j]) : 0u);
-    if (V == 1) {
-        top = __reduce_max_sync(FULL, top);
-    } else {
-        top = max(top, __shfl_xor_sync(FULL, top, 1));
-        top = max(top, __shfl_xor_sync(FULL, top, 2));
-    }
-    if (!in) return;
-    const uint32_t b = exponent_byte(top);
-    const float inv = b == 255u ? 0.f : __uint_as_float((254u - b) << 23);
-    // 64 of the largest step are 2^128, which is no fp32 number: 63 are kept there
-    const int most = b == 249u ? 63 : 127;
-    uint32_t q[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j)                          // (a block that stands for NaN has codes of 0)
-        q[j] = static_cast<uint32_t>(b == 255u ? 0 : max(-most, min(most, __float2int_rn(v[j] * inv)))) & 0xFFu;
-    if (V == 1) {
-        codes[col] = static_cast<int8_t>(q[0]);
-    } else {
-        uint32_t w[V / 4 + 1];
-#pragma unroll
-        for (int i = 0; i < V / 4; ++i) w[i] = q[4 * i] | q[4 * i + 1] << 8 | q[4 * i + 2] << 16 | q[4 * i + 3] << 24;
-        *reinterpret_cast<uint2 *>(codes + col) = make_uint2(w[0], w[1 % (V / 4 + 1)]);
-    }
-    if (col % BLOCK8 == 0) exps[col / BLOCK8] = static_cast<uint8_t>(b);
+    const float most = 63.f * 0x1p122f;
+    return b == 249u ? fmaxf(-most, fminf(most, x)) : x;
 }
 
-__device__ __forceinline__ float step_of(uint32_t b) { return __uint_as_float(b == 255u ? 0x7FC00000u : b << 23); }
-
-// V entries of a row's checkpoint.
+// Checkpoint of V consecutive entries a thread owns of a row; the warp together, `in` where there is something to store (entries
+// beyond the row's end are 0).
 template <int V>
-__device__ __forceinline__ void get_packed(const int8_t *codes, const uint8_t *exps, uint32_t col, float (&v)[V])
+__device__ __forceinline__ void put_packed_granule(int8_t *codes, uint8_t *exps, uint32_t col, bool in, const uint64_t *v)
 {
-    const float step = step_of(exps[col / BLOCK8]);
-    if (V == 1) {
-        v[0] = static_cast<float>(codes[col]) * step;
-    } else {
-        const uint2 w = *reinterpret_cast<const uint2 *>(codes + col);
+    float f[V];
+    uint32_t top = 0;
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const uint32_t u = j < 4 ? w.x : w.y;
-            v[j] = static_cast<float>(static_cast<int>(u << (24 - 8 * (j & 3))) >> 24) * step;
+    for (int i = 0; i < V / 2; ++i) {
+        unpair(v[i], f[2 * i], f[2 * i + 1]);
+        top = max(top, max(magnitude_bits(f[2 * i]), magnitude_bits(f[2 * i + 1])));
+    }
+    top = in ? top : 0u;
+#pragma unroll
+    for (int o = 1; o < 32 / V; o *= 2) top = max(top, __shfl_xor_sync(FULL, top, o));
+    if (!in) return;
+    const uint32_t b = exponent_byte(top);
+    uint32_t w[V / 4];
+#pragma unroll
+    for (int i = 0; i < V / 4; ++i) w[i] = 0;            // (a block that stands for NaN has codes of 0)
+    if (b < 250u) {
+        const uint64_t inv = twice(inverse_step(b)), magic = twice(TO_INTEGER);
+        uint32_t q[V];
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+            float x, y;
+            unpair(fma2(b == 249u ? pair(kept(f[2 * i], b), kept(f[2 * i + 1], b)) : v[i], inv, magic), x, y);
+            q[2 * i] = __float_as_uint(x);
+            q[2 * i + 1] = __float_as_uint(y);
+        }
+#pragma unroll
+        for (int i = 0; i < V / 4; ++i)
+            w[i] = __byte_perm(__byte_perm(q[4 * i], q[4 * i + 1], 0x0040), __byte_perm(q[4 * i + 2], q[4 * i + 3], 0x0040), 0x5410);
+    }
+    if (V == 8) *reinterpret_cast<uint2 *>(codes + col) = make_uint2(w[0], w[V / 4 - 1]);
+    else *reinterpret_cast<uint32_t *>(codes + col) = w[0];
+    if (col % BLOCK8 == 0) exps[col / BLOCK8] = static_cast<uint8_t>(b);
+}
+__device__ __forceinline__ void put_packed1(int8_t *codes, uint8_t *exps, uint32_t col, bool in, float v)
+{
+    const uint32_t b = exponent_byte(__reduce_max_sync(FULL, in ? magnitude_bits(v) : 0u));
+    if (!in) return;
+    codes[col] = b < 250u ? static_cast<int8_t>(__float_as_uint(__fmaf_rn(kept(v, b), inverse_step(b), TO_INTEGER))) : int8_t(0);
+    if (col % BLOCK8 == 0) exps[col / BLOCK8] = static_cast<uint8_t>(b);
+}
+template <int V, int N>
+__device__ __forceinline__ void put_packed(const Own<V, N> &own, int8_t *codes, uint8_t *exps, bool live, const uint64_t (&v)[N / 2])
+{
+    const uint32_t end = (own.cols + BLOCK8 - 1) / BLOCK8 * BLOCK8;
+    if constexpr (V > 1) {
+#pragma unroll
+        for (int e = 0; e < N; e += V) put_packed_granule<V>(codes, exps, own.col(e), live && own.col(e) < end, v + e / 2);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+            float a, b;
+            unpair(v[i], a, b);
+            put_packed1(codes, exps, own.col(2 * i), live && own.col(2 * i) < end, a);
+            put_packed1(codes, exps, own.col(2 * i + 1), live && own.col(2 * i + 1) < end, b);
         }
     }
 }
+
+__device__ __forceinline__ float step_of(uint32_t b) { return __uint_as_float(b == 255u ? 0x7FC00000u : b << 23); }
+__device__ __forceinline__ float get_packed1(const int8_t *codes, const uint8_t *exps, uint32_t col)
+{
+    return static_cast<float>(codes[col]) * step_of(exps[col / BLOCK8]);
+}
+// Four codes and their exponent byte as pairs of fp32 numbers.  A code with its sign bit turned, in the place of the lowest
+// byte of 2^23, is 2^23 + 128 + code.
+__device__ __forceinline__ void values4(uint32_t codes, uint32_t b, uint64_t *v)
+{
+    const uint64_t step = twice(step_of(b)), off = twice(-8388736.f);
+    const uint32_t w = codes ^ 0x80808080u;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const float x = __uint_as_float(__byte_perm(w, 0x4B000000u, i ? 0x7542 : 0x7540));
+        const float y = __uint_as_float(__byte_perm(w, 0x4B000000u, i ? 0x7543 : 0x7541));
+        v[i] = mul2(add2(pair(x, y), off), step);
+    }
+}
+
+// Units of 32 V consecutive columns of a row, UNITS of them a warp's, their loads under way together.  (Measured, 32768 x 2048
+// bf16: 63 us to pack with one unit a warp.)
+constexpr int UNITS = 4;
+struct Place {
+    uint64_t row;
+    uint32_t col;
+    __device__ __forceinline__ Place(uint64_t unit, uint64_t units, uint32_t chunks, uint32_t width)
+    {
+        if (units <= 0xFFFFFFFFull) row = static_cast<uint32_t>(unit) / chunks;
+        else row = unit / chunks;
+        col = static_cast<uint32_t>(unit - row * chunks) * width;
+    }
+};
 
 template <typename T, int V>
 __global__ void __launch_bounds__(256)
 pack_kernel(const T *x, uint64_t stride, uint32_t cols, uint32_t chunks, uint64_t units, int8_t *codes, uint8_t *exps)
 {
-    // a unit is 32 * V consecutive columns of a row, a warp's
-    const uint64_t unit = static_cast<uint64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
-    if (unit >= units) return;
-    const uint64_t row = unit / chunks;
-    const uint32_t col = static_cast<uint32_t>(unit - row * chunks) * (32 * V) + (threadIdx.x & 31) * V;
-    const uint32_t blocks = (cols + BLOCK8 - 1) / BLOCK8;
-    float v[V];
+    const uint64_t first = (static_cast<uint64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5)) * UNITS;
+    const uint32_t lane = threadIdx.x & 31, blocks = (cols + BLOCK8 - 1) / BLOCK8;
+    uint4 g[UNITS];
+    float f[UNITS];
+    uint64_t row[UNITS];
+    uint32_t col[UNITS];
+    Place at(first, units, chunks, 32 * V);
 #pragma unroll
-    for (int j = 0; j < V; ++j) v[j] = 0.f;
-    if (col < cols) get<V>(x + row * stride + col, v);
-    put_packed<V>(codes + row * blocks * BLOCK8, exps + row * blocks, col, col < blocks * BLOCK8, v);
+    for (int i = 0; i < UNITS; ++i) {
+        row[i] = at.row;
+        col[i] = at.col + lane * V;
+        f[i] = 0.f;
+        g[i] = make_uint4(0, 0, 0, 0);
+        if (first + i < units && col[i] < cols) {
+            if (V > 1) g[i] = *reinterpret_cast<const uint4 *>(x + row[i] * stride + col[i]);
+            else f[i] = get1(x + row[i] * stride + col[i]);
+        }
+        at.col += 32 * V;
+        if (at.col >= chunks * (32 * V)) {
+            at.col = 0;
+            at.row += 1;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) {
+        const bool in = first + i < units && col[i] < blocks * BLOCK8;
+        int8_t *c = codes + row[i] * blocks * BLOCK8;
+        uint8_t *e = exps + row[i] * blocks;
+        if constexpr (V > 1) {
+            uint64_t v[V / 2];
+            pairs_of(g[i], v, x);
+            put_packed_granule<V>(c, e, col[i], in, v);
+        } else {
+            put_packed1(c, e, col[i], in, f[i]);
+        }
+    }
+}
+
+__device__ __forceinline__ void put_values(float *p, uint2 codes, uint32_t b)
+{
+    uint64_t v[2];
+    values4(codes.x, b, v);
+    put_granule(p, v);
+}
+__device__ __forceinline__ void put_values(__nv_bfloat16 *p, uint2 codes, uint32_t b)
+{
+    *reinterpret_cast<uint4 *>(p) = converted(codes.x, codes.y, deco::bf16_step(b) * 0x10001u);
 }
 
 template <typename T, int V>
 __global__ void __launch_bounds__(256)
 unpack_kernel(const int8_t *codes, const uint8_t *exps, uint32_t cols, uint32_t chunks, uint64_t units, T *y, uint64_t stride)
 {
-    const uint64_t unit = static_cast<uint64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
-    if (unit >= units) return;
-    const uint64_t row = unit / chunks;
-    const uint32_t col = static_cast<uint32_t>(unit - row * chunks) * (32 * V) + (threadIdx.x & 31) * V;
-    const uint32_t blocks = (cols + BLOCK8 - 1) / BLOCK8;
-    if (col >= cols) return;
-    float v[V];
-    get_packed<V>(codes + row * blocks * BLOCK8, exps + row * blocks, col, v);
-    put<V>(y + row * stride + col, v);
+    const uint64_t first = (static_cast<uint64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5)) * UNITS;
+    const uint32_t lane = threadIdx.x & 31, blocks = (cols + BLOCK8 - 1) / BLOCK8;
+    uint2 c[UNITS];
+    uint32_t e[UNITS], col[UNITS];
+    uint64_t row[UNITS];
+    Place at(first, units, chunks, 32 * V);
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) {
+        row[i] = at.row;
+        col[i] = at.col + lane * V;
+        c[i] = make_uint2(0, 0);
+        e[i] = 0;
+        if (first + i >= units) col[i] = cols;
+        if (col[i] < cols) {
+            const int8_t *p = codes + row[i] * blocks * BLOCK8 + col[i];
+            if (V == 8) c[i] = *reinterpret_cast<const uint2 *>(p);
+            else if (V == 4) c[i].x = *reinterpret_cast<const uint32_t *>(p);
+            else c[i].x = static_cast<uint32_t>(static_cast<int>(*p));
+            e[i] = exps[row[i] * blocks + col[i] / BLOCK8];
+        }
+        at.col += 32 * V;
+        if (at.col >= chunks * (32 * V)) {
+            at.col = 0;
+            at.row += 1;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) {
+        if (col[i] >= cols) continue;
+        T *p = y + row[i] * stride + col[i];
+        if (V > 1) put_values(p, c[i], e[i]);
+        else put1(p, static_cast<float>(static_cast<int>(c[i].x)) * step_of(e[i]));
+    }
 }
 
 // ------------------------------------------------------------------------------ layer norm
@@ -193,128 +361,227 @@ struct NormArgs {
     float *mean, *rstd;
     int8_t *codes;
     uint8_t *exps;
-    float eps;
+    float eps, inv_cols;
     uint32_t cols, warps;                // warps of a row's group
 };
 
-// Statistics of the entries of some warp: count, mean, sum of squared deviations from it.
-struct Moments {
-    float n, mean, m2;
+// Statistics of the entries of some warp: count, mean (as a number and what is left of it), sum of squared deviations from it.
+struct __align__(16) Moments {
+    float n, mean, rest, m2;
 };
 
-// Of a group of `warps` warps from their own, in every thread.  Means are joined as differences from the first, so that a
-// common offset of the row costs no digits.
-__device__ __forceinline__ Moments join(const Moments *m, uint32_t warps)
+// Of a group of `warps` warps (up to WIDTH) from their own, in every thread; the warp together.  Means are joined as differences from
+// the first, so that a common offset of the row costs no digits.
+template <int WIDTH>
+__device__ __forceinline__ Moments join(const Moments *m, uint32_t warps, float inv_cols)
 {
+    const uint32_t i = threadIdx.x & (WIDTH - 1);
     const float base = m[0].mean;
-    float n = 0.f, sum = 0.f;
-    for (uint32_t w = 0; w < warps; ++w) {
-        n += m[w].n;
-        sum = __fmaf_rn(m[w].n, m[w].mean - base, sum);
+    const Moments a = i < warps ? m[i] : Moments{0.f, base, 0.f, 0.f};
+    const float d = a.mean - base + a.rest;
+    float sum = a.n * d;
+#pragma unroll
+    for (int o = 1; o < WIDTH; o *= 2) sum += __shfl_xor_sync(FULL, sum, o);
+    const float off = sum * inv_cols, e = d - off;
+    float m2 = __fmaf_rn(a.n * e, e, a.m2);
+#pragma unroll
+    for (int o = 1; o < WIDTH; o *= 2) m2 += __shfl_xor_sync(FULL, m2, o);
+    return {0.f, base + off, 0.f, m2};
+}
+__device__ __forceinline__ float reciprocal(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// One step of Newton's method on the approximate root's reciprocal: within 2 roundings.
+__device__ __forceinline__ float root_reciprocal(float v)
+{
+    const float y = rsqrtf(v);
+    return __fmaf_rn(0.5f * y, __fmaf_rn(-v * y, y, 1.f), y);
+}
+// Of a warp's entries in pairs, `n` of them: those beyond the row are 0 and counted out by `mask` (a bit a pair's entry).
+template <int N>
+__device__ __forceinline__ Moments warp_moments(const uint64_t (&v)[N / 2], float n, bool whole, uint32_t mask)
+{
+    uint64_t s = 0;
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) s = add2(s, v[i]);
+    const float inv = reciprocal(fmaxf(n, 1.f)), m = warp_sum(both(s)) * inv;
+    const uint64_t mm = twice(-m);
+    uint64_t d1 = 0, d2 = 0;
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+        uint64_t d = add2(v[i], mm);
+        if (!whole) {
+            float p, q;
+            unpair(d, p, q);
+            d = pair(mask >> (2 * i) & 1 ? p : 0.f, mask >> (2 * i + 1) & 1 ? q : 0.f);
+        }
+        d1 = add2(d1, d);
+        d2 = fma2(d, d, d2);
     }
-    const float off = sum / n;
-    float m2 = 0.f;
-    for (uint32_t w = 0; w < warps; ++w) {
-        const float d = m[w].mean - base - off;
-        m2 += __fmaf_rn(m[w].n * d, d, m[w].m2);
-    }
-    return {n, base + off, m2};
+    const float t1 = warp_sum(both(d1)), t2 = warp_sum(both(d2)), rest = t1 * inv, m2 = __fmaf_rn(-t1, rest, t2);
+    return {n, m, rest, m2 < 0.f ? 0.f : m2};                    // (a NaN stays)
 }
 
-// One pass: the row stays in registers between its statistics and its output.  Deviations are summed from the warp's own
-// mean, and what rounding did to that mean is taken back by their sum.
-template <typename T, int V, int ITEMS, bool ADD, bool KEEP>
-__global__ void __launch_bounds__(1024)
+// One pass: a row stays in registers between its statistics and its output.  Deviations are summed from the warp's own mean,
+// and what rounding did to that mean is taken back by their sum.  Every group goes from row to row; what keeps memory busy
+// between a row's arrival and its output are the copies of the group's next rows, in shared memory that is each thread's alone.
+template <typename T, bool ADD, bool KEEP, int E>
+__global__ void __launch_bounds__(THREADS, E == 8 ? 2 : 1)
 norm_kernel(const NormArgs a)
 {
-    __shared__ Moments moments[32];
+    constexpr int V = VEC<T>, A = AHEAD, U = ADD ? 2 : 1, G = E / V;
+    extern __shared__ uint4 ring[];                              // [A][G][U][thread]
+    __shared__ Moments moments[2][THREADS / 32];                 // (a warp may be one row ahead of the group's others)
+    const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5, group = wid / a.warps, groups = (blockDim.x >> 5) / a.warps;
+    const uint32_t threads = a.warps * 32, t = threadIdx.x - group * threads, cols = a.cols, all = blockDim.x;
+    const uint32_t blocks = (cols + BLOCK8 - 1) / BLOCK8;
+    const Own<V, E> own = {cols, threads, t};
+    uint64_t w[E / 2], b[E / 2];
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) {
+        w[i] = own.per_column(a.weight, 1.f, i);
+        b[i] = own.per_column(a.bias, 0.f, i);
+    }
+    float n = 0.f;                                               // the warp's entries
+    uint32_t mask = 0;
+#pragma unroll
+    for (int e = 0; e < E; e += V) {
+        const uint32_t c0 = own.col(e) - lane * V;
+        if (c0 < cols) n += static_cast<float>(min(cols - c0, 32u * V));
+        if (own.col(e) < cols) mask |= ((1u << V) - 1) << e;
+    }
+    const bool whole = __all_sync(FULL, mask == (1u << E) - 1);
+    uint4 *mine = ring + threadIdx.x;
+    const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(mine));
+    // (columns beyond the last stay 0 in the ring)
+    for (uint32_t u = 0; u < A * G * U; ++u) mine[u * all] = make_uint4(0, 0, 0, 0);
+    const uint64_t step = static_cast<uint64_t>(gridDim.x) * groups;
+    uint64_t row = static_cast<uint64_t>(blockIdx.x) * groups + group, next = row;
+    const T *x_next = static_cast<const T *>(a.x) + row * a.x_stride, *add_next = static_cast<const T *>(a.add) + row * a.add_stride;
+    T *y = static_cast<T *>(a.y) + row * a.y_stride, *sum = static_cast<T *>(a.sum) + row * a.sum_stride;
+    auto ask = [&](uint32_t s) {
+        if (next < a.rows) {
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                const uint32_t col = own.col(V * g), at = to + (s * G + g) * U * all * 16;
+                if (col >= cols) continue;
+                copy_async(at, x_next + col);
+                if (ADD) copy_async(at + all * 16, add_next + col);
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        next += step;
+        x_next += step * a.x_stride;
+        if (ADD) add_next += step * a.add_stride;
+    };
+#pragma unroll
+    for (int s = 0; s < A; ++s) ask(s);
+    uint32_t parity = 0, s = 0;
+    for (; row < a.rows; row += step) {
+        asm volatile("cp.async.wait_group %0;" :: "n"(A - 1) : "memory");
+        uint64_t v[E / 2];
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            const uint4 *q = mine + (s * G + g) * U * all;
+            pairs_of(*q, v + V / 2 * g, y);
+            if (ADD) {
+                uint64_t r[V / 2];
+                pairs_of(q[all], r, y);
+#pragma unroll
+                for (int i = 0; i < V / 2; ++i) {
+                    float f, h;
+                    unpair(add2(v[V / 2 * g + i], r[i]), f, h);
+                    v[V / 2 * g + i] = pair(rounded(f, y), rounded(h, y));
+                }
+            }
+        }
+        ask(s);
+        s = s + 1 == A ? 0 : s + 1;
+        if (ADD) {
+            if (a.sum) own.store(sum, true, v);
+            sum += step * a.sum_stride;
+        }
+        Moments mo = warp_moments<E>(v, n, whole, mask);
+        float mean = mo.mean + mo.rest;
+        if (a.warps > 1) {
+            if (lane == 0) moments[parity][wid] = mo;
+            asm volatile("bar.sync %0, %1;" :: "r"(1 + group), "r"(threads) : "memory");
+            mo = join<THREADS / 32>(moments[parity] + group * a.warps, a.warps, a.inv_cols);
+            mean = mo.mean;
+            parity ^= 1;
+        }
+        const float rstd = root_reciprocal(__fmaf_rn(mo.m2, a.inv_cols, a.eps));
+        if (t == 0) {
+            if (a.mean) a.mean[row] = mean;
+            if (a.rstd) a.rstd[row] = rstd;
+        }
+        if (KEEP) put_packed(own, a.codes + row * blocks * BLOCK8, a.exps + row * blocks, true, v);
+        const uint64_t mm = twice(-mean), rr = twice(rstd);
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) v[i] = fma2(mul2(add2(v[i], mm), rr), w[i], b[i]);
+        own.store(y, true, v);
+        y += step * a.y_stride;
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+}
+
+// The same for rows and columns of any alignment, and for more columns than that: every group a row, up to 1024 threads.
+template <typename T, bool ADD, bool KEEP, int BLOCK>
+__global__ void __launch_bounds__(BLOCK, BLOCK == 256 ? 3 : 1)
+norm_any_kernel(const NormArgs a)
+{
+    constexpr int N = ANY_ENTRIES;
+    __shared__ Moments moments[BLOCK / 32];
     const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5, group = wid / a.warps;
     const uint32_t threads = a.warps * 32, t = threadIdx.x - group * threads, cols = a.cols;
     const uint64_t row = static_cast<uint64_t>(blockIdx.x) * ((blockDim.x >> 5) / a.warps) + group;
     const bool live = row < a.rows;
+    const Own<1, N> own = {cols, threads, t};
     const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
-    const T *add = static_cast<const T *>(a.add) + row * a.add_stride;
-    T *sum = static_cast<T *>(a.sum) + row * a.sum_stride;
-    float v[ITEMS][V];
-    float s = 0.f, n = 0.f;
-#pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-        const uint32_t col = (i * threads + t) * V;
-#pragma unroll
-        for (int j = 0; j < V; ++j) v[i][j] = 0.f;
-        if (live && col < cols) get<V>(x + col, v[i]);
-    }
+    uint64_t v[N / 2];
+    own.load(x, live, v);
     if (ADD) {
-        float w[ITEMS][V];
+        uint64_t w[N / 2];
+        own.load(static_cast<const T *>(a.add) + row * a.add_stride, live, w);
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i) {
-            const uint32_t col = (i * threads + t) * V;
-#pragma unroll
-            for (int j = 0; j < V; ++j) w[i][j] = 0.f;
-            if (live && col < cols) get<V>(add + col, w[i]);
+        for (int i = 0; i < N / 2; ++i) {
+            float p, q;
+            unpair(add2(v[i], w[i]), p, q);
+            v[i] = pair(rounded(p, x), rounded(q, x));
         }
-#pragma unroll
-        for (int i = 0; i < ITEMS; ++i) {
-            const uint32_t col = (i * threads + t) * V;
-#pragma unroll
-            for (int j = 0; j < V; ++j) v[i][j] = rounded(v[i][j] + w[i][j], x);
-            if (live && col < cols && a.sum) put<V>(sum + col, v[i]);
-        }
+        if (a.sum) own.store(static_cast<T *>(a.sum) + row * a.sum_stride, live, v);
     }
+    float n = 0.f;
+    uint32_t mask = 0;
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-        const uint32_t c0 = (i * threads + t - lane) * V;        // the warp's first column
-        if (c0 < cols) n += static_cast<float>(min(cols - c0, 32u * V));
-#pragma unroll
-        for (int j = 0; j < V; ++j) s += v[i][j];
+    for (int e = 0; e < N; ++e) {
+        const uint32_t c0 = own.col(e) - lane;
+        if (c0 < cols) n += static_cast<float>(min(cols - c0, 32u));
+        if (own.col(e) < cols) mask |= 1u << e;
     }
-    const float m = warp_sum(s) / fmaxf(n, 1.f);
-    float d1 = 0.f, d2 = 0.f;
-#pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-        if ((i * threads + t) * V < cols) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const float d = v[i][j] - m;
-                d1 += d;
-                d2 = __fmaf_rn(d, d, d2);
-            }
-        }
-    }
-    d1 = warp_sum(d1);
-    d2 = warp_sum(d2);
-    const float rest = d1 / fmaxf(n, 1.f);
-    const float m2 = __fmaf_rn(-d1, rest, d2);
-    Moments mo = {n, m + rest, m2 < 0.f ? 0.f : m2};             // (a NaN stays)
+    Moments mo = warp_moments<N>(v, n, false, mask);
+    float mean = mo.mean + mo.rest;
     if (a.warps > 1) {
         if (lane == 0) moments[wid] = mo;
         __syncthreads();
-        mo = join(moments + group * a.warps, a.warps);
+        mo = join<32>(moments + group * a.warps, a.warps, a.inv_cols);
+        mean = mo.mean;
     }
-    const float rstd = 1.f / sqrtf(mo.m2 / mo.n + a.eps);
+    const float rstd = root_reciprocal(__fmaf_rn(mo.m2, a.inv_cols, a.eps));
     if (live && t == 0) {
-        if (a.mean) a.mean[row] = mo.mean;
+        if (a.mean) a.mean[row] = mean;
         if (a.rstd) a.rstd[row] = rstd;
     }
-    T *y = static_cast<T *>(a.y) + row * a.y_stride;
     const uint32_t blocks = (cols + BLOCK8 - 1) / BLOCK8;
+    if (KEEP) put_packed(own, a.codes + row * blocks * BLOCK8, a.exps + row * blocks, live, v);
+    const uint64_t mm = twice(-mean), rr = twice(rstd);
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-        const uint32_t col = (i * threads + t) * V;
-        if (KEEP) put_packed<V>(a.codes + row * blocks * BLOCK8, a.exps + row * blocks, col, live && col < blocks * BLOCK8, v[i]);
-        if (!live || col >= cols) continue;
-        float w[V], b[V], o[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            w[j] = 1.f;
-            b[j] = 0.f;
-        }
-        if (a.weight) get<V>(a.weight + col, w);
-        if (a.bias) get<V>(a.bias + col, b);
-#pragma unroll
-        for (int j = 0; j < V; ++j) o[j] = __fmaf_rn((v[i][j] - mo.mean) * rstd, w[j], b[j]);
-        put<V>(y + col, o);
-    }
+    for (int i = 0; i < N / 2; ++i)
+        v[i] = fma2(mul2(add2(v[i], mm), rr), own.per_column(a.weight, 1.f, i), own.per_column(a.bias, 0.f, i));
+    own.store(static_cast<T *>(a.y) + row * a.y_stride, live, v);
 }
 
 // Rows that do not fit the registers of 1024 threads: one CTA a row, which reads it once for its sum, once for its
@@ -330,11 +597,8 @@ norm_wide_kernel(const NormArgs a)
     const T *add = a.add ? static_cast<const T *>(a.add) + row * a.add_stride : nullptr;
     T *sum = a.sum ? static_cast<T *>(a.sum) + row * a.sum_stride : nullptr;
     auto value = [&](uint32_t col) {
-        float v[1], w[1];
-        get<1>(x + col, v);
-        if (!add) return v[0];
-        get<1>(add + col, w);
-        return rounded(v[0] + w[0], x);
+        const float v = get1(x + col);
+        return add ? rounded(v + get1(add + col), x) : v;
     };
     // the sum may be stored over x or add: the output pass stores it, entry by entry
     float s = 0.f, n = 0.f;
@@ -351,10 +615,10 @@ norm_wide_kernel(const NormArgs a)
     d2 = warp_sum(d2);
     const float rest = d1 / n;
     const float m2 = __fmaf_rn(-d1, rest, d2);
-    if (lane == 0) moments[wid] = {n, m + rest, m2 < 0.f ? 0.f : m2};
+    if (lane == 0) moments[wid] = {n, m, rest, m2 < 0.f ? 0.f : m2};
     __syncthreads();
-    const Moments mo = join(moments, 32);
-    const float rstd = 1.f / sqrtf(mo.m2 / mo.n + a.eps);
+    const Moments mo = join<32>(moments, 32, a.inv_cols);
+    const float rstd = root_reciprocal(__fmaf_rn(mo.m2, a.inv_cols, a.eps));
     if (t == 0) {
         if (a.mean) a.mean[row] = mo.mean;
         if (a.rstd) a.rstd[row] = rstd;
@@ -362,13 +626,11 @@ norm_wide_kernel(const NormArgs a)
     T *y = static_cast<T *>(a.y) + row * a.y_stride;
     const uint32_t blocks = (cols + BLOCK8 - 1) / BLOCK8;
     for (uint32_t col = t; col - lane < cols; col += 1024) {
-        float v[1] = {0.f};
-        if (col < cols) v[0] = value(col);
-        if (a.codes) put_packed<1>(a.codes + row * blocks * BLOCK8, a.exps + row * blocks, col, col < blocks * BLOCK8, v);
+        const float v = col < cols ? value(col) : 0.f;
+        if (a.codes) put_packed1(a.codes + row * blocks * BLOCK8, a.exps + row * blocks, col, col < blocks * BLOCK8, v);
         if (col >= cols) continue;
-        if (sum) put<1>(sum + col, v);
-        const float o[1] = {__fmaf_rn((v[0] - mo.mean) * rstd, a.weight ? a.weight[col] : 1.f, a.bias ? a.bias[col] : 0.f)};
-        put<1>(y + col, o);
+        if (sum) put1(sum + col, v);
+        put1(y + col, __fmaf_rn((v - mo.mean) * rstd, a.weight ? a.weight[col] : 1.f, a.bias ? a.bias[col] : 0.f));
     }
 }
 
@@ -386,144 +648,255 @@ struct NormGradArgs {
     uint32_t cols, warps;
 };
 
-constexpr int E = 8;                     // entries of a row that a thread holds
 
-template <typename T, int V>
-__device__ __forceinline__ void get_row(const NormGradArgs &a, const void *base, uint64_t stride, uint64_t row, uint32_t t,
-                                        uint32_t threads, float (&v)[E])
+template <typename T> constexpr int GRAD_AHEAD = VEC<T> == 8 ? 3 : 2;    // (what fits shared memory twice)
+
+// Four weights that start on 16 bytes.
+__device__ __forceinline__ uint4 quad_of(const float *p, uint32_t col, uint32_t cols)
 {
-    const T *p = static_cast<const T *>(base) + row * stride;
-#pragma unroll
-    for (int i = 0; i < E / V; ++i) {
-        const uint32_t col = (i * threads + t) * V;
-        float w[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) w[j] = 0.f;
-        if (col < a.cols) get<V>(p + col, w);
-#pragma unroll
-        for (int j = 0; j < V; ++j) v[i * V + j] = w[j];
-    }
-}
-template <typename T, int V, bool PACKED>
-__device__ __forceinline__ void get_x(const NormGradArgs &a, uint64_t row, uint32_t t, uint32_t threads, float (&v)[E])
-{
-    if (!PACKED) {
-        get_row<T, V>(a, a.x, a.x_stride, row, t, threads, v);
-        return;
-    }
-    const uint32_t blocks = (a.cols + BLOCK8 - 1) / BLOCK8;
-#pragma unroll
-    for (int i = 0; i < E / V; ++i) {
-        const uint32_t col = (i * threads + t) * V;
-        float w[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) w[j] = 0.f;
-        if (col < a.cols) get_packed<V>(a.codes + row * blocks * BLOCK8, a.exps + row * blocks, col, w);
-#pragma unroll
-        for (int j = 0; j < V; ++j) v[i * V + j] = w[j];
-    }
+    return p && col < cols ? __ldg(reinterpret_cast<const uint4 *>(p + col)) : make_uint4(0x3F800000u, 0x3F800000u, 0x3F800000u, 0x3F800000u);
 }
 
-// xhat = (x - mean) rstd, g = dy w;  dx = rstd (g - mean g - xhat mean(g xhat)) (+ add).  A group takes every
-// (groups)th row, and each thread sums dy xhat and dy of its own columns over its rows in registers; the groups of
-// a CTA are joined in shared memory in their order, the CTAs by sum_parts_kernel in theirs: the same bits every time.
-template <typename T, int V, bool PACKED, bool ADD>
-__global__ void __launch_bounds__(1024)
-norm_grad_kernel(const NormGradArgs a)
+// What a thread knows of its columns, over the rows of its group.
+template <int E> struct Columns {
+    uint64_t dw[E / 2], db[E / 2];
+};
+struct GroupSums {
+    float2 s[2][THREADS / 32];           // (a warp may be one row ahead of the group's others)
+};
+
+// A row's x and dy of the thread's columns in pairs -> in x xhat, in dy g, and -mean g and -mean(g xhat).
+template <int E, typename W>
+__device__ __forceinline__ void means(Columns<E> &c, W weight, uint64_t (&x)[E / 2], uint64_t (&dy)[E / 2], float mean, float rstd,
+                                      float inv, GroupSums &sums, uint32_t parity, uint32_t group, uint32_t warps, uint64_t &c1, uint64_t &c2)
 {
-    extern __shared__ float joined[];                            // [2][threads * E] of a row's group; groups > 1
-    __shared__ float2 sums[2][32];
-    const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5, group = wid / a.warps, groups = (blockDim.x >> 5) / a.warps;
-    const uint32_t threads = a.warps * 32, t = threadIdx.x - group * threads, cols = a.cols;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    float w[E], dw[E], db[E];
+    const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    const uint64_t mm = twice(-mean), rr = twice(rstd);
+    uint64_t p1 = 0, p2 = 0;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const uint32_t col = V == 1 ? e * threads + t : t * V + e;
-        w[e] = a.weight && col < cols ? a.weight[col] : 1.f;
-        dw[e] = db[e] = 0.f;
+    for (int i = 0; i < E / 2; ++i) {
+        x[i] = mul2(add2(x[i], mm), rr);
+        c.dw[i] = fma2(dy[i], x[i], c.dw[i]);
+        c.db[i] = add2(c.db[i], dy[i]);
+        dy[i] = mul2(dy[i], weight(i));
+        p1 = add2(p1, dy[i]);
+        p2 = fma2(dy[i], x[i], p2);
     }
-    const float inv = 1.f / static_cast<float>(cols);
-    const uint64_t step = static_cast<uint64_t>(gridDim.x) * groups;
-    uint32_t parity = 0;
-    for (uint64_t row = static_cast<uint64_t>(blockIdx.x) * groups + group; row < a.rows; row += step) {
-        float x[E], dy[E];
-        get_x<T, V, PACKED>(a, row, t, threads, x);
-        get_row<T, V>(a, a.dy, a.dy_stride, row, t, threads, dy);
-        const float mean = a.mean[row], rstd = a.rstd[row];
-        float s1 = 0.f, s2 = 0.f;
+    float s1 = warp_sum(both(p1)), s2 = warp_sum(both(p2));
+    if (warps > 1) {
+        if (lane == 0) sums.s[parity][wid] = make_float2(s1, s2);
+        asm volatile("bar.sync %0, %1;" :: "r"(1 + group), "r"(warps * 32) : "memory");
+        const uint32_t i = lane & (THREADS / 32 - 1);
+        const float2 p = i < warps ? sums.s[parity][group * warps + i] : make_float2(0.f, 0.f);
+        s1 = p.x;
+        s2 = p.y;
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const uint32_t col = V == 1 ? e * threads + t : t * V + e;
-            x[e] = col < cols ? (x[e] - mean) * rstd : 0.f;
-            dw[e] = __fmaf_rn(dy[e], x[e], dw[e]);
-            db[e] += dy[e];
-            dy[e] *= w[e];
-            s1 += dy[e];
-            s2 = __fmaf_rn(dy[e], x[e], s2);
-        }
-        s1 = warp_sum(s1);
-        s2 = warp_sum(s2);
-        if (a.warps > 1) {
-            if (lane == 0) sums[parity][wid] = make_float2(s1, s2);
-            asm volatile("bar.sync %0, %1;" :: "r"(1 + group), "r"(threads) : "memory");
-            s1 = s2 = 0.f;
-            for (uint32_t i = 0; i < a.warps; ++i) {
-                const float2 p = sums[parity][group * a.warps + i];
-                s1 += p.x;
-                s2 += p.y;
-            }
-            parity ^= 1;                                         // (a warp may be one row ahead of the group's others)
-        }
-        const float c1 = s1 * inv, c2 = s2 * inv;
-        if (ADD) {
-            float r[E];
-            get_row<T, V>(a, a.add, a.add_stride, row, t, threads, r);
-#pragma unroll
-            for (int e = 0; e < E; ++e) dy[e] = __fmaf_rn(__fmaf_rn(-x[e], c2, dy[e] - c1), rstd, r[e]);
-        } else {
-#pragma unroll
-            for (int e = 0; e < E; ++e) dy[e] = __fmaf_rn(-x[e], c2, dy[e] - c1) * rstd;
-        }
-        T *dx = static_cast<T *>(a.dx) + row * a.dx_stride;
-#pragma unroll
-        for (int i = 0; i < E / V; ++i) {
-            const uint32_t col = (i * threads + t) * V;
-            float o[V];
-#pragma unroll
-            for (int j = 0; j < V; ++j) o[j] = dy[i * V + j];
-            if (col < cols) put<V>(dx + col, o);
+        for (int o = 1; o < THREADS / 32; o *= 2) {
+            s1 += __shfl_xor_sync(FULL, s1, o);
+            s2 += __shfl_xor_sync(FULL, s2, o);
         }
     }
-    if (!a.parts) return;
+    c1 = twice(-s1 * inv);
+    c2 = twice(-s2 * inv);
+}
+
+// The groups' sums over their rows, joined in shared memory in the groups' order, as the CTA's part.
+template <int V, int E>
+__device__ __forceinline__ void put_part(const NormGradArgs &a, const Columns<E> &c, const Own<V, E> &own, uint32_t group,
+                                         uint32_t groups, float *joined)
+{
+    const uint32_t threads = own.threads, cols = a.cols;
     float *part = a.parts + static_cast<uint64_t>(blockIdx.x) * 2 * cols;
-    if (groups == 1) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const uint32_t col = V == 1 ? e * threads + t : t * V + e;
-            if (col >= cols) continue;
-            part[col] = dw[e];
-            part[cols + col] = db[e];
-        }
-        return;
-    }
     for (uint32_t g = 0; g < groups; ++g) {
         if (group == g) {
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const uint32_t at = e * threads + t;
-                joined[at] = g ? joined[at] + dw[e] : dw[e];
-                joined[E * threads + at] = g ? joined[E * threads + at] + db[e] : db[e];
+                const uint32_t at = e * threads + own.t;
+                float x, y, dw, db;
+                unpair(c.dw[e / 2], x, y);
+                dw = e & 1 ? y : x;
+                unpair(c.db[e / 2], x, y);
+                db = e & 1 ? y : x;
+                if (g) {
+                    dw += joined[at];
+                    db += joined[E * threads + at];
+                }
+                if (g + 1 < groups) {
+                    joined[at] = dw;
+                    joined[E * threads + at] = db;
+                } else if (own.col(e) < cols) {
+                    part[own.col(e)] = dw;
+                    part[cols + own.col(e)] = db;
+                }
             }
         }
-        __syncthreads();
+        if (g + 1 < groups) __syncthreads();
     }
-    for (uint32_t at = threadIdx.x; at < E * threads; at += blockDim.x) {
-        const uint32_t e = at / threads, tt = at - e * threads, col = V == 1 ? at : tt * V + e;
-        if (col >= cols) continue;
-        part[col] = joined[at];
-        part[cols + col] = joined[E * threads + at];
+}
+
+// xhat = (x - mean) rstd, g = dy w;  dx = rstd (g - mean g - xhat mean(g xhat)) (+ add).  A group goes from row to
+// row, and each thread sums dy xhat and dy of its own columns over its rows in registers; the groups of
+// a CTA are joined in their order, the CTAs by sum_parts_kernel in theirs: the same bits every time.  What keeps memory
+// busy between a row's arrival and its result are the copies of the group's next rows.
+template <typename T, bool PACKED, bool ADD, int E>
+__global__ void __launch_bounds__(THREADS, E == 8 ? 2 : 1)
+norm_grad_kernel(const NormGradArgs a)
+{
+    constexpr int V = VEC<T>, A = GRAD_AHEAD<T>, U = ADD ? 3 : 2, G = E / V;
+    extern __shared__ uint4 ring[];                              // [A][G][U][thread], weights [E / 4][thread] if V = 8; then the groups' sums
+    __shared__ GroupSums sums;
+    const uint32_t wid = threadIdx.x >> 5, group = wid / a.warps, groups = (blockDim.x >> 5) / a.warps;
+    const uint32_t threads = a.warps * 32, t = threadIdx.x - group * threads, cols = a.cols, all = blockDim.x;
+    const uint32_t blocks = (cols + BLOCK8 - 1) / BLOCK8;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const Own<V, E> own = {cols, threads, t};
+    Columns<E> c;
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) c.dw[i] = c.db[i] = 0;
+    const float inv = 1.f / static_cast<float>(cols);
+    const uint64_t step = static_cast<uint64_t>(gridDim.x) * groups;
+    uint4 *mine = ring + threadIdx.x, *weights = mine + A * G * U * all;
+    const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(mine));
+    uint64_t row = static_cast<uint64_t>(blockIdx.x) * groups + group, next = row;
+    // (columns beyond the last stay 0 in the ring)
+    for (uint32_t u = 0; u < A * G * U; ++u) mine[u * all] = make_uint4(0, 0, 0, 0);
+    // (with V = 4 a warp reads the weights as consecutive bytes from the cache; with V = 8 it would not)
+#pragma unroll
+    for (int i = 0; V == 8 && i < E / 4; ++i) {
+        const uint64_t p[2] = {own.per_column(a.weight, 1.f, 2 * i), own.per_column(a.weight, 1.f, 2 * i + 1)};
+        weights[i * all] = *reinterpret_cast<const uint4 *>(p);
     }
+    uint32_t exps[A][G];                                         // of rows ahead
+    float mean[A], rstd[A];
+    auto ask = [&](int s) {
+        if (next < a.rows) {
+            mean[s] = __ldg(a.mean + next);
+            rstd[s] = __ldg(a.rstd + next);
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                const uint32_t col = own.col(V * g), at = to + (s * G + g) * U * all * 16;
+                if (col >= cols) continue;
+                if (PACKED) {
+                    copy_async_small<V>(at, a.codes + next * blocks * BLOCK8 + col);
+                    exps[s][g] = __ldg(a.exps + next * blocks + col / BLOCK8);
+                } else {
+                    copy_async(at, static_cast<const T *>(a.x) + next * a.x_stride + col);
+                }
+                copy_async(at + all * 16, static_cast<const T *>(a.dy) + next * a.dy_stride + col);
+                if (ADD) copy_async(at + 2 * all * 16, static_cast<const T *>(a.add) + next * a.add_stride + col);
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        next += step;
+    };
+#pragma unroll
+    for (int s = 0; s < A; ++s) {
+#pragma unroll
+        for (int g = 0; g < G; ++g) exps[s][g] = 0;
+        mean[s] = rstd[s] = 0.f;
+        ask(s);
+    }
+    uint32_t parity = 0;
+    while (row < a.rows) {
+#pragma unroll
+        for (int s = 0; s < A; ++s) {
+            if (row >= a.rows) break;
+            asm volatile("cp.async.wait_group %0;" :: "n"(A - 1) : "memory");
+            uint64_t x[E / 2], dy[E / 2], c1, c2;
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                const uint4 *q = mine + (s * G + g) * U * all;
+                if (PACKED) {
+                    const uint2 codes = *reinterpret_cast<const uint2 *>(q);
+                    values4(codes.x, exps[s][g], x + V / 2 * g);
+                    if (V == 8) values4(codes.y, exps[s][g], x + V / 2 * g + 2);
+                } else {
+                    pairs_of(*q, x + V / 2 * g, static_cast<const T *>(nullptr));
+                }
+                pairs_of(q[all], dy + V / 2 * g, static_cast<const T *>(nullptr));
+            }
+            const uint64_t rr = twice(rstd[s]);
+            uint64_t w[E / 2];
+#pragma unroll
+            for (int i = 0; i < E / 4; ++i) {
+                const uint4 q = V == 8 ? weights[i * all] : quad_of(a.weight, own.col(4 * i), cols);
+                w[2 * i] = pair(__uint_as_float(q.x), __uint_as_float(q.y));
+                w[2 * i + 1] = pair(__uint_as_float(q.z), __uint_as_float(q.w));
+            }
+            T *dx = static_cast<T *>(a.dx) + row * a.dx_stride;
+            means<E>(c, [&](int i) { return w[i]; }, x, dy, mean[s], rstd[s], inv, sums, parity, group, a.warps, c1, c2);
+            parity ^= 1;
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                uint64_t add[V / 2];
+                if (ADD) pairs_of(mine[((s * G + g) * U + 2) * all], add, static_cast<const T *>(nullptr));
+#pragma unroll
+                for (int i = 0; i < V / 2; ++i) {
+                    const int k = V / 2 * g + i;
+                    const uint64_t h = fma2(x[k], c2, add2(dy[k], c1));
+                    x[k] = ADD ? fma2(h, rr, add[i]) : mul2(h, rr);
+                }
+                if (own.col(V * g) < cols) put_granule(dx + own.col(V * g), x + V / 2 * g);
+            }
+            ask(s);
+            row += step;
+        }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    if (!a.parts) return;
+    __syncthreads();
+    put_part<V, E>(a, c, own, group, groups, reinterpret_cast<float *>(ring));
+}
+
+// The same for rows and columns of any alignment.
+template <typename T, bool PACKED, bool ADD, int E>
+__global__ void __launch_bounds__(THREADS, 1)
+norm_grad_any_kernel(const NormGradArgs a)
+{
+    extern __shared__ float joined[];                            // [2][threads * E] of a row's group; groups > 1
+    __shared__ GroupSums sums;
+    const uint32_t wid = threadIdx.x >> 5, group = wid / a.warps, groups = (blockDim.x >> 5) / a.warps;
+    const uint32_t threads = a.warps * 32, t = threadIdx.x - group * threads, cols = a.cols;
+    const uint32_t blocks = (cols + BLOCK8 - 1) / BLOCK8;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const Own<1, E> own = {cols, threads, t};
+    Columns<E> c;
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) c.dw[i] = c.db[i] = 0;
+    const float inv = 1.f / static_cast<float>(cols);
+    const uint64_t step = static_cast<uint64_t>(gridDim.x) * groups;
+    uint32_t parity = 0;
+    for (uint64_t row = static_cast<uint64_t>(blockIdx.x) * groups + group; row < a.rows; row += step) {
+        uint64_t x[E / 2], dy[E / 2], add[E / 2], c1, c2;
+        if (PACKED) {
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) {
+                float v[2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const uint32_t col = own.col(2 * i + k);
+                    v[k] = col < cols ? get_packed1(a.codes + row * blocks * BLOCK8, a.exps + row * blocks, col) : 0.f;
+                }
+                x[i] = pair(v[0], v[1]);
+            }
+        } else {
+            own.load(static_cast<const T *>(a.x) + row * a.x_stride, true, x);
+        }
+        own.load(static_cast<const T *>(a.dy) + row * a.dy_stride, true, dy);
+        if (ADD) own.load(static_cast<const T *>(a.add) + row * a.add_stride, true, add);
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        means<E>(c, [&](int i) { return own.per_column(a.weight, 1.f, i); }, x, dy, mean, rstd, inv, sums, parity, group, a.warps, c1, c2);
+        parity ^= 1;
+        const uint64_t rr = twice(rstd);
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) {
+            const uint64_t g = fma2(x[i], c2, add2(dy[i], c1));
+            x[i] = ADD ? fma2(g, rr, add[i]) : mul2(g, rr);
+        }
+        own.store(static_cast<T *>(a.dx) + row * a.dx_stride, true, x);
+    }
+    if (!a.parts) return;
+    put_part<1, E>(a, c, own, group, groups, joined);
 }
 
 // Rows of more columns than a CTA's threads can hold, in two launches.  First c = (mean g, mean(g xhat)) of each row ...
@@ -537,13 +910,11 @@ norm_grad_rows_kernel(const NormGradArgs a)
     const float mean = a.mean[row], rstd = a.rstd[row];
     float s1 = 0.f, s2 = 0.f;
     for (uint32_t col = threadIdx.x; col < a.cols; col += 1024) {
-        float x[1], dy[1];
-        if (PACKED) get_packed<1>(a.codes + row * blocks * BLOCK8, a.exps + row * blocks, col, x);
-        else get<1>(static_cast<const T *>(a.x) + row * a.x_stride + col, x);
-        get<1>(static_cast<const T *>(a.dy) + row * a.dy_stride + col, dy);
-        const float g = a.weight ? dy[0] * a.weight[col] : dy[0];
+        const float x = PACKED ? get_packed1(a.codes + row * blocks * BLOCK8, a.exps + row * blocks, col)
+                               : get1(static_cast<const T *>(a.x) + row * a.x_stride + col);
+        const float dy = get1(static_cast<const T *>(a.dy) + row * a.dy_stride + col), g = a.weight ? dy * a.weight[col] : dy;
         s1 += g;
-        s2 = __fmaf_rn(g, (x[0] - mean) * rstd, s2);
+        s2 = __fmaf_rn(g, (x - mean) * rstd, s2);
     }
     s1 = warp_sum(s1);
     s2 = warp_sum(s2);
@@ -570,16 +941,15 @@ norm_grad_columns_kernel(const NormGradArgs a)
 #pragma unroll 4
     for (uint64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
         const float mean = a.mean[row], rstd = a.rstd[row];
-        float x[1], dy[1], r[1] = {0.f};
-        if (PACKED) get_packed<1>(a.codes + row * blocks * BLOCK8, a.exps + row * blocks, col, x);
-        else get<1>(static_cast<const T *>(a.x) + row * a.x_stride + col, x);
-        get<1>(static_cast<const T *>(a.dy) + row * a.dy_stride + col, dy);
-        if (a.add) get<1>(static_cast<const T *>(a.add) + row * a.add_stride + col, r);
-        const float h = (x[0] - mean) * rstd;
-        dw = __fmaf_rn(dy[0], h, dw);
-        db += dy[0];
-        const float o[1] = {__fmaf_rn(__fmaf_rn(-h, a.c[2 * row + 1], dy[0] * w - a.c[2 * row]), rstd, r[0])};
-        put<1>(static_cast<T *>(a.dx) + row * a.dx_stride + col, o);
+        const float x = PACKED ? get_packed1(a.codes + row * blocks * BLOCK8, a.exps + row * blocks, col)
+                               : get1(static_cast<const T *>(a.x) + row * a.x_stride + col);
+        const float dy = get1(static_cast<const T *>(a.dy) + row * a.dy_stride + col);
+        const float r = a.add ? get1(static_cast<const T *>(a.add) + row * a.add_stride + col) : 0.f;
+        const float h = (x - mean) * rstd;
+        dw = __fmaf_rn(dy, h, dw);
+        db += dy;
+        put1(static_cast<T *>(a.dx) + row * a.dx_stride + col,
+             __fmaf_rn(__fmaf_rn(-h, a.c[2 * row + 1], dy * w - a.c[2 * row]), rstd, r));
     }
     if (!a.parts) return;
     float *part = a.parts + static_cast<uint64_t>(blockIdx.y) * 2 * a.cols;
@@ -609,17 +979,13 @@ sum_parts_kernel(const float *parts, uint32_t n, uint32_t cols, G *dweight, G *d
         v = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) v += s[i][lane];
-        float old[1] = {0.f};
-        if (accumulate) get<1>(out + col, old);
-        const float o[1] = {old[0] + v};
-        put<1>(out + col, o);
+        put1(out + col, accumulate ? get1(out + col) + v : v);
     }
 }
 
 // ------------------------------------------------------------------------------------ host
 
-constexpr uint32_t MAX_ENTRIES = 32;                             // of a row in a thread's registers, forward
-constexpr uint32_t CTAS = 296;                                   // two of 512 threads on each of 148 SMs
+constexpr uint32_t SMS = 148;
 constexpr uint64_t MAX_ROWS = 1ull << 28;
 constexpr uint32_t MAX_COLS = 1u << 24;
 constexpr uint64_t MAX_STRIDE = 1ull << 40;
@@ -636,10 +1002,10 @@ bool bad_rows(const Rows &r, int32_t dtype, uint32_t cols)
 {
     return r.p && (r.stride < cols || r.stride > MAX_STRIDE || !aligned_to(r.p, unit_of(dtype)));
 }
-// 16-byte accesses: all rows start on 16 bytes
+// 16-byte accesses: all rows start on 16 bytes and have whole granules
 bool wide_rows(std::initializer_list<Rows> all, int32_t dtype, uint32_t cols)
 {
-    if (cols % 8) return false;
+    if (cols * unit_of(dtype) % 16) return false;
     for (const Rows &r : all)
         if (r.p && (!aligned_to(r.p, 16) || r.stride * unit_of(dtype) % 16)) return false;
     return true;
@@ -649,29 +1015,95 @@ bool same_start(const Rows &a, const Rows &b) { return a.p && a.p == b.p && a.st
 
 deco_status result() { return cudaGetLastError() == cudaSuccess ? DECO_OK : DECO_ERR_CUDA; }
 
-template <typename T, int V, bool ADD, bool KEEP>
-void launch_norm_items(const NormArgs &a, uint32_t items, unsigned grid, unsigned block, cudaStream_t s)
+// How rows are shared out among groups of warps that go from row to row: 8 entries a thread (two CTAs of 512 threads an SM), 16
+// where the columns need it.  As many groups as 512 threads make, but few rows are spread over the device.
+struct Spread {
+    uint32_t entries, warps, groups, ctas;
+};
+Spread spread(uint64_t rows, uint32_t cols)
 {
-    if (items <= 8) norm_kernel<T, V, 8 / V, ADD, KEEP><<<grid, block, 0, s>>>(a);
-    else if (items <= 16) norm_kernel<T, V, 16 / V, ADD, KEEP><<<grid, block, 0, s>>>(a);
-    else norm_kernel<T, V, 32 / V, ADD, KEEP><<<grid, block, 0, s>>>(a);
-}
-template <typename T, int V>
-void launch_norm(const NormArgs &a, uint32_t items, unsigned grid, unsigned block, cudaStream_t s)
-{
-    if (a.add && a.codes) launch_norm_items<T, V, true, true>(a, items, grid, block, s);
-    else if (a.add) launch_norm_items<T, V, true, false>(a, items, grid, block, s);
-    else if (a.codes) launch_norm_items<T, V, false, true>(a, items, grid, block, s);
-    else launch_norm_items<T, V, false, false>(a, items, grid, block, s);
+    Spread p = {};
+    if (cols > THREADS * 16) return p;                           // (too many)
+    p.entries = cols <= THREADS * 8 ? 8 : 16;
+    p.warps = (cols + 32 * p.entries - 1) / (32 * p.entries);
+    const uint64_t most = p.entries == 8 ? 2 * SMS : SMS, groups = p.warps == 1 ? 16 : std::min<uint64_t>(8, THREADS / 32 / p.warps);
+    p.groups = static_cast<uint32_t>(std::min<uint64_t>(groups, (rows + most - 1) / most));
+    p.ctas = static_cast<uint32_t>(std::min<uint64_t>((rows + p.groups - 1) / p.groups, most));
+    return p;
 }
 
-template <typename T, int V>
-void launch_grad(const NormGradArgs &a, unsigned grid, unsigned block, size_t smem, cudaStream_t s)
+template <typename K>
+cudaError_t allow(K kernel, size_t bytes)
 {
-    if (a.codes && a.add) norm_grad_kernel<T, V, true, true><<<grid, block, smem, s>>>(a);
-    else if (a.codes) norm_grad_kernel<T, V, true, false><<<grid, block, smem, s>>>(a);
-    else if (a.add) norm_grad_kernel<T, V, false, true><<<grid, block, smem, s>>>(a);
-    else norm_grad_kernel<T, V, false, false><<<grid, block, smem, s>>>(a);
+    const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+    if (err != cudaSuccess) cudaGetLastError();                  // (pending, it would be taken for the next call's)
+    return err;
+}
+
+template <typename T, bool ADD, bool KEEP, int E>
+cudaError_t launch_norm_as(const NormArgs &a, const Spread &p, cudaStream_t s)
+{
+    constexpr size_t BYTES = 16ull * AHEAD * (ADD ? 2 : 1) * (E / VEC<T>);                           // a thread's
+    static_assert(BYTES * THREADS <= (E == 8 ? 110 : 224) * 1024, "a CTA's shared memory");
+    const auto kernel = norm_kernel<T, ADD, KEEP, E>;
+    const cudaError_t err = allow(kernel, BYTES * THREADS);
+    if (err != cudaSuccess) return err;
+    const unsigned block = p.groups * p.warps * 32;
+    kernel<<<p.ctas, block, BYTES * block, s>>>(a);
+    return cudaGetLastError();
+}
+template <typename T, bool ADD, bool KEEP>
+cudaError_t launch_norm_rows(NormArgs a, bool wide, cudaStream_t s)
+{
+    const Spread p = spread(a.rows, a.cols);
+    if (wide && p.entries) {
+        a.warps = p.warps;
+        return p.entries == 8 ? launch_norm_as<T, ADD, KEEP, 8>(a, p, s) : launch_norm_as<T, ADD, KEEP, 16>(a, p, s);
+    }
+    a.warps = (a.cols + 32 * ANY_ENTRIES - 1) / (32 * ANY_ENTRIES);
+    const uint32_t groups = a.warps > 8 ? 1 : 8 / a.warps;
+    const unsigned block = groups * a.warps * 32, grid = static_cast<unsigned>((a.rows + groups - 1) / groups);
+    if (block <= 256) norm_any_kernel<T, ADD, KEEP, 256><<<grid, block, 0, s>>>(a);
+    else norm_any_kernel<T, ADD, KEEP, 1024><<<grid, block, 0, s>>>(a);
+    return cudaGetLastError();
+}
+template <typename T>
+cudaError_t launch_norm(const NormArgs &a, bool wide, cudaStream_t s)
+{
+    if (a.add && a.codes) return launch_norm_rows<T, true, true>(a, wide, s);
+    if (a.add) return launch_norm_rows<T, true, false>(a, wide, s);
+    if (a.codes) return launch_norm_rows<T, false, true>(a, wide, s);
+    return launch_norm_rows<T, false, false>(a, wide, s);
+}
+
+template <typename T, bool PACKED, bool ADD, int E>
+cudaError_t launch_grad_as(const NormGradArgs &a, bool wide, unsigned grid, unsigned block, cudaStream_t s)
+{
+    const size_t joined = block > a.warps * 32 ? 2ull * a.warps * 32 * E * sizeof(float) : 0;       // (at most 32 KB)
+    if (!wide) {
+        norm_grad_any_kernel<T, PACKED, ADD, E><<<grid, block, joined, s>>>(a);
+        return cudaGetLastError();
+    }
+    constexpr size_t BYTES = 16ull * (GRAD_AHEAD<T> * (ADD ? 3 : 2) * (E / VEC<T>) + (VEC<T> == 8 ? E / 4 : 0));     // a thread's
+    static_assert(BYTES * THREADS <= (E == 8 ? 112 : 224) * 1024, "a CTA's shared memory");
+    const auto kernel = norm_grad_kernel<T, PACKED, ADD, E>;
+    const cudaError_t err = allow(kernel, BYTES * THREADS);
+    if (err != cudaSuccess) return err;
+    kernel<<<grid, block, std::max(joined, BYTES * block), s>>>(a);
+    return cudaGetLastError();
+}
+template <typename T, bool PACKED, bool ADD>
+cudaError_t launch_grad_rows(const NormGradArgs &a, uint32_t entries, bool wide, unsigned grid, unsigned block, cudaStream_t s)
+{
+    return entries == 8 ? launch_grad_as<T, PACKED, ADD, 8>(a, wide, grid, block, s) : launch_grad_as<T, PACKED, ADD, 16>(a, wide, grid, block, s);
+}
+template <typename T>
+cudaError_t launch_grad(const NormGradArgs &a, uint32_t entries, bool wide, unsigned grid, unsigned block, cudaStream_t s)
+{
+    if (a.codes && a.add) return launch_grad_rows<T, true, true>(a, entries, wide, grid, block, s);
+    if (a.codes) return launch_grad_rows<T, true, false>(a, entries, wide, grid, block, s);
+    if (a.add) return launch_grad_rows<T, false, true>(a, entries, wide, grid, block, s);
+    return launch_grad_rows<T, false, false>(a, entries, wide, grid, block, s);
 }
 template <typename T>
 void launch_grad_wide(const NormGradArgs &a, uint32_t parts, cudaStream_t s)
@@ -689,23 +1121,25 @@ void launch_grad_wide(const NormGradArgs &a, uint32_t parts, cudaStream_t s)
 // How a gradient's rows are shared out.
 struct GradPlan {
     bool wide;                           // more columns than the threads of a CTA hold
-    uint32_t warps, groups, parts;
+    uint32_t entries, warps, groups, parts;
     uint64_t bytes() const { return c_floats * 4 + part_floats * 4; }
     uint64_t c_floats, part_floats;
 };
 GradPlan grad_plan(uint64_t rows, uint32_t cols)
 {
     GradPlan p = {};
-    p.warps = (cols + 32 * E - 1) / (32 * E);
-    p.wide = p.warps > 32;
+    const Spread q = spread(rows, cols);
+    p.wide = q.entries == 0;
     if (p.wide) {
         // the columns alone make cols / 256 CTAs: rows are cut so that eight CTAs stand on an SM
         const uint64_t across = (cols + 255) / 256;
-        p.parts = static_cast<uint32_t>(std::min<uint64_t>(rows, std::max<uint64_t>(1, 4 * CTAS / across)));
+        p.parts = static_cast<uint32_t>(std::min<uint64_t>(rows, std::max<uint64_t>(1, 8 * SMS / across)));
         p.c_floats = 2 * rows;
     } else {
-        p.groups = std::min<uint32_t>(8, std::max<uint32_t>(1, 16 / p.warps));
-        p.parts = static_cast<uint32_t>(std::min<uint64_t>((rows + p.groups - 1) / p.groups, CTAS));
+        p.entries = q.entries;
+        p.warps = q.warps;
+        p.groups = q.groups;
+        p.parts = q.ctas;
     }
     p.part_floats = 2ull * p.parts * cols;
     return p;
@@ -755,30 +1189,20 @@ extern "C" deco_status deco_layernorm(const void *x, int32_t dtype, uint64_t row
     a.weight = weight;
     a.bias = bias;
     a.eps = eps;
+    a.inv_cols = 1.f / static_cast<float>(cols);
     a.mean = mean;
     a.rstd = rstd;
     a.codes = codes;
     a.exps = exponents;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (cols > 1024 * MAX_ENTRIES) {
+    if (cols > 1024 * ANY_ENTRIES) {
         if (dtype == DECO_F32) norm_wide_kernel<float><<<static_cast<unsigned>(rows), 1024, 0, s>>>(a);
         else norm_wide_kernel<__nv_bfloat16><<<static_cast<unsigned>(rows), 1024, 0, s>>>(a);
         return result();
     }
-    const bool wide = wide_rows({rx, ra, rs, ry}, dtype, cols) && aligned_to(weight, 16) && aligned_to(bias, 16);
-    // A warp alone needs no barrier: rows of up to 1024 columns are one warp's each, 8 rows a CTA.
-    a.warps = (cols + 32 * MAX_ENTRIES - 1) / (32 * MAX_ENTRIES);
-    const uint32_t items = (cols + a.warps * 32 - 1) / (a.warps * 32);
-    const uint32_t groups = std::max<uint32_t>(1, 8 / a.warps), block = groups * a.warps * 32;
-    const unsigned grid = static_cast<unsigned>((rows + groups - 1) / groups);
-    if (dtype == DECO_F32) {
-        if (wide) launch_norm<float, 8>(a, items, grid, block, s);
-        else launch_norm<float, 1>(a, items, grid, block, s);
-    } else {
-        if (wide) launch_norm<__nv_bfloat16, 8>(a, items, grid, block, s);
-        else launch_norm<__nv_bfloat16, 1>(a, items, grid, block, s);
-    }
-    return result();
+    const bool wide = wide_rows({rx, ra, rs, ry}, dtype, cols);
+    const cudaError_t err = dtype == DECO_F32 ? launch_norm<float>(a, wide, s) : launch_norm<__nv_bfloat16>(a, wide, s);
+    return err == cudaSuccess ? DECO_OK : DECO_ERR_CUDA;
 }
 
 extern "C" uint64_t deco_layernorm_grad_workspace(uint64_t rows, uint32_t cols)
@@ -837,18 +1261,13 @@ extern "C" deco_status deco_layernorm_grad(const void *x, int32_t dtype, uint64_
         else launch_grad_wide<__nv_bfloat16>(a, plan.parts, s);
     } else {
         const unsigned block = plan.groups * plan.warps * 32;
-        const size_t smem = sums && plan.groups > 1 ? 2ull * plan.warps * 32 * E * sizeof(float) : 0;    // (16 KB at most)
-        const bool wide = wide_rows({rx, rg, ra, rd}, dtype, cols);
-        if (dtype == DECO_F32) {
-            if (wide) launch_grad<float, 8>(a, plan.parts, block, smem, s);
-            else launch_grad<float, 1>(a, plan.parts, block, smem, s);
-        } else {
-            if (wide) launch_grad<__nv_bfloat16, 8>(a, plan.parts, block, smem, s);
-            else launch_grad<__nv_bfloat16, 1>(a, plan.parts, block, smem, s);
-        }
+        const bool wide = wide_rows({rx, rg, ra, rd}, dtype, cols) && aligned_to(weight, 16);
+        const cudaError_t err = dtype == DECO_F32 ? launch_grad<float>(a, plan.entries, wide, plan.parts, block, s)
+                                                  : launch_grad<__nv_bfloat16>(a, plan.entries, wide, plan.parts, block, s);
+        if (err != cudaSuccess) return DECO_ERR_CUDA;
     }
-    const deco_status st = result();
-    if (st != DECO_OK || !sums) return st;
+    if (plan.wide && result() != DECO_OK) return DECO_ERR_CUDA;
+    if (!sums) return DECO_OK;
     return sum(a.parts, plan.parts) == cudaSuccess ? DECO_OK : DECO_ERR_CUDA;
 }
 
@@ -861,14 +1280,14 @@ extern "C" deco_status deco_pack8(const void *x, int32_t dtype, uint64_t rows, u
     if (!x || bad_rows(rx, dtype, cols) || bad_packed(codes, exponents)) return DECO_ERR_INVALID_ARG;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool wide = wide_rows({rx}, dtype, cols);
-    const uint32_t chunks = (cols + (wide ? 255 : 31)) / (wide ? 256 : 32);
-    const uint64_t units = rows * chunks;
-    if ((units + 7) / 8 > 0x7FFFFFFFull) return DECO_ERR_INVALID_ARG;
-    const unsigned grid = static_cast<unsigned>((units + 7) / 8);
+    const uint32_t width = 32 * (wide ? 16 / unit_of(dtype) : 1), chunks = (cols + width - 1) / width;
+    const uint64_t units = rows * chunks, ctas = (units + 8 * UNITS - 1) / (8 * UNITS);
+    if (ctas > 0x7FFFFFFFull) return DECO_ERR_INVALID_ARG;
+    const unsigned grid = static_cast<unsigned>(ctas);
     const float *f = static_cast<const float *>(x);
     const __nv_bfloat16 *h = static_cast<const __nv_bfloat16 *>(x);
     if (dtype == DECO_F32) {
-        if (wide) pack_kernel<float, 8><<<grid, 256, 0, s>>>(f, x_stride, cols, chunks, units, codes, exponents);
+        if (wide) pack_kernel<float, 4><<<grid, 256, 0, s>>>(f, x_stride, cols, chunks, units, codes, exponents);
         else pack_kernel<float, 1><<<grid, 256, 0, s>>>(f, x_stride, cols, chunks, units, codes, exponents);
     } else {
         if (wide) pack_kernel<__nv_bfloat16, 8><<<grid, 256, 0, s>>>(h, x_stride, cols, chunks, units, codes, exponents);
@@ -886,14 +1305,14 @@ extern "C" deco_status deco_unpack8(const int8_t *codes, const uint8_t *exponent
     if (!y || bad_rows(ry, dtype, cols) || bad_packed(codes, exponents)) return DECO_ERR_INVALID_ARG;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool wide = wide_rows({ry}, dtype, cols);
-    const uint32_t chunks = (cols + (wide ? 255 : 31)) / (wide ? 256 : 32);
-    const uint64_t units = rows * chunks;
-    if ((units + 7) / 8 > 0x7FFFFFFFull) return DECO_ERR_INVALID_ARG;
-    const unsigned grid = static_cast<unsigned>((units + 7) / 8);
+    const uint32_t width = 32 * (wide ? 16 / unit_of(dtype) : 1), chunks = (cols + width - 1) / width;
+    const uint64_t units = rows * chunks, ctas = (units + 8 * UNITS - 1) / (8 * UNITS);
+    if (ctas > 0x7FFFFFFFull) return DECO_ERR_INVALID_ARG;
+    const unsigned grid = static_cast<unsigned>(ctas);
     float *f = static_cast<float *>(y);
     __nv_bfloat16 *h = static_cast<__nv_bfloat16 *>(y);
     if (dtype == DECO_F32) {
-        if (wide) unpack_kernel<float, 8><<<grid, 256, 0, s>>>(codes, exponents, cols, chunks, units, f, y_stride);
+        if (wide) unpack_kernel<float, 4><<<grid, 256, 0, s>>>(codes, exponents, cols, chunks, units, f, y_stride);
         else unpack_kernel<float, 1><<<grid, 256, 0, s>>>(codes, exponents, cols, chunks, units, f, y_stride);
     } else {
         if (wide) unpack_kernel<__nv_bfloat16, 8><<<grid, 256, 0, s>>>(codes, exponents, cols, chunks, units, h, y_stride);

@@ -9,7 +9,7 @@ eps times the sum of magnitudes.
   y        |w| rstd (tol of mean + eps |d|) + |xhat w| (tol of rstd + 3 eps) + eps |y|, and half a unit of the type
   dx       xhat carries 2 eps, g one, c1 = mean g: depth eps mean|g|, c2 = mean(g xhat): (depth + 4) eps mean|g xhat|;
            dx: rstd (tol c1 + |xhat| tol c2 + 6 eps (|g| + |c1| + |xhat c2|)) + eps |dx|, and half a unit of the type
-  dweight  a thread adds up rows / 296 rows at most, then up to 8 groups, 37 parts a warp and 8 warps: (rows / 296 + 64) eps
+  dweight  a thread adds up rows / 148 rows at most, then up to 8 groups, 19 parts a warp and 8 warps: (rows / 148 + 64) eps
            sum |dy xhat|; dbias likewise of sum |dy|; and half a unit of the gradients' type
 
 Checkpoints are compared bit by bit.
@@ -269,7 +269,7 @@ def reference_grad(x, mean, rstd, w, dy, add):
         dx = dx + add.double()
         tol = tol + EPS * dx.abs()
     tol = tol + HALF[dy.dtype] * (dx.abs() + tol) + 1e-40
-    dep = (rows / 296 + 64) * EPS
+    dep = (rows / 148 + 64) * EPS
     return dx, tol, (g0 * h).sum(0), dep * (g0 * h).abs().sum(0) + 1e-40, g0.sum(0), dep * g0.abs().sum(0) + 1e-40
 
 
