@@ -649,7 +649,7 @@ struct NormGradArgs {
 };
 
 
-template <typename T> constexpr int GRAD_AHEAD = VEC<T> == 8 ? 3 : 2;    // (what fits shared memory twice)
+template <typename T> constexpr int GRAD_AHEAD = VEC<T> == 8 ? 3 : 2;    // (what fits shared memory, twice with 8 entries)
 
 // Four weights that start on 16 bytes.
 __device__ __forceinline__ uint4 quad_of(const float *p, uint32_t col, uint32_t cols)
@@ -957,12 +957,12 @@ norm_grad_columns_kernel(const NormGradArgs a)
     part[a.cols + col] = db;
 }
 
-// Sum of the parts in their order, 32 columns a CTA: 8 warps take every eighth part each and are joined in order.
+// Sum of the parts in their order, 32 columns a CTA: 32 warps take every 32nd part each and are joined in order.
 template <typename G>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(1024)
 sum_parts_kernel(const float *parts, uint32_t n, uint32_t cols, G *dweight, G *dbias, int accumulate)
 {
-    __shared__ float s[8][32];
+    __shared__ float s[32][33];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
     G *out = blockIdx.y ? dbias : dweight;
@@ -970,17 +970,14 @@ sum_parts_kernel(const float *parts, uint32_t n, uint32_t cols, G *dweight, G *d
     float v = 0.f;
     if (col < cols) {
         const float *p = parts + (blockIdx.y ? cols : 0) + col;
-#pragma unroll 8
-        for (uint32_t i = wid; i < n; i += 8) v += p[static_cast<uint64_t>(i) * 2 * cols];
+#pragma unroll 5
+        for (uint32_t i = wid; i < n; i += 32) v += p[static_cast<uint64_t>(i) * 2 * cols];
     }
-    s[wid][lane] = v;
+    s[lane][wid] = v;
     __syncthreads();
-    if (wid == 0 && col < cols) {
-        v = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v += s[i][lane];
-        put1(out + col, accumulate ? get1(out + col) + v : v);
-    }
+    v = warp_sum(s[wid][lane]);                                  // warp w: column w of the 32
+    const uint32_t c = blockIdx.x * 32 + wid;
+    if (lane == 0 && c < cols) put1(out + c, accumulate ? get1(out + c) + v : v);
 }
 
 // ------------------------------------------------------------------------------------ host
@@ -1015,16 +1012,20 @@ bool same_start(const Rows &a, const Rows &b) { return a.p && a.p == b.p && a.st
 
 deco_status result() { return cudaGetLastError() == cudaSuccess ? DECO_OK : DECO_ERR_CUDA; }
 
-// How rows are shared out among groups of warps that go from row to row: 8 entries a thread (two CTAs of 512 threads an SM), 16
-// where the columns need it.  As many groups as 512 threads make, but few rows are spread over the device.
+// How rows are shared out among groups of warps that go from row to row.  Entries of a row that a thread holds: 8 (two CTAs of 512
+// threads an SM) or more (one).  A warp spends about 100 instructions on a row whatever its share is, which 16-bit rows cannot
+// afford for 8 entries (32768 x 2048 bf16, gradient with residual: 111 us with 8, 91 with 16; fp32: 134 and 141); a
+// row of one warp needs no barrier (65536 x 768 bf16 forward: 57 us with 16, 39 with 24; the gradient has no registers for
+// 24).  As many groups as 512 threads make, but few rows are spread over the device.
 struct Spread {
     uint32_t entries, warps, groups, ctas;
 };
-Spread spread(uint64_t rows, uint32_t cols)
+Spread spread(uint64_t rows, uint32_t cols, int32_t dtype, bool gradient)
 {
     Spread p = {};
     if (cols > THREADS * 16) return p;                           // (too many)
-    p.entries = cols <= THREADS * 8 ? 8 : 16;
+    if (dtype == DECO_F32) p.entries = cols <= 256 || cols > 512 ? (cols <= THREADS * 8 ? 8 : 16) : 16;
+    else p.entries = cols <= 256 ? 8 : !gradient && cols > 512 && cols <= 768 ? 24 : 16;
     p.warps = (cols + 32 * p.entries - 1) / (32 * p.entries);
     const uint64_t most = p.entries == 8 ? 2 * SMS : SMS, groups = p.warps == 1 ? 16 : std::min<uint64_t>(8, THREADS / 32 / p.warps);
     p.groups = static_cast<uint32_t>(std::min<uint64_t>(groups, (rows + most - 1) / most));
@@ -1055,10 +1056,14 @@ cudaError_t launch_norm_as(const NormArgs &a, const Spread &p, cudaStream_t s)
 template <typename T, bool ADD, bool KEEP>
 cudaError_t launch_norm_rows(NormArgs a, bool wide, cudaStream_t s)
 {
-    const Spread p = spread(a.rows, a.cols);
+    const Spread p = spread(a.rows, a.cols, sizeof(T) == 4 ? DECO_F32 : DECO_BF16, false);
     if (wide && p.entries) {
         a.warps = p.warps;
-        return p.entries == 8 ? launch_norm_as<T, ADD, KEEP, 8>(a, p, s) : launch_norm_as<T, ADD, KEEP, 16>(a, p, s);
+        if (p.entries == 8) return launch_norm_as<T, ADD, KEEP, 8>(a, p, s);
+        if constexpr (sizeof(T) == 2) {
+            if (p.entries == 24) return launch_norm_as<T, ADD, KEEP, 24>(a, p, s);
+        }
+        return launch_norm_as<T, ADD, KEEP, 16>(a, p, s);
     }
     a.warps = (a.cols + 32 * ANY_ENTRIES - 1) / (32 * ANY_ENTRIES);
     const uint32_t groups = a.warps > 8 ? 1 : 8 / a.warps;
@@ -1125,10 +1130,10 @@ struct GradPlan {
     uint64_t bytes() const { return c_floats * 4 + part_floats * 4; }
     uint64_t c_floats, part_floats;
 };
-GradPlan grad_plan(uint64_t rows, uint32_t cols)
+GradPlan grad_plan(uint64_t rows, uint32_t cols, int32_t dtype)
 {
     GradPlan p = {};
-    const Spread q = spread(rows, cols);
+    const Spread q = spread(rows, cols, dtype, true);
     p.wide = q.entries == 0;
     if (p.wide) {
         // the columns alone make cols / 256 CTAs: rows are cut so that eight CTAs stand on an SM
@@ -1150,7 +1155,7 @@ cudaError_t launch_sum(const float *parts, uint32_t n, uint32_t cols, void *dwei
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((cols + 31) / 32, 2);
-    cfg.blockDim = dim3(256);
+    cfg.blockDim = dim3(1024);
     cfg.stream = s;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -1208,7 +1213,7 @@ extern "C" deco_status deco_layernorm(const void *x, int32_t dtype, uint64_t row
 extern "C" uint64_t deco_layernorm_grad_workspace(uint64_t rows, uint32_t cols)
 {
     if (rows == 0 || rows >= MAX_ROWS || cols == 0 || cols > MAX_COLS) return 0;
-    return grad_plan(rows, cols).bytes();
+    return std::max(grad_plan(rows, cols, DECO_F32).bytes(), grad_plan(rows, cols, DECO_BF16).bytes());
 }
 
 extern "C" deco_status deco_layernorm_grad(const void *x, int32_t dtype, uint64_t rows, uint32_t cols, uint64_t x_stride,
@@ -1238,7 +1243,7 @@ extern "C" deco_status deco_layernorm_grad(const void *x, int32_t dtype, uint64_
     for (const float *p : {mean, rstd, weight})
         if (!aligned_to(p, 4)) return DECO_ERR_INVALID_ARG;
     if ((codes || exponents) && bad_packed(codes, exponents)) return DECO_ERR_INVALID_ARG;
-    const GradPlan plan = grad_plan(rows, cols);
+    const GradPlan plan = grad_plan(rows, cols, dtype);
     const bool sums = dweight || dbias;
     if (sums || plan.wide) {
         if (!workspace || !aligned_to(workspace, 16)) return DECO_ERR_INVALID_ARG;

@@ -9,7 +9,7 @@ eps times the sum of magnitudes.
   y        |w| rstd (tol of mean + eps |d|) + |xhat w| (tol of rstd + 3 eps) + eps |y|, and half a unit of the type
   dx       xhat carries 2 eps, g one, c1 = mean g: depth eps mean|g|, c2 = mean(g xhat): (depth + 4) eps mean|g xhat|;
            dx: rstd (tol c1 + |xhat| tol c2 + 6 eps (|g| + |c1| + |xhat c2|)) + eps |dx|, and half a unit of the type
-  dweight  a thread adds up rows / 148 rows at most, then up to 8 groups, 19 parts a warp and 8 warps: (rows / 148 + 64) eps
+  dweight  a thread adds up rows / 148 rows at most, then up to 16 groups, 10 parts a warp and 5 steps of a tree: (rows / 148 + 64) eps
            sum |dy xhat|; dbias likewise of sum |dy|; and half a unit of the gradients' type
 
 Checkpoints are compared bit by bit.
