@@ -715,6 +715,8 @@ def _like(x, where, name, device, dtype, shape):
         return None, 0
     if x.dtype != dtype or x.shape != shape:
         raise ValueError("%s: %s must be %s of shape %s" % (where, name, dtype, tuple(shape)))
+    if x.is_cuda and x.get_device() == device and x.is_contiguous():
+        return x.data_ptr(), shape[1]
     row = _rows_of(x, where, name, device)
     return row[0], row[4]
 
@@ -767,12 +769,15 @@ def deco_layernorm_grad_workspace(rows, cols):
     return load().deco_layernorm_grad_workspace(rows, cols)
 
 
-def _grad_kind(where, *grads):
-    """Type code of gradients that are given (all of one type); f32 if none is."""
-    kinds = {g.dtype for g in grads if g is not None}
-    if len(kinds) > 1:
+def _grad_kind(where, a, b):
+    """Type code of one or two gradients (of one type); f32 if none is given."""
+    if a is None:
+        a = b
+    if a is None:
+        return DECO_F32
+    if b is not None and b.dtype != a.dtype:
         raise ValueError("%s: the gradients must have one type" % where)
-    return DECO_BF16 if kinds and "bfloat16" in str(kinds.pop()) else DECO_F32
+    return DECO_BF16 if _dtype_name(a) == "bfloat16" else DECO_F32
 
 
 def deco_layernorm_grad(x, mean, rstd, weight, dy, dx, dweight=None, dbias=None, add=None, accumulate=False,

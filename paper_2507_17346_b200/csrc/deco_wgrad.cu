@@ -63,7 +63,7 @@ constexpr size_t SMEM = A_STAGES * OPERAND + X_STAGES * (OPERAND + RAW_BYTES) + 
 constexpr uint32_t CHUNK = 8;            // blocks an accumulator takes before it is emptied
 constexpr uint32_t SMS = 148;
 constexpr uint32_t MIN_BLOCKS = 8;       // a worker's share, if tiles have to be cut for it
-constexpr uint32_t PART_BLOCKS = 8, EVEN_BLOCKS = 24;     // what cutting tiles costs
+constexpr uint32_t PART_BLOCKS = 2, CUT_BLOCKS = 8;      // what cutting a tile costs: a part, and at all
 
 // A tile is CG * 128 columns of dY by CG * h of X, h a multiple of 16.  A CTA (of a pair) makes the operand of h of the
 // product's columns and, in tiles that sum db too, of 16 of ones behind them.
@@ -422,13 +422,18 @@ wgrad_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
 #pragma unroll
                     for (int j = 0; j < 16; ++j) x[j] = 0.f;
 #pragma unroll 1
-                    for (uint32_t w = a; w <= b; ++w) {
-                        const float *part = slot(w) + p * TILE_M;
-                        float y[16];
+                    for (uint32_t w = a; w <= b; w += 4) {       // (four parts' reads under way together)
+                        float y[4][16];
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) y[j] = w == worker ? __uint_as_float(v[j]) : __ldcg(part + j * TILE_M);
+                        for (uint32_t k = 0; k < 4; ++k) {
+                            const float *part = slot(min(w + k, b)) + p * TILE_M;
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) x[j] += y[j];
+                            for (int j = 0; j < 16; ++j) y[k][j] = w + k == worker ? __uint_as_float(v[j]) : __ldcg(part + j * TILE_M);
+                        }
+#pragma unroll
+                        for (uint32_t k = 0; k < 4; ++k)
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) x[j] += w + k <= b ? y[k][j] : 0.f;
                     }
                 }
                 if (dead) {
@@ -478,50 +483,73 @@ wgrad_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
     }
 }
 
-// What the products need besides: the steps of X as bf16, 16 bytes per token and CTA's share of a tile's columns (0 beyond
-// the last token), and the parts' counters at 0.
-__global__ void __launch_bounds__(256)
-prepare_kernel(const uint8_t *exps, uint32_t rows, uint32_t blocks8, uint32_t h, uint32_t shares, uint32_t tokens, uint4 *steps,
-               uint32_t *counters, uint32_t n_counters)
-{
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const uint32_t first = blockIdx.x * 256 + threadIdx.x, all = gridDim.x * 256;
-    for (uint32_t i = first; i < n_counters; i += all) counters[i] = 0;
-    // (neighbouring threads take neighbouring shares of a token, whose bytes lie side by side)
-    const uint64_t n = static_cast<uint64_t>(shares) * tokens;
-    for (uint64_t i = first; i < n; i += all) {
-        const uint32_t t = static_cast<uint32_t>(i / shares), j = static_cast<uint32_t>(i - static_cast<uint64_t>(t) * shares);
-        uint32_t e[5];
-#pragma unroll
-        for (uint32_t q = 0; q < 5; ++q) {
-            const uint32_t b = j * h / BLOCK8 + q;
-            e[q] = t < rows && b < blocks8 ? bf16_step(exps[static_cast<uint64_t>(t) * blocks8 + b]) : 0u;
-        }
-        // a share begins at a block of 32 columns or in its middle
-        uint32_t o[4];
-#pragma unroll
-        for (uint32_t u = 0; u < 4; ++u) o[u] = e[u] | ((j * h) & 16 ? e[u + 1] : e[u]) << 16;
-        steps[static_cast<uint64_t>(j) * tokens + t] = make_uint4(o[0], o[1], o[2], o[3]);
-    }
-}
-
-// dY as bf16 rows that start on 16 bytes, in planes of which each holds what the ones before it left; rows beyond the last are 0.
+// What the products need besides dY and codes, by one launch.
+//   Steps of X as bf16, 16 bytes per token and CTA's share of a tile's columns (0 beyond the last token).
+//   The parts' counters at 0.
+//   dY, where it cannot be read as it is, as bf16 rows that start on 16 bytes, in planes of which each holds what the ones
+//   before it left; rows beyond the last are 0.  (8192 x 5632 fp32 in three planes: 77 us, 6.0 TB/s.)
+struct PrepareArgs {
+    const uint8_t *exps;
+    uint32_t rows, blocks8, h, shares, tokens;
+    uint4 *steps;
+    uint32_t *counters, n_counters;
+    uint32_t step_blocks, plane_blocks_x, plane_blocks_y;        // blocks of threads for the steps; for the planes
+    const void *dy;
+    uint64_t stride;
+    uint32_t out, pitch, planes;
+    __nv_bfloat16 *to;
+};
 template <typename T>
 __global__ void __launch_bounds__(256)
-planes_kernel(const T *dy, uint64_t stride, uint32_t rows, uint32_t out, uint32_t pitch, uint32_t planes, uint32_t plane_rows,
-              __nv_bfloat16 *to)
+prepare_kernel(const PrepareArgs a)
 {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const uint32_t col = (blockIdx.x * 256 + threadIdx.x) * 8;
-    if (col >= pitch) return;
-    for (uint32_t row = blockIdx.y; row < plane_rows; row += gridDim.y) {
+    if (blockIdx.x < a.step_blocks) {
+        const uint32_t first = blockIdx.x * 256 + threadIdx.x, all = a.step_blocks * 256;
+        for (uint32_t i = first; i < a.n_counters; i += all) a.counters[i] = 0;
+        // (neighbouring threads take neighbouring shares of a token, whose bytes lie side by side)
+        const uint64_t n = static_cast<uint64_t>(a.shares) * a.tokens;
+        for (uint64_t i = first; i < n; i += all) {
+            const uint32_t t = static_cast<uint32_t>(i / a.shares), j = static_cast<uint32_t>(i - static_cast<uint64_t>(t) * a.shares);
+            uint32_t e[5];
+#pragma unroll
+            for (uint32_t q = 0; q < 5; ++q) {
+                const uint32_t b = j * a.h / BLOCK8 + q;
+                e[q] = t < a.rows && b < a.blocks8 ? bf16_step(a.exps[static_cast<uint64_t>(t) * a.blocks8 + b]) : 0u;
+            }
+            // a share begins at a block of 32 columns or in its middle
+            uint32_t o[4];
+#pragma unroll
+            for (uint32_t u = 0; u < 4; ++u) o[u] = e[u] | ((j * a.h) & 16 ? e[u + 1] : e[u]) << 16;
+            a.steps[static_cast<uint64_t>(j) * a.tokens + t] = make_uint4(o[0], o[1], o[2], o[3]);
+        }
+        return;
+    }
+    __shared__ __align__(16) uint16_t staged[8][256];
+    const uint32_t block = blockIdx.x - a.step_blocks, lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    const uint32_t warp_col = (block % a.plane_blocks_x * 8 + wid) * 256, col = warp_col + lane * 8;
+    if (warp_col >= a.pitch) return;
+    for (uint32_t row = block / a.plane_blocks_x; row < a.tokens; row += a.plane_blocks_y) {
+        const T *dy = static_cast<const T *>(a.dy) + row * a.stride;
+        uint4 *to = reinterpret_cast<uint4 *>(a.to + static_cast<uint64_t>(row) * a.pitch + col);
+        if (sizeof(T) == 2) {
+            // through shared memory: lanes read neighbouring entries and write eight
+            const uint16_t *p = reinterpret_cast<const uint16_t *>(dy);
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) {
+                const uint32_t c = warp_col + j * 32 + lane;
+                staged[wid][j * 32 + lane] = row < a.rows && c < a.out ? p[c] : uint16_t(0);
+            }
+            __syncwarp();
+            if (col < a.pitch) *to = *reinterpret_cast<const uint4 *>(&staged[wid][lane * 8]);
+            __syncwarp();
+            continue;
+        }
+        if (col >= a.pitch) continue;
         float v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            v[j] = 0.f;
-            if (row < rows && col + j < out) v[j] = static_cast<float>(dy[row * stride + col + j]);
-        }
-        for (uint32_t p = 0; p < planes; ++p) {
+        for (int j = 0; j < 8; ++j) v[j] = row < a.rows && col + j < a.out ? static_cast<float>(dy[col + j]) : 0.f;
+        for (uint32_t p = 0; p < a.planes; ++p) {
             uint32_t w[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -533,8 +561,7 @@ planes_kernel(const T *dy, uint64_t stride, uint32_t rows, uint32_t out, uint32_
                 v[j] = number ? x - h : 0.f;
                 w[j] = __float_as_uint(h) >> 16;
             }
-            *reinterpret_cast<uint4 *>(to + (static_cast<uint64_t>(p) * plane_rows + row) * pitch + col) =
-                make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
+            to[static_cast<uint64_t>(p) * a.tokens * a.pitch / 8] = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
         }
     }
 }
@@ -575,22 +602,23 @@ Plan make_plan(const void *dy, int32_t dtype, uint64_t rows, uint32_t out, uint6
     p.h = ((cols + p.tiles_n - 1) / p.tiles_n + unit - 1) / unit * 16;
     p.tiles_m = (out + p.cg * TILE_M - 1) / (p.cg * TILE_M);
     p.tiles = static_cast<uint64_t>(p.tiles_m) * p.tiles_n;
-    // How long the worker with most to do takes, in blocks: with whole tiles, with tiles in 2 to 8 equal parts (a part's way through
-    // memory takes as long as some blocks), or with all blocks dealt out evenly, wherever that cuts tiles.
-    const uint64_t most_workers = SMS / p.cg, kb = p.k_blocks;
+    // How long the worker with most to do takes, in blocks: with whole tiles, with tiles in q equal parts, or with all blocks dealt
+    // out evenly, wherever that cuts tiles; whoever is last adds up a tile's parts, each as long as some blocks.
+    const uint64_t most_workers = SMS / p.cg, kb = p.k_blocks, units = p.tiles * kb;
     uint64_t best = (p.tiles + most_workers - 1) / most_workers * kb;
     uint32_t parts = 1;
-    for (uint32_t q = 2; q <= 8; ++q) {
-        const uint64_t grain = (kb + q - 1) / q, cost = (p.tiles * q + most_workers - 1) / most_workers * grain + PART_BLOCKS * (q - 1);
-        if (grain >= MIN_BLOCKS && cost < best) {
+    for (uint32_t q = 2; q <= 64 && (kb + q - 1) / q >= MIN_BLOCKS; ++q) {
+        const uint64_t cost = (p.tiles * q + most_workers - 1) / most_workers * ((kb + q - 1) / q) + PART_BLOCKS * (q - 1) + CUT_BLOCKS;
+        if (cost < best) {
             best = cost;
             parts = q;
         }
     }
-    const uint64_t units = p.tiles * kb, even_workers = std::min(most_workers, std::max<uint64_t>(1, units / MIN_BLOCKS));
+    const uint64_t even_workers = std::min(most_workers, std::max<uint64_t>(1, units / MIN_BLOCKS));
+    const uint64_t even_blocks = (units + even_workers - 1) / even_workers, even_parts = (kb + even_blocks - 1) / even_blocks + 1;
     p.cut = parts > 1;
     p.grain = static_cast<uint32_t>((kb + parts - 1) / parts);
-    if ((units + even_workers - 1) / even_workers + EVEN_BLOCKS < best) {
+    if (even_blocks + PART_BLOCKS * (even_parts - 1) + CUT_BLOCKS < best) {
         p.cut = true;
         p.grain = 1;
         p.workers = static_cast<uint32_t>(even_workers);
@@ -728,23 +756,32 @@ extern "C" deco_status deco_weight_grad8(const void *dy, int32_t dtype, uint64_t
     a.steps = steps;
     a.slots = reinterpret_cast<float *>(room + p.step_bytes());
     a.arrived = reinterpret_cast<uint32_t *>(room + p.step_bytes() + p.slot_bytes());
-    const uint32_t shares = p.tiles_n * p.cg;
-    const uint64_t records = static_cast<uint64_t>(shares) * p.plane_rows;
-    prepare_kernel<<<static_cast<unsigned>(std::min<uint64_t>(8 * SMS, (records + 255) / 256)), 256, 0, s>>>(
-        exponents, static_cast<uint32_t>(rows), static_cast<uint32_t>(pitch / BLOCK8), p.h, shares, p.plane_rows, steps, a.arrived,
-        static_cast<uint32_t>(p.counters()));
-    if (cudaGetLastError() != cudaSuccess) return DECO_ERR_CUDA;
+    PrepareArgs b = {};
+    b.exps = exponents;
+    b.rows = static_cast<uint32_t>(rows);
+    b.blocks8 = static_cast<uint32_t>(pitch / BLOCK8);
+    b.h = p.h;
+    b.shares = p.tiles_n * p.cg;
+    b.tokens = p.plane_rows;
+    b.steps = steps;
+    b.counters = a.arrived;
+    b.n_counters = static_cast<uint32_t>(p.counters());
+    const uint64_t records = static_cast<uint64_t>(b.shares) * p.plane_rows;
+    b.step_blocks = static_cast<uint32_t>(std::min<uint64_t>(8 * SMS, (records + 255) / 256));
     if (p.planes) {
-        const dim3 grid((p.pitch + 2047) / 2048, std::min<uint32_t>(p.plane_rows, 8 * SMS));
-        __nv_bfloat16 *to = static_cast<__nv_bfloat16 *>(workspace);
-        if (dtype == DECO_F32)
-            planes_kernel<float><<<grid, 256, 0, s>>>(static_cast<const float *>(dy), dy_stride, static_cast<uint32_t>(rows), out, p.pitch, p.planes,
-                                                      p.plane_rows, to);
-        else
-            planes_kernel<__nv_bfloat16><<<grid, 256, 0, s>>>(static_cast<const __nv_bfloat16 *>(dy), dy_stride, static_cast<uint32_t>(rows), out, p.pitch,
-                                                              p.planes, p.plane_rows, to);
-        if (cudaGetLastError() != cudaSuccess) return DECO_ERR_CUDA;
+        b.dy = dy;
+        b.stride = dy_stride;
+        b.out = out;
+        b.pitch = p.pitch;
+        b.planes = p.planes;
+        b.to = static_cast<__nv_bfloat16 *>(workspace);
+        b.plane_blocks_x = (p.pitch + 2047) / 2048;
+        b.plane_blocks_y = std::min<uint32_t>(p.plane_rows, std::max<uint32_t>(1, 16 * SMS / b.plane_blocks_x));
     }
+    const unsigned blocks = b.step_blocks + b.plane_blocks_x * b.plane_blocks_y;
+    if (dtype == DECO_F32) prepare_kernel<float><<<blocks, 256, 0, s>>>(b);
+    else prepare_kernel<__nv_bfloat16><<<blocks, 256, 0, s>>>(b);
+    if (cudaGetLastError() != cudaSuccess) return DECO_ERR_CUDA;
     const bool f32 = grad_dtype == DECO_F32;
     const cudaError_t err = p.cg == 2 ? (f32 ? launch_all<2, float>(map, code_map, a, p, s) : launch_all<2, __nv_bfloat16>(map, code_map, a, p, s))
                                       : (f32 ? launch_all<1, float>(map, code_map, a, p, s) : launch_all<1, __nv_bfloat16>(map, code_map, a, p, s));
