@@ -1,6 +1,6 @@
 """A small language model trained by simulated workers over the compressed exchange.
 
-    python -m paper_2507_17346_b200.example_lm [--steps N] [--workers N] [--delta R] [--tau T]
+    python -m paper_2507_17346_b200.example_lm [--steps N] [--workers N] [--delta R] [--tau T] [--norm8]
 
 Every worker computes the loss of its own tokens and the gradient of its logits
 (``deco_token_logprobs``, ``deco_token_logprobs_grad``), the messages are compressed and summed
@@ -8,6 +8,10 @@ Every worker computes the loss of its own tokens and the gradient of its logits
 orthogonalised directions (``deco_apply_update_orth``).  The model is an embedding, one hidden
 layer and a head over a synthetic Markov chain whose entropy rate is known, so that the loss has
 something to fall to; its few products are torch's.
+
+With --norm8 the hidden layer's input is normalised (``deco_layernorm``), what the backward pass needs is kept in 8 bits
+(``deco_pack8``), and the weights' gradients are computed from that, straight into the flat gradient vector
+(``deco_weight_grad8``, ``deco_layernorm_grad``).
 """
 import argparse
 
@@ -59,6 +63,61 @@ class Model:
         return logprob
 
 
+class NormModel(Model):
+    """logits = relu(norm(embed[token]) @ hidden) @ head^T.  Of its activations only checkpoints in 8 bits outlive the forward
+    pass.  The flat vector ends with the norm's weight and bias, which belong to no matrix."""
+
+    def __init__(self, vocab, width, hidden, seed=0, device="cuda"):
+        super().__init__(vocab, width, hidden, seed, device)
+        matrices = self.params
+        self.width, self.at = width, self.d
+        self.d += 2 * width
+        self.params = torch.zeros(self.d, device=device)
+        self.params[:self.at] = matrices
+        self.params[self.at:self.at + width] = 1.0
+
+    def norm_views(self, flat):
+        return flat[self.at:self.at + self.width], flat[self.at + self.width:]
+
+    def forward(self, tokens):
+        """-> (hidden activations, logits, what the backward pass needs)."""
+        embed, hidden, head = self.views(self.params)
+        weight, bias = self.norm_views(self.params)
+        x = embed[tokens]
+        rows, width = x.shape
+        y, mean, rstd = torch.empty_like(x), torch.empty(rows, device=x.device), torch.empty(rows, device=x.device)
+        x8, y8, h8 = (B.packed8_empty(rows, n, x.device) for n in (width, width, hidden.shape[1]))
+        B.deco_layernorm(x, weight, bias, y, mean=mean, rstd=rstd, packed=x8)
+        B.deco_pack8(y, y8)
+        h = torch.relu(y @ hidden)
+        B.deco_pack8(h, h8)
+        return h, h @ head.t(), (x8, mean, rstd, y8, h8)
+
+    def logits(self, tokens):
+        h, logits, _ = self.forward(tokens)
+        return None, h, logits
+
+    def gradient(self, tokens, targets, out):
+        rows = len(tokens)
+        h, logits, (x8, mean, rstd, y8, h8) = self.forward(tokens)
+        logprob, lse = torch.empty(rows, device=h.device), torch.empty(rows, device=h.device)
+        B.deco_token_logprobs(logits, targets, logprob, lse=lse)
+        scale = torch.full((rows,), -1.0 / rows, device=h.device)
+        B.deco_token_logprobs_grad(logits, targets, lse, logits, g_logprob=scale)       # in place
+        _, hidden, head = self.views(self.params)
+        weight, _ = self.norm_views(self.params)
+        d_embed, d_hidden, d_head = self.views(out)
+        d_weight, d_bias = self.norm_views(out)
+        B.deco_weight_grad8(logits, h8, d_head)
+        B.deco_unpack8(h8, h)                                    # (where it is 0 the unit passes nothing on)
+        dh = (logits @ head) * (h > 0)
+        B.deco_weight_grad8(dh, y8, d_hidden, transposed=True)
+        dx = dh @ hidden.t()
+        B.deco_layernorm_grad(x8, mean, rstd, weight, dx, dx, dweight=d_weight, dbias=d_bias)
+        d_embed.zero_().index_add_(0, tokens, dx)
+        return logprob
+
+
 class Chain:
     """A Markov chain in which every token has a few likely successors."""
 
@@ -77,9 +136,9 @@ class Chain:
 
 
 def train(steps=200, workers=4, vocab=512, width=128, hidden=256, batch=1024, delta=0.05, tau=1,
-          lr=0.02, momentum=0.9, weight_decay=0.0, log=None):
+          lr=0.02, momentum=0.9, weight_decay=0.0, log=None, norm8=False):
     """-> (losses per step, model, chain): the mean loss over the workers' batches."""
-    model, chain = Model(vocab, width, hidden), Chain(vocab)
+    model, chain = (NormModel if norm8 else Model)(vocab, width, hidden), Chain(vocab)
     ctx = B.deco_init(model.d, workers, delta, tau, lr, lr_at_server=True, params=model.params)
     orth = B.deco_orth_init(model.d, model.matrices, momentum=momentum,
                             scale=B.DECO_ORTH_SCALE_SPECTRAL)
@@ -122,9 +181,10 @@ def main():
     ap.add_argument("--workers", type=int, default=4)
     ap.add_argument("--delta", type=float, default=0.05)
     ap.add_argument("--tau", type=int, default=1)
+    ap.add_argument("--norm8", action="store_true", help="with a norm, and activations kept in 8 bits")
     args = ap.parse_args()
     losses, model, chain = train(steps=args.steps, workers=args.workers, delta=args.delta,
-                                 tau=args.tau, log=print)
+                                 tau=args.tau, log=print, norm8=args.norm8)
     print("loss %.4f -> %.4f (the chain's entropy rate: %.4f)"
           % (losses[0], losses[-1], chain.entropy_rate()))
     found, entropy = alternatives(model, 7)
