@@ -2,11 +2,11 @@
 // activations put away in 8 bits.
 //
 // All four are bound by memory; at 16 bits there are six entries a cycle and SM to be dealt with, so arithmetic goes by pairs of
-// fp32 numbers.  A row belongs to a group of warps.  A thread owns the same columns of every row of its group: where every
-// row of every array starts on 16 bytes, granules of 16 bytes (V = 4 or 8 entries), granule i of thread t from column
-// (i * threads + t) * V on, so that a warp's access is 512 consecutive bytes (two granules of 16 bytes side by side in a thread made
-// fp32 rows 1.7 times slower: every 32-byte sector is asked for twice); with V = 1 (any alignment, any stride) entry i is column
-// i * threads + t.  Either way a block of 32 columns lies in one warp.
+// fp32 numbers.  A row belongs to a group of warps, each with 32 N consecutive columns of every row, N a thread's.  Where every
+// row of every array starts on 16 bytes a thread's are granules of 16 bytes (V = 4 or 8 entries), and an access of the warp
+// 512 consecutive bytes (two granules side by side in a thread made fp32 rows 1.7 times slower: every 32-byte sector is
+// asked for twice); with V = 1 (any alignment, any stride) it is 32 consecutive entries.  Either way the places of a
+// thread's entries are constants apart, and a block of 32 columns lies in one warp.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <math.h>
@@ -27,7 +27,7 @@ using deco::converted;
 
 constexpr uint32_t FULL = 0xFFFFFFFFu;
 constexpr int THREADS = 512;             // of a CTA whose groups go from row to row
-constexpr int ANY_ENTRIES = 16;          // of a thread that holds a part of a row of any alignment
+constexpr uint32_t MAX_COLS_HELD = THREADS * 16;                 // of a row whose entries a CTA's threads hold
 
 // ----------------------------------------------------------------------------- entries
 
@@ -78,30 +78,38 @@ __device__ __forceinline__ void put_granule(__nv_bfloat16 *p, const uint64_t *v)
 // read as 0 and are not stored.
 template <int V, int N>
 struct Own {
-    uint32_t cols, threads, t;
-    __device__ __forceinline__ uint32_t col(int e) const { return (e / V * threads + t) * V + e % V; }
-    template <typename T> __device__ __forceinline__ void load(const T *p, bool live, uint64_t (&v)[N / 2]) const
+    uint32_t cols, first, mask;          // the thread's first column; a bit for each of its entries that exists
+    __device__ __forceinline__ Own(uint32_t cols_, uint32_t t) : cols(cols_), first(t / 32 * (32 * N) + t % 32 * V), mask(0)
+    {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (col(e) < cols) mask |= 1u << e;
+    }
+    static __device__ __forceinline__ constexpr uint32_t offset(int e) { return e / V * (32 * V) + e % V; }
+    __device__ __forceinline__ uint32_t col(int e) const { return first + offset(e); }
+    __device__ __forceinline__ bool has(int e) const { return mask >> e & 1; }
+    template <typename T> __device__ __forceinline__ void load(const T *row, uint64_t (&v)[N / 2]) const
     {
         static_assert(V == 1, "granules come through the ring");
+        const T *p = row + first;
 #pragma unroll
-        for (int i = 0; i < N / 2; ++i) {
-            const uint32_t a = col(2 * i), b = col(2 * i + 1);
-            v[i] = pair(live && a < cols ? get1(p + a) : 0.f, live && b < cols ? get1(p + b) : 0.f);
-        }
+        for (int i = 0; i < N / 2; ++i)
+            v[i] = pair(has(2 * i) ? get1(p + offset(2 * i)) : 0.f, has(2 * i + 1) ? get1(p + offset(2 * i + 1)) : 0.f);
     }
-    template <typename T> __device__ __forceinline__ void store(T *p, bool live, const uint64_t (&v)[N / 2]) const
+    template <typename T> __device__ __forceinline__ void store(T *row, const uint64_t (&v)[N / 2]) const
     {
+        T *p = row + first;
         if (V > 1) {
 #pragma unroll
             for (int e = 0; e < N; e += V)
-                if (live && col(e) < cols) put_granule(p + col(e), v + e / 2);
+                if (has(e)) put_granule(p + offset(e), v + e / 2);
         } else {
 #pragma unroll
             for (int i = 0; i < N / 2; ++i) {
                 float a, b;
                 unpair(v[i], a, b);
-                if (live && col(2 * i) < cols) put1(p + col(2 * i), a);
-                if (live && col(2 * i + 1) < cols) put1(p + col(2 * i + 1), b);
+                if (has(2 * i)) put1(p + offset(2 * i), a);
+                if (has(2 * i + 1)) put1(p + offset(2 * i + 1), b);
             }
         }
     }
@@ -109,8 +117,13 @@ struct Own {
     __device__ __forceinline__ uint64_t per_column(const float *p, float otherwise, int i) const
     {
         if (!p) return pair(otherwise, otherwise);
-        const uint32_t a = col(2 * i), b = col(2 * i + 1);
-        return pair(a < cols ? p[a] : otherwise, b < cols ? p[b] : otherwise);
+        return pair(has(2 * i) ? p[col(2 * i)] : otherwise, has(2 * i + 1) ? p[col(2 * i + 1)] : otherwise);
+    }
+    // how many of the warp's entries exist
+    __device__ __forceinline__ float of_warp() const
+    {
+        const uint32_t begin = first - threadIdx.x % 32 * V;
+        return begin < cols ? static_cast<float>(min(cols - begin, 32u * N)) : 0.f;
     }
 };
 
@@ -209,19 +222,19 @@ __device__ __forceinline__ void put_packed1(int8_t *codes, uint8_t *exps, uint32
     if (col % BLOCK8 == 0) exps[col / BLOCK8] = static_cast<uint8_t>(b);
 }
 template <int V, int N>
-__device__ __forceinline__ void put_packed(const Own<V, N> &own, int8_t *codes, uint8_t *exps, bool live, const uint64_t (&v)[N / 2])
+__device__ __forceinline__ void put_packed(const Own<V, N> &own, int8_t *codes, uint8_t *exps, const uint64_t (&v)[N / 2])
 {
     const uint32_t end = (own.cols + BLOCK8 - 1) / BLOCK8 * BLOCK8;
     if constexpr (V > 1) {
 #pragma unroll
-        for (int e = 0; e < N; e += V) put_packed_granule<V>(codes, exps, own.col(e), live && own.col(e) < end, v + e / 2);
+        for (int e = 0; e < N; e += V) put_packed_granule<V>(codes, exps, own.col(e), own.col(e) < end, v + e / 2);
     } else {
 #pragma unroll
         for (int i = 0; i < N / 2; ++i) {
             float a, b;
             unpair(v[i], a, b);
-            put_packed1(codes, exps, own.col(2 * i), live && own.col(2 * i) < end, a);
-            put_packed1(codes, exps, own.col(2 * i + 1), live && own.col(2 * i + 1) < end, b);
+            put_packed1(codes, exps, own.col(2 * i), own.col(2 * i) < end, a);
+            put_packed1(codes, exps, own.col(2 * i + 1), own.col(2 * i + 1) < end, b);
         }
     }
 }
@@ -438,22 +451,15 @@ norm_kernel(const NormArgs a)
     const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5, group = wid / a.warps, groups = (blockDim.x >> 5) / a.warps;
     const uint32_t threads = a.warps * 32, t = threadIdx.x - group * threads, cols = a.cols, all = blockDim.x;
     const uint32_t blocks = (cols + BLOCK8 - 1) / BLOCK8;
-    const Own<V, E> own = {cols, threads, t};
+    const Own<V, E> own(cols, t);
     uint64_t w[E / 2], b[E / 2];
 #pragma unroll
     for (int i = 0; i < E / 2; ++i) {
         w[i] = own.per_column(a.weight, 1.f, i);
         b[i] = own.per_column(a.bias, 0.f, i);
     }
-    float n = 0.f;                                               // the warp's entries
-    uint32_t mask = 0;
-#pragma unroll
-    for (int e = 0; e < E; e += V) {
-        const uint32_t c0 = own.col(e) - lane * V;
-        if (c0 < cols) n += static_cast<float>(min(cols - c0, 32u * V));
-        if (own.col(e) < cols) mask |= ((1u << V) - 1) << e;
-    }
-    const bool whole = __all_sync(FULL, mask == (1u << E) - 1);
+    const float n = own.of_warp();
+    const bool whole = n == 32.f * E;
     uint4 *mine = ring + threadIdx.x;
     const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(mine));
     // (columns beyond the last stay 0 in the ring)
@@ -466,10 +472,10 @@ norm_kernel(const NormArgs a)
         if (next < a.rows) {
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-                const uint32_t col = own.col(V * g), at = to + (s * G + g) * U * all * 16;
-                if (col >= cols) continue;
-                copy_async(at, x_next + col);
-                if (ADD) copy_async(at + all * 16, add_next + col);
+                const uint32_t at = to + (s * G + g) * U * all * 16;
+                if (!own.has(V * g)) continue;
+                copy_async(at, x_next + own.col(V * g));
+                if (ADD) copy_async(at + all * 16, add_next + own.col(V * g));
             }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
@@ -501,10 +507,10 @@ norm_kernel(const NormArgs a)
         ask(s);
         s = s + 1 == A ? 0 : s + 1;
         if (ADD) {
-            if (a.sum) own.store(sum, true, v);
+            if (a.sum) own.store(sum, v);
             sum += step * a.sum_stride;
         }
-        Moments mo = warp_moments<E>(v, n, whole, mask);
+        Moments mo = warp_moments<E>(v, n, whole, own.mask);
         float mean = mo.mean + mo.rest;
         if (a.warps > 1) {
             if (lane == 0) moments[parity][wid] = mo;
@@ -518,73 +524,73 @@ norm_kernel(const NormArgs a)
             if (a.mean) a.mean[row] = mean;
             if (a.rstd) a.rstd[row] = rstd;
         }
-        if (KEEP) put_packed(own, a.codes + row * blocks * BLOCK8, a.exps + row * blocks, true, v);
+        if (KEEP) put_packed(own, a.codes + row * blocks * BLOCK8, a.exps + row * blocks, v);
         const uint64_t mm = twice(-mean), rr = twice(rstd);
 #pragma unroll
         for (int i = 0; i < E / 2; ++i) v[i] = fma2(mul2(add2(v[i], mm), rr), w[i], b[i]);
-        own.store(y, true, v);
+        own.store(y, v);
         y += step * a.y_stride;
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
-// The same for rows and columns of any alignment, and for more columns than that: every group a row, up to 1024 threads.
-template <typename T, bool ADD, bool KEEP, int BLOCK>
-__global__ void __launch_bounds__(BLOCK, BLOCK == 256 ? 3 : 1)
+// The same for rows and columns of any alignment: what keeps memory busy is the number of warps.
+template <typename T, bool ADD, bool KEEP, int E>
+__global__ void __launch_bounds__(THREADS, E == 8 ? 2 : 1)
 norm_any_kernel(const NormArgs a)
 {
-    constexpr int N = ANY_ENTRIES;
-    __shared__ Moments moments[BLOCK / 32];
-    const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5, group = wid / a.warps;
-    const uint32_t threads = a.warps * 32, t = threadIdx.x - group * threads, cols = a.cols;
-    const uint64_t row = static_cast<uint64_t>(blockIdx.x) * ((blockDim.x >> 5) / a.warps) + group;
-    const bool live = row < a.rows;
-    const Own<1, N> own = {cols, threads, t};
-    const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
-    uint64_t v[N / 2];
-    own.load(x, live, v);
-    if (ADD) {
-        uint64_t w[N / 2];
-        own.load(static_cast<const T *>(a.add) + row * a.add_stride, live, w);
+    __shared__ Moments moments[2][THREADS / 32];
+    const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5, group = wid / a.warps, groups = (blockDim.x >> 5) / a.warps;
+    const uint32_t threads = a.warps * 32, t = threadIdx.x - group * threads, blocks = (a.cols + BLOCK8 - 1) / BLOCK8;
+    const Own<1, E> own(a.cols, t);
+    uint64_t w[E / 2], b[E / 2];
 #pragma unroll
-        for (int i = 0; i < N / 2; ++i) {
-            float p, q;
-            unpair(add2(v[i], w[i]), p, q);
-            v[i] = pair(rounded(p, x), rounded(q, x));
+    for (int i = 0; i < E / 2; ++i) {
+        w[i] = own.per_column(a.weight, 1.f, i);
+        b[i] = own.per_column(a.bias, 0.f, i);
+    }
+    const float n = own.of_warp();
+    const bool whole = n == 32.f * E;
+    const uint64_t step = static_cast<uint64_t>(gridDim.x) * groups;
+    uint32_t parity = 0;
+    for (uint64_t row = static_cast<uint64_t>(blockIdx.x) * groups + group; row < a.rows; row += step) {
+        const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
+        uint64_t v[E / 2];
+        own.load(x, v);
+        if (ADD) {
+            uint64_t r[E / 2];
+            own.load(static_cast<const T *>(a.add) + row * a.add_stride, r);
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) {
+                float p, q;
+                unpair(add2(v[i], r[i]), p, q);
+                v[i] = pair(rounded(p, x), rounded(q, x));
+            }
+            if (a.sum) own.store(static_cast<T *>(a.sum) + row * a.sum_stride, v);
         }
-        if (a.sum) own.store(static_cast<T *>(a.sum) + row * a.sum_stride, live, v);
-    }
-    float n = 0.f;
-    uint32_t mask = 0;
+        Moments mo = warp_moments<E>(v, n, whole, own.mask);
+        float mean = mo.mean + mo.rest;
+        if (a.warps > 1) {
+            if (lane == 0) moments[parity][wid] = mo;
+            asm volatile("bar.sync %0, %1;" :: "r"(1 + group), "r"(threads) : "memory");
+            mo = join<THREADS / 32>(moments[parity] + group * a.warps, a.warps, a.inv_cols);
+            mean = mo.mean;
+            parity ^= 1;
+        }
+        const float rstd = root_reciprocal(__fmaf_rn(mo.m2, a.inv_cols, a.eps));
+        if (t == 0) {
+            if (a.mean) a.mean[row] = mean;
+            if (a.rstd) a.rstd[row] = rstd;
+        }
+        if (KEEP) put_packed(own, a.codes + row * blocks * BLOCK8, a.exps + row * blocks, v);
+        const uint64_t mm = twice(-mean), rr = twice(rstd);
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-        const uint32_t c0 = own.col(e) - lane;
-        if (c0 < cols) n += static_cast<float>(min(cols - c0, 32u));
-        if (own.col(e) < cols) mask |= 1u << e;
+        for (int i = 0; i < E / 2; ++i) v[i] = fma2(mul2(add2(v[i], mm), rr), w[i], b[i]);
+        own.store(static_cast<T *>(a.y) + row * a.y_stride, v);
     }
-    Moments mo = warp_moments<N>(v, n, false, mask);
-    float mean = mo.mean + mo.rest;
-    if (a.warps > 1) {
-        if (lane == 0) moments[wid] = mo;
-        __syncthreads();
-        mo = join<32>(moments + group * a.warps, a.warps, a.inv_cols);
-        mean = mo.mean;
-    }
-    const float rstd = root_reciprocal(__fmaf_rn(mo.m2, a.inv_cols, a.eps));
-    if (live && t == 0) {
-        if (a.mean) a.mean[row] = mean;
-        if (a.rstd) a.rstd[row] = rstd;
-    }
-    const uint32_t blocks = (cols + BLOCK8 - 1) / BLOCK8;
-    if (KEEP) put_packed(own, a.codes + row * blocks * BLOCK8, a.exps + row * blocks, live, v);
-    const uint64_t mm = twice(-mean), rr = twice(rstd);
-#pragma unroll
-    for (int i = 0; i < N / 2; ++i)
-        v[i] = fma2(mul2(add2(v[i], mm), rr), own.per_column(a.weight, 1.f, i), own.per_column(a.bias, 0.f, i));
-    own.store(static_cast<T *>(a.y) + row * a.y_stride, live, v);
 }
 
-// Rows that do not fit the registers of 1024 threads: one CTA a row, which reads it once for its sum, once for its
+// Rows of more columns than that: one CTA a row, which reads it once for its sum, once for its
 // deviations and once for the output (the second and third time from the caches).
 template <typename T>
 __global__ void __launch_bounds__(1024)
@@ -702,16 +708,16 @@ __device__ __forceinline__ void means(Columns<E> &c, W weight, uint64_t (&x)[E /
 
 // The groups' sums over their rows, joined in shared memory in the groups' order, as the CTA's part.
 template <int V, int E>
-__device__ __forceinline__ void put_part(const NormGradArgs &a, const Columns<E> &c, const Own<V, E> &own, uint32_t group,
-                                         uint32_t groups, float *joined)
+__device__ __forceinline__ void put_part(const NormGradArgs &a, const Columns<E> &c, const Own<V, E> &own, uint32_t t, uint32_t threads,
+                                         uint32_t group, uint32_t groups, float *joined)
 {
-    const uint32_t threads = own.threads, cols = a.cols;
+    const uint32_t cols = a.cols;
     float *part = a.parts + static_cast<uint64_t>(blockIdx.x) * 2 * cols;
     for (uint32_t g = 0; g < groups; ++g) {
         if (group == g) {
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const uint32_t at = e * threads + own.t;
+                const uint32_t at = e * threads + t;
                 float x, y, dw, db;
                 unpair(c.dw[e / 2], x, y);
                 dw = e & 1 ? y : x;
@@ -724,7 +730,7 @@ __device__ __forceinline__ void put_part(const NormGradArgs &a, const Columns<E>
                 if (g + 1 < groups) {
                     joined[at] = dw;
                     joined[E * threads + at] = db;
-                } else if (own.col(e) < cols) {
+                } else if (own.has(e)) {
                     part[own.col(e)] = dw;
                     part[cols + own.col(e)] = db;
                 }
@@ -749,7 +755,7 @@ norm_grad_kernel(const NormGradArgs a)
     const uint32_t threads = a.warps * 32, t = threadIdx.x - group * threads, cols = a.cols, all = blockDim.x;
     const uint32_t blocks = (cols + BLOCK8 - 1) / BLOCK8;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const Own<V, E> own = {cols, threads, t};
+    const Own<V, E> own(cols, t);
     Columns<E> c;
 #pragma unroll
     for (int i = 0; i < E / 2; ++i) c.dw[i] = c.db[i] = 0;
@@ -775,7 +781,7 @@ norm_grad_kernel(const NormGradArgs a)
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 const uint32_t col = own.col(V * g), at = to + (s * G + g) * U * all * 16;
-                if (col >= cols) continue;
+                if (!own.has(V * g)) continue;
                 if (PACKED) {
                     copy_async_small<V>(at, a.codes + next * blocks * BLOCK8 + col);
                     exps[s][g] = __ldg(a.exps + next * blocks + col / BLOCK8);
@@ -836,7 +842,7 @@ norm_grad_kernel(const NormGradArgs a)
                     const uint64_t h = fma2(x[k], c2, add2(dy[k], c1));
                     x[k] = ADD ? fma2(h, rr, add[i]) : mul2(h, rr);
                 }
-                if (own.col(V * g) < cols) put_granule(dx + own.col(V * g), x + V / 2 * g);
+                if (own.has(V * g)) put_granule(dx + own.col(V * g), x + V / 2 * g);
             }
             ask(s);
             row += step;
@@ -845,12 +851,12 @@ norm_grad_kernel(const NormGradArgs a)
     asm volatile("cp.async.wait_all;" ::: "memory");
     if (!a.parts) return;
     __syncthreads();
-    put_part<V, E>(a, c, own, group, groups, reinterpret_cast<float *>(ring));
+    put_part<V, E>(a, c, own, t, threads, group, groups, reinterpret_cast<float *>(ring));
 }
 
 // The same for rows and columns of any alignment.
 template <typename T, bool PACKED, bool ADD, int E>
-__global__ void __launch_bounds__(THREADS, 1)
+__global__ void __launch_bounds__(THREADS, E == 8 ? 2 : 1)
 norm_grad_any_kernel(const NormGradArgs a)
 {
     extern __shared__ float joined[];                            // [2][threads * E] of a row's group; groups > 1
@@ -859,7 +865,7 @@ norm_grad_any_kernel(const NormGradArgs a)
     const uint32_t threads = a.warps * 32, t = threadIdx.x - group * threads, cols = a.cols;
     const uint32_t blocks = (cols + BLOCK8 - 1) / BLOCK8;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const Own<1, E> own = {cols, threads, t};
+    const Own<1, E> own(cols, t);
     Columns<E> c;
 #pragma unroll
     for (int i = 0; i < E / 2; ++i) c.dw[i] = c.db[i] = 0;
@@ -867,36 +873,39 @@ norm_grad_any_kernel(const NormGradArgs a)
     const uint64_t step = static_cast<uint64_t>(gridDim.x) * groups;
     uint32_t parity = 0;
     for (uint64_t row = static_cast<uint64_t>(blockIdx.x) * groups + group; row < a.rows; row += step) {
-        uint64_t x[E / 2], dy[E / 2], add[E / 2], c1, c2;
+        uint64_t x[E / 2], dy[E / 2], c1, c2;
         if (PACKED) {
+            const int8_t *codes = a.codes + row * blocks * BLOCK8 + own.first;
+            const uint8_t *exps = a.exps + row * blocks + own.first / BLOCK8;
 #pragma unroll
             for (int i = 0; i < E / 2; ++i) {
                 float v[2];
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    const uint32_t col = own.col(2 * i + k);
-                    v[k] = col < cols ? get_packed1(a.codes + row * blocks * BLOCK8, a.exps + row * blocks, col) : 0.f;
+                    const int e = 2 * i + k;                     // (entry e is in the thread's block e: 32 columns on)
+                    v[k] = own.has(e) ? static_cast<float>(codes[own.offset(e)]) * step_of(exps[e]) : 0.f;
                 }
                 x[i] = pair(v[0], v[1]);
             }
         } else {
-            own.load(static_cast<const T *>(a.x) + row * a.x_stride, true, x);
+            own.load(static_cast<const T *>(a.x) + row * a.x_stride, x);
         }
-        own.load(static_cast<const T *>(a.dy) + row * a.dy_stride, true, dy);
-        if (ADD) own.load(static_cast<const T *>(a.add) + row * a.add_stride, true, add);
+        own.load(static_cast<const T *>(a.dy) + row * a.dy_stride, dy);
         const float mean = a.mean[row], rstd = a.rstd[row];
         means<E>(c, [&](int i) { return own.per_column(a.weight, 1.f, i); }, x, dy, mean, rstd, inv, sums, parity, group, a.warps, c1, c2);
         parity ^= 1;
         const uint64_t rr = twice(rstd);
+        uint64_t add[E / 2];
+        if (ADD) own.load(static_cast<const T *>(a.add) + row * a.add_stride, add);
 #pragma unroll
         for (int i = 0; i < E / 2; ++i) {
             const uint64_t g = fma2(x[i], c2, add2(dy[i], c1));
             x[i] = ADD ? fma2(g, rr, add[i]) : mul2(g, rr);
         }
-        own.store(static_cast<T *>(a.dx) + row * a.dx_stride, true, x);
+        own.store(static_cast<T *>(a.dx) + row * a.dx_stride, x);
     }
     if (!a.parts) return;
-    put_part<1, E>(a, c, own, group, groups, joined);
+    put_part<1, E>(a, c, own, t, threads, group, groups, joined);
 }
 
 // Rows of more columns than a CTA's threads can hold, in two launches.  First c = (mean g, mean(g xhat)) of each row ...
@@ -1020,11 +1029,12 @@ deco_status result() { return cudaGetLastError() == cudaSuccess ? DECO_OK : DECO
 struct Spread {
     uint32_t entries, warps, groups, ctas;
 };
-Spread spread(uint64_t rows, uint32_t cols, int32_t dtype, bool gradient)
+Spread spread(uint64_t rows, uint32_t cols, int32_t dtype, bool wide, bool gradient)
 {
     Spread p = {};
-    if (cols > THREADS * 16) return p;                           // (too many)
-    if (dtype == DECO_F32) p.entries = cols <= 256 || cols > 512 ? (cols <= THREADS * 8 ? 8 : 16) : 16;
+    if (cols > MAX_COLS_HELD) return p;                          // (too many)
+    if (!wide) p.entries = cols <= THREADS * 8 ? 8 : 16;
+    else if (dtype == DECO_F32) p.entries = cols <= 256 || cols > 512 ? (cols <= THREADS * 8 ? 8 : 16) : 16;
     else p.entries = cols <= 256 ? 8 : !gradient && cols > 512 && cols <= 768 ? 24 : 16;
     p.warps = (cols + 32 * p.entries - 1) / (32 * p.entries);
     const uint64_t most = p.entries == 8 ? 2 * SMS : SMS, groups = p.warps == 1 ? 16 : std::min<uint64_t>(8, THREADS / 32 / p.warps);
@@ -1056,21 +1066,19 @@ cudaError_t launch_norm_as(const NormArgs &a, const Spread &p, cudaStream_t s)
 template <typename T, bool ADD, bool KEEP>
 cudaError_t launch_norm_rows(NormArgs a, bool wide, cudaStream_t s)
 {
-    const Spread p = spread(a.rows, a.cols, sizeof(T) == 4 ? DECO_F32 : DECO_BF16, false);
-    if (wide && p.entries) {
-        a.warps = p.warps;
-        if (p.entries == 8) return launch_norm_as<T, ADD, KEEP, 8>(a, p, s);
-        if constexpr (sizeof(T) == 2) {
-            if (p.entries == 24) return launch_norm_as<T, ADD, KEEP, 24>(a, p, s);
-        }
-        return launch_norm_as<T, ADD, KEEP, 16>(a, p, s);
+    const Spread p = spread(a.rows, a.cols, sizeof(T) == 4 ? DECO_F32 : DECO_BF16, wide, false);
+    a.warps = p.warps;
+    if (!wide) {
+        const unsigned block = p.groups * p.warps * 32;
+        if (p.entries == 8) norm_any_kernel<T, ADD, KEEP, 8><<<p.ctas, block, 0, s>>>(a);
+        else norm_any_kernel<T, ADD, KEEP, 16><<<p.ctas, block, 0, s>>>(a);
+        return cudaGetLastError();
     }
-    a.warps = (a.cols + 32 * ANY_ENTRIES - 1) / (32 * ANY_ENTRIES);
-    const uint32_t groups = a.warps > 8 ? 1 : 8 / a.warps;
-    const unsigned block = groups * a.warps * 32, grid = static_cast<unsigned>((a.rows + groups - 1) / groups);
-    if (block <= 256) norm_any_kernel<T, ADD, KEEP, 256><<<grid, block, 0, s>>>(a);
-    else norm_any_kernel<T, ADD, KEEP, 1024><<<grid, block, 0, s>>>(a);
-    return cudaGetLastError();
+    if (p.entries == 8) return launch_norm_as<T, ADD, KEEP, 8>(a, p, s);
+    if constexpr (sizeof(T) == 2) {
+        if (p.entries == 24) return launch_norm_as<T, ADD, KEEP, 24>(a, p, s);
+    }
+    return launch_norm_as<T, ADD, KEEP, 16>(a, p, s);
 }
 template <typename T>
 cudaError_t launch_norm(const NormArgs &a, bool wide, cudaStream_t s)
@@ -1130,10 +1138,10 @@ struct GradPlan {
     uint64_t bytes() const { return c_floats * 4 + part_floats * 4; }
     uint64_t c_floats, part_floats;
 };
-GradPlan grad_plan(uint64_t rows, uint32_t cols, int32_t dtype)
+GradPlan grad_plan(uint64_t rows, uint32_t cols, int32_t dtype, bool aligned)
 {
     GradPlan p = {};
-    const Spread q = spread(rows, cols, dtype, true);
+    const Spread q = spread(rows, cols, dtype, aligned, true);
     p.wide = q.entries == 0;
     if (p.wide) {
         // the columns alone make cols / 256 CTAs: rows are cut so that eight CTAs stand on an SM
@@ -1200,7 +1208,7 @@ extern "C" deco_status deco_layernorm(const void *x, int32_t dtype, uint64_t row
     a.codes = codes;
     a.exps = exponents;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (cols > 1024 * ANY_ENTRIES) {
+    if (cols > MAX_COLS_HELD) {
         if (dtype == DECO_F32) norm_wide_kernel<float><<<static_cast<unsigned>(rows), 1024, 0, s>>>(a);
         else norm_wide_kernel<__nv_bfloat16><<<static_cast<unsigned>(rows), 1024, 0, s>>>(a);
         return result();
@@ -1213,7 +1221,10 @@ extern "C" deco_status deco_layernorm(const void *x, int32_t dtype, uint64_t row
 extern "C" uint64_t deco_layernorm_grad_workspace(uint64_t rows, uint32_t cols)
 {
     if (rows == 0 || rows >= MAX_ROWS || cols == 0 || cols > MAX_COLS) return 0;
-    return std::max(grad_plan(rows, cols, DECO_F32).bytes(), grad_plan(rows, cols, DECO_BF16).bytes());
+    uint64_t most = 0;                                           // of all types and alignments
+    for (const int32_t dtype : {DECO_F32, DECO_BF16})
+        for (const bool aligned : {false, true}) most = std::max(most, grad_plan(rows, cols, dtype, aligned).bytes());
+    return most;
 }
 
 extern "C" deco_status deco_layernorm_grad(const void *x, int32_t dtype, uint64_t rows, uint32_t cols, uint64_t x_stride,
@@ -1243,7 +1254,8 @@ extern "C" deco_status deco_layernorm_grad(const void *x, int32_t dtype, uint64_
     for (const float *p : {mean, rstd, weight})
         if (!aligned_to(p, 4)) return DECO_ERR_INVALID_ARG;
     if ((codes || exponents) && bad_packed(codes, exponents)) return DECO_ERR_INVALID_ARG;
-    const GradPlan plan = grad_plan(rows, cols, dtype);
+    const bool aligned = wide_rows({rx, rg, ra, rd}, dtype, cols) && aligned_to(weight, 16);
+    const GradPlan plan = grad_plan(rows, cols, dtype, aligned);
     const bool sums = dweight || dbias;
     if (sums || plan.wide) {
         if (!workspace || !aligned_to(workspace, 16)) return DECO_ERR_INVALID_ARG;
@@ -1266,9 +1278,8 @@ extern "C" deco_status deco_layernorm_grad(const void *x, int32_t dtype, uint64_
         else launch_grad_wide<__nv_bfloat16>(a, plan.parts, s);
     } else {
         const unsigned block = plan.groups * plan.warps * 32;
-        const bool wide = wide_rows({rx, rg, ra, rd}, dtype, cols) && aligned_to(weight, 16);
-        const cudaError_t err = dtype == DECO_F32 ? launch_grad<float>(a, plan.entries, wide, plan.parts, block, s)
-                                                  : launch_grad<__nv_bfloat16>(a, plan.entries, wide, plan.parts, block, s);
+        const cudaError_t err = dtype == DECO_F32 ? launch_grad<float>(a, plan.entries, aligned, plan.parts, block, s)
+                                                  : launch_grad<__nv_bfloat16>(a, plan.entries, aligned, plan.parts, block, s);
         if (err != cudaSuccess) return DECO_ERR_CUDA;
     }
     if (plan.wide && result() != DECO_OK) return DECO_ERR_CUDA;
