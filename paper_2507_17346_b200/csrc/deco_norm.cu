@@ -14,6 +14,7 @@
 
 #include <algorithm>
 #include <initializer_list>
+#include <type_traits>
 
 #include "deco.h"
 #include "deco_packed8.h"
@@ -152,6 +153,13 @@ template <int BYTES> __device__ __forceinline__ void copy_async_small(uint32_t t
 {
     asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" :: "r"(to), "l"(from), "n"(BYTES) : "memory");
 }
+// Four numbers of an array per column, on 16 bytes.
+__device__ __forceinline__ uint4 quad_of(const float *p, uint32_t col, bool has, float otherwise)
+{
+    const uint32_t o = __float_as_uint(otherwise);
+    return p && has ? __ldg(reinterpret_cast<const uint4 *>(p + col)) : make_uint4(o, o, o, o);
+}
+
 // --------------------------------------------------------------------- 8-bit checkpoints
 
 // Exponent byte of a block whose largest magnitude has the bits `top` (sign cleared): the smallest b >= 1 for
@@ -258,59 +266,58 @@ __device__ __forceinline__ void values4(uint32_t codes, uint32_t b, uint64_t *v)
     }
 }
 
-// Units of 32 V consecutive columns of a row, UNITS of them a warp's, their loads under way together.  (Measured, 32768 x 2048
-// bf16: 63 us to pack with one unit a warp.)
-constexpr int UNITS = 4;
-struct Place {
+// A warp takes 32 N consecutive columns of ROWS rows, so that four granules (or 16 entries) of a thread are under way together.
+// (Measured, 32768 x 2048 bf16: 63 us to pack with one granule.)
+template <int V, int G> constexpr int PACK_ROWS = (V > 1 ? 4 : 16) / G;
+struct Part {
     uint64_t row;
-    uint32_t col;
-    __device__ __forceinline__ Place(uint64_t unit, uint64_t units, uint32_t chunks, uint32_t width)
+    uint32_t chunk;
+    bool any;
+    __device__ __forceinline__ Part(uint64_t row_groups, uint32_t chunks, uint32_t rows)
     {
-        if (units <= 0xFFFFFFFFull) row = static_cast<uint32_t>(unit) / chunks;
-        else row = unit / chunks;
-        col = static_cast<uint32_t>(unit - row * chunks) * width;
+        const uint64_t unit = static_cast<uint64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5), units = row_groups * chunks;
+        any = unit < units;
+        const uint64_t group = units <= 0xFFFFFFFFull ? static_cast<uint32_t>(unit) / chunks : unit / chunks;
+        chunk = static_cast<uint32_t>(unit - group * chunks);
+        row = group * rows;
     }
 };
 
-template <typename T, int V>
+template <typename T, int V, int G>
 __global__ void __launch_bounds__(256)
-pack_kernel(const T *x, uint64_t stride, uint32_t cols, uint32_t chunks, uint64_t units, int8_t *codes, uint8_t *exps)
+pack_kernel(const T *x, uint64_t rows, uint64_t stride, uint32_t cols, uint64_t row_groups, uint32_t chunks, int8_t *codes, uint8_t *exps)
 {
-    const uint64_t first = (static_cast<uint64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5)) * UNITS;
-    const uint32_t lane = threadIdx.x & 31, blocks = (cols + BLOCK8 - 1) / BLOCK8;
-    uint4 g[UNITS];
-    float f[UNITS];
-    uint64_t row[UNITS];
-    uint32_t col[UNITS];
-    Place at(first, units, chunks, 32 * V);
+    constexpr int N = V * G, R = PACK_ROWS<V, G>;
+    const Part part(row_groups, chunks, R);
+    if (!part.any) return;
+    const Own<V, N> own(cols, part.chunk * 32 + (threadIdx.x & 31));
+    const uint32_t blocks = (cols + BLOCK8 - 1) / BLOCK8;
+    uint4 w[R][G];
+    uint64_t v[R][N / 2];
 #pragma unroll
-    for (int i = 0; i < UNITS; ++i) {
-        row[i] = at.row;
-        col[i] = at.col + lane * V;
-        f[i] = 0.f;
-        g[i] = make_uint4(0, 0, 0, 0);
-        if (first + i < units && col[i] < cols) {
-            if (V > 1) g[i] = *reinterpret_cast<const uint4 *>(x + row[i] * stride + col[i]);
-            else f[i] = get1(x + row[i] * stride + col[i]);
-        }
-        at.col += 32 * V;
-        if (at.col >= chunks * (32 * V)) {
-            at.col = 0;
-            at.row += 1;
+    for (int r = 0; r < R; ++r) {
+        const T *p = x + (part.row + r) * stride;
+        const bool live = part.row + r < rows;
+        if constexpr (V > 1) {
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                w[r][g] = make_uint4(0, 0, 0, 0);
+                if (live && own.has(V * g)) w[r][g] = *reinterpret_cast<const uint4 *>(p + own.col(V * g));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) v[r][i] = 0;
+            if (live) own.load(p, v[r]);
         }
     }
 #pragma unroll
-    for (int i = 0; i < UNITS; ++i) {
-        const bool in = first + i < units && col[i] < blocks * BLOCK8;
-        int8_t *c = codes + row[i] * blocks * BLOCK8;
-        uint8_t *e = exps + row[i] * blocks;
+    for (int r = 0; r < R; ++r) {
+        if (part.row + r >= rows) return;
         if constexpr (V > 1) {
-            uint64_t v[V / 2];
-            pairs_of(g[i], v, x);
-            put_packed_granule<V>(c, e, col[i], in, v);
-        } else {
-            put_packed1(c, e, col[i], in, f[i]);
+#pragma unroll
+            for (int g = 0; g < G; ++g) pairs_of(w[r][g], v[r] + V / 2 * g, x);
         }
+        put_packed(own, codes + (part.row + r) * blocks * BLOCK8, exps + (part.row + r) * blocks, v[r]);
     }
 }
 
@@ -325,42 +332,42 @@ __device__ __forceinline__ void put_values(__nv_bfloat16 *p, uint2 codes, uint32
     *reinterpret_cast<uint4 *>(p) = converted(codes.x, codes.y, deco::bf16_step(b) * 0x10001u);
 }
 
-template <typename T, int V>
+template <typename T, int V, int G>
 __global__ void __launch_bounds__(256)
-unpack_kernel(const int8_t *codes, const uint8_t *exps, uint32_t cols, uint32_t chunks, uint64_t units, T *y, uint64_t stride)
+unpack_kernel(const int8_t *codes, const uint8_t *exps, uint64_t rows, uint32_t cols, uint64_t row_groups, uint32_t chunks, T *y,
+              uint64_t stride)
 {
-    const uint64_t first = (static_cast<uint64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5)) * UNITS;
-    const uint32_t lane = threadIdx.x & 31, blocks = (cols + BLOCK8 - 1) / BLOCK8;
-    uint2 c[UNITS];
-    uint32_t e[UNITS], col[UNITS];
-    uint64_t row[UNITS];
-    Place at(first, units, chunks, 32 * V);
+    constexpr int N = V * G, R = PACK_ROWS<V, G>;
+    const Part part(row_groups, chunks, R);
+    if (!part.any) return;
+    const Own<V, N> own(cols, part.chunk * 32 + (threadIdx.x & 31));
+    const uint32_t blocks = (cols + BLOCK8 - 1) / BLOCK8;
+    uint2 c[R][G];
+    uint32_t e[R][G];
 #pragma unroll
-    for (int i = 0; i < UNITS; ++i) {
-        row[i] = at.row;
-        col[i] = at.col + lane * V;
-        c[i] = make_uint2(0, 0);
-        e[i] = 0;
-        if (first + i >= units) col[i] = cols;
-        if (col[i] < cols) {
-            const int8_t *p = codes + row[i] * blocks * BLOCK8 + col[i];
-            if (V == 8) c[i] = *reinterpret_cast<const uint2 *>(p);
-            else if (V == 4) c[i].x = *reinterpret_cast<const uint32_t *>(p);
-            else c[i].x = static_cast<uint32_t>(static_cast<int>(*p));
-            e[i] = exps[row[i] * blocks + col[i] / BLOCK8];
-        }
-        at.col += 32 * V;
-        if (at.col >= chunks * (32 * V)) {
-            at.col = 0;
-            at.row += 1;
+    for (int r = 0; r < R; ++r) {
+        const int8_t *p = codes + (part.row + r) * blocks * BLOCK8 + own.first;
+        const uint8_t *q = exps + (part.row + r) * blocks + own.first / BLOCK8;
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            c[r][g] = make_uint2(0, 0);
+            e[r][g] = 0;
+            if (part.row + r >= rows || !own.has(V * g)) continue;
+            if (V == 8) c[r][g] = *reinterpret_cast<const uint2 *>(p + own.offset(V * g));
+            else if (V == 4) c[r][g].x = *reinterpret_cast<const uint32_t *>(p + own.offset(V * g));
+            else c[r][g].x = static_cast<uint32_t>(static_cast<int>(p[own.offset(g)]));
+            e[r][g] = q[own.offset(V * g) / BLOCK8];             // (32 V columns on are whole blocks on)
         }
     }
 #pragma unroll
-    for (int i = 0; i < UNITS; ++i) {
-        if (col[i] >= cols) continue;
-        T *p = y + row[i] * stride + col[i];
-        if (V > 1) put_values(p, c[i], e[i]);
-        else put1(p, static_cast<float>(static_cast<int>(c[i].x)) * step_of(e[i]));
+    for (int r = 0; r < R; ++r) {
+        T *p = y + (part.row + r) * stride + own.first;
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            if (part.row + r >= rows || !own.has(V * g)) continue;
+            if constexpr (V > 1) put_values(p + own.offset(V * g), c[r][g], e[r][g]);
+            else put1(p + own.offset(g), static_cast<float>(static_cast<int>(c[r][g].x)) * step_of(e[r][g]));
+        }
     }
 }
 
@@ -452,9 +459,10 @@ norm_kernel(const NormArgs a)
     const uint32_t threads = a.warps * 32, t = threadIdx.x - group * threads, cols = a.cols, all = blockDim.x;
     const uint32_t blocks = (cols + BLOCK8 - 1) / BLOCK8;
     const Own<V, E> own(cols, t);
+    // (with V = 4 a warp reads weights and bias as consecutive bytes from the cache, which leaves registers)
     uint64_t w[E / 2], b[E / 2];
 #pragma unroll
-    for (int i = 0; i < E / 2; ++i) {
+    for (int i = 0; V == 8 && i < E / 2; ++i) {
         w[i] = own.per_column(a.weight, 1.f, i);
         b[i] = own.per_column(a.bias, 0.f, i);
     }
@@ -526,6 +534,11 @@ norm_kernel(const NormArgs a)
         }
         if (KEEP) put_packed(own, a.codes + row * blocks * BLOCK8, a.exps + row * blocks, v);
         const uint64_t mm = twice(-mean), rr = twice(rstd);
+#pragma unroll
+        for (int i = 0; V == 4 && i < E / 4; ++i) {
+            pairs_of(quad_of(a.weight, own.col(4 * i), own.has(4 * i), 1.f), w + 2 * i, static_cast<const float *>(nullptr));
+            pairs_of(quad_of(a.bias, own.col(4 * i), own.has(4 * i), 0.f), b + 2 * i, static_cast<const float *>(nullptr));
+        }
 #pragma unroll
         for (int i = 0; i < E / 2; ++i) v[i] = fma2(mul2(add2(v[i], mm), rr), w[i], b[i]);
         own.store(y, v);
@@ -656,12 +669,6 @@ struct NormGradArgs {
 
 
 template <typename T> constexpr int GRAD_AHEAD = VEC<T> == 8 ? 3 : 2;    // (what fits shared memory, twice with 8 entries)
-
-// Four weights that start on 16 bytes.
-__device__ __forceinline__ uint4 quad_of(const float *p, uint32_t col, uint32_t cols)
-{
-    return p && col < cols ? __ldg(reinterpret_cast<const uint4 *>(p + col)) : make_uint4(0x3F800000u, 0x3F800000u, 0x3F800000u, 0x3F800000u);
-}
 
 // What a thread knows of its columns, over the rows of its group.
 template <int E> struct Columns {
@@ -825,7 +832,7 @@ norm_grad_kernel(const NormGradArgs a)
             uint64_t w[E / 2];
 #pragma unroll
             for (int i = 0; i < E / 4; ++i) {
-                const uint4 q = V == 8 ? weights[i * all] : quad_of(a.weight, own.col(4 * i), cols);
+                const uint4 q = V == 8 ? weights[i * all] : quad_of(a.weight, own.col(4 * i), own.has(4 * i), 1.f);
                 w[2 * i] = pair(__uint_as_float(q.x), __uint_as_float(q.y));
                 w[2 * i + 1] = pair(__uint_as_float(q.z), __uint_as_float(q.w));
             }
@@ -1131,6 +1138,27 @@ void launch_grad_wide(const NormGradArgs &a, uint32_t parts, cudaStream_t s)
     }
 }
 
+// Granules of a row that a thread of the packing kernels takes: as many as leave few lanes empty.  V = 1: 8 entries.
+template <typename F>
+deco_status by_shape(uint32_t vec, uint64_t rows, uint32_t cols, F launch)
+{
+    const auto chunks = [&](uint32_t g) { return (cols + 32 * vec * g - 1) / (32 * vec * g); };
+    const auto fits = [&](uint32_t g) { return static_cast<uint64_t>(chunks(g)) * (32 * vec * g) * 8 <= static_cast<uint64_t>(cols) * 9; };
+    const uint32_t g = vec == 1 ? 8 : fits(4) ? 4 : fits(2) ? 2 : 1, together = (vec > 1 ? 4 : 16) / g;
+    const uint64_t row_groups = (rows + together - 1) / together, ctas = (row_groups * chunks(g) + 7) / 8;
+    if (ctas > 0x7FFFFFFFull) return DECO_ERR_INVALID_ARG;
+    const unsigned grid = static_cast<unsigned>(ctas);
+    const auto with = [&](auto v) {
+        if (g == 4) launch(v, std::integral_constant<int, 4>(), row_groups, chunks(g), grid);
+        else if (g == 2) launch(v, std::integral_constant<int, 2>(), row_groups, chunks(g), grid);
+        else launch(v, std::integral_constant<int, 1>(), row_groups, chunks(g), grid);
+    };
+    if (vec == 8) with(std::integral_constant<int, 8>());
+    else if (vec == 4) with(std::integral_constant<int, 4>());
+    else launch(std::integral_constant<int, 1>(), std::integral_constant<int, 8>(), row_groups, chunks(g), grid);
+    return result();
+}
+
 // How a gradient's rows are shared out.
 struct GradPlan {
     bool wide;                           // more columns than the threads of a CTA hold
@@ -1213,7 +1241,7 @@ extern "C" deco_status deco_layernorm(const void *x, int32_t dtype, uint64_t row
         else norm_wide_kernel<__nv_bfloat16><<<static_cast<unsigned>(rows), 1024, 0, s>>>(a);
         return result();
     }
-    const bool wide = wide_rows({rx, ra, rs, ry}, dtype, cols);
+    const bool wide = wide_rows({rx, ra, rs, ry}, dtype, cols) && aligned_to(weight, 16) && aligned_to(bias, 16);
     const cudaError_t err = dtype == DECO_F32 ? launch_norm<float>(a, wide, s) : launch_norm<__nv_bfloat16>(a, wide, s);
     return err == cudaSuccess ? DECO_OK : DECO_ERR_CUDA;
 }
@@ -1296,20 +1324,16 @@ extern "C" deco_status deco_pack8(const void *x, int32_t dtype, uint64_t rows, u
     if (!x || bad_rows(rx, dtype, cols) || bad_packed(codes, exponents)) return DECO_ERR_INVALID_ARG;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool wide = wide_rows({rx}, dtype, cols);
-    const uint32_t width = 32 * (wide ? 16 / unit_of(dtype) : 1), chunks = (cols + width - 1) / width;
-    const uint64_t units = rows * chunks, ctas = (units + 8 * UNITS - 1) / (8 * UNITS);
-    if (ctas > 0x7FFFFFFFull) return DECO_ERR_INVALID_ARG;
-    const unsigned grid = static_cast<unsigned>(ctas);
-    const float *f = static_cast<const float *>(x);
-    const __nv_bfloat16 *h = static_cast<const __nv_bfloat16 *>(x);
-    if (dtype == DECO_F32) {
-        if (wide) pack_kernel<float, 4><<<grid, 256, 0, s>>>(f, x_stride, cols, chunks, units, codes, exponents);
-        else pack_kernel<float, 1><<<grid, 256, 0, s>>>(f, x_stride, cols, chunks, units, codes, exponents);
-    } else {
-        if (wide) pack_kernel<__nv_bfloat16, 8><<<grid, 256, 0, s>>>(h, x_stride, cols, chunks, units, codes, exponents);
-        else pack_kernel<__nv_bfloat16, 1><<<grid, 256, 0, s>>>(h, x_stride, cols, chunks, units, codes, exponents);
-    }
-    return result();
+    return by_shape(wide ? 16 / unit_of(dtype) : 1, rows, cols, [&](auto v, auto g, uint64_t row_groups, uint32_t chunks, unsigned grid) {
+        constexpr int V = decltype(v)::value, G = decltype(g)::value;
+        if constexpr (V != 8)
+            if (dtype == DECO_F32)
+                pack_kernel<float, V, G><<<grid, 256, 0, s>>>(static_cast<const float *>(x), rows, x_stride, cols, row_groups, chunks, codes, exponents);
+        if constexpr (V != 4)
+            if (dtype == DECO_BF16)
+                pack_kernel<__nv_bfloat16, V, G><<<grid, 256, 0, s>>>(static_cast<const __nv_bfloat16 *>(x), rows, x_stride, cols, row_groups,
+                                                                     chunks, codes, exponents);
+    });
 }
 
 extern "C" deco_status deco_unpack8(const int8_t *codes, const uint8_t *exponents, uint64_t rows, uint32_t cols,
@@ -1321,18 +1345,14 @@ extern "C" deco_status deco_unpack8(const int8_t *codes, const uint8_t *exponent
     if (!y || bad_rows(ry, dtype, cols) || bad_packed(codes, exponents)) return DECO_ERR_INVALID_ARG;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool wide = wide_rows({ry}, dtype, cols);
-    const uint32_t width = 32 * (wide ? 16 / unit_of(dtype) : 1), chunks = (cols + width - 1) / width;
-    const uint64_t units = rows * chunks, ctas = (units + 8 * UNITS - 1) / (8 * UNITS);
-    if (ctas > 0x7FFFFFFFull) return DECO_ERR_INVALID_ARG;
-    const unsigned grid = static_cast<unsigned>(ctas);
-    float *f = static_cast<float *>(y);
-    __nv_bfloat16 *h = static_cast<__nv_bfloat16 *>(y);
-    if (dtype == DECO_F32) {
-        if (wide) unpack_kernel<float, 4><<<grid, 256, 0, s>>>(codes, exponents, cols, chunks, units, f, y_stride);
-        else unpack_kernel<float, 1><<<grid, 256, 0, s>>>(codes, exponents, cols, chunks, units, f, y_stride);
-    } else {
-        if (wide) unpack_kernel<__nv_bfloat16, 8><<<grid, 256, 0, s>>>(codes, exponents, cols, chunks, units, h, y_stride);
-        else unpack_kernel<__nv_bfloat16, 1><<<grid, 256, 0, s>>>(codes, exponents, cols, chunks, units, h, y_stride);
-    }
-    return result();
+    return by_shape(wide ? 16 / unit_of(dtype) : 1, rows, cols, [&](auto v, auto g, uint64_t row_groups, uint32_t chunks, unsigned grid) {
+        constexpr int V = decltype(v)::value, G = decltype(g)::value;
+        if constexpr (V != 8)
+            if (dtype == DECO_F32)
+                unpack_kernel<float, V, G><<<grid, 256, 0, s>>>(codes, exponents, rows, cols, row_groups, chunks, static_cast<float *>(y), y_stride);
+        if constexpr (V != 4)
+            if (dtype == DECO_BF16)
+                unpack_kernel<__nv_bfloat16, V, G><<<grid, 256, 0, s>>>(codes, exponents, rows, cols, row_groups, chunks,
+                                                                       static_cast<__nv_bfloat16 *>(y), y_stride);
+    });
 }
