@@ -1032,7 +1032,7 @@ deco_status result() { return cudaGetLastError() == cudaSuccess ? DECO_OK : DECO
 // threads an SM) or more (one).  A warp spends about 100 instructions on a row whatever its share is, which 16-bit rows cannot
 // afford for 8 entries (32768 x 2048 bf16, gradient with residual: 111 us with 8, 91 with 16; fp32: 134 and 141); a
 // row of one warp needs no barrier (65536 x 768 bf16 forward: 57 us with 16, 39 with 24; the gradient has no registers for
-// 24).  As many groups as 512 threads make, but few rows are spread over the device.
+// 24, and of 8192 rows 8 entries, three warps, make 22 us, 16 and two 25).  As many groups as 512 threads make, but few rows are spread over the device.
 struct Spread {
     uint32_t entries, warps, groups, ctas;
 };
@@ -1042,7 +1042,8 @@ Spread spread(uint64_t rows, uint32_t cols, int32_t dtype, bool wide, bool gradi
     if (cols > MAX_COLS_HELD) return p;                          // (too many)
     if (!wide) p.entries = cols <= THREADS * 8 ? 8 : 16;
     else if (dtype == DECO_F32) p.entries = cols <= 256 || cols > 512 ? (cols <= THREADS * 8 ? 8 : 16) : 16;
-    else p.entries = cols <= 256 ? 8 : !gradient && cols > 512 && cols <= 768 ? 24 : 16;
+    else if (gradient) p.entries = cols <= 256 || (cols > 512 && cols <= 768) ? 8 : 16;
+    else p.entries = cols <= 256 ? 8 : cols > 512 && cols <= 768 ? 24 : 16;
     p.warps = (cols + 32 * p.entries - 1) / (32 * p.entries);
     const uint64_t most = p.entries == 8 ? 2 * SMS : SMS, groups = p.warps == 1 ? 16 : std::min<uint64_t>(8, THREADS / 32 / p.warps);
     p.groups = static_cast<uint32_t>(std::min<uint64_t>(groups, (rows + most - 1) / most));

@@ -203,3 +203,27 @@ def test_refusals():
     with pytest.raises(B.DecoError) as e:
         B.deco_weight_grad8(dy, packed, dw, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
     assert e.value.status == B.DECO_ERR_CAPACITY
+
+
+def test_rows_whose_offsets_pass_32_bits():
+    """Rows of dY 2^31 entries apart, read as they are and through planes; many tiles, more than workers."""
+    rows, out, cols = 3, 40, 70
+    packed = checkpoint(rows, cols, 14)
+    for stride in (2 ** 31 + 24, 2 ** 31 + 25):
+        buf = torch.zeros((rows - 1) * stride + out, dtype=torch.bfloat16, device="cuda")
+        dy = torch.as_strided(buf, (rows, out), (stride, 1))
+        dy.copy_(gradients(rows, out, "bf16", 15))
+        dw, db = torch.empty(out, cols, device="cuda"), torch.empty(out, device="cuda")
+        B.deco_weight_grad8(dy, packed, dw, db=db)
+        check(dy, packed, cols, dw, db, False)
+        del buf, dy
+
+
+@pytest.mark.parametrize("gtype", ["f32", "bf16"])
+def test_more_tiles_than_workers_and_parts_of_many(gtype):
+    """Whole tiles several to a worker; a tile in dozens of parts; blocks dealt out across tiles."""
+    for rows, out, cols in ((70, 3000, 2500), (20000, 33, 50), (9000, 1500, 230)):
+        packed, dy = checkpoint(rows, cols, 16), gradients(rows, out, "bf16", 17)
+        dw, db = torch.empty(out, cols, device="cuda", dtype=DT[gtype]), torch.empty(out, device="cuda", dtype=DT[gtype])
+        B.deco_weight_grad8(dy, packed, dw, db=db)
+        check(dy, packed, cols, dw, db, False)
