@@ -410,37 +410,47 @@ wgrad_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
                 out = __shfl_sync(0xFFFFFFFFu, before, 0) == b - a;
                 __threadfence();
             }
+            // (Short code: what runs once per segment waits for its instructions longer than for anything else.)
+            const bool two = b - a == 1;
+            const float *other = slot(worker == a ? b : a);
+            const uint32_t col0 = nt * CG * g.h, o0 = mt * TILE_M + quad * 32, o = o0 + lane;
 #pragma unroll 1
             for (uint32_t p = 0; out && p < mine; p += 16) {
                 uint32_t v[16];
                 float x[16];
-                tmem_load16(acc + p, v);
-                if (whole) {
+                const uint32_t n0 = side * SIDE + p;
+                if (two) {                                       // (0 + a) + b in whichever order: it is simply added
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) x[j] = __uint_as_float(v[j]);
+                    for (int j = 0; j < 16; ++j) x[j] = __ldcg(other + (p + j) * TILE_M);
                 } else {
 #pragma unroll
                     for (int j = 0; j < 16; ++j) x[j] = 0.f;
+                }
+                tmem_load16(acc + p, v);
+                if (whole || two) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) x[j] += __uint_as_float(v[j]);
+                } else {
 #pragma unroll 1
                     for (uint32_t w = a; w <= b; w += 4) {       // (four parts' reads under way together)
                         float y[4][16];
 #pragma unroll
                         for (uint32_t k = 0; k < 4; ++k) {
-                            const float *part = slot(min(w + k, b)) + p * TILE_M;
+                            const float *part = slot(w + k) + p * TILE_M;
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) y[k][j] = w + k == worker ? __uint_as_float(v[j]) : __ldcg(part + j * TILE_M);
+                            for (int j = 0; j < 16; ++j)
+                                y[k][j] = w + k == worker ? __uint_as_float(v[j]) : w + k <= b ? __ldcg(part + j * TILE_M) : 0.f;
                         }
 #pragma unroll
                         for (uint32_t k = 0; k < 4; ++k)
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) x[j] += w + k <= b ? y[k][j] : 0.f;
+                            for (int j = 0; j < 16; ++j) x[j] += y[k][j];
                     }
                 }
                 if (dead) {
 #pragma unroll
                     for (int j = 0; j < 16; ++j) x[j] = __uint_as_float(0x7FC00000u);
                 }
-                const uint32_t n0 = side * SIDE + p, col0 = nt * CG * g.h, o = mt * TILE_M + quad * 32 + lane;
                 if (c.ones && n0 == c.h) {                                           // (the columns of ones are all alike)
                     if (o < g.out) store_grad<G>(g.db, o, x[0], g.accumulate);
                     continue;
@@ -448,10 +458,11 @@ wgrad_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
                 if (!c.in(n0)) continue;
                 const uint32_t col = col0 + c.col(n0);                               // of the sixteen, one behind the other
                 if (g.transposed) {
+                    G *to = static_cast<G *>(g.dw) + static_cast<uint64_t>(col) * g.out + o;
+                    const uint32_t end = o < g.out ? g.cols - min(col, g.cols) : 0;
 #pragma unroll
-                    for (uint32_t j = 0; j < 16; ++j)
-                        if (col + j < g.cols && o < g.out)
-                            store_grad<G>(g.dw, static_cast<uint64_t>(col + j) * g.out + o, x[j], g.accumulate);
+                    for (uint32_t j = 0; j < 16; ++j, to += g.out)
+                        if (j < end) store_grad<G>(to, 0, x[j], g.accumulate);
                     continue;
                 }
                 // through shared memory, so that neighbouring lanes write neighbouring entries
@@ -459,14 +470,13 @@ wgrad_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
 #pragma unroll
                 for (uint32_t j = 0; j < 16; ++j) staging[lane * (STAGING_COLS + 1) + j] = x[j];
                 __syncwarp();
-                const uint32_t at = col + (lane & 15);
-#pragma unroll 8
-                for (uint32_t q = lane >> 4; q < 32; q += 2) {
-                    const uint32_t row = mt * TILE_M + quad * 32 + q;
-                    if (at < g.cols && row < g.out)
-                        store_grad<G>(g.dw, static_cast<uint64_t>(row) * g.cols + at, staging[q * (STAGING_COLS + 1) + (lane & 15)],
-                                      g.accumulate);
-                }
+                const uint32_t at = col + (lane & 15), first_row = o0 + (lane >> 4);
+                G *to = static_cast<G *>(g.dw) + static_cast<uint64_t>(first_row) * g.cols + at;
+                const float *from = staging + (lane >> 4) * (STAGING_COLS + 1) + (lane & 15);
+                const uint32_t rows = at < g.cols && first_row < g.out ? (g.out - first_row + 1) / 2 : 0;
+#pragma unroll 4
+                for (uint32_t q = 0; q < 16; ++q, to += 2 * static_cast<uint64_t>(g.cols), from += 2 * (STAGING_COLS + 1))
+                    if (q < rows) store_grad<G>(to, 0, *from, g.accumulate);
             }
             done();
         }
