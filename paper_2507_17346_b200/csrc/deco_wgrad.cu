@@ -1,7 +1,7 @@
 // deco_weight_grad8: the weight gradient of a linear layer whose input was put away in 8 bits,
 //     dW[o][i] = sum_t dY[t][o] X[t][i],   db[o] = sum_t dY[t][o],
 // on the tensor cores.  X's entries, 8-bit integers times a power of two, are bf16 numbers, so the products are exact and
-// X is never written out: box copies bring codes (a byte an entry) into shared memory, eight warps make bf16 of them
+// X is never written out: box copies bring codes (a byte an entry) into shared memory, twelve warps make bf16 of them
 // (five instructions for two) and put them in the place of the operand, while dY comes as it is.  Both operands have
 // their outer dimension consecutive, 128-byte swizzle.
 //
@@ -19,6 +19,13 @@
 // Shares.  The blocks of all tiles in a row, cut into equal ranges, one per worker (a CTA or a pair): where whole tiles
 // would leave too many idle, a worker begins and ends inside tiles.  Parts of a tile are left in the workspace, and whoever
 // comes last adds them up, in their order whoever it is: the same bits every time.
+//
+// What bounds it (8192 x 5632 x 2048 bf16, 1.09 PFLOP/s; tensor cores busy 71 % of the cycles): shared memory.  64 tokens of a pair's
+// tile take each SM 23 KB of copies in, 8 KB of codes and steps read and 14 KB of bf16 written to convert, and 32 KB read by
+// the tensor cores: 77 KB, 600 cycles at 128 bytes a cycle, where the products take 448 to 512; 640 are measured, 476 without
+// conversion and copies.  In a loop the power cap is next: clocks fall to 1.5 GHz.  Short sums (8192 x 2304 x 768, 45 us): the products
+// of a worker's one part 43 thousand cycles, of which its end is 21 thousand more if it comes last: sums to tensor memory 2.7, the part
+// to memory 3 to 4, the fence 2 to 3, the other part in and the result out 13.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
