@@ -721,12 +721,25 @@ def _like(x, where, name, device, dtype, shape):
     return row[0], row[4]
 
 
+def _vector(x, where, name, device, n, kind="float32"):
+    """_tensor for a vector of n entries.  (Two numbers are compared sooner than two shapes.)"""
+    if x is None:
+        return None
+    if x.get_device() == device and _dtypes.get(x.dtype) == kind and x.numel() == n and x.dim() == 1 and x.is_contiguous():
+        return x.data_ptr()
+    return _tensor(x, where, name, device, (kind,), (n,))
+
+
 def _packed(packed, where, device, rows, cols):
     """Addresses of a checkpoint's two tensors."""
     if packed is None:
         return None, None
     codes, exps = packed
     blocks = (cols + 31) // 32
+    if codes.get_device() == device == exps.get_device() and _dtypes.get(codes.dtype) == "int8" and \
+            _dtypes.get(exps.dtype) == "uint8" and codes.dim() == 2 == exps.dim() and codes.size(1) == 32 * blocks and \
+            exps.size(1) == blocks and codes.size(0) == rows == exps.size(0) and codes.is_contiguous() and exps.is_contiguous():
+        return codes.data_ptr(), exps.data_ptr()
     return (_tensor(codes, where, "codes", device, ("int8",), (rows, 32 * blocks)),
             _tensor(exps, where, "exponents", device, ("uint8",), (rows, blocks)))
 
@@ -758,9 +771,9 @@ def deco_layernorm(x, weight, bias, y, mean=None, rstd=None, eps=1e-5, add=None,
     yp, ystride = _like(y, w, "y", dev, x.dtype, x.shape)
     codes, exps = _packed(packed, w, dev, rows, cols)
     _check(load().deco_layernorm(
-        p, kind, rows, cols, stride, ap, astride, tp, tstride, _tensor(weight, w, "weight", dev, ("float32",), (cols,)),
-        _tensor(bias, w, "bias", dev, ("float32",), (cols,)), eps, yp, ystride,
-        _tensor(mean, w, "mean", dev, ("float32",), (rows,)), _tensor(rstd, w, "rstd", dev, ("float32",), (rows,)),
+        p, kind, rows, cols, stride, ap, astride, tp, tstride, _vector(weight, w, "weight", dev, cols),
+        _vector(bias, w, "bias", dev, cols), eps, yp, ystride,
+        _vector(mean, w, "mean", dev, rows), _vector(rstd, w, "rstd", dev, rows),
         codes, exps, _stream_on(stream, dev)), w)
 
 
@@ -801,8 +814,8 @@ def deco_layernorm_grad(x, mean, rstd, weight, dy, dx, dweight=None, dbias=None,
     room, wp, nbytes = _workspace(workspace, w, need, dev, stream)
     both = ("float32", "bfloat16")
     _check(load().deco_layernorm_grad(
-        xp, kind, rows, cols, xstride, codes, exps, _tensor(mean, w, "mean", dev, ("float32",), (rows,)),
-        _tensor(rstd, w, "rstd", dev, ("float32",), (rows,)), _tensor(weight, w, "weight", dev, ("float32",), (cols,)),
+        xp, kind, rows, cols, xstride, codes, exps, _vector(mean, w, "mean", dev, rows),
+        _vector(rstd, w, "rstd", dev, rows), _vector(weight, w, "weight", dev, cols),
         p, stride, ap, astride, dp, dstride, _tensor(dweight, w, "dweight", dev, both, (cols,)),
         _tensor(dbias, w, "dbias", dev, both, (cols,)), gkind, int(bool(accumulate)), wp, nbytes,
         _stream_on(stream, dev)), w)

@@ -19,6 +19,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <atomic>
 #include <initializer_list>
 #include <type_traits>
 
@@ -1057,11 +1058,17 @@ Spread spread(uint64_t rows, uint32_t cols, int32_t dtype, bool wide, bool gradi
     return p;
 }
 
-template <typename K>
-cudaError_t allow(K kernel, size_t bytes)
+// A kernel's shared memory, once per device.
+template <auto KERNEL>
+cudaError_t allow(size_t bytes)
 {
-    const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+    static std::atomic<uint64_t> done{0};
+    int dev = 0;
+    cudaError_t err = cudaGetDevice(&dev);
+    if (err == cudaSuccess && dev >= 0 && dev < 64 && (done.load() >> dev & 1)) return cudaSuccess;
+    if (err == cudaSuccess) err = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
     if (err != cudaSuccess) cudaGetLastError();                  // (pending, it would be taken for the next call's)
+    else if (dev >= 0 && dev < 64) done.fetch_or(1ull << dev);
     return err;
 }
 
@@ -1070,11 +1077,10 @@ cudaError_t launch_norm_as(const NormArgs &a, const Spread &p, cudaStream_t s)
 {
     constexpr size_t BYTES = 16ull * AHEAD * (ADD ? 2 : 1) * (E / VEC<T>);                           // a thread's
     static_assert(BYTES * THREADS <= (E == 8 ? 110 : 224) * 1024, "a CTA's shared memory");
-    const auto kernel = norm_kernel<T, ADD, KEEP, E>;
-    const cudaError_t err = allow(kernel, BYTES * THREADS);
+    const cudaError_t err = allow<norm_kernel<T, ADD, KEEP, E>>(BYTES * THREADS);
     if (err != cudaSuccess) return err;
     const unsigned block = p.groups * p.warps * 32;
-    kernel<<<p.ctas, block, BYTES * block, s>>>(a);
+    norm_kernel<T, ADD, KEEP, E><<<p.ctas, block, BYTES * block, s>>>(a);
     return cudaGetLastError();
 }
 template <typename T, bool ADD, bool KEEP>
@@ -1113,10 +1119,9 @@ cudaError_t launch_grad_as(const NormGradArgs &a, bool wide, unsigned grid, unsi
     }
     constexpr size_t BYTES = 16ull * (GRAD_AHEAD<T> * (ADD ? 3 : 2) * (E / VEC<T>) + (VEC<T> == 8 ? E / 4 : 0));     // a thread's
     static_assert(BYTES * THREADS <= (E == 8 ? 112 : 224) * 1024, "a CTA's shared memory");
-    const auto kernel = norm_grad_kernel<T, PACKED, ADD, E>;
-    const cudaError_t err = allow(kernel, BYTES * THREADS);
+    const cudaError_t err = allow<norm_grad_kernel<T, PACKED, ADD, E>>(BYTES * THREADS);
     if (err != cudaSuccess) return err;
-    kernel<<<grid, block, std::max(joined, BYTES * block), s>>>(a);
+    norm_grad_kernel<T, PACKED, ADD, E><<<grid, block, std::max(joined, BYTES * block), s>>>(a);
     return cudaGetLastError();
 }
 template <typename T, bool PACKED, bool ADD>

@@ -30,6 +30,9 @@ class Tensor:
     def numel(self):
         return self.shape.numel()
 
+    def size(self, i):
+        return self.shape[i]
+
     def stride(self):
         return (self.shape[1], 1)
 
