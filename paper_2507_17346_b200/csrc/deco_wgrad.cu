@@ -98,12 +98,14 @@ struct __align__(8) Control {
 };
 
 // A worker's blocks in their order: segments of tiles, in them chunks, in those planes (the smallest first), in those blocks of
-// tokens.  Either function may end the walk by false.
+// tokens.  Every second segment goes from its last tokens to its first, so that it begins with what the last one has just
+// brought into L2.  Either function may end the walk by false.
 template <typename S, typename B>
 __device__ __forceinline__ void walk(const Args &g, uint32_t worker, S segment, B block)
 {
     const uint64_t end = g.begin(worker + 1);
-    for (uint64_t u = g.begin(worker); u < end;) {
+    bool back = false;
+    for (uint64_t u = g.begin(worker); u < end; back = !back) {
         const uint32_t tile = static_cast<uint32_t>(u / g.k_blocks);
         const uint32_t first = static_cast<uint32_t>(u - static_cast<uint64_t>(tile) * g.k_blocks);
         const uint32_t last = static_cast<uint32_t>(min(static_cast<uint64_t>(g.k_blocks), first + (end - u)));
@@ -112,7 +114,7 @@ __device__ __forceinline__ void walk(const Args &g, uint32_t worker, S segment, 
             const uint32_t c1 = min(c0 + g.chunk, last);
             for (uint32_t plane = g.planes; plane-- > 0;)
                 for (uint32_t k = c0; k < c1; ++k)
-                    if (!block(k, plane)) return;
+                    if (!block(back ? first + last - 1 - k : k, plane)) return;
             c0 = c1;
         }
         u += last - first;
