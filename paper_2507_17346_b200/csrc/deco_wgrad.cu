@@ -65,8 +65,8 @@ constexpr int A_STAGES = 4, X_STAGES = 2 * TEAMS;
 // Registers: a launch gives 768 threads 80 each (61440).  256 threads hold 128 sums each, the others need few:
 // 256 * 168 + 384 * 32 + 128 * 48 = 61440.
 constexpr int SUM_REGISTERS = 168, CONVERT_REGISTERS = 32, OTHER_REGISTERS = 48;
-constexpr uint32_t STAGING_COLS = 16, STAGING_FLOATS = 32 * (STAGING_COLS + 1);      // of a warp
-constexpr size_t SMEM = A_STAGES * OPERAND + X_STAGES * (OPERAND + RAW_BYTES) + SUM_WARPS * STAGING_FLOATS * 4 + 1024;
+constexpr uint32_t STAGING_BYTES = 32 * 16 * 4;      // of a warp: 32 rows, 16 columns
+constexpr size_t SMEM = A_STAGES * OPERAND + X_STAGES * (OPERAND + RAW_BYTES) + SUM_WARPS * STAGING_BYTES + 1024;
 constexpr uint32_t CHUNK = 8;            // blocks an accumulator takes before it is emptied
 constexpr uint32_t SMS = 148;
 constexpr uint32_t MIN_BLOCKS = 8;       // a worker's share, if tiles have to be cut for it
@@ -348,7 +348,6 @@ wgrad_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(SUM_REGISTERS));
         const uint32_t quad = wid & 3, side = wid >> 2;          // lanes of the tensor memory, half of the columns
-        float *staging = reinterpret_cast<float *>(raw + (raws - smem_addr(raw)) + X_STAGES * RAW_BYTES) + wid * STAGING_FLOATS;
         float sum[SIDE];                                         // this warp's half of the columns, a row a thread
         uint32_t n = 0;
         bool dead = false;                                       // a wait has run out, NaN from here on
@@ -422,12 +421,31 @@ wgrad_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
             // (Short code: what runs once per segment waits for its instructions longer than for anything else.)
             const bool two = b - a == 1;
             const float *other = slot(worker == a ? b : a);
-            const uint32_t col0 = nt * CG * g.h, o0 = mt * TILE_M + quad * 32, o = o0 + lane;
+            uint32_t thread;                                     // (so that nothing made of it takes a register before)
+            asm volatile("mov.u32 %0, %%tid.x;" : "=r"(thread));
+            const uint32_t l = thread & 31;
+            float4 *const staging = reinterpret_cast<float4 *>(raw + (raws - smem_addr(raw)) + X_STAGES * RAW_BYTES + (thread >> 5) * STAGING_BYTES);
+            const uint32_t col0 = nt * CG * g.h, o0 = mt * TILE_M + quad * 32, o = o0 + l;
 #pragma unroll 1
             for (uint32_t p = 0; out && p < mine; p += 16) {
                 uint32_t v[16];
                 float x[16];
-                const uint32_t n0 = side * SIDE + p;
+                const uint32_t n0 = side * SIDE + p, col = col0 + c.col(n0);
+                // Where this l's sixteen entries go, `valid` of them, `step` apart: with `transposed` one of each of the sixteen
+                // columns, else sixteen rows' of one of them.
+                uint64_t at, step;
+                uint32_t valid = 0;
+                if (g.transposed) {
+                    at = static_cast<uint64_t>(col) * g.out + o;
+                    step = g.out;
+                    if (c.in(n0) && o < g.out) valid = g.cols - min(col, g.cols);
+                } else {
+                    const uint32_t mine_col = col + (l & 15), row = o0 + (l >> 4);
+                    at = static_cast<uint64_t>(row) * g.cols + mine_col;
+                    step = 2ull * g.cols;
+                    if (c.in(n0) && mine_col < g.cols && row < g.out) valid = (g.out - row + 1) / 2;
+                }
+                G *const to = static_cast<G *>(g.dw) + at;
                 if (two) {                                       // (0 + a) + b in whichever order: it is simply added
 #pragma unroll
                     for (int j = 0; j < 16; ++j) x[j] = __ldcg(other + (p + j) * TILE_M);
@@ -465,27 +483,28 @@ wgrad_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
                     continue;
                 }
                 if (!c.in(n0)) continue;
-                const uint32_t col = col0 + c.col(n0);                               // of the sixteen, one behind the other
-                if (g.transposed) {
-                    G *to = static_cast<G *>(g.dw) + static_cast<uint64_t>(col) * g.out + o;
-                    const uint32_t end = o < g.out ? g.cols - min(col, g.cols) : 0;
+                if (!g.transposed) {
+                    // through shared memory, so that neighbouring lanes write neighbouring entries (a row's four units of 16 bytes at
+                    // their numbers exclusive-or half the row's: no bank conflicts on either side)
+                    __syncwarp();
 #pragma unroll
-                    for (uint32_t j = 0; j < 16; ++j, to += g.out)
-                        if (j < end) store_grad<G>(to, 0, x[j], g.accumulate);
-                    continue;
+                    for (uint32_t q = 0; q < 4; ++q)
+                        staging[l * 4 + (q ^ ((l >> 1) & 3))] = make_float4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
+                    __syncwarp();
+                    const float *from = reinterpret_cast<const float *>(staging) + (l >> 4) * 16 + (l & 3);
+#pragma unroll
+                    for (uint32_t q = 0; q < 16; ++q) x[q] = from[q * 32 + (((l >> 2) ^ q) & 3) * 4];
                 }
-                // through shared memory, so that neighbouring lanes write neighbouring entries
-                __syncwarp();
+                if (g.accumulate) {
+                    float old[16];
 #pragma unroll
-                for (uint32_t j = 0; j < 16; ++j) staging[lane * (STAGING_COLS + 1) + j] = x[j];
-                __syncwarp();
-                const uint32_t at = col + (lane & 15), first_row = o0 + (lane >> 4);
-                G *to = static_cast<G *>(g.dw) + static_cast<uint64_t>(first_row) * g.cols + at;
-                const float *from = staging + (lane >> 4) * (STAGING_COLS + 1) + (lane & 15);
-                const uint32_t rows = at < g.cols && first_row < g.out ? (g.out - first_row + 1) / 2 : 0;
-#pragma unroll 4
-                for (uint32_t q = 0; q < 16; ++q, to += 2 * static_cast<uint64_t>(g.cols), from += 2 * (STAGING_COLS + 1))
-                    if (q < rows) store_grad<G>(to, 0, *from, g.accumulate);
+                    for (uint32_t j = 0; j < 16; ++j) old[j] = j < valid ? grad_at<G>(to + j * step) : 0.f;
+#pragma unroll
+                    for (uint32_t j = 0; j < 16; ++j) x[j] = old[j] + x[j];
+                }
+#pragma unroll
+                for (uint32_t j = 0; j < 16; ++j)
+                    if (j < valid) put_grad(to + j * step, x[j]);
             }
             done();
         }
