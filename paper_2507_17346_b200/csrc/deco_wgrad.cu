@@ -83,7 +83,7 @@ struct Args {
     uint32_t grain;                      // ranges are whole numbers of so many blocks: 1, or k_blocks (whole tiles)
     uint64_t grains;
     void *dw, *db;
-    int transposed, accumulate;
+    int transposed, accumulate, wide;    // wide: not transposed, and each row of dw starts on 32 bytes
     float *slots;                        // [worker][2][CG][columns of a tile's product][TILE_M]: parts of tiles
     uint32_t *arrived;                   // [tile][CG][SUM_WARPS]: how many of a tile's parts are there
     // where a worker's range of blocks begins
@@ -153,6 +153,54 @@ template <typename G> __device__ __forceinline__ void store_grad(void *base, uin
 {
     G *p = static_cast<G *>(base) + at;
     put_grad(p, accumulate ? grad_at<G>(p) + v : v);
+}
+
+// Sixteen entries side by side, from 32 bytes' boundary on.
+__device__ __forceinline__ void load_wide(const void *p, uint32_t *w)
+{
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p) : "memory");
+}
+__device__ __forceinline__ void store_wide(void *p, const uint32_t *w)
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 :: "l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+}
+__device__ __forceinline__ void load16(const float *p, float *v)
+{
+    uint32_t w[16];
+    load_wide(p, w);
+    load_wide(p + 8, w + 8);
+#pragma unroll
+    for (int j = 0; j < 16; ++j) v[j] = __uint_as_float(w[j]);
+}
+__device__ __forceinline__ void load16(const __nv_bfloat16 *p, float *v)
+{
+    uint32_t w[8];
+    load_wide(p, w);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        v[2 * j] = __uint_as_float(w[j] << 16);
+        v[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ void store16(float *p, const float *v)
+{
+    uint32_t w[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) w[j] = __float_as_uint(v[j]);
+    store_wide(p, w);
+    store_wide(p + 8, w + 8);
+}
+__device__ __forceinline__ void store16(__nv_bfloat16 *p, const float *v)
+{
+    uint32_t w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const __nv_bfloat162 two = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+        w[j] = *reinterpret_cast<const uint32_t *>(&two);
+    }
+    store_wide(p, w);
 }
 
 // Where the 8 columns from 8 c on of token k lie in an operand's stage.
@@ -431,21 +479,6 @@ wgrad_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
                 uint32_t v[16];
                 float x[16];
                 const uint32_t n0 = side * SIDE + p, col = col0 + c.col(n0);
-                // Where this l's sixteen entries go, `valid` of them, `step` apart: with `transposed` one of each of the sixteen
-                // columns, else sixteen rows' of one of them.
-                uint64_t at, step;
-                uint32_t valid = 0;
-                if (g.transposed) {
-                    at = static_cast<uint64_t>(col) * g.out + o;
-                    step = g.out;
-                    if (c.in(n0) && o < g.out) valid = g.cols - min(col, g.cols);
-                } else {
-                    const uint32_t mine_col = col + (l & 15), row = o0 + (l >> 4);
-                    at = static_cast<uint64_t>(row) * g.cols + mine_col;
-                    step = 2ull * g.cols;
-                    if (c.in(n0) && mine_col < g.cols && row < g.out) valid = (g.out - row + 1) / 2;
-                }
-                G *const to = static_cast<G *>(g.dw) + at;
                 if (two) {                                       // (0 + a) + b in whichever order: it is simply added
 #pragma unroll
                     for (int j = 0; j < 16; ++j) x[j] = __ldcg(other + (p + j) * TILE_M);
@@ -483,9 +516,34 @@ wgrad_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
                     continue;
                 }
                 if (!c.in(n0)) continue;
-                if (!g.transposed) {
+                if (g.wide && col + 16 <= g.cols) {              // a lane writes its row's sixteen entries
+                    G *const to = static_cast<G *>(g.dw) + static_cast<uint64_t>(o) * g.cols + col;
+                    if (o < g.out) {
+                        if (g.accumulate) {
+                            float old[16];
+                            load16(to, old);
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) x[j] = old[j] + x[j];
+                        }
+                        store16(to, x);
+                    }
+                    continue;
+                }
+                // Where this lane's sixteen entries go, `valid` of them, `step` apart: with `transposed` one of each of the sixteen
+                // columns, else sixteen rows' of one of them.
+                uint64_t at, step;
+                uint32_t valid = 0;
+                if (g.transposed) {
+                    at = static_cast<uint64_t>(col) * g.out + o;
+                    step = g.out;
+                    if (o < g.out) valid = g.cols - min(col, g.cols);
+                } else {
+                    const uint32_t mine_col = col + (l & 15), row = o0 + (l >> 4);
+                    at = static_cast<uint64_t>(row) * g.cols + mine_col;
+                    step = 2ull * g.cols;
+                    if (mine_col < g.cols && row < g.out) valid = (g.out - row + 1) / 2;
                     // through shared memory, so that neighbouring lanes write neighbouring entries (a row's four units of 16 bytes at
-                    // their numbers exclusive-or half the row's: no bank conflicts on either side)
+                    // their numbers exclusive-or half the row's)
                     __syncwarp();
 #pragma unroll
                     for (uint32_t q = 0; q < 4; ++q)
@@ -495,6 +553,7 @@ wgrad_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
 #pragma unroll
                     for (uint32_t q = 0; q < 16; ++q) x[q] = from[q * 32 + (((l >> 2) ^ q) & 3) * 4];
                 }
+                G *const to = static_cast<G *>(g.dw) + at;
                 if (g.accumulate) {
                     float old[16];
 #pragma unroll
@@ -789,6 +848,7 @@ extern "C" deco_status deco_weight_grad8(const void *dy, int32_t dtype, uint64_t
     a.db = db;
     a.transposed = transposed != 0;
     a.accumulate = accumulate != 0;
+    a.wide = !transposed && aligned_to(dw, 32) && cols % (32 / gsize) == 0;
     uint8_t *room = static_cast<uint8_t *>(workspace) + p.plane_bytes();
     uint4 *steps = reinterpret_cast<uint4 *>(room);
     a.steps = steps;

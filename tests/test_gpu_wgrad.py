@@ -227,3 +227,17 @@ def test_more_tiles_than_workers_and_parts_of_many(gtype):
         dw, db = torch.empty(out, cols, device="cuda", dtype=DT[gtype]), torch.empty(out, device="cuda", dtype=DT[gtype])
         B.deco_weight_grad8(dy, packed, dw, db=db)
         check(dy, packed, cols, dw, db, False)
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("lead", [16, 4])
+@pytest.mark.parametrize("gtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,out,cols", [(70, 201, 240), (70, 129, 200), (700, 64, 1008), (9000, 700, 608)])
+def test_rows_that_start_on_32_bytes_and_rows_that_do_not(rows, out, cols, gtype, lead, accumulate):
+    """Whole rows of sixteen entries are written at once where they can be; what is around the matrix stays."""
+    flat = torch.full((lead + out * cols + 40,), 0.5, device="cuda", dtype=DT[gtype])
+    dw = flat[lead:lead + out * cols].view(out, cols)
+    packed, dy = checkpoint(rows, cols, 20), gradients(rows, out, "bf16", 21)
+    B.deco_weight_grad8(dy, packed, dw, accumulate=accumulate)
+    check(dy, packed, cols, dw, None, False, old=0.5 if accumulate else 0.0)
+    assert (flat[:lead] == 0.5).all() and (flat[lead + out * cols:] == 0.5).all()
