@@ -474,48 +474,18 @@ wgrad_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
             const uint32_t l = thread & 31;
             float4 *const staging = reinterpret_cast<float4 *>(raw + (raws - smem_addr(raw)) + X_STAGES * RAW_BYTES + (thread >> 5) * STAGING_BYTES);
             const uint32_t col0 = nt * CG * g.h, o0 = mt * TILE_M + quad * 32, o = o0 + l;
-#pragma unroll 1
-            for (uint32_t p = 0; out && p < mine; p += 16) {
-                uint32_t v[16];
-                float x[16];
+            // sixteen columns from the tile's p-th on, this lane's row of them in x
+            auto put = [&](uint32_t p, float (&x)[16]) {
                 const uint32_t n0 = side * SIDE + p, col = col0 + c.col(n0);
-                if (two) {                                       // (0 + a) + b in whichever order: it is simply added
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) x[j] = __ldcg(other + (p + j) * TILE_M);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) x[j] = 0.f;
-                }
-                tmem_load16(acc + p, v);
-                if (whole || two) {
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) x[j] += __uint_as_float(v[j]);
-                } else {
-#pragma unroll 1
-                    for (uint32_t w = a; w <= b; w += 4) {       // (four parts' reads under way together)
-                        float y[4][16];
-#pragma unroll
-                        for (uint32_t k = 0; k < 4; ++k) {
-                            const float *part = slot(w + k) + p * TILE_M;
-#pragma unroll
-                            for (int j = 0; j < 16; ++j)
-                                y[k][j] = w + k == worker ? __uint_as_float(v[j]) : w + k <= b ? __ldcg(part + j * TILE_M) : 0.f;
-                        }
-#pragma unroll
-                        for (uint32_t k = 0; k < 4; ++k)
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) x[j] += y[k][j];
-                    }
-                }
                 if (dead) {
 #pragma unroll
                     for (int j = 0; j < 16; ++j) x[j] = __uint_as_float(0x7FC00000u);
                 }
                 if (c.ones && n0 == c.h) {                                           // (the columns of ones are all alike)
                     if (o < g.out) store_grad<G>(g.db, o, x[0], g.accumulate);
-                    continue;
+                    return;
                 }
-                if (!c.in(n0)) continue;
+                if (!c.in(n0)) return;
                 if (g.wide && col + 16 <= g.cols) {              // a lane writes its row's sixteen entries
                     G *const to = static_cast<G *>(g.dw) + static_cast<uint64_t>(o) * g.cols + col;
                     if (o < g.out) {
@@ -527,7 +497,7 @@ wgrad_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
                         }
                         store16(to, x);
                     }
-                    continue;
+                    return;
                 }
                 // Where this lane's sixteen entries go, `valid` of them, `step` apart: with `transposed` one of each of the sixteen
                 // columns, else sixteen rows' of one of them.
@@ -564,6 +534,54 @@ wgrad_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
 #pragma unroll
                 for (uint32_t j = 0; j < 16; ++j)
                     if (j < valid) put_grad(to + j * step, x[j]);
+            };
+            if (two && out) {                                    // (the other part's a step ahead)
+                float next[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) next[j] = __ldcg(other + j * TILE_M);
+#pragma unroll 1
+                for (uint32_t p = 0; p < mine; p += 16) {
+                    uint32_t v[16];
+                    float x[16];
+                    tmem_load16(acc + p, v);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) x[j] = next[j] + __uint_as_float(v[j]);     // (0 + a) + b in whichever order
+                    if (p + 16 < mine) {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) next[j] = __ldcg(other + (p + 16 + j) * TILE_M);
+                    }
+                    put(p, x);
+                }
+                out = false;
+            }
+#pragma unroll 1
+            for (uint32_t p = 0; out && p < mine; p += 16) {
+                uint32_t v[16];
+                float x[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) x[j] = 0.f;
+                tmem_load16(acc + p, v);
+                if (whole) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) x[j] += __uint_as_float(v[j]);
+                } else {
+#pragma unroll 1
+                    for (uint32_t w = a; w <= b; w += 4) {       // (four parts' reads under way together)
+                        float y[4][16];
+#pragma unroll
+                        for (uint32_t k = 0; k < 4; ++k) {
+                            const float *part = slot(w + k) + p * TILE_M;
+#pragma unroll
+                            for (int j = 0; j < 16; ++j)
+                                y[k][j] = w + k == worker ? __uint_as_float(v[j]) : w + k <= b ? __ldcg(part + j * TILE_M) : 0.f;
+                        }
+#pragma unroll
+                        for (uint32_t k = 0; k < 4; ++k)
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) x[j] += y[k][j];
+                    }
+                }
+                put(p, x);
             }
             done();
         }
