@@ -20,12 +20,14 @@
 // would leave too many idle, a worker begins and ends inside tiles.  Parts of a tile are left in the workspace, and whoever
 // comes last adds them up, in their order whoever it is: the same bits every time.
 //
-// What bounds it (8192 x 5632 x 2048 bf16, 1.09 PFLOP/s; tensor cores busy 71 % of the cycles): shared memory.  64 tokens of a pair's
+// What bounds it (8192 x 5632 x 2048 bf16, 1.13 PFLOP/s; tensor cores busy 70 % of the cycles): shared memory.  64 tokens of a pair's
 // tile take each SM 23 KB of copies in, 8 KB of codes and steps read and 14 KB of bf16 written to convert, and 32 KB read by
 // the tensor cores: 77 KB, 600 cycles at 128 bytes a cycle, where the products take 448 to 512; 640 are measured, 476 without
-// conversion and copies.  In a loop the power cap is next: clocks fall to 1.5 GHz.  Short sums (8192 x 2304 x 768, 45 us): the products
-// of a worker's one part 43 thousand cycles, of which its end is 21 thousand more if it comes last: sums to tensor memory 2.7, the part
-// to memory 3 to 4, the fence 2 to 3, the other part in and the result out 13.
+// conversion and copies.  In a loop the power cap is next: clocks fall to 1.5 GHz.  Short sums (8192 x 2304 x 768, 44 us): the products
+// of a worker's one part 43 thousand cycles, and its end 17 to 21 thousand more if it comes last: sums to tensor memory 2.7, the part
+// to memory 3 to 4, the fence 2 to 3, the other part in and the result out the rest.  Few tokens (64 x 6000 x 6000 bf16, 41 us,
+// 1.8 TB/s written): instructions of the eight warps that write the result, 1000 cycles for sixteen columns.  Leaving out the stores
+// alone saves nothing, shorter code does: 32 bytes a store take 41 us, one entry a store 64.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
