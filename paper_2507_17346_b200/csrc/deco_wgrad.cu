@@ -25,9 +25,9 @@
 // the tensor cores: 77 KB, 600 cycles at 128 bytes a cycle, where the products take 448 to 512; 640 are measured, 476 without
 // conversion and copies.  In a loop the power cap is next: clocks fall to 1.5 GHz.  Short sums (8192 x 2304 x 768, 44 us): the products
 // of a worker's one part 43 thousand cycles, and its end 17 to 21 thousand more if it comes last: sums to tensor memory 2.7, the part
-// to memory 3 to 4, the fence 2 to 3, the other part in and the result out the rest.  Few tokens (64 x 6000 x 6000 bf16, 41 us,
-// 1.8 TB/s written): instructions of the eight warps that write the result, 1000 cycles for sixteen columns.  Leaving out the stores
-// alone saves nothing, shorter code does: 32 bytes a store take 41 us, one entry a store 64.
+// to memory 3 to 4, the fence 2 to 3, the other part in and the result out the rest.  Few tokens (64 x 6000 x 6000 bf16, 33 us,
+// 2.2 TB/s written): instructions of the eight warps that write the result, 1000 cycles for sixteen columns.  Leaving out the stores
+// alone saves nothing, shorter code does: 32 bytes a store took 41 us, one entry a store 64 (by single CTAs).
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -711,9 +711,11 @@ Plan make_plan(const void *dy, int32_t dtype, uint64_t rows, uint32_t out, uint6
     else if (!aligned_to(dy, 16) || stride % 8 || stride >= (1ull << 39)) p.planes = 1;      // (what box copies can address)
     p.pitch = (out + 7) / 8 * 8;
     p.k_blocks = static_cast<uint32_t>((rows + BK - 1) / BK);
-    // Pairs of CTAs read half as much per product; small results are left to single CTAs, whose tiles are a quarter.
+    // Pairs of CTAs read half as much per product, and begin and end half as many tiles; small results are left to single CTAs, whose
+    // tiles are a quarter.  (Single and pairs, us: 64 x 4096 x 3000, 864 tiles of one block, 17 and 20; 64 x 6000 x 6000, 2538,
+    // 38 and 33; 300 x 2500 x 2500 from fp32, 460 of 15, 34 and 26.)
     const uint64_t area = static_cast<uint64_t>((out + TILE_M - 1) / TILE_M) * ((cols + MAX_H - 1) / MAX_H);
-    p.cg = area * p.k_blocks >= 4 * SMS * MIN_BLOCKS ? 2 : 1;
+    p.cg = area * p.k_blocks * std::max<uint32_t>(1, p.planes) >= 4 * SMS * MIN_BLOCKS || area >= 8 * SMS ? 2 : 1;
     const uint32_t most = p.cg * MAX_H, unit = 16 * p.cg;
     p.tiles_n = (cols + most - 1) / most;
     p.h = ((cols + p.tiles_n - 1) / p.tiles_n + unit - 1) / unit * 16;

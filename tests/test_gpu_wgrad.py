@@ -241,3 +241,13 @@ def test_rows_that_start_on_32_bytes_and_rows_that_do_not(rows, out, cols, gtype
     B.deco_weight_grad8(dy, packed, dw, accumulate=accumulate)
     check(dy, packed, cols, dw, None, False, old=0.5 if accumulate else 0.0)
     assert (flat[:lead] == 0.5).all() and (flat[lead + out * cols:] == 0.5).all()
+
+
+@pytest.mark.parametrize("dtype,transposed", [("bf16", False), ("bf16", True), ("f32", False)])
+def test_few_tokens_and_many_tiles(dtype, transposed):
+    """Pairs of CTAs whose tiles are of one block or two of tokens."""
+    for rows, out, cols in ((40, 4300, 4000), (100, 4000, 4241)):
+        packed, dy = checkpoint(rows, cols, 22), gradients(rows, out, dtype, 23)
+        dw, db = torch.empty((cols, out) if transposed else (out, cols), device="cuda"), torch.empty(out, device="cuda")
+        B.deco_weight_grad8(dy, packed, dw, db=db, transposed=transposed)
+        check(dy, packed, cols, dw, db, transposed)
