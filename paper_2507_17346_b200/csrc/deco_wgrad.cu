@@ -12,8 +12,8 @@
 // product, for an eighth of the tensor cores' time in the tiles of the first columns, and no second pass over dY.
 //
 // Sums.  The tensor cores' fp32 sums are cut off, not rounded: over 8192 products the result is 9e-6 off (in the 2-norm), over
-// 512 5e-7.  So, where the result is fp32, the accumulators are emptied every CHUNK blocks of 64 tokens into
-// registers, where sums are rounded; the two accumulators take turns, and the products go on.
+// 512 5e-7, and sums of one sign lose up to 2^-23 for every 16 products.  So the accumulators are emptied every CHUNK (fp32 results)
+// or LONG_CHUNK (bf16) blocks of 64 tokens into registers, where sums are rounded; the two accumulators take turns, and the products go on.
 // lo's and mid's products of a chunk come before hi's, while the sum is still small.
 //
 // Shares.  The blocks of all tiles in a row, cut into equal ranges, one per worker (a CTA or a pair): where whole tiles
@@ -69,7 +69,10 @@ constexpr int A_STAGES = 4, X_STAGES = 2 * TEAMS;
 constexpr int SUM_REGISTERS = 168, CONVERT_REGISTERS = 32, OTHER_REGISTERS = 48;
 constexpr uint32_t STAGING_BYTES = 32 * 16 * 4;      // of a warp: 32 rows, 16 columns
 constexpr size_t SMEM = A_STAGES * OPERAND + X_STAGES * (OPERAND + RAW_BYTES) + SUM_WARPS * STAGING_BYTES + 1024;
-constexpr uint32_t CHUNK = 8;            // blocks an accumulator takes before it is emptied
+// Blocks an accumulator takes before it is emptied; LONG_CHUNK where the result is bf16: 2048 tokens' sums are cut off by at most
+// 2^-16 a plane, far below half a unit of bf16, 2^-9 to 2^-8.  (8192 x 5632 x 2048 bf16 with 8, 16, 32, 64 and all 128 blocks:
+// 172, 168, 166, 165 and 164 us; 0.02, 0.04, 0.08, 0.16 and 0.30 % of the entries are rounded otherwise than the exact sum.)
+constexpr uint32_t CHUNK = 8, LONG_CHUNK = 32;
 constexpr uint32_t SMS = 148;
 constexpr uint32_t MIN_BLOCKS = 8;       // a worker's share, if tiles have to be cut for it
 constexpr uint32_t PART_BLOCKS = 2, CUT_BLOCKS = 8;      // what cutting a tile costs: a part, and at all
@@ -862,7 +865,7 @@ extern "C" deco_status deco_weight_grad8(const void *dy, int32_t dtype, uint64_t
     a.k_blocks = p.k_blocks;
     a.planes = std::max<uint32_t>(1, p.planes);
     a.plane_rows = p.plane_rows;
-    a.chunk = grad_dtype == DECO_F32 ? CHUNK : p.k_blocks;       // (bf16 rounds by 2^-9: sums may be cut off)
+    a.chunk = grad_dtype == DECO_F32 ? CHUNK : LONG_CHUNK;
     a.workers = p.workers;
     a.grain = p.grain;
     a.grains = p.tiles * (p.k_blocks / p.grain);
