@@ -755,7 +755,12 @@ def _workspace(workspace, where, nbytes, device, stream):
     if stream is None:
         room = torch.empty(nbytes, dtype=torch.uint8, device=device)
     else:
-        with torch.cuda.stream(torch.cuda.ExternalStream(_stream(stream), device)):
+        address = _stream(stream)
+        if address == 2:                                                # cudaStreamPerThread: another one in each thread
+            raise ValueError("%s: the per-thread default stream needs a workspace of the caller's" % where)
+        # (0 and 1, cudaStreamLegacy, are the default stream; of address 0 ExternalStream makes one of torch's own pool)
+        on = torch.cuda.default_stream(device) if address in (0, 1) else torch.cuda.ExternalStream(address, device)
+        with torch.cuda.stream(on):
             room = torch.empty(nbytes, dtype=torch.uint8, device=device)
     return room, room.data_ptr(), nbytes
 
