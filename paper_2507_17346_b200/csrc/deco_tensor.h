@@ -6,6 +6,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "deco.h"
 
 namespace deco {
@@ -238,13 +240,20 @@ typedef CUresult (*EncodeFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, voi
                              const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
                              CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-inline EncodeFn encode_function()
+// Looked up until it is found; null, with no error left pending (the next call would take it for its own), where it is not.
+// (Of internal linkage: what an inline function keeps, all libraries of a process would share that are built from this file.)
+static EncodeFn encode_function()
 {
-    void *fn = nullptr;
+    static std::atomic<void *> known{nullptr};
+    void *fn = known.load();
+    if (fn) return reinterpret_cast<EncodeFn>(fn);
     cudaDriverEntryPointQueryResult found;
     if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess ||
-        found != cudaDriverEntryPointSuccess)
+        found != cudaDriverEntryPointSuccess) {
+        cudaGetLastError();
         return nullptr;
+    }
+    known.store(fn);
     return reinterpret_cast<EncodeFn>(fn);
 }
 

@@ -772,7 +772,10 @@ bool allow_shared_memory()
 {
     static std::atomic<uint64_t> done{0};
     int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return false;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) {
+        cudaGetLastError();                                      // (pending, it would be taken for the next call's)
+        return false;
+    }
     if (dev < 64 && (done.load() >> dev & 1)) return true;
     if (!allow<1, float>() || !allow<1, __nv_bfloat16>() || !allow<2, float>() || !allow<2, __nv_bfloat16>()) {
         cudaGetLastError();
@@ -845,7 +848,7 @@ extern "C" deco_status deco_weight_grad8(const void *dy, int32_t dtype, uint64_t
         return DECO_ERR_INVALID_ARG;
     if (!workspace || !aligned_to(workspace, 16)) return DECO_ERR_INVALID_ARG;
     if (workspace_bytes < p.bytes()) return DECO_ERR_CAPACITY;
-    static const EncodeFn encode = encode_function();
+    const EncodeFn encode = encode_function();
     if (!encode || !allow_shared_memory()) return DECO_ERR_CUDA;
     const void *operand = p.planes ? workspace : dy;
     const uint64_t pitch = (cols + BLOCK8 - 1) / BLOCK8 * static_cast<uint64_t>(BLOCK8);
