@@ -64,8 +64,9 @@ class Model:
 
 
 class NormModel(Model):
-    """logits = relu(norm(embed[token]) @ hidden) @ head^T.  Of its activations only checkpoints in 8 bits outlive the forward
-    pass.  The flat vector ends with the norm's weight and bias, which belong to no matrix."""
+    """logits = q(relu(norm(embed[token]) @ hidden)) @ head^T, where q puts away in 8 bits and takes back: the head is given what the
+    backward pass will have, so that both agree on the units that are 0.  Of its activations only checkpoints in 8 bits outlive the
+    forward pass.  The flat vector ends with the norm's weight and bias, which belong to no matrix."""
 
     def __init__(self, vocab, width, hidden, seed=0, device="cuda"):
         super().__init__(vocab, width, hidden, seed, device)
@@ -80,7 +81,7 @@ class NormModel(Model):
         return flat[self.at:self.at + self.width], flat[self.at + self.width:]
 
     def forward(self, tokens):
-        """-> (hidden activations, logits, what the backward pass needs)."""
+        """-> (hidden activations as the checkpoint has them, logits, what the backward pass needs)."""
         embed, hidden, head = self.views(self.params)
         weight, bias = self.norm_views(self.params)
         x = embed[tokens]
@@ -91,6 +92,7 @@ class NormModel(Model):
         B.deco_pack8(y, y8)
         h = torch.relu(y @ hidden)
         B.deco_pack8(h, h8)
+        B.deco_unpack8(h8, h)
         return h, h @ head.t(), (x8, mean, rstd, y8, h8)
 
     def logits(self, tokens):
@@ -99,16 +101,17 @@ class NormModel(Model):
 
     def gradient(self, tokens, targets, out):
         rows = len(tokens)
-        h, logits, (x8, mean, rstd, y8, h8) = self.forward(tokens)
-        logprob, lse = torch.empty(rows, device=h.device), torch.empty(rows, device=h.device)
+        logits, (x8, mean, rstd, y8, h8) = self.forward(tokens)[1:]
+        logprob, lse = torch.empty(rows, device=logits.device), torch.empty(rows, device=logits.device)
         B.deco_token_logprobs(logits, targets, logprob, lse=lse)
-        scale = torch.full((rows,), -1.0 / rows, device=h.device)
+        scale = torch.full((rows,), -1.0 / rows, device=logits.device)
         B.deco_token_logprobs_grad(logits, targets, lse, logits, g_logprob=scale)       # in place
         _, hidden, head = self.views(self.params)
         weight, _ = self.norm_views(self.params)
         d_embed, d_hidden, d_head = self.views(out)
         d_weight, d_bias = self.norm_views(out)
         B.deco_weight_grad8(logits, h8, d_head)
+        h = torch.empty(rows, hidden.shape[1], device=logits.device)
         B.deco_unpack8(h8, h)                                    # (where it is 0 the unit passes nothing on)
         dh = (logits @ head) * (h > 0)
         B.deco_weight_grad8(dh, y8, d_hidden, transposed=True)
