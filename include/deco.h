@@ -631,8 +631,8 @@ deco_status deco_orth_get_stats(deco_orth *h, void *stream, deco_orth_stats *out
  *   weight, bias   [cols] fp32; NULL: 1 and 0
  *   mean, rstd     [rows] fp32, what the gradient needs; may be NULL
  *   codes, exponents   NULL, or the checkpoint of u
- * 0 < eps < inf.  y, and sum, may be x's or add's own buffer (same stride), not each other's.  A row with a NaN or an infinity
- * gives NaN; entries beyond 2^60 in magnitude may overflow the variance, which gives 0 or NaN.
+ * 0 < eps < inf.  y, and sum, may be x's or add's own buffer (of more than one row: same stride), not each other's.  A row with a NaN or
+ * an infinity gives NaN; entries beyond 2^60 in magnitude may overflow the variance, which gives 0 or NaN.
  */
 deco_status deco_layernorm(const void *x, int32_t dtype, uint64_t rows, uint32_t cols, uint64_t x_stride,
                            const void *add, uint64_t add_stride, void *sum, uint64_t sum_stride,
@@ -645,7 +645,7 @@ deco_status deco_layernorm(const void *x, int32_t dtype, uint64_t rows, uint32_t
  *   dweight = sum over rows of dy h,   dbias = sum over rows of dy
  *   x          rows of dtype (what was normalised: sum where there was one); or NULL, and codes and exponents its checkpoint
  *   add        NULL, or rows of dtype: the gradient that reaches x beside the norm
- *   dx         may be x's, dy's or add's own buffer (same stride)
+ *   dx         may be x's, dy's or add's own buffer (of more than one row: same stride)
  *   dweight, dbias   [cols] of grad_dtype, overwritten, or added to if `accumulate`; either may be NULL
  *   workspace  at least deco_layernorm_grad_workspace(rows, cols) bytes, 16-byte aligned, whose contents do not matter
  *              (may be NULL if dweight and dbias are, and cols <= 8192); fewer: DECO_ERR_CAPACITY

@@ -1031,7 +1031,8 @@ bool wide_rows(std::initializer_list<Rows> all, int32_t dtype, uint32_t cols)
     return true;
 }
 bool bad_packed(const int8_t *codes, const uint8_t *exps) { return !codes || !exps || !aligned_to(codes, 16); }
-bool same_start(const Rows &a, const Rows &b) { return a.p && a.p == b.p && a.stride != b.stride; }
+// Rows of one buffer that do not lie over one another.  (One row has no distance to the next.)
+bool askew(const Rows &a, const Rows &b, uint64_t rows) { return rows > 1 && a.p && a.p == b.p && a.stride != b.stride; }
 
 deco_status result() { return cudaGetLastError() == cudaSuccess ? DECO_OK : DECO_ERR_CUDA; }
 
@@ -1230,7 +1231,7 @@ extern "C" deco_status deco_layernorm(const void *x, int32_t dtype, uint64_t row
     if (!x || !y || (sum && !add) || sum == y) return DECO_ERR_INVALID_ARG;
     if (bad_rows(rx, dtype, cols) || bad_rows(ra, dtype, cols) || bad_rows(rs, dtype, cols) || bad_rows(ry, dtype, cols))
         return DECO_ERR_INVALID_ARG;
-    if (same_start(ry, rx) || same_start(ry, ra) || same_start(rs, rx) || same_start(rs, ra)) return DECO_ERR_INVALID_ARG;
+    if (askew(ry, rx, rows) || askew(ry, ra, rows) || askew(rs, rx, rows) || askew(rs, ra, rows)) return DECO_ERR_INVALID_ARG;
     for (const float *p : {weight, bias, static_cast<const float *>(mean), static_cast<const float *>(rstd)})
         if (!aligned_to(p, 4)) return DECO_ERR_INVALID_ARG;
     if ((codes || exponents) && bad_packed(codes, exponents)) return DECO_ERR_INVALID_ARG;
@@ -1290,7 +1291,7 @@ extern "C" deco_status deco_layernorm_grad(const void *x, int32_t dtype, uint64_
     if (!dy || !dx || !mean || !rstd || !x == !codes) return DECO_ERR_INVALID_ARG;
     if (bad_rows(rx, dtype, cols) || bad_rows(rg, dtype, cols) || bad_rows(ra, dtype, cols) || bad_rows(rd, dtype, cols))
         return DECO_ERR_INVALID_ARG;
-    if (same_start(rd, rx) || same_start(rd, rg) || same_start(rd, ra)) return DECO_ERR_INVALID_ARG;
+    if (askew(rd, rx, rows) || askew(rd, rg, rows) || askew(rd, ra, rows)) return DECO_ERR_INVALID_ARG;
     for (const float *p : {mean, rstd, weight})
         if (!aligned_to(p, 4)) return DECO_ERR_INVALID_ARG;
     if ((codes || exponents) && bad_packed(codes, exponents)) return DECO_ERR_INVALID_ARG;
