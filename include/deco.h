@@ -674,7 +674,8 @@ deco_status deco_unpack8(const int8_t *codes, const uint8_t *exponents, uint64_t
  *              the flat gradient vector.  Overwritten, or added to if `accumulate`; db may be NULL
  *   workspace  at least deco_weight_grad8_workspace(...) bytes for the same dy (whose alignment matters), dtype, rows, out, dy_stride,
  *              cols and grad_dtype; 16-byte aligned, its contents do not matter; fewer: DECO_ERR_CAPACITY
- * Products are exact: X's values are bf16 numbers, fp32 dy is taken as a sum of three (two where grad_dtype is bf16).  Sums are fp32,
+ * X's values are bf16 numbers, and products with bf16 dy exact.  fp32 dy is taken as a sum of three bf16 numbers, which is exact down to
+ * 2^-110 in magnitude (parts below 2^-133 are lost); where grad_dtype is bf16 of two, which leaves out up to 2^-17 of an entry.  Sums are fp32,
  * on the tensor cores over at most 512 tokens at a time (2048 where grad_dtype is bf16).  out, cols <= 2^24.  rows = 0 gives sums of 0.
  * Should one of the kernel's bounded waits run out, the sums concerned come out as NaN.
  */

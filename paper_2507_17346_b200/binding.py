@@ -803,7 +803,7 @@ def deco_layernorm_grad(x, mean, rstd, weight, dy, dx, dweight=None, dbias=None,
     """Gradient of deco_layernorm: `dx` ([rows, cols], the type of `dy`), and if given `dweight` and `dbias` ([cols], f32 or
     bf16; added to with `accumulate`).  `x`: what was normalised, or its checkpoint (codes, exponents).  `add`: the
     gradient that reaches x beside the norm.  `workspace`: uint8 tensor of deco_layernorm_grad_workspace bytes; by
-    default the call makes one."""
+    default the call makes one, of its stream."""
     w = "deco_layernorm_grad"
     p, kind, rows, cols, stride, dev = _rows_of(dy, w, "dy")
     codes = exps = None
@@ -852,7 +852,8 @@ def deco_weight_grad8(dy, packed, dw, db=None, transposed=False, accumulate=Fals
     """Weight gradient of a linear layer whose input was kept in 8 bits: `dy` [tokens, out] (f32 or bf16), `packed` = (codes,
     exponents) of the input [tokens, cols], `dw` [out, cols] ([cols, out] with `transposed`) and if given `db` [out], of one
     type (f32 or bf16), views of the flat gradient vector perhaps; added to with `accumulate`.  `workspace`: uint8
-    tensor of deco_weight_grad8_workspace bytes; by default the call makes one."""
+    tensor of deco_weight_grad8_workspace bytes; by default the call makes one, of its stream.  f32 `dy` is taken to 16 bits
+    where the gradients are bf16, to all 24 where they are f32."""
     w = "deco_weight_grad8"
     p, kind, rows, out, stride, dev = _rows_of(dy, w, "dy")
     if dw.dim() != 2 or dw.shape[1 if transposed else 0] != out:

@@ -10,8 +10,8 @@
 //
 // Measured at 32768 x 2048 (of the copy rate, 6.54 TB/s): norm of bf16 rows 65 us (63 %), with residual 102 (80 %), with residual and
 // checkpoint 109 (85 %), of fp32 rows 93 (88 %); gradient of bf16 rows 76 us (81 %), with residual 89 (92 %), from the checkpoint with
-// residual 96 (75 %), of fp32 rows 132 (93 %); packing bf16 39 us (79 %), fp32 54 (96 %), taking back bf16 35 (89 %).  What is not
-// memory there is instruction issue (60 to 70 % of the slots).  Rows that do not start on 16 bytes, 65536 x 1001 bf16: norm 105 us (38 %),
+// residual 96 (75 %), of fp32 rows 132 (93 %); packing bf16 39 us (79 %), fp32 54 (96 %), taking back bf16 35 (89 %).  Where it is
+// not memory, no limit is reached: issue slots are 60 to 70 % busy, a quarter of the warps there.  Rows that do not start on 16 bytes, 65536 x 1001 bf16: norm 105 us (38 %),
 // gradient 125 (48 %), packing 126 (24 %): an instruction an entry for each access, and for a code and its block's maximum.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -611,7 +611,8 @@ norm_any_kernel(const NormArgs a)
 }
 
 // Rows of more columns than that: one CTA a row, which reads it once for its sum, once for its
-// deviations and once for the output (the second and third time from the caches).
+// deviations and once for the output (the second and third time from the caches), an entry an access.  (8192 x 12288 bf16: 430 us,
+// 0.94 TB/s; 4096 x 16384: 264.)
 template <typename T>
 __global__ void __launch_bounds__(1024)
 norm_wide_kernel(const NormArgs a)
@@ -922,7 +923,8 @@ norm_grad_any_kernel(const NormGradArgs a)
     put_part<1, E>(a, c, own, t, threads, group, groups, joined);
 }
 
-// Rows of more columns than a CTA's threads can hold, in two launches.  First c = (mean g, mean(g xhat)) of each row ...
+// Rows of more columns than a CTA's threads can hold, in two launches, x and dy read twice.  (8192 x 12288 bf16: 362 us, 1.67 TB/s;
+// 4096 x 16384: 244.)  First c = (mean g, mean(g xhat)) of each row ...
 template <typename T, bool PACKED>
 __global__ void __launch_bounds__(1024)
 norm_grad_rows_kernel(const NormGradArgs a)
@@ -1040,7 +1042,8 @@ deco_status result() { return cudaGetLastError() == cudaSuccess ? DECO_OK : DECO
 // threads an SM) or more (one).  A warp spends about 100 instructions on a row whatever its share is, which 16-bit rows cannot
 // afford for 8 entries (32768 x 2048 bf16, gradient with residual: 111 us with 8, 91 with 16; fp32: 134 and 141); a
 // row of one warp needs no barrier (65536 x 768 bf16 forward: 57 us with 16, 39 with 24; the gradient has no registers for
-// 24, and of 8192 rows 8 entries, three warps, make 22 us, 16 and two 25).  As many groups as 512 threads make, but few rows are spread over the device.
+// 24, and of 8192 rows 8 entries, three warps, make 22 us, 16 and two 25; more rows of 513 to 768 columns were not
+// measured).  As many groups as 512 threads make, but few rows are spread over the device.
 struct Spread {
     uint32_t entries, warps, groups, ctas;
 };

@@ -5,7 +5,8 @@
 // (five instructions for two) and put them in the place of the operand, while dY comes as it is.  Both operands have
 // their outer dimension consecutive, 128-byte swizzle.
 //
-// fp32 dY is taken as the sum of bf16 numbers, hi + mid + lo (24 bits; hi + mid where the result is bf16), split by a
+// fp32 dY is taken as the sum of bf16 numbers, hi + mid + lo (24 bits).  Where the result is bf16 hi + mid do: they leave out up
+// to 2^-17 of a term, 2^-8 of what the result's own rounding may take, and save a third of the products.  They are split by a
 // launch before; the same launch lays out bf16 rows that do not start on 16 bytes.
 //
 // db.  Sixteen columns of ones behind a CTA's columns of X in shared memory make it one more column of the
@@ -20,7 +21,7 @@
 // would leave too many idle, a worker begins and ends inside tiles.  Parts of a tile are left in the workspace, and whoever
 // comes last adds them up, in their order whoever it is: the same bits every time.
 //
-// What bounds it (8192 x 5632 x 2048 bf16, 1.13 PFLOP/s; tensor cores busy 70 % of the cycles): shared memory.  64 tokens of a pair's
+// What bounds it (8192 x 5632 x 2048 bf16, 166 us, 1.14 PFLOP/s; tensor cores busy 70 % of the cycles): shared memory.  64 tokens of a pair's
 // tile take each SM 23 KB of copies in, 8 KB of codes and steps read and 14 KB of bf16 written to convert, and 32 KB read by
 // the tensor cores: 77 KB, 600 cycles at 128 bytes a cycle, where the products take 448 to 512; 640 are measured, 476 without
 // conversion and copies.  In a loop the power cap is next: clocks fall to 1.5 GHz.  Short sums (8192 x 2304 x 768, 44 us): the products
@@ -716,7 +717,8 @@ Plan make_plan(const void *dy, int32_t dtype, uint64_t rows, uint32_t out, uint6
     p.k_blocks = static_cast<uint32_t>((rows + BK - 1) / BK);
     // Pairs of CTAs read half as much per product, and begin and end half as many tiles; small results are left to single CTAs, whose
     // tiles are a quarter.  (Single and pairs, us: 64 x 4096 x 3000, 864 tiles of one block, 17 and 20; 64 x 6000 x 6000, 2538,
-    // 38 and 33; 300 x 2500 x 2500 from fp32, 460 of 15, 34 and 26.)
+    // 38 and 33; 300 x 2500 x 2500 from fp32, 460 of 15, 34 and 26.  4000 x 777 x 600 from fp32, 42 of 189, goes by pairs too and
+// loses by it: 42 and 47.)
     const uint64_t area = static_cast<uint64_t>((out + TILE_M - 1) / TILE_M) * ((cols + MAX_H - 1) / MAX_H);
     p.cg = area * p.k_blocks * std::max<uint32_t>(1, p.planes) >= 4 * SMS * MIN_BLOCKS || area >= 8 * SMS ? 2 : 1;
     const uint32_t most = p.cg * MAX_H, unit = 16 * p.cg;
